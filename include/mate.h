@@ -268,6 +268,137 @@ int mate_attn_bwd_noalloc(const mate_plan_t *plan, const void *Q, const void *K,
                           const void *O, const float *LSE, const void *dO, int d, int dtype,
                           float scale, void *dQ, void *dK, void *dV, void *stream);
 
+/* ------------------------------------------------------------------------------------------------
+ * Rotary positions.
+ *
+ * The first `rot` elements of every head are taken as pairs and each pair (a, b) is turned by the
+ * angle t = position * freqs[pair] and scaled by mscale:
+ *     forward                 a' = mscale (a cos t - b sin t),   b' = mscale (a sin t + b cos t)
+ *     MATE_ROPE_BACKWARD      the transpose (t -> -t): gradients of the inputs from those of the outputs
+ * Elements rot .. d-1 are passed on.  Pair i is (i, i + rot / 2), with MATE_ROPE_INTERLEAVED (2 i, 2 i + 1).
+ *
+ *   tensors    n_tensors (1 or 2: queries and keys, whose numbers of heads may differ) views of B x
+ *              heads x N rows of d contiguous elements of type dtype; x is read, y is written, by strides in
+ *              elements (batch, head, token) of their own.  y == x with equal strides works in place;
+ *              otherwise they must not overlap.  Any alignment that fits the type (16 bytes and sizes that
+ *              are multiples of it are faster).
+ *   positions  device int32, position of token n of example b at positions[b * position_stride + n] (stride 0: one
+ *              row for all examples).  Any value: the angle is formed in 64 bits.  For a table whose positions start
+ *              again in every cell the caller says so here.
+ *   freqs      device float64 [rot / 2], radians per position (scaled for long contexts as the caller likes)
+ * rot is even, 0 <= rot <= d <= 1024.  For packed batches B = 1 and N = T.  Asynchronous on `stream`; no
+ * workspace.  Bound by memory: every element is read once and written once. */
+typedef struct {
+    const void *x;
+    void *y;
+    int64_t x_stride[3], y_stride[3]; /* batch, head, token */
+    int32_t heads;
+} mate_rope_tensor_t;
+
+enum { MATE_ROPE_INTERLEAVED = 1, MATE_ROPE_BACKWARD = 2 };
+
+int mate_rope(const mate_rope_tensor_t *tensors, int n_tensors, int B, int N, int d, int dtype, const int32_t *positions,
+              int64_t position_stride, const double *freqs, int rot, float mscale, unsigned flags, void *stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * One new token at a time: a paged cache of keys and values, and the row of the pattern that belongs to
+ * the newest token of every sequence.
+ *
+ * The cache is the caller's memory, described by this struct, which the calls read while they run on the host and do not
+ * keep.  A sequence is a row of `table`: its tokens 0 .. lens[s] - 1 stand in the slots of the pages table[s][0],
+ * table[s][1], ..., page_size to a page.  Every cached token has its row id and its column id (as given to mate_plan:
+ * a negative id marks padding, which is never attended, whatever its key and value hold); the first prefix[s] tokens are the
+ * prefix.  MATE_ID_TEXT as both ids marks a token that belongs to the text wherever it stands (an answer
+ * written behind the table): it attends, and is attended by, every token.
+ *
+ * A page may be shared by several sequences; refs[page] counts them, 0 = free.  lens, table, refs and prefix are device
+ * memory that only the calls below (and the caller, between them) change; every call is asynchronous on its stream
+ * and can be captured into a graph.  Calls on one cache must be ordered (one stream, or events).
+ *
+ * What the kernels find on the device and cannot do -- a sequence, length or page out of range, a sequence twice
+ * in a list, no free page left -- they leave out, and say so in status[0], which mate_cache_status reads.  No
+ * such content makes a kernel read or write outside of the arrays. */
+#define MATE_ID_TEXT 0x7fffffff
+enum { MATE_VIEW_EITHER = 2 }; /* entry of mate_cache_t.head_view: the same row OR the same column (mate_plan_sat) */
+
+typedef struct {
+    void *k, *v;                 /* [layers, pages, kv_heads, page_size, d] by the strides below; 16-byte aligned  */
+    int32_t *row_ids, *col_ids;  /* [pages, page_size], shared by all layers                                       */
+    int32_t *table;              /* [seqs, width]                                                                   */
+    int32_t *lens;               /* [seqs]                                                                          */
+    int32_t *prefix;             /* [seqs]                                                                          */
+    int32_t *refs;               /* [pages]                                                                         */
+    int32_t *status;             /* [1], zero at the start                                                          */
+    const uint8_t *head_view;    /* HOST [heads], MATE_VIEW_*; query head h uses kv head h / (heads / kv_heads)    */
+    int64_t layer_stride, page_stride, head_stride, slot_stride; /* elements, multiples of 16 bytes, of k and v     */
+    int32_t layers, pages, page_size, seqs, width, heads, kv_heads, d, dtype, device;
+} mate_cache_t;
+
+/* Makes room: for every i, sequence seqs[i] (null: i) grows by counts[i] >= 0 tokens; lens[s] += counts[i], and the
+ * pages that it needs beyond those it has are the lowest free ones, dealt out in the order of the list.
+ * granted[i] = counts[i]; 0, and the sequence as it was, where there is no room: the table's row is too short,
+ * or no page is free (then nobody behind it in the list who needs pages gets any either).  The second and further
+ * entries with the same sequence get nothing.  seqs, counts, granted: device int32 [n], n <= 4096. */
+int mate_cache_extend(const mate_cache_t *cache, const int32_t *seqs, const int32_t *counts, int n, int32_t *granted, void *stream);
+
+/* Writes the last counts[i] (null: N) tokens of sequence seqs[i] (null: i) into one layer of the cache: token j < counts[i]
+ * of entry i goes to position lens[s] - counts[i] + j.  To be called behind mate_cache_extend, with what it granted.
+ * A sequence stands at most once in the list (of two entries with the same one either may be what stays).
+ *   K, V       new rows, [B, kv_heads, N, d] by strides (batch, head, token)
+ *   Q, Q_out   queries of the new tokens, [B, heads, N, d] by strides, and where they go rotated; null: none.  All B N
+ *              tokens are rotated, whatever counts says
+ *   row_ids, col_ids   device int32 [B, N], or both null (the ids in the cache stay: further layers)
+ *   freqs      as in mate_rope, applied to K (and Q); null: neither is rotated (and Q must be null)
+ *   positions  device int32 [B, N]; null: the tokens' positions in their sequences
+ * A page that several sequences share must not be written: mate_cache_fork sees to that. */
+int mate_cache_append(const mate_cache_t *cache, int layer, const void *K, const void *V, const int64_t *k_stride,
+                      const int64_t *v_stride, int B, int N, const int32_t *seqs, const int32_t *counts, const int32_t *row_ids,
+                      const int32_t *col_ids, const int32_t *positions, const double *freqs, int rot, float mscale, unsigned flags,
+                      const void *Q, const int64_t *q_stride, void *Q_out, const int64_t *q_out_stride, void *stream);
+
+/* For every i: sequence children[i], which must be empty, becomes a copy of parents[i].  Full pages are shared; a
+ * last page that is filled in part is copied, in all layers, to the lowest free page (in the order of the list).  lens and
+ * prefix are copied.  All parents are read as they are before the call.  A child that is not empty, or that
+ * stands in the list for the second time, is left as it is; one for whose copy no page is free stays empty.
+ * parents, children: device int32 [n], n <= 4096.  workspace: device, mate_cache_workspace_bytes. */
+int mate_cache_fork(const mate_cache_t *cache, const int32_t *parents, const int32_t *children, int n, void *workspace,
+                    size_t workspace_bytes, void *stream);
+
+/* Every sequence of the list (null: 0 .. n - 1) becomes empty: its pages lose a reference, its row of the table becomes -1, its length 0.
+ * Sequences that are empty already are no error, so one may stand in the list twice. */
+int mate_cache_free(const mate_cache_t *cache, const int32_t *seqs, int n, void *stream);
+
+/* Moves the pages in use to the front: afterwards pages 0 .. n_live - 1 are in use and all others free.  The pages
+ * in use at n_live and above go, in order, to the free ones below; all layers, ids, refs and the table follow.
+ * n_live: device int32 [1].  workspace: device, mate_cache_workspace_bytes. */
+int mate_cache_compact(const mate_cache_t *cache, int32_t *n_live, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Scratch of mate_cache_fork with n entries, of mate_cache_compact, and of mate_attn_decode with n tokens (any may be null). */
+int mate_cache_workspace_bytes(const mate_cache_t *cache, int n, size_t *fork_bytes, size_t *compact_bytes, size_t *decode_bytes);
+
+/* Waits for `stream`, clears status[0] and returns MATE_ERR_NOMEM if pages ran out since the last call, MATE_ERR_INVALID_ARG if
+ * something was out of range or not as it must be, else MATE_OK. */
+int mate_cache_status(const mate_cache_t *cache, void *stream);
+
+/* The forward's row of one token per sequence: for entry i and head h, with s = seqs[i] (null: i),
+ *     O = sum_j softmax_j(scale q.k_j) v_j  over the tokens j < lens[s] that are not padding and that
+ *     belong to the prefix or the text, or share the new token's row (row heads) / column (column heads) / either of them;
+ *     a new token of the text attends them all.
+ * The new token's own key and value are attended like every other, if they have been appended.
+ *   Q          [B, heads, d] by strides (batch, head), of the cache's type, 16-byte aligned rows
+ *   row_ids, col_ids   device int32 [B], the new token's ids (MATE_ID_TEXT: text; negative: padding, O = 0 and LSE = -inf, as
+ *              for a sequence without a token that may be attended)
+ *   scale      any finite value
+ *   max_len    an upper bound of the sequences' lengths that the caller knows (0: what the table can hold); tokens at
+ *              and beyond it do not count, and status says so
+ *   O, LSE     [B, heads, d] of the cache's type, float32 [B, heads]; fully overwritten
+ *   workspace  device, 256-byte aligned, mate_cache_workspace_bytes; contents undefined afterwards; calls that overlap need one each
+ * Scores, softmax and sums in fp32; with bf16 the weights are rounded to bf16 ahead of the product with V, as in
+ * mate_attn_fwd.  Asynchronous on `stream`. */
+int mate_attn_decode(const mate_cache_t *cache, int layer, const void *Q, const int64_t *q_stride, int B, const int32_t *seqs,
+                     const int32_t *row_ids, const int32_t *col_ids, float scale, int max_len, void *O, float *LSE, void *workspace,
+                     size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -11,7 +11,8 @@ _LIB_PATH = os.path.join(_PKG, "libmate.so")
 
 IMPL_AUTO, IMPL_SIMT, IMPL_TCGEN05 = 0, 1, 2
 FLAG_VIEW_ORDER, FLAG_BULK_TILES, FLAG_GATHER_TILES = 4, 8, 16   # or-ed to the implementation choice (see mate.h)
-VIEW_ROW, VIEW_COL = 0, 1
+VIEW_ROW, VIEW_COL, VIEW_EITHER = 0, 1, 2   # (either: of a Cache only)
+ID_TEXT = 0x7FFFFFFF   # ids of a cached or new token that belongs to the text, wherever it stands (see mate.h)
 _BF16, _F32 = 0, 1
 
 _lib = None
@@ -81,6 +82,9 @@ def _load():
         raise ImportError("the native binding is not built: run `python -m paper_2109_04312_b200.build`") from e
     _native.bind(*(C.cast(f, C.c_void_p).value for f in (lib.mate_attn_workspace_bytes, lib.mate_attn_fwd,
                                                          lib.mate_attn_bwd, lib.mate_cell_mean)), MateError)
+    cache_calls = (lib.mate_rope, lib.mate_cache_extend, lib.mate_cache_append, lib.mate_cache_fork, lib.mate_cache_free,
+                   lib.mate_cache_compact, lib.mate_cache_workspace_bytes, lib.mate_cache_status, lib.mate_attn_decode)
+    _native.bind_cache(*(C.cast(f, C.c_void_p).value for f in cache_calls))
     _lib = lib
     return lib
 
@@ -330,3 +334,95 @@ def mate_attn_bwd_noalloc(plan, Q, K, V, O, LSE, dO, dQ, dK, dV, scale=None):
                                              _dev(dK, "dK"), _dev(dV, "dV"), _stream()),
                "mate_attn_bwd_noalloc")
     return dQ, dK, dV
+
+
+def mate_rope_freqs(rot, base=10000.0, factor=1.0, original_len=None, low=1.0, high=4.0, device="cuda"):
+    """Radians per position of the rot / 2 pairs, base ** (-2 i / rot), as a float64 tensor.  factor stretches them for contexts
+    `factor` times as long: all of them, or, where original_len is given, by how often a pair turns within it -- those with at least
+    `high` turns are kept, those with at most `low` are stretched, between them the two are mixed."""
+    if rot < 0 or rot % 2 or not factor > 0 or not high > low:
+        raise ValueError("rot must be even, factor positive, high larger than low")
+    f = base ** (-np.arange(0, rot, 2, dtype=np.float64) / max(rot, 1))
+    keep = 0.0 if original_len is None else np.clip((original_len * f / (2 * np.pi) - low) / (high - low), 0.0, 1.0)
+    return torch.from_numpy(f * keep + f / factor * (1 - keep)).to(device)
+
+
+def mate_rope(Q, positions, freqs, K=None, interleaved=False, mscale=1.0, backward=False, out=None):
+    """Rotary positions (see mate_rope in mate.h).  Q, and K with heads of its own: [B, H, N, d] (or [H, T, d]) CUDA tensors, bf16 or
+    f32, of any strides with contiguous rows, for example views of a fused projection's output.  positions: int32 [B, N], or [N] for
+    all examples; freqs: float64 [rot / 2] (mate_rope_freqs).  backward: gradients of the inputs from those of the outputs.
+    out: where the result goes (a pair with K), any strides, the inputs themselves included; else new contiguous
+    tensors.  Returns Q' or (Q', K')."""
+    _load()
+    from . import _native
+    q, k = (out, None) if K is None else (None, None) if out is None else out
+    return _native.rope(Q, K, positions, freqs, interleaved, mscale, backward, q, k)
+
+
+class Cache:
+    """A paged cache of keys and values (see mate_cache_t in mate.h): the caller's tensors, which the calls read and write.
+
+    k, v: [layers, pages, kv_heads, page_size, d] bf16 or f32 (a cache laid out slot by slot is passed as a transposed view);
+    row_ids, col_ids: int32 [pages, page_size]; table: int32 [seqs, width]; lens, prefix: int32 [seqs]; refs: int32 [pages];
+    head_view: VIEW_ROW, VIEW_COL or VIEW_EITHER for every query head."""
+
+    def __init__(self, k, v, row_ids, col_ids, table, lens, prefix, refs, head_view):
+        _load()
+        from . import _native
+        self.k, self.v, self.row_ids, self.col_ids = k, v, row_ids, col_ids
+        self.table, self.lens, self.prefix, self.refs = table, lens, prefix, refs
+        self.head_view = np.ascontiguousarray(np.asarray(head_view, dtype=np.uint8))
+        self.status_word = torch.zeros(1, dtype=torch.int32, device=k.device)
+        self._native = _native
+        self._info = _native.cache_info(k, v, row_ids, col_ids, table, lens, prefix, refs, self.status_word, self.head_view.tobytes())
+
+    @classmethod
+    def empty(cls, pages, page_size, kv_heads, d, seqs, width, head_view, layers=1, dtype=torch.bfloat16, device="cuda"):
+        """A cache without a token: `pages` pages of `page_size` slots, up to `seqs` sequences of up to `width` pages."""
+        def ints(*shape, value=0):
+            return torch.full(shape, value, dtype=torch.int32, device=device)
+        k, v = (torch.zeros((layers, pages, kv_heads, page_size, d), dtype=dtype, device=device) for _ in range(2))
+        return cls(k, v, ints(pages, page_size), ints(pages, page_size), ints(seqs, width, value=-1), ints(seqs), ints(seqs), ints(pages),
+                   head_view)
+
+    def status(self):
+        """Waits, and raises MateError if a call found something out of range, or no free page, since the last time."""
+        self._native.cache_status(self._info)
+
+
+def mate_cache_extend(cache, seqs, counts, granted=None):
+    """Room for counts[i] more tokens of sequence seqs[i] (None: i): pages are handed out and lens grow (see
+    mate_cache_extend in mate.h).  int32 CUDA tensors [n].  Returns granted: counts[i], or 0 where there was no room."""
+    return cache._native.cache_extend(cache._info, seqs, counts, granted)
+
+
+def mate_cache_append(cache, K, V, seqs=None, counts=None, row_ids=None, col_ids=None, layer=0, freqs=None, positions=None,
+                      interleaved=False, mscale=1.0, Q=None, out=None):
+    """The last counts[i] (None: N) tokens of sequence seqs[i] (None: i) into one layer of the cache (see mate_cache_append in mate.h).
+    K, V: [B, kv_heads, N, d] with contiguous rows; row_ids, col_ids: int32 [B, N], None for further layers.  With freqs
+    K is rotated on the way, and Q [B, heads, N, d] too, which is returned."""
+    return cache._native.cache_append(cache._info, layer, K, V, seqs, counts, row_ids, col_ids, positions, freqs, interleaved, mscale, Q,
+                                      out)
+
+
+def mate_cache_fork(cache, parents, children):
+    """children[i], which must be empty, becomes a copy of parents[i]: full pages are shared, a last one that is filled in part is
+    copied in all layers (see mate_cache_fork in mate.h).  int32 CUDA tensors [n]."""
+    cache._native.cache_fork(cache._info, parents, children)
+
+
+def mate_cache_free(cache, seqs=None):
+    """The sequences (None: all) become empty, their pages lose a reference (see mate_cache_free in mate.h)."""
+    cache._native.cache_free(cache._info, seqs)
+
+
+def mate_cache_compact(cache, n_live=None):
+    """Moves the pages in use to the front (see mate_cache_compact in mate.h); returns their number, an int32 CUDA tensor."""
+    return cache._native.cache_compact(cache._info, n_live)
+
+
+def mate_attn_decode(cache, Q, row_ids, col_ids, seqs=None, layer=0, scale=None, max_len=None, out=None, lse=None):
+    """Attention of one new token per sequence over what is cached (see mate_attn_decode in mate.h).  Q: [B, heads, d]; row_ids,
+    col_ids: int32 [B], the new tokens' ids (ID_TEXT: text); seqs: int32 [B] (None: 0 .. B - 1); max_len: an upper bound of
+    the sequences' lengths.  Returns (O, LSE)."""
+    return cache._native.attn_decode(cache._info, layer, Q, seqs, row_ids, col_ids, scale, max_len, out, lse)

@@ -10,7 +10,7 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libmate.so")
-BINDING = os.path.join(CSRC, "binding.cpp")
+BINDING = [os.path.join(CSRC, "binding.cpp"), os.path.join(CSRC, "binding_cache.cpp")]
 NATIVE = os.path.join(PKG, "_native.so")
 TRACE_LIB = os.path.join(PKG, "libmate_trace.so")   # same sources with -DMATE_TRACE (cycle counters per role)
 
@@ -26,7 +26,7 @@ def _deps():
 
 def build_binding(force: bool = False) -> str:
     """The native module of the Python binding (host code against torch's C++ headers; libmate is not linked)."""
-    deps = [BINDING, os.path.join(ROOT, "include", "mate.h")]
+    deps = BINDING + [os.path.join(CSRC, "binding.h"), os.path.join(ROOT, "include", "mate.h")]
     if not force and os.path.exists(NATIVE) and all(os.path.getmtime(p) <= os.path.getmtime(NATIVE) for p in deps):
         return NATIVE
     import torch
@@ -39,7 +39,7 @@ def build_binding(force: bool = False) -> str:
     libs = os.path.join(os.path.dirname(torch.__file__), "lib")
     subprocess.run([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC", "-fvisibility=hidden",
                     "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI]
-                   + ["-I" + d for d in include] + ["-o", tmp, BINDING, "-L" + libs, "-Wl,-rpath," + libs]
+                   + ["-I" + d for d in include] + ["-o", tmp] + BINDING + ["-L" + libs, "-Wl,-rpath," + libs]
                    + ["-l" + x for x in ("c10", "c10_cuda", "torch_cpu", "torch_cuda", "torch_python")], check=True)
     os.replace(tmp, NATIVE)
     return NATIVE

@@ -4,20 +4,12 @@
 // through ctypes and torch's Python layer took 20 to 30 us, more than the kernels of a small table.
 //
 // The library is not linked: api.py loads it (MATE_LIB may name another build) and hands over the addresses.
-#define PY_SSIZE_T_CLEAN
-#include <Python.h>
+#include "binding.h"
 
-#include <ATen/cuda/EmptyTensor.h>
-#include <c10/cuda/CUDAFunctions.h>
-#include <c10/cuda/CUDAGuard.h>
-#include <c10/cuda/CUDAStream.h>
-#include <torch/csrc/Exceptions.h>
-#include <torch/csrc/autograd/python_variable.h>
-
-#include <cmath>
-#include <optional>
-
-#include "mate.h"
+namespace mate_binding {
+PyObject *mate_error = nullptr;
+}
+using namespace mate_binding;
 
 namespace {
 
@@ -27,7 +19,6 @@ struct Library {
     decltype(&mate_attn_bwd) bwd = nullptr;
     decltype(&mate_cell_mean) cell_mean = nullptr;
 } lib;
-PyObject *mate_error = nullptr;  // exception class, called with (status, where)
 
 // What a call needs to know of a plan; lives in a capsule of the Python object.
 struct PlanInfo {
@@ -40,49 +31,6 @@ struct PlanInfo {
 };
 const char kCapsule[] = "mate_plan_info";
 
-struct Raised {};  // a Python exception is set
-
-// Other Python threads run while a call may wait: the allocator for memory to become free, a launch for room in
-// the queue, the first use of a plan on another stream for its upload.
-struct NoGil {
-    PyThreadState *state = PyEval_SaveThread();
-    NoGil() = default;
-    NoGil(const NoGil &) = delete;
-    ~NoGil() { PyEval_RestoreThread(state); }
-};
-
-[[noreturn]] void fail(PyObject *type, const char *msg) {
-    PyErr_SetString(type, msg);
-    throw Raised();
-}
-[[noreturn]] void fail_named(PyObject *type, const char *format, const char *name) {
-    PyErr_Format(type, format, name);
-    throw Raised();
-}
-void check(int status, const char *where) {
-    if (status == MATE_OK) return;
-    PyObject *e = PyObject_CallFunction(mate_error, "is", status, where);
-    if (e) {
-        PyErr_SetObject(mate_error, e);
-        Py_DECREF(e);
-    }
-    throw Raised();
-}
-
-const at::Tensor &tensor(PyObject *o, const char *name) {
-    if (!THPVariable_Check(o)) fail_named(PyExc_ValueError, "%s must be a contiguous CUDA tensor", name);
-    return THPVariable_Unpack(o);
-}
-void *dev(const at::Tensor &t, const char *name) {
-    if (!t.is_cuda() || !t.is_contiguous()) fail_named(PyExc_ValueError, "%s must be a contiguous CUDA tensor", name);
-    return t.data_ptr();
-}
-int dtype_code(const at::Tensor &t) {
-    if (t.scalar_type() == at::kBFloat16) return MATE_BF16;
-    if (t.scalar_type() == at::kFloat) return MATE_F32;
-    PyErr_Format(PyExc_TypeError, "libmate takes bfloat16 or float32 tensors, got %s", c10::toString(t.scalar_type()));
-    throw Raised();
-}
 PlanInfo &plan_info(PyObject *o) {
     void *p = PyCapsule_GetPointer(o, kCapsule);
     if (!p) throw Raised();
@@ -98,28 +46,6 @@ int64_t split(const PlanInfo &pi, const at::Tensor &q) {
         fail(PyExc_ValueError, "tensor shapes do not match the plan");
     return q.size(3);
 }
-float scale_of(PyObject *o, int64_t d) {
-    if (o == Py_None) return (float)(1.0 / std::sqrt((double)d));
-    const double s = PyFloat_AsDouble(o);
-    if (s == -1.0 && PyErr_Occurred()) throw Raised();
-    return (float)s;
-}
-unsigned flags_of(PyObject *o) {
-    const unsigned long f = PyLong_AsUnsignedLongMask(o);
-    if (PyErr_Occurred()) throw Raised();
-    return (unsigned)f;
-}
-at::Tensor empty(c10::IntArrayRef size, at::ScalarType type, c10::Device device) {
-    return at::Tensor(at::detail::empty_cuda(size, type, device, std::nullopt));
-}
-
-// A tensor that is read or written as `n` elements of a type has that type, and at least as many.
-void holds(const at::Tensor &t, at::ScalarType type, int64_t n, const char *name) {
-    if (t.scalar_type() == type && t.numel() >= n) return;
-    PyErr_Format(PyExc_ValueError, "%s must be a %s tensor of %lld elements", name, c10::toString(type), (long long)n);
-    throw Raised();
-}
-
 // The caller's workspace, or the plan's own (allocated at the first call, kept afterwards).
 struct Workspace {
     void *ptr = nullptr;
@@ -147,18 +73,6 @@ struct Workspace {
         }
     }
 };
-
-template <typename F>
-PyObject *guarded(F &&f) {
-    try {
-        return f();
-    } catch (const Raised &) {
-        return nullptr;
-    } catch (const std::exception &e) {
-        torch::translate_exception_to_python(std::current_exception());
-        return nullptr;
-    }
-}
 
 // attn_fwd(info, Q, K, V, scale, impl, out, lse, workspace) -> (O, LSE)
 PyObject *attn_fwd(PyObject *, PyObject *const *a, Py_ssize_t n) {
@@ -336,4 +250,8 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nu
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__native() { return PyModule_Create(&module); }
+PyMODINIT_FUNC PyInit__native() {
+    PyObject *m = PyModule_Create(&module);
+    if (m && PyModule_AddFunctions(m, cache_methods) != 0) Py_CLEAR(m);
+    return m;
+}

@@ -1,0 +1,488 @@
+// Pages of a cache: room for new tokens (mate_cache_extend), sequences that share their pages (mate_cache_fork), pages
+// given back (mate_cache_free) and moved together (mate_cache_compact).
+//
+// What is decided -- who gets which page -- is whole numbers and the same on every launch: one block reads the
+// reference counts, each thread a run of consecutive pages, and a scan over the block ranks the free ones; the r-th
+// lowest free page goes to the r-th request.  Latency: a few dependent loads and two or three scans.  What is moved
+// (rows of keys and values, every layer) is bound by memory and done by a second kernel over all SMs.
+//
+// A sequence that stands in a list twice: every entry writes "INT_MIN + its place in the list" into the sequence's length
+// by atomicMin, so the first entry wins, whatever the order of the threads.
+#include "mate_cache.h"
+#include "sm100_ptx.cuh"
+
+namespace mate {
+namespace {
+
+constexpr int kThreads = 1024;   // of the deciding block
+constexpr int kPer = 4;          // entries of a list per thread: lists of up to 4096
+constexpr int kMost = kThreads * kPer;
+constexpr int kCopyThreads = 256;
+
+// Exclusive sum over the block's threads; *total gets the sum.  All threads call it.
+__device__ int block_scan(int x, int *total) {
+    __shared__ int s_warp[kThreads / 32 + 1];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int sum = x;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(~0u, sum, o);
+        if (lane >= o) sum += y;
+    }
+    __syncthreads();  // an earlier scan has been read
+    if (lane == 31) s_warp[warp] = sum;
+    __syncthreads();
+    if (warp == 0) {
+        const int w = s_warp[lane];
+        int t = w;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int y = __shfl_up_sync(~0u, t, o);
+            if (lane >= o) t += y;
+        }
+        s_warp[lane] = t - w;
+        if (lane == 31) s_warp[32] = t;
+    }
+    __syncthreads();
+    *total = s_warp[32];
+    return s_warp[warp] + sum - x;
+}
+
+// The thread's run of pages.
+struct PageRun {
+    int lo, hi;
+};
+__device__ __forceinline__ PageRun my_pages(int pages) {
+    const int per = (pages + kThreads - 1) / kThreads;
+    const int lo = min(pages, (int)threadIdx.x * per);
+    return {lo, min(pages, lo + per)};
+}
+
+__device__ __forceinline__ int claim_of(int i) { return INT32_MIN + i; }
+
+__global__ void __launch_bounds__(kThreads) extend_kernel(const __grid_constant__ CacheArgs c, const int32_t *seqs, const int32_t *counts, int n,
+                                                          int32_t *granted) {
+    __shared__ int s_off[kMost + 1], s_used;
+    ptx::launch_dependents();
+    ptx::wait_prior_grid();
+    const int tid = threadIdx.x, i0 = tid * kPer;
+    int s[kPer], len[kPer], count[kPer], need[kPer], status = 0;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+        s[j] = -1, need[j] = 0, len[j] = 0, count[j] = 0;
+        if (i0 + j >= n) continue;
+        s[j] = seq_of(seqs, i0 + j, c.seqs);
+        count[j] = counts[i0 + j];
+        if (s[j] >= 0) len[j] = c.lens[s[j]];
+        const int most = c.width * c.page_size;
+        if (s[j] < 0 || count[j] < 0 || len[j] < 0 || len[j] > most) {
+            status |= kCacheBad;
+            s[j] = -1;
+        } else if (count[j] > most - len[j]) {
+            status |= kCacheFull;
+            s[j] = -1;
+        }
+    }
+    if (tid == 0) s_used = 0;
+    __syncthreads();  // every length has been read
+#pragma unroll
+    for (int j = 0; j < kPer; ++j)
+        if (s[j] >= 0) atomicMin(&c.lens[s[j]], claim_of(i0 + j));
+    __syncthreads();
+    int sum = 0;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+        if (s[j] >= 0 && __ldcg(&c.lens[s[j]]) != claim_of(i0 + j)) {
+            status |= kCacheBad;  // the second entry of a sequence
+            s[j] = -1;
+        }
+        if (s[j] >= 0) need[j] = pages_of(len[j] + count[j], c.page_size) - pages_of(len[j], c.page_size);
+        sum += need[j];
+    }
+    int wanted;
+    int off = block_scan(sum, &wanted);
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+        s_off[i0 + j] = off;
+        off += need[j];
+    }
+    int n_free = 0, rank = 0;
+    const PageRun mine = my_pages(c.pages);
+    if (wanted > 0) {
+        int free_here = 0;
+        for (int p = mine.lo; p < mine.hi; ++p) free_here += c.refs[p] <= 0;
+        rank = block_scan(free_here, &n_free);
+    }
+    // granted: who fits into what is free; the pages that go out are the first `used` free ones
+    int used = 0;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+        const int end = s_off[i0 + j] + need[j];
+        const bool fits = s[j] >= 0 && (need[j] == 0 || end <= n_free);
+        if (s[j] >= 0 && !fits) status |= kCacheFull;
+        if (fits && need[j] > 0) used = max(used, end);
+        if (s[j] >= 0) c.lens[s[j]] = fits ? len[j] + count[j] : len[j];
+        if (i0 + j < n) granted[i0 + j] = fits ? count[j] : 0;
+    }
+    if (status) atomicOr(c.status, status);
+    if (wanted == 0) return;
+    if (used > 0) atomicMax(&s_used, used);
+    __syncthreads();
+    for (int p = mine.lo; p < mine.hi && rank < s_used; ++p) {
+        if (c.refs[p] > 0) continue;
+        const int i = owner_of(s_off, min(n, kMost), rank), q = seq_of(seqs, i, c.seqs);
+        // the owner's new length is known: its pages end there
+        const int at = pages_of(__ldcg(&c.lens[q]), c.page_size);
+        const int end = i + 1 < kMost ? s_off[i + 1] : wanted;
+        c.table[(size_t)q * c.width + at - (end - rank)] = p;
+        c.refs[p] = 1;
+        ++rank;
+    }
+}
+
+// What mate_cache_fork leaves for its copies, per entry of the list.
+struct ForkItem {
+    int32_t parent, child;  // child -1: nothing to do
+    int32_t full, fill;     // shared pages; filled slots of the page behind them
+    int32_t src, dst;       // that page, and the one it is copied to (-1: none)
+};
+
+__global__ void __launch_bounds__(kThreads) fork_kernel(const __grid_constant__ CacheArgs c, const int32_t *parents, const int32_t *children,
+                                                        int n, ForkItem *items) {
+    __shared__ int s_off[kMost + 1], s_dst[kMost];
+    ptx::launch_dependents();
+    ptx::wait_prior_grid();
+    const int tid = threadIdx.x, i0 = tid * kPer;
+    int p[kPer], ch[kPer], len[kPer], status = 0, sum = 0;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+        p[j] = ch[j] = -1, len[j] = 0;
+        if (i0 + j >= n) continue;
+        p[j] = seq_of(parents, i0 + j, c.seqs);
+        ch[j] = seq_of(children, i0 + j, c.seqs);
+        if (p[j] >= 0) len[j] = c.lens[p[j]];
+        if (p[j] < 0 || ch[j] < 0 || len[j] < 0 || len[j] > c.width * c.page_size || c.lens[ch[j]] != 0) {
+            status |= kCacheBad;
+            ch[j] = -1;
+        }
+    }
+    __syncthreads();  // every length has been read
+#pragma unroll
+    for (int j = 0; j < kPer; ++j)
+        if (ch[j] >= 0) atomicMin(&c.lens[ch[j]], claim_of(i0 + j));
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+        if (ch[j] >= 0 && __ldcg(&c.lens[ch[j]]) != claim_of(i0 + j)) {
+            status |= kCacheBad;  // the second entry of a child
+            ch[j] = -1;
+        }
+        sum += ch[j] >= 0 && len[j] % c.page_size != 0;
+    }
+    int wanted;
+    int off = block_scan(sum, &wanted);
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+        s_off[i0 + j] = off;
+        s_dst[i0 + j] = -1;
+        off += ch[j] >= 0 && len[j] % c.page_size != 0;
+    }
+    __syncthreads();
+    if (wanted > 0) {
+        const PageRun mine = my_pages(c.pages);
+        int free_here = 0, n_free;
+        for (int q = mine.lo; q < mine.hi; ++q) free_here += c.refs[q] <= 0;
+        int rank = block_scan(free_here, &n_free);
+        for (int q = mine.lo; q < mine.hi && rank < wanted; ++q) {
+            if (c.refs[q] > 0) continue;
+            s_dst[owner_of(s_off, min(n, kMost), rank++)] = q;
+            c.refs[q] = 1;
+        }
+        __syncthreads();
+    }
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+        if (i0 + j >= n) continue;
+        ForkItem it = {p[j], ch[j], 0, 0, -1, -1};
+        if (ch[j] >= 0) {
+            it.full = len[j] / c.page_size;
+            it.fill = len[j] - it.full * c.page_size;
+            if (it.fill > 0) {
+                it.src = c.table[(size_t)p[j] * c.width + it.full];
+                it.dst = s_dst[i0 + j];
+                if (it.dst < 0) status |= kCacheFull;
+            }
+            const bool done = it.fill == 0 || it.dst >= 0;
+            c.lens[ch[j]] = done ? len[j] : 0;
+            if (done) c.prefix[ch[j]] = c.prefix[p[j]];
+            if (!done) it.child = -1;
+            if (done && it.dst >= 0 && !in_range(it.src, c.pages)) {
+                status |= kCacheBad;  // nothing to copy from
+                it.src = -1;
+            }
+        }
+        items[i0 + j] = it;
+    }
+    if (status) atomicOr(c.status, status);
+}
+
+// How the rows of a page lie.
+struct PageShape {
+    int64_t page_stride, head_stride, slot_stride, layer_stride;  // bytes
+    int heads, row_bytes, layers, page_size;
+};
+// Copies one page of one layer's keys or values, its first `fill` slots.
+__device__ __forceinline__ void copy_page(const PageShape &sh, char *base, int src, int dst, int fill, int tid, int threads) {
+    const char *from = base + src * sh.page_stride;
+    char *to = base + dst * sh.page_stride;
+    const int per_row = sh.row_bytes / 16, n = sh.heads * fill * per_row;
+    constexpr int kFlight = 4;
+    for (int i = tid; i < n; i += threads * kFlight) {
+        uint4 v[kFlight];
+        int64_t at[kFlight];
+#pragma unroll
+        for (int j = 0; j < kFlight; ++j) {
+            const int u = i + j * threads;
+            if (u >= n) break;
+            const int row = u / per_row, part = u - row * per_row, head = row / fill, slot = row - head * fill;
+            at[j] = head * sh.head_stride + slot * sh.slot_stride + part * 16;
+            v[j] = *reinterpret_cast<const uint4 *>(from + at[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < kFlight; ++j)
+            if (i + j * threads < n) *reinterpret_cast<uint4 *>(to + at[j]) = v[j];
+    }
+}
+__device__ __forceinline__ void copy_ids(const CacheArgs &c, int src, int dst, int fill, int tid, int threads) {
+    for (int i = tid; i < fill; i += threads) {
+        c.row_ids[(size_t)dst * c.page_size + i] = c.row_ids[(size_t)src * c.page_size + i];
+        c.col_ids[(size_t)dst * c.page_size + i] = c.col_ids[(size_t)src * c.page_size + i];
+    }
+}
+
+// grid: (entry, layer and keys / values; one more for the table and the ids)
+__global__ void __launch_bounds__(kCopyThreads) fork_copy_kernel(const __grid_constant__ CacheArgs c, const __grid_constant__ PageShape sh,
+                                                                 const ForkItem *items) {
+    ptx::launch_dependents();
+    ptx::wait_prior_grid();
+    const ForkItem it = items[blockIdx.x];
+    if (it.child < 0) return;
+    const int part = blockIdx.y;
+    if (part < 2 * sh.layers) {
+        if (it.src < 0 || it.dst < 0) return;
+        copy_page(sh, (char *)(part & 1 ? c.v : c.k) + (part >> 1) * sh.layer_stride, it.src, it.dst, it.fill, threadIdx.x, kCopyThreads);
+        return;
+    }
+    if (it.src >= 0 && it.dst >= 0) copy_ids(c, it.src, it.dst, it.fill, threadIdx.x, kCopyThreads);
+    const int32_t *from = c.table + (size_t)it.parent * c.width;
+    int32_t *to = c.table + (size_t)it.child * c.width;
+    bool bad = false;
+    for (int i = threadIdx.x; i < it.full; i += kCopyThreads) {
+        const int page = from[i];
+        to[i] = page;
+        if (in_range(page, c.pages))
+            atomicAdd(&c.refs[page], 1);
+        else
+            bad = true;
+    }
+    if (threadIdx.x == 0 && it.dst >= 0) to[it.full] = it.dst;
+    if (bad) atomicOr(c.status, kCacheBad);
+}
+
+__global__ void __launch_bounds__(kCopyThreads) free_kernel(const __grid_constant__ CacheArgs c, const int32_t *seqs) {
+    __shared__ int s_len;
+    ptx::launch_dependents();
+    ptx::wait_prior_grid();
+    const int s = seq_of(seqs, blockIdx.x, c.seqs);
+    if (s < 0) {
+        if (threadIdx.x == 0) atomicOr(c.status, kCacheBad);
+        return;
+    }
+    if (threadIdx.x == 0) s_len = atomicExch(&c.lens[s], 0);  // (of two entries with one sequence one gets its length)
+    __syncthreads();
+    const int len = s_len;
+    bool bad = false;
+    const int n = pages_of(clip_len(len, c.width * c.page_size, &bad), c.page_size);
+    if (len != 0)
+        for (int i = threadIdx.x; i < c.width; i += kCopyThreads) {
+            int32_t *at = c.table + (size_t)s * c.width + i;
+            if (i < n) {
+                const int page = *at;
+                if (!in_range(page, c.pages)) {
+                    bad = true;
+                } else if (atomicSub(&c.refs[page], 1) <= 0) {
+                    atomicAdd(&c.refs[page], 1);  // it was free already
+                    bad = true;
+                }
+            }
+            *at = -1;
+        }
+    if (bad) atomicOr(c.status, kCacheBad);
+}
+
+// What mate_cache_compact leaves for its copies: the number of moves; from / to of each; the new place of every page
+// (-1: it has none).
+struct Moves {
+    int32_t *n, *from, *to, *place;
+};
+__global__ void __launch_bounds__(kThreads) compact_kernel(const __grid_constant__ CacheArgs c, Moves m, int32_t *n_live_out) {
+    ptx::launch_dependents();
+    ptx::wait_prior_grid();
+    const PageRun mine = my_pages(c.pages);
+    int live_here = 0, n_live, n_moves;
+    for (int p = mine.lo; p < mine.hi; ++p) live_here += c.refs[p] > 0;
+    block_scan(live_here, &n_live);
+    int holes = 0, movers = 0, n_holes;
+    for (int p = mine.lo; p < mine.hi; ++p) {
+        const bool live = c.refs[p] > 0;
+        holes += p < n_live && !live;
+        movers += p >= n_live && live;
+    }
+    int hole = block_scan(holes, &n_holes), mover = block_scan(movers, &n_moves);  // as many of the one as of the other
+    for (int p = mine.lo; p < mine.hi; ++p) {
+        const bool live = c.refs[p] > 0;
+        m.place[p] = p < n_live && live ? p : -1;
+        if (p < n_live && !live) m.to[hole++] = p;
+        if (p >= n_live && live) m.from[mover++] = p;
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < n_moves; i += kThreads) {
+        const int from = __ldcg(&m.from[i]), to = __ldcg(&m.to[i]);
+        m.place[from] = to;
+        c.refs[to] = c.refs[from];
+        c.refs[from] = 0;
+    }
+    if (threadIdx.x == 0) {
+        m.n[0] = n_moves;
+        *n_live_out = n_live;
+    }
+}
+
+// Blocks take (move, layer, keys / values) in turn, and then the table's rows.
+__global__ void __launch_bounds__(kCopyThreads) compact_copy_kernel(const __grid_constant__ CacheArgs c, const __grid_constant__ PageShape sh,
+                                                                    Moves m) {
+    ptx::launch_dependents();
+    ptx::wait_prior_grid();
+    const int n_moves = m.n[0], parts = 2 * sh.layers + 1;
+    for (int64_t w = blockIdx.x; w < (int64_t)n_moves * parts; w += gridDim.x) {
+        const int i = (int)(w / parts), part = (int)(w - (int64_t)i * parts), src = m.from[i], dst = m.to[i];
+        if (part < 2 * sh.layers)
+            copy_page(sh, (char *)(part & 1 ? c.v : c.k) + (part >> 1) * sh.layer_stride, src, dst, c.page_size, threadIdx.x, kCopyThreads);
+        else
+            copy_ids(c, src, dst, c.page_size, threadIdx.x, kCopyThreads);
+    }
+    bool bad = false;
+    for (int q = blockIdx.x; q < c.seqs; q += gridDim.x) {
+        const int n = pages_of(clip_len(c.lens[q], c.width * c.page_size, &bad), c.page_size);
+        for (int i = threadIdx.x; i < n; i += kCopyThreads) {
+            int32_t *at = c.table + (size_t)q * c.width + i;
+            const int page = *at, place = in_range(page, c.pages) ? m.place[page] : -1;
+            if (place < 0)
+                bad = true;  // no page, or one that nothing counts
+            else if (place != page)
+                *at = place;
+        }
+    }
+    if (bad) atomicOr(c.status, kCacheBad);
+}
+
+PageShape page_shape(const mate_cache_t *c) {
+    const int64_t size = (int64_t)elem_size(c->dtype);
+    return {c->page_stride * size, c->head_stride * size, c->slot_stride * size, c->layer_stride * size,
+            c->kv_heads, c->d * (int)size, c->layers, c->page_size};
+}
+size_t fork_bytes(int n) { return sizeof(ForkItem) * (size_t)n; }
+size_t compact_bytes(const mate_cache_t *c) { return sizeof(int32_t) * (64 + 3 * (size_t)c->pages); }
+
+int check_list(const mate_cache_t *c, const int32_t *list, int n, bool may_be_null) {
+    if (n < 0 || (n > 0 && !list && (!may_be_null || n > c->seqs))) return MATE_ERR_INVALID_ARG;
+    return n > kMost ? MATE_ERR_UNSUPPORTED : MATE_OK;
+}
+int check_workspace(const void *workspace, size_t have, size_t need) {
+    if (!workspace || have < need) return MATE_ERR_WORKSPACE;
+    return is_aligned(workspace, 256) ? MATE_OK : MATE_ERR_ALIGNMENT;
+}
+int as_status(cudaError_t e) { return e == cudaSuccess ? MATE_OK : MATE_ERR_CUDA; }
+
+}  // namespace
+
+size_t decode_workspace(const mate_cache_t *cache, int B);  // mate_decode.cu
+
+}  // namespace mate
+
+using namespace mate;
+
+extern "C" {
+
+int mate_cache_extend(const mate_cache_t *cache, const int32_t *seqs, const int32_t *counts, int n, int32_t *granted, void *stream) {
+    int rc = check_cache(cache);
+    if (rc == MATE_OK) rc = check_list(cache, seqs, n, true);
+    if (rc == MATE_OK && n > 0 && (!counts || !granted)) rc = MATE_ERR_INVALID_ARG;
+    if (rc == MATE_OK) rc = check_cache_device(cache);
+    if (rc != MATE_OK || n == 0) return rc;
+    return as_status(launch_after(extend_kernel, dim3(1), kThreads, 0, (cudaStream_t)stream, cache_args(cache, 0), seqs, counts, n, granted));
+}
+
+int mate_cache_fork(const mate_cache_t *cache, const int32_t *parents, const int32_t *children, int n, void *workspace,
+                    size_t workspace_bytes, void *stream) {
+    int rc = check_cache(cache);
+    if (rc == MATE_OK) rc = check_list(cache, parents, n, false);
+    if (rc == MATE_OK) rc = check_list(cache, children, n, false);
+    if (rc == MATE_OK && n > 0) rc = check_workspace(workspace, workspace_bytes, fork_bytes(n));
+    if (rc == MATE_OK) rc = check_cache_device(cache);
+    if (rc != MATE_OK || n == 0) return rc;
+    const CacheArgs c = cache_args(cache, 0);
+    ForkItem *items = static_cast<ForkItem *>(workspace);
+    cudaError_t e = launch_after(fork_kernel, dim3(1), kThreads, 0, (cudaStream_t)stream, c, parents, children, n, items);
+    if (e == cudaSuccess)
+        e = launch_after(fork_copy_kernel, dim3((unsigned)n, 2 * (unsigned)cache->layers + 1), kCopyThreads, 0, (cudaStream_t)stream, c,
+                         page_shape(cache), (const ForkItem *)items);
+    return as_status(e);
+}
+
+int mate_cache_free(const mate_cache_t *cache, const int32_t *seqs, int n, void *stream) {
+    int rc = check_cache(cache);
+    if (rc == MATE_OK && (n < 0 || (!seqs && n > cache->seqs))) rc = MATE_ERR_INVALID_ARG;
+    if (rc == MATE_OK) rc = check_cache_device(cache);
+    if (rc != MATE_OK || n == 0) return rc;
+    return as_status(launch_after(free_kernel, dim3((unsigned)n), kCopyThreads, 0, (cudaStream_t)stream, cache_args(cache, 0), seqs));
+}
+
+int mate_cache_compact(const mate_cache_t *cache, int32_t *n_live, void *workspace, size_t workspace_bytes, void *stream) {
+    int rc = check_cache(cache);
+    if (rc == MATE_OK && !n_live) rc = MATE_ERR_INVALID_ARG;
+    if (rc == MATE_OK) rc = check_workspace(workspace, workspace_bytes, compact_bytes(cache));
+    if (rc == MATE_OK) rc = check_cache_device(cache);
+    if (rc != MATE_OK) return rc;
+    const CacheArgs c = cache_args(cache, 0);
+    int32_t *w = static_cast<int32_t *>(workspace);
+    const Moves m = {w, w + 64, w + 64 + (size_t)cache->pages, w + 64 + 2 * (size_t)cache->pages};
+    cudaError_t e = launch_after(compact_kernel, dim3(1), kThreads, 0, (cudaStream_t)stream, c, m, n_live);
+    if (e == cudaSuccess)
+        e = launch_after(compact_copy_kernel, dim3((unsigned)(n_sms(cache->device) * 8)), kCopyThreads, 0, (cudaStream_t)stream, c, page_shape(cache), m);
+    return as_status(e);
+}
+
+int mate_cache_workspace_bytes(const mate_cache_t *cache, int n, size_t *fork, size_t *compact, size_t *decode) {
+    const int rc = check_cache(cache);
+    if (rc != MATE_OK) return rc;
+    if (n < 0) return MATE_ERR_INVALID_ARG;
+    if (fork) *fork = fork_bytes(n);
+    if (compact) *compact = compact_bytes(cache);
+    if (decode) *decode = decode_workspace(cache, n);
+    return MATE_OK;
+}
+
+int mate_cache_status(const mate_cache_t *cache, void *stream) {
+    int rc = check_cache(cache);
+    if (rc == MATE_OK) rc = check_cache_device(cache);
+    if (rc != MATE_OK) return rc;
+    cudaStream_t st = (cudaStream_t)stream;
+    int32_t s = 0;
+    if (cudaMemcpyAsync(&s, cache->status, sizeof s, cudaMemcpyDeviceToHost, st) != cudaSuccess ||
+        cudaMemsetAsync(cache->status, 0, sizeof s, st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess)
+        return MATE_ERR_CUDA;
+    return s & kCacheFull ? MATE_ERR_NOMEM : s ? MATE_ERR_INVALID_ARG : MATE_OK;
+}
+
+}  // extern "C"
