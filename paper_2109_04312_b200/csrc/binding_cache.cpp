@@ -55,9 +55,8 @@ const at::Tensor &on_gpu(PyObject *o, const char *name, const c10::Device *devic
     if (device && t.device() != *device) fail_shape(name, "on the device of the others");
     return t;
 }
-// A contiguous int32 tensor of the given shape; null for None where that is allowed.
-int32_t *ints(PyObject *o, const char *name, c10::IntArrayRef shape, const c10::Device &device, bool may_be_none) {
-    if (o == Py_None && may_be_none) return nullptr;
+// An int32 tensor of the given shape.
+const at::Tensor &int_tensor(PyObject *o, const char *name, c10::IntArrayRef shape) {
     if (!THPVariable_Check(o)) fail_shape(name, "a contiguous int32 CUDA tensor");
     const at::Tensor &t = THPVariable_Unpack(o);
     if (t.scalar_type() != at::kInt || t.sizes() != shape) {
@@ -65,6 +64,12 @@ int32_t *ints(PyObject *o, const char *name, c10::IntArrayRef shape, const c10::
                      (long long)c10::multiply_integers(shape), (int)shape.size());
         throw Raised();
     }
+    return t;
+}
+// The same, contiguous and on the GPU; null for None where that is allowed.
+int32_t *ints(PyObject *o, const char *name, c10::IntArrayRef shape, const c10::Device &device, bool may_be_none) {
+    if (o == Py_None && may_be_none) return nullptr;
+    const at::Tensor &t = int_tensor(o, name, shape);
     if (!t.is_cuda() || !t.is_contiguous() || t.device() != device) fail_shape(name, "a contiguous CUDA tensor on the device of the others");
     return t.data_ptr<int32_t>();
 }
@@ -205,22 +210,21 @@ PyObject *new_cache(PyObject *, PyObject *const *a, Py_ssize_t n) {
         const int dt = dtype_code(k);
         rows(k, "k"), rows(v, "v");
         if (k.strides() != v.strides() || !distinct(k)) fail_shape("k and v", "laid out alike, without elements that share their memory");
-        for (int i = 2; i < 9; ++i)
-            if (!THPVariable_Check(a[i])) fail_shape("the cache's arrays", "int32 CUDA tensors");
+        if (!THPVariable_Check(a[4]) || THPVariable_Unpack(a[4]).dim() != 2) fail_shape("table", "an int32 CUDA tensor [seqs, width]");
         const at::Tensor &table = THPVariable_Unpack(a[4]);
-        if (table.dim() != 2) fail_shape("table", "[seqs, width]");
         if (!PyBytes_Check(a[9])) fail_shape("head_view", "bytes");
         const int64_t pages = k.size(1), page_size = k.size(3), seqs = table.size(0), width = table.size(1);
         const c10::Device device = k.device();
         auto info = std::make_unique<CacheInfo>(CacheInfo{{}, {}, k.scalar_type(), device});
         mate_cache_t &c = info->c;
-        c.row_ids = ints(a[2], "row_ids", {pages, page_size}, device, false);
-        c.col_ids = ints(a[3], "col_ids", {pages, page_size}, device, false);
-        c.table = ints(a[4], "table", {seqs, width}, device, false);
-        c.lens = ints(a[5], "lens", {seqs}, device, false);
-        c.prefix = ints(a[6], "prefix", {seqs}, device, false);
-        c.refs = ints(a[7], "refs", {pages}, device, false);
-        c.status = ints(a[8], "status", {1}, device, false);
+        struct {
+            int32_t **to;
+            const char *name;
+            std::vector<int64_t> shape;
+        } arrays[] = {{&c.row_ids, "row_ids", {pages, page_size}}, {&c.col_ids, "col_ids", {pages, page_size}}, {&c.table, "table", {seqs, width}},
+                      {&c.lens, "lens", {seqs}}, {&c.prefix, "prefix", {seqs}}, {&c.refs, "refs", {pages}}, {&c.status, "status", {1}}};
+        for (int i = 0; i < 7; ++i) int_tensor(a[2 + i], arrays[i].name, arrays[i].shape);
+        for (int i = 0; i < 7; ++i) *arrays[i].to = ints(a[2 + i], arrays[i].name, arrays[i].shape, device, false);
         if (!k.is_cuda() || v.device() != device) fail_shape("k and v", "CUDA tensors on one device");
         const uint8_t *view = reinterpret_cast<const uint8_t *>(PyBytes_AS_STRING(a[9]));
         info->head_view.assign(view, view + PyBytes_GET_SIZE(a[9]));

@@ -153,20 +153,20 @@ __global__ void __launch_bounds__(kThreads) fork_kernel(const __grid_constant__ 
     ptx::launch_dependents();
     ptx::wait_prior_grid();
     const int tid = threadIdx.x, i0 = tid * kPer;
-    int p[kPer], ch[kPer], len[kPer], status = 0, sum = 0;
+    int p[kPer], ch[kPer], len[kPer], prefix[kPer], status = 0, sum = 0;
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
-        p[j] = ch[j] = -1, len[j] = 0;
+        p[j] = ch[j] = -1, len[j] = prefix[j] = 0;
         if (i0 + j >= n) continue;
         p[j] = seq_of(parents, i0 + j, c.seqs);
         ch[j] = seq_of(children, i0 + j, c.seqs);
-        if (p[j] >= 0) len[j] = c.lens[p[j]];
+        if (p[j] >= 0) len[j] = c.lens[p[j]], prefix[j] = c.prefix[p[j]];
         if (p[j] < 0 || ch[j] < 0 || len[j] < 0 || len[j] > c.width * c.page_size || c.lens[ch[j]] != 0) {
             status |= kCacheBad;
             ch[j] = -1;
         }
     }
-    __syncthreads();  // every length has been read
+    __syncthreads();  // every length and prefix has been read
 #pragma unroll
     for (int j = 0; j < kPer; ++j)
         if (ch[j] >= 0) atomicMin(&c.lens[ch[j]], claim_of(i0 + j));
@@ -214,7 +214,7 @@ __global__ void __launch_bounds__(kThreads) fork_kernel(const __grid_constant__ 
             }
             const bool done = it.fill == 0 || it.dst >= 0;
             c.lens[ch[j]] = done ? len[j] : 0;
-            if (done) c.prefix[ch[j]] = c.prefix[p[j]];
+            if (done) c.prefix[ch[j]] = prefix[j];
             if (!done) it.child = -1;
             if (done && it.dst >= 0 && !in_range(it.src, c.pages)) {
                 status |= kCacheBad;  // nothing to copy from
