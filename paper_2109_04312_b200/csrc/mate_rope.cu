@@ -2,12 +2,14 @@
 // rows of up to three tensors (queries, keys; values are only copied) and writes them by strides or through a page table.
 //
 // A pair (a, b) becomes m (a cos t - b sin t, a sin t + b cos t), t = position * freqs[pair]; the transpose has -t.  The
-// angle is reduced in 64 bits (position * freqs / 2 pi, minus the nearest whole number of turns), which leaves an error
-// of 1e-9 of a turn at positions of 10^7; sine and cosine of what is left are taken in fp32 by sincospif.
+// angle's whole turns do not matter, so a frequency is kept as a 64-bit fraction of a turn per position and multiplied by the
+// position modulo 2^64: exact but for the fraction's own rounding (2^-65 turns per position and the 2^-53 of the 64-bit
+// frequency), for three integer instructions.  (In 64-bit floating point the same took most of the kernel's time.)  Sine and
+// cosine of the fraction that is left are taken in fp32 by sincospif.
 //
-// Bound by memory: one read and one write of every element.  A block takes up to kTokens tokens and a slice of the heads:
-// all its loads are under way (kUnits of them per thread, 16 bytes each half) before the tokens' sines and cosines are worked
-// out, once per block into shared memory, for all heads of the slice.
+// Bound by memory: one read and one write of every element.  A thread has one token and one unit of its rows -- two runs of VEC
+// elements, which are VEC pairs -- works out their sines and cosines once and takes the heads of its slice in turn, kFlight at
+// a time with all their loads under way (the first ones before the sines).
 #include <cuda_bf16.h>
 
 #include "mate_cache.h"
@@ -16,9 +18,8 @@
 namespace mate {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kTokens = 16;  // tokens of a block, at most (wide rows: 8, 4, 2 or 1)
-constexpr int kUnits = 4;    // units of a thread: a unit is two runs of VEC elements of one head of one token
+constexpr int kThreads = 128;
+constexpr int kFlight = 4;  // heads of a thread that are under way together
 
 struct Side {
     const void *x;
@@ -26,32 +27,51 @@ struct Side {
     int64_t xs[3], ys[3];
     int heads;
     int turned, to_keys;
+    int first_slice;  // slices of heads are numbered through over the sides
 };
 struct RopeParams {
     Side side[3];
-    int n_sides, n_heads;  // heads of all sides together
+    int n_sides;
     int B, N, d, rot, interleaved;
     const int32_t *positions;
     int64_t position_stride;
     const double *freqs;
     float mscale, sign;
-    int n_chunks, turned_chunks;      // units of a head, and how many of them are pairs
-    unsigned magic;                   // x / n_chunks = x * magic >> 20 for x below 2^10 and up to 2^10 chunks
-    int heads_per_block, token_bits;  // (2^token_bits tokens)
+    int n_chunks, turned_chunks;  // units of a head, and how many of them are pairs
+    int heads_of_thread;
     // new tokens of a cache
     int paged;
     CacheArgs cache;
     const int32_t *seqs, *counts, *row_ids, *col_ids;
 };
 
+// VEC elements, as they lie in memory and as numbers
 template <typename T, int VEC>
 struct alignas(sizeof(T) * VEC) Run {
     T v[VEC];
 };
-__device__ __forceinline__ float to_f32(float x) { return x; }
-__device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
-__device__ __forceinline__ void from_f32(float x, float &y) { y = x; }
-__device__ __forceinline__ void from_f32(float x, __nv_bfloat16 &y) { y = __float2bfloat16_rn(x); }
+template <int VEC>
+__device__ __forceinline__ void unpack(const Run<float, VEC> &r, float (&x)[VEC]) {
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) x[i] = r.v[i];
+}
+template <int VEC>
+__device__ __forceinline__ void pack(const float (&x)[VEC], Run<float, VEC> &r) {
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) r.v[i] = x[i];
+}
+__device__ __forceinline__ void unpack(const Run<__nv_bfloat16, 1> &r, float (&x)[1]) { x[0] = __bfloat162float(r.v[0]); }
+__device__ __forceinline__ void pack(const float (&x)[1], Run<__nv_bfloat16, 1> &r) { r.v[0] = __float2bfloat16_rn(x[0]); }
+__device__ __forceinline__ void unpack(const Run<__nv_bfloat16, 8> &r, float (&x)[8]) {
+    const uint4 u = *reinterpret_cast<const uint4 *>(&r);
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[2 * i] = __uint_as_float(w[i] << 16), x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+}
+__device__ __forceinline__ void pack(const float (&x)[8], Run<__nv_bfloat16, 8> &r) {
+    *reinterpret_cast<uint4 *>(&r) = make_uint4(ptx::cvt_bf16x2(x[0], x[1]), ptx::cvt_bf16x2(x[2], x[3]), ptx::cvt_bf16x2(x[4], x[5]),
+                                                ptx::cvt_bf16x2(x[6], x[7]));
+}
 
 // Element offsets of a unit's two runs within a row; the second one is missing at the end of an odd row.
 struct Place {
@@ -67,153 +87,143 @@ __device__ __forceinline__ Place place(const RopeParams &p, int chunk, bool turn
 }
 
 template <typename T, int VEC>
-__global__ void __launch_bounds__(kThreads) rope_kernel(const __grid_constant__ RopeParams p) {
-    extern __shared__ float s_trig[];  // [tokens][rot / 2] cosines, then sines
-    __shared__ int64_t s_from[3][kTokens], s_to[3][kTokens];
-    __shared__ int s_pos[kTokens];
+__global__ void __launch_bounds__(kThreads, 6) rope_kernel(const __grid_constant__ RopeParams p) {
+    extern __shared__ uint64_t s_turn[];  // [rot / 2] turns per position, in 2^-64
     ptx::launch_dependents();
     ptx::wait_prior_grid();
-    const int tid = threadIdx.x, pairs = p.rot / 2, tokens = 1 << p.token_bits;
-    const int64_t first = (int64_t)blockIdx.x << p.token_bits, n_tokens = (int64_t)p.B * p.N;
-    const int h0 = blockIdx.y * p.heads_per_block, n_heads = min(p.heads_per_block, p.n_heads - h0);
-
-    // where the tokens' rows are: -1 = nowhere
-    if (tid < tokens) {
-        const int64_t t = first + tid;
-        const bool exists = t < n_tokens;
-        const int b = exists ? (int)(t / p.N) : 0, n = exists ? (int)(t - (int64_t)b * p.N) : 0;
-        int position = 0;
-        int64_t page_at = -1;
-        if (p.paged && exists) {
-            bool bad = false;
-            const int s = seq_of(p.seqs, b, p.cache.seqs), count = p.counts ? p.counts[b] : p.N;
-            if (s < 0 || count < 0 || count > p.N) {
-                bad = true;
-            } else if (n < count) {
-                const int at = clip_len(p.cache.lens[s], p.cache.width * p.cache.page_size, &bad) - count + n;
-                position = at;
-                if (at < 0) bad = true;
-                if (!bad) {
-                    const int i = at / p.cache.page_size, slot = at - i * p.cache.page_size;
-                    const int page = p.cache.table[(size_t)s * p.cache.width + i];
-                    if (!in_range(page, p.cache.pages)) {
-                        bad = true;
-                    } else {
-                        page_at = page * p.cache.page_stride + slot * p.cache.slot_stride;
-                        if (p.row_ids && blockIdx.y == 0) {
-                            const size_t to = (size_t)page * p.cache.page_size + slot;
-                            p.cache.row_ids[to] = p.row_ids[t];
-                            p.cache.col_ids[to] = p.col_ids[t];
-                        }
+    const int64_t at = (int64_t)blockIdx.x * kThreads + threadIdx.x, t = at / p.n_chunks;
+    const int chunk = (int)(at - t * p.n_chunks), b = (int)(t / p.N), n = (int)(t - (int64_t)b * p.N);
+    const int side = (int)(p.n_sides > 1 && blockIdx.y >= p.side[1].first_slice) + (int)(p.n_sides > 2 && blockIdx.y >= p.side[2].first_slice);
+    const Side &s = p.side[side];
+    const int h0 = (blockIdx.y - s.first_slice) * p.heads_of_thread, n_heads = min(s.heads - h0, p.heads_of_thread);
+    const bool exists = b < p.B;
+    int position = 0;
+    int64_t page_at = -1;  // where the token's row is in the pages, -1: nowhere
+    if (p.paged && exists) {
+        bool bad = false;
+        const int q = seq_of(p.seqs, b, p.cache.seqs), count = p.counts ? p.counts[b] : p.N;
+        if (q < 0 || count < 0 || count > p.N) {
+            bad = true;
+        } else if (n < count) {
+            const int at = clip_len(p.cache.lens[q], p.cache.width * p.cache.page_size, &bad) - count + n;
+            position = at;
+            if (at < 0) bad = true;
+            if (!bad) {
+                const int i = at / p.cache.page_size, slot = at - i * p.cache.page_size;
+                const int page = p.cache.table[(size_t)q * p.cache.width + i];
+                if (!in_range(page, p.cache.pages)) {
+                    bad = true;
+                } else {
+                    page_at = page * p.cache.page_stride + slot * p.cache.slot_stride;
+                    if (p.row_ids && blockIdx.y == 0 && chunk == 0) {
+                        const size_t to = (size_t)page * p.cache.page_size + slot;
+                        p.cache.row_ids[to] = p.row_ids[t];
+                        p.cache.col_ids[to] = p.col_ids[t];
                     }
                 }
             }
-            if (bad && blockIdx.y == 0) atomicOr(p.cache.status, kCacheBad);
         }
-        if (exists && p.positions) position = p.positions[b * p.position_stride + n];
-        s_pos[tid] = position;
-        for (int i = 0; i < p.n_sides; ++i) {
-            const Side &s = p.side[i];
-            const bool goes = exists && (s.y || page_at >= 0);
-            s_from[i][tid] = goes ? b * s.xs[0] + n * s.xs[2] : -1;
-            s_to[i][tid] = s.y ? b * s.ys[0] + n * s.ys[2] : page_at;
-        }
+        if (bad && blockIdx.y == 0 && chunk == 0) atomicOr(p.cache.status, kCacheBad);
     }
-    __syncthreads();
+    if (p.positions && exists) position = p.positions[b * p.position_stride + n];
 
-    Run<T, VEC> a[kUnits], b[kUnits];
-    const int units = (n_heads << p.token_bits) * p.n_chunks;
-    // head (within the slice), token and chunk of a unit: chunks next to one another, then tokens, then heads
-    auto locate = [&](int u, int &side, int &head, int &token, int &chunk) {
-        const int row = (int)((unsigned)u * p.magic >> 20);
-        chunk = u - row * p.n_chunks;
-        token = row & (tokens - 1);
-        head = h0 + (row >> p.token_bits);
-        side = 0;
-        while (side + 1 < p.n_sides && head >= p.side[side].heads) head -= p.side[side++].heads;
+    const bool goes = exists && (s.y || page_at >= 0);
+    const Place place_of = place<VEC>(p, chunk, s.turned);
+    const int second = place_of.b - place_of.a;  // from one run to the other
+    const bool two = VEC > 1 || place_of.has_b;
+    const T *from = (const T *)s.x + b * s.xs[0] + h0 * s.xs[1] + n * s.xs[2] + place_of.a;
+    T *to = s.y ? (T *)s.y + b * s.ys[0] + h0 * s.ys[1] + n * s.ys[2] + place_of.a
+                : (T *)(s.to_keys ? p.cache.k : p.cache.v) + page_at + h0 * p.cache.head_stride + place_of.a;
+    const int64_t from_step = s.xs[1], to_step = s.y ? s.ys[1] : p.cache.head_stride;
+    Run<T, VEC> x[kFlight], y[kFlight];
+    auto load = [&](int h) {
+        if (!goes) return;
+#pragma unroll
+        for (int i = 0; i < kFlight; ++i) {
+            if (h + i >= n_heads) break;
+            x[i] = *reinterpret_cast<const Run<T, VEC> *>(from);
+            if (two) y[i] = *reinterpret_cast<const Run<T, VEC> *>(from + second);
+            from += from_step;
+        }
     };
-#pragma unroll
-    for (int i = 0; i < kUnits; ++i) {
-        const int u = tid + i * kThreads;
-        if (u >= units) break;
-        int side, head, token, chunk;
-        locate(u, side, head, token, chunk);
-        const Side &s = p.side[side];
-        if (s_from[side][token] < 0) continue;
-        const T *x = (const T *)s.x + s_from[side][token] + head * s.xs[1];
-        const Place at = place<VEC>(p, chunk, s.turned);
-        a[i] = *reinterpret_cast<const Run<T, VEC> *>(x + at.a);
-        if (at.has_b) b[i] = *reinterpret_cast<const Run<T, VEC> *>(x + at.b);
-    }
-    for (int i = tid; i < tokens * pairs; i += kThreads) {
-        const int token = i / pairs, pair = i - token * pairs;
-        const double turns = (double)s_pos[token] * (p.freqs[pair] * 0.15915494309189533577);
-        float sn, cs;
-        sincospif(2.f * (float)(turns - rint(turns)), &sn, &cs);
-        s_trig[i] = cs * p.mscale;
-        s_trig[tokens * pairs + i] = sn * p.mscale * p.sign;
+    load(0);
+
+    for (int i = threadIdx.x; i < p.rot / 2; i += kThreads) {
+        const double turns = p.freqs[i] * 0.15915494309189533577;
+        s_turn[i] = (uint64_t)__double2ull_rn((turns - floor(turns)) * 18446744073709551616.0);
     }
     __syncthreads();
+    if (!goes) return;
+    const bool turned = s.turned && chunk < p.turned_chunks;
+    float cs[VEC], sn[VEC];
+    if (turned) {
 #pragma unroll
-    for (int i = 0; i < kUnits; ++i) {
-        const int u = tid + i * kThreads;
-        if (u >= units) break;
-        int side, head, token, chunk;
-        locate(u, side, head, token, chunk);
-        const Side &s = p.side[side];
-        if (s_from[side][token] < 0) continue;
-        const Place at = place<VEC>(p, chunk, s.turned);
-        if (s.turned && chunk < p.turned_chunks) {
-            const float *cs = s_trig + token * pairs + chunk * VEC, *sn = cs + tokens * pairs;
-            if (p.interleaved && VEC > 1) {  // pairs lie side by side: VEC / 2 in each run
-#pragma unroll
-                for (int e = 0; e < VEC; e += 2)
-#pragma unroll
-                    for (int half = 0; half < 2; ++half) {
-                        T *r = half ? &b[i].v[e & (VEC - 1)] : &a[i].v[e & (VEC - 1)];
-                        const float c = cs[half * VEC / 2 + e / 2], z = sn[half * VEC / 2 + e / 2], x = to_f32(r[0]), y = to_f32(r[1 & (VEC - 1)]);
-                        from_f32(x * c - y * z, r[0]);
-                        from_f32(x * z + y * c, r[1 & (VEC - 1)]);
-                    }
-            } else {
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    const float c = cs[e], z = sn[e], x = to_f32(a[i].v[e]), y = to_f32(b[i].v[e]);
-                    from_f32(x * c - y * z, a[i].v[e]);
-                    from_f32(x * z + y * c, b[i].v[e]);
-                }
-            }
+        for (int e = 0; e < VEC; ++e) {
+            const int64_t turn = (int64_t)(s_turn[chunk * VEC + e] * (uint64_t)(int64_t)position);
+            sincospif((float)(int32_t)(turn >> 32) * 4.656612873077393e-10f, &sn[e], &cs[e]);  // 2^-31
+            cs[e] *= p.mscale;
+            sn[e] *= p.mscale * p.sign;
         }
-        T *y = (T *)(s.y ? s.y : s.to_keys ? p.cache.k : p.cache.v) + s_to[side][token] + head * (s.y ? s.ys[1] : p.cache.head_stride);
-        *reinterpret_cast<Run<T, VEC> *>(y + at.a) = a[i];
-        if (at.has_b) *reinterpret_cast<Run<T, VEC> *>(y + at.b) = b[i];
+    }
+    for (int h = 0; h < n_heads; h += kFlight) {
+        if (h > 0) load(h);
+#pragma unroll
+        for (int i = 0; i < kFlight; ++i) {
+            if (h + i >= n_heads) break;
+            if (turned) {
+                float u[VEC], w[VEC];
+                unpack(x[i], u);
+                unpack(y[i], w);
+                if (p.interleaved && VEC > 1) {  // pairs lie side by side, VEC / 2 in each run
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) {
+                        float &c = (e < VEC / 2 ? u : w)[2 * e % VEC], &d = (e < VEC / 2 ? u : w)[(2 * e + 1) % VEC];
+                        const float c0 = c;
+                        c = c0 * cs[e] - d * sn[e];
+                        d = c0 * sn[e] + d * cs[e];
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) {
+                        const float u0 = u[e];
+                        u[e] = u0 * cs[e] - w[e] * sn[e];
+                        w[e] = u0 * sn[e] + w[e] * cs[e];
+                    }
+                }
+                pack(u, x[i]);
+                pack(w, y[i]);
+            }
+            *reinterpret_cast<Run<T, VEC> *>(to) = x[i];
+            if (two) *reinterpret_cast<Run<T, VEC> *>(to + second) = y[i];
+            to += to_step;
+        }
     }
 }
 
 template <typename T, int VEC>
-int launch(RopeParams &p, cudaStream_t st) {
+int launch(RopeParams &p, int device, cudaStream_t st) {
     p.turned_chunks = p.rot / 2 / VEC;
     p.n_chunks = VEC == 1 ? (p.d + 1) / 2 : p.d / (2 * VEC);
-    p.magic = ((1u << 20) + p.n_chunks - 1) / p.n_chunks;
-    // a block's units are at most kUnits for each thread
-    int tokens = kTokens;
-    p.token_bits = 4;
-    while (kUnits * kThreads < tokens * p.n_chunks) tokens >>= 1, --p.token_bits;
-    static_assert(kUnits * kThreads >= 512, "a row has up to 512 units");
-    const int most = kUnits * kThreads / (tokens * p.n_chunks);
-    p.heads_per_block = most < p.n_heads ? most : p.n_heads;
-    const int64_t tiles = ((int64_t)p.B * p.N + tokens - 1) / tokens;
-    const int64_t slices = ((int64_t)p.n_heads + p.heads_per_block - 1) / p.heads_per_block;
-    if (tiles > INT32_MAX || slices > 65535) return MATE_ERR_UNSUPPORTED;
-    return launch_after(rope_kernel<T, VEC>, dim3((unsigned)tiles, (unsigned)slices), kThreads, sizeof(float) * tokens * p.rot, st, p) == cudaSuccess
+    const int64_t threads = (int64_t)p.B * p.N * p.n_chunks, blocks = (threads + kThreads - 1) / kThreads;
+    // as many heads to a thread as leave every SM 1024 of them, in whole batches
+    int64_t n_heads = 0, slices = 0;
+    for (int i = 0; i < p.n_sides; ++i) n_heads += p.side[i].heads;
+    const int64_t heads = threads * n_heads / (1024 * (int64_t)n_sms(device));
+    p.heads_of_thread = heads <= 2 ? (heads < 1 ? 1 : (int)heads) : (int)((heads < n_heads ? heads : n_heads) + kFlight - 1) / kFlight * kFlight;
+    for (int i = 0; i < p.n_sides; ++i) {
+        p.side[i].first_slice = (int)slices;
+        slices += (p.side[i].heads + p.heads_of_thread - 1) / p.heads_of_thread;
+    }
+    if (blocks > INT32_MAX || slices > 65535) return MATE_ERR_UNSUPPORTED;
+    return launch_after(rope_kernel<T, VEC>, dim3((unsigned)blocks, (unsigned)slices), kThreads, sizeof(uint64_t) * (p.rot / 2), st, p) == cudaSuccess
                ? MATE_OK
                : MATE_ERR_CUDA;
 }
 
 // Whole runs of 16 bytes where the pairs, the rest of the row, every address and every stride allow it, else one
 // element at a time.
-int run(RopeParams &p, int dtype, cudaStream_t st) {
-    if (p.B == 0 || p.N == 0 || p.n_heads == 0) return MATE_OK;
+int run(RopeParams &p, int dtype, int device, cudaStream_t st) {
+    if (p.B == 0 || p.N == 0 || p.n_sides == 0) return MATE_OK;
     const size_t size = elem_size(dtype);
     const int vec = (int)(16 / size);
     bool wide = p.rot % (2 * vec) == 0 && p.d % (2 * vec) == 0;
@@ -222,8 +232,8 @@ int run(RopeParams &p, int dtype, cudaStream_t st) {
         wide = is_aligned(s.x, 16) && (!s.y || is_aligned(s.y, 16));
         for (int j = 0; j < 3 && wide; ++j) wide = s.xs[j] % vec == 0 && (!s.y || s.ys[j] % vec == 0);
     }
-    if (dtype == MATE_F32) return wide ? launch<float, 4>(p, st) : launch<float, 1>(p, st);
-    return wide ? launch<__nv_bfloat16, 8>(p, st) : launch<__nv_bfloat16, 1>(p, st);
+    if (dtype == MATE_F32) return wide ? launch<float, 4>(p, device, st) : launch<float, 1>(p, device, st);
+    return wide ? launch<__nv_bfloat16, 8>(p, device, st) : launch<__nv_bfloat16, 1>(p, device, st);
 }
 
 bool set_angles(RopeParams &p, const int32_t *positions, int64_t stride, const double *freqs, int rot, float mscale, unsigned flags) {
@@ -258,10 +268,10 @@ extern "C" int mate_rope(const mate_rope_tensor_t *tensors, int n_tensors, int B
         Side &s = p.side[p.n_sides++];
         s.x = t.x, s.y = t.y, s.heads = t.heads, s.turned = rot > 0;
         for (int j = 0; j < 3; ++j) s.xs[j] = t.x_stride[j], s.ys[j] = t.y_stride[j];
-        if (p.n_heads > INT32_MAX - t.heads) return MATE_ERR_UNSUPPORTED;
-        p.n_heads += t.heads;
     }
-    return run(p, dtype, (cudaStream_t)stream);
+    int device = 0;
+    if (cudaGetDevice(&device) != cudaSuccess) return MATE_ERR_CUDA;
+    return run(p, dtype, device, (cudaStream_t)stream);
 }
 
 extern "C" int mate_cache_append(const mate_cache_t *cache, int layer, const void *K, const void *V, const int64_t *k_stride,
@@ -288,7 +298,6 @@ extern "C" int mate_cache_append(const mate_cache_t *cache, int layer, const voi
         Side &s = p.side[p.n_sides++];
         s.x = x, s.y = y, s.heads = heads, s.turned = turned, s.to_keys = to_keys;
         for (int j = 0; j < 3; ++j) s.xs[j] = xs[j], s.ys[j] = ys ? ys[j] : 0;
-        p.n_heads += heads;
     };
     if (Q) add(Q, Q_out, q_stride, q_out_stride, cache->heads, rot > 0, false);
     add(K, nullptr, k_stride, nullptr, cache->kv_heads, rot > 0, true);
@@ -296,5 +305,5 @@ extern "C" int mate_cache_append(const mate_cache_t *cache, int layer, const voi
     p.paged = 1;
     p.cache = cache_args(cache, layer);
     p.seqs = seqs, p.counts = counts, p.row_ids = row_ids, p.col_ids = col_ids;
-    return run(p, cache->dtype, (cudaStream_t)stream);
+    return run(p, cache->dtype, cache->device, (cudaStream_t)stream);
 }
