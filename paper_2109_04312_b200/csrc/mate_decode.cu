@@ -4,7 +4,7 @@
 //
 // Bound by memory: a key and a value are read once for the whole group (4 d bytes in bf16 for 4 d flops per head), the ids of all
 // cached tokens (4 or 8 bytes each, mostly from L2: the kv heads share them) decide which.  Hence
-//   - a warp works alone: it looks through 32 tokens at a time (page, ids; the next 32 are on their way meanwhile), puts the
+//   - a warp works alone: it looks through 128 tokens at a time (page, ids; the next ones' are on their way meanwhile), puts the
 //     places of those that count into a list, and copies 16 bytes per lane and instruction from there into its own ring of stages
 //     of 8 KB, with kRing - 1 stages under way; no block barrier until the sequence's part is done.  What nobody attends is never
 //     read, padding's keys and values included.
@@ -23,14 +23,20 @@ namespace mate {
 namespace {
 
 constexpr int kWarps = 4, kThreads = 32 * kWarps;
-constexpr int kUnit = 32 * kWarps;       // tokens of a unit: what the warps look through in one go
+constexpr int kUnit = 128;               // tokens of a unit of work
+constexpr int kLook = 4;                 // tokens of a lane that are looked at together
 constexpr int kStage = 8192;             // bytes of a stage: keys, then values
 constexpr int kRing = 3;                 // stages of a warp
-constexpr int kList = 64;                // entries of a warp's list of places
+constexpr int kList = 256;               // entries of a warp's list of places: less than a stage, and one look
 constexpr int kBlocksPerSm = 2;
-constexpr int kJoinThreads = 256;
+constexpr int kJoinThreads = 128;
 constexpr int kMaxHeads = 1024;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+// An item that a block begins and others go on with: results [slot] of the block, then [0] of the next ones up to `last`.
+struct Joint {
+    int32_t b, item, slot, last;  // last < 0: there is none
+};
 
 struct DecodeParams {
     CacheArgs cache;
@@ -41,9 +47,14 @@ struct DecodeParams {
     float scale_log2;  // scale / ln 2: weights are powers of two
     void *O;
     float *LSE;
-    float *partial;    // [grid][2][rows of a block][d + 2]; null: a block per sequence, kv head and block of the group
+    unsigned page_mul, page_shift;  // x / page_size = (umulhi(x, page_mul) + x) >> page_shift for x < 2^31
+    Joint *joints;  // [grid]; null: a block per sequence, kv head and block of the group
+    float *partial;        // [grid][2][rows of a block][d + 2]
     uint32_t views[kMaxHeads / 16];  // two bits a head
 };
+__device__ __forceinline__ int page_index(const DecodeParams &p, int token) {
+    return (int)((__umulhi((unsigned)token, p.page_mul) + (unsigned)token) >> p.page_shift);
+}
 __device__ __forceinline__ int view_at(const DecodeParams &p, int h) { return p.views[h >> 4] >> 2 * (h & 15) & 3; }
 
 // ---- types
@@ -110,15 +121,14 @@ __device__ __forceinline__ int entry_len(const DecodeParams &p, int b, bool *bad
 
 struct Start {
     int64_t total, before;  // units of the batch; of the entries in front of `entry`
-    int entry;
+    int entry, blocks;      // blocks that get any: no more than there are units
 };
-// All threads call it: the entry that unit `at` belongs to (fixed < 0), or the units in front of entry `fixed`.
-template <int kN>
-__device__ Start find_start(const DecodeParams &p, int items, int fixed, int block, int blocks) {
-    __shared__ int64_t s_sum[kN / 32];
+// All threads call it: the entry that the block's first unit belongs to.
+__device__ Start find_start(const DecodeParams &p, int items) {
+    __shared__ int64_t s_sum[kWarps];
     __shared__ Start s_start;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int per = (p.B + kN - 1) / kN, b0 = min(p.B, tid * per), b1 = min(p.B, b0 + per);
+    const int per = (p.B + kThreads - 1) / kThreads, b0 = min(p.B, tid * per), b1 = min(p.B, b0 + per);
     bool bad = false;
     int64_t own = 0;
     for (int b = b0; b < b1; ++b) own += units_of(entry_len(p, b, &bad));
@@ -133,21 +143,22 @@ __device__ Start find_start(const DecodeParams &p, int items, int fixed, int blo
     __syncthreads();
     int64_t total = 0, before = sum - own;
 #pragma unroll
-    for (int w = 0; w < kN / 32; ++w) {
+    for (int w = 0; w < kWarps; ++w) {
         if (w < warp) before += s_sum[w];
         total += s_sum[w];
     }
-    const int64_t at = share(total, blocks, block);
-    if (b0 < b1 && (fixed < 0 ? at >= before && at < before + own : fixed >= b0 && fixed < b1)) {
+    const int blocks = (int)min(total, (int64_t)gridDim.x);
+    const int64_t at = share(total, blocks, min((int)blockIdx.x, blocks - 1));
+    if (at >= before && at < before + own) {
         int b = b0;
         for (; b < b1 - 1; ++b) {
             const int64_t n = (int64_t)units_of(entry_len(p, b, &bad)) * items;
-            if (fixed < 0 ? at < before + n : b == fixed) break;
+            if (at < before + n) break;
             before += n;
         }
-        s_start = {total, before, b};
+        s_start = {total, before, b, blocks};
     }
-    if (bad && block == 0) atomicOr(p.cache.status, kCacheBad);
+    if (bad && blockIdx.x == 0) atomicOr(p.cache.status, kCacheBad);
     __syncthreads();
     return s_start;
 }
@@ -179,16 +190,18 @@ __device__ __forceinline__ bool next_part(const DecodeParams &p, int items, Walk
 // ---- the loading side of a warp
 
 struct Meta {  // of a stage
-    int n, end;           // keys; the last stage of a part
+    int n, end;  // keys; the last stage of a part
     uint32_t by_row, by_col;
-    int b, item, whole, more;  // the part; whether there is one (behind the last one: no)
+    int b, item, state, units;  // the part
 };
+enum { kNoPart = 0, kWhole = 1, kBegins = 2, kGoesOn = 3 };  // Meta.state: behind the last one; an item; its first units; others
 
 template <typename T, int DP, int NB>
 struct Loader {
     using S = Shape<T, DP, NB>;
     const DecodeParams &p;
-    int64_t *list;
+    uint32_t *list;  // places, in 16 bytes from the cache's beginning
+    uint8_t *marks;  // 1: attended by row, 2: by column
     Meta *meta;
     uint32_t ring;
     int lane, warp, items;
@@ -196,30 +209,32 @@ struct Loader {
     // the present part
     Part part;
     bool active;
-    int s, prefix, q_row, q_col, first, end;  // tokens [first, end) of the warp, in steps of kUnit
+    int s, prefix, q_row, q_col, end;    // tokens up to `end` are the warp's
     int64_t head_at;
     bool text, need_row, need_col;
-    int next;                            // first of the 32 tokens that are looked at next
-    int page, page2, slot, row, col;     // of the lane's token there: its ids have been asked for; page2: of the one a step on
-    bool there;
+    int next;                            // first of the tokens that are looked at next
+    int page[kLook], row[kLook], col[kLook];  // of the lane's tokens there (page -1: there is none): their ids have been asked for
     bool bad;
     int pending, list_at, filled;        // list; stages so far
 
-    __device__ void look_page(int j, int &pg) {
-        pg = -1;
-        if (j < end) {
-            pg = p.cache.table[(size_t)s * p.cache.width + j / p.cache.page_size];
-            if (!in_range(pg, p.cache.pages)) bad = true, pg = -1;
+    __device__ void ask() {
+#pragma unroll
+        for (int i = 0; i < kLook; ++i) {
+            const int j = next + 32 * i + lane;
+            page[i] = -1;
+            if (j < end) {
+                page[i] = p.cache.table[(size_t)s * p.cache.width + page_index(p, j)];
+                if (!in_range(page[i], p.cache.pages)) bad = true, page[i] = -1;
+            }
         }
-    }
-    __device__ void look_ids(int j) {
-        there = j < end && page >= 0;
-        if (there) {
-            slot = j % p.cache.page_size;
-            const size_t at = (size_t)page * p.cache.page_size + slot;
-            if (need_row || text) row = p.cache.row_ids[at];
-            if (need_col && !text) col = p.cache.col_ids[at];
-        }
+#pragma unroll
+        for (int i = 0; i < kLook; ++i)
+            if (page[i] >= 0) {
+                const int j = next + 32 * i + lane;
+                const int64_t at = (int64_t)page[i] * p.cache.page_size + (j - page_index(p, j) * p.cache.page_size);
+                if (need_row) row[i] = p.cache.row_ids[at];
+                if (need_col) col[i] = p.cache.col_ids[at];
+            }
     }
     __device__ void begin() {
         int len;
@@ -239,28 +254,33 @@ struct Loader {
             need_row |= v != MATE_VIEW_COL;
             need_col |= v != MATE_VIEW_ROW;
         }
-        next = part.u0 * kUnit + warp * 32;
-        end = min(len, part.u1 * kUnit);
-        look_page(next + lane, page);
-        look_ids(next + lane);
-        look_page(next + kUnit + lane, page2);
+        if (text) need_row = true, need_col = false;  // padding has neither
+        // the part's tokens in four, in whole 32
+        const int t0 = part.u0 * kUnit, t1 = min(len, part.u1 * kUnit), quarter = ((t1 - t0 + kWarps - 1) / kWarps + 31) & ~31;
+        next = t0 + warp * quarter;
+        end = min(t1, next + quarter);
+        ask();
     }
-    // One look at 32 tokens: those that count go onto the list, the next ones' ids are asked for.
+    // One look at 32 kLook tokens: those that count go onto the list, the next ones' ids are asked for.
     __device__ void look() {
-        const int j = next + lane;
-        const bool all = text || j < prefix;
-        const bool by_row = there && (need_row || text) && row >= 0 && (all || row == MATE_ID_TEXT || row == q_row);
-        const bool by_col = text ? by_row : there && need_col && col >= 0 && (all || col == MATE_ID_TEXT || col == q_col);
-        const unsigned counts = __ballot_sync(~0u, by_row || by_col);
-        if (by_row || by_col) {
-            const int64_t at = (page * p.cache.page_stride + slot * p.cache.slot_stride + head_at) * (int64_t)sizeof(T);
-            list[(list_at + pending + __popc(counts & ((1u << lane) - 1))) & (kList - 1)] = at | (by_row ? 1 : 0) | (by_col ? 2 : 0);
+#pragma unroll
+        for (int i = 0; i < kLook; ++i) {
+            const int j = next + 32 * i + lane;
+            const bool there = page[i] >= 0, all = text || j < prefix;
+            const bool by_row = there && need_row && row[i] >= 0 && (all || row[i] == MATE_ID_TEXT || row[i] == q_row);
+            const bool by_col = text ? by_row : there && need_col && col[i] >= 0 && (all || col[i] == MATE_ID_TEXT || col[i] == q_col);
+            const unsigned counts = __ballot_sync(~0u, by_row || by_col);
+            if (by_row || by_col) {
+                const int slot = j - page_index(p, j) * p.cache.page_size;
+                const int64_t at = page[i] * p.cache.page_stride + slot * p.cache.slot_stride + head_at;
+                const int to = (list_at + pending + __popc(counts & ((1u << lane) - 1))) & (kList - 1);
+                list[to] = (uint32_t)(at / (16 / (int)sizeof(T)));
+                marks[to] = (by_row ? 1 : 0) | (by_col ? 2 : 0);
+            }
+            pending += __popc(counts);
         }
-        pending += __popc(counts);
-        next += kUnit;
-        page = page2;
-        look_ids(next + lane);
-        look_page(next + kUnit + lane, page2);
+        next += 32 * kLook;
+        if (next < end) ask();
     }
     // Copies of the next stage are put under way (or, at the end of the share, none: the groups are counted).
     __device__ void fill() {
@@ -269,9 +289,9 @@ struct Loader {
             __syncwarp();
             const int n = min(pending, S::kKeys), slot_of_ring = filled % kRing;
             const bool last = pending <= S::kKeys && next >= end;
-            const int64_t mine = lane < n ? list[(list_at + lane) & (kList - 1)] : 0;
+            const int mine = lane < n ? marks[(list_at + lane) & (kList - 1)] : 0;
             const uint32_t by_row = __ballot_sync(~0u, mine & 1), by_col = __ballot_sync(~0u, mine & 2);
-            if (lane == 0) meta[slot_of_ring] = {n, last, by_row, by_col, part.b, part.item, part.whole, 1};
+            if (lane == 0) meta[slot_of_ring] = {n, last, by_row, by_col, part.b, part.item, part.whole ? kWhole : part.u0 == 0 ? kBegins : kGoesOn, part.u1 - part.u0};
             const uint32_t to = ring + slot_of_ring * kStage;
             constexpr int kPerPass = 32 / S::kChunks > 0 ? 32 / S::kChunks : 1;  // keys of a pass (rows have 8, 16 or 32 chunks)
             const int chunk = lane % S::kChunks, chunks = p.d * (int)sizeof(T) / 16;
@@ -280,7 +300,7 @@ struct Loader {
                 for (int i = 0; i < S::kKeys / kPerPass; ++i) {
                     const int key = i * kPerPass + lane / S::kChunks;
                     const bool there_is = key < n;
-                    const int64_t at = there_is ? (list[(list_at + key) & (kList - 1)] & ~(int64_t)15) + chunk * 16 : 0;
+                    const int64_t at = there_is ? ((int64_t)list[(list_at + key) & (kList - 1)] + chunk) * 16 : 0;
                     const uint32_t dst = to + S::chunk_at(key, chunk);
                     cp_async16_or_zero(dst, (const char *)p.cache.k + at, there_is);
                     cp_async16_or_zero(dst + kStage / 2, (const char *)p.cache.v + at, there_is);
@@ -291,7 +311,7 @@ struct Loader {
             __syncwarp();  // the list has been read
             if (last) begin();
         } else if (lane == 0) {
-            meta[filled % kRing] = {0, 1, 0u, 0u, 0, 0, 0, 0};
+            meta[filled % kRing] = {0, 1, 0u, 0u, 0, 0, kNoPart, 0};
         }
         ++filled;
         cp_async_commit();
@@ -445,10 +465,11 @@ struct Reader<float, DP, NB> {
     static constexpr int kShare = 32 / S::kKeys;  // lanes that share a key
     static constexpr int kCols = DP / 32;         // columns of a lane
     float m[S::kRows], l[S::kRows], o[S::kRows][kCols];
-    int n;
+    int n, warp;
 
-    // `own`: the warp's queries [kRows][DP], then weights [kRows][kKeys]
+    // `own`: queries [kRows][DP] (of the block; every warp writes the same), then the warp's weights [kRows][kKeys] each
     __device__ void begin(const DecodeParams &p, int b, int h0, int n_rows, int lane, float *own) {
+        warp = threadIdx.x >> 5;
         const float *Q = (const float *)p.Q + b * p.q_batch;
         n = n_rows;
         __syncwarp();
@@ -469,7 +490,7 @@ struct Reader<float, DP, NB> {
     uint32_t views;
     __device__ void add(const DecodeParams &p, uint32_t stage, const Meta &meta, int lane, float *own) {
         const int key = lane / kShare, part = lane % kShare;
-        float *weights = own + S::kRows * DP;
+        float *weights = own + S::kRows * (DP + warp * S::kKeys);
         float s[S::kRows];
 #pragma unroll
         for (int r = 0; r < S::kRows; ++r) s[r] = 0.f;
@@ -545,34 +566,38 @@ struct Reader<float, DP, NB> {
 __device__ __forceinline__ void put(float x, float *y) { *y = x; }
 __device__ __forceinline__ void put(float x, __nv_bfloat16 *y) { *y = __float2bfloat16_rn(x); }
 
-// Floats of shared memory behind the ring: results of the warps, their maxima and sums; fp32: a warp's queries and weights.
+// Bytes of shared memory behind the ring: fp32's queries and weights.
 template <typename T, int DP, int NB>
-__host__ __device__ constexpr int extra_floats(int rows, int d) {
-    return kWarps * rows * (d + 2) + (sizeof(T) == 4 ? kWarps * Shape<T, DP, NB>::kRows * (DP + Shape<T, DP, NB>::kKeys) : 0);
-}
+constexpr int kExtra = sizeof(T) == 4 ? 4 * Shape<T, DP, NB>::kRows * (DP + kWarps * Shape<T, DP, NB>::kKeys) : 0;
 
 template <typename T, int DP, int NB>
 __global__ void __launch_bounds__(kThreads, kBlocksPerSm) decode_kernel(const __grid_constant__ DecodeParams p) {
     using S = Shape<T, DP, NB>;
     extern __shared__ __align__(128) char smem[];
-    __shared__ int64_t s_list[kWarps][kList];
+    __shared__ uint32_t s_list[kWarps][kList];
+    __shared__ uint8_t s_marks[kWarps][kList];
     __shared__ Meta s_meta[kWarps][kRing];
+    __shared__ float s_stats[kWarps][2 * S::kRows];
+    __shared__ int s_out_at[kWarps];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, items = p.kv_heads * p.blocks_of_group;
     const int max_rows = min(S::kRows, p.group);
-    float *own = reinterpret_cast<float *>(smem + kWarps * kRing * kStage) + (sizeof(T) == 4 ? warp * S::kRows * (DP + S::kKeys) : 0);
-    float *s_out = reinterpret_cast<float *>(smem + kWarps * kRing * kStage) + (sizeof(T) == 4 ? kWarps * S::kRows * (DP + S::kKeys) : 0);
-    float *s_stats = s_out + kWarps * max_rows * p.d;
+    float *own = reinterpret_cast<float *>(smem + kWarps * kRing * kStage);
     ptx::launch_dependents();
     if (p.d < DP)  // columns that no copy writes
         for (int i = tid; i < kWarps * kRing * kStage / 16; i += kThreads) reinterpret_cast<uint4 *>(smem)[i] = make_uint4(0, 0, 0, 0);
     ptx::wait_prior_grid();
 
     Walk walk;
-    if (p.partial) {
-        const Start start = find_start<kThreads>(p, items, -1, blockIdx.x, gridDim.x);
-        const int64_t at = share(start.total, gridDim.x, blockIdx.x);
-        walk.left = share(start.total, gridDim.x, blockIdx.x + 1) - at;
-        if (walk.left == 0) return;
+    Start start = {};
+    if (p.joints) {
+        start = find_start(p, items);
+        if (blockIdx.x >= start.blocks) {
+            if (tid == 0) p.joints[blockIdx.x].last = -1;
+            return;
+        }
+        if (tid == 0) p.joints[blockIdx.x].last = -1;
+        const int64_t at = share(start.total, start.blocks, blockIdx.x);
+        walk.left = share(start.total, start.blocks, blockIdx.x + 1) - at;
         bool bad = false;
         const int n = units_of(entry_len(p, start.entry, &bad));
         walk.b = start.entry;
@@ -586,7 +611,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) decode_kernel(const __
         __syncthreads();
     }
 
-    Loader<T, DP, NB> load = {p, s_list[warp], s_meta[warp], ptx::smem_u32(smem) + warp * kRing * kStage, lane, warp, items, walk};
+    Loader<T, DP, NB> load = {p, s_list[warp], s_marks[warp], s_meta[warp], ptx::smem_u32(smem) + warp * kRing * kStage, lane, warp, items, walk};
     load.bad = false, load.pending = load.list_at = load.filled = 0;
     load.begin();
     for (int i = 0; i < kRing - 1; ++i) load.fill();
@@ -597,7 +622,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) decode_kernel(const __
     bool first = true;
     for (int t = 0;;) {
         Meta meta = s_meta[warp][t % kRing];
-        if (!meta.more) break;
+        if (meta.state == kNoPart) break;
         const Meta part = meta;
         const int kv = part.item / p.blocks_of_group, block = part.item - kv * p.blocks_of_group;
         const int h0 = kv * p.group + block * S::kRows, n_rows = min(S::kRows, p.group - block * S::kRows);
@@ -611,24 +636,34 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) decode_kernel(const __
             more = !meta.end;
         }
         __syncwarp();
-        read.store(s_out + warp * max_rows * p.d, s_stats + warp * max_rows * 2, n_rows, p.d, lane);
+        // the warp's result goes into the stage that was read last, which the next fill() is the first to write
+        static_assert(S::kRows * DP * 4 <= kStage, "a warp's result fits a stage");
+        const int out_at = (t - 1) % kRing * kStage;
+        read.store(reinterpret_cast<float *>(smem + warp * kRing * kStage + out_at), s_stats[warp], n_rows, p.d, lane);
+        if (lane == 0) s_out_at[warp] = warp * kRing * kStage + out_at;
         __syncthreads();
         // the warps' results together: the whole item's, or a partial one
-        float *to = p.partial + (size_t)(2 * blockIdx.x + (first ? 0 : 1)) * max_rows * (p.d + 2);
+        const int slot = first ? 0 : 1;
+        float *to = p.partial + (size_t)(2 * blockIdx.x + slot) * max_rows * (p.d + 2);
+        if (part.state == kBegins && tid == 0) {  // the share's last part: who has the item's last unit?
+            bool bad = false;
+            const int64_t end = share(start.total, start.blocks, blockIdx.x + 1) - part.units + units_of(entry_len(p, part.b, &bad));
+            p.joints[blockIdx.x] = {part.b, part.item, slot, (int)min((end * start.blocks - 1) / start.total, (int64_t)start.blocks - 1)};
+        }
         for (int i = tid; i < n_rows * p.d; i += kThreads) {
             const int r = i / p.d, e = i - r * p.d;
             float top = -INFINITY;
 #pragma unroll
-            for (int w = 0; w < kWarps; ++w) top = fmaxf(top, s_stats[(w * max_rows + r) * 2]);
+            for (int w = 0; w < kWarps; ++w) top = fmaxf(top, s_stats[w][2 * r]);
             const float base = top == -INFINITY ? 0.f : top;
             float sum = 0.f, x = 0.f;
 #pragma unroll
             for (int w = 0; w < kWarps; ++w) {
-                const float f = ptx::ex2(s_stats[(w * max_rows + r) * 2] - base);
-                sum = fmaf(f, s_stats[(w * max_rows + r) * 2 + 1], sum);
-                x = fmaf(f, s_out[(w * max_rows + r) * p.d + e], x);
+                const float f = ptx::ex2(s_stats[w][2 * r] - base);
+                sum = fmaf(f, s_stats[w][2 * r + 1], sum);
+                x = fmaf(f, *reinterpret_cast<const float *>(smem + s_out_at[w] + 4 * i), x);
             }
-            if (part.whole) {
+            if (part.state == kWhole) {
                 const size_t row = (size_t)part.b * p.heads + h0 + r;
                 put(sum == 0.f ? 0.f : x / sum, (T *)p.O + row * p.d + e);
                 if (e == 0) p.LSE[row] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
@@ -638,82 +673,68 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) decode_kernel(const __
             }
         }
         __syncthreads();
+        if (p.d < DP)
+            for (int i = lane; i < kStage / 16; i += 32) reinterpret_cast<uint4 *>(smem + warp * kRing * kStage + out_at)[i] = make_uint4(0, 0, 0, 0);
         first = false;
     }
     cp_async_wait<0>();
     if (load.bad) atomicOr(p.cache.status, kCacheBad);
 }
 
-// Joins the partial results of an item that fell to several blocks of the kernel before.  grid: (entry, item)
+// Joins the partial results of an item that fell to several blocks of the kernel before.  grid: (block that began it, row)
 template <typename T>
-__global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ DecodeParams p, int blocks, int block_rows) {
-    extern __shared__ float s_join[];  // weights [rows][parts], then sums [groups][rows][d]
+__global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ DecodeParams p, int block_rows) {
+    extern __shared__ float s_weight[];  // of every part
+    __shared__ float s_red[2][kJoinThreads / 32], s_sum[2 * kJoinThreads];
     ptx::launch_dependents();
     ptx::wait_prior_grid();
-    const int tid = threadIdx.x, items = p.kv_heads * p.blocks_of_group, b = blockIdx.x, item = blockIdx.y;
-    const Start start = find_start<kJoinThreads>(p, items, b, 1, blocks);
-    bool bad = false;
-    const int n = units_of(entry_len(p, b, &bad));
-    const int64_t U = start.total, s = start.before + (int64_t)item * n, e = s + n;
-    // block i has unit x: the largest i with i U / blocks <= x
-    const int i0 = (int)(((s + 1) * blocks - 1) / U), i1 = (int)((e * blocks - 1) / U);
-    if (i0 == i1) return;
-    const int kv = item / p.blocks_of_group, part = item - kv * p.blocks_of_group, max_rows = min(block_rows, p.group);
-    const int h0 = kv * p.group + part * block_rows, rows = min(block_rows, p.group - part * block_rows), width = p.d + 2, parts = i1 - i0 + 1;
-    // (a block without units has no result; an item's first part in a block that has begun another one before is its second)
-    auto result = [&](int i) -> const float * {
-        const int64_t lo = share(U, blocks, i);
-        if (lo == share(U, blocks, i + 1)) return nullptr;
-        return p.partial + (size_t)(2 * i + (s <= lo ? 0 : 1)) * max_rows * width;
-    };
-    float *s_w = s_join, *s_sum = s_join + rows * parts;
-    for (int r = tid >> 5; r < rows; r += kJoinThreads / 32) {
-        const int lane = tid & 31;
-        float top = -INFINITY;
-        for (int i = lane; i < parts; i += 32)
-            if (const float *x = result(i0 + i)) top = fmaxf(top, x[r * width]);
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, r = blockIdx.y, width = p.d + 2;
+    const Joint joint = p.joints[blockIdx.x];
+    const int kv = joint.item / p.blocks_of_group, part = joint.item - kv * p.blocks_of_group, max_rows = min(block_rows, p.group);
+    const int parts = joint.last - (int)blockIdx.x + 1;
+    if (joint.last < 0 || parts <= 1 || r >= p.group - part * block_rows) return;
+    auto result = [&](int i) { return p.partial + ((size_t)(2 * (blockIdx.x + i) + (i == 0 ? joint.slot : 0)) * max_rows + r) * width; };
+    float top = -INFINITY;
+    for (int i = tid; i < parts; i += kJoinThreads) top = fmaxf(top, s_weight[i] = *result(i));
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
-        const float base = top == -INFINITY ? 0.f : top;
-        float sum = 0.f;
-        for (int i = lane; i < parts; i += 32) {
-            const float *x = result(i0 + i);
-            const float w = x ? ptx::ex2(x[r * width] - base) : 0.f;
-            s_w[r * parts + i] = w;
-            if (x) sum = fmaf(w, x[r * width + 1], sum);
-        }
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
-        const float inverse = sum == 0.f ? 0.f : 1.f / sum;
-        for (int i = lane; i < parts; i += 32) s_w[r * parts + i] *= inverse;
-        if (lane == 0) p.LSE[(size_t)b * p.heads + h0 + r] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
-    }
+    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
+    if (lane == 0) s_red[0][warp] = top;
     __syncthreads();
-    // pairs of columns, and for few of them several groups of threads that take the parts in turn
-    const int pairs = rows * p.d / 2, groups = max(1, kJoinThreads / pairs), group = tid / pairs;
-    for (int c = groups > 1 ? tid % pairs : tid; c < pairs && group < groups; c += groups > 1 ? pairs : kJoinThreads) {
-        const int r = c / (p.d / 2), at = r * width + 2 + 2 * (c - r * (p.d / 2));
-        float x = 0.f, y = 0.f;
+#pragma unroll
+    for (int w = 0; w < kJoinThreads / 32; ++w) top = fmaxf(top, s_red[0][w]);
+    const float base = top == -INFINITY ? 0.f : top;
+    float sum = 0.f;
+    for (int i = tid; i < parts; i += kJoinThreads) {
+        const float w = ptx::ex2(s_weight[i] - base);
+        s_weight[i] = w;
+        sum = fmaf(w, result(i)[1], sum);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
+    if (lane == 0) s_red[1][warp] = sum;
+    __syncthreads();
+    sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < kJoinThreads / 32; ++w) sum += s_red[1][w];
+    // pairs of columns; groups of threads take the parts in turn
+    const int pairs = p.d / 2, groups = kJoinThreads / pairs, group = tid / pairs, c = tid - group * pairs;
+    float x = 0.f, y = 0.f;
+    if (group < groups) {
 #pragma unroll 4
-        for (int i = groups > 1 ? group : 0; i < parts; i += groups)
-            if (const float *z = result(i0 + i)) {
-                const float2 v = *reinterpret_cast<const float2 *>(z + at);
-                x = fmaf(s_w[r * parts + i], v.x, x), y = fmaf(s_w[r * parts + i], v.y, y);
-            }
-        if (groups == 1) {
-            T *to = (T *)p.O + ((size_t)b * p.heads + h0) * p.d + 2 * c;
-            put(x, to), put(y, to + 1);
-            continue;
+        for (int i = group; i < parts; i += groups) {
+            const float2 v = *reinterpret_cast<const float2 *>(result(i) + 2 + 2 * c);
+            x = fmaf(s_weight[i], v.x, x), y = fmaf(s_weight[i], v.y, y);
         }
-        s_sum[(group * pairs + c) * 2] = x, s_sum[(group * pairs + c) * 2 + 1] = y;
+        s_sum[2 * tid] = x, s_sum[2 * tid + 1] = y;
     }
-    if (groups == 1) return;
     __syncthreads();
-    for (int c = tid; c < 2 * pairs; c += kJoinThreads) {
-        float x = 0.f;
-        for (int g = 0; g < groups; ++g) x += s_sum[g * pairs * 2 + c];
-        put(x, (T *)p.O + ((size_t)b * p.heads + h0) * p.d + c);
+    const size_t row = (size_t)joint.b * p.heads + kv * p.group + part * block_rows + r;
+    if (tid < p.d) {
+        float z = 0.f;
+        for (int g = 0; g < groups; ++g) z += s_sum[g * p.d + tid];
+        put(sum == 0.f ? 0.f : z / sum, (T *)p.O + row * p.d + tid);
     }
+    if (tid == 0) p.LSE[row] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
 }
 
 // ---- host
@@ -729,22 +750,19 @@ int shares(const mate_cache_t *c, int B, int max_len) {
 
 template <typename T, int DP, int NB>
 int launch(const DecodeParams &p, int blocks, int device, cudaStream_t st) {
-    static SmemAttrOnce attr, join_attr;
+    static SmemAttrOnce attr;
     using S = Shape<T, DP, NB>;
     const int rows = S::kRows < p.group ? S::kRows : p.group;
-    constexpr int kMostSmem = kWarps * kRing * kStage + 4 * extra_floats<T, DP, NB>(S::kRows, DP);
-    const int smem = kWarps * kRing * kStage + 4 * extra_floats<T, DP, NB>(rows, p.d);
-    int rc = attr.ensure((const void *)decode_kernel<T, DP, NB>, kMostSmem, device);
+    constexpr int kSmem = kWarps * kRing * kStage + kExtra<T, DP, NB>;
+    int rc = attr.ensure((const void *)decode_kernel<T, DP, NB>, kSmem, device);
     if (rc != MATE_OK) return rc;
     const int64_t items = (int64_t)p.kv_heads * p.blocks_of_group, grid = blocks ? blocks : p.B * items;
     if (grid > INT32_MAX) return MATE_ERR_UNSUPPORTED;
-    if (launch_after(decode_kernel<T, DP, NB>, dim3((unsigned)grid), kThreads, (size_t)smem, st, p) != cudaSuccess) return MATE_ERR_CUDA;
+    if (launch_after(decode_kernel<T, DP, NB>, dim3((unsigned)grid), kThreads, kSmem, st, p) != cudaSuccess) return MATE_ERR_CUDA;
     if (!blocks) return MATE_OK;
-    const size_t join = sizeof(float) * ((size_t)rows * blocks + 2 * kJoinThreads);
-    rc = join_attr.ensure((const void *)join_kernel<T>, 100 * 1024, device);
-    if (rc != MATE_OK) return rc;
-    return launch_after(join_kernel<T>, dim3((unsigned)p.B, (unsigned)items), kJoinThreads, join, st, p, blocks, S::kRows) == cudaSuccess ? MATE_OK
-                                                                                                                                  : MATE_ERR_CUDA;
+    return launch_after(join_kernel<T>, dim3((unsigned)blocks, (unsigned)rows), kJoinThreads, sizeof(float) * blocks, st, p, S::kRows) == cudaSuccess
+               ? MATE_OK
+               : MATE_ERR_CUDA;
 }
 
 }  // namespace
@@ -752,7 +770,7 @@ int launch(const DecodeParams &p, int blocks, int device, cudaStream_t st) {
 size_t decode_workspace(const mate_cache_t *c, int B) {
     const int blocks = B > 0 ? shares(c, B, c->width * c->page_size) : 0;
     const int group = c->heads / c->kv_heads, rows = block_rows(c) < group ? block_rows(c) : group;
-    return sizeof(float) * 2 * (size_t)blocks * rows * (c->d + 2);
+    return (sizeof(Joint) + sizeof(float) * 2 * rows * (c->d + 2)) * (size_t)blocks;
 }
 
 }  // namespace mate
@@ -765,7 +783,8 @@ extern "C" int mate_attn_decode(const mate_cache_t *cache, int layer, const void
     if (rc != MATE_OK) return rc;
     if (layer < 0 || layer >= cache->layers || B < 0 || max_len < 0 || (!seqs && B > cache->seqs)) return MATE_ERR_INVALID_ARG;
     if (B > 0 && (!Q || !q_stride || !row_ids || !col_ids || !O || !LSE)) return MATE_ERR_INVALID_ARG;
-    if (cache->heads > kMaxHeads) return MATE_ERR_UNSUPPORTED;
+    const int64_t reach = (cache->pages - 1) * cache->page_stride + (cache->kv_heads - 1) * cache->head_stride + (cache->page_size - 1) * cache->slot_stride;
+    if (cache->heads > kMaxHeads || reach / (int64_t)(16 / elem_size(cache->dtype)) > UINT32_MAX) return MATE_ERR_UNSUPPORTED;
     const int vec = (int)(16 / elem_size(cache->dtype));
     if (B > 0 && (!is_aligned(Q, 16) || !is_aligned(O, 16) || !is_aligned(LSE, 4) || q_stride[0] % vec != 0 || q_stride[1] % vec != 0))
         return MATE_ERR_ALIGNMENT;
@@ -781,11 +800,14 @@ extern "C" int mate_attn_decode(const mate_cache_t *cache, int layer, const void
     p.seqs = seqs, p.row_ids = row_ids, p.col_ids = col_ids;
     p.scale_log2 = scale * kLog2e, p.O = O, p.LSE = LSE;
     for (int h = 0; h < cache->heads; ++h) p.views[h >> 4] |= (uint32_t)cache->head_view[h] << 2 * (h & 15);
+    for (p.page_shift = 0; 1u << p.page_shift < (unsigned)cache->page_size;) ++p.page_shift;
+    p.page_mul = (unsigned)((((uint64_t)1 << 32) * (((uint64_t)1 << p.page_shift) - cache->page_size)) / cache->page_size + 1);
     const int blocks = shares(cache, B, p.max_len);
     if (blocks) {
         if (!workspace || workspace_bytes < decode_workspace(cache, B)) return MATE_ERR_WORKSPACE;
         if (!is_aligned(workspace, 256)) return MATE_ERR_ALIGNMENT;
-        p.partial = static_cast<float *>(workspace);
+        p.joints = static_cast<Joint *>(workspace);
+        p.partial = reinterpret_cast<float *>(p.joints + blocks);
     }
     cudaStream_t st = (cudaStream_t)stream;
     const bool narrow = cache->d <= 64;
