@@ -26,10 +26,11 @@ constexpr int kWarps = 4, kThreads = 32 * kWarps;
 constexpr int kUnit = 128;               // tokens of a unit of work
 constexpr int kLook = 4;                 // tokens of a lane that are looked at together
 constexpr int kStage = 8192;             // bytes of a stage: keys, then values
-constexpr int kRing = 3;                 // stages of a warp
+constexpr int kAlign = 256;              // of the ring: the longest row of tensor-core operands
+constexpr int kRing = 2;                 // stages of a warp
 constexpr int kList = 256;               // entries of a warp's list of places: less than a stage, and one look
-constexpr int kBlocksPerSm = 2;
-constexpr int kJoinThreads = 128;
+constexpr int kBlocksPerSm = 3;
+constexpr int kJoinThreads = 256;
 constexpr int kMaxHeads = 1024;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
@@ -47,6 +48,7 @@ struct DecodeParams {
     float scale_log2;  // scale / ln 2: weights are powers of two
     void *O;
     float *LSE;
+    unsigned page16, head16, slot16;  // strides in 16 bytes; no place is beyond 2^32 of them
     unsigned page_mul, page_shift;  // x / page_size = (umulhi(x, page_mul) + x) >> page_shift for x < 2^31
     Joint *joints;  // [grid]; null: a block per sequence, kv head and block of the group
     float *partial;        // [grid][2][rows of a block][d + 2]
@@ -105,58 +107,60 @@ __device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], 
 // ---- shares of the work
 
 // An item is one sequence's kv head and block of its group; items of a sequence follow one another.  Its units are numbered through
-// over all items; block i of C gets units [i U / C, (i + 1) U / C).  (Every item has a unit: empty ones are written too.)
-__device__ __forceinline__ int units_of(int len) { return len > kUnit ? (len + kUnit - 1) / kUnit : 1; }
-__device__ __forceinline__ int64_t share(int64_t U, int C, int i) { return U * i / C; }
+// over all items (fewer than 2^31, the host sees to that); block i of C gets units [i U / C, (i + 1) U / C).  (Every item has a unit:
+// empty ones are written too.)
+__host__ __device__ __forceinline__ int units_of(int len) { return len > kUnit ? (len + kUnit - 1) / kUnit : 1; }
+__device__ __forceinline__ unsigned share(unsigned U, unsigned C, unsigned i) { return U / C * i + U % C * i / C; }
 
-// Length that counts of entry b of the batch, 0 where the entry is none.
+// Tokens that entry b of the batch has to look through; none for an entry that is no sequence, or padding.
 __device__ __forceinline__ int entry_len(const DecodeParams &p, int b, bool *bad) {
-    const int s = seq_of(p.seqs, b, p.cache.seqs);
-    if (s < 0) {
+    const int s = p.seqs ? p.seqs[b] : b, q_row = p.row_ids[b], q_col = p.col_ids[b];
+    if (!in_range(s, p.cache.seqs)) {
         *bad = true;
         return 0;
     }
-    return clip_len(p.cache.lens[s], p.max_len, bad);
+    const int len = clip_len(p.cache.lens[s], p.max_len, bad);
+    return q_row < 0 || q_col < 0 ? 0 : len;
 }
 
 struct Start {
-    int64_t total, before;  // units of the batch; of the entries in front of `entry`
-    int entry, blocks;      // blocks that get any: no more than there are units
+    unsigned total, before;  // units of the batch; of the entries in front of `entry`
+    unsigned blocks;         // that get any: no more than there are units
+    int entry;
 };
 // All threads call it: the entry that the block's first unit belongs to.
 __device__ Start find_start(const DecodeParams &p, int items) {
-    __shared__ int64_t s_sum[kWarps];
+    __shared__ unsigned s_sum[kWarps];
     __shared__ Start s_start;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int per = (p.B + kThreads - 1) / kThreads, b0 = min(p.B, tid * per), b1 = min(p.B, b0 + per);
     bool bad = false;
-    int64_t own = 0;
+    unsigned own = 0;
     for (int b = b0; b < b1; ++b) own += units_of(entry_len(p, b, &bad));
     own *= items;
-    int64_t sum = own;
+    unsigned sum = own;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-        const int64_t y = __shfl_up_sync(~0u, sum, o);
+        const unsigned y = __shfl_up_sync(~0u, sum, o);
         if (lane >= o) sum += y;
     }
     if (lane == 31) s_sum[warp] = sum;
     __syncthreads();
-    int64_t total = 0, before = sum - own;
+    unsigned total = 0, before = sum - own;
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) {
         if (w < warp) before += s_sum[w];
         total += s_sum[w];
     }
-    const int blocks = (int)min(total, (int64_t)gridDim.x);
-    const int64_t at = share(total, blocks, min((int)blockIdx.x, blocks - 1));
+    const unsigned blocks = min(total, gridDim.x), at = share(total, blocks, min(blockIdx.x, blocks - 1));
     if (at >= before && at < before + own) {
         int b = b0;
         for (; b < b1 - 1; ++b) {
-            const int64_t n = (int64_t)units_of(entry_len(p, b, &bad)) * items;
+            const unsigned n = units_of(entry_len(p, b, &bad)) * items;
             if (at < before + n) break;
             before += n;
         }
-        s_start = {total, before, b, blocks};
+        s_start = {total, before, blocks, b};
     }
     if (bad && blockIdx.x == 0) atomicOr(p.cache.status, kCacheBad);
     __syncthreads();
@@ -170,8 +174,8 @@ struct Part {
 };
 // Walks the parts of a block's share.  (It comes to an end whatever it finds: every part takes a unit off the share.)
 struct Walk {
-    int b, item, u;       // next unit: of entry b, item, unit u
-    int64_t left;         // units of the share
+    int b, item, u;  // next unit: of entry b, item, unit u
+    int left;        // units of the share
 };
 __device__ __forceinline__ bool next_part(const DecodeParams &p, int items, Walk &w, Part &part, int *len) {
     if (w.left <= 0 || w.b >= p.B) return false;
@@ -179,13 +183,16 @@ __device__ __forceinline__ bool next_part(const DecodeParams &p, int items, Walk
     *len = entry_len(p, w.b, &bad);
     const int n = units_of(*len);
     part.b = w.b, part.item = w.item, part.u0 = w.u;
-    part.u1 = (int)min((int64_t)n, w.u + w.left);
+    part.u1 = min(n, w.u + w.left);
     part.whole = part.u0 == 0 && part.u1 == n;
     w.left -= max(1, part.u1 - part.u0);
     w.u = 0;
     if (++w.item == items) w.item = 0, ++w.b;
     return true;
 }
+
+__device__ __forceinline__ void put(float x, float *y) { *y = x; }
+__device__ __forceinline__ void put(float x, __nv_bfloat16 *y) { *y = __float2bfloat16_rn(x); }
 
 // ---- the loading side of a warp
 
@@ -209,101 +216,130 @@ struct Loader {
     // the present part
     Part part;
     bool active;
-    int s, prefix, q_row, q_col, end;    // tokens up to `end` are the warp's
-    int64_t head_at;
+    int s, prefix, q_row, q_col, end;
+    unsigned head_at;
     bool text, need_row, need_col;
-    int next;                            // first of the tokens that are looked at next
-    int page[kLook], row[kLook], col[kLook];  // of the lane's tokens there (page -1: there is none): their ids have been asked for
+    int next;                           // first of the tokens that are looked at next; 32 of every 32 kWarps are the warp's
+    unsigned at[kLook];                 // places of the lane's tokens there, whose ids have been asked for
+    int row[kLook], col[kLook];
+    unsigned there;                     // a bit for each that exists
     bool bad;
-    int pending, list_at, filled;        // list; stages so far
+    int pending, list_at, filled;       // list (list_at: a multiple of a stage's keys); stages so far
 
     __device__ void ask() {
+        int page[kLook];
+        there = 0;
 #pragma unroll
         for (int i = 0; i < kLook; ++i) {
-            const int j = next + 32 * i + lane;
-            page[i] = -1;
+            const int j = next + 32 * kWarps * i + lane;
             if (j < end) {
                 page[i] = p.cache.table[(size_t)s * p.cache.width + page_index(p, j)];
-                if (!in_range(page[i], p.cache.pages)) bad = true, page[i] = -1;
+                there |= 1u << i;
             }
         }
 #pragma unroll
-        for (int i = 0; i < kLook; ++i)
-            if (page[i] >= 0) {
-                const int j = next + 32 * i + lane;
-                const int64_t at = (int64_t)page[i] * p.cache.page_size + (j - page_index(p, j) * p.cache.page_size);
-                if (need_row) row[i] = p.cache.row_ids[at];
-                if (need_col) col[i] = p.cache.col_ids[at];
+        for (int i = 0; i < kLook; ++i) {
+            if (!(there >> i & 1)) continue;
+            if (!in_range(page[i], p.cache.pages)) {
+                bad = true, there &= ~(1u << i);
+                continue;
             }
+            const int j = next + 32 * kWarps * i + lane, slot = j - page_index(p, j) * p.cache.page_size;
+            const int id = page[i] * p.cache.page_size + slot;
+            if (need_row) row[i] = p.cache.row_ids[id];
+            if (need_col) col[i] = p.cache.col_ids[id];
+            at[i] = (unsigned)page[i] * p.page16 + (unsigned)slot * p.slot16 + head_at;
+        }
     }
     __device__ void begin() {
-        int len;
-        active = next_part(p, items, walk, part, &len);
-        if (!active) return;
-        s = seq_of(p.seqs, part.b, p.cache.seqs);
+        int len, kv, h0, n;
+        for (;;) {
+            active = next_part(p, items, walk, part, &len);
+            if (!active) return;
+            kv = part.item / p.blocks_of_group;
+            const int block = part.item - kv * p.blocks_of_group;
+            h0 = kv * p.group + block * S::kRows, n = min(S::kRows, p.group - block * S::kRows);
+            if (len > 0) break;
+            // an item without tokens is done with here
+            const size_t row = (size_t)part.b * p.heads + h0;
+            if (warp == 0) {
+                for (int i = lane; i < n * p.d; i += 32) put(0.f, (T *)p.O + row * p.d + i);
+                for (int i = lane; i < n; i += 32) p.LSE[row + i] = -INFINITY;
+            }
+        }
+        s = p.seqs ? p.seqs[part.b] : part.b;
         q_row = p.row_ids[part.b], q_col = p.col_ids[part.b];
-        prefix = s >= 0 ? p.cache.prefix[s] : 0;
+        prefix = p.cache.prefix[s];
         text = q_row == MATE_ID_TEXT || q_col == MATE_ID_TEXT;
-        if (q_row < 0 || q_col < 0) len = 0;
-        const int kv = part.item / p.blocks_of_group, block = part.item - kv * p.blocks_of_group;
-        head_at = kv * p.cache.head_stride;
+        head_at = (unsigned)kv * p.head16;
         need_row = need_col = false;
-        const int h0 = kv * p.group + block * S::kRows, n = min(S::kRows, p.group - block * S::kRows);
         for (int i = 0; i < n; ++i) {
             const int v = view_at(p, h0 + i);
             need_row |= v != MATE_VIEW_COL;
             need_col |= v != MATE_VIEW_ROW;
         }
         if (text) need_row = true, need_col = false;  // padding has neither
-        // the part's tokens in four, in whole 32
-        const int t0 = part.u0 * kUnit, t1 = min(len, part.u1 * kUnit), quarter = ((t1 - t0 + kWarps - 1) / kWarps + 31) & ~31;
-        next = t0 + warp * quarter;
-        end = min(t1, next + quarter);
+        next = part.u0 * kUnit + 32 * warp;
+        end = min(len, part.u1 * kUnit);
+        list_at = 0;
         ask();
     }
     // One look at 32 kLook tokens: those that count go onto the list, the next ones' ids are asked for.
     __device__ void look() {
 #pragma unroll
         for (int i = 0; i < kLook; ++i) {
-            const int j = next + 32 * i + lane;
-            const bool there = page[i] >= 0, all = text || j < prefix;
-            const bool by_row = there && need_row && row[i] >= 0 && (all || row[i] == MATE_ID_TEXT || row[i] == q_row);
-            const bool by_col = text ? by_row : there && need_col && col[i] >= 0 && (all || col[i] == MATE_ID_TEXT || col[i] == q_col);
+            const int j = next + 32 * kWarps * i + lane;
+            const bool is = there >> i & 1, all = text || j < prefix;
+            const bool by_row = is && need_row && row[i] >= 0 && (all || row[i] == MATE_ID_TEXT || row[i] == q_row);
+            const bool by_col = is && need_col && col[i] >= 0 && (all || col[i] == MATE_ID_TEXT || col[i] == q_col);
             const unsigned counts = __ballot_sync(~0u, by_row || by_col);
             if (by_row || by_col) {
-                const int slot = j - page_index(p, j) * p.cache.page_size;
-                const int64_t at = page[i] * p.cache.page_stride + slot * p.cache.slot_stride + head_at;
                 const int to = (list_at + pending + __popc(counts & ((1u << lane) - 1))) & (kList - 1);
-                list[to] = (uint32_t)(at / (16 / (int)sizeof(T)));
-                marks[to] = (by_row ? 1 : 0) | (by_col ? 2 : 0);
+                list[to] = at[i];
+                if (need_row && need_col) marks[to] = (by_row ? 1 : 0) | (by_col ? 2 : 0);
             }
             pending += __popc(counts);
         }
-        next += 32 * kLook;
+        next += 32 * kWarps * kLook;
         if (next < end) ask();
     }
     // Copies of the next stage are put under way (or, at the end of the share, none: the groups are counted).
     __device__ void fill() {
+        const int slot = filled % kRing;
         if (active) {
             while (pending < S::kKeys && next < end) look();
             __syncwarp();
-            const int n = min(pending, S::kKeys), slot_of_ring = filled % kRing;
+            const int n = min(pending, S::kKeys);
             const bool last = pending <= S::kKeys && next >= end;
-            const int mine = lane < n ? marks[(list_at + lane) & (kList - 1)] : 0;
-            const uint32_t by_row = __ballot_sync(~0u, mine & 1), by_col = __ballot_sync(~0u, mine & 2);
-            if (lane == 0) meta[slot_of_ring] = {n, last, by_row, by_col, part.b, part.item, part.whole ? kWhole : part.u0 == 0 ? kBegins : kGoesOn, part.u1 - part.u0};
-            const uint32_t to = ring + slot_of_ring * kStage;
-            constexpr int kPerPass = 32 / S::kChunks > 0 ? 32 / S::kChunks : 1;  // keys of a pass (rows have 8, 16 or 32 chunks)
-            const int chunk = lane % S::kChunks, chunks = p.d * (int)sizeof(T) / 16;
-            if (n > 0 && chunk < chunks) {
+            uint32_t by_row = n < 32 ? (1u << n) - 1 : ~0u, by_col = by_row;
+            if (need_row && need_col) {  // heads of both kinds: who attends what
+                const int mine = lane < n ? marks[list_at + lane] : 0;
+                by_row = __ballot_sync(~0u, mine & 1), by_col = __ballot_sync(~0u, mine & 2);
+            }
+            if (lane == 0)
+                meta[slot] = {n, last, by_row, by_col, part.b, part.item, part.whole ? kWhole : part.u0 == 0 ? kBegins : kGoesOn, part.u1 - part.u0};
+            // a lane copies a 16-byte column of eight keys
+            const int chunk = lane % S::kChunks, first = lane / S::kChunks * 8;
+            if (n > 0 && chunk < p.d * (int)sizeof(T) / 16) {
+                const uint4 lo = *reinterpret_cast<const uint4 *>(list + list_at + first), hi = *reinterpret_cast<const uint4 *>(list + list_at + first + 4);
+                const unsigned from[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+                const char *k = (const char *)p.cache.k + chunk * 16, *v = (const char *)p.cache.v + chunk * 16;
+                const uint32_t to = ring + slot * kStage + first * S::kRowBytes;
+                if (n == S::kKeys) {
 #pragma unroll
-                for (int i = 0; i < S::kKeys / kPerPass; ++i) {
-                    const int key = i * kPerPass + lane / S::kChunks;
-                    const bool there_is = key < n;
-                    const int64_t at = there_is ? ((int64_t)list[(list_at + key) & (kList - 1)] + chunk) * 16 : 0;
-                    const uint32_t dst = to + S::chunk_at(key, chunk);
-                    cp_async16_or_zero(dst, (const char *)p.cache.k + at, there_is);
-                    cp_async16_or_zero(dst + kStage / 2, (const char *)p.cache.v + at, there_is);
+                    for (int i = 0; i < 8; ++i) {
+                        const uint32_t dst = to + S::chunk_at(i, chunk);  // (first is a multiple of 8: the swizzle goes by i)
+                        ptx::cp_async16(dst, k + (size_t)from[i] * 16);
+                        ptx::cp_async16(dst + kStage / 2, v + (size_t)from[i] * 16);
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const bool is = first + i < n;
+                        const uint32_t dst = to + S::chunk_at(i, chunk);
+                        cp_async16_or_zero(dst, k + (is ? (size_t)from[i] * 16 : 0), is);
+                        cp_async16_or_zero(dst + kStage / 2, v + (is ? (size_t)from[i] * 16 : 0), is);
+                    }
                 }
             }
             list_at = (list_at + n) & (kList - 1);
@@ -311,7 +347,7 @@ struct Loader {
             __syncwarp();  // the list has been read
             if (last) begin();
         } else if (lane == 0) {
-            meta[filled % kRing] = {0, 1, 0u, 0u, 0, 0, kNoPart, 0};
+            meta[slot] = {0, 1, 0u, 0u, 0, 0, kNoPart, 0};
         }
         ++filled;
         cp_async_commit();
@@ -367,15 +403,20 @@ struct Reader<__nv_bfloat16, DP, NB> {
             for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) s[t][nb][i] = 0.f;
+        // (a stage begins at a multiple of its rows' length, so the swizzled column 2 k + i of a lane is column i's address ^ 32 k)
+        const uint32_t key_at = stage + S::chunk_at(lane & 15, lane >> 4);
+        const uint32_t value_at = stage + kStage / 2 + S::chunk_at((lane & 7) + (lane >> 4) * 8, lane >> 3 & 1);
 #pragma unroll
         for (int k = 0; k < DP / 16; ++k)
 #pragma unroll
             for (int t = 0; t < kTiles; ++t) {
                 uint32_t a[4];
-                ldmatrix4(a, stage + S::chunk_at(t * 16 + (lane & 15), 2 * k + (lane >> 4)));
+                ldmatrix4(a, (key_at ^ 32 * k) + t * 16 * S::kRowBytes);
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb) mma16816(s[t][nb], a, q[k][nb]);
             }
+        constexpr uint32_t kAll = S::kKeys < 32 ? (1u << S::kKeys) - 1 : ~0u;
+        const bool all = (meta.by_row & meta.by_col) == kAll;
         uint32_t w[kTiles][NB][2];
         float keep[NB][2];
         bool moved = false;
@@ -383,16 +424,23 @@ struct Reader<__nv_bfloat16, DP, NB> {
         for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
-                const uint32_t counts = (meta.by_row & rows_of[nb][c]) | (meta.by_col & cols_of[nb][c]);
                 float top = m[nb][c];
 #pragma unroll
                 for (int t = 0; t < kTiles; ++t)
 #pragma unroll
-                    for (int half = 0; half < 2; ++half) {
-                        float &x = s[t][nb][2 * half + c];
-                        x = counts >> (t * 16 + half * 8 + lane / 4) & 1 ? x * p.scale_log2 : -INFINITY;
-                        top = fmaxf(top, x);
-                    }
+                    for (int half = 0; half < 2; ++half) s[t][nb][2 * half + c] *= p.scale_log2;
+                if (!all) {
+                    const uint32_t counts = ((meta.by_row & rows_of[nb][c]) | (meta.by_col & cols_of[nb][c])) >> lane / 4;
+#pragma unroll
+                    for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+                        for (int half = 0; half < 2; ++half)
+                            if (!(counts >> (t * 16 + half * 8) & 1)) s[t][nb][2 * half + c] = -INFINITY;
+                }
+#pragma unroll
+                for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) top = fmaxf(top, s[t][nb][2 * half + c]);
                 top = fmaxf(top, __shfl_xor_sync(~0u, top, 4));
                 top = fmaxf(top, __shfl_xor_sync(~0u, top, 8));
                 top = fmaxf(top, __shfl_xor_sync(~0u, top, 16));
@@ -430,7 +478,7 @@ struct Reader<__nv_bfloat16, DP, NB> {
 #pragma unroll
             for (int t = 0; t < kTiles; ++t) {
                 uint32_t a[4];
-                ldmatrix4_trans(a, stage + kStage / 2 + S::chunk_at(t * 16 + (lane & 7) + (lane >> 4) * 8, 2 * k + (lane >> 3 & 1)));
+                ldmatrix4_trans(a, (value_at ^ 32 * k) + t * 16 * S::kRowBytes);
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb) mma16816(o[k][nb], a, w[t][nb]);
             }
@@ -563,9 +611,6 @@ struct Reader<float, DP, NB> {
     }
 };
 
-__device__ __forceinline__ void put(float x, float *y) { *y = x; }
-__device__ __forceinline__ void put(float x, __nv_bfloat16 *y) { *y = __float2bfloat16_rn(x); }
-
 // Bytes of shared memory behind the ring: fp32's queries and weights.
 template <typename T, int DP, int NB>
 constexpr int kExtra = sizeof(T) == 4 ? 4 * Shape<T, DP, NB>::kRows * (DP + kWarps * Shape<T, DP, NB>::kKeys) : 0;
@@ -573,16 +618,16 @@ constexpr int kExtra = sizeof(T) == 4 ? 4 * Shape<T, DP, NB>::kRows * (DP + kWar
 template <typename T, int DP, int NB>
 __global__ void __launch_bounds__(kThreads, kBlocksPerSm) decode_kernel(const __grid_constant__ DecodeParams p) {
     using S = Shape<T, DP, NB>;
-    extern __shared__ __align__(128) char smem[];
-    __shared__ uint32_t s_list[kWarps][kList];
+    extern __shared__ char smem_raw[];
+    char *smem = smem_raw + (-ptx::smem_u32(smem_raw) & (kAlign - 1));
+    __shared__ __align__(16) uint32_t s_list[kWarps][kList];
     __shared__ uint8_t s_marks[kWarps][kList];
     __shared__ Meta s_meta[kWarps][kRing];
-    __shared__ float s_stats[kWarps][2 * S::kRows];
+    __shared__ __align__(8) float s_stats[kWarps][2 * S::kRows];
     __shared__ int s_out_at[kWarps];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, items = p.kv_heads * p.blocks_of_group;
     const int max_rows = min(S::kRows, p.group);
     float *own = reinterpret_cast<float *>(smem + kWarps * kRing * kStage);
-    ptx::launch_dependents();
     if (p.d < DP)  // columns that no copy writes
         for (int i = tid; i < kWarps * kRing * kStage / 16; i += kThreads) reinterpret_cast<uint4 *>(smem)[i] = make_uint4(0, 0, 0, 0);
     ptx::wait_prior_grid();
@@ -596,13 +641,13 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) decode_kernel(const __
             return;
         }
         if (tid == 0) p.joints[blockIdx.x].last = -1;
-        const int64_t at = share(start.total, start.blocks, blockIdx.x);
-        walk.left = share(start.total, start.blocks, blockIdx.x + 1) - at;
+        const unsigned at = share(start.total, start.blocks, blockIdx.x);
+        walk.left = (int)(share(start.total, start.blocks, blockIdx.x + 1) - at);
         bool bad = false;
-        const int n = units_of(entry_len(p, start.entry, &bad));
+        const unsigned n = units_of(entry_len(p, start.entry, &bad));
         walk.b = start.entry;
         walk.item = min(items - 1, (int)((at - start.before) / n));
-        walk.u = (int)(at - start.before - (int64_t)walk.item * n);
+        walk.u = (int)(at - start.before - walk.item * n);
     } else {
         bool bad = false;
         walk.b = blockIdx.x / items, walk.item = blockIdx.x - walk.b * items, walk.u = 0;
@@ -643,40 +688,47 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) decode_kernel(const __
         if (lane == 0) s_out_at[warp] = warp * kRing * kStage + out_at;
         __syncthreads();
         // the warps' results together: the whole item's, or a partial one
-        const int slot = first ? 0 : 1;
+        const int slot = first ? 0 : 1, e = tid % DP;
         float *to = p.partial + (size_t)(2 * blockIdx.x + slot) * max_rows * (p.d + 2);
-        if (part.state == kBegins && tid == 0) {  // the share's last part: who has the item's last unit?
-            bool bad = false;
-            const int64_t end = share(start.total, start.blocks, blockIdx.x + 1) - part.units + units_of(entry_len(p, part.b, &bad));
-            p.joints[blockIdx.x] = {part.b, part.item, slot, (int)min((end * start.blocks - 1) / start.total, (int64_t)start.blocks - 1)};
-        }
-        for (int i = tid; i < n_rows * p.d; i += kThreads) {
-            const int r = i / p.d, e = i - r * p.d;
-            float top = -INFINITY;
-#pragma unroll
-            for (int w = 0; w < kWarps; ++w) top = fmaxf(top, s_stats[w][2 * r]);
-            const float base = top == -INFINITY ? 0.f : top;
-            float sum = 0.f, x = 0.f;
+#pragma unroll 4
+        for (int r = tid / DP; r < n_rows; r += kThreads / DP) {
+            float2 stat[kWarps];
+            float x[kWarps], top = -INFINITY;
 #pragma unroll
             for (int w = 0; w < kWarps; ++w) {
-                const float f = ptx::ex2(s_stats[w][2 * r] - base);
-                sum = fmaf(f, s_stats[w][2 * r + 1], sum);
-                x = fmaf(f, *reinterpret_cast<const float *>(smem + s_out_at[w] + 4 * i), x);
+                stat[w] = *reinterpret_cast<const float2 *>(&s_stats[w][2 * r]);
+                x[w] = e < p.d ? *reinterpret_cast<const float *>(smem + s_out_at[w] + 4 * (r * p.d + e)) : 0.f;
+                top = fmaxf(top, stat[w].x);
             }
+            const float base = top == -INFINITY ? 0.f : top;
+            float sum = 0.f, y = 0.f;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) {
+                const float f = ptx::ex2(stat[w].x - base);
+                sum = fmaf(f, stat[w].y, sum);
+                y = fmaf(f, x[w], y);
+            }
+            if (e >= p.d) continue;
             if (part.state == kWhole) {
                 const size_t row = (size_t)part.b * p.heads + h0 + r;
-                put(sum == 0.f ? 0.f : x / sum, (T *)p.O + row * p.d + e);
+                put(sum == 0.f ? 0.f : y / sum, (T *)p.O + row * p.d + e);
                 if (e == 0) p.LSE[row] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
             } else {
-                to[r * (p.d + 2) + 2 + e] = x;
-                if (e == 0) to[r * (p.d + 2)] = top, to[r * (p.d + 2) + 1] = sum;
+                to[r * (p.d + 2) + 2 + e] = y;
+                if (e == 0) *reinterpret_cast<float2 *>(to + r * (p.d + 2)) = make_float2(top, sum);
             }
         }
         __syncthreads();
         if (p.d < DP)
             for (int i = lane; i < kStage / 16; i += 32) reinterpret_cast<uint4 *>(smem + warp * kRing * kStage + out_at)[i] = make_uint4(0, 0, 0, 0);
         first = false;
+        if (part.state == kBegins && tid == 0) {  // the share's last part: who has the item's last unit?
+            bool bad = false;
+            const int64_t end = (int64_t)share(start.total, start.blocks, blockIdx.x + 1) - part.units + units_of(entry_len(p, part.b, &bad));
+            p.joints[blockIdx.x] = {part.b, part.item, slot, (int)min((end * start.blocks - 1) / start.total, (int64_t)start.blocks - 1)};
+        }
     }
+    ptx::launch_dependents();
     cp_async_wait<0>();
     if (load.bad) atomicOr(p.cache.status, kCacheBad);
 }
@@ -718,12 +770,18 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
     for (int w = 0; w < kJoinThreads / 32; ++w) sum += s_red[1][w];
     // pairs of columns; groups of threads take the parts in turn
     const int pairs = p.d / 2, groups = kJoinThreads / pairs, group = tid / pairs, c = tid - group * pairs;
+    constexpr int kBatch = 8;  // loads of a thread that are under way together
     float x = 0.f, y = 0.f;
     if (group < groups) {
-#pragma unroll 4
-        for (int i = group; i < parts; i += groups) {
-            const float2 v = *reinterpret_cast<const float2 *>(result(i) + 2 + 2 * c);
-            x = fmaf(s_weight[i], v.x, x), y = fmaf(s_weight[i], v.y, y);
+        for (int i0 = group; i0 < parts; i0 += kBatch * groups) {
+            float2 v[kBatch];
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j) v[j] = *reinterpret_cast<const float2 *>(result(min(i0 + j * groups, parts - 1)) + 2 + 2 * c);
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j) {
+                const float w = i0 + j * groups < parts ? s_weight[i0 + j * groups] : 0.f;
+                x = fmaf(w, v[j].x, x), y = fmaf(w, v[j].y, y);
+            }
         }
         s_sum[2 * tid] = x, s_sum[2 * tid + 1] = y;
     }
@@ -743,7 +801,7 @@ int block_rows(const mate_cache_t *c) { return c->dtype == MATE_BF16 && c->heads
 int blocks_of_group(const mate_cache_t *c) { return (c->heads / c->kv_heads + block_rows(c) - 1) / block_rows(c); }
 // Blocks that share the work, 0 where each takes one item.
 int shares(const mate_cache_t *c, int B, int max_len) {
-    const int64_t items = (int64_t)B * c->kv_heads * blocks_of_group(c), units = items * ((max_len + kUnit - 1) / kUnit);
+    const int64_t items = (int64_t)B * c->kv_heads * blocks_of_group(c), units = items * units_of(max_len);
     const int most = kBlocksPerSm * n_sms(c->device);
     return units == items ? 0 : (int)(units < most ? units : most);
 }
@@ -753,7 +811,7 @@ int launch(const DecodeParams &p, int blocks, int device, cudaStream_t st) {
     static SmemAttrOnce attr;
     using S = Shape<T, DP, NB>;
     const int rows = S::kRows < p.group ? S::kRows : p.group;
-    constexpr int kSmem = kWarps * kRing * kStage + kExtra<T, DP, NB>;
+    constexpr int kSmem = kAlign + kWarps * kRing * kStage + kExtra<T, DP, NB>;
     int rc = attr.ensure((const void *)decode_kernel<T, DP, NB>, kSmem, device);
     if (rc != MATE_OK) return rc;
     const int64_t items = (int64_t)p.kv_heads * p.blocks_of_group, grid = blocks ? blocks : p.B * items;
@@ -790,18 +848,21 @@ extern "C" int mate_attn_decode(const mate_cache_t *cache, int layer, const void
         return MATE_ERR_ALIGNMENT;
     if ((rc = check_cache_device(cache)) != MATE_OK) return rc;
     if (B == 0) return MATE_OK;
+    const int most = cache->width * cache->page_size;
+    if (max_len == 0 || max_len > most) max_len = most;
+    if ((int64_t)B * cache->kv_heads * blocks_of_group(cache) > INT32_MAX / units_of(max_len)) return MATE_ERR_UNSUPPORTED;
     DecodeParams p = {};
     p.cache = cache_args(cache, layer);
     p.Q = Q, p.q_batch = q_stride[0], p.q_head = q_stride[1];
     p.B = B, p.heads = cache->heads, p.kv_heads = cache->kv_heads, p.group = cache->heads / cache->kv_heads;
     p.blocks_of_group = blocks_of_group(cache), p.d = cache->d;
-    const int most = cache->width * cache->page_size;
-    p.max_len = max_len > 0 && max_len < most ? max_len : most;
+    p.max_len = max_len;
     p.seqs = seqs, p.row_ids = row_ids, p.col_ids = col_ids;
     p.scale_log2 = scale * kLog2e, p.O = O, p.LSE = LSE;
     for (int h = 0; h < cache->heads; ++h) p.views[h >> 4] |= (uint32_t)cache->head_view[h] << 2 * (h & 15);
     for (p.page_shift = 0; 1u << p.page_shift < (unsigned)cache->page_size;) ++p.page_shift;
     p.page_mul = (unsigned)((((uint64_t)1 << 32) * (((uint64_t)1 << p.page_shift) - cache->page_size)) / cache->page_size + 1);
+    p.page16 = (unsigned)(cache->page_stride / vec), p.head16 = (unsigned)(cache->head_stride / vec), p.slot16 = (unsigned)(cache->slot_stride / vec);
     const int blocks = shares(cache, B, p.max_len);
     if (blocks) {
         if (!workspace || workspace_bytes < decode_workspace(cache, B)) return MATE_ERR_WORKSPACE;
