@@ -279,11 +279,11 @@ PyObject *cache_append(PyObject *, PyObject *const *a, Py_ssize_t n) {
         const int layer = as_int(whole(a[1]), "layer");
         const at::Tensor &K = on_gpu(a[2], "K", &ci.device), &V = on_gpu(a[3], "V", &ci.device);
         int64_t ks[3], vs[3];
-        for (const at::Tensor *t : {&K, &V}) {
+        for (const auto &[t, strides] : {std::pair(&K, ks), std::pair(&V, vs)}) {  // (K and V may be one tensor)
             if (t->dim() != 4 || t->size(1) != ci.c.kv_heads || t->size(3) != ci.c.d || t->sizes() != K.sizes() || t->scalar_type() != ci.type)
                 fail_shape("K and V", "[B, kv_heads, N, d] of the cache's type");
             rows(*t, "K and V");
-            for (int i = 0; i < 3; ++i) (t == &K ? ks : vs)[i] = t->size(i) > 1 ? t->stride(i) : 0;
+            for (int i = 0; i < 3; ++i) strides[i] = t->size(i) > 1 ? t->stride(i) : 0;
         }
         const int64_t B = K.size(0), N = K.size(2);
         const int32_t *seqs = ints(a[4], "seqs", {B}, ci.device, true), *counts = ints(a[5], "counts", {B}, ci.device, true);

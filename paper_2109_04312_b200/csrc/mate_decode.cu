@@ -4,8 +4,8 @@
 //
 // Bound by memory: a key and a value are read once for the whole group (4 d bytes in bf16 for 4 d flops per head), the ids of all
 // cached tokens (4 or 8 bytes each, mostly from L2: the kv heads share them) decide which.  Hence
-//   - a warp works alone: it looks through 128 tokens at a time (page, ids; the next ones' are on their way meanwhile), puts the
-//     places of those that count into a list, and copies 16 bytes per lane and instruction from there into its own ring of stages
+//   - a warp works alone: it looks through 32 tokens at a time (the next ones' ids and the pages behind them are on their way
+//     meanwhile; four tokens per lane at a time took up to 5 % longer), puts the places of those that count into a list, and copies 16 bytes per lane and instruction from there into its own ring of stages
 //     of 8 KB, with kRing - 1 stages under way; no block barrier until the sequence's part is done.  What nobody attends is never
 //     read, padding's keys and values included.
 //   - the products are tensor-core ones (m16n8k16) with the keys as the 16 rows and the heads as the 8 columns, so that a group
@@ -23,20 +23,20 @@ namespace mate {
 namespace {
 
 constexpr int kWarps = 4, kThreads = 32 * kWarps;
-constexpr int kUnit = 128;               // tokens of a unit of work
-constexpr int kLook = 4;                 // tokens of a lane that are looked at together
+constexpr int kUnit = 32 * kWarps;       // tokens of a unit of work: what the warps look through in one go
 constexpr int kStage = 8192;             // bytes of a stage: keys, then values
 constexpr int kAlign = 256;              // of the ring: the longest row of tensor-core operands
 constexpr int kRing = 2;                 // stages of a warp
-constexpr int kList = 256;               // entries of a warp's list of places: less than a stage, and one look
+constexpr int kList = 64;                // entries of a warp's list of places: less than a stage, and one look
 constexpr int kBlocksPerSm = 3;
-constexpr int kJoinThreads = 256;
+constexpr int kOver = 1;                 // units that an item costs besides its tokens
+constexpr int kWhole = 4;                // units of tokens up to which a block takes a whole item
 constexpr int kMaxHeads = 1024;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
-// An item that a block begins and others go on with: results [slot] of the block, then [0] of the next ones up to `last`.
+// Where the results of an item are: [slot] of the block that begins it, then [0] of the next ones up to `last`.
 struct Joint {
-    int32_t b, item, slot, last;  // last < 0: there is none
+    int32_t slot, first, last, unused;  // slot < 0: it is done
 };
 
 struct DecodeParams {
@@ -50,7 +50,7 @@ struct DecodeParams {
     float *LSE;
     unsigned page16, head16, slot16;  // strides in 16 bytes; no place is beyond 2^32 of them
     unsigned page_mul, page_shift;  // x / page_size = (umulhi(x, page_mul) + x) >> page_shift for x < 2^31
-    Joint *joints;  // [grid]; null: a block per sequence, kv head and block of the group
+    Joint *joints;         // [B][items]; null: a block per item
     float *partial;        // [grid][2][rows of a block][d + 2]
     uint32_t views[kMaxHeads / 16];  // two bits a head
 };
@@ -107,9 +107,10 @@ __device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], 
 // ---- shares of the work
 
 // An item is one sequence's kv head and block of its group; items of a sequence follow one another.  Its units are numbered through
-// over all items (fewer than 2^31, the host sees to that); block i of C gets units [i U / C, (i + 1) U / C).  (Every item has a unit:
-// empty ones are written too.)
-__host__ __device__ __forceinline__ int units_of(int len) { return len > kUnit ? (len + kUnit - 1) / kUnit : 1; }
+// over all items (fewer than 2^31, the host sees to that); block i of C gets units [i U / C, (i + 1) U / C).  The first kOver units
+// stand for what an item costs whatever its length (none of its tokens belong to them); a share that ends among them ends in front
+// of the item.  An item without tokens, which is written too, has one unit.
+__host__ __device__ __forceinline__ int units_of(int len) { return len > 0 ? kOver + (len + kUnit - 1) / kUnit : 1; }
 __device__ __forceinline__ unsigned share(unsigned U, unsigned C, unsigned i) { return U / C * i + U % C * i / C; }
 
 // Tokens that entry b of the batch has to look through; none for an entry that is no sequence, or padding.
@@ -184,6 +185,7 @@ __device__ __forceinline__ bool next_part(const DecodeParams &p, int items, Walk
     const int n = units_of(*len);
     part.b = w.b, part.item = w.item, part.u0 = w.u;
     part.u1 = min(n, w.u + w.left);
+    if (part.u1 <= kOver && part.u1 < n) return false;
     part.whole = part.u0 == 0 && part.u1 == n;
     w.left -= max(1, part.u1 - part.u0);
     w.u = 0;
@@ -201,7 +203,7 @@ struct Meta {  // of a stage
     uint32_t by_row, by_col;
     int b, item, state, units;  // the part
 };
-enum { kNoPart = 0, kWhole = 1, kBegins = 2, kGoesOn = 3 };  // Meta.state: behind the last one; an item; its first units; others
+enum { kNoPart = 0, kAll = 1, kBegins = 2, kGoesOn = 3 };  // Meta.state: behind the last one; an item; its first units; others
 
 template <typename T, int DP, int NB>
 struct Loader {
@@ -219,37 +221,26 @@ struct Loader {
     int s, prefix, q_row, q_col, end;
     unsigned head_at;
     bool text, need_row, need_col;
-    int next;                           // first of the tokens that are looked at next; 32 of every 32 kWarps are the warp's
-    unsigned at[kLook];                 // places of the lane's tokens there, whose ids have been asked for
-    int row[kLook], col[kLook];
-    unsigned there;                     // a bit for each that exists
+    int next;                           // first of the 32 tokens that are looked at next; 32 of every kUnit are the warp's
+    bool there;                         // the lane's token there exists; its ids have been asked for
+    unsigned at;
+    int row, col;
+    int page;                           // page of the one behind it, which has been asked for too
     bool bad;
     int pending, list_at, filled;       // list (list_at: a multiple of a stage's keys); stages so far
 
-    __device__ void ask() {
-        int page[kLook];
-        there = 0;
-#pragma unroll
-        for (int i = 0; i < kLook; ++i) {
-            const int j = next + 32 * kWarps * i + lane;
-            if (j < end) {
-                page[i] = p.cache.table[(size_t)s * p.cache.width + page_index(p, j)];
-                there |= 1u << i;
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < kLook; ++i) {
-            if (!(there >> i & 1)) continue;
-            if (!in_range(page[i], p.cache.pages)) {
-                bad = true, there &= ~(1u << i);
-                continue;
-            }
-            const int j = next + 32 * kWarps * i + lane, slot = j - page_index(p, j) * p.cache.page_size;
-            const int id = page[i] * p.cache.page_size + slot;
-            if (need_row) row[i] = p.cache.row_ids[id];
-            if (need_col) col[i] = p.cache.col_ids[id];
-            at[i] = (unsigned)page[i] * p.page16 + (unsigned)slot * p.slot16 + head_at;
-        }
+    // page of the lane's token `j`
+    __device__ void ask_page(int j) { page = j < end ? p.cache.table[(size_t)s * p.cache.width + page_index(p, j)] : -1; }
+    // ids of the lane's token of `next`, whose page has come
+    __device__ void ask_ids() {
+        const int j = next + lane;
+        there = j < end && in_range(page, p.cache.pages);
+        if (j < end && !there) bad = true;
+        if (!there) return;
+        const int slot = j - page_index(p, j) * p.cache.page_size, id = page * p.cache.page_size + slot;
+        if (need_row) row = p.cache.row_ids[id];
+        if (need_col) col = p.cache.col_ids[id];
+        at = (unsigned)page * p.page16 + (unsigned)slot * p.slot16 + head_at;
     }
     __device__ void begin() {
         int len, kv, h0, n;
@@ -265,9 +256,13 @@ struct Loader {
             if (warp == 0) {
                 for (int i = lane; i < n * p.d; i += 32) put(0.f, (T *)p.O + row * p.d + i);
                 for (int i = lane; i < n; i += 32) p.LSE[row + i] = -INFINITY;
+                if (p.joints && lane == 0) p.joints[part.b * items + part.item].slot = -1;
             }
         }
         s = p.seqs ? p.seqs[part.b] : part.b;
+        next = max(0, part.u0 - kOver) * kUnit + 32 * warp;
+        end = min(len, (part.u1 - kOver) * kUnit);
+        ask_page(next + lane);
         q_row = p.row_ids[part.b], q_col = p.col_ids[part.b];
         prefix = p.cache.prefix[s];
         text = q_row == MATE_ID_TEXT || q_col == MATE_ID_TEXT;
@@ -279,29 +274,27 @@ struct Loader {
             need_col |= v != MATE_VIEW_ROW;
         }
         if (text) need_row = true, need_col = false;  // padding has neither
-        next = part.u0 * kUnit + 32 * warp;
-        end = min(len, part.u1 * kUnit);
         list_at = 0;
-        ask();
+        ask_ids();
+        ask_page(next + kUnit + lane);
     }
-    // One look at 32 kLook tokens: those that count go onto the list, the next ones' ids are asked for.
+    // One look at 32 tokens: those that count go onto the list, the next ones' ids are asked for.
     __device__ void look() {
-#pragma unroll
-        for (int i = 0; i < kLook; ++i) {
-            const int j = next + 32 * kWarps * i + lane;
-            const bool is = there >> i & 1, all = text || j < prefix;
-            const bool by_row = is && need_row && row[i] >= 0 && (all || row[i] == MATE_ID_TEXT || row[i] == q_row);
-            const bool by_col = is && need_col && col[i] >= 0 && (all || col[i] == MATE_ID_TEXT || col[i] == q_col);
-            const unsigned counts = __ballot_sync(~0u, by_row || by_col);
-            if (by_row || by_col) {
-                const int to = (list_at + pending + __popc(counts & ((1u << lane) - 1))) & (kList - 1);
-                list[to] = at[i];
-                if (need_row && need_col) marks[to] = (by_row ? 1 : 0) | (by_col ? 2 : 0);
-            }
-            pending += __popc(counts);
+        const bool all = text || next + lane < prefix;
+        const bool by_row = there && need_row && row >= 0 && (all || row == MATE_ID_TEXT || row == q_row);
+        const bool by_col = there && need_col && col >= 0 && (all || col == MATE_ID_TEXT || col == q_col);
+        const unsigned counts = __ballot_sync(~0u, by_row || by_col);
+        if (by_row || by_col) {
+            const int to = (list_at + pending + __popc(counts & ((1u << lane) - 1))) & (kList - 1);
+            list[to] = at;
+            if (need_row && need_col) marks[to] = (by_row ? 1 : 0) | (by_col ? 2 : 0);
         }
-        next += 32 * kWarps * kLook;
-        if (next < end) ask();
+        pending += __popc(counts);
+        next += kUnit;
+        if (next < end) {
+            ask_ids();
+            ask_page(next + kUnit + lane);
+        }
     }
     // Copies of the next stage are put under way (or, at the end of the share, none: the groups are counted).
     __device__ void fill() {
@@ -317,7 +310,7 @@ struct Loader {
                 by_row = __ballot_sync(~0u, mine & 1), by_col = __ballot_sync(~0u, mine & 2);
             }
             if (lane == 0)
-                meta[slot] = {n, last, by_row, by_col, part.b, part.item, part.whole ? kWhole : part.u0 == 0 ? kBegins : kGoesOn, part.u1 - part.u0};
+                meta[slot] = {n, last, by_row, by_col, part.b, part.item, part.whole ? kAll : part.u0 == 0 ? kBegins : kGoesOn, part.u1 - part.u0};
             // a lane copies a 16-byte column of eight keys
             const int chunk = lane % S::kChunks, first = lane / S::kChunks * 8;
             if (n > 0 && chunk < p.d * (int)sizeof(T) / 16) {
@@ -415,8 +408,8 @@ struct Reader<__nv_bfloat16, DP, NB> {
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb) mma16816(s[t][nb], a, q[k][nb]);
             }
-        constexpr uint32_t kAll = S::kKeys < 32 ? (1u << S::kKeys) - 1 : ~0u;
-        const bool all = (meta.by_row & meta.by_col) == kAll;
+        constexpr uint32_t kFull = S::kKeys < 32 ? (1u << S::kKeys) - 1 : ~0u;
+        const bool all = (meta.by_row & meta.by_col) == kFull;
         uint32_t w[kTiles][NB][2];
         float keep[NB][2];
         bool moved = false;
@@ -636,11 +629,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) decode_kernel(const __
     Start start = {};
     if (p.joints) {
         start = find_start(p, items);
-        if (blockIdx.x >= start.blocks) {
-            if (tid == 0) p.joints[blockIdx.x].last = -1;
-            return;
-        }
-        if (tid == 0) p.joints[blockIdx.x].last = -1;
+        if (blockIdx.x >= start.blocks) return;
         const unsigned at = share(start.total, start.blocks, blockIdx.x);
         walk.left = (int)(share(start.total, start.blocks, blockIdx.x + 1) - at);
         bool bad = false;
@@ -648,6 +637,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) decode_kernel(const __
         walk.b = start.entry;
         walk.item = min(items - 1, (int)((at - start.before) / n));
         walk.u = (int)(at - start.before - walk.item * n);
+        if (walk.u <= kOver) walk.left += walk.u, walk.u = 0;
     } else {
         bool bad = false;
         walk.b = blockIdx.x / items, walk.item = blockIdx.x - walk.b * items, walk.u = 0;
@@ -709,7 +699,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) decode_kernel(const __
                 y = fmaf(f, x[w], y);
             }
             if (e >= p.d) continue;
-            if (part.state == kWhole) {
+            if (part.state == kAll) {
                 const size_t row = (size_t)part.b * p.heads + h0 + r;
                 put(sum == 0.f ? 0.f : y / sum, (T *)p.O + row * p.d + e);
                 if (e == 0) p.LSE[row] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
@@ -722,10 +712,14 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) decode_kernel(const __
         if (p.d < DP)
             for (int i = lane; i < kStage / 16; i += 32) reinterpret_cast<uint4 *>(smem + warp * kRing * kStage + out_at)[i] = make_uint4(0, 0, 0, 0);
         first = false;
-        if (part.state == kBegins && tid == 0) {  // the share's last part: who has the item's last unit?
-            bool bad = false;
-            const int64_t end = (int64_t)share(start.total, start.blocks, blockIdx.x + 1) - part.units + units_of(entry_len(p, part.b, &bad));
-            p.joints[blockIdx.x] = {part.b, part.item, slot, (int)min((end * start.blocks - 1) / start.total, (int64_t)start.blocks - 1)};
+        if (p.joints && tid == 0) {
+            Joint &joint = p.joints[part.b * items + part.item];
+            if (part.state == kAll) joint.slot = -1;
+            if (part.state == kBegins) {  // the share's last part: who has the item's last unit?
+                bool bad = false;
+                const int64_t end = (int64_t)share(start.total, start.blocks, blockIdx.x + 1) - part.units + units_of(entry_len(p, part.b, &bad));
+                joint = {slot, (int)blockIdx.x, (int)min((end * start.blocks - 1) / start.total, (int64_t)start.blocks - 1), 0};
+            }
         }
     }
     ptx::launch_dependents();
@@ -733,30 +727,41 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) decode_kernel(const __
     if (load.bad) atomicOr(p.cache.status, kCacheBad);
 }
 
-// Joins the partial results of an item that fell to several blocks of the kernel before.  grid: (block that began it, row)
-template <typename T>
-__global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ DecodeParams p, int block_rows) {
+// Joins the partial results of an item that fell to several blocks of the kernel before.  grid: (item, row of its block of the group)
+template <typename T, int kN>
+__global__ void __launch_bounds__(kN) join_kernel(const __grid_constant__ DecodeParams p, int block_rows) {
     extern __shared__ float s_weight[];  // of every part
-    __shared__ float s_red[2][kJoinThreads / 32], s_sum[2 * kJoinThreads];
+    __shared__ float s_red[2][kN / 32], s_sum[2 * kN];
     ptx::launch_dependents();
     ptx::wait_prior_grid();
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, r = blockIdx.y, width = p.d + 2;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, r = blockIdx.y, width = p.d + 2, items = p.kv_heads * p.blocks_of_group;
     const Joint joint = p.joints[blockIdx.x];
-    const int kv = joint.item / p.blocks_of_group, part = joint.item - kv * p.blocks_of_group, max_rows = min(block_rows, p.group);
-    const int parts = joint.last - (int)blockIdx.x + 1;
-    if (joint.last < 0 || parts <= 1 || r >= p.group - part * block_rows) return;
-    auto result = [&](int i) { return p.partial + ((size_t)(2 * (blockIdx.x + i) + (i == 0 ? joint.slot : 0)) * max_rows + r) * width; };
+    const int b = blockIdx.x / items, item = blockIdx.x - b * items;
+    const int kv = item / p.blocks_of_group, part = item - kv * p.blocks_of_group, max_rows = min(block_rows, p.group);
+    const int parts = joint.last - joint.first + 1;
+    if (joint.slot < 0 || r >= p.group - part * block_rows) return;
+    auto result = [&](int i) { return p.partial + ((size_t)(2 * (joint.first + i) + (i == 0 ? joint.slot : 0)) * max_rows + r) * width; };
+    // pairs of columns; groups of threads take the parts in turn, the first kBatch of them ahead of the weights
+    constexpr int kBatch = 8;
+    const int pairs = p.d / 2, groups = kN / pairs, group = tid / pairs, c = tid - group * pairs;
+    float2 v[kBatch];
+    auto load = [&](int i0) {
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j)
+            if (i0 + j * groups < parts) v[j] = *reinterpret_cast<const float2 *>(result(i0 + j * groups) + 2 + 2 * c);
+    };
+    if (group < groups) load(group);
     float top = -INFINITY;
-    for (int i = tid; i < parts; i += kJoinThreads) top = fmaxf(top, s_weight[i] = *result(i));
+    for (int i = tid; i < parts; i += kN) top = fmaxf(top, s_weight[i] = *result(i));
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
     if (lane == 0) s_red[0][warp] = top;
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < kJoinThreads / 32; ++w) top = fmaxf(top, s_red[0][w]);
+    for (int w = 0; w < kN / 32; ++w) top = fmaxf(top, s_red[0][w]);
     const float base = top == -INFINITY ? 0.f : top;
     float sum = 0.f;
-    for (int i = tid; i < parts; i += kJoinThreads) {
+    for (int i = tid; i < parts; i += kN) {
         const float w = ptx::ex2(s_weight[i] - base);
         s_weight[i] = w;
         sum = fmaf(w, result(i)[1], sum);
@@ -767,26 +772,22 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
     __syncthreads();
     sum = 0.f;
 #pragma unroll
-    for (int w = 0; w < kJoinThreads / 32; ++w) sum += s_red[1][w];
-    // pairs of columns; groups of threads take the parts in turn
-    const int pairs = p.d / 2, groups = kJoinThreads / pairs, group = tid / pairs, c = tid - group * pairs;
-    constexpr int kBatch = 8;  // loads of a thread that are under way together
-    float x = 0.f, y = 0.f;
+    for (int w = 0; w < kN / 32; ++w) sum += s_red[1][w];
     if (group < groups) {
+        float x = 0.f, y = 0.f;
         for (int i0 = group; i0 < parts; i0 += kBatch * groups) {
-            float2 v[kBatch];
-#pragma unroll
-            for (int j = 0; j < kBatch; ++j) v[j] = *reinterpret_cast<const float2 *>(result(min(i0 + j * groups, parts - 1)) + 2 + 2 * c);
+            if (i0 > group) load(i0);
 #pragma unroll
             for (int j = 0; j < kBatch; ++j) {
-                const float w = i0 + j * groups < parts ? s_weight[i0 + j * groups] : 0.f;
+                if (i0 + j * groups >= parts) break;
+                const float w = s_weight[i0 + j * groups];
                 x = fmaf(w, v[j].x, x), y = fmaf(w, v[j].y, y);
             }
         }
         s_sum[2 * tid] = x, s_sum[2 * tid + 1] = y;
     }
     __syncthreads();
-    const size_t row = (size_t)joint.b * p.heads + kv * p.group + part * block_rows + r;
+    const size_t row = (size_t)b * p.heads + kv * p.group + part * block_rows + r;
     if (tid < p.d) {
         float z = 0.f;
         for (int g = 0; g < groups; ++g) z += s_sum[g * p.d + tid];
@@ -803,7 +804,7 @@ int blocks_of_group(const mate_cache_t *c) { return (c->heads / c->kv_heads + bl
 int shares(const mate_cache_t *c, int B, int max_len) {
     const int64_t items = (int64_t)B * c->kv_heads * blocks_of_group(c), units = items * units_of(max_len);
     const int most = kBlocksPerSm * n_sms(c->device);
-    return units == items ? 0 : (int)(units < most ? units : most);
+    return units <= (kOver + kWhole) * items ? 0 : (int)(units < most ? units : most);
 }
 
 template <typename T, int DP, int NB>
@@ -814,11 +815,16 @@ int launch(const DecodeParams &p, int blocks, int device, cudaStream_t st) {
     constexpr int kSmem = kAlign + kWarps * kRing * kStage + kExtra<T, DP, NB>;
     int rc = attr.ensure((const void *)decode_kernel<T, DP, NB>, kSmem, device);
     if (rc != MATE_OK) return rc;
-    const int64_t items = (int64_t)p.kv_heads * p.blocks_of_group, grid = blocks ? blocks : p.B * items;
+    const int items = p.kv_heads * p.blocks_of_group;
+    const int64_t grid = blocks ? blocks : (int64_t)p.B * items;
     if (grid > INT32_MAX) return MATE_ERR_UNSUPPORTED;
     if (launch_after(decode_kernel<T, DP, NB>, dim3((unsigned)grid), kThreads, kSmem, st, p) != cudaSuccess) return MATE_ERR_CUDA;
     if (!blocks) return MATE_OK;
-    return launch_after(join_kernel<T>, dim3((unsigned)blocks, (unsigned)rows), kJoinThreads, sizeof(float) * blocks, st, p, S::kRows) == cudaSuccess
+    // few items in many parts: more threads each
+    const dim3 joins((unsigned)(p.B * items), (unsigned)rows);
+    const size_t bytes = sizeof(float) * blocks;
+    return (blocks > 16 * p.B * items ? launch_after(join_kernel<T, 1024>, joins, 1024, bytes, st, p, S::kRows)
+                                      : launch_after(join_kernel<T, 128>, joins, 128, bytes, st, p, S::kRows)) == cudaSuccess
                ? MATE_OK
                : MATE_ERR_CUDA;
 }
@@ -828,7 +834,7 @@ int launch(const DecodeParams &p, int blocks, int device, cudaStream_t st) {
 size_t decode_workspace(const mate_cache_t *c, int B) {
     const int blocks = B > 0 ? shares(c, B, c->width * c->page_size) : 0;
     const int group = c->heads / c->kv_heads, rows = block_rows(c) < group ? block_rows(c) : group;
-    return (sizeof(Joint) + sizeof(float) * 2 * rows * (c->d + 2)) * (size_t)blocks;
+    return blocks ? sizeof(Joint) * B * c->kv_heads * blocks_of_group(c) + sizeof(float) * 2 * rows * (c->d + 2) * (size_t)blocks : 0;
 }
 
 }  // namespace mate
@@ -868,7 +874,7 @@ extern "C" int mate_attn_decode(const mate_cache_t *cache, int layer, const void
         if (!workspace || workspace_bytes < decode_workspace(cache, B)) return MATE_ERR_WORKSPACE;
         if (!is_aligned(workspace, 256)) return MATE_ERR_ALIGNMENT;
         p.joints = static_cast<Joint *>(workspace);
-        p.partial = reinterpret_cast<float *>(p.joints + blocks);
+        p.partial = reinterpret_cast<float *>(p.joints + (size_t)B * cache->kv_heads * p.blocks_of_group);
     }
     cudaStream_t st = (cudaStream_t)stream;
     const bool narrow = cache->d <= 64;

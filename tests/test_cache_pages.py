@@ -234,6 +234,21 @@ def test_append_rotates(d, rot, interleaved, dtype):
 
 
 @pytest.mark.gpu
+def test_one_tensor_as_keys_and_values():
+    import paper_2109_04312_b200 as m
+    c = m.Cache.empty(9, 4, 2, 16, 3, 3, [0, 1])
+    n = ints([5, 0, 9])
+    m.mate_cache_extend(c, None, n)
+    x = torch.randn(3, 2, 9, 16, device="cuda").bfloat16()
+    m.mate_cache_append(c, x, x, counts=n)
+    assert torch.equal(c.k, c.v)
+    for s, k in enumerate([5, 0, 9]):
+        for j in range(k):
+            assert torch.equal(c.k[0, c.table[s, j // 4], :, j % 4], x[s, :, j])
+    c.status()
+
+
+@pytest.mark.gpu
 def test_long_lists_and_many_pages():
     import paper_2109_04312_b200 as m
     pages, S = 70001, 4096
