@@ -31,10 +31,10 @@ inline int check_cache(const mate_cache_t *c) {
     if (c->layers < 1 || c->pages < 1 || c->page_size < 1 || c->seqs < 1 || c->width < 1 || c->heads < 1 || c->kv_heads < 1 ||
         c->heads % c->kv_heads != 0)
         return MATE_ERR_INVALID_ARG;
-    // slots, positions and the elements of a page are 32-bit numbers (with room for a block's stride)
+    // slots, positions and the elements of a page are 32-bit numbers (with room for a block's stride), rows of a page exact in fp32
     constexpr int64_t kMost = 1 << 30;
     if ((int64_t)c->pages * c->page_size > kMost || (int64_t)c->width * c->page_size > kMost ||
-        (int64_t)c->kv_heads * c->d > kMost / c->page_size || c->layers > 32767)
+        (int64_t)c->kv_heads * c->d > kMost / c->page_size || (int64_t)c->kv_heads * c->page_size > 1 << 20 || c->layers > 32767)
         return MATE_ERR_UNSUPPORTED;
     for (int64_t s : {c->layer_stride, c->page_stride, c->head_stride, c->slot_stride})
         if (s < 0 || s % (int64_t)(16 / elem_size(c->dtype)) != 0) return MATE_ERR_ALIGNMENT;

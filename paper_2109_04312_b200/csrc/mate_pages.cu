@@ -17,7 +17,8 @@ namespace {
 constexpr int kThreads = 1024;   // of the deciding block
 constexpr int kPer = 4;          // entries of a list per thread: lists of up to 4096
 constexpr int kMost = kThreads * kPer;
-constexpr int kCopyThreads = 256;
+constexpr int kEarly = 16;       // pages of a thread whose reference counts are read before it is known whether any is wanted
+constexpr int kCopyThreads = 128, kCopyBlocks = 8;  // blocks per SM
 
 // Exclusive sum over the block's threads; *total gets the sum.  All threads call it.
 __device__ int block_scan(int x, int *total) {
@@ -58,14 +59,24 @@ __device__ __forceinline__ PageRun my_pages(int pages) {
     return {lo, min(pages, lo + per)};
 }
 
+__device__ __forceinline__ int free_pages(const CacheArgs &c, const PageRun &run) {
+    int n = 0;
+#pragma unroll 8
+    for (int p = run.lo; p < run.hi; ++p) n += c.refs[p] <= 0;
+    return n;
+}
+
 __device__ __forceinline__ int claim_of(int i) { return INT32_MIN + i; }
 
-__global__ void __launch_bounds__(kThreads) extend_kernel(const __grid_constant__ CacheArgs c, const int32_t *seqs, const int32_t *counts, int n,
+__global__ void __launch_bounds__(kThreads, 1) extend_kernel(const __grid_constant__ CacheArgs c, const int32_t *seqs, const int32_t *counts, int n,
                                                           int32_t *granted) {
     __shared__ int s_off[kMost + 1], s_used;
     ptx::launch_dependents();
     ptx::wait_prior_grid();
     const int tid = threadIdx.x, i0 = tid * kPer;
+    const PageRun mine = my_pages(c.pages);
+    const bool early = c.pages <= kEarly * kThreads;
+    int free_here = early ? free_pages(c, mine) : 0;
     int s[kPer], len[kPer], count[kPer], need[kPer], status = 0;
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
@@ -107,10 +118,8 @@ __global__ void __launch_bounds__(kThreads) extend_kernel(const __grid_constant_
         off += need[j];
     }
     int n_free = 0, rank = 0;
-    const PageRun mine = my_pages(c.pages);
     if (wanted > 0) {
-        int free_here = 0;
-        for (int p = mine.lo; p < mine.hi; ++p) free_here += c.refs[p] <= 0;
+        if (!early) free_here = free_pages(c, mine);
         rank = block_scan(free_here, &n_free);
     }
     // granted: who fits into what is free; the pages that go out are the first `used` free ones
@@ -147,16 +156,19 @@ struct ForkItem {
     int32_t src, dst;       // that page, and the one it is copied to (-1: none)
 };
 
-__global__ void __launch_bounds__(kThreads) fork_kernel(const __grid_constant__ CacheArgs c, const int32_t *parents, const int32_t *children,
+__global__ void __launch_bounds__(kThreads, 1) fork_kernel(const __grid_constant__ CacheArgs c, const int32_t *parents, const int32_t *children,
                                                         int n, ForkItem *items) {
     __shared__ int s_off[kMost + 1], s_dst[kMost];
     ptx::launch_dependents();
     ptx::wait_prior_grid();
     const int tid = threadIdx.x, i0 = tid * kPer;
-    int p[kPer], ch[kPer], len[kPer], prefix[kPer], status = 0, sum = 0;
+    const PageRun mine = my_pages(c.pages);
+    const bool early = c.pages <= kEarly * kThreads;
+    int free_here = early ? free_pages(c, mine) : 0;
+    int p[kPer], ch[kPer], len[kPer], prefix[kPer], src[kPer], status = 0, sum = 0;
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
-        p[j] = ch[j] = -1, len[j] = prefix[j] = 0;
+        p[j] = ch[j] = src[j] = -1, len[j] = prefix[j] = 0;
         if (i0 + j >= n) continue;
         p[j] = seq_of(parents, i0 + j, c.seqs);
         ch[j] = seq_of(children, i0 + j, c.seqs);
@@ -164,6 +176,8 @@ __global__ void __launch_bounds__(kThreads) fork_kernel(const __grid_constant__ 
         if (p[j] < 0 || ch[j] < 0 || len[j] < 0 || len[j] > c.width * c.page_size || c.lens[ch[j]] != 0) {
             status |= kCacheBad;
             ch[j] = -1;
+        } else if (len[j] % c.page_size != 0) {
+            src[j] = c.table[(size_t)p[j] * c.width + len[j] / c.page_size];
         }
     }
     __syncthreads();  // every length and prefix has been read
@@ -189,10 +203,8 @@ __global__ void __launch_bounds__(kThreads) fork_kernel(const __grid_constant__ 
     }
     __syncthreads();
     if (wanted > 0) {
-        const PageRun mine = my_pages(c.pages);
-        int free_here = 0, n_free;
-        for (int q = mine.lo; q < mine.hi; ++q) free_here += c.refs[q] <= 0;
-        int rank = block_scan(free_here, &n_free);
+        if (!early) free_here = free_pages(c, mine);
+        int n_free, rank = block_scan(free_here, &n_free);
         for (int q = mine.lo; q < mine.hi && rank < wanted; ++q) {
             if (c.refs[q] > 0) continue;
             s_dst[owner_of(s_off, min(n, kMost), rank++)] = q;
@@ -208,7 +220,7 @@ __global__ void __launch_bounds__(kThreads) fork_kernel(const __grid_constant__ 
             it.full = len[j] / c.page_size;
             it.fill = len[j] - it.full * c.page_size;
             if (it.fill > 0) {
-                it.src = c.table[(size_t)p[j] * c.width + it.full];
+                it.src = src[j];
                 it.dst = s_dst[i0 + j];
                 if (it.dst < 0) status |= kCacheFull;
             }
@@ -231,26 +243,28 @@ struct PageShape {
     int64_t page_stride, head_stride, slot_stride, layer_stride;  // bytes
     int heads, row_bytes, layers, page_size;
 };
-// Copies one page of one layer's keys or values, its first `fill` slots.
-__device__ __forceinline__ void copy_page(const PageShape &sh, char *base, int src, int dst, int fill, int tid, int threads) {
+// Copies one page of one layer's keys or values, its first `fill` slots.  Units of 16 bytes, kFlight of a thread under way; the
+// quotients by way of fp32 (exact: rows are fewer than 2^21, the host sees to that).
+__device__ __forceinline__ void copy_page(const PageShape &sh, char *base, int src, int dst, int fill) {
     const char *from = base + src * sh.page_stride;
     char *to = base + dst * sh.page_stride;
     const int per_row = sh.row_bytes / 16, n = sh.heads * fill * per_row;
+    const float by_fill = 1.f / (float)fill;
     constexpr int kFlight = 4;
-    for (int i = tid; i < n; i += threads * kFlight) {
+    for (int i = threadIdx.x; i < n; i += kCopyThreads * kFlight) {
         uint4 v[kFlight];
         int64_t at[kFlight];
 #pragma unroll
         for (int j = 0; j < kFlight; ++j) {
-            const int u = i + j * threads;
+            const int u = i + j * kCopyThreads;
             if (u >= n) break;
-            const int row = u / per_row, part = u - row * per_row, head = row / fill, slot = row - head * fill;
-            at[j] = head * sh.head_stride + slot * sh.slot_stride + part * 16;
+            const int row = u / per_row, head = (int)(((float)row + 0.5f) * by_fill);
+            at[j] = head * sh.head_stride + (row - head * fill) * sh.slot_stride + (u - row * per_row) * 16;
             v[j] = *reinterpret_cast<const uint4 *>(from + at[j]);
         }
 #pragma unroll
         for (int j = 0; j < kFlight; ++j)
-            if (i + j * threads < n) *reinterpret_cast<uint4 *>(to + at[j]) = v[j];
+            if (i + j * kCopyThreads < n) *reinterpret_cast<uint4 *>(to + at[j]) = v[j];
     }
 }
 __device__ __forceinline__ void copy_ids(const CacheArgs &c, int src, int dst, int fill, int tid, int threads) {
@@ -261,7 +275,7 @@ __device__ __forceinline__ void copy_ids(const CacheArgs &c, int src, int dst, i
 }
 
 // grid: (entry, layer and keys / values; one more for the table and the ids)
-__global__ void __launch_bounds__(kCopyThreads) fork_copy_kernel(const __grid_constant__ CacheArgs c, const __grid_constant__ PageShape sh,
+__global__ void __launch_bounds__(kCopyThreads, kCopyBlocks) fork_copy_kernel(const __grid_constant__ CacheArgs c, const __grid_constant__ PageShape sh,
                                                                  const ForkItem *items) {
     ptx::launch_dependents();
     ptx::wait_prior_grid();
@@ -270,7 +284,7 @@ __global__ void __launch_bounds__(kCopyThreads) fork_copy_kernel(const __grid_co
     const int part = blockIdx.y;
     if (part < 2 * sh.layers) {
         if (it.src < 0 || it.dst < 0) return;
-        copy_page(sh, (char *)(part & 1 ? c.v : c.k) + (part >> 1) * sh.layer_stride, it.src, it.dst, it.fill, threadIdx.x, kCopyThreads);
+        copy_page(sh, (char *)(part & 1 ? c.v : c.k) + (part >> 1) * sh.layer_stride, it.src, it.dst, it.fill);
         return;
     }
     if (it.src >= 0 && it.dst >= 0) copy_ids(c, it.src, it.dst, it.fill, threadIdx.x, kCopyThreads);
@@ -325,7 +339,7 @@ __global__ void __launch_bounds__(kCopyThreads) free_kernel(const __grid_constan
 struct Moves {
     int32_t *n, *from, *to, *place;
 };
-__global__ void __launch_bounds__(kThreads) compact_kernel(const __grid_constant__ CacheArgs c, Moves m, int32_t *n_live_out) {
+__global__ void __launch_bounds__(kThreads, 1) compact_kernel(const __grid_constant__ CacheArgs c, Moves m, int32_t *n_live_out) {
     ptx::launch_dependents();
     ptx::wait_prior_grid();
     const PageRun mine = my_pages(c.pages);
@@ -359,7 +373,7 @@ __global__ void __launch_bounds__(kThreads) compact_kernel(const __grid_constant
 }
 
 // Blocks take (move, layer, keys / values) in turn, and then the table's rows.
-__global__ void __launch_bounds__(kCopyThreads) compact_copy_kernel(const __grid_constant__ CacheArgs c, const __grid_constant__ PageShape sh,
+__global__ void __launch_bounds__(kCopyThreads, kCopyBlocks) compact_copy_kernel(const __grid_constant__ CacheArgs c, const __grid_constant__ PageShape sh,
                                                                     Moves m) {
     ptx::launch_dependents();
     ptx::wait_prior_grid();
@@ -367,7 +381,7 @@ __global__ void __launch_bounds__(kCopyThreads) compact_copy_kernel(const __grid
     for (int64_t w = blockIdx.x; w < (int64_t)n_moves * parts; w += gridDim.x) {
         const int i = (int)(w / parts), part = (int)(w - (int64_t)i * parts), src = m.from[i], dst = m.to[i];
         if (part < 2 * sh.layers)
-            copy_page(sh, (char *)(part & 1 ? c.v : c.k) + (part >> 1) * sh.layer_stride, src, dst, c.page_size, threadIdx.x, kCopyThreads);
+            copy_page(sh, (char *)(part & 1 ? c.v : c.k) + (part >> 1) * sh.layer_stride, src, dst, c.page_size);
         else
             copy_ids(c, src, dst, c.page_size, threadIdx.x, kCopyThreads);
     }
@@ -459,7 +473,7 @@ int mate_cache_compact(const mate_cache_t *cache, int32_t *n_live, void *workspa
     const Moves m = {w, w + 64, w + 64 + (size_t)cache->pages, w + 64 + 2 * (size_t)cache->pages};
     cudaError_t e = launch_after(compact_kernel, dim3(1), kThreads, 0, (cudaStream_t)stream, c, m, n_live);
     if (e == cudaSuccess)
-        e = launch_after(compact_copy_kernel, dim3((unsigned)(n_sms(cache->device) * 8)), kCopyThreads, 0, (cudaStream_t)stream, c, page_shape(cache), m);
+        e = launch_after(compact_copy_kernel, dim3((unsigned)(n_sms(cache->device) * kCopyBlocks)), kCopyThreads, 0, (cudaStream_t)stream, c, page_shape(cache), m);
     return as_status(e);
 }
 

@@ -97,43 +97,19 @@ __global__ void __launch_bounds__(kThreads, 6) rope_kernel(const __grid_constant
     const Side &s = p.side[side];
     const int h0 = (blockIdx.y - s.first_slice) * p.heads_of_thread, n_heads = min(s.heads - h0, p.heads_of_thread);
     const bool exists = b < p.B;
-    int position = 0;
-    int64_t page_at = -1;  // where the token's row is in the pages, -1: nowhere
+    // a row of queries always goes somewhere; one of keys or values if its sequence has the token
+    int q = 0, count = p.N;
     if (p.paged && exists) {
-        bool bad = false;
-        const int q = seq_of(p.seqs, b, p.cache.seqs), count = p.counts ? p.counts[b] : p.N;
-        if (q < 0 || count < 0 || count > p.N) {
-            bad = true;
-        } else if (n < count) {
-            const int at = clip_len(p.cache.lens[q], p.cache.width * p.cache.page_size, &bad) - count + n;
-            position = at;
-            if (at < 0) bad = true;
-            if (!bad) {
-                const int i = at / p.cache.page_size, slot = at - i * p.cache.page_size;
-                const int page = p.cache.table[(size_t)q * p.cache.width + i];
-                if (!in_range(page, p.cache.pages)) {
-                    bad = true;
-                } else {
-                    page_at = page * p.cache.page_stride + slot * p.cache.slot_stride;
-                    if (p.row_ids && blockIdx.y == 0 && chunk == 0) {
-                        const size_t to = (size_t)page * p.cache.page_size + slot;
-                        p.cache.row_ids[to] = p.row_ids[t];
-                        p.cache.col_ids[to] = p.col_ids[t];
-                    }
-                }
-            }
-        }
-        if (bad && blockIdx.y == 0 && chunk == 0) atomicOr(p.cache.status, kCacheBad);
+        q = seq_of(p.seqs, b, p.cache.seqs);
+        if (p.counts) count = p.counts[b];
+        if ((q < 0 || count < 0 || count > p.N) && chunk == 0 && blockIdx.y == 0) atomicOr(p.cache.status, kCacheBad);
+        if (q < 0 || count > p.N) count = 0;
     }
-    if (p.positions && exists) position = p.positions[b * p.position_stride + n];
-
-    const bool goes = exists && (s.y || page_at >= 0);
+    bool goes = exists && (s.y || n < count);
     const Place place_of = place<VEC>(p, chunk, s.turned);
     const int second = place_of.b - place_of.a;  // from one run to the other
     const bool two = VEC > 1 || place_of.has_b;
     const T *from = (const T *)s.x + b * s.xs[0] + h0 * s.xs[1] + n * s.xs[2] + place_of.a;
-    T *to = s.y ? (T *)s.y + b * s.ys[0] + h0 * s.ys[1] + n * s.ys[2] + place_of.a
-                : (T *)(s.to_keys ? p.cache.k : p.cache.v) + page_at + h0 * p.cache.head_stride + place_of.a;
     const int64_t from_step = s.xs[1], to_step = s.y ? s.ys[1] : p.cache.head_stride;
     Run<T, VEC> x[kFlight], y[kFlight];
     auto load = [&](int h) {
@@ -147,6 +123,34 @@ __global__ void __launch_bounds__(kThreads, 6) rope_kernel(const __grid_constant
         }
     };
     load(0);
+
+    // the token's position and, in a cache, its slot (the loads above are under way)
+    int position = 0;
+    int64_t page_at = 0;
+    if (p.paged && exists && n < count) {
+        bool bad = false;
+        position = clip_len(p.cache.lens[q], p.cache.width * p.cache.page_size, &bad) - count + n;
+        int page = -1;
+        if (position >= 0 && !bad) {
+            const int i = position / p.cache.page_size, slot = position - i * p.cache.page_size;
+            page = p.cache.table[(size_t)q * p.cache.width + i];
+            if (in_range(page, p.cache.pages)) {
+                page_at = page * p.cache.page_stride + slot * p.cache.slot_stride;
+                if (p.row_ids && blockIdx.y == 0 && chunk == 0) {
+                    const size_t id = (size_t)page * p.cache.page_size + slot;
+                    p.cache.row_ids[id] = p.row_ids[t];
+                    p.cache.col_ids[id] = p.col_ids[t];
+                }
+            }
+        }
+        if (!in_range(page, p.cache.pages)) {
+            if (blockIdx.y == 0 && chunk == 0) atomicOr(p.cache.status, kCacheBad);
+            goes = s.y;
+        }
+    }
+    if (p.positions && exists) position = p.positions[b * p.position_stride + n];
+    T *to = s.y ? (T *)s.y + b * s.ys[0] + h0 * s.ys[1] + n * s.ys[2] + place_of.a
+                : (T *)(s.to_keys ? p.cache.k : p.cache.v) + page_at + h0 * p.cache.head_stride + place_of.a;
 
     for (int i = threadIdx.x; i < p.rot / 2; i += kThreads) {
         const double turns = p.freqs[i] * 0.15915494309189533577;
