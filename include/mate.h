@@ -315,6 +315,8 @@ int mate_rope(const mate_rope_tensor_t *tensors, int n_tensors, int B, int N, in
  * memory that only the calls below (and the caller, between them) change; every call is asynchronous on its stream
  * and can be captured into a graph.  Calls on one cache must be ordered (one stream, or events).
  *
+ * d is a multiple of 8 and at most 128; pages * page_size and width * page_size are at most 2^30, kv_heads * page_size 2^20.
+ *
  * What the kernels find on the device and cannot do -- a sequence, length or page out of range, a sequence twice
  * in a list, no free page left -- they leave out, and say so in status[0], which mate_cache_status reads.  No
  * such content makes a kernel read or write outside of the arrays. */
@@ -393,8 +395,9 @@ int mate_cache_status(const mate_cache_t *cache, void *stream);
  *              and beyond it do not count, and status says so
  *   O, LSE     [B, heads, d] of the cache's type, float32 [B, heads]; fully overwritten
  *   workspace  device, 256-byte aligned, mate_cache_workspace_bytes; contents undefined afterwards; calls that overlap need one each
- * Scores, softmax and sums in fp32; with bf16 the weights are rounded to bf16 ahead of the product with V, as in
- * mate_attn_fwd.  Asynchronous on `stream`. */
+ * Scores, softmax and sums in fp32; with bf16 the weights enter the product with V as the sum of two bf16 (16 bits of
+ * mantissa), and only the result is rounded to bf16.  A NaN or Inf in the key or value of a token that one head of a group attends may
+ * also reach the others of the group.  heads <= 1024.  Asynchronous on `stream`. */
 int mate_attn_decode(const mate_cache_t *cache, int layer, const void *Q, const int64_t *q_stride, int B, const int32_t *seqs,
                      const int32_t *row_ids, const int32_t *col_ids, float scale, int max_len, void *O, float *LSE, void *workspace,
                      size_t workspace_bytes, void *stream);

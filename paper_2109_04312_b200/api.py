@@ -16,6 +16,7 @@ ID_TEXT = 0x7FFFFFFF   # ids of a cached or new token that belongs to the text, 
 _BF16, _F32 = 0, 1
 
 _lib = None
+_cache_calls = None   # the native module, once the library is loaded
 
 
 class MateError(RuntimeError):
@@ -32,7 +33,7 @@ def library_path() -> str:
 
 def _load():
     """Loads the CUDA library; there is no fallback: a missing library is an error."""
-    global _lib
+    global _lib, _cache_calls
     if _lib is not None:
         return _lib
     path = library_path()
@@ -82,9 +83,10 @@ def _load():
         raise ImportError("the native binding is not built: run `python -m paper_2109_04312_b200.build`") from e
     _native.bind(*(C.cast(f, C.c_void_p).value for f in (lib.mate_attn_workspace_bytes, lib.mate_attn_fwd,
                                                          lib.mate_attn_bwd, lib.mate_cell_mean)), MateError)
-    cache_calls = (lib.mate_rope, lib.mate_cache_extend, lib.mate_cache_append, lib.mate_cache_fork, lib.mate_cache_free,
-                   lib.mate_cache_compact, lib.mate_cache_workspace_bytes, lib.mate_cache_status, lib.mate_attn_decode)
-    _native.bind_cache(*(C.cast(f, C.c_void_p).value for f in cache_calls))
+    entries = (lib.mate_rope, lib.mate_cache_extend, lib.mate_cache_append, lib.mate_cache_fork, lib.mate_cache_free,
+               lib.mate_cache_compact, lib.mate_cache_workspace_bytes, lib.mate_cache_status, lib.mate_attn_decode)
+    _native.bind_cache(*(C.cast(f, C.c_void_p).value for f in entries))
+    _cache_calls = _native
     _lib = lib
     return lib
 
@@ -353,10 +355,10 @@ def mate_rope(Q, positions, freqs, K=None, interleaved=False, mscale=1.0, backwa
     all examples; freqs: float64 [rot / 2] (mate_rope_freqs).  backward: gradients of the inputs from those of the outputs.
     out: where the result goes (a pair with K), any strides, the inputs themselves included; else new contiguous
     tensors.  Returns Q' or (Q', K')."""
-    _load()
-    from . import _native
+    if _lib is None:
+        _load()
     q, k = (out, None) if K is None else (None, None) if out is None else out
-    return _native.rope(Q, K, positions, freqs, interleaved, mscale, backward, q, k)
+    return _cache_calls.rope(Q, K, positions, freqs, interleaved, mscale, backward, q, k)
 
 
 class Cache:
@@ -368,13 +370,12 @@ class Cache:
 
     def __init__(self, k, v, row_ids, col_ids, table, lens, prefix, refs, head_view):
         _load()
-        from . import _native
         self.k, self.v, self.row_ids, self.col_ids = k, v, row_ids, col_ids
         self.table, self.lens, self.prefix, self.refs = table, lens, prefix, refs
         self.head_view = np.ascontiguousarray(np.asarray(head_view, dtype=np.uint8))
         self.status_word = torch.zeros(1, dtype=torch.int32, device=k.device)
-        self._native = _native
-        self._info = _native.cache_info(k, v, row_ids, col_ids, table, lens, prefix, refs, self.status_word, self.head_view.tobytes())
+        self._native = _cache_calls
+        self._info = _cache_calls.cache_info(k, v, row_ids, col_ids, table, lens, prefix, refs, self.status_word, self.head_view.tobytes())
 
     @classmethod
     def empty(cls, pages, page_size, kv_heads, d, seqs, width, head_view, layers=1, dtype=torch.bfloat16, device="cuda"):

@@ -10,11 +10,15 @@
 //     read, padding's keys and values included.
 //   - the products are tensor-core ones (m16n8k16) with the keys as the 16 rows and the heads as the 8 columns, so that a group
 //     of up to 8 costs one of them; they take a tenth of the time that the copies take.  The weights go from one product's
-//     result to the other's operand by transposing 8 x 8 pieces between the lanes.  fp32 caches: multiply-adds.
+//     result to the other's operand by transposing 8 x 8 pieces between the lanes, as the sum of two bf16: the second product costs
+//     1 % (64 sequences, 72.1 -> 73.1 us), rounding them to bf16 would make the error against 64 bits 2.4e-3 instead of the 1.7e-3 that the
+//     result's own rounding makes.  fp32 caches: multiply-adds.
 //   - blocks get equal shares of all sequences' tokens in units of kUnit (found by every block from the lengths, which the host does not
 //     know), so one long sequence is spread over the GPU and short ones are put together.  A sequence that falls to several
 //     blocks is joined by a second kernel from their partial results, in the order of its tokens: the same bits on every launch.
 #include <cuda_bf16.h>
+
+#include <type_traits>
 
 #include "mate_cache.h"
 #include "sm100_ptx.cuh"
@@ -28,7 +32,6 @@ constexpr int kStage = 8192;             // bytes of a stage: keys, then values
 constexpr int kAlign = 256;              // of the ring: the longest row of tensor-core operands
 constexpr int kRing = 2;                 // stages of a warp
 constexpr int kList = 64;                // entries of a warp's list of places: less than a stage, and one look
-constexpr int kBlocksPerSm = 3;
 constexpr int kOver = 1;                 // units that an item costs besides its tokens
 constexpr int kWhole = 4;                // units of tokens up to which a block takes a whole item
 constexpr int kMaxHeads = 1024;
@@ -61,15 +64,18 @@ __device__ __forceinline__ int view_at(const DecodeParams &p, int h) { return p.
 
 // ---- types
 
+// DP: elements of a row, padded; NB: query heads of a block, in eights with bf16
 template <typename T, int DP, int NB>
 struct Shape {
-    static constexpr int kRows = 8 * NB;                                    // query heads of a block
+    static constexpr int kRows = sizeof(T) == 2 ? 8 * NB : NB;              // query heads of a block
     static constexpr int kRowBytes = DP * (int)sizeof(T);
     static constexpr int kKeys = kStage / 2 / kRowBytes;                    // of a stage
     static constexpr int kChunks = kRowBytes / 16;
     // What a row's chunks are permuted by: eight rows of 16 bytes (bf16: ldmatrix) or the lanes of an eighth of a warp, of which
     // 32 / kKeys share a key (fp32), then fall into different banks.
     static constexpr int kSwizzle = sizeof(T) == 2 ? 1 : 32 / kKeys;
+    // (three need the registers below 168: 28 bytes of spills for 16 heads of 128 elements, 32 x 4096 tokens 28.0 us instead of 26.9)
+    static constexpr int kBlocksPerSm = sizeof(T) == 2 && DP == 128 && NB == 2 ? 2 : 3;
     __device__ static int chunk_at(int key, int chunk) { return key * kRowBytes + ((chunk ^ (key * kSwizzle & 7)) << 4); }
 };
 
@@ -388,7 +394,8 @@ struct Reader<__nv_bfloat16, DP, NB> {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) o[k][nb][i] = 0.f;
     }
-    __device__ void add(const DecodeParams &p, uint32_t stage, const Meta &meta, int lane, float *) {
+    __device__ void add(const DecodeParams &p, const char *at, const Meta &meta, int lane, float *) {
+        const uint32_t stage = ptx::smem_u32(at);
         float s[kTiles][NB][4];
 #pragma unroll
         for (int t = 0; t < kTiles; ++t)
@@ -410,7 +417,7 @@ struct Reader<__nv_bfloat16, DP, NB> {
             }
         constexpr uint32_t kFull = S::kKeys < 32 ? (1u << S::kKeys) - 1 : ~0u;
         const bool all = (meta.by_row & meta.by_col) == kFull;
-        uint32_t w[kTiles][NB][2];
+        uint32_t w[kTiles][NB][2], rest[kTiles][NB][2];
         float keep[NB][2];
         bool moved = false;
 #pragma unroll
@@ -465,7 +472,12 @@ struct Reader<__nv_bfloat16, DP, NB> {
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-                for (int half = 0; half < 2; ++half) w[t][nb][half] = transpose8(ptx::cvt_bf16x2(s[t][nb][2 * half], s[t][nb][2 * half + 1]));
+                for (int half = 0; half < 2; ++half) {
+                    const float x = s[t][nb][2 * half], y = s[t][nb][2 * half + 1];
+                    const uint32_t xy = ptx::cvt_bf16x2(x, y);
+                    w[t][nb][half] = transpose8(xy);
+                    rest[t][nb][half] = transpose8(ptx::cvt_bf16x2(x - __uint_as_float(xy << 16), y - __uint_as_float(xy & 0xffff0000u)));
+                }
 #pragma unroll
         for (int k = 0; k < DP / 16; ++k)
 #pragma unroll
@@ -473,7 +485,10 @@ struct Reader<__nv_bfloat16, DP, NB> {
                 uint32_t a[4];
                 ldmatrix4_trans(a, (value_at ^ 32 * k) + t * 16 * S::kRowBytes);
 #pragma unroll
-                for (int nb = 0; nb < NB; ++nb) mma16816(o[k][nb], a, w[t][nb]);
+                for (int nb = 0; nb < NB; ++nb) {
+                    mma16816(o[k][nb], a, w[t][nb]);
+                    mma16816(o[k][nb], a, rest[t][nb]);
+                }
             }
     }
     // The warp's result: [n_rows][d] un-normalised, then maxima and sums.
@@ -506,60 +521,64 @@ struct Reader<float, DP, NB> {
     static constexpr int kShare = 32 / S::kKeys;  // lanes that share a key
     static constexpr int kCols = DP / 32;         // columns of a lane
     float m[S::kRows], l[S::kRows], o[S::kRows][kCols];
-    int n, warp;
+    uint32_t views;  // two bits a head
 
-    // `own`: queries [kRows][DP] (of the block; every warp writes the same), then the warp's weights [kRows][kKeys] each
+    // `own`: queries [kRows][DP] (of the block; every warp writes the same), then the warps' weights [kRows][kKeys] each
     __device__ void begin(const DecodeParams &p, int b, int h0, int n_rows, int lane, float *own) {
-        warp = threadIdx.x >> 5;
         const float *Q = (const float *)p.Q + b * p.q_batch;
-        n = n_rows;
-        __syncwarp();
-        for (int i = lane; i < S::kRows * DP; i += 32) {
-            const int r = i / DP, e = i % DP;
-            own[i] = r < n_rows && e < p.d ? Q[(h0 + r) * p.q_head + e] : 0.f;
-        }
         __syncwarp();
 #pragma unroll
+        for (int i = 0; i < S::kRows * DP / 32; ++i) {
+            const int r = (i * 32 + lane) / DP, e = (i * 32 + lane) % DP;
+            own[i * 32 + lane] = r < n_rows && e < p.d ? Q[(h0 + r) * p.q_head + e] : 0.f;
+        }
+        __syncwarp();
+        views = 0;
+#pragma unroll
         for (int r = 0; r < S::kRows; ++r) {
+            views |= (uint32_t)(r < n_rows ? view_at(p, h0 + r) : MATE_VIEW_EITHER) << 2 * r;
             m[r] = -INFINITY, l[r] = 0.f;
 #pragma unroll
             for (int c = 0; c < kCols; ++c) o[r][c] = 0.f;
         }
-        views = 0;
-        for (int r = 0; r < n_rows; ++r) views |= (uint32_t)view_at(p, h0 + r) << 2 * r;
     }
-    uint32_t views;
-    __device__ void add(const DecodeParams &p, uint32_t stage, const Meta &meta, int lane, float *own) {
+    // (all kRows rows, also where the block has fewer heads: branches between them cost more than the multiply-adds)
+    __device__ void add(const DecodeParams &p, const char *stage, const Meta &meta, int lane, float *own) {
         const int key = lane / kShare, part = lane % kShare;
-        float *weights = own + S::kRows * (DP + warp * S::kKeys);
+        float *weights = own + S::kRows * (DP + (threadIdx.x >> 5) * S::kKeys);
         float s[S::kRows];
 #pragma unroll
         for (int r = 0; r < S::kRows; ++r) s[r] = 0.f;
 #pragma unroll
         for (int i = 0; i < S::kChunks / kShare; ++i) {
             const int chunk = i * kShare + part;
-            const float4 k = ptx::ld_shared_f4(stage + S::chunk_at(key, chunk));
+            const float4 k = *reinterpret_cast<const float4 *>(stage + S::chunk_at(key, chunk));
 #pragma unroll
             for (int r = 0; r < S::kRows; ++r) {
-                if (r >= n) break;
                 const float4 x = *reinterpret_cast<const float4 *>(own + r * DP + chunk * 4);
                 s[r] = fmaf(x.x, k.x, fmaf(x.y, k.y, fmaf(x.z, k.z, fmaf(x.w, k.w, s[r]))));
             }
         }
 #pragma unroll
+        for (int step = 1; step < kShare; step <<= 1)
+#pragma unroll
+            for (int r = 0; r < S::kRows; ++r) s[r] += __shfl_xor_sync(~0u, s[r], step);
+        float top[S::kRows];
+#pragma unroll
         for (int r = 0; r < S::kRows; ++r) {
-            if (r >= n) break;
             const int v = views >> 2 * r & 3;
             const uint32_t counts = (v != MATE_VIEW_COL ? meta.by_row : 0u) | (v != MATE_VIEW_ROW ? meta.by_col : 0u);
-            float x = s[r];
+            s[r] = counts >> key & 1 ? s[r] * p.scale_log2 : -INFINITY;
+            top[r] = fmaxf(m[r], s[r]);
+        }
 #pragma unroll
-            for (int step = 1; step < kShare; step <<= 1) x += __shfl_xor_sync(~0u, x, step);
-            x = counts >> key & 1 ? x * p.scale_log2 : -INFINITY;
-            float top = fmaxf(m[r], x);
+        for (int step = kShare; step < 32; step <<= 1)
 #pragma unroll
-            for (int step = kShare; step < 32; step <<= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, step));
-            const float base = top == -INFINITY ? 0.f : top, keep = ptx::ex2(m[r] - base), w = ptx::ex2(x - base);
-            m[r] = top;
+            for (int r = 0; r < S::kRows; ++r) top[r] = fmaxf(top[r], __shfl_xor_sync(~0u, top[r], step));
+#pragma unroll
+        for (int r = 0; r < S::kRows; ++r) {
+            const float base = top[r] == -INFINITY ? 0.f : top[r], keep = ptx::ex2(m[r] - base), w = ptx::ex2(s[r] - base);
+            m[r] = top[r];
             l[r] = fmaf(l[r], keep, w);  // (kShare lanes count the same key)
 #pragma unroll
             for (int c = 0; c < kCols; ++c) o[r][c] *= keep;
@@ -571,17 +590,17 @@ struct Reader<float, DP, NB> {
             float v[4][kCols];
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                const uint32_t at = stage + kStage / 2 + S::chunk_at(k0 + k, lane * kCols / 4) + (lane * kCols % 4) * 4;
+                const char *at = stage + kStage / 2 + S::chunk_at(k0 + k, lane * kCols / 4) + (lane * kCols % 4) * 4;
                 if (kCols == 4) {
-                    const float4 x = ptx::ld_shared_f4(at);
+                    const float4 x = *reinterpret_cast<const float4 *>(at);
                     v[k][0] = x.x, v[k][1] = x.y, v[k][kCols - 2] = x.z, v[k][kCols - 1] = x.w;
                 } else {
-                    asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(v[k][0]), "=f"(v[k][1]) : "r"(at));
+                    const float2 x = *reinterpret_cast<const float2 *>(at);
+                    v[k][0] = x.x, v[k][1] = x.y;
                 }
             }
 #pragma unroll
             for (int r = 0; r < S::kRows; ++r) {
-                if (r >= n) break;
                 const float4 w = *reinterpret_cast<const float4 *>(weights + r * S::kKeys + k0);
 #pragma unroll
                 for (int c = 0; c < kCols; ++c) o[r][c] = fmaf(w.x, v[0][c], fmaf(w.y, v[1][c], fmaf(w.z, v[2][c], fmaf(w.w, v[3][c], o[r][c]))));
@@ -609,7 +628,7 @@ template <typename T, int DP, int NB>
 constexpr int kExtra = sizeof(T) == 4 ? 4 * Shape<T, DP, NB>::kRows * (DP + kWarps * Shape<T, DP, NB>::kKeys) : 0;
 
 template <typename T, int DP, int NB>
-__global__ void __launch_bounds__(kThreads, kBlocksPerSm) decode_kernel(const __grid_constant__ DecodeParams p) {
+__global__ void __launch_bounds__(kThreads, Shape<T, DP, NB>::kBlocksPerSm) decode_kernel(const __grid_constant__ DecodeParams p) {
     using S = Shape<T, DP, NB>;
     extern __shared__ char smem_raw[];
     char *smem = smem_raw + (-ptx::smem_u32(smem_raw) & (kAlign - 1));
@@ -667,7 +686,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) decode_kernel(const __
             __syncwarp();
             load.fill();
             meta = s_meta[warp][t % kRing];
-            if (meta.n > 0) read.add(p, ptx::smem_u32(smem) + (warp * kRing + t % kRing) * kStage, meta, lane, own);
+            if (meta.n > 0) read.add(p, smem + (warp * kRing + t % kRing) * kStage, meta, lane, own);
             more = !meta.end;
         }
         __syncwarp();
@@ -798,12 +817,17 @@ __global__ void __launch_bounds__(kN) join_kernel(const __grid_constant__ Decode
 
 // ---- host
 
-int block_rows(const mate_cache_t *c) { return c->dtype == MATE_BF16 && c->heads / c->kv_heads > 8 ? 16 : 8; }
+// Query heads of a block: 8 or 16 with bf16, 2 or 8 with fp32
+int block_rows(const mate_cache_t *c) {
+    const int group = c->heads / c->kv_heads;
+    return c->dtype == MATE_BF16 ? group > 8 ? 16 : 8 : group > 2 ? 8 : 2;
+}
 int blocks_of_group(const mate_cache_t *c) { return (c->heads / c->kv_heads + block_rows(c) - 1) / block_rows(c); }
 // Blocks that share the work, 0 where each takes one item.
 int shares(const mate_cache_t *c, int B, int max_len) {
     const int64_t items = (int64_t)B * c->kv_heads * blocks_of_group(c), units = items * units_of(max_len);
-    const int most = kBlocksPerSm * n_sms(c->device);
+    const bool large = c->dtype == MATE_BF16 && c->d > 64 && block_rows(c) == 16;
+    const int most = (large ? Shape<__nv_bfloat16, 128, 2>::kBlocksPerSm : Shape<__nv_bfloat16, 64, 1>::kBlocksPerSm) * n_sms(c->device);
     return units <= (kOver + kWhole) * items ? 0 : (int)(units < most ? units : most);
 }
 
@@ -877,10 +901,15 @@ extern "C" int mate_attn_decode(const mate_cache_t *cache, int layer, const void
         p.partial = reinterpret_cast<float *>(p.joints + (size_t)B * cache->kv_heads * p.blocks_of_group);
     }
     cudaStream_t st = (cudaStream_t)stream;
-    const bool narrow = cache->d <= 64;
-    if (cache->dtype == MATE_F32)
-        return narrow ? launch<float, 64, 1>(p, blocks, cache->device, st) : launch<float, 128, 1>(p, blocks, cache->device, st);
-    if (block_rows(cache) == 8)
-        return narrow ? launch<__nv_bfloat16, 64, 1>(p, blocks, cache->device, st) : launch<__nv_bfloat16, 128, 1>(p, blocks, cache->device, st);
-    return narrow ? launch<__nv_bfloat16, 64, 2>(p, blocks, cache->device, st) : launch<__nv_bfloat16, 128, 2>(p, blocks, cache->device, st);
+    const auto run = [&](auto wide) {
+        constexpr int DP = wide ? 128 : 64;
+        switch (block_rows(cache)) {
+            case 2: return launch<float, DP, 2>(p, blocks, cache->device, st);
+            case 16: return launch<__nv_bfloat16, DP, 2>(p, blocks, cache->device, st);
+            default:
+                return cache->dtype == MATE_F32 ? launch<float, DP, 8>(p, blocks, cache->device, st)
+                                                : launch<__nv_bfloat16, DP, 1>(p, blocks, cache->device, st);
+        }
+    };
+    return cache->d <= 64 ? run(std::false_type()) : run(std::true_type());
 }

@@ -226,8 +226,10 @@ int launch(RopeParams &p, int device, cudaStream_t st) {
 
 // Whole runs of 16 bytes where the pairs, the rest of the row, every address and every stride allow it, else one
 // element at a time.
-int run(RopeParams &p, int dtype, int device, cudaStream_t st) {
+int run(RopeParams &p, int dtype, cudaStream_t st) {
     if (p.B == 0 || p.N == 0 || p.n_sides == 0) return MATE_OK;
+    int device = 0;
+    if (cudaGetDevice(&device) != cudaSuccess) return MATE_ERR_CUDA;
     const size_t size = elem_size(dtype);
     const int vec = (int)(16 / size);
     bool wide = p.rot % (2 * vec) == 0 && p.d % (2 * vec) == 0;
@@ -273,9 +275,7 @@ extern "C" int mate_rope(const mate_rope_tensor_t *tensors, int n_tensors, int B
         s.x = t.x, s.y = t.y, s.heads = t.heads, s.turned = rot > 0;
         for (int j = 0; j < 3; ++j) s.xs[j] = t.x_stride[j], s.ys[j] = t.y_stride[j];
     }
-    int device = 0;
-    if (cudaGetDevice(&device) != cudaSuccess) return MATE_ERR_CUDA;
-    return run(p, dtype, device, (cudaStream_t)stream);
+    return run(p, dtype, (cudaStream_t)stream);
 }
 
 extern "C" int mate_cache_append(const mate_cache_t *cache, int layer, const void *K, const void *V, const int64_t *k_stride,
@@ -309,5 +309,5 @@ extern "C" int mate_cache_append(const mate_cache_t *cache, int layer, const voi
     p.paged = 1;
     p.cache = cache_args(cache, layer);
     p.seqs = seqs, p.counts = counts, p.row_ids = row_ids, p.col_ids = col_ids;
-    return run(p, cache->dtype, cache->device, (cudaStream_t)stream);
+    return run(p, cache->dtype, (cudaStream_t)stream);
 }

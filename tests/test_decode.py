@@ -24,8 +24,8 @@ def bounds(q, k, v, want, scale, dtype):
     sums = (n + 40) * 2.0 ** -24   # sums over the keys, joined over warps and blocks, and one division
     top = np.abs(v).max()
     o = (2 * w + 2 * sums) * top
-    if dtype == "bf16":            # weights rounded to bf16, and the result: half a step each
-        o += 2.0 ** -8 * top + 2.0 ** -8 * np.abs(want[0])
+    if dtype == "bf16":            # weights as the sum of two bf16 (half a step of half a step), the result rounded to bf16
+        o += 2.0 ** -16 * top + 2.0 ** -8 * np.abs(want[0])
     return o, w + sums + x + 2.0 ** -22 * (1 + abs(want[1]))
 
 
