@@ -27,13 +27,16 @@ namespace mate {
 namespace {
 
 constexpr int kWarps = 4, kThreads = 32 * kWarps;
+constexpr int kManyWarps = 8;            // of a block that has an item and an SM to itself
 constexpr int kUnit = 32 * kWarps;       // tokens of a unit of work: what the warps look through in one go
 constexpr int kStage = 8192;             // bytes of a stage: keys, then values
 constexpr int kAlign = 256;              // of the ring: the longest row of tensor-core operands
 constexpr int kRing = 2;                 // stages of a warp
 constexpr int kList = 64;                // entries of a warp's list of places: less than a stage, and one look
-constexpr int kOver = 1;                 // units that an item costs besides its tokens
-constexpr int kWhole = 4;                // units of tokens up to which a block takes a whole item
+constexpr int kOver = 1;                 // units that an item costs besides its tokens (0, 1, 2, 3: 64 sequences 79.7, 77.7, 78.8, 80.0 us)
+// Units of tokens up to which a block takes a whole item.  One sequence of 12 heads and 400 tokens 7.0 us whole, 7.8 shared out and
+// joined; of 1000 tokens 10.0 whole, 7.9 shared out (64 sequences of up to 1000: 21.4 and 21.2).
+constexpr int kWhole = 4;
 constexpr int kMaxHeads = 1024;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
@@ -211,8 +214,9 @@ struct Meta {  // of a stage
 };
 enum { kNoPart = 0, kAll = 1, kBegins = 2, kGoesOn = 3 };  // Meta.state: behind the last one; an item; its first units; others
 
-template <typename T, int DP, int NB>
+template <typename T, int DP, int NB, int W>
 struct Loader {
+    static constexpr int kStep = 32 * W;  // tokens that the block's warps look through in one go
     using S = Shape<T, DP, NB>;
     const DecodeParams &p;
     uint32_t *list;  // places, in 16 bytes from the cache's beginning
@@ -227,7 +231,7 @@ struct Loader {
     int s, prefix, q_row, q_col, end;
     unsigned head_at;
     bool text, need_row, need_col;
-    int next;                           // first of the 32 tokens that are looked at next; 32 of every kUnit are the warp's
+    int next;                           // first of the 32 tokens that are looked at next; 32 of every kStep are the warp's
     bool there;                         // the lane's token there exists; its ids have been asked for
     unsigned at;
     int row, col;
@@ -282,7 +286,7 @@ struct Loader {
         if (text) need_row = true, need_col = false;  // padding has neither
         list_at = 0;
         ask_ids();
-        ask_page(next + kUnit + lane);
+        ask_page(next + kStep + lane);
     }
     // One look at 32 tokens: those that count go onto the list, the next ones' ids are asked for.
     __device__ void look() {
@@ -296,10 +300,10 @@ struct Loader {
             if (need_row && need_col) marks[to] = (by_row ? 1 : 0) | (by_col ? 2 : 0);
         }
         pending += __popc(counts);
-        next += kUnit;
+        next += kStep;
         if (next < end) {
             ask_ids();
-            ask_page(next + kUnit + lane);
+            ask_page(next + kStep + lane);
         }
     }
     // Copies of the next stage are put under way (or, at the end of the share, none: the groups are counted).
@@ -624,29 +628,30 @@ struct Reader<float, DP, NB> {
 };
 
 // Bytes of shared memory behind the ring: fp32's queries and weights.
-template <typename T, int DP, int NB>
-constexpr int kExtra = sizeof(T) == 4 ? 4 * Shape<T, DP, NB>::kRows * (DP + kWarps * Shape<T, DP, NB>::kKeys) : 0;
+template <typename T, int DP, int NB, int W>
+constexpr int kExtra = sizeof(T) == 4 ? 4 * Shape<T, DP, NB>::kRows * (DP + W * Shape<T, DP, NB>::kKeys) : 0;
 
-template <typename T, int DP, int NB>
-__global__ void __launch_bounds__(kThreads, Shape<T, DP, NB>::kBlocksPerSm) decode_kernel(const __grid_constant__ DecodeParams p) {
+// W = kManyWarps: every block takes an item
+template <typename T, int DP, int NB, int W>
+__global__ void __launch_bounds__(32 * W, W == kWarps ? Shape<T, DP, NB>::kBlocksPerSm : 1) decode_kernel(const __grid_constant__ DecodeParams p) {
     using S = Shape<T, DP, NB>;
     extern __shared__ char smem_raw[];
     char *smem = smem_raw + (-ptx::smem_u32(smem_raw) & (kAlign - 1));
-    __shared__ __align__(16) uint32_t s_list[kWarps][kList];
-    __shared__ uint8_t s_marks[kWarps][kList];
-    __shared__ Meta s_meta[kWarps][kRing];
-    __shared__ __align__(8) float s_stats[kWarps][2 * S::kRows];
-    __shared__ int s_out_at[kWarps];
+    __shared__ __align__(16) uint32_t s_list[W][kList];
+    __shared__ uint8_t s_marks[W][kList];
+    __shared__ Meta s_meta[W][kRing];
+    __shared__ __align__(8) float s_stats[W][2 * S::kRows];
+    __shared__ int s_out_at[W];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, items = p.kv_heads * p.blocks_of_group;
     const int max_rows = min(S::kRows, p.group);
-    float *own = reinterpret_cast<float *>(smem + kWarps * kRing * kStage);
+    float *own = reinterpret_cast<float *>(smem + W * kRing * kStage);
     if (p.d < DP)  // columns that no copy writes
-        for (int i = tid; i < kWarps * kRing * kStage / 16; i += kThreads) reinterpret_cast<uint4 *>(smem)[i] = make_uint4(0, 0, 0, 0);
+        for (int i = tid; i < W * kRing * kStage / 16; i += 32 * W) reinterpret_cast<uint4 *>(smem)[i] = make_uint4(0, 0, 0, 0);
     ptx::wait_prior_grid();
 
     Walk walk;
     Start start = {};
-    if (p.joints) {
+    if (W == kWarps && p.joints) {
         start = find_start(p, items);
         if (blockIdx.x >= start.blocks) return;
         const unsigned at = share(start.total, start.blocks, blockIdx.x);
@@ -665,7 +670,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, DP, NB>::kBlocksPerSm) deco
         __syncthreads();
     }
 
-    Loader<T, DP, NB> load = {p, s_list[warp], s_marks[warp], s_meta[warp], ptx::smem_u32(smem) + warp * kRing * kStage, lane, warp, items, walk};
+    Loader<T, DP, NB, W> load = {p, s_list[warp], s_marks[warp], s_meta[warp], ptx::smem_u32(smem) + warp * kRing * kStage, lane, warp, items, walk};
     load.bad = false, load.pending = load.list_at = load.filled = 0;
     load.begin();
     for (int i = 0; i < kRing - 1; ++i) load.fill();
@@ -700,11 +705,11 @@ __global__ void __launch_bounds__(kThreads, Shape<T, DP, NB>::kBlocksPerSm) deco
         const int slot = first ? 0 : 1, e = tid % DP;
         float *to = p.partial + (size_t)(2 * blockIdx.x + slot) * max_rows * (p.d + 2);
 #pragma unroll 4
-        for (int r = tid / DP; r < n_rows; r += kThreads / DP) {
-            float2 stat[kWarps];
-            float x[kWarps], top = -INFINITY;
+        for (int r = tid / DP; r < n_rows; r += 32 * W / DP) {
+            float2 stat[W];
+            float x[W], top = -INFINITY;
 #pragma unroll
-            for (int w = 0; w < kWarps; ++w) {
+            for (int w = 0; w < W; ++w) {
                 stat[w] = *reinterpret_cast<const float2 *>(&s_stats[w][2 * r]);
                 x[w] = e < p.d ? *reinterpret_cast<const float *>(smem + s_out_at[w] + 4 * (r * p.d + e)) : 0.f;
                 top = fmaxf(top, stat[w].x);
@@ -712,7 +717,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, DP, NB>::kBlocksPerSm) deco
             const float base = top == -INFINITY ? 0.f : top;
             float sum = 0.f, y = 0.f;
 #pragma unroll
-            for (int w = 0; w < kWarps; ++w) {
+            for (int w = 0; w < W; ++w) {
                 const float f = ptx::ex2(stat[w].x - base);
                 sum = fmaf(f, stat[w].y, sum);
                 y = fmaf(f, x[w], y);
@@ -731,7 +736,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, DP, NB>::kBlocksPerSm) deco
         if (p.d < DP)
             for (int i = lane; i < kStage / 16; i += 32) reinterpret_cast<uint4 *>(smem + warp * kRing * kStage + out_at)[i] = make_uint4(0, 0, 0, 0);
         first = false;
-        if (p.joints && tid == 0) {
+        if (W == kWarps && p.joints && tid == 0) {
             Joint &joint = p.joints[part.b * items + part.item];
             if (part.state == kAll) joint.slot = -1;
             if (part.state == kBegins) {  // the share's last part: who has the item's last unit?
@@ -831,24 +836,31 @@ int shares(const mate_cache_t *c, int B, int max_len) {
     return units <= (kOver + kWhole) * items ? 0 : (int)(units < most ? units : most);
 }
 
+template <typename T, int DP, int NB, int W>
+int launch_warps(const DecodeParams &p, unsigned grid, int device, cudaStream_t st) {
+    static SmemAttrOnce attr;
+    constexpr int kSmem = kAlign + W * kRing * kStage + kExtra<T, DP, NB, W>;
+    const int rc = attr.ensure((const void *)decode_kernel<T, DP, NB, W>, kSmem, device);
+    if (rc != MATE_OK) return rc;
+    return launch_after(decode_kernel<T, DP, NB, W>, dim3(grid), 32 * W, kSmem, st, p) == cudaSuccess ? MATE_OK : MATE_ERR_CUDA;
+}
 template <typename T, int DP, int NB>
 int launch(const DecodeParams &p, int blocks, int device, cudaStream_t st) {
-    static SmemAttrOnce attr;
-    using S = Shape<T, DP, NB>;
-    const int rows = S::kRows < p.group ? S::kRows : p.group;
-    constexpr int kSmem = kAlign + kWarps * kRing * kStage + kExtra<T, DP, NB>;
-    int rc = attr.ensure((const void *)decode_kernel<T, DP, NB>, kSmem, device);
+    constexpr int kRows = Shape<T, DP, NB>::kRows;
+    const int rows = kRows < p.group ? kRows : p.group, items = p.kv_heads * p.blocks_of_group;
+    const int64_t all = (int64_t)p.B * items;
+    // An item to each block; where there is an SM for each, eight warps: 12 items of 64 elements and 250 or 512 tokens 4.6 and 5.4 us
+    // (with four 5.6 and 6.1), 8 items of 4 heads of 128 elements 6.3 and 7.1 (8.0 and 8.2).
+    if (!blocks)
+        return all <= n_sms(device) ? launch_warps<T, DP, NB, kManyWarps>(p, (unsigned)all, device, st)
+                                    : launch_warps<T, DP, NB, kWarps>(p, (unsigned)all, device, st);
+    const int rc = launch_warps<T, DP, NB, kWarps>(p, (unsigned)blocks, device, st);
     if (rc != MATE_OK) return rc;
-    const int items = p.kv_heads * p.blocks_of_group;
-    const int64_t grid = blocks ? blocks : (int64_t)p.B * items;
-    if (grid > INT32_MAX) return MATE_ERR_UNSUPPORTED;
-    if (launch_after(decode_kernel<T, DP, NB>, dim3((unsigned)grid), kThreads, kSmem, st, p) != cudaSuccess) return MATE_ERR_CUDA;
-    if (!blocks) return MATE_OK;
     // few items in many parts: more threads each
     const dim3 joins((unsigned)(p.B * items), (unsigned)rows);
     const size_t bytes = sizeof(float) * blocks;
-    return (blocks > 16 * p.B * items ? launch_after(join_kernel<T, 1024>, joins, 1024, bytes, st, p, S::kRows)
-                                      : launch_after(join_kernel<T, 128>, joins, 128, bytes, st, p, S::kRows)) == cudaSuccess
+    return (blocks > 16 * p.B * items ? launch_after(join_kernel<T, 1024>, joins, 1024, bytes, st, p, kRows)
+                                      : launch_after(join_kernel<T, 128>, joins, 128, bytes, st, p, kRows)) == cudaSuccess
                ? MATE_OK
                : MATE_ERR_CUDA;
 }
