@@ -285,7 +285,7 @@ int mate_attn_bwd_noalloc(const mate_plan_t *plan, const void *Q, const void *K,
  *   positions  device int32, position of token n of example b at positions[b * position_stride + n] (stride 0: one
  *              row for all examples).  Any value: the angle is formed in 64 bits.  For a table whose positions start
  *              again in every cell the caller says so here.
- *   freqs      device float64 [rot / 2], radians per position (scaled for long contexts as the caller likes)
+ *   freqs      device float64 [rot / 2], radians per position, finite (scaled for long contexts as the caller likes)
  * rot is even, 0 <= rot <= d <= 1024.  For packed batches B = 1 and N = T.  Asynchronous on `stream`; no
  * workspace.  Bound by memory: every element is read once and written once. */
 typedef struct {
@@ -367,7 +367,7 @@ int mate_cache_fork(const mate_cache_t *cache, const int32_t *parents, const int
                     size_t workspace_bytes, void *stream);
 
 /* Every sequence of the list (null: 0 .. n - 1) becomes empty: its pages lose a reference, its row of the table becomes -1, its length 0.
- * Sequences that are empty already are no error, so one may stand in the list twice. */
+ * Sequences that are empty already are no error, so one may stand in the list twice.  prefix stays as it is. */
 int mate_cache_free(const mate_cache_t *cache, const int32_t *seqs, int n, void *stream);
 
 /* Moves the pages in use to the front: afterwards pages 0 .. n_live - 1 are in use and all others free.  The pages

@@ -357,7 +357,9 @@ def mate_rope(Q, positions, freqs, K=None, interleaved=False, mscale=1.0, backwa
     tensors.  Returns Q' or (Q', K')."""
     if _lib is None:
         _load()
-    q, k = (out, None) if K is None else (None, None) if out is None else out
+    if K is not None and out is not None and not (isinstance(out, (tuple, list)) and len(out) == 2):
+        raise ValueError("out must be a pair of tensors where Q and K are given")
+    q, k = (out, None) if K is None else out or (None, None)
     return _cache_calls.rope(Q, K, positions, freqs, interleaved, mscale, backward, q, k)
 
 
@@ -366,7 +368,8 @@ class Cache:
 
     k, v: [layers, pages, kv_heads, page_size, d] bf16 or f32 (a cache laid out slot by slot is passed as a transposed view);
     row_ids, col_ids: int32 [pages, page_size]; table: int32 [seqs, width]; lens, prefix: int32 [seqs]; refs: int32 [pages];
-    head_view: VIEW_ROW, VIEW_COL or VIEW_EITHER for every query head."""
+    head_view: VIEW_ROW, VIEW_COL or VIEW_EITHER for every query head.  The calls go by the tensors given here: change them in
+    place (cache.prefix[s] = 128), not for others."""
 
     def __init__(self, k, v, row_ids, col_ids, table, lens, prefix, refs, head_view):
         _load()

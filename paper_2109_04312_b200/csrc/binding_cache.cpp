@@ -209,7 +209,8 @@ PyObject *new_cache(PyObject *, PyObject *const *a, Py_ssize_t n) {
             fail_shape("k and v", "of one type and shape, [layers, pages, kv_heads, page_size, d]");
         const int dt = dtype_code(k);
         rows(k, "k"), rows(v, "v");
-        if (k.strides() != v.strides() || !distinct(k)) fail_shape("k and v", "laid out alike, without elements that share their memory");
+        if (k.strides() != v.strides() || !distinct(k) || (k.numel() && k.data_ptr() == v.data_ptr()))
+            fail_shape("k and v", "laid out alike, without elements that share their memory");
         if (!THPVariable_Check(a[4]) || THPVariable_Unpack(a[4]).dim() != 2) fail_shape("table", "an int32 CUDA tensor [seqs, width]");
         const at::Tensor &table = THPVariable_Unpack(a[4]);
         if (!PyBytes_Check(a[9])) fail_shape("head_view", "bytes");

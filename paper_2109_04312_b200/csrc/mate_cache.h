@@ -65,7 +65,8 @@ __host__ __device__ inline int clip_len(int len, int most, bool *bad) {
 }
 // Owner of the r-th of the things that the entries want, off[i] being what those in front of entry i want, off[0] = 0 <= r: the
 // last entry with off[i] <= r.
-__host__ __device__ inline int owner_of(const int *off, int n, int r) {
+template <typename N>
+__host__ __device__ inline int owner_of(const N *off, int n, int r) {
     int lo = 0, hi = n;
     while (hi - lo > 1) {
         const int mid = (lo + hi) / 2;

@@ -249,8 +249,8 @@ struct SmemAttrOnce {
 
 // Launches a kernel that may start while the one in front of it in the stream drains: all kernels that are launched so
 // wait for the one before (griddepcontrol.wait) before they read or write anything that another kernel writes or reads, and
-// all but those of mate_simt.cu let the next one start early (griddepcontrol.launch_dependents; the fp32 forward takes 48.7 us
-// instead of 36.8 in an earlier form, where blocks of the next kernel pile up on the SMs that finish first).  Takes the launch gap (about 2 us)
+// all but those of mate_simt.cu and mate_decode.cu's first let the next one start early (griddepcontrol.launch_dependents; the fp32
+// forward takes 48.7 us instead of 36.8 in an earlier form, where blocks of the next kernel pile up on the SMs that finish first).  Takes the launch gap (about 2 us)
 // and the set-up of the tensor-core kernels out of a layer's time.
 template <typename... P, typename... A>
 cudaError_t launch_after(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t stream, A &&...args) {

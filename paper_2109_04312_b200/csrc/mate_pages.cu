@@ -21,24 +21,25 @@ constexpr int kEarly = 16;       // pages of a thread whose reference counts are
 constexpr int kCopyThreads = 128, kCopyBlocks = 8;  // blocks per SM
 
 // Exclusive sum over the block's threads; *total gets the sum.  All threads call it.
-__device__ int block_scan(int x, int *total) {
-    __shared__ int s_warp[kThreads / 32 + 1];
+template <typename N>
+__device__ N block_scan(N x, N *total) {
+    __shared__ N s_warp[kThreads / 32 + 1];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    int sum = x;
+    N sum = x;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-        const int y = __shfl_up_sync(~0u, sum, o);
+        const N y = __shfl_up_sync(~0u, sum, o);
         if (lane >= o) sum += y;
     }
     __syncthreads();  // an earlier scan has been read
     if (lane == 31) s_warp[warp] = sum;
     __syncthreads();
     if (warp == 0) {
-        const int w = s_warp[lane];
-        int t = w;
+        const N w = s_warp[lane];
+        N t = w;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const int y = __shfl_up_sync(~0u, t, o);
+            const N y = __shfl_up_sync(~0u, t, o);
             if (lane >= o) t += y;
         }
         s_warp[lane] = t - w;
@@ -70,7 +71,8 @@ __device__ __forceinline__ int claim_of(int i) { return INT32_MIN + i; }
 
 __global__ void __launch_bounds__(kThreads, 1) extend_kernel(const __grid_constant__ CacheArgs c, const int32_t *seqs, const int32_t *counts, int n,
                                                           int32_t *granted) {
-    __shared__ int s_off[kMost + 1], s_used;
+    __shared__ int64_t s_off[kMost + 1];  // (the list may want more pages than 32 bits count)
+    __shared__ int s_used;
     ptx::launch_dependents();
     ptx::wait_prior_grid();
     const int tid = threadIdx.x, i0 = tid * kPer;
@@ -100,7 +102,7 @@ __global__ void __launch_bounds__(kThreads, 1) extend_kernel(const __grid_consta
     for (int j = 0; j < kPer; ++j)
         if (s[j] >= 0) atomicMin(&c.lens[s[j]], claim_of(i0 + j));
     __syncthreads();
-    int sum = 0;
+    int64_t sum = 0;
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
         if (s[j] >= 0 && __ldcg(&c.lens[s[j]]) != claim_of(i0 + j)) {
@@ -110,8 +112,8 @@ __global__ void __launch_bounds__(kThreads, 1) extend_kernel(const __grid_consta
         if (s[j] >= 0) need[j] = pages_of(len[j] + count[j], c.page_size) - pages_of(len[j], c.page_size);
         sum += need[j];
     }
-    int wanted;
-    int off = block_scan(sum, &wanted);
+    int64_t wanted;
+    int64_t off = block_scan(sum, &wanted);
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
         s_off[i0 + j] = off;
@@ -126,10 +128,10 @@ __global__ void __launch_bounds__(kThreads, 1) extend_kernel(const __grid_consta
     int used = 0;
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
-        const int end = s_off[i0 + j] + need[j];
+        const int64_t end = s_off[i0 + j] + need[j];
         const bool fits = s[j] >= 0 && (need[j] == 0 || end <= n_free);
         if (s[j] >= 0 && !fits) status |= kCacheFull;
-        if (fits && need[j] > 0) used = max(used, end);
+        if (fits && need[j] > 0) used = max(used, (int)end);
         if (s[j] >= 0) c.lens[s[j]] = fits ? len[j] + count[j] : len[j];
         if (i0 + j < n) granted[i0 + j] = fits ? count[j] : 0;
     }
@@ -142,8 +144,8 @@ __global__ void __launch_bounds__(kThreads, 1) extend_kernel(const __grid_consta
         const int i = owner_of(s_off, min(n, kMost), rank), q = seq_of(seqs, i, c.seqs);
         // the owner's new length is known: its pages end there
         const int at = pages_of(__ldcg(&c.lens[q]), c.page_size);
-        const int end = i + 1 < kMost ? s_off[i + 1] : wanted;
-        c.table[(size_t)q * c.width + at - (end - rank)] = p;
+        const int64_t end = i + 1 < kMost ? s_off[i + 1] : wanted;
+        c.table[(size_t)q * c.width + at - (int)(end - rank)] = p;
         c.refs[p] = 1;
         ++rank;
     }

@@ -11,4 +11,5 @@ int clip_len_(int len, int most, int *bad) {
     return r;
 }
 int owner_of_(const int *off, int n, int r) { return mate::owner_of(off, n, r); }
+int owner_of_64(const int64_t *off, int n, int r) { return mate::owner_of(off, n, r); }
 }

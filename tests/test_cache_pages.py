@@ -65,7 +65,7 @@ def append(m, c, model, seqs, counts, next_mark, ids=True):
 @pytest.mark.gpu
 @pytest.mark.parametrize("kw", [dict(), dict(slots_first=True, page_size=3, d=8, kv_heads=1), dict(dtype=torch.float32, page_size=1, width=20),
                                 dict(page_size=5, kv_heads=3, heads=6, d=40, seqs=9, pages=23, width=5, layers=1),
-                                dict(page_size=16, d=128, kv_heads=4, seqs=12, pages=1500, width=40, slots_first=True, layers=3)])
+                                dict(page_size=16, d=128, kv_heads=4, seqs=12, pages=260, width=40, slots_first=True, layers=3)])
 @pytest.mark.parametrize("seed", range(3))
 def test_a_history_of_calls(kw, seed):
     import paper_2109_04312_b200 as m
@@ -272,6 +272,23 @@ def test_long_lists_and_many_pages():
 
 
 @pytest.mark.gpu
+def test_wishes_beyond_32_bits():
+    # together the list wants 2^31 pages and more; whoever fits in front of it gets theirs, nobody behind it
+    import paper_2109_04312_b200 as m
+    S, W = 4096, 530000
+    c = m.Cache.empty(70, 1, 1, 8, S, W, [0])
+    counts = torch.full((S,), W, dtype=torch.int32, device="cuda")
+    counts[0], counts[2], counts[-1] = 60, 0, 1
+    granted = m.mate_cache_extend(c, None, counts)
+    want = torch.zeros_like(granted)
+    want[0] = 60
+    assert torch.equal(granted, want) and torch.equal(c.lens, want)
+    assert c.table[0, :60].tolist() == list(range(60)) and int((c.table >= 0).sum()) == 60 and int(c.refs.sum()) == 60
+    with pytest.raises(m.MateError, match="out of memory"):
+        c.status()
+
+
+@pytest.mark.gpu
 def test_a_step_in_a_graph():
     # extend and append captured once, replayed for token after token; forks and frees between the replays
     import paper_2109_04312_b200 as m
@@ -411,6 +428,8 @@ def test_refusals_of_the_binding():
             cache(**kw)
     with pytest.raises(ValueError, match="CUDA"):
         cache()
+    with pytest.raises(ValueError, match="^k and v"):
+        cache(_1=k)
     with pytest.raises(TypeError):
         cache(_0=k.half(), _1=k.half())
 
@@ -441,3 +460,5 @@ def test_index_arithmetic(arithmetic):
         owners = np.repeat(np.arange(len(need)), need)
         for r, want in enumerate(owners):
             assert a.owner_of_(off.ctypes.data_as(ctypes.c_void_p), len(need), r) == want
+            long = np.concatenate([off[:-1], [2 ** 40]]).astype(np.int64)   # the last one wants more than there can be
+            assert a.owner_of_64(long.ctypes.data_as(ctypes.c_void_p), len(need), r) == want

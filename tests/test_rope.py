@@ -169,6 +169,8 @@ def test_refusals():
             call()
     with pytest.raises(TypeError):
         m.mate_rope(x.half(), pos, f)
+    with pytest.raises(ValueError, match="pair"):
+        m.mate_rope(x, pos, f, K=x, out=torch.zeros(2, 1, 2, 3, 8, device="cuda"))
     with pytest.raises(m.MateError):
         m.mate_rope(torch.zeros(1, 1, 3, 1026, device="cuda"), pos, f)
 
