@@ -40,9 +40,10 @@ constexpr int kAlign = 256;              // of the ring: the longest row of tens
 constexpr int kRing = 2;                 // stages of a warp
 constexpr int kList = 64;                // entries of a warp's list of places: less than a stage, and one look
 constexpr int kOver = 1;                 // units that an item costs besides its tokens (0, 1, 2, 3: 64 sequences 79.7, 77.7, 78.8, 80.0 us)
-// Units of tokens up to which a block takes a whole item.  One sequence of 12 heads and 400 tokens 7.0 us whole, 7.8 shared out and
-// joined; of 1000 tokens 10.0 whole, 7.9 shared out (64 sequences of up to 1000: 21.4 and 21.2).
-constexpr int kWhole = 4;
+// Units of tokens up to which a block takes a whole item: for few items, and for many.  One sequence of 12 heads and 400 tokens 7.0 us
+// whole, 7.8 shared out and joined; eight items of 128 elements and 1000 tokens 11.1 whole, 9.4 shared out.  Four sequences of 12 heads
+// and up to 700 tokens 7.1 whole, 8.7 shared out, 40 of up to 1000 16.4 and 17.3 (cells 9.2 and 14.3); up to 1500 22.0 and 21.3.
+constexpr int kWhole = 4, kWholeOfMany = 8, kMany = 32;
 constexpr int kMaxHeads = 1024;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
@@ -839,7 +840,7 @@ int shares(const mate_cache_t *c, int B, int max_len) {
     const int64_t items = (int64_t)B * c->kv_heads * blocks_of_group(c), units = items * units_of(max_len);
     const bool large = c->dtype == MATE_BF16 && c->d > 64 && block_rows(c) == 16;
     const int most = (large ? Shape<__nv_bfloat16, 128, 2>::kBlocksPerSm : Shape<__nv_bfloat16, 64, 1>::kBlocksPerSm) * n_sms(c->device);
-    return units <= (kOver + kWhole) * items ? 0 : (int)(units < most ? units : most);
+    return units <= (kOver + (items < kMany ? kWhole : kWholeOfMany)) * items ? 0 : (int)(units < most ? units : most);
 }
 
 template <typename T, int DP, int NB, int W>
