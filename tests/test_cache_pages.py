@@ -203,7 +203,7 @@ def test_contents_that_make_no_sense_are_left_out():
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("interleaved", [False, True])
-@pytest.mark.parametrize("d,rot", [(64, 64), (64, 16), (24, 20), (128, 128)])
+@pytest.mark.parametrize("d,rot", [(64, 64), (64, 16), (24, 20), (128, 128), (40, 24), (80, 40)])
 def test_append_rotates(d, rot, interleaved, dtype):
     import paper_2109_04312_b200 as m
     T = {"f32": torch.float32, "bf16": torch.bfloat16}[dtype]

@@ -34,7 +34,8 @@ def check(got, x, pos, freqs, dtype, **kw):
 @pytest.mark.parametrize("interleaved", [False, True])
 @pytest.mark.parametrize("B,H,Hk,N,d,rot", [(1, 1, 1, 1, 2, 2), (1, 4, 4, 1, 64, 64), (2, 3, 1, 17, 64, 32), (3, 5, 2, 33, 40, 20), (1, 2, 2, 5, 33, 6),
                                             (2, 12, 12, 130, 64, 64), (1, 32, 8, 47, 128, 128), (1, 1, 3, 19, 1024, 512),
-                                            (1, 2, 1, 3, 1023, 1022), (2, 7, 1, 16, 128, 0), (1, 3, 2, 9, 48, 16)])
+                                            (1, 2, 1, 3, 1023, 1022), (2, 7, 1, 16, 128, 0), (1, 3, 2, 9, 48, 16), (2, 3, 2, 19, 80, 40),
+                                            (1, 2, 3, 21, 24, 8), (3, 1, 1, 5, 128, 72)])
 def test_rope(B, H, Hk, N, d, rot, interleaved, dtype):
     import paper_2109_04312_b200 as m
     g = torch.Generator().manual_seed(B * 1000 + d)
