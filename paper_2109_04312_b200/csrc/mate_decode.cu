@@ -829,10 +829,10 @@ __global__ void __launch_bounds__(kN) join_kernel(const __grid_constant__ Decode
 
 // ---- host
 
-// Query heads of a block: 8 or 16 with bf16, 2 or 8 with fp32
+// Query heads of a block: 8 or 16 with bf16, 2, 4 or 8 with fp32
 int block_rows(const mate_cache_t *c) {
     const int group = c->heads / c->kv_heads;
-    return c->dtype == MATE_BF16 ? group > 8 ? 16 : 8 : group > 2 ? 8 : 2;
+    return c->dtype == MATE_BF16 ? group > 8 ? 16 : 8 : group > 4 ? 8 : group > 2 ? 4 : 2;
 }
 int blocks_of_group(const mate_cache_t *c) { return (c->heads / c->kv_heads + block_rows(c) - 1) / block_rows(c); }
 // Blocks that share the work, 0 where each takes one item.
@@ -924,6 +924,7 @@ extern "C" int mate_attn_decode(const mate_cache_t *cache, int layer, const void
         constexpr int DP = wide ? 128 : 64;
         switch (block_rows(cache)) {
             case 2: return launch<float, DP, 2>(p, blocks, cache->device, st);
+            case 4: return launch<float, DP, 4>(p, blocks, cache->device, st);
             case 16: return launch<__nv_bfloat16, DP, 2>(p, blocks, cache->device, st);
             default:
                 return cache->dtype == MATE_F32 ? launch<float, DP, 8>(p, blocks, cache->device, st)
