@@ -245,15 +245,23 @@ struct PageShape {
     int64_t page_stride, head_stride, slot_stride, layer_stride;  // bytes
     int heads, row_bytes, layers, page_size;
 };
-// Copies one page of one layer's keys or values, its first `fill` slots.  Units of 16 bytes, kFlight of a thread under way; the
-// quotients by way of fp32 (exact: rows are fewer than 2^21, the host sees to that).
-__device__ __forceinline__ void copy_page(const PageShape &sh, char *base, int src, int dst, int fill) {
+// Copies a piece of one page of one layer's keys or values, of whose slots the first `fill` count.  Units of 16 bytes, kPiece of them to
+// a block, kFlight of a thread under way; the quotients by way of fp32 (exact: rows are fewer than 2^21, the host sees to that).
+// Compaction, whose pages are whole: small pieces (a few pages of 196 KB in two layers 6.9 us, 8.9 with 2048 units, 24.6 with a page to
+// each block).  Forks, whose pages are filled in part: larger ones (64 pages of 98 KB in twelve layers 19.0 us, 30.6 with 512 units).
+constexpr int kMovePiece = 512, kForkPiece = 2048;
+template <int kPiece>
+__host__ __device__ inline int pieces_of(const PageShape &sh) {
+    return (sh.heads * sh.page_size * (sh.row_bytes / 16) + kPiece - 1) / kPiece;
+}
+template <int kPiece>
+__device__ __forceinline__ void copy_piece(const PageShape &sh, char *base, int src, int dst, int fill, int piece) {
     const char *from = base + src * sh.page_stride;
     char *to = base + dst * sh.page_stride;
-    const int per_row = sh.row_bytes / 16, n = sh.heads * fill * per_row;
+    const int per_row = sh.row_bytes / 16, n = min(sh.heads * fill * per_row, (piece + 1) * kPiece);
     const float by_fill = 1.f / (float)fill;
     constexpr int kFlight = 4;
-    for (int i = threadIdx.x; i < n; i += kCopyThreads * kFlight) {
+    for (int i = piece * kPiece + threadIdx.x; i < n; i += kCopyThreads * kFlight) {
         uint4 v[kFlight];
         int64_t at[kFlight];
 #pragma unroll
@@ -276,7 +284,7 @@ __device__ __forceinline__ void copy_ids(const CacheArgs &c, int src, int dst, i
     }
 }
 
-// grid: (entry, layer and keys / values; one more for the table and the ids)
+// grid: (entry, layer and keys / values, piece of the page); one more layer's block for the table and the ids
 __global__ void __launch_bounds__(kCopyThreads, kCopyBlocks) fork_copy_kernel(const __grid_constant__ CacheArgs c, const __grid_constant__ PageShape sh,
                                                                  const ForkItem *items) {
     ptx::launch_dependents();
@@ -286,9 +294,10 @@ __global__ void __launch_bounds__(kCopyThreads, kCopyBlocks) fork_copy_kernel(co
     const int part = blockIdx.y;
     if (part < 2 * sh.layers) {
         if (it.src < 0 || it.dst < 0) return;
-        copy_page(sh, (char *)(part & 1 ? c.v : c.k) + (part >> 1) * sh.layer_stride, it.src, it.dst, it.fill);
+        copy_piece<kForkPiece>(sh, (char *)(part & 1 ? c.v : c.k) + (part >> 1) * sh.layer_stride, it.src, it.dst, it.fill, blockIdx.z);
         return;
     }
+    if (blockIdx.z > 0) return;
     if (it.src >= 0 && it.dst >= 0) copy_ids(c, it.src, it.dst, it.fill, threadIdx.x, kCopyThreads);
     const int32_t *from = c.table + (size_t)it.parent * c.width;
     int32_t *to = c.table + (size_t)it.child * c.width;
@@ -374,18 +383,23 @@ __global__ void __launch_bounds__(kThreads, 1) compact_kernel(const __grid_const
     }
 }
 
-// Blocks take (move, layer, keys / values) in turn, and then the table's rows.
+// Blocks take the tasks in turn, and then the table's rows.
 __global__ void __launch_bounds__(kCopyThreads, kCopyBlocks) compact_copy_kernel(const __grid_constant__ CacheArgs c, const __grid_constant__ PageShape sh,
                                                                     Moves m) {
     ptx::launch_dependents();
     ptx::wait_prior_grid();
-    const int n_moves = m.n[0], parts = 2 * sh.layers + 1;
-    for (int64_t w = blockIdx.x; w < (int64_t)n_moves * parts; w += gridDim.x) {
-        const int i = (int)(w / parts), part = (int)(w - (int64_t)i * parts), src = m.from[i], dst = m.to[i];
-        if (part < 2 * sh.layers)
-            copy_page(sh, (char *)(part & 1 ? c.v : c.k) + (part >> 1) * sh.layer_stride, src, dst, c.page_size);
-        else
+    // tasks: the pieces of a move's layers' keys and values, and its ids
+    const int n_moves = m.n[0], pieces = pieces_of<kMovePiece>(sh);
+    const int64_t tasks = (int64_t)2 * sh.layers * pieces + 1;
+    for (int64_t w = blockIdx.x; w < n_moves * tasks; w += gridDim.x) {
+        const int i = (int)(w / tasks), src = m.from[i], dst = m.to[i];
+        const int64_t task = w - i * tasks;
+        if (task < tasks - 1) {
+            const int part = (int)(task / pieces);
+            copy_piece<kMovePiece>(sh, (char *)(part & 1 ? c.v : c.k) + (part >> 1) * sh.layer_stride, src, dst, c.page_size, (int)(task - (int64_t)part * pieces));
+        } else {
             copy_ids(c, src, dst, c.page_size, threadIdx.x, kCopyThreads);
+        }
     }
     bool bad = false;
     for (int q = blockIdx.x; q < c.seqs; q += gridDim.x) {
@@ -451,7 +465,7 @@ int mate_cache_fork(const mate_cache_t *cache, const int32_t *parents, const int
     ForkItem *items = static_cast<ForkItem *>(workspace);
     cudaError_t e = launch_after(fork_kernel, dim3(1), kThreads, 0, (cudaStream_t)stream, c, parents, children, n, items);
     if (e == cudaSuccess)
-        e = launch_after(fork_copy_kernel, dim3((unsigned)n, 2 * (unsigned)cache->layers + 1), kCopyThreads, 0, (cudaStream_t)stream, c,
+        e = launch_after(fork_copy_kernel, dim3((unsigned)n, 2 * (unsigned)cache->layers + 1, (unsigned)pieces_of<kForkPiece>(page_shape(cache))), kCopyThreads, 0, (cudaStream_t)stream, c,
                          page_shape(cache), (const ForkItem *)items);
     return as_status(e);
 }
