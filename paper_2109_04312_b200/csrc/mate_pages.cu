@@ -2,12 +2,13 @@
 // given back (mate_cache_free) and moved together (mate_cache_compact).
 //
 // What is decided -- who gets which page -- is whole numbers and the same on every launch: one block reads the
-// reference counts, each thread a run of consecutive pages, and a scan over the block ranks the free ones; the r-th
+// reference counts, each warp a run of consecutive pages, and a scan over the block ranks the free ones; the r-th
 // lowest free page goes to the r-th request.  Latency: a few dependent loads and two or three scans.  What is moved
 // (rows of keys and values, every layer) is bound by memory and done by a second kernel over all SMs.
 //
-// A sequence that stands in a list twice: every entry writes "INT_MIN + its place in the list" into the sequence's length
-// by atomicMin, so the first entry wins, whatever the order of the threads.
+// A sequence that stands in a list twice: every entry puts its place in the list by atomicMin where the sequence has a word of its
+// own, so the first entry wins, whatever the order of the threads: in shared memory, and for more than 4096 sequences in
+// their lengths (as INT_MIN + place), which costs two more round trips to L2.
 #include "mate_cache.h"
 #include "sm100_ptx.cuh"
 
@@ -17,7 +18,7 @@ namespace {
 constexpr int kThreads = 1024;   // of the deciding block
 constexpr int kPer = 4;          // entries of a list per thread: lists of up to 4096
 constexpr int kMost = kThreads * kPer;
-constexpr int kEarly = 16;       // pages of a thread whose reference counts are read before it is known whether any is wanted
+constexpr int kEarly = 16384;    // pages up to which the reference counts are read before it is known whether any is wanted
 constexpr int kCopyThreads = 128, kCopyBlocks = 8;  // blocks per SM
 
 // Exclusive sum over the block's threads; *total gets the sum.  All threads call it.
@@ -50,35 +51,73 @@ __device__ N block_scan(N x, N *total) {
     return s_warp[warp] + sum - x;
 }
 
-// The thread's run of pages.
+// The warp's run of pages, and what can be done with those that are free.
 struct PageRun {
     int lo, hi;
-};
-__device__ __forceinline__ PageRun my_pages(int pages) {
-    const int per = (pages + kThreads - 1) / kThreads;
-    const int lo = min(pages, (int)threadIdx.x * per);
-    return {lo, min(pages, lo + per)};
-}
-
-__device__ __forceinline__ int free_pages(const CacheArgs &c, const PageRun &run) {
-    int n = 0;
+    __device__ explicit PageRun(int pages) {
+        const int per = ((pages + kThreads - 1) / kThreads) * 32;
+        lo = min(pages, (int)(threadIdx.x >> 5) * per), hi = min(pages, lo + per);
+    }
+    // pages for which f holds, of the lane's
+    template <typename F>
+    __device__ int count(F &&f) const {
+        int n = 0;
 #pragma unroll 8
-    for (int p = run.lo; p < run.hi; ++p) n += c.refs[p] <= 0;
-    return n;
+        for (int p = lo + (threadIdx.x & 31); p < hi; p += 32) n += f(p);
+        return n;
+    }
+    // g(page, rank) for the pages for which f holds, in order, ranks from `rank` to below `limit`
+    template <typename F, typename G>
+    __device__ void each(int rank, int limit, F &&f, G &&g) const {
+        const int lane = threadIdx.x & 31;
+        for (int p0 = lo; p0 < hi && rank < limit; p0 += 32) {
+            const bool is = p0 + lane < hi && f(p0 + lane);
+            const unsigned all = __ballot_sync(~0u, is);
+            const int mine = rank + __popc(all & ((1u << lane) - 1));
+            if (is && mine < limit) g(p0 + lane, mine);
+            rank += __popc(all);
+        }
+    }
+};
+// Rank of the warp's first among all that were counted (by lanes); *total: how many there are.
+__device__ __forceinline__ int warp_rank(int of_lane, int *total) {
+    const int of_warp = __reduce_add_sync(~0u, of_lane);
+    return __shfl_sync(~0u, block_scan((threadIdx.x & 31) == 0 ? of_warp : 0, total), 0);
 }
 
-__device__ __forceinline__ int claim_of(int i) { return INT32_MIN + i; }
+// Who of the entries with one sequence comes first: put() by all, a barrier, first().  `s_claim`: kMost words of shared memory, cleared by
+// clear() and a barrier.
+struct Claims {
+    int *s_claim;
+    const CacheArgs &c;
+    __device__ bool shared() const { return c.seqs <= kMost; }
+    __device__ void clear() const {
+        if (shared())
+            for (int i = threadIdx.x; i < c.seqs; i += kThreads) s_claim[i] = INT32_MAX;
+    }
+    __device__ void put(int seq, int i) const {
+        if (shared())
+            atomicMin(s_claim + seq, i);
+        else
+            atomicMin(c.lens + seq, INT32_MIN + i);
+    }
+    __device__ bool first(int seq, int i) const { return shared() ? s_claim[seq] == i : __ldcg(c.lens + seq) == INT32_MIN + i; }
+};
 
+constexpr int kExtendSmem = kMost * (int)(sizeof(int64_t) + 2 * sizeof(int));
 __global__ void __launch_bounds__(kThreads, 1) extend_kernel(const __grid_constant__ CacheArgs c, const int32_t *seqs, const int32_t *counts, int n,
-                                                          int32_t *granted) {
-    __shared__ int64_t s_off[kMost + 1];  // (the list may want more pages than 32 bits count)
+                                                             int32_t *granted) {
+    extern __shared__ int64_t s_at[];                     // [kMost] where in the table an entry's first new page goes
+    int *s_off = reinterpret_cast<int *>(s_at + kMost);   // [kMost] pages that the entries in front of it want
+    const Claims claims = {s_off + kMost, c};
     __shared__ int s_used;
     ptx::launch_dependents();
     ptx::wait_prior_grid();
     const int tid = threadIdx.x, i0 = tid * kPer;
-    const PageRun mine = my_pages(c.pages);
-    const bool early = c.pages <= kEarly * kThreads;
-    int free_here = early ? free_pages(c, mine) : 0;
+    const PageRun run(c.pages);
+    const auto is_free = [&](int page) { return c.refs[page] <= 0; };
+    const bool early = c.pages <= kEarly;
+    int free_here = early ? run.count(is_free) : 0;
     int s[kPer], len[kPer], count[kPer], need[kPer], status = 0;
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
@@ -97,15 +136,16 @@ __global__ void __launch_bounds__(kThreads, 1) extend_kernel(const __grid_consta
         }
     }
     if (tid == 0) s_used = 0;
+    claims.clear();
     __syncthreads();  // every length has been read
 #pragma unroll
     for (int j = 0; j < kPer; ++j)
-        if (s[j] >= 0) atomicMin(&c.lens[s[j]], claim_of(i0 + j));
+        if (s[j] >= 0) claims.put(s[j], i0 + j);
     __syncthreads();
-    int64_t sum = 0;
+    int64_t sum = 0;  // (the list may want more pages than 32 bits count)
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
-        if (s[j] >= 0 && __ldcg(&c.lens[s[j]]) != claim_of(i0 + j)) {
+        if (s[j] >= 0 && !claims.first(s[j], i0 + j)) {
             status |= kCacheBad;  // the second entry of a sequence
             s[j] = -1;
         }
@@ -114,41 +154,34 @@ __global__ void __launch_bounds__(kThreads, 1) extend_kernel(const __grid_consta
     }
     int64_t wanted;
     int64_t off = block_scan(sum, &wanted);
-#pragma unroll
-    for (int j = 0; j < kPer; ++j) {
-        s_off[i0 + j] = off;
-        off += need[j];
-    }
     int n_free = 0, rank = 0;
     if (wanted > 0) {
-        if (!early) free_here = free_pages(c, mine);
-        rank = block_scan(free_here, &n_free);
+        if (!early) free_here = run.count(is_free);
+        rank = warp_rank(free_here, &n_free);
     }
     // granted: who fits into what is free; the pages that go out are the first `used` free ones
     int used = 0;
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
-        const int64_t end = s_off[i0 + j] + need[j];
+        const int64_t end = off + need[j];
         const bool fits = s[j] >= 0 && (need[j] == 0 || end <= n_free);
         if (s[j] >= 0 && !fits) status |= kCacheFull;
         if (fits && need[j] > 0) used = max(used, (int)end);
         if (s[j] >= 0) c.lens[s[j]] = fits ? len[j] + count[j] : len[j];
         if (i0 + j < n) granted[i0 + j] = fits ? count[j] : 0;
+        s_off[i0 + j] = (int)min(off, (int64_t)INT32_MAX);
+        s_at[i0 + j] = (int64_t)s[j] * c.width + pages_of(len[j], c.page_size);
+        off = end;
     }
     if (status) atomicOr(c.status, status);
     if (wanted == 0) return;
     if (used > 0) atomicMax(&s_used, used);
     __syncthreads();
-    for (int p = mine.lo; p < mine.hi && rank < s_used; ++p) {
-        if (c.refs[p] > 0) continue;
-        const int i = owner_of(s_off, min(n, kMost), rank), q = seq_of(seqs, i, c.seqs);
-        // the owner's new length is known: its pages end there
-        const int at = pages_of(__ldcg(&c.lens[q]), c.page_size);
-        const int64_t end = i + 1 < kMost ? s_off[i + 1] : wanted;
-        c.table[(size_t)q * c.width + at - (int)(end - rank)] = p;
-        c.refs[p] = 1;
-        ++rank;
-    }
+    run.each(rank, s_used, is_free, [&](int page, int r) {
+        const int i = owner_of(s_off, min(n, kMost), r);
+        c.table[s_at[i] + (r - s_off[i])] = page;
+        c.refs[page] = 1;
+    });
 }
 
 // What mate_cache_fork leaves for its copies, per entry of the list.
@@ -159,14 +192,16 @@ struct ForkItem {
 };
 
 __global__ void __launch_bounds__(kThreads, 1) fork_kernel(const __grid_constant__ CacheArgs c, const int32_t *parents, const int32_t *children,
-                                                        int n, ForkItem *items) {
-    __shared__ int s_off[kMost + 1], s_dst[kMost];
+                                                           int n, ForkItem *items) {
+    __shared__ int s_off[kMost], s_dst[kMost];  // (s_dst: the claims at first)
+    const Claims claims = {s_dst, c};
     ptx::launch_dependents();
     ptx::wait_prior_grid();
     const int tid = threadIdx.x, i0 = tid * kPer;
-    const PageRun mine = my_pages(c.pages);
-    const bool early = c.pages <= kEarly * kThreads;
-    int free_here = early ? free_pages(c, mine) : 0;
+    const PageRun run(c.pages);
+    const auto is_free = [&](int page) { return c.refs[page] <= 0; };
+    const bool early = c.pages <= kEarly;
+    int free_here = early ? run.count(is_free) : 0;
     int p[kPer], ch[kPer], len[kPer], prefix[kPer], src[kPer], status = 0, sum = 0;
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
@@ -182,21 +217,22 @@ __global__ void __launch_bounds__(kThreads, 1) fork_kernel(const __grid_constant
             src[j] = c.table[(size_t)p[j] * c.width + len[j] / c.page_size];
         }
     }
+    claims.clear();
     __syncthreads();  // every length and prefix has been read
 #pragma unroll
     for (int j = 0; j < kPer; ++j)
-        if (ch[j] >= 0) atomicMin(&c.lens[ch[j]], claim_of(i0 + j));
+        if (ch[j] >= 0) claims.put(ch[j], i0 + j);
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
-        if (ch[j] >= 0 && __ldcg(&c.lens[ch[j]]) != claim_of(i0 + j)) {
+        if (ch[j] >= 0 && !claims.first(ch[j], i0 + j)) {
             status |= kCacheBad;  // the second entry of a child
             ch[j] = -1;
         }
         sum += ch[j] >= 0 && len[j] % c.page_size != 0;
     }
     int wanted;
-    int off = block_scan(sum, &wanted);
+    int off = block_scan(sum, &wanted);  // (its barriers: the claims have been read)
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
         s_off[i0 + j] = off;
@@ -205,13 +241,13 @@ __global__ void __launch_bounds__(kThreads, 1) fork_kernel(const __grid_constant
     }
     __syncthreads();
     if (wanted > 0) {
-        if (!early) free_here = free_pages(c, mine);
-        int n_free, rank = block_scan(free_here, &n_free);
-        for (int q = mine.lo; q < mine.hi && rank < wanted; ++q) {
-            if (c.refs[q] > 0) continue;
-            s_dst[owner_of(s_off, min(n, kMost), rank++)] = q;
-            c.refs[q] = 1;
-        }
+        if (!early) free_here = run.count(is_free);
+        int n_free;
+        const int rank = warp_rank(free_here, &n_free);
+        run.each(rank, wanted, is_free, [&](int page, int r) {
+            s_dst[owner_of(s_off, min(n, kMost), r)] = page;
+            c.refs[page] = 1;
+        });
         __syncthreads();
     }
 #pragma unroll
@@ -353,23 +389,15 @@ struct Moves {
 __global__ void __launch_bounds__(kThreads, 1) compact_kernel(const __grid_constant__ CacheArgs c, Moves m, int32_t *n_live_out) {
     ptx::launch_dependents();
     ptx::wait_prior_grid();
-    const PageRun mine = my_pages(c.pages);
-    int live_here = 0, n_live, n_moves;
-    for (int p = mine.lo; p < mine.hi; ++p) live_here += c.refs[p] > 0;
-    block_scan(live_here, &n_live);
-    int holes = 0, movers = 0, n_holes;
-    for (int p = mine.lo; p < mine.hi; ++p) {
-        const bool live = c.refs[p] > 0;
-        holes += p < n_live && !live;
-        movers += p >= n_live && live;
-    }
-    int hole = block_scan(holes, &n_holes), mover = block_scan(movers, &n_moves);  // as many of the one as of the other
-    for (int p = mine.lo; p < mine.hi; ++p) {
-        const bool live = c.refs[p] > 0;
-        m.place[p] = p < n_live && live ? p : -1;
-        if (p < n_live && !live) m.to[hole++] = p;
-        if (p >= n_live && live) m.from[mover++] = p;
-    }
+    const PageRun run(c.pages);
+    int n_live, n_moves, n_holes;  // (as many holes as moves)
+    warp_rank(run.count([&](int p) { return c.refs[p] > 0; }), &n_live);
+    const auto is_hole = [&](int p) { return p < n_live && c.refs[p] <= 0; };
+    const auto is_mover = [&](int p) { return p >= n_live && c.refs[p] > 0; };
+    const int hole = warp_rank(run.count(is_hole), &n_holes), mover = warp_rank(run.count(is_mover), &n_moves);
+    for (int p = run.lo + (threadIdx.x & 31); p < run.hi; p += 32) m.place[p] = p < n_live && c.refs[p] > 0 ? p : -1;
+    run.each(hole, n_holes, is_hole, [&](int page, int r) { m.to[r] = page; });
+    run.each(mover, n_moves, is_mover, [&](int page, int r) { m.from[r] = page; });
     __syncthreads();
     for (int i = threadIdx.x; i < n_moves; i += kThreads) {
         const int from = __ldcg(&m.from[i]), to = __ldcg(&m.to[i]);
@@ -450,7 +478,10 @@ int mate_cache_extend(const mate_cache_t *cache, const int32_t *seqs, const int3
     if (rc == MATE_OK && n > 0 && (!counts || !granted)) rc = MATE_ERR_INVALID_ARG;
     if (rc == MATE_OK) rc = check_cache_device(cache);
     if (rc != MATE_OK || n == 0) return rc;
-    return as_status(launch_after(extend_kernel, dim3(1), kThreads, 0, (cudaStream_t)stream, cache_args(cache, 0), seqs, counts, n, granted));
+    static SmemAttrOnce attr;
+    rc = attr.ensure((const void *)extend_kernel, kExtendSmem, cache->device);
+    if (rc != MATE_OK) return rc;
+    return as_status(launch_after(extend_kernel, dim3(1), kThreads, kExtendSmem, (cudaStream_t)stream, cache_args(cache, 0), seqs, counts, n, granted));
 }
 
 int mate_cache_fork(const mate_cache_t *cache, const int32_t *parents, const int32_t *children, int n, void *workspace,

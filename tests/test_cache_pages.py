@@ -249,19 +249,21 @@ def test_one_tensor_as_keys_and_values():
 
 
 @pytest.mark.gpu
-def test_long_lists_and_many_pages():
+@pytest.mark.parametrize("pages,S", [(70001, 4096), (70001, 5000), (9000, 4097), (31, 33)])
+def test_long_lists_and_many_pages(pages, S):
     import paper_2109_04312_b200 as m
-    pages, S = 70001, 4096
     c = m.Cache.empty(pages, 2, 1, 8, S, 20, [0])
     model = CacheModel(pages, 2, S, 20)
     rng = np.random.default_rng(3)
-    seqs, counts = rng.permutation(S).tolist(), rng.integers(0, 41, S).tolist()
+    seqs, counts = rng.permutation(S)[:4096].tolist(), rng.integers(0, 41, min(S, 4096)).tolist()
+    seqs[5], seqs[-1] = seqs[3], seqs[0]   # (one entry more of two sequences)
     for _ in range(2):
         assert m.mate_cache_extend(c, ints(seqs), ints(counts)).tolist() == model.extend(seqs, counts)
         gone = rng.permutation(S)[:S // 2].tolist()
         m.mate_cache_free(c, ints(gone))
         model.free(gone)
-    parents, children = rng.integers(0, S, S).tolist(), rng.permutation(S).tolist()
+    parents, children = rng.integers(0, S, S)[:4096].tolist(), rng.permutation(S)[:4096].tolist()
+    children[1] = children[-1]
     m.mate_cache_fork(c, ints(parents), ints(children))
     model.fork(parents, children)
     assert int(m.mate_cache_compact(c)) == model.compact()
@@ -269,6 +271,19 @@ def test_long_lists_and_many_pages():
         assert np.array_equal(getattr(c, name).cpu().numpy(), getattr(model, name)), name
     with pytest.raises(m.MateError, match="unsupported"):
         m.mate_cache_extend(c, ints([0] * 4097), ints([0] * 4097))
+
+
+@pytest.mark.gpu
+def test_granted_over_its_own_inputs():
+    import paper_2109_04312_b200 as m
+    for which in range(2):
+        c, model = make(m)
+        args = [ints([4, 0, 3]), ints([9, 13, 1])]
+        granted = m.mate_cache_extend(c, *args, granted=args[which])
+        assert granted is args[which] and granted.tolist() == model.extend([4, 0, 3], [9, 13, 1])
+        for name in ("table", "lens", "refs"):
+            assert np.array_equal(getattr(c, name).cpu().numpy(), getattr(model, name)), name
+        c.status()
 
 
 @pytest.mark.gpu
