@@ -279,33 +279,28 @@ __global__ void __launch_bounds__(kThreads, 1) fork_kernel(const __grid_constant
 // How the rows of a page lie.
 struct PageShape {
     int64_t page_stride, head_stride, slot_stride, layer_stride;  // bytes
-    int heads, row_bytes, layers, page_size;
+    int heads, per_row, layers, page_size;                        // per_row: units of 16 bytes
+    unsigned row_mul;                                             // u / per_row = umulhi(u, row_mul) for u < 2^27; 0: per_row is 1
+    int piece, pieces;                                            // units of a piece, pieces of a page
 };
-// Copies a piece of one page of one layer's keys or values, of whose slots the first `fill` count.  Units of 16 bytes, kPiece of them to
-// a block, kFlight of a thread under way; the quotients by way of fp32 (exact: rows are fewer than 2^21, the host sees to that).
-// Compaction, whose pages are whole: small pieces (a few pages of 196 KB in two layers 6.9 us, 8.9 with 2048 units, 24.6 with a page to
-// each block).  Forks, whose pages are filled in part: larger ones (64 pages of 98 KB in twelve layers 19.0 us, 30.6 with 512 units).
-constexpr int kMovePiece = 512, kForkPiece = 2048;
-template <int kPiece>
-__host__ __device__ inline int pieces_of(const PageShape &sh) {
-    return (sh.heads * sh.page_size * (sh.row_bytes / 16) + kPiece - 1) / kPiece;
-}
-template <int kPiece>
+// Copies a piece of one page of one layer's keys or values, of whose slots the first `fill` count.  Units of 16 bytes, kFlight of a
+// thread under way; slots by way of fp32 (exact: rows are fewer than 2^21, the host sees to that).  Bound by memory as long as
+// the arithmetic of a unit is short: quotients by the instruction took the copies of a compaction (230 MB) from 36.3 to 39.8 us.
 __device__ __forceinline__ void copy_piece(const PageShape &sh, char *base, int src, int dst, int fill, int piece) {
     const char *from = base + src * sh.page_stride;
     char *to = base + dst * sh.page_stride;
-    const int per_row = sh.row_bytes / 16, n = min(sh.heads * fill * per_row, (piece + 1) * kPiece);
+    const int n = min(sh.heads * fill * sh.per_row, (piece + 1) * sh.piece);
     const float by_fill = 1.f / (float)fill;
     constexpr int kFlight = 4;
-    for (int i = piece * kPiece + threadIdx.x; i < n; i += kCopyThreads * kFlight) {
+    for (int i = piece * sh.piece + threadIdx.x; i < n; i += kCopyThreads * kFlight) {
         uint4 v[kFlight];
         int64_t at[kFlight];
 #pragma unroll
         for (int j = 0; j < kFlight; ++j) {
             const int u = i + j * kCopyThreads;
             if (u >= n) break;
-            const int row = u / per_row, head = (int)(((float)row + 0.5f) * by_fill);
-            at[j] = head * sh.head_stride + (row - head * fill) * sh.slot_stride + (u - row * per_row) * 16;
+            const int row = sh.row_mul ? (int)__umulhi((unsigned)u, sh.row_mul) : u, head = (int)(((float)row + 0.5f) * by_fill);
+            at[j] = head * sh.head_stride + (row - head * fill) * sh.slot_stride + (u - row * sh.per_row) * 16;
             v[j] = *reinterpret_cast<const uint4 *>(from + at[j]);
         }
 #pragma unroll
@@ -330,7 +325,7 @@ __global__ void __launch_bounds__(kCopyThreads, kCopyBlocks) fork_copy_kernel(co
     const int part = blockIdx.y;
     if (part < 2 * sh.layers) {
         if (it.src < 0 || it.dst < 0) return;
-        copy_piece<kForkPiece>(sh, (char *)(part & 1 ? c.v : c.k) + (part >> 1) * sh.layer_stride, it.src, it.dst, it.fill, blockIdx.z);
+        copy_piece(sh, (char *)(part & 1 ? c.v : c.k) + (part >> 1) * sh.layer_stride, it.src, it.dst, it.fill, blockIdx.z);
         return;
     }
     if (blockIdx.z > 0) return;
@@ -417,14 +412,14 @@ __global__ void __launch_bounds__(kCopyThreads, kCopyBlocks) compact_copy_kernel
     ptx::launch_dependents();
     ptx::wait_prior_grid();
     // tasks: the pieces of a move's layers' keys and values, and its ids
-    const int n_moves = m.n[0], pieces = pieces_of<kMovePiece>(sh);
+    const int n_moves = m.n[0], pieces = sh.pieces;
     const int64_t tasks = (int64_t)2 * sh.layers * pieces + 1;
     for (int64_t w = blockIdx.x; w < n_moves * tasks; w += gridDim.x) {
         const int i = (int)(w / tasks), src = m.from[i], dst = m.to[i];
         const int64_t task = w - i * tasks;
         if (task < tasks - 1) {
             const int part = (int)(task / pieces);
-            copy_piece<kMovePiece>(sh, (char *)(part & 1 ? c.v : c.k) + (part >> 1) * sh.layer_stride, src, dst, c.page_size, (int)(task - (int64_t)part * pieces));
+            copy_piece(sh, (char *)(part & 1 ? c.v : c.k) + (part >> 1) * sh.layer_stride, src, dst, c.page_size, (int)(task - (int64_t)part * pieces));
         } else {
             copy_ids(c, src, dst, c.page_size, threadIdx.x, kCopyThreads);
         }
@@ -446,8 +441,13 @@ __global__ void __launch_bounds__(kCopyThreads, kCopyBlocks) compact_copy_kernel
 
 PageShape page_shape(const mate_cache_t *c) {
     const int64_t size = (int64_t)elem_size(c->dtype);
+    const unsigned per_row = (unsigned)(c->d * size / 16), units = (unsigned)(c->kv_heads * c->page_size) * per_row;
+    // even pieces of up to 2048 units, whole rounds of the threads (a few pages of 196 KB in two layers moved in 8.4 us; with a page to
+    // each block 24.6)
+    const unsigned pieces = (units + 2047) / 2048, piece = ((units + pieces - 1) / pieces + kCopyThreads - 1) / kCopyThreads * kCopyThreads;
     return {c->page_stride * size, c->head_stride * size, c->slot_stride * size, c->layer_stride * size,
-            c->kv_heads, c->d * (int)size, c->layers, c->page_size};
+            c->kv_heads, (int)per_row, c->layers, c->page_size, per_row > 1 ? (unsigned)(((uint64_t)1 << 32) / per_row + 1) : 0,
+            (int)piece, (int)((units + piece - 1) / piece)};
 }
 size_t fork_bytes(int n) { return sizeof(ForkItem) * (size_t)n; }
 size_t compact_bytes(const mate_cache_t *c) { return sizeof(int32_t) * (64 + 3 * (size_t)c->pages); }
@@ -496,7 +496,7 @@ int mate_cache_fork(const mate_cache_t *cache, const int32_t *parents, const int
     ForkItem *items = static_cast<ForkItem *>(workspace);
     cudaError_t e = launch_after(fork_kernel, dim3(1), kThreads, 0, (cudaStream_t)stream, c, parents, children, n, items);
     if (e == cudaSuccess)
-        e = launch_after(fork_copy_kernel, dim3((unsigned)n, 2 * (unsigned)cache->layers + 1, (unsigned)pieces_of<kForkPiece>(page_shape(cache))), kCopyThreads, 0, (cudaStream_t)stream, c,
+        e = launch_after(fork_copy_kernel, dim3((unsigned)n, 2 * (unsigned)cache->layers + 1, (unsigned)page_shape(cache).pieces), kCopyThreads, 0, (cudaStream_t)stream, c,
                          page_shape(cache), (const ForkItem *)items);
     return as_status(e);
 }
