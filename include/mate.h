@@ -307,8 +307,8 @@ int mate_rope(const mate_rope_tensor_t *tensors, int n_tensors, int B, int N, in
  * The cache is the caller's memory, described by this struct, which the calls read while they run on the host and do not
  * keep.  A sequence is a row of `table`: its tokens 0 .. lens[s] - 1 stand in the slots of the pages table[s][0],
  * table[s][1], ..., page_size to a page.  Every cached token has its row id and its column id (as given to mate_plan:
- * a negative id marks padding, which is never attended, whatever its key and value hold); the first prefix[s] tokens are the
- * prefix.  MATE_ID_TEXT as both ids marks a token that belongs to the text wherever it stands (an answer
+ * negative ones, in both arrays, mark padding, which is never attended, whatever its key and value hold); the first prefix[s]
+ * tokens are the prefix.  MATE_ID_TEXT as both ids marks a token that belongs to the text wherever it stands (an answer
  * written behind the table): it attends, and is attended by, every token.
  *
  * A page may be shared by several sequences; refs[page] counts them, 0 = free.  lens, table, refs and prefix are device

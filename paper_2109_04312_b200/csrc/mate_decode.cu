@@ -10,7 +10,7 @@
 //     read; twelve such warps to an SM keep 96 KB under way.  (Three stages and eight warps: 64 sequences 93 us instead of 78.)  No
 //     block barrier until the sequence's part is done.  What nobody attends is never read, padding's keys and values included.
 //   - the products are tensor-core ones (m16n8k16) with the keys as the 16 rows and the heads as the 8 columns, so that a group
-//     of up to 8 costs one of them; they take a tenth of the time that the copies take.  The weights go from one product's
+//     of up to 8 costs one of them; the tensor pipe is 14 % busy while HBM is the limit.  The weights go from one product's
 //     result to the other's operand by transposing 8 x 8 pieces between the lanes, as the sum of two bf16: the second product costs
 //     1 % (64 sequences, 72.1 -> 73.1 us), rounding them to bf16 would make the error against 64 bits 2.4e-3 instead of the 1.7e-3 that the
 //     result's own rounding makes.  fp32 caches: multiply-adds.
@@ -864,9 +864,9 @@ int launch(const DecodeParams &p, int blocks, int device, cudaStream_t st) {
     const int rc = launch_warps<T, DP, NB, kWarps>(p, (unsigned)blocks, device, st);
     if (rc != MATE_OK) return rc;
     // few items in many parts: more threads each
-    const dim3 joins((unsigned)(p.B * items), (unsigned)rows);
+    const dim3 joins((unsigned)all, (unsigned)rows);
     const size_t bytes = sizeof(float) * blocks;
-    return (blocks > 16 * p.B * items ? launch_after(join_kernel<T, 1024>, joins, 1024, bytes, st, p, kRows)
+    return (blocks > 16 * all ? launch_after(join_kernel<T, 1024>, joins, 1024, bytes, st, p, kRows)
                                       : launch_after(join_kernel<T, 128>, joins, 128, bytes, st, p, kRows)) == cudaSuccess
                ? MATE_OK
                : MATE_ERR_CUDA;

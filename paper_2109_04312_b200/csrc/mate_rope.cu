@@ -210,6 +210,7 @@ template <typename T, int VEC>
 int launch(RopeParams &p, int device, cudaStream_t st) {
     p.turned_chunks = p.rot / 2 / VEC;
     p.n_chunks = VEC == 1 ? (p.d + 1) / 2 : p.d / (2 * VEC);
+    if ((int64_t)p.B * p.N > (int64_t)INT32_MAX * kThreads / p.n_chunks) return MATE_ERR_UNSUPPORTED;
     const int64_t threads = (int64_t)p.B * p.N * p.n_chunks, blocks = (threads + kThreads - 1) / kThreads;
     // As many heads to a thread as leave every SM 1024 of them, in whole batches (4 x 2048 tokens, 12 and 12 heads: 9.1 us; with 2048
     // threads, that is four heads each, 12.8).  New tokens of a cache, whose slots have to be looked up first: 2048 (eight tables in
@@ -222,7 +223,7 @@ int launch(RopeParams &p, int device, cudaStream_t st) {
         p.side[i].first_slice = (int)slices;
         slices += (p.side[i].heads + p.heads_of_thread - 1) / p.heads_of_thread;
     }
-    if (blocks > INT32_MAX || slices > 65535) return MATE_ERR_UNSUPPORTED;
+    if (slices > 65535) return MATE_ERR_UNSUPPORTED;
     return launch_after(rope_kernel<T, VEC>, dim3((unsigned)blocks, (unsigned)slices), kThreads, sizeof(uint64_t) * (p.rot / 2), st, p) == cudaSuccess
                ? MATE_OK
                : MATE_ERR_CUDA;

@@ -304,6 +304,23 @@ def test_wishes_beyond_32_bits():
 
 
 @pytest.mark.gpu
+def test_more_tokens_than_a_launch_takes():
+    import paper_2109_04312_b200 as m
+    cache = m.Cache.empty(2, 4, 2, 128, 2, 1, [0, 1])
+    for B, offset in ((2, 0), (1024, 0), (1024, 1)):      # (one element at a time where the address is odd: eight times as many threads)
+        K = torch.ones(129, device="cuda", dtype=torch.bfloat16)[offset:offset + 128].expand(B, 2, 2 ** 31 - 1, 128)
+        many = torch.zeros(B, dtype=torch.int32, device="cuda")
+        if B == 2:
+            K = K[:, :, :0]                               # none at all is fine
+            m.mate_cache_append(cache, K, K, many, many)
+            continue
+        with pytest.raises(m.MateError, match="unsupported"):
+            m.mate_cache_append(cache, K, K, many, many)
+    cache.status()
+    assert not cache.k.any() and not cache.lens.any()
+
+
+@pytest.mark.gpu
 def test_a_step_in_a_graph():
     # extend and append captured once, replayed for token after token; forks and frees between the replays
     import paper_2109_04312_b200 as m
