@@ -93,6 +93,7 @@ __global__ void __launch_bounds__(kThreads, 6) rope_kernel(const __grid_constant
     extern __shared__ uint64_t s_turn[];  // [rot / 2] turns per position, in 2^-64
     ptx::launch_dependents();
     ptx::wait_prior_grid();
+    const double freq = threadIdx.x < p.rot / 2 ? p.freqs[threadIdx.x] : 0.;  // (ahead of all else: what it becomes is waited for by all)
     const int64_t at = (int64_t)blockIdx.x * kThreads + threadIdx.x, t = at / p.n_chunks;
     const int chunk = (int)(at - t * p.n_chunks), b = (int)(t / p.N), n = (int)(t - (int64_t)b * p.N);
     const int side = (int)(p.n_sides > 1 && blockIdx.y >= p.side[1].first_slice) + (int)(p.n_sides > 2 && blockIdx.y >= p.side[2].first_slice);
@@ -127,14 +128,15 @@ __global__ void __launch_bounds__(kThreads, 6) rope_kernel(const __grid_constant
     load(0);
 
     // the token's position and, in a cache, its slot (the loads above are under way)
-    int position = 0;
+    int position = p.positions && exists ? p.positions[b * p.position_stride + n] : 0;
     int64_t page_at = 0;
     if (p.paged && exists && n < count) {
         bool bad = false;
-        position = clip_len(p.cache.lens[q], p.cache.width * p.cache.page_size, &bad) - count + n;
+        const int place_in = clip_len(p.cache.lens[q], p.cache.width * p.cache.page_size, &bad) - count + n;
+        if (!p.positions) position = place_in;
         int page = -1;
-        if (position >= 0 && !bad) {
-            const int i = position / p.cache.page_size, slot = position - i * p.cache.page_size;
+        if (place_in >= 0 && !bad) {
+            const int i = place_in / p.cache.page_size, slot = place_in - i * p.cache.page_size;
             page = p.cache.table[(size_t)q * p.cache.width + i];
             if (in_range(page, p.cache.pages)) {
                 page_at = page * p.cache.page_stride + slot * p.cache.slot_stride;
@@ -150,12 +152,11 @@ __global__ void __launch_bounds__(kThreads, 6) rope_kernel(const __grid_constant
             goes = s.y;
         }
     }
-    if (p.positions && exists) position = p.positions[b * p.position_stride + n];
     T *to = s.y ? (T *)s.y + b * s.ys[0] + h0 * s.ys[1] + n * s.ys[2] + place_of.a
                 : (T *)(s.to_keys ? p.cache.k : p.cache.v) + page_at + h0 * p.cache.head_stride + place_of.a;
 
     for (int i = threadIdx.x; i < p.rot / 2; i += kThreads) {
-        const double turns = p.freqs[i] * 0.15915494309189533577;
+        const double turns = (i < kThreads ? freq : p.freqs[i]) * 0.15915494309189533577;
         s_turn[i] = (uint64_t)__double2ull_rn((turns - floor(turns)) * 18446744073709551616.0);
     }
     __syncthreads();
