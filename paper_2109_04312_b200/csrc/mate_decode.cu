@@ -21,7 +21,7 @@
 // up, and the SMs do not get three blocks each (64 sequences, calls back to back, 106 us instead of 78).
 // Measured (one B200, calls back to back): 64 sequences of up to 4096 tokens, 8 kv heads of 128 elements, 400 MB, 73 us (5470 GB/s, of
 // which 67 us this kernel, the first 6 of them until the first products); one of 131072 tokens, 4 kv heads, 51 us (5250 GB/s); cells
-// of 16 tables of up to 8192 tokens 18 us, one table of 512 tokens 6.3 us: chains of dependent loads (sequence, length, page, ids, keys).
+// of 16 tables of up to 8192 tokens 18 us, one table of 512 tokens 6.0 us: chains of dependent loads (sequence, length, page, ids, keys).
 #include <cuda_bf16.h>
 
 #include <type_traits>

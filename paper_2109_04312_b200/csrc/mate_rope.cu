@@ -213,7 +213,7 @@ int launch(RopeParams &p, int device, cudaStream_t st) {
     p.n_chunks = VEC == 1 ? (p.d + 1) / 2 : p.d / (2 * VEC);
     if ((int64_t)p.B * p.N > (int64_t)INT32_MAX * kThreads / p.n_chunks) return MATE_ERR_UNSUPPORTED;
     const int64_t threads = (int64_t)p.B * p.N * p.n_chunks, blocks = (threads + kThreads - 1) / kThreads;
-    // As many heads to a thread as leave every SM 1024 of them, in whole batches (4 x 2048 tokens, 12 and 12 heads: 9.1 us; with 2048
+    // As many heads to a thread as leave every SM 1024 of them, in whole batches (4 x 2048 tokens, 12 and 12 heads: 9.0 us; with 2048
     // threads, that is four heads each, 12.8).  New tokens of a cache, whose slots have to be looked up first: 2048 (eight tables in
     // 23.0 us; 23.9 with 1024, 28.1 with 4096).
     int64_t n_heads = 0, slices = 0;
