@@ -21,7 +21,7 @@
 // up, and the SMs do not get three blocks each (64 sequences, calls back to back, 106 us instead of 78).
 // Measured (one B200, calls back to back): 64 sequences of up to 4096 tokens, 8 kv heads of 128 elements, 400 MB, 73 us (5470 GB/s, of
 // which 67 us this kernel, the first 6 of them until the first products); one of 131072 tokens, 4 kv heads, 51 us (5250 GB/s); cells
-// of 16 tables of up to 8192 tokens 18 us, one table of 512 tokens 6.0 us: chains of dependent loads (sequence, length, page, ids, keys).
+// of 16 tables of up to 8192 tokens 18 us, one table of 512 tokens 5.9 us: chains of dependent loads (sequence, length, page, ids, keys).
 #include <cuda_bf16.h>
 
 #include <type_traits>
@@ -248,6 +248,12 @@ struct Loader {
 
     // page of the lane's token `j`
     __device__ void ask_page(int j) { page = j < end ? p.cache.table[(size_t)s * p.cache.width + page_index(p, j)] : -1; }
+    // The same of its first token of entry b, while the sequence's length is on its way: kManyWarps only, whose block has one item and
+    // begins with its first token (512 tokens, 12 heads of 64 elements, 6.25 -> 5.93 us).
+    __device__ void ask_early(int b) {
+        const int sequence = p.seqs ? p.seqs[b] : b, j = 32 * warp + lane;
+        page = in_range(sequence, p.cache.seqs) && j < p.max_len ? p.cache.table[(size_t)sequence * p.cache.width + page_index(p, j)] : -1;
+    }
     // ids of the lane's token of `next`, whose page has come
     __device__ void ask_ids() {
         const int j = next + lane;
@@ -279,7 +285,7 @@ struct Loader {
         s = p.seqs ? p.seqs[part.b] : part.b;
         next = max(0, part.u0 - kOver) * kUnit + 32 * warp;
         end = min(len, (part.u1 - kOver) * kUnit);
-        ask_page(next + lane);
+        if (W != kManyWarps) ask_page(next + lane);
         q_row = p.row_ids[part.b], q_col = p.col_ids[part.b];
         prefix = p.cache.prefix[s];
         text = q_row == MATE_ID_TEXT || q_col == MATE_ID_TEXT;
@@ -656,6 +662,8 @@ __global__ void __launch_bounds__(32 * W, W == kWarps ? Shape<T, DP, NB>::kBlock
         for (int i = tid; i < W * kRing * kStage / 16; i += 32 * W) reinterpret_cast<uint4 *>(smem)[i] = make_uint4(0, 0, 0, 0);
     ptx::wait_prior_grid();
 
+    Loader<T, DP, NB, W> load = {p, s_list[warp], s_marks[warp], s_meta[warp], ptx::smem_u32(smem) + warp * kRing * kStage, lane, warp, items};
+    load.bad = false, load.pending = load.list_at = load.filled = 0;
     Walk walk;
     Start start = {};
     if (W == kWarps && p.joints) {
@@ -672,13 +680,13 @@ __global__ void __launch_bounds__(32 * W, W == kWarps ? Shape<T, DP, NB>::kBlock
     } else {
         bool bad = false;
         walk.b = blockIdx.x / items, walk.item = blockIdx.x - walk.b * items, walk.u = 0;
+        if (W == kManyWarps) load.ask_early(walk.b);
         walk.left = units_of(entry_len(p, walk.b, &bad));
         if (bad && tid == 0) atomicOr(p.cache.status, kCacheBad);
         __syncthreads();
     }
 
-    Loader<T, DP, NB, W> load = {p, s_list[warp], s_marks[warp], s_meta[warp], ptx::smem_u32(smem) + warp * kRing * kStage, lane, warp, items, walk};
-    load.bad = false, load.pending = load.list_at = load.filled = 0;
+    load.walk = walk;
     load.begin();
     for (int i = 0; i < kRing - 1; ++i) load.fill();
 
