@@ -118,29 +118,27 @@ __global__ void __launch_bounds__(kThreads, 1) extend_kernel(const __grid_consta
     const auto is_free = [&](int page) { return c.refs[page] <= 0; };
     const bool early = c.pages <= kEarly;
     int free_here = early ? run.count(is_free) : 0;
-    int s[kPer], len[kPer], count[kPer], need[kPer], status = 0;
+    int s[kPer], len[kPer], count[kPer], need[kPer], refused[kPer], status = 0;
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
-        s[j] = -1, need[j] = 0, len[j] = 0, count[j] = 0;
+        s[j] = -1, need[j] = 0, len[j] = 0, count[j] = 0, refused[j] = 0;
         if (i0 + j >= n) continue;
         s[j] = seq_of(seqs, i0 + j, c.seqs);
         count[j] = counts[i0 + j];
         if (s[j] >= 0) len[j] = c.lens[s[j]];
         const int most = c.width * c.page_size;
-        if (s[j] < 0 || count[j] < 0 || len[j] < 0 || len[j] > most) {
-            status |= kCacheBad;
-            s[j] = -1;
-        } else if (count[j] > most - len[j]) {
-            status |= kCacheFull;
-            s[j] = -1;
-        }
+        if (s[j] < 0 || count[j] < 0 || len[j] < 0 || len[j] > most)
+            refused[j] = kCacheBad;
+        else if (count[j] > most - len[j])
+            refused[j] = kCacheFull;
+        status |= refused[j];
     }
     if (tid == 0) s_used = 0;
     claims.clear();
     __syncthreads();  // every length has been read
 #pragma unroll
     for (int j = 0; j < kPer; ++j)
-        if (s[j] >= 0) claims.put(s[j], i0 + j);
+        if (s[j] >= 0) claims.put(s[j], i0 + j);  // (a refused entry too: it is its sequence's first all the same)
     __syncthreads();
     int64_t sum = 0;  // (the list may want more pages than 32 bits count)
 #pragma unroll
@@ -149,7 +147,7 @@ __global__ void __launch_bounds__(kThreads, 1) extend_kernel(const __grid_consta
             status |= kCacheBad;  // the second entry of a sequence
             s[j] = -1;
         }
-        if (s[j] >= 0) need[j] = pages_of(len[j] + count[j], c.page_size) - pages_of(len[j], c.page_size);
+        if (s[j] >= 0 && !refused[j]) need[j] = pages_of(len[j] + count[j], c.page_size) - pages_of(len[j], c.page_size);
         sum += need[j];
     }
     int64_t wanted;
@@ -164,8 +162,8 @@ __global__ void __launch_bounds__(kThreads, 1) extend_kernel(const __grid_consta
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
         const int64_t end = off + need[j];
-        const bool fits = s[j] >= 0 && (need[j] == 0 || end <= n_free);
-        if (s[j] >= 0 && !fits) status |= kCacheFull;
+        const bool fits = s[j] >= 0 && !refused[j] && (need[j] == 0 || end <= n_free);
+        if (s[j] >= 0 && !refused[j] && !fits) status |= kCacheFull;
         if (fits && need[j] > 0) used = max(used, (int)end);
         if (s[j] >= 0) c.lens[s[j]] = fits ? len[j] + count[j] : len[j];
         if (i0 + j < n) granted[i0 + j] = fits ? count[j] : 0;

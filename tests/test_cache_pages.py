@@ -494,3 +494,27 @@ def test_index_arithmetic(arithmetic):
             assert a.owner_of_(off.ctypes.data_as(ctypes.c_void_p), len(need), r) == want
             long = np.concatenate([off[:-1], [2 ** 40]]).astype(np.int64)   # the last one wants more than there can be
             assert a.owner_of_64(long.ctypes.data_as(ctypes.c_void_p), len(need), r) == want
+
+
+# ---- lists with an entry that is refused ahead of another one of the same sequence
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("seqs", [6, 5000])   # (claims in shared memory, and in the lengths)
+def test_a_refused_entry_is_its_sequences_first_all_the_same(seqs):
+    import paper_2109_04312_b200 as m
+    c = m.Cache.empty(40, 4, 1, 8, seqs, 3, [0])
+    m.mate_cache_extend(c, ints([3]), ints([2]))
+    # sequence 1: more than its row of the table holds, then what would fit; 2: a negative count, then one; 3: 2 + 11 tokens, then 4;
+    # 4 stands once
+    granted = m.mate_cache_extend(c, ints([1, 1, 2, 2, 3, 3, 4, 1]), ints([13, 5, -1, 1, 11, 4, 12, 1]))
+    assert granted.tolist() == [0, 0, 0, 0, 0, 0, 12, 0]
+    assert c.lens[:6].tolist() == [0, 0, 0, 2, 12, 0] and not c.lens[6:].any()
+    assert int(c.refs.sum()) == 4 and c.table[4].tolist() == [1, 2, 3] and c.table[3].tolist() == [0, -1, -1]
+    with pytest.raises(m.MateError):
+        c.status()
+    # lengths that are none stay as they are, and nobody gets anything on their account
+    c.lens[0], c.lens[5] = -7, 13
+    assert m.mate_cache_extend(c, ints([0, 5, 0, 5, 2]), ints([1, 1, 2, 2, 1])).tolist() == [0, 0, 0, 0, 1]
+    assert c.lens[:6].tolist() == [-7, 0, 1, 2, 12, 13]
+    with pytest.raises(m.MateError, match="invalid argument"):
+        c.status()
