@@ -200,17 +200,19 @@ __global__ void __launch_bounds__(kThreads, 1) fork_kernel(const __grid_constant
     const auto is_free = [&](int page) { return c.refs[page] <= 0; };
     const bool early = c.pages <= kEarly;
     int free_here = early ? run.count(is_free) : 0;
-    int p[kPer], ch[kPer], len[kPer], prefix[kPer], src[kPer], status = 0, sum = 0;
+    int p[kPer], ch[kPer], len[kPer], child_len[kPer], prefix[kPer], src[kPer], status = 0, sum = 0;
+    bool refused[kPer];
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
-        p[j] = ch[j] = src[j] = -1, len[j] = prefix[j] = 0;
+        p[j] = ch[j] = src[j] = -1, len[j] = child_len[j] = prefix[j] = 0, refused[j] = false;
         if (i0 + j >= n) continue;
         p[j] = seq_of(parents, i0 + j, c.seqs);
         ch[j] = seq_of(children, i0 + j, c.seqs);
         if (p[j] >= 0) len[j] = c.lens[p[j]], prefix[j] = c.prefix[p[j]];
-        if (p[j] < 0 || ch[j] < 0 || len[j] < 0 || len[j] > c.width * c.page_size || c.lens[ch[j]] != 0) {
+        if (ch[j] >= 0) child_len[j] = c.lens[ch[j]];
+        if (p[j] < 0 || ch[j] < 0 || len[j] < 0 || len[j] > c.width * c.page_size || child_len[j] != 0) {
             status |= kCacheBad;
-            ch[j] = -1;
+            refused[j] = true;
         } else if (len[j] % c.page_size != 0) {
             src[j] = c.table[(size_t)p[j] * c.width + len[j] / c.page_size];
         }
@@ -219,7 +221,7 @@ __global__ void __launch_bounds__(kThreads, 1) fork_kernel(const __grid_constant
     __syncthreads();  // every length and prefix has been read
 #pragma unroll
     for (int j = 0; j < kPer; ++j)
-        if (ch[j] >= 0) claims.put(ch[j], i0 + j);
+        if (ch[j] >= 0) claims.put(ch[j], i0 + j);  // (a refused entry too: it is its child's first all the same)
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
@@ -227,12 +229,16 @@ __global__ void __launch_bounds__(kThreads, 1) fork_kernel(const __grid_constant
             status |= kCacheBad;  // the second entry of a child
             ch[j] = -1;
         }
-        sum += ch[j] >= 0 && len[j] % c.page_size != 0;
+        sum += ch[j] >= 0 && !refused[j] && len[j] % c.page_size != 0;
     }
     int wanted;
     int off = block_scan(sum, &wanted);  // (its barriers: the claims have been read)
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
+        if (ch[j] >= 0 && refused[j]) {
+            c.lens[ch[j]] = child_len[j];  // (where the claim was put)
+            ch[j] = -1;
+        }
         s_off[i0 + j] = off;
         s_dst[i0 + j] = -1;
         off += ch[j] >= 0 && len[j] % c.page_size != 0;

@@ -518,3 +518,23 @@ def test_a_refused_entry_is_its_sequences_first_all_the_same(seqs):
     assert c.lens[:6].tolist() == [-7, 0, 1, 2, 12, 13]
     with pytest.raises(m.MateError, match="invalid argument"):
         c.status()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("seqs", [6, 5000])
+def test_a_refused_entry_is_its_childs_first_all_the_same(seqs):
+    import paper_2109_04312_b200 as m
+    c = m.Cache.empty(40, 4, 1, 8, seqs, 3, [0])
+    assert m.mate_cache_extend(c, ints([1, 4]), ints([6, 3])).tolist() == [6, 3]
+    lens, table, refs = c.lens.clone(), c.table.clone(), c.refs.clone()
+    # child 0: of no parent, then of 1; child 2: of a sequence that is out of range, then of 1; child 4: not empty, twice
+    m.mate_cache_fork(c, ints([-1, 1, seqs, 1, 1, 1]), ints([0, 0, 2, 2, 4, 4]))
+    assert torch.equal(c.lens, lens) and torch.equal(c.table, table) and torch.equal(c.refs, refs)
+    with pytest.raises(m.MateError, match="invalid argument"):
+        c.status()
+    # a parent whose length is none; then the children are still to be had
+    c.lens[3] = -5
+    m.mate_cache_fork(c, ints([3, 1, 1]), ints([0, 0, 2]))
+    assert c.lens[:6].tolist() == [0, 6, 6, -5, 3, 0] and c.table[2, 0] == c.table[1, 0] and c.refs[:4].tolist() == [2, 1, 1, 1]
+    with pytest.raises(m.MateError, match="invalid argument"):
+        c.status()
