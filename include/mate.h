@@ -280,7 +280,7 @@ int mate_attn_bwd_noalloc(const mate_plan_t *plan, const void *Q, const void *K,
  *   tensors    n_tensors (1 or 2: queries and keys, whose numbers of heads may differ) views of B x
  *              heads x N rows of d contiguous elements of type dtype; x is read, y is written, by strides in
  *              elements (batch, head, token) of their own.  y == x with equal strides works in place;
- *              otherwise they must not overlap.  Any alignment that fits the type (16 bytes and sizes that
+ *              otherwise a y must overlap neither an x nor the other y.  Any alignment that fits the type (16 bytes and sizes that
  *              are multiples of it are faster).
  *   positions  device int32, position of token n of example b at positions[b * position_stride + n] (stride 0: one
  *              row for all examples).  Any value: the angle is formed in 64 bits.  For a table whose positions start

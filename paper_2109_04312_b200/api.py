@@ -353,8 +353,8 @@ def mate_rope(Q, positions, freqs, K=None, interleaved=False, mscale=1.0, backwa
     """Rotary positions (see mate_rope in mate.h).  Q, and K with heads of its own: [B, H, N, d] (or [H, T, d]) CUDA tensors, bf16 or
     f32, of any strides with contiguous rows, for example views of a fused projection's output.  positions: int32 [B, N], or [N] for
     all examples; freqs: float64 [rot / 2] (mate_rope_freqs).  backward: gradients of the inputs from those of the outputs.
-    out: where the result goes (a pair with K), any strides, the inputs themselves included; else new contiguous
-    tensors.  Returns Q' or (Q', K')."""
+    out: where the result goes (a pair with K), any strides: the inputs themselves, or tensors that share no memory with them or with
+    one another; else new contiguous tensors.  Returns Q' or (Q', K')."""
     if _lib is None:
         _load()
     if K is not None and out is not None and not (isinstance(out, (tuple, list)) and len(out) == 2):

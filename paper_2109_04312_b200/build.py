@@ -26,7 +26,7 @@ def _deps():
 
 def build_binding(force: bool = False) -> str:
     """The native module of the Python binding (host code against torch's C++ headers; libmate is not linked)."""
-    deps = BINDING + [os.path.join(CSRC, "binding.h"), os.path.join(ROOT, "include", "mate.h")]
+    deps = BINDING + [os.path.join(CSRC, "binding.h"), os.path.join(CSRC, "overlap.h"), os.path.join(ROOT, "include", "mate.h")]
     if not force and os.path.exists(NATIVE) and all(os.path.getmtime(p) <= os.path.getmtime(NATIVE) for p in deps):
         return NATIVE
     import torch

@@ -2,6 +2,7 @@
 // workspace allocation, the call.  Workspaces are allocated anew for every call (stream-ordered, out of torch's pool, a
 // captured graph's own pool included), so that calls and graphs that overlap share none.
 #include "binding.h"
+#include "overlap.h"
 
 #include <algorithm>
 #include <memory>
@@ -90,6 +91,19 @@ bool distinct(const at::Tensor &t) {
     }
     return true;
 }
+Extent extent(const at::Tensor &t) {
+    Extent e = {reinterpret_cast<int64_t>(t.data_ptr()), (int64_t)t.element_size(), {}};
+    for (int64_t i = 0; i < t.dim(); ++i) e.dims.emplace_back(t.stride(i) * (int64_t)t.element_size(), t.size(i));
+    return e;
+}
+bool overlap(const at::Tensor &a, const at::Tensor &b) { return overlap(extent(a), extent(b)); }
+// The same elements in the same places.
+bool same_place(const at::Tensor &a, const at::Tensor &b) {
+    if (a.data_ptr() != b.data_ptr() || a.scalar_type() != b.scalar_type() || a.sizes() != b.sizes()) return false;
+    for (int64_t i = 0; i < a.dim(); ++i)
+        if (a.size(i) > 1 && a.stride(i) != b.stride(i)) return false;
+    return true;
+}
 int as_int(int64_t x, const char *name) {
     if (x < 0 || x > INT32_MAX) fail_shape(name, "between 0 and 2^31 - 1, and its sizes too");
     return (int)x;
@@ -165,6 +179,12 @@ PyObject *rope(PyObject *, PyObject *const *a, Py_ssize_t n) {
         t[0] = turned(a[0], a[7], "Q", "out", nullptr);
         const bool two = a[1] != Py_None;
         if (two) t[1] = turned(a[1], a[8], "K", "out", &t[0].x);
+        // An output that is given is its own input, or apart from all that is read; two of them are apart.
+        for (int i = 0; i < 1 + two; ++i)
+            for (int j = 0; t[i].y.defined() && j < 1 + two; ++j)
+                if (i == j ? !same_place(t[i].y, t[i].x) && overlap(t[i].y, t[i].x)
+                           : overlap(t[i].y, t[j].x) || (t[j].y.defined() && overlap(t[i].y, t[j].y)))
+                    fail_shape("out", "the inputs themselves, or without memory in common with them, and with one another");
         const at::Tensor &Q = t[0].x;
         const c10::Device device = Q.device();
         const int dt = dtype_code(Q);

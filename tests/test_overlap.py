@@ -1,0 +1,93 @@
+"""Outputs that share memory with inputs or with one another: the check itself against bytes counted one by one, and the calls that
+refuse such outputs."""
+import ctypes
+import os
+import subprocess
+
+import numpy as np
+import pytest
+import torch
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+@pytest.fixture(scope="module")
+def overlap(tmp_path_factory):
+    so = str(tmp_path_factory.mktemp("overlap") / "overlap.so")
+    subprocess.run([os.environ.get("CXX", "g++"), "-O1", "-std=c++17", "-shared", "-fPIC", "-I", os.path.join(ROOT, "paper_2109_04312_b200", "csrc"),
+                    "-o", so, os.path.join(ROOT, "tests", "overlap.cpp")], check=True)
+    lib = ctypes.CDLL(so)
+
+    def call(a, b):
+        args = [(ctypes.c_int64 * (3 + 2 * len(dims)))(at, size, len(dims), *[x for d in dims for x in d]) for at, size, dims in (a, b)]
+        return bool(lib.overlap_(*args))
+    return call
+
+
+def bytes_of(view):
+    at, size, dims = view
+    starts = np.array([at])
+    for stride, n in dims:
+        starts = (starts[:, None] + stride * np.arange(n)).reshape(-1)
+    return {int(s) + i for s in starts for i in range(size)}
+
+
+def test_against_bytes_counted_one_by_one(overlap):
+    rng = np.random.default_rng(0)
+    found = [0, 0]
+    for trial in range(6000):
+        views = []
+        for _ in range(2):
+            size = int(rng.choice([2, 4]))
+            dims = [(int(rng.choice([0, 1, 2, 3, 5, 6, 8, 12, 24, 40])) * size, int(rng.integers(0, 5) if trial % 50 == 0 else rng.integers(1, 5)))
+                    for _ in range(rng.integers(0, 5))]
+            views.append((int(rng.integers(0, 300)) * 2, size, dims))
+        want = bool(bytes_of(views[0]) & bytes_of(views[1]))
+        found[want] += 1
+        assert overlap(*views) == want == overlap(views[1], views[0]), views
+    assert min(found) > 500   # (both answers are met)
+
+
+def test_views_of_large_tensors(overlap):
+    # parts of a fused projection [B, N, H + 2 Hk, d] in bf16, as [B, h, N, d]
+    B, N, H, Hk, d = 64, 32768, 32, 8, 128
+    row = (H + 2 * Hk) * d
+
+    def part(first, heads, tokens=N, shift=0):
+        return (2 * (first * d + shift), 2, [(2 * N * row, B), (2 * d, heads), (2 * row, tokens), (2, d)])
+    assert not overlap(part(0, H), part(H, Hk)) and not overlap(part(H, Hk), part(H + Hk, Hk))
+    assert overlap(part(0, H + 1), part(H, Hk)) and overlap(part(0, H), part(0, H)) and overlap(part(0, H, shift=1), part(H, Hk))
+    # the same memory in another order, and next to it
+    there = (0, 2, [(2 * N * H * d, B), (2 * d, H), (2 * H * d, N), (2, d)])
+    assert overlap(there, (0, 2, [(2 * N * H * d, B), (2 * N * d, H), (2 * d, N), (2, d)]))
+    assert not overlap(there, (2 * B * N * H * d, 2, [(2 * N * H * d, B), (2 * N * d, H), (2 * d, N), (2, d)]))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_rope_refuses_outputs_that_overlap(dtype):
+    import paper_2109_04312_b200 as m
+    B, N, H, d = 2, 40, 3, 16
+    pos, f = torch.arange(N, dtype=torch.int32, device="cuda"), m.mate_rope_freqs(d)
+    flat = torch.randn(4 * B * H * N * d, device="cuda").to(dtype)
+    at = lambda first: flat[first:first + B * H * N * d].view(B, H, N, d)  # noqa: E731
+    Q, K, other = at(0), at(B * H * N * d), at(2 * B * H * N * d)
+    before = flat.clone()
+    for call in (lambda: m.mate_rope(Q, pos, f, out=at(d)), lambda: m.mate_rope(at(d), pos, f, out=Q),                  # shifted by a token
+                 lambda: m.mate_rope(Q, pos, f, out=flat[:B * H * N * d].view(B, N, H, d).transpose(1, 2)),           # in another order
+                 lambda: m.mate_rope(Q, pos, f, K=K, out=(other, other)), lambda: m.mate_rope(Q, pos, f, K=K, out=(K, Q)),
+                 lambda: m.mate_rope(Q, pos, f, K=K, out=(K, other)), lambda: m.mate_rope(Q, pos, f, K=Q, out=(Q, other)),
+                 lambda: m.mate_rope(Q, pos, f, K=K, out=(other, at(2 * B * H * N * d - d))), lambda: m.mate_rope(Q, pos, f, K=K, out=(None, Q))):
+        with pytest.raises(ValueError, match="^out must be the inputs themselves"):
+            call()
+    torch.cuda.synchronize()
+    assert torch.equal(flat, before)
+    q, k = m.mate_rope(Q, pos, f, K=K)
+    # what does not overlap goes through: Q and K in place, one of them only, next to one another, interleaved row by row
+    two = torch.zeros(B, H, 2 * N, d, device="cuda").to(dtype)
+    r = m.mate_rope(Q, pos, f, K=K, out=(two[:, :, 0::2], two[:, :, 1::2]))
+    assert torch.equal(r[0], q) and torch.equal(r[1], k)
+    assert torch.equal(m.mate_rope(Q, pos, f, K=K, out=(other, None))[0], q)
+    assert torch.equal(m.mate_rope(Q, pos, f, K=Q, out=(other, at(3 * B * H * N * d)))[1], q)
+    m.mate_rope(Q, pos, f, K=K, out=(Q, K))
+    assert torch.equal(Q, q) and torch.equal(K, k)
