@@ -346,9 +346,9 @@ int mate_cache_extend(const mate_cache_t *cache, const int32_t *seqs, const int3
 /* Writes the last counts[i] (null: N) tokens of sequence seqs[i] (null: i) into one layer of the cache: token j < counts[i]
  * of entry i goes to position lens[s] - counts[i] + j.  To be called behind mate_cache_extend, with what it granted.
  * A sequence stands at most once in the list (of two entries with the same one either may be what stays).
- *   K, V       new rows, [B, kv_heads, N, d] by strides (batch, head, token)
- *   Q, Q_out   queries of the new tokens, [B, heads, N, d] by strides, and where they go rotated; null: none.  All B N
- *              tokens are rotated, whatever counts says
+ *   K, V       new rows, [B, kv_heads, N, d] by strides (batch, head, token), outside of the cache
+ *   Q, Q_out   queries of the new tokens, [B, heads, N, d] by strides, and where they go rotated (Q itself with equal strides, or
+ *              apart from Q, K and V); null: none.  All B N tokens are rotated, whatever counts says
  *   row_ids, col_ids   device int32 [B, N], or both null (the ids in the cache stay: further layers)
  *   freqs      as in mate_rope, applied to K (and Q); null: neither is rotated (and Q must be null)
  *   positions  device int32 [B, N]; null: the tokens' positions in their sequences

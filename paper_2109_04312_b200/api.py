@@ -404,7 +404,8 @@ def mate_cache_append(cache, K, V, seqs=None, counts=None, row_ids=None, col_ids
                       interleaved=False, mscale=1.0, Q=None, out=None):
     """The last counts[i] (None: N) tokens of sequence seqs[i] (None: i) into one layer of the cache (see mate_cache_append in mate.h).
     K, V: [B, kv_heads, N, d] with contiguous rows; row_ids, col_ids: int32 [B, N], None for further layers.  With freqs
-    K is rotated on the way, and Q [B, heads, N, d] too, which is returned."""
+    K is rotated on the way, and Q [B, heads, N, d] too, which is returned (out: where it goes, Q itself or a tensor that shares no
+    memory with Q, K and V)."""
     return cache._native.cache_append(cache._info, layer, K, V, seqs, counts, row_ids, col_ids, positions, freqs, interleaved, mscale, Q,
                                       out)
 

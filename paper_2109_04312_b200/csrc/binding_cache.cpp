@@ -321,6 +321,8 @@ PyObject *cache_append(PyObject *, PyObject *const *a, Py_ssize_t n) {
             if (q.x.dim() != 4 || q.x.size(0) != B || q.x.size(1) != ci.c.heads || q.x.size(2) != N || q.x.size(3) != ci.c.d ||
                 q.x.scalar_type() != ci.type || q.x.device() != ci.device)
                 fail_shape("Q", "[B, heads, N, d] of the cache's type");
+            if (q.y.defined() && ((!same_place(q.y, q.x) && overlap(q.y, q.x)) || overlap(q.y, K) || overlap(q.y, V)))
+                fail_shape("out", "Q itself, or without memory in common with Q, K and V");
         }
         const int b = as_int(B, "K"), nn = as_int(N, "K");
         const OnDevice on(ci.device);

@@ -91,3 +91,25 @@ def test_rope_refuses_outputs_that_overlap(dtype):
     assert torch.equal(m.mate_rope(Q, pos, f, K=Q, out=(other, at(3 * B * H * N * d)))[1], q)
     m.mate_rope(Q, pos, f, K=K, out=(Q, K))
     assert torch.equal(Q, q) and torch.equal(K, k)
+
+
+@pytest.mark.gpu
+def test_append_refuses_an_output_that_overlaps():
+    import paper_2109_04312_b200 as m
+    B, N, H, Hk, d = 3, 4, 4, 2, 16
+    c, f = m.Cache.empty(9, 4, Hk, d, B, 2, [0, 1] * 2), m.mate_rope_freqs(d)
+    m.mate_cache_extend(c, None, torch.full((B,), N, dtype=torch.int32, device="cuda"))
+    flat = torch.randn(B, N, H + 2 * Hk + H, d, device="cuda").bfloat16()
+    Q, K, V, other = (t.transpose(1, 2) for t in flat.split([H, Hk, Hk, H], 2))
+    want = m.mate_cache_append(c, K, V, freqs=f, Q=Q).clone()
+    before = flat.clone()
+    for out in (flat[:, :, 1:H + 1].transpose(1, 2), flat[:, :, H:2 * H].transpose(1, 2), flat[:, :, H + 1:2 * H + 1].transpose(1, 2),
+                flat[:, :, H + 2:2 * H + 2].transpose(1, 2)):
+        with pytest.raises(ValueError, match="^out must be Q itself"):
+            m.mate_cache_append(c, K, V, freqs=f, Q=Q, out=out)
+    torch.cuda.synchronize()
+    assert torch.equal(flat, before)
+    for out in (other, Q):
+        assert m.mate_cache_append(c, K, V, freqs=f, Q=Q, out=out) is out and torch.equal(out, want)
+    assert torch.equal(flat[:, :, H:H + 2 * Hk], before[:, :, H:H + 2 * Hk])
+    c.status()
