@@ -393,7 +393,8 @@ int mate_cache_status(const mate_cache_t *cache, void *stream);
  *   scale      any finite value
  *   max_len    an upper bound of the sequences' lengths that the caller knows (0: what the table can hold); tokens at
  *              and beyond it do not count, and status says so
- *   O, LSE     [B, heads, d] of the cache's type, float32 [B, heads]; fully overwritten
+ *   O, LSE     [B, heads, d] of the cache's type, float32 [B, heads]; fully overwritten.  O may be Q, if that is contiguous; otherwise the
+ *              three share no memory
  *   workspace  device, 256-byte aligned, mate_cache_workspace_bytes; contents undefined afterwards; calls that overlap need one each
  * Scores, softmax and sums in fp32; with bf16 the weights enter the product with V as the sum of two bf16 (16 bits of
  * mantissa), and only the result is rounded to bf16.  A NaN or Inf in the key or value of a token that one head of a group attends may

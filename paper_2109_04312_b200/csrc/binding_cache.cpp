@@ -454,6 +454,8 @@ PyObject *attn_decode(PyObject *, PyObject *const *a, Py_ssize_t n) {
             if (LSE.sizes() != Q.sizes().slice(0, 2) || LSE.scalar_type() != at::kFloat || !LSE.is_contiguous())
                 fail_shape("LSE", "a contiguous float32 tensor [B, heads]");
         }
+        if (O.defined() && !same_place(O, Q) && overlap(O, Q)) fail_shape("O", "Q itself, or without memory in common with it");
+        if (LSE.defined() && (overlap(LSE, Q) || (O.defined() && overlap(LSE, O)))) fail_shape("LSE", "without memory in common with Q and O");
         const int64_t qs[2] = {B > 1 ? Q.stride(0) : 0, ci.c.heads > 1 ? Q.stride(1) : 0};
         const int b = as_int(B, "Q");
         const OnDevice on(ci.device);

@@ -113,3 +113,38 @@ def test_append_refuses_an_output_that_overlaps():
         assert m.mate_cache_append(c, K, V, freqs=f, Q=Q, out=out) is out and torch.equal(out, want)
     assert torch.equal(flat[:, :, H:H + 2 * Hk], before[:, :, H:H + 2 * Hk])
     c.status()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_decode_refuses_outputs_that_overlap(dtype):
+    import paper_2109_04312_b200 as m
+    B, H, d = 5, 4, 16
+    c = m.Cache.empty(9, 4, 2, d, B, 1, [0, 1] * 2, dtype=dtype)
+    m.mate_cache_extend(c, None, torch.full((B,), 1, dtype=torch.int32, device="cuda"))
+    c.v.normal_()
+    text = torch.full((B,), m.ID_TEXT, dtype=torch.int32, device="cuda")
+    flat = torch.randn(2 * B + 2, H, d, device="cuda").to(dtype)
+    Q = flat[:B]
+    want, lse = m.mate_attn_decode(c, Q, text, text)
+    before = flat.clone()
+    words = flat.view(-1).view(torch.float32)
+    for out in (flat[1:B + 1], flat[B - 1:2 * B - 1]):
+        with pytest.raises(ValueError, match="^O must be Q itself"):
+            m.mate_attn_decode(c, Q, text, text, out=out)
+    with pytest.raises(ValueError, match="^O must be Q itself"):                       # the same beginning, other strides
+        m.mate_attn_decode(c, flat[:2 * B:2], text, text, out=flat[:B])
+    with pytest.raises(ValueError, match="^LSE must be"):
+        m.mate_attn_decode(c, Q, text, text, lse=words[7:7 + B * H].view(B, H))
+    with pytest.raises(ValueError, match="^LSE must be"):
+        m.mate_attn_decode(c, Q, text, text, out=flat[B:2 * B], lse=words[flat[:B + 1].numel() * flat.element_size() // 4:][:B * H].view(B, H))
+    torch.cuda.synchronize()
+    assert torch.equal(flat, before)
+    # every other row is a query, the rows between are not touched
+    o, l = m.mate_attn_decode(c, flat[:2 * B:2], text, text, out=torch.empty_like(want), lse=torch.empty_like(lse))
+    assert torch.equal(flat, before)
+    # next to one another, and in place
+    o, l = m.mate_attn_decode(c, Q, text, text, out=flat[B:2 * B], lse=words[-B * H:].view(B, H))
+    assert torch.equal(o, want) and torch.equal(l, lse)
+    assert torch.equal(m.mate_attn_decode(c, Q, text, text, out=Q)[0], want)
+    c.status()
