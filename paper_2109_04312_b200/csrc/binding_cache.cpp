@@ -96,7 +96,16 @@ Extent extent(const at::Tensor &t) {
     for (int64_t i = 0; i < t.dim(); ++i) e.dims.emplace_back(t.stride(i) * (int64_t)t.element_size(), t.size(i));
     return e;
 }
-bool overlap(const at::Tensor &a, const at::Tensor &b) { return overlap(extent(a), extent(b)); }
+bool overlap(const at::Tensor &a, const at::Tensor &b) {
+    const auto end = [](const at::Tensor &t) {
+        int64_t last = 0;
+        for (int64_t i = 0; i < t.dim(); ++i) last += t.stride(i) * (t.size(i) - 1);
+        return reinterpret_cast<int64_t>(t.data_ptr()) + (last + 1) * (int64_t)t.element_size();
+    };
+    const int64_t at_a = reinterpret_cast<int64_t>(a.data_ptr()), at_b = reinterpret_cast<int64_t>(b.data_ptr());
+    if (end(a) <= at_b || end(b) <= at_a) return false;  // (as most of them: no lists are made)
+    return overlap(extent(a), extent(b));
+}
 // The same elements in the same places.
 bool same_place(const at::Tensor &a, const at::Tensor &b) {
     if (a.data_ptr() != b.data_ptr() || a.scalar_type() != b.scalar_type() || a.sizes() != b.sizes()) return false;
@@ -229,7 +238,7 @@ PyObject *new_cache(PyObject *, PyObject *const *a, Py_ssize_t n) {
             fail_shape("k and v", "of one type and shape, [layers, pages, kv_heads, page_size, d]");
         const int dt = dtype_code(k);
         rows(k, "k"), rows(v, "v");
-        if (k.strides() != v.strides() || !distinct(k) || (k.numel() && k.data_ptr() == v.data_ptr()))
+        if (k.strides() != v.strides() || !distinct(k) || overlap(k, v))
             fail_shape("k and v", "laid out alike, without elements that share their memory");
         if (!THPVariable_Check(a[4]) || THPVariable_Unpack(a[4]).dim() != 2) fail_shape("table", "an int32 CUDA tensor [seqs, width]");
         const at::Tensor &table = THPVariable_Unpack(a[4]);

@@ -148,3 +148,19 @@ def test_decode_refuses_outputs_that_overlap(dtype):
     assert torch.equal(o, want) and torch.equal(l, lse)
     assert torch.equal(m.mate_attn_decode(c, Q, text, text, out=Q)[0], want)
     c.status()
+
+
+def test_a_cache_refuses_keys_and_values_that_overlap():
+    # (host tensors: what passes stops at the next check)
+    import paper_2109_04312_b200 as m
+    z = lambda *s: torch.zeros(s, dtype=torch.int32)  # noqa: E731
+    rest = [z(4, 4), z(4, 4), z(2, 3), z(2), z(2), z(4)]
+    n = 4 * 2 * 4 * 16
+    flat, both = torch.zeros(2 * n), torch.zeros(4, 2, 2, 4, 16)
+    at = lambda first: flat[first:first + n].view(1, 4, 2, 4, 16)  # noqa: E731
+    for k, v in ((at(0), at(0)), (at(0), at(16)), (at(n - 4), at(0)), (at(0), at(n - 128))):
+        with pytest.raises(ValueError, match="^k and v must be laid out alike"):
+            m.Cache(k, v, *rest, [0, 1])
+    for k, v in ((at(0), at(n)), (at(n), at(0)), (both[None, :, 0], both[None, :, 1])):   # keys and values side by side in every page
+        with pytest.raises(ValueError, match="CUDA"):
+            m.Cache(k, v, *rest, [0, 1])
