@@ -176,7 +176,8 @@ int frequencies(PyObject *o, int64_t d, const c10::Device &device, const double 
     const at::Tensor &f = on_gpu(o, "freqs", &device);
     if (f.scalar_type() != at::kDouble || f.dim() != 1 || !f.is_contiguous()) fail_shape("freqs", "a contiguous float64 tensor [rot / 2]");
     if (2 * f.size(0) > d) fail_shape("freqs", "at most d / 2 numbers");
-    *at = f.data_ptr<double>();
+    static const double none = 0.;  // (an empty tensor has no address; the library takes a null one for no rotation, and then no queries)
+    *at = f.size(0) ? f.data_ptr<double>() : &none;
     return (int)(2 * f.size(0));
 }
 

@@ -538,3 +538,23 @@ def test_a_refused_entry_is_its_childs_first_all_the_same(seqs):
     assert c.lens[:6].tolist() == [0, 6, 6, -5, 3, 0] and c.table[2, 0] == c.table[1, 0] and c.refs[:4].tolist() == [2, 1, 1, 1]
     with pytest.raises(m.MateError, match="invalid argument"):
         c.status()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_append_with_no_pairs_to_turn(dtype):
+    # as mate_rope: every element is passed on, queries too
+    import paper_2109_04312_b200 as m
+    c = m.Cache.empty(9, 4, 2, 16, 3, 3, [0, 1, 1, 0], dtype=dtype)
+    n = ints([5, 0, 3])
+    m.mate_cache_extend(c, None, n)
+    Q, K, V = (torch.randn(3, h, 5, 16, device="cuda").to(dtype) for h in (4, 2, 2))
+    none = m.mate_rope_freqs(0)
+    assert torch.equal(m.mate_rope(Q, ints([[7] * 5] * 3), none), Q)
+    for positions in (None, ints([[7] * 5] * 3)):
+        q = m.mate_cache_append(c, K, V, counts=n, freqs=none, positions=positions, mscale=3.0, Q=Q)
+        assert torch.equal(q, Q) and q.data_ptr() != Q.data_ptr()
+    for s, count in enumerate([5, 0, 3]):
+        for j in range(count):
+            assert torch.equal(c.k[0, c.table[s, j // 4], :, j % 4], K[s, :, j]) and torch.equal(c.v[0, c.table[s, j // 4], :, j % 4], V[s, :, j])
+    c.status()
