@@ -325,6 +325,7 @@ PyObject *cache_append(PyObject *, PyObject *const *a, Py_ssize_t n) {
         const unsigned flags = truth(a[10]) ? MATE_ROPE_INTERLEAVED : 0;
         const float mscale = (float)number(a[11]);
         const bool with_q = a[12] != Py_None;
+        if (!with_q && a[13] != Py_None) fail(PyExc_ValueError, "out must be None where no Q is given");
         Turned q = {};
         if (with_q) {
             q = turned(a[12], a[13], "Q", "out", nullptr);

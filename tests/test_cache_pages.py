@@ -558,3 +558,12 @@ def test_append_with_no_pairs_to_turn(dtype):
         for j in range(count):
             assert torch.equal(c.k[0, c.table[s, j // 4], :, j % 4], K[s, :, j]) and torch.equal(c.v[0, c.table[s, j // 4], :, j % 4], V[s, :, j])
     c.status()
+
+
+@pytest.mark.gpu
+def test_append_refuses_an_output_without_queries():
+    import paper_2109_04312_b200 as m
+    c = m.Cache.empty(9, 4, 2, 16, 3, 3, [0, 1, 1, 0])
+    K = torch.zeros(3, 2, 1, 16, device="cuda").bfloat16()
+    with pytest.raises(ValueError, match="^out must be None"):
+        m.mate_cache_append(c, K, K, freqs=m.mate_rope_freqs(16), out=torch.zeros(3, 4, 1, 16, device="cuda").bfloat16())
