@@ -218,13 +218,15 @@ int launch(RopeParams &p, int device, cudaStream_t st) {
     // 23.0 us; 23.9 with 1024, 28.1 with 4096).
     int64_t n_heads = 0, slices = 0;
     for (int i = 0; i < p.n_sides; ++i) n_heads += p.side[i].heads;
-    const int64_t heads = threads * n_heads / ((p.paged ? 2048 : 1024) * (int64_t)n_sms(device));
-    p.heads_of_thread = heads <= 2 ? (heads < 1 ? 1 : (int)heads) : (int)((heads < n_heads ? heads : n_heads) + kFlight - 1) / kFlight * kFlight;
+    const double per_thread = (double)threads * n_heads / ((p.paged ? 2048. : 1024.) * n_sms(device));  // (the product passes 64 bits)
+    const int64_t heads = per_thread < n_heads ? (int64_t)per_thread : n_heads;
+    p.heads_of_thread = heads <= 2 ? (heads < 1 ? 1 : (int)heads) : (int)(heads + kFlight - 1) / kFlight * kFlight;
+    constexpr int kSlices = 65535 - 3;  // of a launch, less the last ones of three tensors, which are not full
+    if (n_heads > (int64_t)kSlices * p.heads_of_thread) p.heads_of_thread = (int)((n_heads + kSlices - 1) / kSlices);
     for (int i = 0; i < p.n_sides; ++i) {
         p.side[i].first_slice = (int)slices;
         slices += (p.side[i].heads + p.heads_of_thread - 1) / p.heads_of_thread;
     }
-    if (slices > 65535) return MATE_ERR_UNSUPPORTED;
     return launch_after(rope_kernel<T, VEC>, dim3((unsigned)blocks, (unsigned)slices), kThreads, sizeof(uint64_t) * (p.rot / 2), st, p) == cudaSuccess
                ? MATE_OK
                : MATE_ERR_CUDA;

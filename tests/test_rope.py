@@ -200,3 +200,17 @@ def test_the_c_entry_refuses_before_anything_is_launched():
         assert call(**kw) == -3, kw
     for kw in (dict(B=0), dict(N=0), dict(heads=0)):
         assert call(**kw) == 0, kw
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("H,Hk,N", [(65535, 2, 1), (65536, 1, 1), (70000, 66000, 1), (140001, 3, 2)])
+def test_more_heads_than_a_launch_has_rows_of_blocks(H, Hk, N, dtype):
+    # examples folded into the heads
+    import paper_2109_04312_b200 as m
+    g = torch.Generator().manual_seed(H)
+    Q, K = (torch.randn(h, N, 8, generator=g).to(DT[dtype]).cuda() for h in (H, Hk))
+    pos, f = torch.arange(N, dtype=torch.int32, device="cuda") + 5, m.mate_rope_freqs(8)
+    q, k = m.mate_rope(Q, pos, f, K=K)
+    check(q, Q, pos, f, dtype)
+    check(k, K, pos, f, dtype)
