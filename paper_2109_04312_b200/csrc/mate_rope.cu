@@ -5,7 +5,8 @@
 // angle's whole turns do not matter, so a frequency is kept as a 64-bit fraction of a turn per position and multiplied by the
 // position modulo 2^64: exact but for the fraction's own rounding (2^-65 turns per position and the 2^-53 of the 64-bit
 // frequency), for three integer instructions.  (In 64-bit floating point the same took most of the kernel's time.)  Sine and
-// cosine of the fraction that is left are taken in fp32 by sincospif.
+// cosine of the fraction that is left are taken in fp32 by sincospif, with 32 bits of it: fp32 holds 24, what they leave (9e-8 rad at
+// most) is added to first order where the elements are fp32.
 //
 // Bound by memory: one read and one write of every element.  A thread has one token and one unit of its rows -- two runs of VEC
 // elements, which are VEC pairs -- works out their sines and cosines once and takes the heads of its slice in turn, kFlight at
@@ -167,7 +168,15 @@ __global__ void __launch_bounds__(kThreads, 6) rope_kernel(const __grid_constant
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
             const int64_t turn = (int64_t)(s_turn[chunk * VEC + e] * (uint64_t)(int64_t)position);
-            sincospif((float)(int32_t)(turn >> 32) * 4.656612873077393e-10f, &sn[e], &cs[e]);  // 2^-31
+            const int32_t half_turns = (int32_t)(turn >> 32);  // in 2^-31
+            const float rounded = (float)half_turns;
+            sincospif(rounded * 4.656612873077393e-10f, &sn[e], &cs[e]);  // 2^-31
+            if (sizeof(T) == 4) {  // bf16 does not show what the rounding left
+                const float rest = (float)(half_turns - __float2int_rn(rounded)) * 1.4629180792671596e-9f;  // pi 2^-31
+                const float c = cs[e];
+                cs[e] = fmaf(-sn[e], rest, c);
+                sn[e] = fmaf(c, rest, sn[e]);
+            }
             cs[e] *= p.mscale;
             sn[e] *= p.mscale * p.sign;
         }

@@ -214,3 +214,22 @@ def test_more_heads_than_a_launch_has_rows_of_blocks(H, Hk, N, dtype):
     q, k = m.mate_rope(Q, pos, f, K=K)
     check(q, Q, pos, f, dtype)
     check(k, K, pos, f, dtype)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("backward", [False, True])
+def test_the_angle_keeps_more_bits_than_fp32(interleaved, backward):
+    # rows of (1, 0) and (0, 1): what comes out is the cosine and the sine themselves.  sincospif is good to an ulp, 2^-24 for values below
+    # 1; what is added to it is rounded with it once, 2^-25; the 32-bit fraction of a turn is cut off by at most pi 2^-31 = 1.5e-9 rad, and the
+    # 64-bit angle on either side (1e5 x 2^-52 rad) does not count.  The angle rounded to fp32 would be off by up to pi 2^-25 = 9.4e-8 rad more.
+    import paper_2109_04312_b200 as m
+    N, d = 20000, 64
+    pos = torch.randint(0, 100000, (N,), generator=torch.Generator().manual_seed(3), dtype=torch.int32).cuda()
+    f = m.mate_rope_freqs(d)
+    x = torch.zeros(1, 2, N, d, device="cuda")
+    first = torch.arange(d, device="cuda") % 2 == 0 if interleaved else torch.arange(d, device="cuda") < d // 2
+    x[:, 0, :, first], x[:, 1, :, ~first] = 1.0, 1.0
+    got = m.mate_rope(x, pos, f, interleaved=interleaved, backward=backward).double().cpu().numpy()
+    want = turn(x.double().cpu().numpy(), pos.cpu().numpy(), f.cpu().numpy(), interleaved, backward=backward)
+    assert np.abs(got - want).max() <= 2.0 ** -24 + 2.0 ** -25 + 2e-9
