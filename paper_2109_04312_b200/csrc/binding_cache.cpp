@@ -23,10 +23,12 @@ struct Library {
     decltype(&mate_attn_decode) decode = nullptr;
 } lib;
 
-// A cache as the calls take it; lives in a capsule of the Python object, which holds the tensors.
+// A cache as the calls take it; lives in a capsule of the Python object.  It holds the tensors' memory itself: an attribute of that object may be
+// set to another tensor, and the calls go on with the addresses in `c`.
 struct CacheInfo {
     mate_cache_t c;
     std::vector<uint8_t> head_view;
+    std::vector<c10::Storage> memory;
     at::ScalarType type;
     c10::Device device;
 };
@@ -246,7 +248,7 @@ PyObject *new_cache(PyObject *, PyObject *const *a, Py_ssize_t n) {
         if (!PyBytes_Check(a[9])) fail_shape("head_view", "bytes");
         const int64_t pages = k.size(1), page_size = k.size(3), seqs = table.size(0), width = table.size(1);
         const c10::Device device = k.device();
-        auto info = std::make_unique<CacheInfo>(CacheInfo{{}, {}, k.scalar_type(), device});
+        auto info = std::make_unique<CacheInfo>(CacheInfo{{}, {}, {}, k.scalar_type(), device});
         mate_cache_t &c = info->c;
         struct {
             int32_t **to;
@@ -259,6 +261,7 @@ PyObject *new_cache(PyObject *, PyObject *const *a, Py_ssize_t n) {
         if (!k.is_cuda() || v.device() != device) fail_shape("k and v", "CUDA tensors on one device");
         const uint8_t *view = reinterpret_cast<const uint8_t *>(PyBytes_AS_STRING(a[9]));
         info->head_view.assign(view, view + PyBytes_GET_SIZE(a[9]));
+        for (int i = 0; i < 9; ++i) info->memory.push_back(THPVariable_Unpack(a[i]).storage());
         c.k = k.data_ptr(), c.v = v.data_ptr();
         c.head_view = info->head_view.data();
         // (a stride that nothing is multiplied by need not fit the alignment)

@@ -567,3 +567,31 @@ def test_append_refuses_an_output_without_queries():
     K = torch.zeros(3, 2, 1, 16, device="cuda").bfloat16()
     with pytest.raises(ValueError, match="^out must be None"):
         m.mate_cache_append(c, K, K, freqs=m.mate_rope_freqs(16), out=torch.zeros(3, 4, 1, 16, device="cuda").bfloat16())
+
+
+@pytest.mark.gpu
+def test_the_memory_stays_while_the_cache_lives():
+    # attributes set to other tensors: the calls go by the ones the cache was made of, whose memory nobody else gets meanwhile
+    import gc
+
+    import paper_2109_04312_b200 as m
+    torch.cuda.synchronize()
+    gc.collect()
+    base = torch.cuda.memory_allocated()
+    c = m.Cache.empty(64, 16, 4, 64, 8, 8, [0] * 4, layers=4)
+    held = torch.cuda.memory_allocated() - base
+    assert held > 2 * 64 * 16 * 4 * 64 * 2 * 4
+    for name in ("k", "v", "row_ids", "col_ids", "table", "lens", "prefix", "refs", "status_word"):
+        setattr(c, name, None)
+    gc.collect()
+    assert torch.cuda.memory_allocated() - base == held
+    assert m.mate_cache_extend(c, ints([3]), ints([17])).tolist() == [17]
+    assert m.mate_cache_compact(c) == 2
+    c.status()
+    c = m.Cache.empty(4, 4, 1, 8, 2, 2, [0])
+    k = c.k.data_ptr()
+    c.k.data = torch.zeros(1, 4, 1, 4, 8, device="cuda").bfloat16()      # the tensor itself gets other memory
+    assert torch.zeros(1, 4, 1, 4, 8, device="cuda").bfloat16().data_ptr() != k
+    del c
+    gc.collect()
+    assert torch.cuda.memory_allocated() == base
