@@ -390,7 +390,7 @@ int mate_cache_status(const mate_cache_t *cache, void *stream);
  *   Q          [B, heads, d] by strides (batch, head), of the cache's type, 16-byte aligned rows
  *   row_ids, col_ids   device int32 [B], the new token's ids (MATE_ID_TEXT: text; negative: padding, O = 0 and LSE = -inf, as
  *              for a sequence without a token that may be attended)
- *   scale      any finite value
+ *   scale      any finite value of up to 2.3e38 in magnitude (scale / ln 2 is what the kernel multiplies by)
  *   max_len    an upper bound of the sequences' lengths that the caller knows (0: what the table can hold); tokens at
  *              and beyond it do not count, and status says so
  *   O, LSE     [B, heads, d] of the cache's type, float32 [B, heads]; fully overwritten.  O may be Q, if that is contiguous; otherwise the

@@ -24,6 +24,7 @@
 // of 16 tables of up to 8192 tokens 18 us, one table of 512 tokens 5.9 us: chains of dependent loads (sequence, length, page, ids, keys).
 #include <cuda_bf16.h>
 
+#include <cmath>
 #include <type_traits>
 
 #include "mate_cache.h"
@@ -898,6 +899,8 @@ extern "C" int mate_attn_decode(const mate_cache_t *cache, int layer, const void
     if (rc != MATE_OK) return rc;
     if (layer < 0 || layer >= cache->layers || B < 0 || max_len < 0 || (!seqs && B > cache->seqs)) return MATE_ERR_INVALID_ARG;
     if (B > 0 && (!Q || !q_stride || !row_ids || !col_ids || !O || !LSE)) return MATE_ERR_INVALID_ARG;
+    if (!std::isfinite(scale)) return MATE_ERR_INVALID_ARG;
+    if (!std::isfinite(scale * kLog2e)) return MATE_ERR_UNSUPPORTED;  // (0 times what it would be is not a number)
     const int64_t reach = (cache->pages - 1) * cache->page_stride + (cache->kv_heads - 1) * cache->head_stride + (cache->page_size - 1) * cache->slot_stride;
     if (cache->heads > kMaxHeads || reach / (int64_t)(16 / elem_size(cache->dtype)) > UINT32_MAX) return MATE_ERR_UNSUPPORTED;
     const int vec = (int)(16 / elem_size(cache->dtype));

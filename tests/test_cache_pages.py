@@ -595,3 +595,19 @@ def test_the_memory_stays_while_the_cache_lives():
     del c
     gc.collect()
     assert torch.cuda.memory_allocated() == base
+
+
+def test_scales_that_the_attention_of_one_token_refuses():
+    from paper_2109_04312_b200 import build
+    lib = ctypes.CDLL(build.build())
+    s, at = struct()
+    P, z = ctypes.c_void_p, (ctypes.c_int64 * 3)(0, 64, 64)
+
+    def decode(scale, B=0):
+        return lib.mate_attn_decode(ctypes.byref(s), 0, P(at), z, B, P(at), P(at), P(at), ctypes.c_float(scale), 0, P(at), P(at), P(at),
+                                    ctypes.c_size_t(1 << 30), None)
+
+    for scale, status in ((float("nan"), -1), (float("inf"), -1), (-float("inf"), -1), (3.4e38, -2), (-2.4e38, -2)):
+        assert decode(scale) == status == decode(scale, 1), scale
+    for scale in (2.3e38, -2.3e38, 0.0, 1e-45):    # these go on to the next check: here, for the device
+        assert decode(scale) not in (-1, -2)
