@@ -11,9 +11,9 @@
 //     block barrier until the sequence's part is done.  What nobody attends is never read, padding's keys and values included.
 //   - the products are tensor-core ones (m16n8k16) with the keys as the 16 rows and the heads as the 8 columns, so that a group
 //     of up to 8 costs one of them; the tensor pipe is 14 % busy while HBM is the limit.  The weights go from one product's
-//     result to the other's operand by transposing 8 x 8 pieces between the lanes, as the sum of two bf16: the second product costs
-//     1 % (64 sequences, 72.1 -> 73.1 us), rounding them to bf16 would make the error against 64 bits 2.4e-3 instead of the 1.7e-3 that the
-//     result's own rounding makes.  fp32 caches: multiply-adds.
+//     result to the other's operand by transposing 8 x 8 pieces between the lanes, as the sum of three bf16, which is all of their 24
+//     bits (one table of 512 tokens 5.67 -> 5.94 us, cells 18.4 -> 18.7, 64 sequences 74.1 -> 74.6 against two, whose 16 bits showed
+//     in one result of 500 that rounded to the neighbouring bf16, and in small differences of large weights).  fp32 caches: multiply-adds.
 //   - blocks get equal shares of all sequences' tokens in units of kUnit (found by every block from the lengths, which the host does not
 //     know), so one long sequence is spread over the GPU and short ones are put together.  A sequence that falls to several
 //     blocks is joined by a second kernel from their partial results, in the order of its tokens: the same bits on every launch.
@@ -380,6 +380,7 @@ template <int DP, int NB>
 struct Reader<__nv_bfloat16, DP, NB> {
     using S = Shape<__nv_bfloat16, DP, NB>;
     static constexpr int kTiles = S::kKeys / 16;
+    static constexpr int kParts = 3;  // bf16 numbers whose sum is a weight
     uint32_t q[DP / 16][NB][2];      // B operand: k = element, n = head
     float o[DP / 16][NB][4];         // rows: elements lane / 4 (+ 8), columns: heads 2 (lane % 4) + {0, 1}
     float m[NB][2], l[NB][2];        // of those heads; l: of the lane's own keys
@@ -435,7 +436,7 @@ struct Reader<__nv_bfloat16, DP, NB> {
             }
         constexpr uint32_t kFull = S::kKeys < 32 ? (1u << S::kKeys) - 1 : ~0u;
         const bool all = (meta.by_row & meta.by_col) == kFull;
-        uint32_t w[kTiles][NB][2], rest[kTiles][NB][2];
+        uint32_t w[kParts][kTiles][NB][2];
         float keep[NB][2];
         bool moved = false;
 #pragma unroll
@@ -491,10 +492,13 @@ struct Reader<__nv_bfloat16, DP, NB> {
             for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
-                    const float x = s[t][nb][2 * half], y = s[t][nb][2 * half + 1];
-                    const uint32_t xy = ptx::cvt_bf16x2(x, y);
-                    w[t][nb][half] = transpose8(xy);
-                    rest[t][nb][half] = transpose8(ptx::cvt_bf16x2(x - __uint_as_float(xy << 16), y - __uint_as_float(xy & 0xffff0000u)));
+                    float x = s[t][nb][2 * half], y = s[t][nb][2 * half + 1];
+#pragma unroll
+                    for (int i = 0; i < kParts; ++i) {
+                        const uint32_t xy = ptx::cvt_bf16x2(x, y);
+                        w[i][t][nb][half] = transpose8(xy);
+                        x -= __uint_as_float(xy << 16), y -= __uint_as_float(xy & 0xffff0000u);
+                    }
                 }
 #pragma unroll
         for (int k = 0; k < DP / 16; ++k)
@@ -503,10 +507,9 @@ struct Reader<__nv_bfloat16, DP, NB> {
                 uint32_t a[4];
                 ldmatrix4_trans(a, (value_at ^ 32 * k) + t * 16 * S::kRowBytes);
 #pragma unroll
-                for (int nb = 0; nb < NB; ++nb) {
-                    mma16816(o[k][nb], a, w[t][nb]);
-                    mma16816(o[k][nb], a, rest[t][nb]);
-                }
+                for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                    for (int i = 0; i < kParts; ++i) mma16816(o[k][nb], a, w[i][t][nb]);
             }
     }
     // The warp's result: [n_rows][d] un-normalised, then maxima and sums.

@@ -432,3 +432,32 @@ def test_a_table_read_token_by_token(name):
         assert (l.double() - torch.logsumexp(x, -1)).abs().max() < 1e-4
     c.status()
     plan.status()
+
+
+@pytest.mark.parametrize("H,d", [(1, 64), (1, 128), (16, 64), (16, 128)])
+def test_weights_keep_their_fp32_bits(H, d):
+    # Three keys with scores 0, -a and -a - 2^-12 and values 0, 1 and -1: O is the small difference of two weights, (w - w') / (1 + w + w'), which shows
+    # what the weights lost on their way to the product with the values.  The scores are exact (a has 8 bits).  A weight: scale / ln 2 is
+    # the same for both (it cancels to first order), its product with the score, below 2, is rounded once (2^-24 of 1, 2^-24 ln 2 of the weight),
+    # ex2 is good to 2^-22.  What is summed after the leading parts have cancelled is below 2^-8 (each sum 2^-23 of that, six of them).  Sum, division: 2^-22
+    # of the result; its rounding to bf16: 2^-8 of it.
+    import paper_2109_04312_b200 as m
+    a = torch.arange(64, 64 + 256, dtype=torch.float64) / 256       # 0.25 to 1.25
+    a = a[a.bfloat16().double() == a]
+    S, delta = len(a), 2.0 ** -12
+    assert S > 100
+    c = m.Cache.empty(S, 16, 1, d, S, 1, [0] * H)
+    m.mate_cache_extend(c, None, torch.full((S,), 3, dtype=torch.int32, device="cuda"))
+    K, V = (torch.zeros(S, 1, 3, d, dtype=torch.float64) for _ in range(2))
+    K[:, 0, 1, 0], K[:, 0, 2, 0], K[:, 0, 2, 1] = -a, -a, -delta
+    V[:, 0, 1], V[:, 0, 2] = 1.0, -1.0
+    ids = torch.full((S, 3), TEXT, dtype=torch.int32, device="cuda")
+    m.mate_cache_append(c, K.bfloat16().cuda(), V.bfloat16().cuda(), row_ids=ids, col_ids=ids)
+    Q = torch.zeros(S, H, d, device="cuda").bfloat16()
+    Q[..., :2] = 1.0
+    O = m.mate_attn_decode(c, Q, ids[:, 0].contiguous(), ids[:, 0].contiguous(), scale=1.0)[0].double().cpu()
+    w, w2 = torch.exp(-a), torch.exp(-a - delta)
+    want = ((w - w2) / (1 + w + w2))[:, None, None]
+    tol = 2 * (w / (1 + 2 * w2))[:, None, None] * (2.0 ** -22 + 2.0 ** -24) + 6 * 2.0 ** -31 + (2.0 ** -22 + 2.0 ** -8) * want
+    assert bool(((O - want).abs() <= tol).all()), ((O - want).abs() / tol).max()
+    c.status()
