@@ -396,8 +396,8 @@ int mate_cache_status(const mate_cache_t *cache, void *stream);
  *   O, LSE     [B, heads, d] of the cache's type, float32 [B, heads]; fully overwritten.  O may be Q, if that is contiguous; otherwise the
  *              three share no memory
  *   workspace  device, 256-byte aligned, mate_cache_workspace_bytes; contents undefined afterwards; calls that overlap need one each
- * Scores, softmax, weights and sums in fp32; with bf16 only the result is rounded.  A NaN or Inf in the key or value of a token that one head of a group attends may
- * also reach the others of the group.  heads <= 1024.  Asynchronous on `stream`. */
+ * Scores, softmax, weights and sums in fp32; with bf16 only the result is rounded.  A NaN or Inf in the key or value of a token
+ * reaches the heads that attend the token and no others.  heads <= 1024.  Asynchronous on `stream`. */
 int mate_attn_decode(const mate_cache_t *cache, int layer, const void *Q, const int64_t *q_stride, int B, const int32_t *seqs,
                      const int32_t *row_ids, const int32_t *col_ids, float scale, int max_len, void *O, float *LSE, void *workspace,
                      size_t workspace_bytes, void *stream);

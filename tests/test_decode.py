@@ -461,3 +461,44 @@ def test_weights_keep_their_fp32_bits(H, d):
     tol = 2 * (w / (1 + 2 * w2))[:, None, None] * (2.0 ** -22 + 2.0 ** -24) + 6 * 2.0 ** -31 + (2.0 ** -22 + 2.0 ** -8) * want
     assert bool(((O - want).abs() <= tol).all()), ((O - want).abs() / tol).max()
     c.status()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("H,Hk,views", [(3, 1, [0, 1, 2]), (8, 1, [0, 1] * 4), (8, 2, [0, 2, 0, 2, 1, 1, 2, 1]), (17, 1, [0, 1, 2] * 5 + [1, 0])])
+@pytest.mark.parametrize("d", [64, 48, 128])
+def test_what_is_not_a_number_reaches_the_heads_that_attend_it(H, Hk, views, d, dtype):
+    # tokens of the new token's row, of its column and of neither get keys and values that are not numbers, each kind in turn: the heads that do
+    # not attend them give the same bits as with zeros there
+    import paper_2109_04312_b200 as m
+    for lens in ([40, 7, 300, 130], [3000, 700], [0, 513] * 40):
+        case = Case(m, lens, H, Hk, d, 16, views, dtype, pad=0.0, rows=6, cols=5, seed=H + d)
+        S = len(lens)
+        q_ids = np.full((2, S), 2, np.int32)
+        i32 = lambda x: torch.tensor(np.asarray(x), dtype=torch.int32, device="cuda")  # noqa: E731
+        Q = torch.randn(S, H, d, device="cuda").to(DT[dtype])
+        clean = [x.clone() for x in (case.c.k, case.c.v)]
+        call = lambda: m.mate_attn_decode(case.c, Q, i32(q_ids[0]), i32(q_ids[1]))  # noqa: E731
+        case.check(Q[:3], list(range(min(S, 3))), q_ids, *[x[:3] for x in call()])
+        for kind in ("row", "col", "both", "neither"):
+            slots, reached = [], np.zeros((S, H), bool)
+            for s, n in enumerate(lens):
+                row, col = case.ids[s]
+                always = (np.arange(n) < case.prefix[s]) | (row == TEXT)
+                own = {"row": (row == 2) & (col != 2), "col": (row != 2) & (col == 2), "both": (row == 2) & (col == 2),
+                       "neither": (row != 2) & (col != 2)}[kind] & ~always
+                slots += [(case.table[s, j // 16], j % 16) for j in np.flatnonzero(own)]
+                sees = {"row": (0, 2), "col": (1, 2), "both": (0, 1, 2), "neither": ()}[kind]
+                reached[s] = own.any() & np.isin(views, sees)
+            at = torch.tensor(slots, device="cuda").T
+            results = []
+            for value in (0.0, float("nan"), float("inf"), -float("inf")):
+                for x, y in zip((case.c.k, case.c.v), clean):
+                    x.copy_(y)
+                    if len(slots):
+                        x[0, at[0], :, at[1]] = value
+                results.append(call())
+            stays = torch.from_numpy(~reached).cuda()
+            for i, (O, LSE) in enumerate(results[1:]):
+                assert torch.equal(O[stays], results[0][0][stays]) and torch.equal(LSE[stays], results[0][1][stays]), (kind, i)
+                assert i or (O[~stays].isnan().all() and LSE[~stays].isnan().all())   # (a NaN; infinite keys may also have weight 0)
+    case.c.status()
