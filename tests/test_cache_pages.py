@@ -611,3 +611,26 @@ def test_scales_that_the_attention_of_one_token_refuses():
         assert decode(scale) == status == decode(scale, 1), scale
     for scale in (2.3e38, -2.3e38, 0.0, 1e-45):    # these go on to the next check: here, for the device
         assert decode(scale) not in (-1, -2)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_queries_turn_by_their_positions_in_their_sequences(interleaved, dtype):
+    # no positions given: token j of the last n of a sequence of L stands at L - n + j, its query as its key; behind them there is no
+    # token, and the queries are turned by position 0
+    import paper_2109_04312_b200 as m
+    B, N, H, Hk, d = 3, 5, 4, 2, 16
+    c, f = m.Cache.empty(40, 4, Hk, d, 6, 9, [0, 1] * 2, dtype=dtype), m.mate_rope_freqs(d)
+    seqs, counts = ints([4, 0, 2]), ints([5, 0, 3])
+    m.mate_cache_extend(c, ints([2, 0]), ints([17, 9]))
+    m.mate_cache_extend(c, seqs, counts)
+    Q, K, V = (torch.randn(B, h, N, d, device="cuda").to(dtype) for h in (H, Hk, Hk))
+    q = m.mate_cache_append(c, K, V, seqs, counts, freqs=f, interleaved=interleaved, mscale=0.9, Q=Q)
+    own = ints([[0, 1, 2, 3, 4], [0, 0, 0, 0, 0], [17, 18, 19, 0, 0]])
+    assert torch.equal(q, m.mate_rope(Q, own, f, interleaved=interleaved, mscale=0.9))
+    want = turn(Q.double().cpu().numpy(), own.cpu().numpy()[:, None], f.cpu().numpy(), interleaved, 0.9)
+    # sine, cosine and their products in fp32 (6e-7 of |a| + |b|), the result's rounding
+    tol = 6e-7 * 2 * Q.abs().max().item() + (np.abs(want) * 2.0 ** -8 if dtype == torch.bfloat16 else 0)
+    assert np.all(np.abs(q.double().cpu().numpy() - want) <= tol)
+    c.status()

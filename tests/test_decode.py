@@ -502,3 +502,33 @@ def test_what_is_not_a_number_reaches_the_heads_that_attend_it(H, Hk, views, d, 
                 assert torch.equal(O[stays], results[0][0][stays]) and torch.equal(LSE[stays], results[0][1][stays]), (kind, i)
                 assert i or (O[~stays].isnan().all() and LSE[~stays].isnan().all())   # (a NaN; infinite keys may also have weight 0)
     case.c.status()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("lens", [[5000], [20000, 3, 700], [2500] * 9, [0, 1, 1025, 0, 3000]])
+@pytest.mark.parametrize("H,Hk,d", [(16, 1, 128), (17, 1, 64), (40, 2, 96), (50, 1, 128), (20, 2, 8)])
+def test_large_groups_shared_out_and_joined(dtype, lens, H, Hk, d):
+    # more than eight heads to a block, several blocks to a group (the last one with fewer heads), items that fall to several blocks
+    import paper_2109_04312_b200 as m
+    case = Case(m, lens, H, Hk, d, 16, [h % 3 if H < 20 else int(h >= 7) for h in range(H)], dtype, seed=len(lens) + H, rows=40, cols=7, prefix=60)
+    run(m, case)
+    run(m, case, max_len=max(lens), seed=5)
+    case.c.status()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("H,Hk,d", [(16, 1, 128), (32, 2, 64), (19, 1, 40)])
+def test_large_groups_a_block_to_each_item(dtype, H, Hk, d):
+    # more items than SMs, none of them long: four warps, an item to a block
+    import paper_2109_04312_b200 as m
+    rng = np.random.default_rng(H)
+    lens = rng.integers(0, 500, 160).tolist()
+    case = Case(m, lens, H, Hk, d, 16, [h % 2 for h in range(H)], dtype, seed=H, rows=9, cols=4)
+    seqs = rng.permutation(160).tolist()
+    q_ids = case.new_ids(seqs)
+    Q = torch.randn(160, H, d, device="cuda").to(DT[dtype])
+    i32 = lambda x: torch.tensor(np.asarray(x), dtype=torch.int32, device="cuda")  # noqa: E731
+    O, LSE = m.mate_attn_decode(case.c, Q, i32(q_ids[0]), i32(q_ids[1]), seqs=i32(seqs), max_len=512)
+    some = rng.permutation(160)[:25].tolist()
+    case.check(Q[some], [seqs[i] for i in some], q_ids[:, some], O[some], LSE[some])
+    case.c.status()
