@@ -634,3 +634,65 @@ def test_queries_turn_by_their_positions_in_their_sequences(interleaved, dtype):
     tol = 6e-7 * 2 * Q.abs().max().item() + (np.abs(want) * 2.0 ** -8 if dtype == torch.bfloat16 else 0)
     assert np.all(np.abs(q.double().cpu().numpy() - want) <= tol)
     c.status()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("slots_first", [False, True])
+def test_pages_of_the_largest_size(slots_first, dtype):
+    # 2^20 rows of keys to a page: partly filled ones copied, whole ones moved
+    import paper_2109_04312_b200 as m
+    ps, pages, d = 1 << 19, 5, 8
+    shape = (1, pages, ps, 2, d) if slots_first else (1, pages, 2, ps, d)
+    k, v = (torch.zeros(shape, dtype=dtype, device="cuda") for _ in range(2))
+    if slots_first:
+        k, v = k.transpose(2, 3), v.transpose(2, 3)
+    z = lambda *s: torch.zeros(s, dtype=torch.int32, device="cuda")  # noqa: E731
+    c = m.Cache(k, v, z(pages, ps), z(pages, ps), z(4, 2) - 1, z(4), z(4), z(pages), [0, 1])
+    n = ints([ps + 5, ps - 3])
+    assert m.mate_cache_extend(c, None, n).tolist() == n.tolist() and c.table[:2].tolist() == [[0, 1], [2, -1]]
+    K, V = (torch.randn(2, 2, ps + 5, d, device="cuda").to(dtype) for _ in range(2))
+    ids = torch.arange(2 * (ps + 5), dtype=torch.int32, device="cuda").view(2, -1)
+    m.mate_cache_append(c, K, V, counts=n, row_ids=ids, col_ids=ids + 1)
+    m.mate_cache_fork(c, ints([1, 0]), ints([3, 2]))
+    assert c.table[2:].tolist() == [[0, 4], [3, -1]] and c.lens.tolist() == [ps + 5, ps - 3] * 2
+    m.mate_cache_free(c, ints([1]))
+    assert int(m.mate_cache_compact(c)) == 4 and c.table.tolist() == [[0, 1], [-1, -1], [0, 2], [3, -1]]
+    for s, of in ((0, 0), (2, 0), (3, 1)):
+        for i, page in enumerate(p for p in c.table[s].tolist() if p >= 0):
+            some = slice(i * ps, min((i + 1) * ps, int(n[of])))
+            fill = some.stop - some.start
+            assert torch.equal(c.k[0, page, :, :fill], K[of, :, some]) and torch.equal(c.v[0, page, :, :fill], V[of, :, some])
+            assert torch.equal(c.row_ids[page, :fill], ids[of, some]) and torch.equal(c.col_ids[page, :fill], ids[of, some] + 1)
+    c.status()
+
+
+@pytest.mark.gpu
+def test_beams_in_a_graph():
+    # children dropped, made anew and moved together, captured once and replayed after the parents have grown; another graph shares no workspace
+    import paper_2109_04312_b200 as m
+    c, model = make(m, pages=70, seqs=8, width=6, page_size=4)
+    parents, children = ints([0, 1, 0, 1]), ints([4, 5, 6, 7])
+    mark = append(m, c, model, [0, 1], m.mate_cache_extend(c, ints([0, 1]), ints([3, 6])).tolist() and model.extend([0, 1], [3, 6]), 1)
+    m.mate_cache_fork(c, parents, children)
+    model.fork([0, 1, 0, 1], [4, 5, 6, 7])
+    graphs, lives = [], []
+    for _ in range(2):
+        g, live = torch.cuda.CUDAGraph(), ints(0)
+        with torch.cuda.graph(g):
+            m.mate_cache_free(c, children)
+            m.mate_cache_fork(c, parents, children)
+            m.mate_cache_compact(c, live)
+        graphs.append(g)
+        lives.append(live)
+    same(c, model, "captured only")
+    for step in range(6):
+        granted = m.mate_cache_extend(c, ints([0, 1]), ints([2, 1])).tolist()
+        assert granted == model.extend([0, 1], [2, 1])
+        mark = append(m, c, model, [0, 1], granted, mark)
+        graphs[step % 2].replay()
+        model.free([4, 5, 6, 7])
+        model.fork([0, 1, 0, 1], [4, 5, 6, 7])
+        assert int(lives[step % 2]) == model.compact()
+        same(c, model, step)
+    c.status()

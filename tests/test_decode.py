@@ -532,3 +532,16 @@ def test_large_groups_a_block_to_each_item(dtype, H, Hk, d):
     some = rng.permutation(160)[:25].tolist()
     case.check(Q[some], [seqs[i] for i in some], q_ids[:, some], O[some], LSE[some])
     case.c.status()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("lens", [[700, 3], [3000]])
+def test_the_most_heads(dtype, lens):
+    import paper_2109_04312_b200 as m
+    case = Case(m, lens, 1024, 1, 8, 16, [(h // 5) % 3 for h in range(1024)], dtype, seed=7, rows=9, cols=5)
+    run(m, case)
+    case.c.status()
+    more = m.Cache(case.c.k, case.c.v, case.c.row_ids, case.c.col_ids, case.c.table, case.c.lens, case.c.prefix, case.c.refs, [0] * 1025)
+    i = torch.zeros(1, dtype=torch.int32, device="cuda")
+    with pytest.raises(m.MateError, match="unsupported"):
+        m.mate_attn_decode(more, torch.zeros(1, 1025, 8, device="cuda").to(DT[dtype]), i, i)
