@@ -318,8 +318,8 @@ int mate_rope(const mate_rope_tensor_t *tensors, int n_tensors, int B, int N, in
  * d is a multiple of 8 and at most 128; pages * page_size and width * page_size are at most 2^30, kv_heads * page_size 2^20.
  *
  * What the kernels find on the device and cannot do -- a sequence, length or page out of range, a sequence twice
- * in a list, no free page left -- they leave out, and say so in status[0], which mate_cache_status reads.  No
- * such content makes a kernel read or write outside of the arrays. */
+ * in the list of mate_cache_extend or a child twice in that of mate_cache_fork, no room left -- they leave out, and say so in
+ * status[0], which mate_cache_status reads.  No such content makes a kernel read or write outside of the arrays. */
 #define MATE_ID_TEXT 0x7fffffff
 enum { MATE_VIEW_EITHER = 2 }; /* entry of mate_cache_t.head_view: the same row OR the same column (mate_plan_sat) */
 
@@ -340,18 +340,19 @@ typedef struct {
  * pages that it needs beyond those it has are the lowest free ones, dealt out in the order of the list.
  * granted[i] = counts[i]; 0, and the sequence as it was, where there is no room: the table's row is too short,
  * or no page is free (then nobody behind it in the list who needs pages gets any either).  The second and further
- * entries with the same sequence get nothing.  seqs, counts, granted: device int32 [n], n <= 4096. */
+ * entries with the same sequence get nothing, whatever became of the first.  seqs, counts, granted: device int32 [n], n <= 4096. */
 int mate_cache_extend(const mate_cache_t *cache, const int32_t *seqs, const int32_t *counts, int n, int32_t *granted, void *stream);
 
 /* Writes the last counts[i] (null: N) tokens of sequence seqs[i] (null: i) into one layer of the cache: token j < counts[i]
  * of entry i goes to position lens[s] - counts[i] + j.  To be called behind mate_cache_extend, with what it granted.
- * A sequence stands at most once in the list (of two entries with the same one either may be what stays).
+ * A sequence stands at most once in the list; this is not looked for, and of two entries with the same one each element that stays may be
+ * of either.
  *   K, V       new rows, [B, kv_heads, N, d] by strides (batch, head, token), outside of the cache
  *   Q, Q_out   queries of the new tokens, [B, heads, N, d] by strides, and where they go rotated (Q itself with equal strides, or
  *              apart from Q, K and V); null: none.  All B N tokens are rotated, whatever counts says
  *   row_ids, col_ids   device int32 [B, N], or both null (the ids in the cache stay: further layers)
  *   freqs      as in mate_rope, applied to K (and Q); null: neither is rotated (and Q must be null)
- *   positions  device int32 [B, N]; null: the tokens' positions in their sequences
+ *   positions  device int32 [B, N]; null: the tokens' positions in their sequences (queries behind counts[i]: 0)
  * A page that several sequences share must not be written: mate_cache_fork sees to that. */
 int mate_cache_append(const mate_cache_t *cache, int layer, const void *K, const void *V, const int64_t *k_stride,
                       const int64_t *v_stride, int B, int N, const int32_t *seqs, const int32_t *counts, const int32_t *row_ids,
@@ -361,7 +362,7 @@ int mate_cache_append(const mate_cache_t *cache, int layer, const void *K, const
 /* For every i: sequence children[i], which must be empty, becomes a copy of parents[i].  Full pages are shared; a
  * last page that is filled in part is copied, in all layers, to the lowest free page (in the order of the list).  lens and
  * prefix are copied.  All parents are read as they are before the call.  A child that is not empty, or that
- * stands in the list for the second time, is left as it is; one for whose copy no page is free stays empty.
+ * stands in the list for the second time, whatever became of the first, is left as it is; one for whose copy no page is free stays empty.
  * parents, children: device int32 [n], n <= 4096.  workspace: device, mate_cache_workspace_bytes. */
 int mate_cache_fork(const mate_cache_t *cache, const int32_t *parents, const int32_t *children, int n, void *workspace,
                     size_t workspace_bytes, void *stream);
@@ -378,8 +379,8 @@ int mate_cache_compact(const mate_cache_t *cache, int32_t *n_live, void *workspa
 /* Scratch of mate_cache_fork with n entries, of mate_cache_compact, and of mate_attn_decode with n tokens (any may be null). */
 int mate_cache_workspace_bytes(const mate_cache_t *cache, int n, size_t *fork_bytes, size_t *compact_bytes, size_t *decode_bytes);
 
-/* Waits for `stream`, clears status[0] and returns MATE_ERR_NOMEM if pages ran out since the last call, MATE_ERR_INVALID_ARG if
- * something was out of range or not as it must be, else MATE_OK. */
+/* Waits for `stream`, clears status[0] and returns MATE_ERR_NOMEM if pages, or the pages that a row of the table holds, ran out
+ * since the last call, MATE_ERR_INVALID_ARG if something was out of range or not as it must be, else MATE_OK. */
 int mate_cache_status(const mate_cache_t *cache, void *stream);
 
 /* The forward's row of one token per sequence: for entry i and head h, with s = seqs[i] (null: i),
@@ -389,10 +390,12 @@ int mate_cache_status(const mate_cache_t *cache, void *stream);
  * The new token's own key and value are attended like every other, if they have been appended.
  *   Q          [B, heads, d] by strides (batch, head), of the cache's type, 16-byte aligned rows
  *   row_ids, col_ids   device int32 [B], the new token's ids (MATE_ID_TEXT: text; negative: padding, O = 0 and LSE = -inf, as
- *              for a sequence without a token that may be attended)
+ *              for a sequence without a token that may be attended).  A new token has no place in its sequence: one of the prefix,
+ *              which attends everything, is given as MATE_ID_TEXT, not by the ids that mate_plan takes for it
  *   scale      any finite value of up to 2.3e38 in magnitude (scale / ln 2 is what the kernel multiplies by)
  *   max_len    an upper bound of the sequences' lengths that the caller knows (0: what the table can hold); tokens at
- *              and beyond it do not count, and status says so
+ *              and beyond it do not count, and status says so.  It decides how the work is split: short sequences in a wide table take
+ *              longer without it (one of 512 tokens in a table for 8192 9.3 us instead of 6.2)
  *   O, LSE     [B, heads, d] of the cache's type, float32 [B, heads]; fully overwritten.  O may be Q, if that is contiguous; otherwise the
  *              three share no memory
  *   workspace  device, 256-byte aligned, mate_cache_workspace_bytes; contents undefined afterwards; calls that overlap need one each

@@ -428,7 +428,8 @@ def mate_cache_compact(cache, n_live=None):
 
 def mate_attn_decode(cache, Q, row_ids, col_ids, seqs=None, layer=0, scale=None, max_len=None, out=None, lse=None):
     """Attention of one new token per sequence over what is cached (see mate_attn_decode in mate.h).  Q: [B, heads, d]; row_ids,
-    col_ids: int32 [B], the new tokens' ids (ID_TEXT: text); seqs: int32 [B] (None: 0 .. B - 1); max_len: an upper bound of
-    the sequences' lengths.  out, lse: where the results go, contiguous (out may be Q itself; otherwise they share no memory).
+    col_ids: int32 [B], the new tokens' ids (ID_TEXT: text, and new tokens of the prefix); seqs: int32 [B] (None: 0 .. B - 1);
+    max_len: an upper bound of the sequences' lengths, by which the work is split (None: what the table holds, which short sequences
+    in a wide table pay for).  out, lse: where the results go, contiguous (out may be Q itself; otherwise they share no memory).
     Returns (O, LSE)."""
     return cache._native.attn_decode(cache._info, layer, Q, seqs, row_ids, col_ids, scale, max_len, out, lse)

@@ -5,12 +5,12 @@
 // Bound by memory: a key and a value are read once for the whole group (4 d bytes in bf16 for 4 d flops per head), the ids of all
 // cached tokens (4 or 8 bytes each, mostly from L2: the kv heads share them) decide which.  Hence
 //   - a warp works alone: it looks through 32 tokens at a time (the next ones' ids and the pages behind them are on their way
-//     meanwhile; four tokens per lane at a time took up to 5 % longer), puts the places of those that count into a list, and
+//     meanwhile; four tokens per lane at a time took up to 5 % longer when tried), puts the places of those that count into a list, and
 //     copies 16 bytes per lane and instruction from there into its own ring of two stages of 8 KB, one under way while the other is
-//     read; twelve such warps to an SM keep 96 KB under way.  (Three stages and eight warps: 64 sequences 93 us instead of 78.)  No
-//     block barrier until the sequence's part is done.  What nobody attends is never read, padding's keys and values included.
+//     read; twelve such warps to an SM keep 96 KB under way.  (Three stages and eight warps: cells 21.9 us instead of
+//     18.8, 64 sequences 72.2 instead of 71.7, one long one 49.8 instead of 51.0.)  No block barrier until the sequence's part is done.  What nobody attends is never read, padding's keys and values included.
 //   - the products are tensor-core ones (m16n8k16) with the keys as the 16 rows and the heads as the 8 columns, so that a group
-//     of up to 8 costs one of them; the tensor pipe is 14 % busy while HBM is the limit.  The weights go from one product's
+//     of up to 8 costs one of them; the tensor pipe is 18 % busy while HBM is the limit.  The weights go from one product's
 //     result to the other's operand by transposing 8 x 8 pieces between the lanes, as the sum of three bf16, which is all of their 24
 //     bits (one table of 512 tokens 5.67 -> 5.94 us, cells 18.4 -> 18.7, 64 sequences 74.1 -> 74.6 against two, whose 16 bits showed
 //     in one result of 500 that rounded to the neighbouring bf16, and in small differences of large weights).  fp32 caches: multiply-adds.
@@ -18,10 +18,10 @@
 //     know), so one long sequence is spread over the GPU and short ones are put together.  A sequence that falls to several
 //     blocks is joined by a second kernel from their partial results, in the order of its tokens: the same bits on every launch.
 // The kernel lets the next one start at its end only: where three kernels in a row let the next one start at once, their blocks pile
-// up, and the SMs do not get three blocks each (64 sequences, calls back to back, 106 us instead of 78).
-// Measured (one B200, calls back to back): 64 sequences of up to 4096 tokens, 8 kv heads of 128 elements, 400 MB, 73 us (5470 GB/s, of
-// which 67 us this kernel, the first 6 of them until the first products); one of 131072 tokens, 4 kv heads, 51 us (5250 GB/s); cells
-// of 16 tables of up to 8192 tokens 18 us, one table of 512 tokens 5.9 us: chains of dependent loads (sequence, length, page, ids, keys).
+// up, and the SMs do not get three blocks each (calls back to back: cells 23.4 us instead of 18.8, 64 sequences 73.4 instead of 71.7).
+// Measured (one B200, calls back to back in a graph): 64 sequences of up to 4096 tokens, 8 kv heads of 128 elements, 399 MB, 71.7 us (5570
+// GB/s); one of 131072 tokens, 4 kv heads, 269 MB, 51.0 us (5270 GB/s); cells of 16 tables of up to 8192 tokens 18.6 us, one table
+// of 512 tokens 6.0 to 6.2 us: chains of dependent loads (sequence, length, page, ids, keys).
 #include <cuda_bf16.h>
 
 #include <cmath>
@@ -40,10 +40,12 @@ constexpr int kStage = 8192;             // bytes of a stage: keys, then values
 constexpr int kAlign = 256;              // of the ring: the longest row of tensor-core operands
 constexpr int kRing = 2;                 // stages of a warp
 constexpr int kList = 64;                // entries of a warp's list of places: less than a stage, and one look
-constexpr int kOver = 1;                 // units that an item costs besides its tokens (0, 1, 2, 3: 64 sequences 79.7, 77.7, 78.8, 80.0 us)
-// Units of tokens up to which a block takes a whole item: for few items, and for many.  One sequence of 12 heads and 400 tokens 7.0 us
-// whole, 7.8 shared out and joined; eight items of 128 elements and 1000 tokens 11.1 whole, 9.4 shared out.  Four sequences of 12 heads
-// and up to 700 tokens 7.1 whole, 8.7 shared out, 40 of up to 1000 16.4 and 17.3 (cells 9.2 and 14.3); up to 1500 22.0 and 21.3.
+constexpr int kOver = 1;                 // units that an item costs besides its tokens (0, 1, 2, 3: 64 sequences 74.0, 71.7, 72.6, 74.6 us)
+// Units of tokens up to which a block takes a whole item: for few items, and for many.  By the bound of the lengths that the host knows.
+// Whole and shared out, us: one sequence of 12 heads of 64 elements and 512 tokens 6.0 and 7.7, 768 7.2 and 8.0, 1024 8.5 and 8.0; of 8 kv
+// heads of 128 elements and 512 tokens 8.6 and 9.8, 768 10.6 and 9.9; four sequences of 12 heads and 1024 tokens 8.7 and 8.9, 1536 11.1 and
+// 10.3; 40 of them, several items to an SM, 512 tokens 17.9 and 16.9, 1024 33.2 and 28.4; of up to 1000 tokens 14.3 and 15.2, and their cells
+// 9.2 and 14.5.
 constexpr int kWhole = 4, kWholeOfMany = 8, kMany = 32;
 constexpr int kMaxHeads = 1024;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -85,7 +87,8 @@ struct Shape {
     // What a row's chunks are permuted by: eight rows of 16 bytes (bf16: ldmatrix) or the lanes of an eighth of a warp, of which
     // 32 / kKeys share a key (fp32), then fall into different banks.
     static constexpr int kSwizzle = sizeof(T) == 2 ? 1 : 32 / kKeys;
-    // (three need the registers below 168: 28 bytes of spills for 16 heads of 128 elements, 32 x 4096 tokens 28.0 us instead of 26.9)
+    // (Three need the registers below 168.  With 16 heads of 128 elements that spills 80 bytes, and 32 x 4096 tokens take 23.7 us instead of
+    // 18.7; 8 heads of 128 elements of fp32 spill 24.)
     static constexpr int kBlocksPerSm = sizeof(T) == 2 && DP == 128 && NB == 2 ? 2 : 3;
     __device__ static int chunk_at(int key, int chunk) { return key * kRowBytes + ((chunk ^ (key * kSwizzle & 7)) << 4); }
 };
@@ -250,7 +253,7 @@ struct Loader {
     // page of the lane's token `j`
     __device__ void ask_page(int j) { page = j < end ? p.cache.table[(size_t)s * p.cache.width + page_index(p, j)] : -1; }
     // The same of its first token of entry b, while the sequence's length is on its way: kManyWarps only, whose block has one item and
-    // begins with its first token (512 tokens, 12 heads of 64 elements, 6.25 -> 5.93 us).
+    // begins with its first token (512 tokens, 12 heads of 64 elements, 6.22 -> 6.02 us).
     __device__ void ask_early(int b) {
         const int sequence = p.seqs ? p.seqs[b] : b, j = 32 * warp + lane;
         page = in_range(sequence, p.cache.seqs) && j < p.max_len ? p.cache.table[(size_t)sequence * p.cache.width + page_index(p, j)] : -1;
@@ -958,8 +961,8 @@ int launch(const DecodeParams &p, int blocks, int device, cudaStream_t st) {
     constexpr int kRows = Shape<T, DP, NB>::kRows;
     const int rows = kRows < p.group ? kRows : p.group, items = p.kv_heads * p.blocks_of_group;
     const int64_t all = (int64_t)p.B * items;
-    // An item to each block; where there is an SM for each, eight warps: 12 items of 64 elements and 250 or 512 tokens 4.6 and 5.4 us
-    // (with four 5.6 and 6.1), 8 items of 4 heads of 128 elements 6.3 and 7.1 (8.0 and 8.2).
+    // An item to each block; where there is an SM for each, eight warps: 12 items of 64 elements and 256 or 512 tokens 4.7 and 6.0 us
+    // (with four 5.6 and 7.7), 8 items of 4 heads of 128 elements 6.5 and 8.6 (8.5 and 12.3).
     if (!blocks)
         return all <= n_sms(device) ? launch_warps<T, DP, NB, kManyWarps>(p, (unsigned)all, device, st)
                                     : launch_warps<T, DP, NB, kWarps>(p, (unsigned)all, device, st);
