@@ -300,6 +300,16 @@ enum { MATE_ROPE_INTERLEAVED = 1, MATE_ROPE_BACKWARD = 2 };
 int mate_rope(const mate_rope_tensor_t *tensors, int n_tensors, int B, int N, int d, int dtype, const int32_t *positions,
               int64_t position_stride, const double *freqs, int rot, float mscale, unsigned flags, void *stream);
 
+/* The same with positions of several axes (the place in a text or cell, row and column of a table; time, height and width of a picture):
+ * pair i is turned by positions[axis axes[i]] * freqs[i].
+ *   positions  device int32, axis a of token n of example b at positions[a * axis_stride + b * position_stride + n]
+ *   axes       HOST [rot / 2], the axis of every pair, each below n_axes; sections or any other order (null where rot = 0)
+ *   n_axes     1 to 4
+ * Everything else as above: with one axis the same results bit for bit. */
+int mate_rope_axes(const mate_rope_tensor_t *tensors, int n_tensors, int B, int N, int d, int dtype, const int32_t *positions,
+                   int64_t axis_stride, int64_t position_stride, const uint8_t *axes, int n_axes, const double *freqs, int rot,
+                   float mscale, unsigned flags, void *stream);
+
 /* ------------------------------------------------------------------------------------------------
  * One new token at a time: a paged cache of keys and values, and the row of the pattern that belongs to
  * the newest token of every sequence.
@@ -359,6 +369,14 @@ int mate_cache_append(const mate_cache_t *cache, int layer, const void *K, const
                       const int32_t *col_ids, const int32_t *positions, const double *freqs, int rot, float mscale, unsigned flags,
                       const void *Q, const int64_t *q_stride, void *Q_out, const int64_t *q_out_stride, void *stream);
 
+/* The same with positions of several axes (see mate_rope_axes): positions is device int32 [n_axes, B, N], and neither it nor freqs may be
+ * null. */
+int mate_cache_append_axes(const mate_cache_t *cache, int layer, const void *K, const void *V, const int64_t *k_stride,
+                           const int64_t *v_stride, int B, int N, const int32_t *seqs, const int32_t *counts, const int32_t *row_ids,
+                           const int32_t *col_ids, const int32_t *positions, const uint8_t *axes, int n_axes, const double *freqs,
+                           int rot, float mscale, unsigned flags, const void *Q, const int64_t *q_stride, void *Q_out,
+                           const int64_t *q_out_stride, void *stream);
+
 /* For every i: sequence children[i], which must be empty, becomes a copy of parents[i].  Full pages are shared; a
  * last page that is filled in part is copied, in all layers, to the lowest free page (in the order of the list).  lens and
  * prefix are copied.  All parents are read as they are before the call.  A child that is not empty, or that
@@ -375,6 +393,16 @@ int mate_cache_free(const mate_cache_t *cache, const int32_t *seqs, int n, void 
  * in use at n_live and above go, in order, to the free ones below; all layers, ids, refs and the table follow.
  * n_live: device int32 [1].  workspace: device, mate_cache_workspace_bytes. */
 int mate_cache_compact(const mate_cache_t *cache, int32_t *n_live, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Which entries of a list of sequences (null: 0 .. n - 1) share their first pages, as mate_cache_fork makes them: entry i belongs to the
+ * group of entry i - 1 if both have at least m full pages and the first m of them are the same, m = max(1, min_len / page_size rounded
+ * up).  (Sequences that share pages but do not follow one another in the list make groups of their own.)  For every entry:
+ *   groups[i]          the first entry of its group
+ *   groups[n + i]      the group's entries, which follow one another
+ *   groups[2 n + i]    tokens that they all share: the largest number of leading full pages that are the same in all of them, times
+ *                      page_size; 0 for a group of one
+ * The same sequence may stand in the list twice.  seqs: device int32 [n], groups: device int32 [3, n], n <= 4096. */
+int mate_cache_groups(const mate_cache_t *cache, const int32_t *seqs, int n, int min_len, int32_t *groups, void *stream);
 
 /* Scratch of mate_cache_fork with n entries, of mate_cache_compact, and of mate_attn_decode with n tokens (any may be null). */
 int mate_cache_workspace_bytes(const mate_cache_t *cache, int n, size_t *fork_bytes, size_t *compact_bytes, size_t *decode_bytes);
@@ -404,6 +432,23 @@ int mate_cache_status(const mate_cache_t *cache, void *stream);
 int mate_attn_decode(const mate_cache_t *cache, int layer, const void *Q, const int64_t *q_stride, int B, const int32_t *seqs,
                      const int32_t *row_ids, const int32_t *col_ids, float scale, int max_len, void *O, float *LSE, void *workspace,
                      size_t workspace_bytes, void *stream);
+
+/* mate_attn_decode for a batch whose sequences share their first tokens: the same results (but for the order of the sums), with the
+ * shared pages of a group read once for all of its sequences, whose query heads are multiplied with them together.
+ *   groups     device int32 [3, B] as mate_cache_groups gives it for the same list; any other way of telling who shares what is
+ *              taken too: for every entry the first entry of its group, the number of its entries, which follow one another, and the
+ *              tokens that they share, the same in all entries of a group, and each sequence at least as long.  An entry whose third
+ *              number is 0 or whose second is 1 is in no group.  The shared tokens are read through the first entry's row of the table, so
+ *              the others' must be the same there; each entry has a prefix and ids of its own
+ *   workspace  device, 256-byte aligned, mate_cache_shared_workspace_bytes; contents undefined afterwards; calls that overlap need one each
+ * Groups that do not fit together, or of more tokens than a sequence (or max_len) has, are left out: their entries are taken
+ * alone, or attend their own tokens only, and status says so.  All other arguments, limits and errors as for mate_attn_decode. */
+int mate_attn_decode_shared(const mate_cache_t *cache, int layer, const void *Q, const int64_t *q_stride, int B, const int32_t *seqs,
+                            const int32_t *row_ids, const int32_t *col_ids, const int32_t *groups, float scale, int max_len, void *O,
+                            float *LSE, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Scratch of mate_attn_decode_shared with n tokens. */
+int mate_cache_shared_workspace_bytes(const mate_cache_t *cache, int n, size_t *bytes);
 
 #ifdef __cplusplus
 }

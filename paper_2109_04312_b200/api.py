@@ -84,7 +84,8 @@ def _load():
     _native.bind(*(C.cast(f, C.c_void_p).value for f in (lib.mate_attn_workspace_bytes, lib.mate_attn_fwd,
                                                          lib.mate_attn_bwd, lib.mate_cell_mean)), MateError)
     entries = (lib.mate_rope, lib.mate_cache_extend, lib.mate_cache_append, lib.mate_cache_fork, lib.mate_cache_free,
-               lib.mate_cache_compact, lib.mate_cache_workspace_bytes, lib.mate_cache_status, lib.mate_attn_decode)
+               lib.mate_cache_compact, lib.mate_cache_workspace_bytes, lib.mate_cache_status, lib.mate_attn_decode, lib.mate_rope_axes,
+               lib.mate_cache_append_axes, lib.mate_cache_groups, lib.mate_attn_decode_shared, lib.mate_cache_shared_workspace_bytes)
     _native.bind_cache(*(C.cast(f, C.c_void_p).value for f in entries))
     _cache_calls = _native
     _lib = lib
@@ -363,6 +364,28 @@ def mate_rope(Q, positions, freqs, K=None, interleaved=False, mscale=1.0, backwa
     return _cache_calls.rope(Q, K, positions, freqs, interleaved, mscale, backward, q, k)
 
 
+def _axes(axes):
+    """One byte for every pair."""
+    if isinstance(axes, bytes):
+        return axes
+    try:
+        return bytes(axes if isinstance(axes, (list, tuple)) else np.asarray(axes).tolist())
+    except (TypeError, ValueError) as e:
+        raise ValueError("axes must be whole numbers, one for each frequency") from e
+
+
+def mate_rope_axes(Q, positions, freqs, axes, K=None, interleaved=False, mscale=1.0, backward=False, out=None):
+    """Rotary positions of several axes (see mate_rope_axes in mate.h), such as place in the cell, row and column of a table.
+    positions: int32 [axes, B, N], or [axes, N] for all examples, up to four axes; axes: the axis of every frequency, a sequence of whole
+    numbers (or bytes, which are taken as they are).  The rest as for mate_rope."""
+    if _lib is None:
+        _load()
+    if K is not None and out is not None and not (isinstance(out, (tuple, list)) and len(out) == 2):
+        raise ValueError("out must be a pair of tensors where Q and K are given")
+    q, k = (out, None) if K is None else out or (None, None)
+    return _cache_calls.rope_axes(Q, K, positions, freqs, interleaved, mscale, backward, q, k, _axes(axes))
+
+
 class Cache:
     """A paged cache of keys and values (see mate_cache_t in mate.h): the caller's tensors, which the calls read and write.
 
@@ -410,6 +433,14 @@ def mate_cache_append(cache, K, V, seqs=None, counts=None, row_ids=None, col_ids
                                       out)
 
 
+def mate_cache_append_axes(cache, K, V, freqs, positions, axes, seqs=None, counts=None, row_ids=None, col_ids=None, layer=0,
+                           interleaved=False, mscale=1.0, Q=None, out=None):
+    """mate_cache_append with rotary positions of several axes (see mate_cache_append_axes in mate.h).  positions: int32 [axes, B, N];
+    axes: as for mate_rope_axes."""
+    return cache._native.cache_append_axes(cache._info, layer, K, V, seqs, counts, row_ids, col_ids, positions, freqs, interleaved, mscale, Q,
+                                           out, _axes(axes))
+
+
 def mate_cache_fork(cache, parents, children):
     """children[i], which must be empty, becomes a copy of parents[i]: full pages are shared, a last one that is filled in part is
     copied in all layers (see mate_cache_fork in mate.h).  int32 CUDA tensors [n]."""
@@ -426,6 +457,13 @@ def mate_cache_compact(cache, n_live=None):
     return cache._native.cache_compact(cache._info, n_live)
 
 
+def mate_cache_groups(cache, seqs=None, min_len=1, out=None):
+    """Which entries of a list of sequences (None: all) that follow one another share their first pages, at least min_len tokens of them
+    (see mate_cache_groups in mate.h).  seqs: int32 CUDA tensor [n].  Returns int32 [3, n]: of every entry its group's first entry, the
+    group's size, and the tokens that its sequences share (0 for a group of one).  out: where it goes, contiguous, apart from seqs."""
+    return cache._native.cache_groups(cache._info, seqs, min_len, out)
+
+
 def mate_attn_decode(cache, Q, row_ids, col_ids, seqs=None, layer=0, scale=None, max_len=None, out=None, lse=None):
     """Attention of one new token per sequence over what is cached (see mate_attn_decode in mate.h).  Q: [B, heads, d]; row_ids,
     col_ids: int32 [B], the new tokens' ids (ID_TEXT: text, and new tokens of the prefix); seqs: int32 [B] (None: 0 .. B - 1);
@@ -433,3 +471,11 @@ def mate_attn_decode(cache, Q, row_ids, col_ids, seqs=None, layer=0, scale=None,
     in a wide table pay for).  out, lse: where the results go, contiguous (out may be Q itself; otherwise they share no memory).
     Returns (O, LSE)."""
     return cache._native.attn_decode(cache._info, layer, Q, seqs, row_ids, col_ids, scale, max_len, out, lse)
+
+
+def mate_attn_decode_shared(cache, Q, row_ids, col_ids, groups, seqs=None, layer=0, scale=None, max_len=None, out=None, lse=None):
+    """mate_attn_decode for sequences that share their first tokens, such as beams or questions about one table: what a group shares is read
+    once for all of its sequences (see mate_attn_decode_shared in mate.h).  groups: int32 [3, B], what mate_cache_groups returns for the same
+    seqs: call it when the batch or the pages of its sequences have changed, once for all layers.  The rest as for mate_attn_decode.
+    Returns (O, LSE)."""
+    return cache._native.attn_decode_shared(cache._info, layer, Q, seqs, row_ids, col_ids, scale, max_len, out, lse, groups)

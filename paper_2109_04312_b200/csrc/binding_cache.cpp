@@ -5,7 +5,9 @@
 #include "overlap.h"
 
 #include <algorithm>
+#include <cstring>
 #include <memory>
+#include <type_traits>
 #include <vector>
 
 namespace mate_binding {
@@ -21,6 +23,11 @@ struct Library {
     decltype(&mate_cache_workspace_bytes) workspace_bytes = nullptr;
     decltype(&mate_cache_status) status = nullptr;
     decltype(&mate_attn_decode) decode = nullptr;
+    decltype(&mate_rope_axes) rope_axes = nullptr;
+    decltype(&mate_cache_append_axes) append_axes = nullptr;
+    decltype(&mate_cache_groups) groups = nullptr;
+    decltype(&mate_attn_decode_shared) decode_shared = nullptr;
+    decltype(&mate_cache_shared_workspace_bytes) shared_workspace_bytes = nullptr;
 } lib;
 
 // A cache as the calls take it; lives in a capsule of the Python object.  It holds the tensors' memory itself: an attribute of that object may be
@@ -183,10 +190,23 @@ int frequencies(PyObject *o, int64_t d, const c10::Device &device, const double 
     return (int)(2 * f.size(0));
 }
 
+// Positions of several axes, [A, ...], and the axis of every pair, as bytes.
+struct Axes {
+    const uint8_t *of_pair;
+    int n;
+    Axes(PyObject *axes, PyObject *positions, int rot) {
+        if (!THPVariable_Check(positions) || THPVariable_Unpack(positions).dim() < 1) fail_shape("positions", "an int32 CUDA tensor, one row for each axis");
+        n = as_int(THPVariable_Unpack(positions).size(0), "positions");
+        if (!PyBytes_Check(axes) || PyBytes_GET_SIZE(axes) != rot / 2) fail_shape("axes", "one number for each frequency");
+        of_pair = reinterpret_cast<const uint8_t *>(PyBytes_AS_STRING(axes));
+    }
+};
+
 // rope(Q, K or None, positions, freqs, interleaved, mscale, backward, out or None, out_k or None) -> Q' or (Q', K')
-PyObject *rope(PyObject *, PyObject *const *a, Py_ssize_t n) {
+// rope_axes(the same, axes)
+PyObject *rope_of(PyObject *const *a, Py_ssize_t n, bool several) {
     return guarded([&]() -> PyObject * {
-        if (n != 9) fail(PyExc_TypeError, "rope takes 9 arguments");
+        if (n != 9 + several) fail(PyExc_TypeError, several ? "rope_axes takes 10 arguments" : "rope takes 9 arguments");
         Turned t[2];
         t[0] = turned(a[0], a[7], "Q", "out", nullptr);
         const bool two = a[1] != Py_None;
@@ -203,9 +223,11 @@ PyObject *rope(PyObject *, PyObject *const *a, Py_ssize_t n) {
         const int64_t d = Q.size(-1), N = Q.size(-2), B = Q.dim() == 4 ? Q.size(0) : 1;
         const double *f = nullptr;
         const int rot = frequencies(a[3], d, device, &f);
-        const bool one_row = THPVariable_Check(a[2]) && THPVariable_Unpack(a[2]).dim() == 1;
-        const int64_t both[2] = {B, N};
-        const int32_t *pos = ints(a[2], "positions", one_row ? c10::IntArrayRef(both + 1, 1) : c10::IntArrayRef(both, 2), device, false);
+        const std::optional<Axes> axes = several ? std::optional<Axes>(Axes(a[9], a[2], rot)) : std::nullopt;
+        const bool one_row = THPVariable_Check(a[2]) && THPVariable_Unpack(a[2]).dim() == 1 + several;
+        const int64_t all[3] = {several ? axes->n : 1, B, N}, row[2] = {all[0], N};
+        const int32_t *pos = ints(a[2], "positions", one_row ? c10::IntArrayRef(row + !several, 1 + several) : c10::IntArrayRef(all + !several, 2 + several),
+                                  device, false);
         const unsigned flags = (truth(a[4]) ? MATE_ROPE_INTERLEAVED : 0) | (truth(a[6]) ? MATE_ROPE_BACKWARD : 0);
         const float mscale = (float)number(a[5]);
         const int b = as_int(B, "Q"), nn = as_int(N, "Q"), dd = as_int(d, "Q");
@@ -219,9 +241,12 @@ PyObject *rope(PyObject *, PyObject *const *a, Py_ssize_t n) {
             int m = 0;
             for (int i = 0; i < 1 + two; ++i)
                 if (t[i].x.numel()) ts[m++] = t[i].t;
-            if (m) status = lib.rope(ts, m, b, nn, dd, dt, pos, one_row ? 0 : N, f, rot, mscale, flags, on.stream.stream());
+            if (m && !several) status = lib.rope(ts, m, b, nn, dd, dt, pos, one_row ? 0 : N, f, rot, mscale, flags, on.stream.stream());
+            if (m && several)
+                status = lib.rope_axes(ts, m, b, nn, dd, dt, pos, one_row ? N : B * N, one_row ? 0 : N, axes->of_pair, axes->n, f, rot, mscale, flags,
+                                       on.stream.stream());
         }
-        check(status, "mate_rope");
+        check(status, several ? "mate_rope_axes" : "mate_rope");
         PyObject *q = given_or(a[7], t[0].y);
         if (!two || !q) return q;
         PyObject *k = given_or(a[8], t[1].y), *r = k ? PyTuple_Pack(2, q, k) : nullptr;
@@ -230,6 +255,9 @@ PyObject *rope(PyObject *, PyObject *const *a, Py_ssize_t n) {
         return r;
     });
 }
+
+PyObject *rope(PyObject *, PyObject *const *a, Py_ssize_t n) { return rope_of(a, n, false); }
+PyObject *rope_axes(PyObject *, PyObject *const *a, Py_ssize_t n) { return rope_of(a, n, true); }
 
 // cache_info(k, v, row_ids, col_ids, table, lens, prefix, refs, status, head_view bytes) -> capsule
 PyObject *new_cache(PyObject *, PyObject *const *a, Py_ssize_t n) {
@@ -306,9 +334,10 @@ PyObject *cache_extend(PyObject *, PyObject *const *a, Py_ssize_t n) {
 }
 
 // cache_append(info, layer, K, V, seqs, counts, row_ids, col_ids, positions, freqs, interleaved, mscale, Q, out) -> rotated Q or None
-PyObject *cache_append(PyObject *, PyObject *const *a, Py_ssize_t n) {
+// cache_append_axes(the same, axes)
+PyObject *append_of(PyObject *const *a, Py_ssize_t n, bool several) {
     return guarded([&]() -> PyObject * {
-        if (n != 14) fail(PyExc_TypeError, "cache_append takes 14 arguments");
+        if (n != 14 + several) fail(PyExc_TypeError, several ? "cache_append_axes takes 15 arguments" : "cache_append takes 14 arguments");
         const CacheInfo &ci = cache_info(a[0]);
         const int layer = as_int(whole(a[1]), "layer");
         const at::Tensor &K = on_gpu(a[2], "K", &ci.device), &V = on_gpu(a[3], "V", &ci.device);
@@ -322,9 +351,11 @@ PyObject *cache_append(PyObject *, PyObject *const *a, Py_ssize_t n) {
         const int64_t B = K.size(0), N = K.size(2);
         const int32_t *seqs = ints(a[4], "seqs", {B}, ci.device, true), *counts = ints(a[5], "counts", {B}, ci.device, true);
         const int32_t *row = ints(a[6], "row_ids", {B, N}, ci.device, true), *col = ints(a[7], "col_ids", {B, N}, ci.device, true);
-        const int32_t *pos = ints(a[8], "positions", {B, N}, ci.device, true);
         const double *f = nullptr;
-        const int rot = a[9] == Py_None ? 0 : frequencies(a[9], ci.c.d, ci.device, &f);
+        const int rot = a[9] == Py_None && !several ? 0 : frequencies(a[9], ci.c.d, ci.device, &f);
+        const std::optional<Axes> axes = several ? std::optional<Axes>(Axes(a[14], a[8], rot)) : std::nullopt;
+        const int64_t all[3] = {several ? axes->n : 1, B, N};
+        const int32_t *pos = ints(a[8], "positions", c10::IntArrayRef(all + !several, 2 + several), ci.device, !several);
         const unsigned flags = truth(a[10]) ? MATE_ROPE_INTERLEAVED : 0;
         const float mscale = (float)number(a[11]);
         const bool with_q = a[12] != Py_None;
@@ -344,15 +375,23 @@ PyObject *cache_append(PyObject *, PyObject *const *a, Py_ssize_t n) {
         {
             const NoGil no_gil;
             if (with_q) set_out(q);
-            if (b > 0 && nn > 0)
+            const void *qx = with_q ? q.t.x : nullptr;
+            void *qy = with_q ? q.t.y : nullptr;
+            if (b > 0 && nn > 0 && !several)
                 status = lib.append(&ci.c, layer, K.data_ptr(), V.data_ptr(), ks, vs, b, nn, seqs, counts, row, col, pos, f, rot, mscale, flags,
-                                    with_q ? q.t.x : nullptr, q.t.x_stride, with_q ? q.t.y : nullptr, q.t.y_stride, on.stream.stream());
+                                    qx, q.t.x_stride, qy, q.t.y_stride, on.stream.stream());
+            if (b > 0 && nn > 0 && several)
+                status = lib.append_axes(&ci.c, layer, K.data_ptr(), V.data_ptr(), ks, vs, b, nn, seqs, counts, row, col, pos, axes->of_pair, axes->n, f,
+                                         rot, mscale, flags, qx, q.t.x_stride, qy, q.t.y_stride, on.stream.stream());
         }
-        check(status, "mate_cache_append");
+        check(status, several ? "mate_cache_append_axes" : "mate_cache_append");
         if (!with_q) Py_RETURN_NONE;
         return given_or(a[13], q.y);
     });
 }
+
+PyObject *cache_append(PyObject *, PyObject *const *a, Py_ssize_t n) { return append_of(a, n, false); }
+PyObject *cache_append_axes(PyObject *, PyObject *const *a, Py_ssize_t n) { return append_of(a, n, true); }
 
 // Workspace of one call.
 struct Scratch {
@@ -427,6 +466,28 @@ PyObject *cache_compact(PyObject *, PyObject *const *a, Py_ssize_t n) {
     });
 }
 
+// cache_groups(info, seqs or None, min_len, out or None) -> groups
+PyObject *cache_groups(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject * {
+        if (n != 4) fail(PyExc_TypeError, "cache_groups takes 4 arguments");
+        const CacheInfo &ci = cache_info(a[0]);
+        const int m = a[1] == Py_None ? ci.c.seqs : entries(a[1], a[1], "seqs"), min_len = as_int(whole(a[2]), "min_len");
+        const int32_t *seqs = ints(a[1], "seqs", {m}, ci.device, true);
+        int32_t *groups = ints(a[3], "out", {3, m}, ci.device, true);
+        if (groups && seqs && overlap(THPVariable_Unpack(a[3]), THPVariable_Unpack(a[1]))) fail_shape("out", "without memory in common with seqs");
+        at::Tensor out;
+        const OnDevice on(ci.device);
+        int status;
+        {
+            const NoGil no_gil;
+            if (!groups) out = empty({3, m}, at::kInt, ci.device), groups = out.data_ptr<int32_t>();
+            status = lib.groups(&ci.c, seqs, m, min_len, groups, on.stream.stream());
+        }
+        check(status, "mate_cache_groups");
+        return given_or(a[3], out);
+    });
+}
+
 // cache_status(info)
 PyObject *cache_status(PyObject *, PyObject *o) {
     return guarded([&]() -> PyObject * {
@@ -443,9 +504,10 @@ PyObject *cache_status(PyObject *, PyObject *o) {
 }
 
 // attn_decode(info, layer, Q, seqs, row_ids, col_ids, scale, max_len, out, lse) -> (O, LSE)
-PyObject *attn_decode(PyObject *, PyObject *const *a, Py_ssize_t n) {
+// attn_decode_shared(the same, groups)
+PyObject *decode_of(PyObject *const *a, Py_ssize_t n, bool shared) {
     return guarded([&]() -> PyObject * {
-        if (n != 10) fail(PyExc_TypeError, "attn_decode takes 10 arguments");
+        if (n != 10 + shared) fail(PyExc_TypeError, shared ? "attn_decode_shared takes 11 arguments" : "attn_decode takes 10 arguments");
         const CacheInfo &ci = cache_info(a[0]);
         const int layer = as_int(whole(a[1]), "layer");
         const at::Tensor &Q = on_gpu(a[2], "Q", &ci.device);
@@ -455,6 +517,7 @@ PyObject *attn_decode(PyObject *, PyObject *const *a, Py_ssize_t n) {
         const int64_t B = Q.size(0);
         const int32_t *seqs = ints(a[3], "seqs", {B}, ci.device, true);
         const int32_t *row = ints(a[4], "row_ids", {B}, ci.device, false), *col = ints(a[5], "col_ids", {B}, ci.device, false);
+        const int32_t *groups = shared ? ints(a[10], "groups", {3, B}, ci.device, false) : nullptr;
         const float scale = scale_of(a[6], ci.c.d);
         const int max_len = a[7] == Py_None ? 0 : as_int(whole(a[7]), "max_len");
         if (a[7] != Py_None && max_len == 0) fail_shape("max_len", "positive");
@@ -474,17 +537,20 @@ PyObject *attn_decode(PyObject *, PyObject *const *a, Py_ssize_t n) {
         const int b = as_int(B, "Q");
         const OnDevice on(ci.device);
         size_t need = 0;
-        check(lib.workspace_bytes(&ci.c, b, nullptr, nullptr, &need), "mate_attn_decode");
+        const char *name = shared ? "mate_attn_decode_shared" : "mate_attn_decode";
+        check(shared ? lib.shared_workspace_bytes(&ci.c, b, &need) : lib.workspace_bytes(&ci.c, b, nullptr, nullptr, &need), name);
         int status;
         {
             const NoGil no_gil;
             if (!O.defined()) O = empty(Q.sizes(), ci.type, ci.device);
             if (!LSE.defined()) LSE = empty(Q.sizes().slice(0, 2), at::kFloat, ci.device);
             const Scratch ws(b ? need : 0, ci.device);
-            status = lib.decode(&ci.c, layer, Q.data_ptr(), qs, b, seqs, row, col, scale, max_len, O.data_ptr(), LSE.data_ptr<float>(), ws.ptr,
-                                ws.bytes, on.stream.stream());
+            status = shared ? lib.decode_shared(&ci.c, layer, Q.data_ptr(), qs, b, seqs, row, col, groups, scale, max_len, O.data_ptr(),
+                                                LSE.data_ptr<float>(), ws.ptr, ws.bytes, on.stream.stream())
+                            : lib.decode(&ci.c, layer, Q.data_ptr(), qs, b, seqs, row, col, scale, max_len, O.data_ptr(), LSE.data_ptr<float>(),
+                                         ws.ptr, ws.bytes, on.stream.stream());
         }
-        check(status, "mate_attn_decode");
+        check(status, name);
         PyObject *po = given_or(a[8], O), *pl = given_or(a[9], LSE), *r = po && pl ? PyTuple_Pack(2, po, pl) : nullptr;
         Py_XDECREF(po);
         Py_XDECREF(pl);
@@ -492,20 +558,22 @@ PyObject *attn_decode(PyObject *, PyObject *const *a, Py_ssize_t n) {
     });
 }
 
+PyObject *attn_decode(PyObject *, PyObject *const *a, Py_ssize_t n) { return decode_of(a, n, false); }
+PyObject *attn_decode_shared(PyObject *, PyObject *const *a, Py_ssize_t n) { return decode_of(a, n, true); }
+
 // bind_cache(addresses of the library's entry points, in the order of Library)
-PyObject *bind_cache(PyObject *, PyObject *args) {
-    unsigned long long p[9];
-    if (!PyArg_ParseTuple(args, "KKKKKKKKK", p, p + 1, p + 2, p + 3, p + 4, p + 5, p + 6, p + 7, p + 8)) return nullptr;
-    lib.rope = reinterpret_cast<decltype(lib.rope)>(p[0]);
-    lib.extend = reinterpret_cast<decltype(lib.extend)>(p[1]);
-    lib.append = reinterpret_cast<decltype(lib.append)>(p[2]);
-    lib.fork = reinterpret_cast<decltype(lib.fork)>(p[3]);
-    lib.free = reinterpret_cast<decltype(lib.free)>(p[4]);
-    lib.compact = reinterpret_cast<decltype(lib.compact)>(p[5]);
-    lib.workspace_bytes = reinterpret_cast<decltype(lib.workspace_bytes)>(p[6]);
-    lib.status = reinterpret_cast<decltype(lib.status)>(p[7]);
-    lib.decode = reinterpret_cast<decltype(lib.decode)>(p[8]);
-    Py_RETURN_NONE;
+PyObject *bind_cache(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject * {
+        void *p[sizeof(Library) / sizeof(void *)];
+        if (n != (Py_ssize_t)(sizeof p / sizeof *p)) fail(PyExc_TypeError, "bind_cache takes an address for each entry point");
+        for (Py_ssize_t i = 0; i < n; ++i) {
+            p[i] = PyLong_AsVoidPtr(a[i]);
+            if (PyErr_Occurred()) throw Raised();
+        }
+        static_assert(sizeof(Library) == sizeof p && std::is_trivially_copyable_v<Library>, "addresses and nothing else");
+        std::memcpy(&lib, p, sizeof p);
+        Py_RETURN_NONE;
+    });
 }
 
 }  // namespace
@@ -517,9 +585,13 @@ PyMethodDef cache_methods[] = {{"rope", reinterpret_cast<PyCFunction>(reinterpre
                                {"cache_fork", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(cache_fork)), METH_FASTCALL, nullptr},
                                {"cache_free", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(cache_free)), METH_FASTCALL, nullptr},
                                {"cache_compact", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(cache_compact)), METH_FASTCALL, nullptr},
+                               {"cache_groups", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(cache_groups)), METH_FASTCALL, nullptr},
                                {"cache_status", cache_status, METH_O, nullptr},
                                {"attn_decode", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(attn_decode)), METH_FASTCALL, nullptr},
-                               {"bind_cache", bind_cache, METH_VARARGS, nullptr},
+                               {"attn_decode_shared", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(attn_decode_shared)), METH_FASTCALL, nullptr},
+                               {"rope_axes", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(rope_axes)), METH_FASTCALL, nullptr},
+                               {"cache_append_axes", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(cache_append_axes)), METH_FASTCALL, nullptr},
+                               {"bind_cache", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(bind_cache)), METH_FASTCALL, nullptr},
                                {nullptr, nullptr, 0, nullptr}};
 
 }  // namespace mate_binding

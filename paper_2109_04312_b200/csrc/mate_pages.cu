@@ -1,5 +1,5 @@
 // Pages of a cache: room for new tokens (mate_cache_extend), sequences that share their pages (mate_cache_fork), pages
-// given back (mate_cache_free) and moved together (mate_cache_compact).
+// given back (mate_cache_free) and moved together (mate_cache_compact); who shares how many with whom (mate_cache_groups).
 //
 // What is decided -- who gets which page -- is whole numbers and the same on every launch: one block reads the
 // reference counts, each warp a run of consecutive pages, and a scan over the block ranks the free ones; the r-th
@@ -443,6 +443,87 @@ __global__ void __launch_bounds__(kCopyThreads, kCopyBlocks) compact_copy_kernel
     if (bad) atomicOr(c.status, kCacheBad);
 }
 
+// Sequence of entry i, and its full pages; none where there is no such sequence.
+__device__ __forceinline__ int full_pages(const CacheArgs &c, const int32_t *seqs, int i, int *s, bool *bad) {
+    *s = seq_of(seqs, i, c.seqs);
+    if (*s < 0) *bad = true;
+    return *s < 0 ? 0 : clip_len(c.lens[*s], c.width * c.page_size, bad) / c.page_size;
+}
+// Leading full pages that every entry has in common with the one before it.  A block each, kRun pairs of a thread under way: latency,
+// as long as a row fits one round of them (2048 pages).
+constexpr int kCommonThreads = 128, kRun = 16;
+__global__ void __launch_bounds__(kCommonThreads) common_kernel(const __grid_constant__ CacheArgs c, const int32_t *seqs, int32_t *common) {
+    __shared__ int s_first;
+    ptx::launch_dependents();
+    ptx::wait_prior_grid();
+    const int i = blockIdx.x, tid = threadIdx.x;
+    int s, t = -1;
+    bool bad = false, unused = false;
+    const int mine = full_pages(c, seqs, i, &s, &bad), n = i > 0 ? min(mine, full_pages(c, seqs, i - 1, &t, &unused)) : 0;
+    if (bad && tid == 0) atomicOr(c.status, kCacheBad);
+    if (tid == 0) s_first = n;  // the first page that they have not in common
+    __syncthreads();
+    const int32_t *a = c.table + (size_t)max(s, 0) * c.width, *b = c.table + (size_t)max(t, 0) * c.width;
+    for (int p0 = 0; p0 < n; p0 += kCommonThreads * kRun) {
+        int x[kRun], y[kRun];
+#pragma unroll
+        for (int j = 0; j < kRun; ++j) {
+            const int p = p0 + j * kCommonThreads + tid;
+            x[j] = p < n ? a[p] : 0, y[j] = p < n ? b[p] : 0;
+        }
+        int first = n;
+#pragma unroll
+        for (int j = kRun - 1; j >= 0; --j) {
+            const int p = p0 + j * kCommonThreads + tid;
+            if (p < n && (x[j] != y[j] || !in_range(x[j], c.pages))) first = p;
+        }
+        if (first < n) atomicMin(&s_first, first);
+        __syncthreads();
+        if (s_first < p0 + kCommonThreads * kRun) break;
+        __syncthreads();
+    }
+    if (tid == 0) common[i] = s_first;
+}
+// An entry begins a group where it has fewer than `least` pages in common with the one before it.  One block; groups[2 n + i] holds what
+// common_kernel found.
+__global__ void __launch_bounds__(kThreads, 1) groups_kernel(int page_size, int n, int least, int32_t *groups) {
+    __shared__ int s_count[kMost], s_shared[kMost], s_warp[kThreads / 32];
+    ptx::launch_dependents();
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, i0 = tid * kPer;
+    for (int i = tid; i < n; i += kThreads) s_count[i] = 0, s_shared[i] = INT32_MAX;
+    ptx::wait_prior_grid();
+    int common[kPer], first[kPer], last = 0;  // last: beginning of the group that the thread's last entry belongs to, as far as it knows
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+        common[j] = i0 + j < n ? groups[2 * n + i0 + j] : INT32_MAX;
+        if (common[j] < least) last = i0 + j;
+    }
+    int top = last;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) top = max(top, __shfl_up_sync(~0u, top, o));  // (lanes below o get their own)
+    if (lane == 31) s_warp[warp] = top;
+    const int before = __shfl_up_sync(~0u, top, 1);
+    __syncthreads();
+    int at = lane > 0 ? before : 0;
+    for (int w = 0; w < warp; ++w) at = max(at, s_warp[w]);
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+        if (i0 + j >= n) break;
+        if (common[j] < least) at = i0 + j;
+        first[j] = at;
+        atomicAdd(&s_count[at], 1);
+        if (at < i0 + j) atomicMin(&s_shared[at], common[j]);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+        if (i0 + j >= n) break;
+        groups[i0 + j] = first[j];
+        groups[n + i0 + j] = s_count[first[j]];
+        groups[2 * n + i0 + j] = s_count[first[j]] > 1 ? s_shared[first[j]] * page_size : 0;
+    }
+}
+
 PageShape page_shape(const mate_cache_t *c) {
     const int64_t size = (int64_t)elem_size(c->dtype);
     const unsigned per_row = (unsigned)(c->d * size / 16), units = (unsigned)(c->kv_heads * c->page_size) * per_row;
@@ -525,6 +606,18 @@ int mate_cache_compact(const mate_cache_t *cache, int32_t *n_live, void *workspa
     cudaError_t e = launch_after(compact_kernel, dim3(1), kThreads, 0, (cudaStream_t)stream, c, m, n_live);
     if (e == cudaSuccess)
         e = launch_after(compact_copy_kernel, dim3((unsigned)(n_sms(cache->device) * kCopyBlocks)), kCopyThreads, 0, (cudaStream_t)stream, c, page_shape(cache), m);
+    return as_status(e);
+}
+
+int mate_cache_groups(const mate_cache_t *cache, const int32_t *seqs, int n, int min_len, int32_t *groups, void *stream) {
+    int rc = check_cache(cache);
+    if (rc == MATE_OK) rc = check_list(cache, seqs, n, true);
+    if (rc == MATE_OK && (min_len < 0 || (n > 0 && !groups))) rc = MATE_ERR_INVALID_ARG;
+    if (rc == MATE_OK) rc = check_cache_device(cache);
+    if (rc != MATE_OK || n == 0) return rc;
+    const int least = min_len > cache->page_size ? pages_of(min_len, cache->page_size) : 1;
+    cudaError_t e = launch_after(common_kernel, dim3((unsigned)n), kCommonThreads, 0, (cudaStream_t)stream, cache_args(cache, 0), seqs, groups + 2 * (size_t)n);
+    if (e == cudaSuccess) e = launch_after(groups_kernel, dim3(1), kThreads, 0, (cudaStream_t)stream, cache->page_size, n, least, groups);
     return as_status(e);
 }
 

@@ -1,5 +1,6 @@
-// Rotary positions (mate_rope) and new tokens into the pages of a cache (mate_cache_append): one kernel, which turns
-// rows of up to three tensors (queries, keys; values are only copied) and writes them by strides or through a page table.
+// Rotary positions of one axis or several (mate_rope, mate_rope_axes) and new tokens into the pages of a cache (mate_cache_append,
+// mate_cache_append_axes): one kernel, which turns rows of up to three tensors (queries, keys; values are only copied) and writes them by
+// strides or through a page table.
 //
 // A pair (a, b) becomes m (a cos t - b sin t, a sin t + b cos t), t = position * freqs[pair]; the transpose has -t.  The
 // angle's whole turns do not matter, so a frequency is kept as a 64-bit fraction of a turn per position and multiplied by the
@@ -31,6 +32,7 @@ struct Side {
     int first_slice;  // slices of heads are numbered through over the sides
 };
 struct RopeParams {
+    static constexpr bool kAxes = false;
     Side side[3];
     int n_sides;
     int B, N, d, rot, interleaved;
@@ -44,6 +46,14 @@ struct RopeParams {
     int paged;
     CacheArgs cache;
     const int32_t *seqs, *counts, *row_ids, *col_ids;
+};
+// Positions of several axes, of which every pair goes by one.  (Parameters of their own: those of one axis are copied with every launch.)
+constexpr int kMaxAxes = 4, kMaxPairs = 512;
+struct AxesParams : RopeParams {
+    static constexpr bool kAxes = true;
+    int n_axes;
+    int64_t axis_stride;
+    uint32_t axis[kMaxPairs / 16];  // two bits a pair; the pairs of a unit lie in one word
 };
 
 // VEC elements, as they lie in memory and as numbers
@@ -89,8 +99,8 @@ __device__ __forceinline__ Place place(const RopeParams &p, int chunk, bool turn
     return {at, at + VEC, at + VEC < p.d};
 }
 
-template <typename T, int VEC>
-__global__ void __launch_bounds__(kThreads, 6) rope_kernel(const __grid_constant__ RopeParams p) {
+template <typename T, int VEC, typename P>
+__global__ void __launch_bounds__(kThreads, 6) rope_kernel(const __grid_constant__ P p) {
     extern __shared__ uint64_t s_turn[];  // [rot / 2] turns per position, in 2^-64
     ptx::launch_dependents();
     ptx::wait_prior_grid();
@@ -130,6 +140,14 @@ __global__ void __launch_bounds__(kThreads, 6) rope_kernel(const __grid_constant
 
     // the token's position and, in a cache, its slot (the loads above are under way)
     int position = p.positions && exists ? p.positions[b * p.position_stride + n] : 0;
+    [[maybe_unused]] int others[kMaxAxes - 1];  // its positions of the other axes
+    [[maybe_unused]] uint32_t axes = 0;         // of the unit's pairs
+    if constexpr (P::kAxes) {
+#pragma unroll
+        for (int a = 1; a < kMaxAxes; ++a)
+            others[a - 1] = p.positions && exists && a < p.n_axes ? p.positions[a * p.axis_stride + b * p.position_stride + n] : 0;
+        if (s.turned && chunk < p.turned_chunks) axes = p.axis[chunk * VEC / 16] >> 2 * (chunk * VEC % 16);
+    }
     int64_t page_at = 0;
     if (p.paged && exists && n < count) {
         bool bad = false;
@@ -167,7 +185,12 @@ __global__ void __launch_bounds__(kThreads, 6) rope_kernel(const __grid_constant
     if (turned) {
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
-            const int64_t turn = (int64_t)(s_turn[chunk * VEC + e] * (uint64_t)(int64_t)position);
+            int at_axis = position;
+            if constexpr (P::kAxes) {
+                const uint32_t a = axes >> 2 * e & 3;
+                at_axis = a & 2 ? (a & 1 ? others[2] : others[1]) : (a & 1 ? others[0] : position);
+            }
+            const int64_t turn = (int64_t)(s_turn[chunk * VEC + e] * (uint64_t)(int64_t)at_axis);
             const int32_t half_turns = (int32_t)(turn >> 32);  // in 2^-31
             const float rounded = (float)half_turns;
             sincospif(rounded * 4.656612873077393e-10f, &sn[e], &cs[e]);  // 2^-31
@@ -216,8 +239,8 @@ __global__ void __launch_bounds__(kThreads, 6) rope_kernel(const __grid_constant
     }
 }
 
-template <typename T, int VEC>
-int launch(RopeParams &p, int device, cudaStream_t st) {
+template <typename T, int VEC, typename P>
+int launch(P &p, int device, cudaStream_t st) {
     p.turned_chunks = p.rot / 2 / VEC;
     p.n_chunks = VEC == 1 ? (p.d + 1) / 2 : p.d / (2 * VEC);
     if ((int64_t)p.B * p.N > (int64_t)INT32_MAX * kThreads / p.n_chunks) return MATE_ERR_UNSUPPORTED;
@@ -236,14 +259,15 @@ int launch(RopeParams &p, int device, cudaStream_t st) {
         p.side[i].first_slice = (int)slices;
         slices += (p.side[i].heads + p.heads_of_thread - 1) / p.heads_of_thread;
     }
-    return launch_after(rope_kernel<T, VEC>, dim3((unsigned)blocks, (unsigned)slices), kThreads, sizeof(uint64_t) * (p.rot / 2), st, p) == cudaSuccess
+    return launch_after(rope_kernel<T, VEC, P>, dim3((unsigned)blocks, (unsigned)slices), kThreads, sizeof(uint64_t) * (p.rot / 2), st, p) == cudaSuccess
                ? MATE_OK
                : MATE_ERR_CUDA;
 }
 
 // Runs of 16 bytes, or of 8, where the pairs, the rest of the row, every address and every stride allow it, else one element at
 // a time.  (4 x 4096 tokens, 12 and 12 heads of 80 elements, 40 of them turned: runs of 8 bytes 23.6 us, single elements 46.0.)
-int run(RopeParams &p, int dtype, cudaStream_t st) {
+template <typename P>
+int run(P &p, int dtype, cudaStream_t st) {
     if (p.B == 0 || p.N == 0 || p.n_sides == 0) return MATE_OK;
     int device = 0;
     if (cudaGetDevice(&device) != cudaSuccess) return MATE_ERR_CUDA;
@@ -278,16 +302,26 @@ bool set_angles(RopeParams &p, const int32_t *positions, int64_t stride, const d
     return true;
 }
 
-}  // namespace
-}  // namespace mate
+bool set_axes(RopeParams &, const uint8_t *, int, int64_t, int) { return true; }
+bool set_axes(AxesParams &p, const uint8_t *axes, int n_axes, int64_t stride, int rot) {
+    if (n_axes < 1 || (rot > 0 && !axes)) return false;
+    p.n_axes = n_axes;
+    p.axis_stride = stride;
+    for (int i = 0; i < rot / 2; ++i) {
+        if (axes[i] >= n_axes) return false;
+        p.axis[i / 16] |= (uint32_t)axes[i] << 2 * (i % 16);
+    }
+    return true;
+}
 
-extern "C" int mate_rope(const mate_rope_tensor_t *tensors, int n_tensors, int B, int N, int d, int dtype, const int32_t *positions,
-                         int64_t position_stride, const double *freqs, int rot, float mscale, unsigned flags, void *stream) {
-    using namespace mate;
+template <typename P>
+int turn(const mate_rope_tensor_t *tensors, int n_tensors, int B, int N, int d, int dtype, const int32_t *positions, int64_t position_stride,
+         const uint8_t *axes, int n_axes, int64_t axis_stride, const double *freqs, int rot, float mscale, unsigned flags, void *stream) {
     if (!tensors || n_tensors < 1 || n_tensors > 2 || B < 0 || N < 0 || d < 1 || rot < 0 || rot > d || rot % 2 != 0) return MATE_ERR_INVALID_ARG;
-    if ((dtype != MATE_BF16 && dtype != MATE_F32) || d > 1024) return MATE_ERR_UNSUPPORTED;
-    RopeParams p = {};
+    if ((dtype != MATE_BF16 && dtype != MATE_F32) || d > 2 * kMaxPairs || n_axes > kMaxAxes) return MATE_ERR_UNSUPPORTED;
+    P p = {};
     if (!set_angles(p, positions, position_stride, freqs, rot, mscale, flags)) return MATE_ERR_INVALID_ARG;
+    if (!set_axes(p, axes, n_axes, axis_stride, rot)) return MATE_ERR_INVALID_ARG;
     if (rot > 0 && (!freqs || !positions)) return MATE_ERR_INVALID_ARG;
     p.B = B, p.N = N, p.d = d;
     for (int i = 0; i < n_tensors; ++i) {
@@ -302,12 +336,11 @@ extern "C" int mate_rope(const mate_rope_tensor_t *tensors, int n_tensors, int B
     return run(p, dtype, (cudaStream_t)stream);
 }
 
-extern "C" int mate_cache_append(const mate_cache_t *cache, int layer, const void *K, const void *V, const int64_t *k_stride,
-                                 const int64_t *v_stride, int B, int N, const int32_t *seqs, const int32_t *counts,
-                                 const int32_t *row_ids, const int32_t *col_ids, const int32_t *positions, const double *freqs, int rot,
-                                 float mscale, unsigned flags, const void *Q, const int64_t *q_stride, void *Q_out,
-                                 const int64_t *q_out_stride, void *stream) {
-    using namespace mate;
+template <typename P>
+int append(const mate_cache_t *cache, int layer, const void *K, const void *V, const int64_t *k_stride, const int64_t *v_stride, int B, int N,
+           const int32_t *seqs, const int32_t *counts, const int32_t *row_ids, const int32_t *col_ids, const int32_t *positions,
+           const uint8_t *axes, int n_axes, const double *freqs, int rot, float mscale, unsigned flags, const void *Q, const int64_t *q_stride,
+           void *Q_out, const int64_t *q_out_stride, void *stream) {
     int rc = check_cache(cache);
     if (rc != MATE_OK) return rc;
     if (layer < 0 || layer >= cache->layers || !K || !V || !k_stride || !v_stride || B < 0 || N < 0 || (!row_ids) != (!col_ids))
@@ -315,8 +348,10 @@ extern "C" int mate_cache_append(const mate_cache_t *cache, int layer, const voi
     if (!seqs && B > cache->seqs) return MATE_ERR_INVALID_ARG;
     if (freqs ? rot < 0 || rot > cache->d || rot % 2 != 0 : rot != 0) return MATE_ERR_INVALID_ARG;
     if (Q ? !freqs || !Q_out || !q_stride || !q_out_stride : Q_out != nullptr) return MATE_ERR_INVALID_ARG;
-    RopeParams p = {};
+    if (n_axes > kMaxAxes) return MATE_ERR_UNSUPPORTED;
+    P p = {};
     if (!set_angles(p, positions, N, freqs, rot, mscale, flags)) return MATE_ERR_INVALID_ARG;
+    if (!set_axes(p, axes, n_axes, (int64_t)B * N, rot) || (P::kAxes && rot > 0 && !positions)) return MATE_ERR_INVALID_ARG;
     const size_t size = elem_size(cache->dtype);
     for (const void *t : {K, V, Q, (const void *)Q_out})
         if (!is_aligned(t, size)) return MATE_ERR_ALIGNMENT;
@@ -335,3 +370,42 @@ extern "C" int mate_cache_append(const mate_cache_t *cache, int layer, const voi
     p.seqs = seqs, p.counts = counts, p.row_ids = row_ids, p.col_ids = col_ids;
     return run(p, cache->dtype, (cudaStream_t)stream);
 }
+
+}  // namespace
+}  // namespace mate
+
+using namespace mate;
+
+extern "C" {
+
+int mate_rope(const mate_rope_tensor_t *tensors, int n_tensors, int B, int N, int d, int dtype, const int32_t *positions,
+              int64_t position_stride, const double *freqs, int rot, float mscale, unsigned flags, void *stream) {
+    return turn<RopeParams>(tensors, n_tensors, B, N, d, dtype, positions, position_stride, nullptr, 1, 0, freqs, rot, mscale, flags, stream);
+}
+
+int mate_rope_axes(const mate_rope_tensor_t *tensors, int n_tensors, int B, int N, int d, int dtype, const int32_t *positions,
+                   int64_t axis_stride, int64_t position_stride, const uint8_t *axes, int n_axes, const double *freqs, int rot, float mscale,
+                   unsigned flags, void *stream) {
+    return turn<AxesParams>(tensors, n_tensors, B, N, d, dtype, positions, position_stride, axes, n_axes, axis_stride, freqs, rot, mscale, flags,
+                            stream);
+}
+
+int mate_cache_append(const mate_cache_t *cache, int layer, const void *K, const void *V, const int64_t *k_stride, const int64_t *v_stride,
+                      int B, int N, const int32_t *seqs, const int32_t *counts, const int32_t *row_ids, const int32_t *col_ids,
+                      const int32_t *positions, const double *freqs, int rot, float mscale, unsigned flags, const void *Q,
+                      const int64_t *q_stride, void *Q_out, const int64_t *q_out_stride, void *stream) {
+    return append<RopeParams>(cache, layer, K, V, k_stride, v_stride, B, N, seqs, counts, row_ids, col_ids, positions, nullptr, 1, freqs, rot,
+                              mscale, flags, Q, q_stride, Q_out, q_out_stride, stream);
+}
+
+int mate_cache_append_axes(const mate_cache_t *cache, int layer, const void *K, const void *V, const int64_t *k_stride,
+                           const int64_t *v_stride, int B, int N, const int32_t *seqs, const int32_t *counts, const int32_t *row_ids,
+                           const int32_t *col_ids, const int32_t *positions, const uint8_t *axes, int n_axes, const double *freqs, int rot,
+                           float mscale, unsigned flags, const void *Q, const int64_t *q_stride, void *Q_out, const int64_t *q_out_stride,
+                           void *stream) {
+    if (!freqs || !positions) return MATE_ERR_INVALID_ARG;
+    return append<AxesParams>(cache, layer, K, V, k_stride, v_stride, B, N, seqs, counts, row_ids, col_ids, positions, axes, n_axes, freqs, rot,
+                              mscale, flags, Q, q_stride, Q_out, q_out_stride, stream);
+}
+
+}  // extern "C"
