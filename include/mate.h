@@ -407,7 +407,8 @@ int mate_cache_groups(const mate_cache_t *cache, const int32_t *seqs, int n, int
 /* Scratch of mate_cache_fork with n entries, of mate_cache_compact, and of mate_attn_decode with n tokens (any may be null). */
 int mate_cache_workspace_bytes(const mate_cache_t *cache, int n, size_t *fork_bytes, size_t *compact_bytes, size_t *decode_bytes);
 
-/* Waits for `stream`, clears status[0] and returns MATE_ERR_NOMEM if pages, or the pages that a row of the table holds, ran out
+/* Waits for `stream`, clears status[0] and returns MATE_ERR_TIMEOUT if a kernel gave up on a bounded wait since the last call (the outputs
+ * of its call are then undefined), MATE_ERR_NOMEM if pages, or the pages that a row of the table holds, ran out
  * since the last call, MATE_ERR_INVALID_ARG if something was out of range or not as it must be, else MATE_OK. */
 int mate_cache_status(const mate_cache_t *cache, void *stream);
 

@@ -4,7 +4,7 @@
 
 namespace mate {
 
-enum { kCacheBad = 1, kCacheFull = 2 };  // bits of mate_cache_t.status
+enum { kCacheBad = 1, kCacheFull = 2, kCacheTimeout = 4 };  // bits of mate_cache_t.status
 
 inline size_t elem_size(int dtype) { return dtype == MATE_F32 ? 4 : 2; }
 inline bool is_aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }

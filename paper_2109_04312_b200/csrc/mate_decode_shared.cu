@@ -269,7 +269,7 @@ struct Rows {
     int2 want[RT];
 };
 // Keys, with what the rows go by.
-struct Key {
+struct alignas(16) Key {
     unsigned at;  // in 16 bytes from the cache's beginning
     int place, row, col;
 };
@@ -358,7 +358,7 @@ __device__ __forceinline__ void put(float x, float *y) { *y = x; }
 __device__ __forceinline__ void put(float x, __nv_bfloat16 *y) { *y = __float2bfloat16_rn(x); }
 __device__ __forceinline__ float natural(float m, float sum) { return sum == 0.f ? -INFINITY : (m + log2f(sum)) * kLn2; }
 
-// ---- the kernel without tensor cores: tiles of 64 rows and 32 keys
+// ---- the kernel for fp32, without tensor cores: tiles of 64 rows and 32 keys
 
 constexpr int kSimtRows = 64, kSimtKeys = 32, kSimtThreads = 256;
 
@@ -371,23 +371,13 @@ struct SimtSmem {
     int counts[4], n, last, plain;
 };
 
-template <typename T>
-__device__ __forceinline__ void load16(const T *from, float *to) {
-    const uint4 x = *reinterpret_cast<const uint4 *>(from);
-    if constexpr (sizeof(T) == 4) {
-        *reinterpret_cast<uint4 *>(to) = x;
-    } else {
-        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) to[2 * i] = __uint_as_float(w[i] << 16), to[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-    }
-}
+__device__ __forceinline__ void load16(const float *from, float *to) { *reinterpret_cast<float4 *>(to) = *reinterpret_cast<const float4 *>(from); }
 
-template <typename T, int DP>
+template <int DP>
 __global__ void __launch_bounds__(kSimtThreads) shared_simt_kernel(const __grid_constant__ SharedParams p) {
     extern __shared__ __align__(16) char smem_raw[];
     auto &sm = *reinterpret_cast<SimtSmem<DP> *>(smem_raw);
-    constexpr int kVec = 16 / sizeof(T), kCols = DP / 32, kR = kSimtRows / (kSimtThreads / 32);
+    constexpr int kVec = 4, kCols = DP / 32, kR = kSimtRows / (kSimtThreads / 32);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, r0 = warp * kR;
     ptx::wait_prior_grid();
     const Start start = find_start<kSimtRows, kSimtThreads>(p);
@@ -407,7 +397,7 @@ __global__ void __launch_bounds__(kSimtThreads) shared_simt_kernel(const __grid_
             const int r = i / (p.d / kVec), c = (i - r * (p.d / kVec)) * kVec;
             if (r >= part.n_rows) continue;
             const int at = part.tile * kSimtRows + r, member = part.seg == 0 ? at / p.group : 0;
-            load16((const T *)p.Q + (part.b + member) * p.q_batch + (part.kv * p.group + at - member * p.group) * p.q_head + c, &sm.q[r][c]);
+            load16((const float *)p.Q + (part.b + member) * p.q_batch + (part.kv * p.group + at - member * p.group) * p.q_head + c, &sm.q[r][c]);
         }
         float o[kR][kCols], m[kR], l[kR];
 #pragma unroll
@@ -435,8 +425,8 @@ __global__ void __launch_bounds__(kSimtThreads) shared_simt_kernel(const __grid_
             for (int i = tid; i < kSimtKeys * (p.d / kVec); i += kSimtThreads) {
                 const int k = i / (p.d / kVec), c = (i - k * (p.d / kVec)) * kVec;
                 if (k < n) {
-                    load16((const T *)p.cache.k + (size_t)sm.keys[k].at * kVec + c, &sm.k[k][c]);
-                    load16((const T *)p.cache.v + (size_t)sm.keys[k].at * kVec + c, &sm.v[k][c]);
+                    load16((const float *)p.cache.k + (size_t)sm.keys[k].at * kVec + c, &sm.k[k][c]);
+                    load16((const float *)p.cache.v + (size_t)sm.keys[k].at * kVec + c, &sm.v[k][c]);
                     for (int e = 0; e < kVec; ++e) odd |= !(fabsf(sm.v[k][c + e]) < INFINITY);
                 } else {
                     for (int e = 0; e < kVec; ++e) sm.k[k][c + e] = sm.v[k][c + e] = 0.f;
@@ -533,7 +523,7 @@ __global__ void __launch_bounds__(kSimtThreads) shared_simt_kernel(const __grid_
                 else if (part.grouped)
                     p.whole[whole * p.d + e] = x;
                 else
-                    put(sum == 0.f ? 0.f : x / sum, (T *)p.O + out * p.d + e);
+                    put(sum == 0.f ? 0.f : x / sum, (float *)p.O + out * p.d + e);
             }
             if (lane > 0) continue;
             if (state != kAll)
@@ -552,6 +542,574 @@ __global__ void __launch_bounds__(kSimtThreads) shared_simt_kernel(const __grid_
         }
     }
     if (look.bad) atomicOr(p.cache.status, kCacheBad);
+}
+
+// ---- the tensor-core kernel (bf16): tiles of 128 rows and 128 keys, one block to an SM
+
+constexpr int kTcRows = 128, kTcKeys = 128;
+constexpr int kSoftmaxWarps = 8;              // two threads to a row: 64 keys each
+constexpr int kLoadWarp0 = kSoftmaxWarps, kLoadWarps = 4;
+constexpr int kMmaWarp = kLoadWarp0 + kLoadWarps;
+constexpr int kTcThreads = 32 * (kMmaWarp + 1);
+constexpr int kMetas = 4;                     // tiles whose keys are known
+constexpr float kRescale = 8.f;               // log2 units that a score may exceed its row's base by
+// tensor memory: O (fp32), S of two tiles (fp32), P (pairs of bf16, the weights' upper and lower halves)
+constexpr uint32_t kTmemCols = 512, kTmemO = 0, kTmemS = 128, kTmemHi = 384, kTmemLo = 448;
+
+template <int DP>
+struct TcShape {
+    static constexpr int kTile = kTcKeys * DP * 2;              // bytes; column halves of 64 elements, 128 bytes a row and swizzled
+    static constexpr int kHalf = kTcKeys * 128;
+    static constexpr int kStages = DP == 64 ? 4 : 2;            // tiles of keys, and of values
+};
+struct alignas(16) Meta {
+    int n, first, last, q;  // keys; of the part; buffer of its Q.  n < 0: the share is done
+    uint32_t plain;         // 0x01010101: every row attends every key
+    alignas(16) int place[kTcKeys], row[kTcKeys], col[kTcKeys];
+};
+template <int DP>
+struct TcSmem {  // from a multiple of 1024 bytes on
+    uint8_t q[2][TcShape<DP>::kTile];
+    uint8_t k[TcShape<DP>::kStages][TcShape<DP>::kTile], v[TcShape<DP>::kStages][TcShape<DP>::kTile];
+    Meta meta[kMetas];
+    Rows<kTcRows> rows[2];
+    Part part[2];
+    Key list[kList];
+    float other[2][kTcRows];  // what the two threads of a row tell one another
+    int counts[4];
+    uint64_t q_full[2], q_empty[2], k_full[4], k_empty[4], v_full[4], v_empty[4], meta_full[kMetas], meta_empty[kMetas], s_full[2], s_free[2], p_full,
+        pv_done, final_;
+    uint32_t tmem;
+    int abort;
+};
+
+__device__ __forceinline__ void cp_async16_or_zero(uint32_t dst, const void *src, bool there) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+// All `threads` of a barrier: whether one of them says so.
+template <int kId, int kThreads>
+__device__ __forceinline__ bool any_of(bool x) {
+    uint32_t r;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\t"
+        "barrier.cta.red.or.pred q, %2, %3, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+        : "=r"(r)
+        : "r"((uint32_t)x), "n"(kId), "n"(kThreads)
+        : "memory");
+    return r != 0;
+}
+
+// 32 scores of a row, scaled; those that do not count become -inf.
+__device__ __forceinline__ void scale_scores(uint32_t (&v)[32], uint64_t scale2) {
+#pragma unroll
+    for (int e = 0; e < 32; e += 2) {
+        float x, y;
+        ptx::unpack_f32x2(ptx::mul_f32x2(ptx::pack_f32x2(v[e], v[e + 1]), scale2), x, y);
+        v[e] = __float_as_uint(x), v[e + 1] = __float_as_uint(y);
+    }
+}
+__device__ __forceinline__ void mask_scores(uint32_t (&v)[32], const Meta &meta, int c0, int want_row, int want_col, int below) {
+#pragma unroll
+    for (int e = 0; e < 32; e += 4) {
+        const int4 place = *reinterpret_cast<const int4 *>(meta.place + c0 + e), row = *reinterpret_cast<const int4 *>(meta.row + c0 + e),
+                   col = *reinterpret_cast<const int4 *>(meta.col + c0 + e);
+        if (!attends(want_row, want_col, below, place.x, row.x, col.x)) v[e] = 0xff800000u;
+        if (!attends(want_row, want_col, below, place.y, row.y, col.y)) v[e + 1] = 0xff800000u;
+        if (!attends(want_row, want_col, below, place.z, row.z, col.z)) v[e + 2] = 0xff800000u;
+        if (!attends(want_row, want_col, below, place.w, row.w, col.w)) v[e + 3] = 0xff800000u;
+    }
+}
+__device__ __forceinline__ void cut_scores(uint32_t (&v)[32], int n) {  // columns from n on
+#pragma unroll
+    for (int e = 0; e < 32; ++e)
+        if (e >= n) v[e] = 0xff800000u;
+}
+__device__ __forceinline__ float top_score(const uint32_t (&v)[32], float top) {
+    float t[4] = {top, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+    for (int e = 0; e < 32; e += 8)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) t[j] = ptx::fmax3(t[j], __uint_as_float(v[e + 2 * j]), __uint_as_float(v[e + 2 * j + 1]));
+    return fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
+}
+// Weights 2^(x - base) as pairs of bf16: rounded, and what the rounding left, rounded (their sum has 16 bits).  The sums take all of them.
+__device__ __forceinline__ void weigh(const uint32_t (&v)[32], uint64_t neg_base2, uint32_t (&hi)[16], uint32_t (&lo)[16], uint64_t (&sum)[2]) {
+#pragma unroll
+    for (int e = 0; e < 32; e += 2) {
+        float x, y;
+        ptx::unpack_f32x2(ptx::add_f32x2(ptx::pack_f32x2(v[e], v[e + 1]), neg_base2), x, y);
+        x = ptx::ex2(x), y = ptx::ex2(y);
+        const uint64_t xy = ptx::pack_f32x2(x, y);
+        sum[e >> 1 & 1] = ptx::add_f32x2(sum[e >> 1 & 1], xy);
+        const uint32_t h = ptx::cvt_bf16x2(x, y);
+        hi[e >> 1] = h;
+        ptx::unpack_f32x2(ptx::sub_f32x2(xy, ptx::pack_f32x2(h << 16, h & 0xffff0000u)), x, y);
+        lo[e >> 1] = ptx::cvt_bf16x2(x, y);
+    }
+}
+
+template <int DP>
+__global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_constant__ SharedParams p) {
+    using namespace ptx;
+    using S = TcShape<DP>;
+    constexpr int kStages = S::kStages, kHalves = DP / 64, kOwn = DP / 2;  // kOwn: columns of O of a thread
+    extern __shared__ uint8_t tc_smem[];
+    TcSmem<DP> &sm = *reinterpret_cast<TcSmem<DP> *>(tc_smem + (-smem_u32(tc_smem) & 1023));
+    const int tid = threadIdx.x, warp = __shfl_sync(~0u, tid >> 5, 0), lane = tid & 31;
+    const auto bar = [](const uint64_t &b) { return smem_u32(&b); };
+
+    if (tid == 0) {
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(bar(sm.q_full[i]), kLoadWarps);
+            mbar_init(bar(sm.q_empty[i]), kSoftmaxWarps + 1);
+            mbar_init(bar(sm.s_full[i]), 1);
+            mbar_init(bar(sm.s_free[i]), kSoftmaxWarps);
+        }
+        for (int i = 0; i < kStages; ++i) {
+            mbar_init(bar(sm.k_full[i]), kLoadWarps), mbar_init(bar(sm.v_full[i]), kLoadWarps);
+            mbar_init(bar(sm.k_empty[i]), 1), mbar_init(bar(sm.v_empty[i]), 1);
+        }
+        for (int i = 0; i < kMetas; ++i) mbar_init(bar(sm.meta_full[i]), kLoadWarps), mbar_init(bar(sm.meta_empty[i]), kSoftmaxWarps + 1);
+        mbar_init(bar(sm.p_full), kSoftmaxWarps), mbar_init(bar(sm.pv_done), 1), mbar_init(bar(sm.final_), 1);
+        sm.abort = 0;
+        fence_mbar_init();
+    }
+    if (warp == kMmaWarp) {
+        tmem_alloc(smem_u32(&sm.tmem), kTmemCols);
+        tmem_relinquish();
+    }
+    if (p.d < DP)  // columns that no copy writes
+        for (int i = tid; i < (2 + 2 * kStages) * S::kTile / 16; i += kTcThreads) reinterpret_cast<uint4 *>(sm.q)[i] = make_uint4(0, 0, 0, 0);
+    fence_proxy_async();
+    tc_fence_before();
+    wait_prior_grid();
+    const Start start = find_start<kTcRows, kTcThreads>(p);  // (its barriers: the set-up is seen by all)
+    tc_fence_after();
+    const uint32_t tmem = __shfl_sync(~0u, sm.tmem, 0);
+
+    // Every wait is bounded; the first one to run out raises the flag that ends all of them.  Warps that meet at a barrier leave together,
+    // when one of them says there that a wait of its own has failed.
+    volatile int *abort = &sm.abort;
+    const auto wait = [&](const uint64_t &b, uint32_t parity) -> bool {
+#pragma unroll 1
+        for (uint32_t i = 0; i < kWaitLimit; ++i) {
+            if (mbar_try_wait(smem_u32(&b), parity)) return true;
+            if (*abort) return false;
+        }
+        *abort = 1;
+        return false;
+    };
+
+    if (blockIdx.x >= start.blocks) {
+    } else if (warp < kSoftmaxWarps) {
+        // ------------------------------------------------------------------ softmax and results
+        const int half = warp >> 2, r = tid & 127;  // columns of S and of O; row, which is the lane of tensor memory
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+        const uint32_t tO = tmem + lanes + kTmemO + half * kOwn, tHi = tmem + lanes + kTmemHi + half * 32, tLo = tmem + lanes + kTmemLo + half * 32;
+        const uint64_t scale2 = pack_f32x2(p.scale_log2, p.scale_log2);
+        int c = 0, pv_seen = 0, parts = 0;  // tiles with keys; those whose P V is known to be done; parts
+        bool failed = false;
+        int want_row = 0, want_col = 0, below = 0, first_c = 0;
+        bool live = false;
+        float m = -INFINITY;
+        uint64_t sum[2] = {0, 0};
+        const auto wait_pv = [&](int done) {  // the P V of the first `done` tiles
+            if (pv_seen >= done) return;
+            pv_seen = done;
+            if (!wait(sm.pv_done, (done - 1) & 1)) failed = true;
+            tc_fence_after();
+        };
+#pragma unroll 1
+        for (int t = 0;; ++t) {
+            Meta &meta = sm.meta[t % kMetas];
+            if (!wait(sm.meta_full[t % kMetas], t / kMetas & 1)) failed = true;
+            const bool over = !failed && meta.n < 0;
+            const int n = failed || over ? 0 : meta.n, qb = meta.q & 1;
+            const Part &part = sm.part[qb];
+            if (!failed && !over && meta.first) {
+                if (!wait(sm.q_full[qb], parts / 2 & 1)) failed = true;
+                const Rows<kTcRows> &rows = sm.rows[qb];
+                want_row = rows.want_row[r], want_col = rows.want_col[r], below = rows.below[r];
+                live = (warp & 3) * 32 < part.n_rows;
+                first_c = c;
+                m = -INFINITY;
+                sum[0] = sum[1] = 0;
+                uint32_t zero[16] = {};
+#pragma unroll
+                for (int i = 0; i < kOwn / 16; ++i) tmem_st16(tO + 16 * i, zero);
+            }
+            const bool plain = meta.plain == 0x01010101u, mine = live && n > 64 * half, both = n > 64 * half + 32;
+            uint32_t x[2][32];
+            float top = -INFINITY;
+            bool odd = false;
+            if (n > 0) {
+                if (!wait(sm.s_full[c & 1], c >> 1 & 1)) failed = true;
+                tc_fence_after();
+                if (mine) {
+                    const uint32_t tS = tmem + lanes + kTmemS + (c & 1) * kTcKeys + half * 64;
+                    tmem_ld32(tS, x[0]);
+                    if (both) tmem_ld32(tS + 32, x[1]);
+                    tc_wait_ld();
+                    reg_fence(x[0]);
+                    reg_fence(x[1]);
+                }
+                tc_fence_before();
+                if (lane == 0) mbar_arrive(bar(sm.s_free[c & 1]));
+                if (mine) {
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        if (i == 1 && !both) break;
+                        const int c0 = 64 * half + 32 * i;
+                        scale_scores(x[i], scale2);
+                        if (!plain)
+                            mask_scores(x[i], meta, c0, want_row, want_col, below);
+                        else if (n < c0 + 32)
+                            cut_scores(x[i], n - c0);
+                        top = top_score(x[i], top);
+                    }
+                }
+                if (!plain) {  // a weight 0 does not undo a value that is not a number: is there one?
+                    if (!wait(sm.v_full[c % kStages], c / kStages & 1)) failed = true;
+                    __nv_bfloat162 z = __floats2bfloat162_rn(0.f, 0.f);
+                    const uint4 *v = reinterpret_cast<const uint4 *>(sm.v[c % kStages]);
+#pragma unroll 4
+                    for (int i = tid; i < kHalves * kTcKeys * 8; i += 32 * kSoftmaxWarps) {
+                        const uint4 y = (i >> 3 & (kTcKeys - 1)) < n ? v[i] : make_uint4(0, 0, 0, 0);
+                        for (uint32_t w : {y.x, y.y, y.z, y.w})
+                            z = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&w), __floats2bfloat162_rn(0.f, 0.f), z);
+                    }
+                    odd = !(__low2float(z) == 0.f && __high2float(z) == 0.f);
+                }
+            }
+            // The base of a row moves when a score exceeds it by kRescale, and with the row's first score.
+            bool odd_one = false;
+            if (any_of<2, 32 * kSoftmaxWarps>(failed || over || odd || top > m + kRescale)) {
+                if (any_of<2, 32 * kSoftmaxWarps>(failed || over)) break;
+                sm.other[half][r] = top;
+                odd_one = any_of<2, 32 * kSoftmaxWarps>(odd);
+                if (live) {
+                    top = fmaxf(top, sm.other[half ^ 1][r]);
+                    float keep = 1.f;
+                    if (top > m + kRescale) keep = ex2(m - top), m = top;
+                    if (c > first_c && __any_sync(~0u, keep != 1.f)) {
+                        wait_pv(c);
+                        const uint64_t keep2 = pack_f32x2(keep, keep);
+                        sum[0] = mul_f32x2(sum[0], keep2), sum[1] = mul_f32x2(sum[1], keep2);
+#pragma unroll 1
+                        for (int i = 0; i < kOwn / 16; ++i) {
+                            uint32_t o[16];
+                            tmem_ld16(tO + 16 * i, o);
+                            tc_wait_ld();
+                            reg_fence(o);
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * keep);
+                            tmem_st16(tO + 16 * i, o);
+                        }
+                    }
+                }
+            }
+            if (n > 0) {
+                const float neg = m == -INFINITY ? 0.f : -m;
+                const uint64_t neg2 = pack_f32x2(neg, neg);
+                if (mine) {
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        if (i == 1 && !both) break;
+                        uint32_t hi[16], lo[16];
+                        weigh(x[i], neg2, hi, lo, sum);
+                        wait_pv(c);
+                        tmem_st16(tHi + 16 * i, hi);
+                        tmem_st16(tLo + 16 * i, lo);
+                    }
+                }
+                wait_pv(c);
+                tc_wait_st();
+                if (odd_one) {
+                    // Values that are not numbers: added here to the rows that attend them, and taken out of the tile.
+                    tc_fence_before();
+                    any_of<2, 32 * kSoftmaxWarps>(false);
+                    tc_fence_after();
+                    uint8_t *v = sm.v[c % kStages];
+                    const auto at = [&](int key, int e) {
+                        return reinterpret_cast<__nv_bfloat16 *>(v + e / 64 * S::kHalf + key * 128 + ((e / 8 & 7) ^ (key & 7)) * 16 + e % 8 * 2);
+                    };
+#pragma unroll 1
+                    for (int key = 0; key < n && live; ++key) {
+                        const bool counts = attends(want_row, want_col, below, meta.place[key], meta.row[key], meta.col[key]);
+#pragma unroll 1
+                        for (int e = 0; e < kOwn; ++e) {
+                            const float y = __bfloat162float(*at(key, half * kOwn + e));
+                            if (fabsf(y) < INFINITY) continue;
+                            const uint32_t col = lanes + (key >> 1), hi = tmem_ld1(tmem + kTmemHi + col), lo = tmem_ld1(tmem + kTmemLo + col);
+                            const uint32_t cut = key & 1 ? 0xffff0000u : 0xffffu, up = key & 1 ? 0 : 16;
+                            const float w = __uint_as_float((hi & cut) << up) + __uint_as_float((lo & cut) << up);
+                            const float o = __uint_as_float(tmem_ld1(tO + e));
+                            tmem_st1(tO + e, __float_as_uint(counts ? fmaf(w, y, o) : o));
+                            tc_wait_st();
+                        }
+                    }
+                    any_of<2, 32 * kSoftmaxWarps>(false);
+                    for (int i = tid; i < n * DP; i += 32 * kSoftmaxWarps) {
+                        __nv_bfloat16 *y = at(i / DP, i % DP);
+                        if (!(fabsf(__bfloat162float(*y)) < INFINITY)) *y = __float2bfloat16_rn(0.f);
+                    }
+                    fence_proxy_async();
+                    __syncwarp();
+                }
+                tc_fence_before();
+                if (lane == 0) mbar_arrive(bar(sm.p_full));
+                ++c;
+            }
+            const bool last = meta.last;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(sm.meta_empty[t % kMetas]));
+            if (!last) continue;
+
+            // the part is done
+            float a, b, l;
+            unpack_f32x2(add_f32x2(sum[0], sum[1]), a, b);
+            l = a + b;
+            sm.other[half][r] = l;
+            wait_pv(c);
+            tc_wait_st();  // (a part without a key: the zeros)
+            any_of<2, 32 * kSoftmaxWarps>(false);
+            l += sm.other[half ^ 1][r];
+            if (below < -1) l = 0.f, m = -INFINITY;  // (a row that attends nothing, whatever the others attend)
+            const int state = part_state(part), slot = parts == 0 ? 0 : 1;
+            const int at = part.tile * kTcRows + r, member = part.seg == 0 ? at / p.group : 0;
+            const size_t out = (size_t)(part.b + member) * p.heads + part.kv * p.group + at - member * p.group;
+            const size_t whole = (size_t)part.seg * p.B * p.heads + out;
+            float *to = p.parts + (size_t)(2 * blockIdx.x + slot) * part_floats(kTcRows, p.d);
+            if (live) {
+                const bool row = r < part.n_rows;
+                const float by = state == kAll && !part.grouped ? 1.f / l : 1.f;
+#pragma unroll 1
+                for (int i = 0; i < kOwn / 16; ++i) {
+                    uint32_t o[16];
+                    tmem_ld16(tO + 16 * i, o);
+                    tc_wait_ld();
+                    reg_fence(o);
+                    if (!row) continue;
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) o[e] = l == 0.f ? 0u : __float_as_uint(__uint_as_float(o[e]) * by);
+#pragma unroll
+                    for (int e = 0; e < 16; e += 8) {
+                        const int col = half * kOwn + 16 * i + e;
+                        if (col >= p.d) break;
+                        const uint4 lo4 = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]), hi4 = make_uint4(o[e + 4], o[e + 5], o[e + 6], o[e + 7]);
+                        if (state != kAll) {
+                            reinterpret_cast<uint4 *>(to)[col / 4 * kTcRows + r] = lo4;
+                            reinterpret_cast<uint4 *>(to)[(col / 4 + 1) * kTcRows + r] = hi4;
+                        } else if (part.grouped) {
+                            reinterpret_cast<uint4 *>(p.whole + whole * p.d + col)[0] = lo4;
+                            reinterpret_cast<uint4 *>(p.whole + whole * p.d + col)[1] = hi4;
+                        } else {
+                            const auto f = [](uint32_t u) { return __uint_as_float(u); };
+                            *reinterpret_cast<uint4 *>((__nv_bfloat16 *)p.O + out * p.d + col) =
+                                make_uint4(cvt_bf16x2(f(lo4.x), f(lo4.y)), cvt_bf16x2(f(lo4.z), f(lo4.w)), cvt_bf16x2(f(hi4.x), f(hi4.y)),
+                                           cvt_bf16x2(f(hi4.z), f(hi4.w)));
+                        }
+                    }
+                }
+                if (row && half == 0) {
+                    if (state != kAll)
+                        reinterpret_cast<float2 *>(to + (size_t)p.d * kTcRows)[r] = make_float2(m, l);
+                    else if (part.grouped)
+                        p.whole_stats[whole] = make_float2(m, l);
+                    else
+                        p.LSE[out] = natural(m, l);
+                }
+            }
+            if (tid == 0 && state != kGoesOn) {
+                Joint *joint = joint_of(p, part.seg, part.kv, part.b, part.tile);
+                if (state == kAll)
+                    joint->slot = -1;
+                else
+                    *joint = joint_from(part, start, slot);
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(sm.q_empty[qb]));
+            ++parts;
+        }
+    } else if (warp < kMmaWarp) {
+        // ------------------------------------------------------------------ who is read, and the copies
+        const int lt = tid - 32 * kLoadWarp0, lw = warp - kLoadWarp0;
+        constexpr int kPer = DP / 8, kRowsOfCopy = 32 / kPer;  // lanes to a row; rows of an instruction
+        const int chunk = lane % kPer, sub = lane / kPer;
+        const bool copies = chunk < p.d / 8;
+        // where a lane's 16 bytes of row 32 lw + sub go; further rows by the row, whose low three bits permute the chunks
+        const auto place = [&](uint32_t tile, int row) { return tile + (chunk >> 3) * S::kHalf + row * 128 + (((chunk & 7) ^ (row & 7)) << 4); };
+        Walk walk = walk_from<kTcRows>(p, start);
+        Looker<kTcRows> look = {p, nullptr, sm.list, sm.counts, lt};
+        look.bad = false;
+        bool ok = true;
+        int t = 0, c = 0, parts = 0;
+        Part part;
+#pragma unroll 1
+        for (; next_part<kTcRows>(p, walk, part); ++parts) {
+            const int qb = parts & 1;
+            if (parts >= 2) ok &= wait(sm.q_empty[qb], (parts / 2 - 1) & 1);
+            if (any_of<1, 32 * kLoadWarps>(!ok)) break;
+            fill_rows(p, part, sm.rows[qb], lt);
+            if (lt == 0) sm.part[qb] = part;
+            look.begin(part, &sm.rows[qb]);
+            const uint32_t q = smem_u32(sm.q[qb]);
+#pragma unroll 1
+            for (int i = 32 * lw + sub; i < 32 * lw + 32; i += kRowsOfCopy) {
+                if (i >= part.n_rows) break;
+                const int at = part.tile * kTcRows + i, member = part.seg == 0 ? at / p.group : 0;
+                const __nv_bfloat16 *from = (const __nv_bfloat16 *)p.Q + (part.b + member) * p.q_batch + (part.kv * p.group + at - member * p.group) * p.q_head;
+                if (copies) cp_async16(place(q, i), from + chunk * 8);
+            }
+            cp_async_arrive(bar(sm.q_full[qb]));
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(sm.q_full[qb]));
+            bool last = false;
+#pragma unroll 1
+            for (bool first = true; !last; first = false, ++t) {
+                while (look.pending < kTcKeys && look.more()) look.look();
+                const int n = min(look.pending, kTcKeys);
+                last = look.pending <= kTcKeys && !look.more();
+                if (t >= kMetas) ok &= wait(sm.meta_empty[t % kMetas], (t / kMetas - 1) & 1);
+                if (any_of<1, 32 * kLoadWarps>(!ok)) break;
+                Meta &meta = sm.meta[t % kMetas];
+                Key key = {0, INT32_MAX, kNever + 1, kNever + 1};  // nobody's
+                if (lt < n) key = sm.list[(look.list_at + lt) % kList];
+                meta.place[lt] = key.place, meta.row[lt] = key.row, meta.col[lt] = key.col;
+                const bool plain = __all_sync(~0u, lt >= n || key.place < sm.rows[qb].least);
+                if (lane == 0) reinterpret_cast<uint8_t *>(&meta.plain)[lw] = plain;
+                if (lt == 0) meta.n = n, meta.first = first, meta.last = last, meta.q = qb;
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(sm.meta_full[t % kMetas]));
+                look.taken(n);
+                if (n == 0) continue;
+                const int stage = c % kStages, rows16 = (n + 15) & ~15;
+#pragma unroll 1
+                for (int kv = 0; kv < 2; ++kv) {
+                    const uint64_t &full = kv ? sm.v_full[stage] : sm.k_full[stage], &empty = kv ? sm.v_empty[stage] : sm.k_empty[stage];
+                    if (c >= kStages && ok) ok = wait(empty, (c / kStages - 1) & 1);
+                    const uint32_t tile = smem_u32(kv ? sm.v[stage] : sm.k[stage]);
+                    const char *base = (const char *)(kv ? p.cache.v : p.cache.k) + chunk * 16;
+#pragma unroll
+                    for (int i = 0; i < 32; i += kRowsOfCopy) {
+                        const int row = 32 * lw + i + sub;
+                        const unsigned from = __shfl_sync(~0u, key.at, i + sub);
+                        if (ok && copies && row < rows16) cp_async16_or_zero(place(tile, row), base + (row < n ? (size_t)from * 16 : 0), row < n);
+                    }
+                    cp_async_arrive(bar(full));
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar(full));
+                }
+                ++c;
+            }
+            if (!last) break;
+        }
+        // behind the last one
+        if (t >= kMetas) ok &= wait(sm.meta_empty[t % kMetas], (t / kMetas - 1) & 1);
+        if (lt == 0) sm.meta[t % kMetas].n = -1;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(sm.meta_full[t % kMetas]));
+        if (look.bad) atomicOr(p.cache.status, kCacheBad);
+    } else {
+        // ------------------------------------------------------------------ the products
+        // S = Q K^T of a tile as soon as its keys are there and one of the two S is free; O += P V as soon as P is.
+        const bool leader = elect_one();
+        int t = 0, parts = 0;          // tile that comes next
+        int cs = 0, cp = 0;            // tiles whose S, and whose P V, have been issued
+        int n_of[2];                   // keys of a tile by the S that it has
+        bool known = false, end = false;
+        Meta *meta = sm.meta;
+        int n = 0;
+        uint32_t idle = 0;
+        const auto is = [&](const uint64_t &b, uint32_t parity) { return mbar_test_wait(smem_u32(&b), parity); };
+#pragma unroll 1
+        while (!end || cp < cs) {
+            bool moved = false;
+            if (!end && !known && is(sm.meta_full[t % kMetas], t / kMetas & 1)) {
+                known = moved = true;
+                meta = &sm.meta[t % kMetas];
+                n = meta->n;
+                if (n < 0) end = true;
+            }
+            if (known && !end) {
+                const int qb = meta->q, stage = cs % kStages, sb = cs & 1;
+                const bool go = n == 0 || (cs - cp < 2 && is(sm.k_full[stage], cs / kStages & 1) && (!meta->first || is(sm.q_full[qb], parts / 2 & 1)) &&
+                                           (cs < 2 || is(sm.s_free[sb], (cs / 2 - 1) & 1)));
+                if (go) {
+                    if (n > 0) {
+                        fence_proxy_async();  // the copies of 16 bytes come through the generic proxy
+                        tc_fence_after();
+                        const uint32_t idesc = idesc_bf16(kTcRows, (n + 15) & ~15, 0, 0), tS = tmem + kTmemS + sb * kTcKeys;
+                        const uint32_t q = smem_desc_lo(smem_u32(sm.q[qb])), k = smem_desc_lo(smem_u32(sm.k[stage]));
+                        if (leader) {
+                            mma_ss_lean<0>(tS, q, k, idesc);
+#pragma unroll
+                            for (int i = 1; i < DP / 16; ++i) {
+                                const uint32_t off = i / 4 * (S::kHalf >> 4) + i % 4 * 2;
+                                mma_ss_lean<1>(tS, q + off, k + off, idesc);
+                            }
+                            mma_commit(bar(sm.s_full[sb]));
+                            mma_commit(bar(sm.k_empty[stage]));
+                        }
+                        n_of[sb] = n;
+                        ++cs;
+                    }
+                    if (meta->last) {
+                        if (leader) mma_commit(bar(sm.q_empty[qb]));
+                        ++parts;
+                    }
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar(sm.meta_empty[t % kMetas]));
+                    ++t;
+                    known = false;
+                    moved = true;
+                }
+            }
+            if (cp < cs && is(sm.p_full, cp & 1)) {
+                tc_fence_after();
+                fence_proxy_async();
+                const int stage = cp % kStages, steps = (((cp & 1) ? n_of[1] : n_of[0]) + 15) / 16;
+                const uint32_t idesc = idesc_bf16(kTcRows, 64, 0, 1), v = smem_desc_lo(smem_u32(sm.v[stage]));
+                moved = true;
+                if (is(sm.v_full[stage], cp / kStages & 1)) {
+                    fence_proxy_async();
+                    if (leader) {
+#pragma unroll 1
+                        for (int ks = 0; ks < steps; ++ks)
+#pragma unroll
+                            for (int h = 0; h < kHalves; ++h) {
+                                const uint32_t b = v + ks * (16 * 128 >> 4) + h * (S::kHalf >> 4);
+                                mma_ts_lean<1>(tmem + kTmemO + 64 * h, tmem + kTmemHi + 8 * ks, b, idesc);
+                                mma_ts_lean<1>(tmem + kTmemO + 64 * h, tmem + kTmemLo + 8 * ks, b, idesc);
+                            }
+                        mma_commit(bar(sm.pv_done));
+                        mma_commit(bar(sm.v_empty[stage]));
+                    }
+                    __syncwarp();
+                    ++cp;
+                } else {
+                    moved = false;
+                }
+            }
+            if (moved) {
+                idle = 0;
+            } else if (*abort) {
+                break;
+            } else if (++idle > 1u << 18) {  // (some 20 ms)
+                *abort = 1;
+            }
+        }
+        if (leader) mma_commit(bar(sm.final_));  // nothing of this block may still run on the tensor pipe when its memory is freed
+        __syncwarp();
+        mbar_wait_bounded(bar(sm.final_), 0, kWaitLimit);
+    }
+    if (*abort)  // copies may still be on their way to shared memory: they take a few microseconds
+        for (int i = 0; i < 50; ++i) __nanosleep(1000);
+    tc_fence_before();
+    __syncthreads();
+    if (tid == 0 && *abort) atomicOr(p.cache.status, kCacheTimeout);
+    if (warp == kMmaWarp) tmem_dealloc(tmem, kTmemCols);
 }
 
 // ---- the results of a row put together
@@ -638,10 +1196,9 @@ __global__ void __launch_bounds__(32 * kJoinWarps) shared_join_kernel(const __gr
 
 // ---- host
 
-constexpr int kBlocksPerSm = 2;
-int rows_of_tile(const mate_cache_t *) { return kSimtRows; }
+int rows_of_tile(const mate_cache_t *c) { return c->dtype == MATE_F32 ? kSimtRows : kTcRows; }
 int own_tiles(const mate_cache_t *c) { return (c->heads / c->kv_heads + rows_of_tile(c) - 1) / rows_of_tile(c); }
-int n_blocks(const mate_cache_t *c) { return kBlocksPerSm * n_sms(c->device); }
+int n_blocks(const mate_cache_t *c) { return (c->dtype == MATE_F32 ? 2 : 1) * n_sms(c->device); }
 
 size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 struct Workspace {
@@ -658,13 +1215,22 @@ Workspace workspace_of(const mate_cache_t *c, int B) {
 
 template <typename T, int DP>
 int launch(const SharedParams &p, int device, int blocks, cudaStream_t st) {
+    constexpr bool kTc = sizeof(T) == 2;
+    constexpr int kRows = kTc ? kTcRows : kSimtRows, kThreads = kTc ? kTcThreads : kSimtThreads;
+    constexpr int kSmem = kTc ? 1024 + (int)sizeof(TcSmem<DP>) : (int)sizeof(SimtSmem<DP>);
+    static_assert(kSmem <= 232448, "shared memory of a block");
+    void (*kernel)(SharedParams);
+    if constexpr (kTc)
+        kernel = shared_tc_kernel<DP>;
+    else
+        kernel = shared_simt_kernel<DP>;
     static SmemAttrOnce attr;
-    const int rc = attr.ensure((const void *)shared_simt_kernel<T, DP>, sizeof(SimtSmem<DP>), device);
+    const int rc = attr.ensure((const void *)kernel, kSmem, device);
     if (rc != MATE_OK) return rc;
-    cudaError_t e = launch_after(shared_simt_kernel<T, DP>, dim3((unsigned)blocks), kSimtThreads, sizeof(SimtSmem<DP>), st, p);
+    cudaError_t e = launch_after(kernel, dim3((unsigned)blocks), kThreads, kSmem, st, p);
     const int64_t joins = (int64_t)p.kv_heads * (((int64_t)p.B * p.group + kJoinRows - 1) / kJoinRows);
     if (e == cudaSuccess)
-        e = launch_after(shared_join_kernel<T, kSimtRows>, dim3((unsigned)joins, (unsigned)((p.d + 15) / 16)), 32 * kJoinWarps, 0, st, p);
+        e = launch_after(shared_join_kernel<T, kRows>, dim3((unsigned)joins, (unsigned)((p.d + 15) / 16)), 32 * kJoinWarps, 0, st, p);
     return e == cudaSuccess ? MATE_OK : MATE_ERR_CUDA;
 }
 

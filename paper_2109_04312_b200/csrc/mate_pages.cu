@@ -640,7 +640,7 @@ int mate_cache_status(const mate_cache_t *cache, void *stream) {
     if (cudaMemcpyAsync(&s, cache->status, sizeof s, cudaMemcpyDeviceToHost, st) != cudaSuccess ||
         cudaMemsetAsync(cache->status, 0, sizeof s, st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess)
         return MATE_ERR_CUDA;
-    return s & kCacheFull ? MATE_ERR_NOMEM : s ? MATE_ERR_INVALID_ARG : MATE_OK;
+    return s & kCacheTimeout ? MATE_ERR_TIMEOUT : s & kCacheFull ? MATE_ERR_NOMEM : s ? MATE_ERR_INVALID_ARG : MATE_OK;
 }
 
 }  // extern "C"
