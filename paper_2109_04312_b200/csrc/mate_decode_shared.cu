@@ -41,6 +41,7 @@ struct SharedParams {
     int own_tiles;  // tiles of rows of an entry's own segment
     const int32_t *seqs, *row_ids, *col_ids, *groups;
     float scale_log2;  // scale / ln 2: weights are powers of two
+    int flip;          // tensor-core kernel: the scale above is positive, and the queries change their sign
     void *O;
     float *LSE;
     unsigned page16, head16, slot16;  // strides in 16 bytes; no place is beyond 2^32 of them
@@ -65,21 +66,23 @@ struct Entry {
     int own0, own1;  // its own tokens
     int count;       // of its group, 0: it is in none
     int first, shared;
-    bool counts;     // the shared tokens are its own too
+    int counts;      // the shared tokens are its own too
+    int q_row, q_col, prefix;
 };
-// What does not fit together on the device leaves an entry without a group: the rows of one group are the same in all of its entries.
+// What does not fit together on the device leaves an entry without a group: the rows of one group are the same in all of its entries.  (Two
+// rounds of loads, the second one's indexes brought into range instead of looked at first.)
 __device__ __forceinline__ Entry entry_of(const SharedParams &p, int b, bool *bad) {
     const int s = p.seqs ? p.seqs[b] : b, q_row = p.row_ids[b], q_col = p.col_ids[b];
     const int first = p.groups[b], count = p.groups[p.B + b], shared = p.groups[2 * p.B + b];
-    Entry e = {in_range(s, p.cache.seqs) ? s : -1, 0, 0, 0, 0, first, 0, false};
-    if (e.s >= 0)
-        e.len = clip_len(p.cache.lens[s], p.max_len, bad);
-    else
-        *bad = true;
-    if (shared < 0) *bad = true;
+    const int at = min(max(s, 0), p.cache.seqs - 1), f = min(max(first, 0), b);
+    int len = p.cache.lens[at];
+    const int prefix = p.cache.prefix[at], first_of = p.groups[f], count_of = p.groups[p.B + f], shared_of = p.groups[2 * p.B + f];
+    Entry e = {s == at ? s : -1, 0, 0, 0, 0, first, 0, 0, q_row, q_col, max(0, prefix)};
+    if (s != at || shared < 0) *bad = true;
+    if (s == at) e.len = clip_len(len, p.max_len, bad);
     if (shared > 0 && count > 1) {
-        if (first >= 0 && first <= b && count <= p.B - first && b - first < count && shared <= p.max_len && p.groups[first] == first &&
-            p.groups[p.B + first] == count && p.groups[2 * p.B + first] == shared)
+        if (first == f && count <= p.B - first && b - first < count && shared <= p.max_len && first_of == first && count_of == count &&
+            shared_of == shared)
             e.count = count, e.shared = shared;
         else
             *bad = true;
@@ -108,10 +111,13 @@ __device__ __forceinline__ Segment segment_of(const SharedParams &p, const Entry
     // (an entry without a token and without a group has a result too)
     return {p.kv_heads * p.own_tiles, e.own1 > e.own0 ? units_of(e.own1 - e.own0) : e.count > 0 ? 0 : 1};
 }
+// (called, not put in line three times: what a block runs through once misses the instruction cache)
 template <int RT>
-__device__ __forceinline__ unsigned entry_units(const SharedParams &p, int b, bool *bad) {
-    const Entry e = entry_of(p, b, bad);
+__device__ __noinline__ unsigned entry_units(const SharedParams &p, int b) {
+    bool bad = false;
+    const Entry e = entry_of(p, b, &bad);
     const Segment x = segment_of<RT>(p, e, b, 0), y = segment_of<RT>(p, e, b, 1);
+    if (bad && blockIdx.x == 0) atomicOr(p.cache.status, kCacheBad);
     return (unsigned)x.items * x.units + (unsigned)y.items * y.units;
 }
 
@@ -127,9 +133,8 @@ __device__ Start find_start(const SharedParams &p) {
     __shared__ Start s_start;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int per = (p.B + NT - 1) / NT, b0 = min(p.B, tid * per), b1 = min(p.B, b0 + per);
-    bool bad = false;
     unsigned own = 0;
-    for (int b = b0; b < b1; ++b) own += entry_units<RT>(p, b, &bad);
+    for (int b = b0; b < b1; ++b) own += entry_units<RT>(p, b);
     unsigned sum = own;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -151,14 +156,13 @@ __device__ Start find_start(const SharedParams &p) {
         if (at >= before && at < before + own) {
             int b = b0;
             for (; b < b1 - 1; ++b) {
-                const unsigned n = entry_units<RT>(p, b, &bad);
+                const unsigned n = entry_units<RT>(p, b);
                 if (at < before + n) break;
                 before += n;
             }
             s_start = {total, before, blocks, b};
         }
     }
-    if (bad && blockIdx.x == 0) atomicOr(p.cache.status, kCacheBad);
     __syncthreads();
     return s_start;
 }
@@ -169,56 +173,11 @@ struct Part {
     int u0, u1, units;
     int t0, t1;      // its tokens
     int n_rows;
-    bool grouped;    // the entry is in a group: its rows' results have to be joined
+    int grouped;     // the entry is in a group: its rows' results have to be joined
+    int s;           // whose pages are read; -1: nobody's
 };
 enum { kAll, kBegins, kGoesOn };
 __device__ __forceinline__ int part_state(const Part &part) { return part.u0 > 0 ? kGoesOn : part.u1 == part.units ? kAll : kBegins; }
-// Walks the parts of a block's share.  (It comes to an end whatever it finds: every part takes a unit off the share.)
-struct Walk {
-    int b, seg, item, u;
-    int left;  // units of the share
-};
-template <int RT>
-__device__ bool next_part(const SharedParams &p, Walk &w, Part &part) {
-    bool bad = false;
-    for (; w.left > 0 && w.b < p.B; w.seg = 0, w.item = 0, w.u = 0, ++w.b) {
-        const Entry e = entry_of(p, w.b, &bad);
-        for (; w.seg < 2; ++w.seg, w.item = 0, w.u = 0) {
-            const Segment s = segment_of<RT>(p, e, w.b, w.seg);
-            if (s.units == 0 || w.item >= s.items) continue;
-            const int u1 = min(s.units, w.u + w.left);
-            if (u1 <= kOver && u1 < s.units) {
-                w.left = 0;
-                return false;
-            }
-            const int tiles = s.items / p.kv_heads, kv = w.item / tiles, tile = w.item - kv * tiles;
-            const int rows = (w.seg == 0 ? e.count : 1) * p.group;
-            const int begin = w.seg == 0 ? 0 : e.own0, end = w.seg == 0 ? min(e.shared, e.len) : e.own1;
-            part = {w.b, w.seg, kv, tile, w.u, u1, s.units, begin + max(0, w.u - kOver) * kUnit, min(end, begin + max(0, u1 - kOver) * kUnit),
-                    min(RT, rows - tile * RT), e.count > 0};
-            w.left -= max(1, u1 - w.u);
-            w.u = 0;
-            ++w.item;
-            return true;
-        }
-    }
-    return false;
-}
-// The first part of a block's share.
-template <int RT>
-__device__ __forceinline__ Walk walk_from(const SharedParams &p, const Start &start) {
-    const unsigned at = share(start.total, start.blocks, blockIdx.x);
-    bool bad = false;
-    const Entry e = entry_of(p, start.entry, &bad);
-    unsigned in = at - start.before;
-    Walk w = {start.entry, 0, 0, 0, (int)(share(start.total, start.blocks, blockIdx.x + 1) - at)};
-    Segment s = segment_of<RT>(p, e, w.b, 0);
-    if (in >= (unsigned)s.items * s.units) in -= (unsigned)s.items * s.units, w.seg = 1, s = segment_of<RT>(p, e, w.b, 1);
-    w.item = (int)(in / max(1, s.units));
-    w.u = (int)(in - (unsigned)w.item * s.units);
-    if (w.u <= kOver) w.left += w.u, w.u = 0;
-    return w;
-}
 __device__ __forceinline__ Joint *joint_of(const SharedParams &p, int seg, int kv, int b, int tile) {
     return p.joints + ((size_t)seg * p.kv_heads + kv) * p.B * p.own_tiles + (size_t)b * p.own_tiles + tile;
 }
@@ -230,129 +189,178 @@ __device__ __forceinline__ Joint joint_from(const Part &part, const Start &start
 
 // ---- who attends what
 
-// A row attends a key if the key's place is below `below` (text keys stand at -1, those of the prefix where they stand), or one of the ids is
-// the one it wants.
-struct RowInfo {
-    int entry, head;  // head -1: there is no such row
-    int want_row, want_col, below;
-};
-template <int RT>
-__device__ RowInfo row_info(const SharedParams &p, const Part &part, int r) {
-    RowInfo x = {part.b, -1, kNever, kNever, -2};
-    if (r >= part.n_rows) return x;
-    const int at = part.tile * RT + r, member = part.seg == 0 ? at / p.group : 0;
-    x.entry = part.b + member;
-    x.head = part.kv * p.group + at - member * p.group;
-    bool bad = false;
-    const Entry e = entry_of(p, x.entry, &bad);
-    if (part.seg == 0 ? !e.counts || e.first != part.b || e.count == 0 : e.own1 <= e.own0) return x;
-    const int q_row = p.row_ids[x.entry], q_col = p.col_ids[x.entry], view = view_at(p, x.head);
-    if (q_row == MATE_ID_TEXT || q_col == MATE_ID_TEXT) {
-        x.below = INT32_MAX;
-        return x;
-    }
-    if (view != MATE_VIEW_COL) x.want_row = q_row;
-    if (view != MATE_VIEW_ROW) x.want_col = q_col;
-    x.below = max(0, p.cache.prefix[e.s]);
-    return x;
-}
+// A row attends a key if the key's place is below `below` (text keys stand at -1, those of the prefix where they stand; -2: the row attends
+// nothing), or one of the ids is the one it wants.
 __device__ __forceinline__ bool attends(int want_row, int want_col, int below, int place, int row, int col) {
     return place < below || row == want_row || col == want_col;
 }
-
-// The rows of a tile, as those who look for keys and those who weigh them need them.
+// The rows of a tile, as those who weigh keys need them,
 template <int RT>
 struct Rows {
     int want_row[RT], want_col[RT], below[RT];
-    int least, most;     // of `below` over the rows that are there
-    int n_want;          // wishes, without repetitions of the row before
+};
+// and as those who look for keys do: without repetitions of the row before.
+template <int RT>
+struct Wishes {
+    int least, most;  // of `below` over the rows that are there
+    int n;
     int2 want[RT];
+    __device__ void clear() { least = INT32_MAX, most = INT32_MIN, n = 0; }
 };
 // Keys, with what the rows go by.
 struct alignas(16) Key {
     unsigned at;  // in 16 bytes from the cache's beginning
     int place, row, col;
 };
-constexpr int kList = 256;
+constexpr int kList = 256, kScouts = 128;
 
-// 128 threads look through the tokens of a part, 128 at a time.  Those that count go onto the list.
+// kScouts threads walk the parts of the block's share and look through their tokens, 128 at a time; the keys that count go onto a list.
+// The next ones' ids, and the pages of the ones behind them, are on their way meanwhile.  Barrier 1 is theirs.
 template <int RT>
-struct Looker {
+struct ScoutSmem {
+    Entry entries[kScouts];  // of the batch, from `base` on
+    Wishes<RT> wishes[2];    // of the parts in turn
+    Key list[kList];         // what look() writes is seen behind the next barrier
+    int counts[2][4];
+};
+template <int RT>
+struct Scout {
     const SharedParams &p;
-    const Rows<RT> *rows;
-    Key *list;       // [kList]
-    int *counts;     // [4]
-    int tid;         // of the 128
-    int s, end, next, pending, list_at;
-    unsigned head_at;
-    bool bad;
+    ScoutSmem<RT> &sm;
+    int tid;
+    // the walk: next item of the share
+    int b, seg, item, u, left;  // left: units of the share
+    int base, parts;
+    // the looks at the present part
+    int s, end, next, pending, list_at, looks;
+    unsigned head_at, at;
+    int row, col, page;
+    bool there, bad;
 
-    __device__ void sync() const { asm volatile("bar.sync 1, 128;" ::: "memory"); }
-    __device__ void begin(const Part &part, const Rows<RT> *of) {
-        rows = of;
-        s = p.seqs ? p.seqs[part.b] : part.b;
-        next = part.t0, end = part.t1;
-        if (!in_range(s, p.cache.seqs)) end = next;
-        head_at = (unsigned)part.kv * p.head16;
-        pending = list_at = 0;
+    __device__ static void sync() { asm volatile("barrier.cta.sync 1, 128;" ::: "memory"); }
+    __device__ void window(int from, int to) {  // entries from .. to (kScouts of them at most) are held
+        if (from >= base && to < base + kScouts) return;
+        sync();
+        bool unused = false;
+        sm.entries[tid] = entry_of(p, min(from + tid, p.B - 1), &unused);
+        base = from;
+        sync();
     }
-    __device__ bool more() const { return next < end; }
-    __device__ void look() {
-        const int j = next + tid;
-        Key key = {0, j, kNever, kNever};
-        bool counts_here = false;
-        if (j < end) {
-            const int i = page_index(p, j), page = p.cache.table[(size_t)s * p.cache.width + i];
-            if (in_range(page, p.cache.pages)) {
-                const int slot = j - i * p.cache.page_size, id = page * p.cache.page_size + slot;
-                key.row = p.cache.row_ids[id], key.col = p.cache.col_ids[id];
-                key.at = (unsigned)page * p.page16 + (unsigned)slot * p.slot16 + head_at;
-                if (key.row == MATE_ID_TEXT || key.col == MATE_ID_TEXT) key.place = -1;
-                counts_here = key.place < rows->most;
-                for (int w = 0; w < rows->n_want && !counts_here; ++w) counts_here = key.row == rows->want[w].x || key.col == rows->want[w].y;
-                if (key.row < 0 || key.col < 0) counts_here = false;
-            } else {
-                bad = true;
+    __device__ void start(const Start &from) {
+        const unsigned begin = share(from.total, from.blocks, blockIdx.x);
+        unsigned in = begin - from.before;
+        b = from.entry, seg = 0, parts = 0, bad = false, looks = 0;
+        left = (int)(share(from.total, from.blocks, blockIdx.x + 1) - begin);
+        base = -2 * kScouts;
+        if (tid == 0) sm.wishes[0].clear();
+        window(b, b);
+        Segment x = segment_of<RT>(p, sm.entries[0], b, 0);
+        const unsigned shared = (unsigned)x.items * x.units;
+        if (in >= shared) in -= shared, seg = 1, x = segment_of<RT>(p, sm.entries[0], b, 1);
+        item = (int)(in / max(1, x.units));
+        u = (int)(in - (unsigned)item * x.units);
+        if (u <= kOver) left += u, u = 0;
+    }
+    // The next part of the share.  (It comes to an end whatever it finds: every part takes a unit off the share.)
+    __device__ bool next_part(Part &part) {
+        for (; left > 0 && b < p.B; seg = 0, item = 0, u = 0, ++b) {
+            window(b, b);
+            const Entry &e = sm.entries[b - base];
+            for (; seg < 2; ++seg, item = 0, u = 0) {
+                const Segment x = segment_of<RT>(p, e, b, seg);
+                if (x.units == 0 || item >= x.items) continue;
+                const int u1 = min(x.units, u + left);
+                if (u1 <= kOver && u1 < x.units) {  // it ends among the units that stand for the item: the next block takes it
+                    left = 0;
+                    return false;
+                }
+                const int tiles = seg == 0 ? x.items / p.kv_heads : p.own_tiles, kv = item / tiles, tile = item - kv * tiles;
+                const int rows = (seg == 0 ? e.count : 1) * p.group, begin = seg == 0 ? 0 : e.own0, stop = seg == 0 ? min(e.shared, e.len) : e.own1;
+                part = {b, seg, kv, tile, u, u1, x.units, begin + max(0, u - kOver) * kUnit, min(stop, begin + max(0, u1 - kOver) * kUnit),
+                        min(RT, rows - tile * RT), e.count > 0, e.s};
+                left -= max(1, u1 - u);
+                u = 0;
+                ++item;
+                return true;
             }
         }
-        const unsigned those = __ballot_sync(~0u, counts_here);
-        if ((tid & 31) == 0) counts[tid >> 5] = __popc(those);
+        return false;
+    }
+    __device__ void ask_page(int j) { page = j < end ? p.cache.table[(size_t)s * p.cache.width + page_index(p, j)] : -1; }
+    __device__ void ask_ids() {  // of the thread's token of `next`, whose page has come
+        const int j = next + tid;
+        there = j < end && in_range(page, p.cache.pages);
+        if (j < end && !there) bad = true;
+        if (!there) return;
+        const int slot = j - page_index(p, j) * p.cache.page_size, id = page * p.cache.page_size + slot;
+        row = p.cache.row_ids[id], col = p.cache.col_ids[id];
+        at = (unsigned)page * p.page16 + (unsigned)slot * p.slot16 + head_at;
+    }
+    // Behind a barrier that the last look at the part before it is in front of.
+    __device__ void begin(const Part &part, Rows<RT> &rows) {
+        s = part.s, next = part.t0, end = s < 0 ? part.t0 : part.t1;
+        head_at = (unsigned)part.kv * p.head16;
+        pending = list_at = 0;
+        ask_page(next + tid);
+        const int at0 = part.tile * RT, first = part.seg == 0 ? at0 / p.group : 0;
+        window(part.b + first, part.b + (part.seg == 0 ? (at0 + part.n_rows - 1) / p.group : 0));
+        Wishes<RT> &w = sm.wishes[parts & 1];
+        ++parts;
+        if (tid == 0) sm.wishes[parts & 1].clear();
+        int want_row = kNever, want_col = kNever, below = -2;
+        if (tid < part.n_rows) {
+            const int member = part.seg == 0 ? (at0 + tid) / p.group : 0, view = view_at(p, part.kv * p.group + at0 + tid - member * p.group);
+            const Entry &e = sm.entries[part.b + member - base];
+            if (part.seg == 0 ? e.counts && e.first == part.b && e.count > 0 : e.own1 > e.own0) {
+                const bool text = e.q_row == MATE_ID_TEXT || e.q_col == MATE_ID_TEXT;
+                below = text ? INT32_MAX : e.prefix;
+                if (!text && view != MATE_VIEW_COL) want_row = e.q_row;
+                if (!text && view != MATE_VIEW_ROW) want_col = e.q_col;
+            }
+        }
+        if (tid < RT) rows.want_row[tid] = want_row, rows.want_col[tid] = want_col, rows.below[tid] = below;
+        const int least = __reduce_min_sync(~0u, below < 0 ? INT32_MAX : below), most = __reduce_max_sync(~0u, below);
+        const int row_before = __shfl_up_sync(~0u, want_row, 1), col_before = __shfl_up_sync(~0u, want_col, 1);
+        const bool again = (tid & 31) > 0 && row_before == want_row && col_before == want_col;
+        if ((tid & 31) == 0 && most >= 0) atomicMin(&w.least, least), atomicMax(&w.most, most);
+        if (!again && (want_row != kNever || want_col != kNever)) w.want[atomicAdd(&w.n, 1)] = make_int2(want_row, want_col);
+        ask_ids();
+        ask_page(next + kUnit + tid);
+        sync();
+    }
+    __device__ const Wishes<RT> &wishes() const { return sm.wishes[parts + 1 & 1]; }  // of the present part
+    __device__ bool more() const { return next < end; }
+    __device__ void look() {
+        const Wishes<RT> &w = wishes();
+        Key key = {at, next + tid, row, col};
+        bool is = there && row >= 0 && col >= 0;
+        if (is) {
+            if (row == MATE_ID_TEXT || col == MATE_ID_TEXT) key.place = -1;
+            is = key.place < w.most;
+#pragma unroll 1
+            for (int i = 0; i < w.n && !is; ++i) is = row == w.want[i].x || col == w.want[i].y;
+        }
+        next += kUnit;
+        if (next < end) {
+            ask_ids();
+            ask_page(next + kUnit + tid);
+        }
+        const unsigned those = __ballot_sync(~0u, is);
+        int *count = sm.counts[looks++ & 1];
+        if ((tid & 31) == 0) count[tid >> 5] = __popc(those);
         sync();
         int before = 0, all = 0;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            if (w < tid >> 5) before += counts[w];
-            all += counts[w];
+        for (int i = 0; i < 4; ++i) {
+            if (i < tid >> 5) before += count[i];
+            all += count[i];
         }
-        if (counts_here) list[(list_at + pending + before + __popc(those & ((1u << (tid & 31)) - 1))) % kList] = key;
+        if (is) sm.list[(list_at + pending + before + __popc(those & ((1u << (tid & 31)) - 1))) % kList] = key;
         pending += all;
-        next += kUnit;
-        sync();
     }
+    __device__ Key key(int i) const { return sm.list[(list_at + i) % kList]; }
     __device__ void taken(int n) { list_at = (list_at + n) % kList, pending -= n; }
 };
-// Filled by the 128 (rows RT or fewer).
-template <int RT>
-__device__ void fill_rows(const SharedParams &p, const Part &part, Rows<RT> &rows, int tid) {
-    const auto sync = [] { asm volatile("bar.sync 1, 128;" ::: "memory"); };
-    if (tid == 0) rows.least = INT32_MAX, rows.most = INT32_MIN, rows.n_want = 0;
-    sync();
-    if (tid < RT) {
-        const RowInfo x = row_info<RT>(p, part, tid);
-        rows.want_row[tid] = x.want_row, rows.want_col[tid] = x.want_col, rows.below[tid] = x.below;
-        if (x.below >= 0) {
-            atomicMin(&rows.least, x.below);
-            atomicMax(&rows.most, x.below);
-        }
-    }
-    sync();
-    if (tid < RT) {
-        const int a = rows.want_row[tid], b = rows.want_col[tid];
-        const bool same = tid > 0 && rows.want_row[tid - 1] == a && rows.want_col[tid - 1] == b;
-        if (!same && (a != kNever || b != kNever)) rows.want[atomicAdd(&rows.n_want, 1)] = make_int2(a, b);
-    }
-    sync();
-}
 
 __device__ __forceinline__ void put(float x, float *y) { *y = x; }
 __device__ __forceinline__ void put(float x, __nv_bfloat16 *y) { *y = __float2bfloat16_rn(x); }
@@ -367,8 +375,10 @@ struct SimtSmem {
     float q[kSimtRows][DP + 4], k[kSimtKeys][DP + 4], v[kSimtKeys][DP];
     float s[kSimtRows][kSimtKeys + 4];
     Rows<kSimtRows> rows;
-    Key list[kList], keys[kSimtKeys];
-    int counts[4], n, last, plain;
+    ScoutSmem<kSimtRows> scout;
+    Part part;
+    Key keys[kSimtKeys];
+    int n, last, plain, done;
 };
 
 __device__ __forceinline__ void load16(const float *from, float *to) { *reinterpret_cast<float4 *>(to) = *reinterpret_cast<const float4 *>(from); }
@@ -383,16 +393,19 @@ __global__ void __launch_bounds__(kSimtThreads) shared_simt_kernel(const __grid_
     const Start start = find_start<kSimtRows, kSimtThreads>(p);
     if (blockIdx.x >= start.blocks) return;
     for (int i = tid; i < (int)(sizeof(SimtSmem<DP>) / 4); i += kSimtThreads) reinterpret_cast<uint32_t *>(smem_raw)[i] = 0;  // columns that nobody writes
-    Walk walk = walk_from<kSimtRows>(p, start);
-    Looker<kSimtRows> look = {p, &sm.rows, sm.list, sm.counts, tid};
-    look.bad = false;
+    Scout<kSimtRows> scout = {p, sm.scout, tid};
     __syncthreads();
-    Part part;
-    for (int n_parts = 0; next_part<kSimtRows>(p, walk, part); ++n_parts) {
-        if (tid < 128) {
-            fill_rows(p, part, sm.rows, tid);
-            look.begin(part, &sm.rows);
+    if (tid < kScouts) scout.start(start);
+    for (int n_parts = 0;; ++n_parts) {
+        Part part;
+        if (tid < kScouts) {
+            const bool is = scout.next_part(part);
+            if (is) scout.begin(part, sm.rows);
+            if (tid == 0) sm.done = !is, sm.part = part;
         }
+        __syncthreads();
+        if (sm.done) break;
+        part = sm.part;
         for (int i = tid; i < kSimtRows * (p.d / kVec); i += kSimtThreads) {
             const int r = i / (p.d / kVec), c = (i - r * (p.d / kVec)) * kVec;
             if (r >= part.n_rows) continue;
@@ -407,16 +420,17 @@ __global__ void __launch_bounds__(kSimtThreads) shared_simt_kernel(const __grid_
             for (int c = 0; c < kCols; ++c) o[r][c] = 0.f;
         }
         for (bool more = true; more;) {
-            if (tid < 128) {
-                while (look.pending < kSimtKeys && look.more()) look.look();
-                const int n = min(look.pending, kSimtKeys);
+            if (tid < kScouts) {
+                while (scout.pending < kSimtKeys && scout.more()) scout.look();
+                scout.sync();
+                const int n = min(scout.pending, kSimtKeys);
                 bool every = true;
                 if (tid < kSimtKeys) {
-                    if (tid < n) sm.keys[tid] = look.list[(look.list_at + tid) % kList];
-                    every = __all_sync(~0u, tid >= n || sm.keys[tid].place < sm.rows.least);
+                    if (tid < n) sm.keys[tid] = scout.key(tid);
+                    every = __all_sync(~0u, tid >= n || sm.keys[tid].place < scout.wishes().least);
                 }
-                if (tid == 0) sm.n = n, sm.last = look.pending <= kSimtKeys && !look.more(), sm.plain = every;
-                look.taken(n);
+                if (tid == 0) sm.n = n, sm.last = scout.pending <= kSimtKeys && !scout.more(), sm.plain = every;
+                scout.taken(n);
             }
             __syncthreads();
             const int n = sm.n;
@@ -541,44 +555,51 @@ __global__ void __launch_bounds__(kSimtThreads) shared_simt_kernel(const __grid_
                 *joint = joint_from(part, start, slot);
         }
     }
-    if (look.bad) atomicOr(p.cache.status, kCacheBad);
+    if (tid < kScouts && scout.bad) atomicOr(p.cache.status, kCacheBad);
 }
 
 // ---- the tensor-core kernel (bf16): tiles of 128 rows and 128 keys, one block to an SM
 
 constexpr int kTcRows = 128, kTcKeys = 128;
-constexpr int kSoftmaxWarps = 8;              // two threads to a row: 64 keys each
-constexpr int kLoadWarp0 = kSoftmaxWarps, kLoadWarps = 4;
-constexpr int kMmaWarp = kLoadWarp0 + kLoadWarps;
+constexpr int kSoftmaxWarps = 8;              // two teams, which take the tiles in turn; a thread to a row
+constexpr int kLoadWarp0 = kSoftmaxWarps, kLoadWarps = kScouts / 32;
+constexpr int kCopyWarp0 = kLoadWarp0 + kLoadWarps, kCopyWarps = 3;
+constexpr int kMmaWarp = kCopyWarp0 + kCopyWarps;
 constexpr int kTcThreads = 32 * (kMmaWarp + 1);
 constexpr int kMetas = 4;                     // tiles whose keys are known
 constexpr float kRescale = 8.f;               // log2 units that a score may exceed its row's base by
-// tensor memory: O (fp32), S of two tiles (fp32), P (pairs of bf16, the weights' upper and lower halves)
-constexpr uint32_t kTmemCols = 512, kTmemO = 0, kTmemS = 128, kTmemHi = 384, kTmemLo = 448;
+// tensor memory: O of the teams (fp32), then S of their tiles (fp32), which P takes the place of: of every 16 keys the weights' upper halves
+// (8 columns of bf16 pairs) and their lower ones
+constexpr uint32_t kTmemCols = 512, kTmemO = 0, kTmemS = 256;
 
 template <int DP>
 struct TcShape {
     static constexpr int kTile = kTcKeys * DP * 2;              // bytes; column halves of 64 elements, 128 bytes a row and swizzled
     static constexpr int kHalf = kTcKeys * 128;
     static constexpr int kStages = DP == 64 ? 4 : 2;            // tiles of keys, and of values
+    // where 16 bytes of a row go
+    __device__ static uint32_t place(uint32_t tile, int row, int chunk) {
+        return tile + (chunk >> 3) * kHalf + row * 128 + (((chunk & 7) ^ (row & 7)) << 4);
+    }
 };
 struct alignas(16) Meta {
-    int n, first, last, q;  // keys; of the part; buffer of its Q.  n < 0: the share is done
-    uint32_t plain;         // 0x01010101: every row attends every key
-    alignas(16) int place[kTcKeys], row[kTcKeys], col[kTcKeys];
+    int n, first, last;  // keys; of the part.  n < 0: the share is done
+    uint32_t plain;      // 0x01010101: every row attends every key
+    int place[kTcKeys], row[kTcKeys], col[kTcKeys];
+    unsigned at[kTcKeys];
 };
 template <int DP>
 struct TcSmem {  // from a multiple of 1024 bytes on
     uint8_t q[2][TcShape<DP>::kTile];
     uint8_t k[TcShape<DP>::kStages][TcShape<DP>::kTile], v[TcShape<DP>::kStages][TcShape<DP>::kTile];
     Meta meta[kMetas];
+    ScoutSmem<kTcRows> scout;
     Rows<kTcRows> rows[2];
     Part part[2];
-    Key list[kList];
-    float other[2][kTcRows];  // what the two threads of a row tell one another
-    int counts[4];
-    uint64_t q_full[2], q_empty[2], k_full[4], k_empty[4], v_full[4], v_empty[4], meta_full[kMetas], meta_empty[kMetas], s_full[2], s_free[2], p_full,
-        pv_done, final_;
+    float2 stats[2][kTcRows];
+    uint64_t q_full[2], q_empty[2], k_full[4], k_empty[4], v_full[4], v_empty[4], meta_full[kMetas], meta_empty[kMetas], s_full[2], p_full[2], pv_done[2],
+        team[2], both, final_;
+    int odd[2];
     uint32_t tmem;
     int abort;
 };
@@ -586,28 +607,19 @@ struct TcSmem {  // from a multiple of 1024 bytes on
 __device__ __forceinline__ void cp_async16_or_zero(uint32_t dst, const void *src, bool there) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
 }
-// All `threads` of a barrier: whether one of them says so.
-template <int kId, int kThreads>
-__device__ __forceinline__ bool any_of(bool x) {
+// Whether one of the scouts says so.  All of them call it.
+__device__ __forceinline__ bool any_scout(bool x) {
     uint32_t r;
     asm volatile(
         "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\t"
-        "barrier.cta.red.or.pred q, %2, %3, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+        "barrier.cta.red.or.pred q, 1, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
         : "=r"(r)
-        : "r"((uint32_t)x), "n"(kId), "n"(kThreads)
+        : "r"((uint32_t)x), "n"(kScouts)
         : "memory");
     return r != 0;
 }
 
-// 32 scores of a row, scaled; those that do not count become -inf.
-__device__ __forceinline__ void scale_scores(uint32_t (&v)[32], uint64_t scale2) {
-#pragma unroll
-    for (int e = 0; e < 32; e += 2) {
-        float x, y;
-        ptx::unpack_f32x2(ptx::mul_f32x2(ptx::pack_f32x2(v[e], v[e + 1]), scale2), x, y);
-        v[e] = __float_as_uint(x), v[e + 1] = __float_as_uint(y);
-    }
-}
+// 32 scores of a row: those that do not count become -inf.
 __device__ __forceinline__ void mask_scores(uint32_t (&v)[32], const Meta &meta, int c0, int want_row, int want_col, int below) {
 #pragma unroll
     for (int e = 0; e < 32; e += 4) {
@@ -619,11 +631,6 @@ __device__ __forceinline__ void mask_scores(uint32_t (&v)[32], const Meta &meta,
         if (!attends(want_row, want_col, below, place.w, row.w, col.w)) v[e + 3] = 0xff800000u;
     }
 }
-__device__ __forceinline__ void cut_scores(uint32_t (&v)[32], int n) {  // columns from n on
-#pragma unroll
-    for (int e = 0; e < 32; ++e)
-        if (e >= n) v[e] = 0xff800000u;
-}
 __device__ __forceinline__ float top_score(const uint32_t (&v)[32], float top) {
     float t[4] = {top, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
@@ -632,19 +639,19 @@ __device__ __forceinline__ float top_score(const uint32_t (&v)[32], float top) {
         for (int j = 0; j < 4; ++j) t[j] = ptx::fmax3(t[j], __uint_as_float(v[e + 2 * j]), __uint_as_float(v[e + 2 * j + 1]));
     return fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
 }
-// Weights 2^(x - base) as pairs of bf16: rounded, and what the rounding left, rounded (their sum has 16 bits).  The sums take all of them.
-__device__ __forceinline__ void weigh(const uint32_t (&v)[32], uint64_t neg_base2, uint32_t (&hi)[16], uint32_t (&lo)[16], uint64_t (&sum)[2]) {
+// Weights 2^(s scale - base) of 16 keys as pairs of bf16: rounded, and what the rounding left, rounded (their sum has 16 bits: an error of
+// 2^-17 of a weight, which the result's rounding to bf16, 2^-9, hides but for one value in some hundred).  The sums take all of them.
+__device__ __forceinline__ void weigh(const uint32_t *v, uint64_t scale2, uint64_t neg_base2, uint32_t (&hi_lo)[16], uint64_t (&sum)[2]) {
 #pragma unroll
-    for (int e = 0; e < 32; e += 2) {
+    for (int e = 0; e < 16; e += 2) {
         float x, y;
-        ptx::unpack_f32x2(ptx::add_f32x2(ptx::pack_f32x2(v[e], v[e + 1]), neg_base2), x, y);
+        ptx::unpack_f32x2(ptx::fma_f32x2(ptx::pack_f32x2(v[e], v[e + 1]), scale2, neg_base2), x, y);
         x = ptx::ex2(x), y = ptx::ex2(y);
         const uint64_t xy = ptx::pack_f32x2(x, y);
         sum[e >> 1 & 1] = ptx::add_f32x2(sum[e >> 1 & 1], xy);
         const uint32_t h = ptx::cvt_bf16x2(x, y);
-        hi[e >> 1] = h;
         ptx::unpack_f32x2(ptx::sub_f32x2(xy, ptx::pack_f32x2(h << 16, h & 0xffff0000u)), x, y);
-        lo[e >> 1] = ptx::cvt_bf16x2(x, y);
+        hi_lo[e >> 1] = h, hi_lo[8 + (e >> 1)] = ptx::cvt_bf16x2(x, y);
     }
 }
 
@@ -652,7 +659,8 @@ template <int DP>
 __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_constant__ SharedParams p) {
     using namespace ptx;
     using S = TcShape<DP>;
-    constexpr int kStages = S::kStages, kHalves = DP / 64, kOwn = DP / 2;  // kOwn: columns of O of a thread
+    constexpr int kStages = S::kStages, kHalves = DP / 64;
+    constexpr int kPer = DP / 8, kRowsOfCopy = 32 / kPer;  // copies: lanes to a row; rows of an instruction
     extern __shared__ uint8_t tc_smem[];
     TcSmem<DP> &sm = *reinterpret_cast<TcSmem<DP> *>(tc_smem + (-smem_u32(tc_smem) & 1023));
     const int tid = threadIdx.x, warp = __shfl_sync(~0u, tid >> 5, 0), lane = tid & 31;
@@ -662,15 +670,16 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
         for (int i = 0; i < 2; ++i) {
             mbar_init(bar(sm.q_full[i]), kLoadWarps);
             mbar_init(bar(sm.q_empty[i]), kSoftmaxWarps + 1);
-            mbar_init(bar(sm.s_full[i]), 1);
-            mbar_init(bar(sm.s_free[i]), kSoftmaxWarps);
+            mbar_init(bar(sm.s_full[i]), 1), mbar_init(bar(sm.pv_done[i]), 1);
+            mbar_init(bar(sm.p_full[i]), kSoftmaxWarps / 2), mbar_init(bar(sm.team[i]), kSoftmaxWarps / 2);
+            sm.odd[i] = 0;
         }
         for (int i = 0; i < kStages; ++i) {
-            mbar_init(bar(sm.k_full[i]), kLoadWarps), mbar_init(bar(sm.v_full[i]), kLoadWarps);
+            mbar_init(bar(sm.k_full[i]), kCopyWarps), mbar_init(bar(sm.v_full[i]), kCopyWarps);
             mbar_init(bar(sm.k_empty[i]), 1), mbar_init(bar(sm.v_empty[i]), 1);
         }
-        for (int i = 0; i < kMetas; ++i) mbar_init(bar(sm.meta_full[i]), kLoadWarps), mbar_init(bar(sm.meta_empty[i]), kSoftmaxWarps + 1);
-        mbar_init(bar(sm.p_full), kSoftmaxWarps), mbar_init(bar(sm.pv_done), 1), mbar_init(bar(sm.final_), 1);
+        for (int i = 0; i < kMetas; ++i) mbar_init(bar(sm.meta_full[i]), kLoadWarps), mbar_init(bar(sm.meta_empty[i]), kSoftmaxWarps + kCopyWarps + 1);
+        mbar_init(bar(sm.both), kSoftmaxWarps), mbar_init(bar(sm.final_), 1);
         sm.abort = 0;
         fence_mbar_init();
     }
@@ -683,12 +692,12 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
     fence_proxy_async();
     tc_fence_before();
     wait_prior_grid();
+    launch_dependents();  // (what is launched next waits for the end of this before it reads results)
     const Start start = find_start<kTcRows, kTcThreads>(p);  // (its barriers: the set-up is seen by all)
     tc_fence_after();
     const uint32_t tmem = __shfl_sync(~0u, sm.tmem, 0);
 
-    // Every wait is bounded; the first one to run out raises the flag that ends all of them.  Warps that meet at a barrier leave together,
-    // when one of them says there that a wait of its own has failed.
+    // Every wait is bounded; the first one to run out raises the flag that ends all of them.
     volatile int *abort = &sm.abort;
     const auto wait = [&](const uint64_t &b, uint32_t parity) -> bool {
 #pragma unroll 1
@@ -703,144 +712,133 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
     if (blockIdx.x >= start.blocks) {
     } else if (warp < kSoftmaxWarps) {
         // ------------------------------------------------------------------ softmax and results
-        const int half = warp >> 2, r = tid & 127;  // columns of S and of O; row, which is the lane of tensor memory
-        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-        const uint32_t tO = tmem + lanes + kTmemO + half * kOwn, tHi = tmem + lanes + kTmemHi + half * 32, tLo = tmem + lanes + kTmemLo + half * 32;
+        const int team = warp >> 2, r = tid & 127;  // row: the lane of tensor memory
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, tS = tmem + lanes + kTmemS + team * kTcKeys, tO = tmem + lanes + kTmemO + team * 128;
         const uint64_t scale2 = pack_f32x2(p.scale_log2, p.scale_log2);
-        int c = 0, pv_seen = 0, parts = 0;  // tiles with keys; those whose P V is known to be done; parts
-        bool failed = false;
-        int want_row = 0, want_col = 0, below = 0, first_c = 0;
+        int c = 0, mine = 0, parts = 0, teams = 0, boths = 0;  // tiles with keys, and the team's; parts; barriers passed
+        const auto sync = [&](const uint64_t &b, int &passed) {  // (bounded like the other waits)
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(b));
+            return wait(b, passed++ & 1);
+        };
+        int want_row = 0, want_col = 0, below = 0, tiles = 0, own = 0;  // tiles of the part; the team's
         bool live = false;
         float m = -INFINITY;
         uint64_t sum[2] = {0, 0};
-        const auto wait_pv = [&](int done) {  // the P V of the first `done` tiles
-            if (pv_seen >= done) return;
-            pv_seen = done;
-            if (!wait(sm.pv_done, (done - 1) & 1)) failed = true;
-            tc_fence_after();
-        };
 #pragma unroll 1
         for (int t = 0;; ++t) {
-            Meta &meta = sm.meta[t % kMetas];
-            if (!wait(sm.meta_full[t % kMetas], t / kMetas & 1)) failed = true;
-            const bool over = !failed && meta.n < 0;
-            const int n = failed || over ? 0 : meta.n, qb = meta.q & 1;
+            const Meta &meta = sm.meta[t % kMetas];
+            if (!wait(sm.meta_full[t % kMetas], t / kMetas & 1)) break;
+            const int n = meta.n, qb = parts & 1;
+            if (n < 0) break;
             const Part &part = sm.part[qb];
-            if (!failed && !over && meta.first) {
-                if (!wait(sm.q_full[qb], parts / 2 & 1)) failed = true;
+            if (meta.first) {
+                if (!wait(sm.q_full[qb], parts / 2 & 1)) break;
                 const Rows<kTcRows> &rows = sm.rows[qb];
                 want_row = rows.want_row[r], want_col = rows.want_col[r], below = rows.below[r];
                 live = (warp & 3) * 32 < part.n_rows;
-                first_c = c;
+                tiles = own = 0;
                 m = -INFINITY;
                 sum[0] = sum[1] = 0;
-                uint32_t zero[16] = {};
-#pragma unroll
-                for (int i = 0; i < kOwn / 16; ++i) tmem_st16(tO + 16 * i, zero);
             }
-            const bool plain = meta.plain == 0x01010101u, mine = live && n > 64 * half, both = n > 64 * half + 32;
-            uint32_t x[2][32];
-            float top = -INFINITY;
-            bool odd = false;
-            if (n > 0) {
-                if (!wait(sm.s_full[c & 1], c >> 1 & 1)) failed = true;
+            const bool last = meta.last;
+            if (n > 0 && (c & 1) == team) {
+                const bool plain = meta.plain == 0x01010101u;
+                // (S is there, so the P V of the team's tile before, whose place it has, is done)
+                if (!wait(sm.s_full[team], mine & 1)) break;
                 tc_fence_after();
-                if (mine) {
-                    const uint32_t tS = tmem + lanes + kTmemS + (c & 1) * kTcKeys + half * 64;
-                    tmem_ld32(tS, x[0]);
-                    if (both) tmem_ld32(tS + 32, x[1]);
-                    tc_wait_ld();
-                    reg_fence(x[0]);
-                    reg_fence(x[1]);
-                }
-                tc_fence_before();
-                if (lane == 0) mbar_arrive(bar(sm.s_free[c & 1]));
-                if (mine) {
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        if (i == 1 && !both) break;
-                        const int c0 = 64 * half + 32 * i;
-                        scale_scores(x[i], scale2);
-                        if (!plain)
-                            mask_scores(x[i], meta, c0, want_row, want_col, below);
-                        else if (n < c0 + 32)
-                            cut_scores(x[i], n - c0);
-                        top = top_score(x[i], top);
-                    }
-                }
+                const int stage = c % kStages;
+                bool odd = false;
                 if (!plain) {  // a weight 0 does not undo a value that is not a number: is there one?
-                    if (!wait(sm.v_full[c % kStages], c / kStages & 1)) failed = true;
+                    if (!wait(sm.v_full[stage], c / kStages & 1)) break;
                     __nv_bfloat162 z = __floats2bfloat162_rn(0.f, 0.f);
-                    const uint4 *v = reinterpret_cast<const uint4 *>(sm.v[c % kStages]);
+                    const uint4 *v = reinterpret_cast<const uint4 *>(sm.v[stage]);
 #pragma unroll 4
-                    for (int i = tid; i < kHalves * kTcKeys * 8; i += 32 * kSoftmaxWarps) {
+                    for (int i = r; i < kHalves * kTcKeys * 8; i += 128) {
                         const uint4 y = (i >> 3 & (kTcKeys - 1)) < n ? v[i] : make_uint4(0, 0, 0, 0);
                         for (uint32_t w : {y.x, y.y, y.z, y.w})
                             z = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&w), __floats2bfloat162_rn(0.f, 0.f), z);
                     }
-                    odd = !(__low2float(z) == 0.f && __high2float(z) == 0.f);
+                    if (__any_sync(~0u, !(__low2float(z) == 0.f && __high2float(z) == 0.f)) && lane == 0) *(volatile int *)&sm.odd[team] = c + 1;
+                    if (!sync(sm.team[team], teams)) break;
+                    odd = *(volatile int *)&sm.odd[team] == c + 1;
                 }
-            }
-            // The base of a row moves when a score exceeds it by kRescale, and with the row's first score.
-            bool odd_one = false;
-            if (any_of<2, 32 * kSoftmaxWarps>(failed || over || odd || top > m + kRescale)) {
-                if (any_of<2, 32 * kSoftmaxWarps>(failed || over)) break;
-                sm.other[half][r] = top;
-                odd_one = any_of<2, 32 * kSoftmaxWarps>(odd);
                 if (live) {
-                    top = fmaxf(top, sm.other[half ^ 1][r]);
-                    float keep = 1.f;
-                    if (top > m + kRescale) keep = ex2(m - top), m = top;
-                    if (c > first_c && __any_sync(~0u, keep != 1.f)) {
-                        wait_pv(c);
+                    float top = -INFINITY;
+#pragma unroll 1
+                    for (int c0 = 0; c0 < n; c0 += 32) {
+                        uint32_t v[32];
+                        tmem_ld32(tS + c0, v);
+                        tc_wait_ld();
+                        reg_fence(v);
+                        if (!plain || n < c0 + 32) {  // (behind the last key there is nobody's, which no row attends)
+                            if (!plain)
+                                mask_scores(v, meta, c0, want_row, want_col, below);
+                            else
+#pragma unroll
+                                for (int e = 0; e < 32; ++e)
+                                    if (e >= n - c0) v[e] = 0xff800000u;
+                            uint32_t half[16];
+#pragma unroll
+                            for (int i = 0; i < 2; ++i) {
+#pragma unroll
+                                for (int e = 0; e < 16; ++e) half[e] = v[16 * i + e];
+                                tmem_st16(tS + c0 + 16 * i, half);
+                            }
+                            tc_wait_st();
+                        }
+                        top = top_score(v, top);
+                    }
+                    // The base of a row moves when a score exceeds it by kRescale, and with the row's first score.
+                    top *= p.scale_log2;
+                    const bool moves = top > m + kRescale;
+                    if (__any_sync(~0u, moves) || own == 0) {
+                        const float keep = moves ? ex2(m - top) : 1.f;
+                        if (moves) m = top;
                         const uint64_t keep2 = pack_f32x2(keep, keep);
                         sum[0] = mul_f32x2(sum[0], keep2), sum[1] = mul_f32x2(sum[1], keep2);
 #pragma unroll 1
-                        for (int i = 0; i < kOwn / 16; ++i) {
-                            uint32_t o[16];
-                            tmem_ld16(tO + 16 * i, o);
-                            tc_wait_ld();
-                            reg_fence(o);
+                        for (int i = 0; i < DP; i += 16) {
+                            uint32_t o[16] = {};
+                            if (own > 0) {
+                                tmem_ld16(tO + i, o);
+                                tc_wait_ld();
+                                reg_fence(o);
+                            }
 #pragma unroll
                             for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * keep);
-                            tmem_st16(tO + 16 * i, o);
+                            tmem_st16(tO + i, o);
                         }
                     }
-                }
-            }
-            if (n > 0) {
-                const float neg = m == -INFINITY ? 0.f : -m;
-                const uint64_t neg2 = pack_f32x2(neg, neg);
-                if (mine) {
+                    const float neg = m == -INFINITY ? 0.f : -m;
+                    const uint64_t neg2 = pack_f32x2(neg, neg);
+#pragma unroll 1
+                    for (int c0 = 0; c0 < n; c0 += 32) {
+                        uint32_t v[32], hi_lo[16];
+                        tmem_ld32(tS + c0, v);
+                        tc_wait_ld();
+                        reg_fence(v);
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        if (i == 1 && !both) break;
-                        uint32_t hi[16], lo[16];
-                        weigh(x[i], neg2, hi, lo, sum);
-                        wait_pv(c);
-                        tmem_st16(tHi + 16 * i, hi);
-                        tmem_st16(tLo + 16 * i, lo);
+                        for (int i = 0; i < 32; i += 16) {
+                            weigh(v + i, scale2, neg2, hi_lo, sum);
+                            tmem_st16(tS + c0 + i, hi_lo);
+                        }
                     }
+                    tc_wait_st();
                 }
-                wait_pv(c);
-                tc_wait_st();
-                if (odd_one) {
+                if (odd) {
                     // Values that are not numbers: added here to the rows that attend them, and taken out of the tile.
-                    tc_fence_before();
-                    any_of<2, 32 * kSoftmaxWarps>(false);
-                    tc_fence_after();
-                    uint8_t *v = sm.v[c % kStages];
                     const auto at = [&](int key, int e) {
-                        return reinterpret_cast<__nv_bfloat16 *>(v + e / 64 * S::kHalf + key * 128 + ((e / 8 & 7) ^ (key & 7)) * 16 + e % 8 * 2);
+                        return reinterpret_cast<__nv_bfloat16 *>(sm.v[stage] + e / 64 * S::kHalf + key * 128 + ((e / 8 & 7) ^ (key & 7)) * 16 + e % 8 * 2);
                     };
 #pragma unroll 1
                     for (int key = 0; key < n && live; ++key) {
                         const bool counts = attends(want_row, want_col, below, meta.place[key], meta.row[key], meta.col[key]);
 #pragma unroll 1
-                        for (int e = 0; e < kOwn; ++e) {
-                            const float y = __bfloat162float(*at(key, half * kOwn + e));
+                        for (int e = 0; e < DP; ++e) {
+                            const float y = __bfloat162float(*at(key, e));
                             if (fabsf(y) < INFINITY) continue;
-                            const uint32_t col = lanes + (key >> 1), hi = tmem_ld1(tmem + kTmemHi + col), lo = tmem_ld1(tmem + kTmemLo + col);
+                            const uint32_t col = tS + key / 16 * 16 + key % 16 / 2, hi = tmem_ld1(col), lo = tmem_ld1(col + 8);
                             const uint32_t cut = key & 1 ? 0xffff0000u : 0xffffu, up = key & 1 ? 0 : 16;
                             const float w = __uint_as_float((hi & cut) << up) + __uint_as_float((lo & cut) << up);
                             const float o = __uint_as_float(tmem_ld1(tO + e));
@@ -848,119 +846,134 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
                             tc_wait_st();
                         }
                     }
-                    any_of<2, 32 * kSoftmaxWarps>(false);
-                    for (int i = tid; i < n * DP; i += 32 * kSoftmaxWarps) {
+                    if (!sync(sm.team[team], teams)) break;
+#pragma unroll 1
+                    for (int i = r; i < n * DP; i += 128) {
                         __nv_bfloat16 *y = at(i / DP, i % DP);
                         if (!(fabsf(__bfloat162float(*y)) < INFINITY)) *y = __float2bfloat16_rn(0.f);
                     }
                     fence_proxy_async();
-                    __syncwarp();
                 }
                 tc_fence_before();
-                if (lane == 0) mbar_arrive(bar(sm.p_full));
-                ++c;
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(sm.p_full[team]));
+                ++mine, ++own;
             }
-            const bool last = meta.last;
+            tiles += n > 0, c += n > 0;
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(sm.meta_empty[t % kMetas]));
             if (!last) continue;
 
-            // the part is done
-            float a, b, l;
-            unpack_f32x2(add_f32x2(sum[0], sum[1]), a, b);
-            l = a + b;
-            sm.other[half][r] = l;
-            wait_pv(c);
-            tc_wait_st();  // (a part without a key: the zeros)
-            any_of<2, 32 * kSoftmaxWarps>(false);
-            l += sm.other[half ^ 1][r];
-            if (below < -1) l = 0.f, m = -INFINITY;  // (a row that attends nothing, whatever the others attend)
-            const int state = part_state(part), slot = parts == 0 ? 0 : 1;
-            const int at = part.tile * kTcRows + r, member = part.seg == 0 ? at / p.group : 0;
-            const size_t out = (size_t)(part.b + member) * p.heads + part.kv * p.group + at - member * p.group;
-            const size_t whole = (size_t)part.seg * p.B * p.heads + out;
-            float *to = p.parts + (size_t)(2 * blockIdx.x + slot) * part_floats(kTcRows, p.d);
-            if (live) {
-                const bool row = r < part.n_rows;
-                const float by = state == kAll && !part.grouped ? 1.f / l : 1.f;
+            // The part is done: by both teams, half of the columns each, if it had more than one tile, else by the one that had it (the first
+            // team, if it had none).
+            const bool joined = tiles > 1;
+            if (joined || own > 0 || (tiles == 0 && team == 0)) {
+                float a, b;
+                unpack_f32x2(add_f32x2(sum[0], sum[1]), a, b);
+                float l = a + b, f[2] = {1.f, 1.f};
+                if (own > 0 && !wait(sm.pv_done[team], (mine - 1) & 1)) break;
+                if (joined) {
+                    sm.stats[team][r] = make_float2(m, l);
+                    if (!sync(sm.both, boths)) break;
+                    const float2 x = sm.stats[0][r], y = sm.stats[1][r];
+                    m = fmaxf(x.x, y.x);
+                    const float base = m == -INFINITY ? 0.f : m;
+                    f[0] = ex2(x.x - base), f[1] = ex2(y.x - base);
+                    l = fmaf(x.y, f[0], y.y * f[1]);
+                }
+                tc_fence_after();
+                if (below < -1) l = 0.f, m = -INFINITY;  // (a row that attends nothing, whatever the others attend)
+                const int state = part_state(part), slot = parts == 0 ? 0 : 1;
+                const int at = part.tile * kTcRows + r, member = part.seg == 0 ? at / p.group : 0;
+                const size_t out = (size_t)(part.b + member) * p.heads + part.kv * p.group + at - member * p.group;
+                const size_t whole = (size_t)part.seg * p.B * p.heads + out;
+                float *to = p.parts + (size_t)(2 * blockIdx.x + slot) * part_floats(kTcRows, p.d);
+                if (live) {
+                    const bool row = r < part.n_rows;
+                    if (state == kAll && !part.grouped) f[0] /= l, f[1] /= l;
+                    const int col0 = joined ? team * (DP / 2) : 0, col1 = joined ? col0 + DP / 2 : DP;
 #pragma unroll 1
-                for (int i = 0; i < kOwn / 16; ++i) {
-                    uint32_t o[16];
-                    tmem_ld16(tO + 16 * i, o);
-                    tc_wait_ld();
-                    reg_fence(o);
-                    if (!row) continue;
+                    for (int col = col0; col < col1; col += 8) {
+                        uint32_t o[8], o2[8] = {};
+                        tmem_ld8(tmem + lanes + kTmemO + (joined ? 0 : team * 128) + col, o);
+                        if (joined) tmem_ld8(tmem + lanes + kTmemO + 128 + col, o2);
+                        tc_wait_ld();
+                        reg_fence(o);
+                        reg_fence(o2);
+                        if (!row || col >= p.d) continue;
+                        float x[8];
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) o[e] = l == 0.f ? 0u : __float_as_uint(__uint_as_float(o[e]) * by);
-#pragma unroll
-                    for (int e = 0; e < 16; e += 8) {
-                        const int col = half * kOwn + 16 * i + e;
-                        if (col >= p.d) break;
-                        const uint4 lo4 = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]), hi4 = make_uint4(o[e + 4], o[e + 5], o[e + 6], o[e + 7]);
-                        if (state != kAll) {
-                            reinterpret_cast<uint4 *>(to)[col / 4 * kTcRows + r] = lo4;
-                            reinterpret_cast<uint4 *>(to)[(col / 4 + 1) * kTcRows + r] = hi4;
-                        } else if (part.grouped) {
-                            reinterpret_cast<uint4 *>(p.whole + whole * p.d + col)[0] = lo4;
-                            reinterpret_cast<uint4 *>(p.whole + whole * p.d + col)[1] = hi4;
-                        } else {
-                            const auto f = [](uint32_t u) { return __uint_as_float(u); };
+                        for (int e = 0; e < 8; ++e) {
+                            x[e] = __uint_as_float(o[e]) * f[0];
+                            if (joined) x[e] = fmaf(__uint_as_float(o2[e]), f[1], x[e]);
+                            if (l == 0.f) x[e] = 0.f;
+                        }
+                        if (state == kAll && !part.grouped) {
                             *reinterpret_cast<uint4 *>((__nv_bfloat16 *)p.O + out * p.d + col) =
-                                make_uint4(cvt_bf16x2(f(lo4.x), f(lo4.y)), cvt_bf16x2(f(lo4.z), f(lo4.w)), cvt_bf16x2(f(hi4.x), f(hi4.y)),
-                                           cvt_bf16x2(f(hi4.z), f(hi4.w)));
+                                make_uint4(cvt_bf16x2(x[0], x[1]), cvt_bf16x2(x[2], x[3]), cvt_bf16x2(x[4], x[5]), cvt_bf16x2(x[6], x[7]));
+                        } else {
+                            float4 *y = state == kAll ? reinterpret_cast<float4 *>(p.whole + whole * p.d + col) : reinterpret_cast<float4 *>(to) + col / 4 * kTcRows + r;
+                            y[0] = make_float4(x[0], x[1], x[2], x[3]);
+                            y[state == kAll ? 1 : kTcRows] = make_float4(x[4], x[5], x[6], x[7]);
                         }
                     }
+                    if (row && (!joined || team == 0)) {
+                        if (state != kAll)
+                            reinterpret_cast<float2 *>(to + (size_t)p.d * kTcRows)[r] = make_float2(m, l);
+                        else if (part.grouped)
+                            p.whole_stats[whole] = make_float2(m, l);
+                        else
+                            p.LSE[out] = natural(m, l);
+                    }
                 }
-                if (row && half == 0) {
-                    if (state != kAll)
-                        reinterpret_cast<float2 *>(to + (size_t)p.d * kTcRows)[r] = make_float2(m, l);
-                    else if (part.grouped)
-                        p.whole_stats[whole] = make_float2(m, l);
+                if (r == 0 && (!joined || team == 0) && state != kGoesOn) {
+                    Joint *joint = joint_of(p, part.seg, part.kv, part.b, part.tile);
+                    if (state == kAll)
+                        joint->slot = -1;
                     else
-                        p.LSE[out] = natural(m, l);
+                        *joint = joint_from(part, start, slot);
                 }
+                tc_fence_before();
+                if (joined && !sync(sm.both, boths)) break;  // O has been read
             }
-            if (tid == 0 && state != kGoesOn) {
-                Joint *joint = joint_of(p, part.seg, part.kv, part.b, part.tile);
-                if (state == kAll)
-                    joint->slot = -1;
-                else
-                    *joint = joint_from(part, start, slot);
-            }
-            tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(sm.q_empty[qb]));
             ++parts;
         }
-    } else if (warp < kMmaWarp) {
-        // ------------------------------------------------------------------ who is read, and the copies
+    } else if (warp < kCopyWarp0) {
+        // ------------------------------------------------------------------ queries, and which keys are read
+        // (These warps meet at barriers: they leave together, when one of them says there that a wait of its own has failed.)
         const int lt = tid - 32 * kLoadWarp0, lw = warp - kLoadWarp0;
-        constexpr int kPer = DP / 8, kRowsOfCopy = 32 / kPer;  // lanes to a row; rows of an instruction
-        const int chunk = lane % kPer, sub = lane / kPer;
-        const bool copies = chunk < p.d / 8;
-        // where a lane's 16 bytes of row 32 lw + sub go; further rows by the row, whose low three bits permute the chunks
-        const auto place = [&](uint32_t tile, int row) { return tile + (chunk >> 3) * S::kHalf + row * 128 + (((chunk & 7) ^ (row & 7)) << 4); };
-        Walk walk = walk_from<kTcRows>(p, start);
-        Looker<kTcRows> look = {p, nullptr, sm.list, sm.counts, lt};
-        look.bad = false;
+        Scout<kTcRows> scout = {p, sm.scout, lt};
+        scout.start(start);
         bool ok = true;
-        int t = 0, c = 0, parts = 0;
+        int t = 0;
         Part part;
 #pragma unroll 1
-        for (; next_part<kTcRows>(p, walk, part); ++parts) {
+        for (int parts = 0; scout.next_part(part); ++parts) {
             const int qb = parts & 1;
             if (parts >= 2) ok &= wait(sm.q_empty[qb], (parts / 2 - 1) & 1);
-            if (any_of<1, 32 * kLoadWarps>(!ok)) break;
-            fill_rows(p, part, sm.rows[qb], lt);
-            if (lt == 0) sm.part[qb] = part;
-            look.begin(part, &sm.rows[qb]);
+            if (any_scout(!ok)) break;
             const uint32_t q = smem_u32(sm.q[qb]);
+            const int chunk = lane % kPer;
 #pragma unroll 1
-            for (int i = 32 * lw + sub; i < 32 * lw + 32; i += kRowsOfCopy) {
-                if (i >= part.n_rows) break;
+            for (int i = 32 * lw + lane / kPer; i < min(32 * lw + 32, part.n_rows); i += kRowsOfCopy) {
                 const int at = part.tile * kTcRows + i, member = part.seg == 0 ? at / p.group : 0;
                 const __nv_bfloat16 *from = (const __nv_bfloat16 *)p.Q + (part.b + member) * p.q_batch + (part.kv * p.group + at - member * p.group) * p.q_head;
-                if (copies) cp_async16(place(q, i), from + chunk * 8);
+                if (chunk < p.d / 8) cp_async16(S::place(q, i, chunk), from + chunk * 8);
+            }
+            __syncwarp();
+            scout.begin(part, sm.rows[qb]);
+            if (lt == 0) sm.part[qb] = part;
+            if (p.flip) {  // a negative scale: its sign goes to the queries
+                asm volatile("cp.async.wait_all;" ::: "memory");
+#pragma unroll 1
+                for (int i = 32 * lw + lane / kPer; i < min(32 * lw + 32, part.n_rows); i += kRowsOfCopy) {
+                    uint4 *x = reinterpret_cast<uint4 *>(sm.q[qb] + (S::place(q, i, chunk) - q));
+                    constexpr uint32_t kSigns = 0x80008000u;
+                    *x = make_uint4(x->x ^ kSigns, x->y ^ kSigns, x->z ^ kSigns, x->w ^ kSigns);
+                }
+                __syncwarp();
             }
             cp_async_arrive(bar(sm.q_full[qb]));
             __syncwarp();
@@ -968,40 +981,21 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
             bool last = false;
 #pragma unroll 1
             for (bool first = true; !last; first = false, ++t) {
-                while (look.pending < kTcKeys && look.more()) look.look();
-                const int n = min(look.pending, kTcKeys);
-                last = look.pending <= kTcKeys && !look.more();
+                while (scout.pending < kTcKeys && scout.more()) scout.look();
+                const int n = min(scout.pending, kTcKeys);
+                last = scout.pending <= kTcKeys && !scout.more();
                 if (t >= kMetas) ok &= wait(sm.meta_empty[t % kMetas], (t / kMetas - 1) & 1);
-                if (any_of<1, 32 * kLoadWarps>(!ok)) break;
+                if (any_scout(!ok)) break;
                 Meta &meta = sm.meta[t % kMetas];
                 Key key = {0, INT32_MAX, kNever + 1, kNever + 1};  // nobody's
-                if (lt < n) key = sm.list[(look.list_at + lt) % kList];
-                meta.place[lt] = key.place, meta.row[lt] = key.row, meta.col[lt] = key.col;
-                const bool plain = __all_sync(~0u, lt >= n || key.place < sm.rows[qb].least);
+                if (lt < n) key = scout.key(lt);
+                meta.place[lt] = key.place, meta.row[lt] = key.row, meta.col[lt] = key.col, meta.at[lt] = key.at;
+                const bool plain = __all_sync(~0u, lt >= n || key.place < scout.wishes().least);
                 if (lane == 0) reinterpret_cast<uint8_t *>(&meta.plain)[lw] = plain;
-                if (lt == 0) meta.n = n, meta.first = first, meta.last = last, meta.q = qb;
+                if (lt == 0) meta.n = n, meta.first = first, meta.last = last;
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar(sm.meta_full[t % kMetas]));
-                look.taken(n);
-                if (n == 0) continue;
-                const int stage = c % kStages, rows16 = (n + 15) & ~15;
-#pragma unroll 1
-                for (int kv = 0; kv < 2; ++kv) {
-                    const uint64_t &full = kv ? sm.v_full[stage] : sm.k_full[stage], &empty = kv ? sm.v_empty[stage] : sm.k_empty[stage];
-                    if (c >= kStages && ok) ok = wait(empty, (c / kStages - 1) & 1);
-                    const uint32_t tile = smem_u32(kv ? sm.v[stage] : sm.k[stage]);
-                    const char *base = (const char *)(kv ? p.cache.v : p.cache.k) + chunk * 16;
-#pragma unroll
-                    for (int i = 0; i < 32; i += kRowsOfCopy) {
-                        const int row = 32 * lw + i + sub;
-                        const unsigned from = __shfl_sync(~0u, key.at, i + sub);
-                        if (ok && copies && row < rows16) cp_async16_or_zero(place(tile, row), base + (row < n ? (size_t)from * 16 : 0), row < n);
-                    }
-                    cp_async_arrive(bar(full));
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(bar(full));
-                }
-                ++c;
+                scout.taken(n);
             }
             if (!last) break;
         }
@@ -1010,17 +1004,45 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
         if (lt == 0) sm.meta[t % kMetas].n = -1;
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(sm.meta_full[t % kMetas]));
-        if (look.bad) atomicOr(p.cache.status, kCacheBad);
+        if (scout.bad) atomicOr(p.cache.status, kCacheBad);
+    } else if (warp < kMmaWarp) {
+        // ------------------------------------------------------------------ copies of keys and values
+        const int chunk = lane % kPer, first = (warp - kCopyWarp0) * kRowsOfCopy + lane / kPer;
+        const bool copies = chunk < p.d / 8;
+        bool ok = true;
+#pragma unroll 1
+        for (int t = 0, c = 0; ok; ++t) {
+            const Meta &meta = sm.meta[t % kMetas];
+            if (!wait(sm.meta_full[t % kMetas], t / kMetas & 1)) break;
+            const int n = meta.n;
+            if (n < 0) break;
+            const int stage = c % kStages, rows16 = (n + 15) & ~15;
+#pragma unroll 1
+            for (int kv = 0; kv < 2 && n > 0; ++kv) {
+                const uint64_t &full = kv ? sm.v_full[stage] : sm.k_full[stage], &empty = kv ? sm.v_empty[stage] : sm.k_empty[stage];
+                if (c >= kStages && !(ok = wait(empty, (c / kStages - 1) & 1))) break;
+                const uint32_t tile = smem_u32(kv ? sm.v[stage] : sm.k[stage]);
+                const char *from = (const char *)(kv ? p.cache.v : p.cache.k) + chunk * 16;
+#pragma unroll 4
+                for (int row = first; row < rows16; row += kCopyWarps * kRowsOfCopy)
+                    if (copies) cp_async16_or_zero(S::place(tile, row, chunk), from + (size_t)meta.at[row] * 16, row < n);
+                __syncwarp();
+                cp_async_arrive(bar(full));
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(full));
+            }
+            c += n > 0;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(sm.meta_empty[t % kMetas]));
+        }
     } else {
         // ------------------------------------------------------------------ the products
-        // S = Q K^T of a tile as soon as its keys are there and one of the two S is free; O += P V as soon as P is.
+        // S = Q K^T of a tile as soon as its keys are there and the team's last P V is done; O += P V as soon as P is there.
         const bool leader = elect_one();
-        int t = 0, parts = 0;          // tile that comes next
-        int cs = 0, cp = 0;            // tiles whose S, and whose P V, have been issued
-        int n_of[2];                   // keys of a tile by the S that it has
+        int t = 0, parts = 0;     // tile that comes next
+        int cs = 0, cp = 0;       // tiles whose S, and whose P V, have been issued
+        int n_even = 0, n_odd = 0, n = 0, first = 0, last = 0;  // keys of the teams' tiles; the tile that comes next
         bool known = false, end = false;
-        Meta *meta = sm.meta;
-        int n = 0;
         uint32_t idle = 0;
         const auto is = [&](const uint64_t &b, uint32_t parity) { return mbar_test_wait(smem_u32(&b), parity); };
 #pragma unroll 1
@@ -1028,69 +1050,63 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
             bool moved = false;
             if (!end && !known && is(sm.meta_full[t % kMetas], t / kMetas & 1)) {
                 known = moved = true;
-                meta = &sm.meta[t % kMetas];
-                n = meta->n;
-                if (n < 0) end = true;
+                const Meta &meta = sm.meta[t % kMetas];
+                n = meta.n, first = meta.first, last = meta.last;
+                end = n < 0;
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(sm.meta_empty[t % kMetas]));
             }
-            if (known && !end) {
-                const int qb = meta->q, stage = cs % kStages, sb = cs & 1;
-                const bool go = n == 0 || (cs - cp < 2 && is(sm.k_full[stage], cs / kStages & 1) && (!meta->first || is(sm.q_full[qb], parts / 2 & 1)) &&
-                                           (cs < 2 || is(sm.s_free[sb], (cs / 2 - 1) & 1)));
-                if (go) {
-                    if (n > 0) {
-                        fence_proxy_async();  // the copies of 16 bytes come through the generic proxy
-                        tc_fence_after();
-                        const uint32_t idesc = idesc_bf16(kTcRows, (n + 15) & ~15, 0, 0), tS = tmem + kTmemS + sb * kTcKeys;
-                        const uint32_t q = smem_desc_lo(smem_u32(sm.q[qb])), k = smem_desc_lo(smem_u32(sm.k[stage]));
-                        if (leader) {
-                            mma_ss_lean<0>(tS, q, k, idesc);
+            const int stage = cs % kStages, team = cs & 1;
+            if (known && !end && (n == 0 || (is(sm.k_full[stage], cs / kStages & 1) && (!first || is(sm.q_full[parts & 1], parts / 2 & 1)) &&
+                                             (cs < 2 || is(sm.pv_done[team], (cs / 2 - 1) & 1))))) {
+                if (n > 0) {
+                    fence_proxy_async();  // the copies of 16 bytes come through the generic proxy
+                    tc_fence_after();
+                    const uint32_t idesc = idesc_bf16(kTcRows, (n + 15) & ~15, 0, 0), tS = tmem + kTmemS + team * kTcKeys;
+                    const uint32_t q = smem_desc_lo(smem_u32(sm.q[parts & 1])), k = smem_desc_lo(smem_u32(sm.k[stage]));
+                    if (leader) {
+                        mma_ss_lean<0>(tS, q, k, idesc);
 #pragma unroll
-                            for (int i = 1; i < DP / 16; ++i) {
-                                const uint32_t off = i / 4 * (S::kHalf >> 4) + i % 4 * 2;
-                                mma_ss_lean<1>(tS, q + off, k + off, idesc);
-                            }
-                            mma_commit(bar(sm.s_full[sb]));
-                            mma_commit(bar(sm.k_empty[stage]));
+                        for (int i = 1; i < DP / 16; ++i) {
+                            const uint32_t off = i / 4 * (S::kHalf >> 4) + i % 4 * 2;
+                            mma_ss_lean<1>(tS, q + off, k + off, idesc);
                         }
-                        n_of[sb] = n;
-                        ++cs;
+                        mma_commit(bar(sm.s_full[team]));
+                        mma_commit(bar(sm.k_empty[stage]));
                     }
-                    if (meta->last) {
-                        if (leader) mma_commit(bar(sm.q_empty[qb]));
-                        ++parts;
-                    }
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(bar(sm.meta_empty[t % kMetas]));
-                    ++t;
-                    known = false;
-                    moved = true;
+                    (team ? n_odd : n_even) = n;
+                    ++cs;
                 }
+                if (last) {
+                    if (leader) mma_commit(bar(sm.q_empty[parts & 1]));
+                    ++parts;
+                }
+                __syncwarp();
+                ++t;
+                known = false;
+                moved = true;
             }
-            if (cp < cs && is(sm.p_full, cp & 1)) {
+            if (cp < cs && is(sm.p_full[cp & 1], cp / 2 & 1) && is(sm.v_full[cp % kStages], cp / kStages & 1)) {
                 tc_fence_after();
                 fence_proxy_async();
-                const int stage = cp % kStages, steps = (((cp & 1) ? n_of[1] : n_of[0]) + 15) / 16;
-                const uint32_t idesc = idesc_bf16(kTcRows, 64, 0, 1), v = smem_desc_lo(smem_u32(sm.v[stage]));
-                moved = true;
-                if (is(sm.v_full[stage], cp / kStages & 1)) {
-                    fence_proxy_async();
-                    if (leader) {
+                const int from = cp % kStages, steps = ((cp & 1 ? n_odd : n_even) + 15) / 16;
+                const uint32_t idesc = idesc_bf16(kTcRows, 64, 0, 1), v = smem_desc_lo(smem_u32(sm.v[from]));
+                const uint32_t tO = tmem + kTmemO + (cp & 1) * 128, tP = tmem + kTmemS + (cp & 1) * kTcKeys;
+                if (leader) {
 #pragma unroll 1
-                        for (int ks = 0; ks < steps; ++ks)
+                    for (int ks = 0; ks < steps; ++ks)
 #pragma unroll
-                            for (int h = 0; h < kHalves; ++h) {
-                                const uint32_t b = v + ks * (16 * 128 >> 4) + h * (S::kHalf >> 4);
-                                mma_ts_lean<1>(tmem + kTmemO + 64 * h, tmem + kTmemHi + 8 * ks, b, idesc);
-                                mma_ts_lean<1>(tmem + kTmemO + 64 * h, tmem + kTmemLo + 8 * ks, b, idesc);
-                            }
-                        mma_commit(bar(sm.pv_done));
-                        mma_commit(bar(sm.v_empty[stage]));
-                    }
-                    __syncwarp();
-                    ++cp;
-                } else {
-                    moved = false;
+                        for (int h = 0; h < kHalves; ++h) {
+                            const uint32_t b = v + ks * (16 * 128 >> 4) + h * (S::kHalf >> 4);
+                            mma_ts_lean<1>(tO + 64 * h, tP + 16 * ks, b, idesc);
+                            mma_ts_lean<1>(tO + 64 * h, tP + 16 * ks + 8, b, idesc);
+                        }
+                    mma_commit(bar(sm.pv_done[cp & 1]));
+                    mma_commit(bar(sm.v_empty[from]));
                 }
+                __syncwarp();
+                ++cp;
+                moved = true;
             }
             if (moved) {
                 idle = 0;
@@ -1121,7 +1137,6 @@ __global__ void __launch_bounds__(32 * kJoinWarps) shared_join_kernel(const __gr
     __shared__ float4 s_sum[kJoinWarps][32];
     __shared__ float2 s_stat[kJoinWarps][32];
     ptx::launch_dependents();
-    ptx::wait_prior_grid();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int per_kv = (p.B * p.group + kJoinRows - 1) / kJoinRows, kv = blockIdx.x / per_kv;
     const int at = (blockIdx.x - kv * per_kv) * kJoinRows + lane % kJoinRows, c4 = blockIdx.y * 4 + lane / kJoinRows;
@@ -1136,8 +1151,10 @@ __global__ void __launch_bounds__(32 * kJoinWarps) shared_join_kernel(const __gr
     int parts[2] = {0, 0};
     const size_t out = (size_t)b * p.heads + kv * p.group + g;
     bool direct = !exists;
+    // (the batch is looked at ahead of the wait: the kernel in front of this one has waited for whoever wrote it before it let this one start)
+    const Entry e = entry_of(p, min(b, p.B - 1), &bad);
+    ptx::wait_prior_grid();
     if (exists) {
-        const Entry e = entry_of(p, b, &bad);
 #pragma unroll
         for (int seg = 0; seg < 2; ++seg) {
             if (seg == 0 ? e.count == 0 : segment_of<RT>(p, e, b, 1).units == 0) continue;
@@ -1289,6 +1306,11 @@ int mate_attn_decode_shared(const mate_cache_t *cache, int layer, const void *Q,
     p.whole_stats = reinterpret_cast<float2 *>(ws + w.stats);
     p.whole = reinterpret_cast<float *>(ws + w.whole);
     p.parts = reinterpret_cast<float *>(ws + w.parts);
+    if (cache->dtype == MATE_BF16) {
+        // a score of -inf stays one whatever it is multiplied by: a factor above 0, so small for a scale of 0 that every weight is 1
+        p.flip = p.scale_log2 < 0.f;
+        p.scale_log2 = std::fmax(std::fabs(p.scale_log2), 0x1p-126f);
+    }
     cudaStream_t st = (cudaStream_t)stream;
     const int blocks = n_blocks(cache), device = cache->device;
     if (cache->dtype == MATE_F32) return cache->d <= 64 ? launch<float, 64>(p, device, blocks, st) : launch<float, 128>(p, device, blocks, st);
