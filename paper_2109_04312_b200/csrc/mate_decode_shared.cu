@@ -13,17 +13,20 @@
 // Tokens are looked through 128 at a time by their ids; those that no row of the tile attends are left out before anything of them is read.
 #include <cuda_bf16.h>
 
+#include <algorithm>
 #include <cmath>
 #include <type_traits>
 
 #include "mate_cache.h"
 #include "sm100_ptx.cuh"
+#include "tc_tiles.cuh"
 
 namespace mate {
 namespace {
 
-constexpr int kUnit = 128;    // tokens of a unit of work: what is looked through in one go
-constexpr int kOver = 1;      // units that an item costs besides its tokens
+constexpr int kUnit = 32;     // tokens of a unit of work: what a warp looks through in one go
+constexpr int kOver = 4;      // units that an item costs besides its tokens
+constexpr int kMaxBatch = 4096;
 constexpr int kMaxHeads = 1024;
 constexpr int kNever = INT32_MIN;  // an id that no token has
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -38,22 +41,26 @@ struct SharedParams {
     const void *Q;
     int64_t q_batch, q_head;
     int B, heads, kv_heads, group, d, max_len;
-    int own_tiles;  // tiles of rows of an entry's own segment
+    int pack, own_tiles;  // entries whose own tokens make an item (their rows fill a tile), or tiles of the rows of one
     const int32_t *seqs, *row_ids, *col_ids, *groups;
     float scale_log2;  // scale / ln 2: weights are powers of two
     int flip;          // tensor-core kernel: the scale above is positive, and the queries change their sign
     void *O;
     float *LSE;
     unsigned page16, head16, slot16;  // strides in 16 bytes; no place is beyond 2^32 of them
-    unsigned page_mul, page_shift;    // x / page_size = (umulhi(x, page_mul) + x) >> page_shift for x < 2^31
-    Joint *joints;                    // [2][kv_heads][B own_tiles]: shared segments, own ones
-    float2 *whole_stats;              // [2][B heads]  m and sum P of rows that one block has done a segment of
+    // x / page_size and x / group by multiplication: (umulhi(x, mul) + x) >> shift for x < 2^31
+    unsigned page_mul, page_shift, group_mul, group_shift;
+    Joint *joints;                    // [2][kv_heads][B own_tiles]: shared tokens, by the first entry of the tile's group, and own ones
+    float2 *whole_stats;              // [2][B heads]  m and sum P of rows whose item one block has done
     float *whole;                     // [2][B heads][d]
     float *parts;                     // [blocks][2]: values in groups of four by row, then the rows' m and sum P
     uint32_t views[kMaxHeads / 16];   // two bits a head
 };
 __device__ __forceinline__ int page_index(const SharedParams &p, int token) {
     return (int)((__umulhi((unsigned)token, p.page_mul) + (unsigned)token) >> p.page_shift);
+}
+__device__ __forceinline__ int by_group(const SharedParams &p, int row) {
+    return (int)((__umulhi((unsigned)row, p.group_mul) + (unsigned)row) >> p.group_shift);
 }
 __device__ __forceinline__ int view_at(const SharedParams &p, int h) { return p.views[h >> 4] >> 2 * (h & 15) & 3; }
 __host__ __device__ constexpr int64_t part_floats(int rows, int d) { return (int64_t)rows * (d + 2); }
@@ -68,10 +75,13 @@ struct Entry {
     int first, shared;
     int counts;      // the shared tokens are its own too
     int q_row, q_col, prefix;
+    int bad;
 };
+// (called, not put in line: what a block runs through once misses the instruction cache, which holds 32 KB for all of its roles)
 // What does not fit together on the device leaves an entry without a group: the rows of one group are the same in all of its entries.  (Two
 // rounds of loads, the second one's indexes brought into range instead of looked at first.)
-__device__ __forceinline__ Entry entry_of(const SharedParams &p, int b, bool *bad) {
+__device__ __noinline__ void entry_of(const SharedParams &p, int b, Entry *to) {
+    bool is_bad = false, *bad = &is_bad;
     const int s = p.seqs ? p.seqs[b] : b, q_row = p.row_ids[b], q_col = p.col_ids[b];
     const int first = p.groups[b], count = p.groups[p.B + b], shared = p.groups[2 * p.B + b];
     const int at = min(max(s, 0), p.cache.seqs - 1), f = min(max(first, 0), b);
@@ -92,49 +102,56 @@ __device__ __forceinline__ Entry entry_of(const SharedParams &p, int b, bool *ba
     e.counts = has && !padding;
     e.own0 = has ? shared : 0;
     e.own1 = padding ? e.own0 : e.len;
-    return e;
+    e.bad = is_bad;
+    *to = e;
 }
-// Units of an item of tokens; the first kOver stand for what an item costs whatever its length (none of its tokens belong to them).
-__host__ __device__ __forceinline__ int units_of(int tokens) { return kOver + (tokens + kUnit - 1) / kUnit; }
+// Units of tokens.  The first kOver units of an item stand for what it costs whatever its length: none of its tokens belong to them.
+__host__ __device__ __forceinline__ int units_of(int tokens) { return (tokens + kUnit - 1) / kUnit; }
 __device__ __forceinline__ unsigned share(unsigned U, unsigned C, unsigned i) { return U / C * i + U % C * i / C; }
-
-// The segments of an entry: [0] the shared tokens of the group that it is the first of, [1] its own.
-struct Segment {
-    int items, units;  // units of an item; 0: there is nothing to do
-};
+// Items of the shared tokens of the group that entry b is the first of: kv heads and tiles of rows.
+__device__ __forceinline__ bool leads(const Entry &e, int b) { return e.count > 0 && e.first == b; }
 template <int RT>
-__device__ __forceinline__ Segment segment_of(const SharedParams &p, const Entry &e, int b, int seg) {
-    if (seg == 0) {
-        const bool leads = e.count > 0 && e.first == b;
-        return {leads ? p.kv_heads * (int)(((int64_t)e.count * p.group + RT - 1) / RT) : 0, leads ? units_of(e.shared) : 0};
-    }
-    // (an entry without a token and without a group has a result too)
-    return {p.kv_heads * p.own_tiles, e.own1 > e.own0 ? units_of(e.own1 - e.own0) : e.count > 0 ? 0 : 1};
+__device__ __forceinline__ int group_tiles(const SharedParams &p, const Entry &e) {
+    return (e.count * p.group + RT - 1) / RT;
 }
-// (called, not put in line three times: what a block runs through once misses the instruction cache)
-template <int RT>
-__device__ __noinline__ unsigned entry_units(const SharedParams &p, int b) {
-    bool bad = false;
-    const Entry e = entry_of(p, b, &bad);
-    const Segment x = segment_of<RT>(p, e, b, 0), y = segment_of<RT>(p, e, b, 1);
-    if (bad && blockIdx.x == 0) atomicOr(p.cache.status, kCacheBad);
-    return (unsigned)x.items * x.units + (unsigned)y.items * y.units;
-}
+// Units of an item of own tokens.  (Without any it has one: its rows have a result too.)
+__device__ __forceinline__ int own_units(int tokens_units) { return tokens_units > 0 ? kOver + tokens_units : 1; }
 
 struct Start {
-    unsigned total, before;  // units of the batch; of the entries in front of `entry`
+    unsigned total, before;  // units of all; of the batches of `pack` entries in front of `batch`
     unsigned blocks;         // that get any: no more than there are units
-    int entry;
+    int batch;
 };
-// All threads call it: the entry that the block's first unit belongs to.
+// All threads call it: the batch that the block's first unit belongs to.  `cost`: [B] in shared memory, free afterwards.
 template <int RT, int NT>
-__device__ Start find_start(const SharedParams &p) {
+__device__ Start find_start(const SharedParams &p, uint2 *cost) {
     __shared__ unsigned s_sum[NT / 32];
     __shared__ Start s_start;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int per = (p.B + NT - 1) / NT, b0 = min(p.B, tid * per), b1 = min(p.B, b0 + per);
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, batches = (p.B + p.pack - 1) / p.pack;
+#pragma unroll 1
+    for (int b = tid; b < p.B; b += NT) {
+        Entry e;
+        entry_of(p, b, &e);
+        cost[b] = make_uint2(units_of(e.own1 - e.own0), leads(e, b) ? p.kv_heads * group_tiles<RT>(p, e) * (kOver + units_of(e.shared)) : 0);
+        if (e.bad && blockIdx.x == 0) atomicOr(p.cache.status, kCacheBad);
+    }
+    if (tid == 0) s_start = {0, 0, 0, 0};
+    __syncthreads();
+    // a warp to each batch; its cost replaces that of its first entry
+#pragma unroll 1
+    for (int i = warp; i < batches; i += NT / 32) {
+        unsigned own = 0, shared = 0;
+#pragma unroll 1
+        for (int b = i * p.pack + lane; b < min(p.B, (i + 1) * p.pack); b += 32) own += cost[b].x, shared += cost[b].y;
+        own = __reduce_add_sync(~0u, own), shared = __reduce_add_sync(~0u, shared);
+        __syncwarp();
+        if (lane == 0) cost[i * p.pack].x = shared + (unsigned)(p.kv_heads * p.own_tiles) * own_units((int)own);
+    }
+    __syncthreads();
+    const int per = (batches + NT - 1) / NT, i0 = min(batches, tid * per), i1 = min(batches, i0 + per);
     unsigned own = 0;
-    for (int b = b0; b < b1; ++b) own += entry_units<RT>(p, b);
+#pragma unroll 1
+    for (int i = i0; i < i1; ++i) own += cost[i * p.pack].x;
     unsigned sum = own;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -142,10 +159,9 @@ __device__ Start find_start(const SharedParams &p) {
         if (lane >= o) sum += y;
     }
     if (lane == 31) s_sum[warp] = sum;
-    if (tid == 0) s_start = {0, 0, 0, 0};
     __syncthreads();
     unsigned total = 0, before = sum - own;
-#pragma unroll
+#pragma unroll 1
     for (int w = 0; w < NT / 32; ++w) {
         if (w < warp) before += s_sum[w];
         total += s_sum[w];
@@ -154,13 +170,10 @@ __device__ Start find_start(const SharedParams &p) {
     if (blockIdx.x < blocks) {
         const unsigned at = share(total, blocks, blockIdx.x);
         if (at >= before && at < before + own) {
-            int b = b0;
-            for (; b < b1 - 1; ++b) {
-                const unsigned n = entry_units<RT>(p, b);
-                if (at < before + n) break;
-                before += n;
-            }
-            s_start = {total, before, blocks, b};
+            int i = i0;
+#pragma unroll 1
+            for (; i < i1 - 1 && at >= before + cost[i * p.pack].x; ++i) before += cost[i * p.pack].x;
+            s_start = {total, before, blocks, i};
         }
     }
     __syncthreads();
@@ -169,20 +182,27 @@ __device__ Start find_start(const SharedParams &p) {
 
 // A part of an item: units [u0, u1) of them.
 struct Part {
-    int b, seg, kv, tile;
+    int b, seg, kv, tile;  // first entry; shared tokens (0) or own ones (1); tile of rows
     int u0, u1, units;
-    int t0, t1;      // its tokens
     int n_rows;
-    int grouped;     // the entry is in a group: its rows' results have to be joined
-    int s;           // whose pages are read; -1: nobody's
 };
 enum { kAll, kBegins, kGoesOn };
 __device__ __forceinline__ int part_state(const Part &part) { return part.u0 > 0 ? kGoesOn : part.u1 == part.units ? kAll : kBegins; }
+// Of a row of the tile: its entry, counted from the part's first, and its place among all rows of the batch.
+template <int RT>
+__device__ __forceinline__ int member_of(const SharedParams &p, const Part &part, int r) {
+    return by_group(p, part.tile * RT + r);
+}
+template <int RT>
+__device__ __forceinline__ size_t row_of(const SharedParams &p, const Part &part, int r, int member) {
+    return (size_t)(part.b + member) * p.heads + part.kv * p.group + part.tile * RT + r - member * p.group;
+}
+// (tiles of a group of n entries: fewer than n own_tiles, so those of different groups have different places)
 __device__ __forceinline__ Joint *joint_of(const SharedParams &p, int seg, int kv, int b, int tile) {
     return p.joints + ((size_t)seg * p.kv_heads + kv) * p.B * p.own_tiles + (size_t)b * p.own_tiles + tile;
 }
 // Of the part that begins an item that goes on in the next blocks (it is the last one of its block's share).
-__device__ __forceinline__ Joint joint_from(const Part &part, const Start &start, int slot) {
+__device__ __noinline__ Joint joint_from(const Part &part, const Start &start, int slot) {
     const int64_t end = (int64_t)share(start.total, start.blocks, blockIdx.x + 1) - (part.u1 - part.u0) + part.units;
     return {slot, (int)blockIdx.x, (int)min((end * start.blocks - 1) / start.total, (int64_t)start.blocks - 1), 0};
 }
@@ -199,13 +219,14 @@ template <int RT>
 struct Rows {
     int want_row[RT], want_col[RT], below[RT];
 };
-// and as those who look for keys do: without repetitions of the row before.
+// and as those who look for keys do.
 template <int RT>
 struct Wishes {
     int least, most;  // of `below` over the rows that are there
-    int n;
+    int views;        // 1: some want a row, 2: a column
+    int n;            // of a group: without repetitions of the row before
     int2 want[RT];
-    __device__ void clear() { least = INT32_MAX, most = INT32_MIN, n = 0; }
+    __device__ void clear() { least = INT32_MAX, most = INT32_MIN, views = n = 0; }
 };
 // Keys, with what the rows go by.
 struct alignas(16) Key {
@@ -214,14 +235,24 @@ struct alignas(16) Key {
 };
 constexpr int kList = 256, kScouts = 128;
 
-// kScouts threads walk the parts of the block's share and look through their tokens, 128 at a time; the keys that count go onto a list.
-// The next ones' ids, and the pages of the ones behind them, are on their way meanwhile.  Barrier 1 is theirs.
+// kScouts threads walk the parts of the block's share and look through their tokens, four units at a time, a warp to each; the keys that
+// count go onto a list.  The next ones' ids, and the pages of the ones behind them, are on their way meanwhile.  Barrier 1 is theirs.
+//
+// Units of own tokens are numbered through over the entries of the batch, each entry beginning with a new one.
 template <int RT>
 struct ScoutSmem {
-    Entry entries[kScouts];  // of the batch, from `base` on
+    Entry entries[kScouts];  // of the batch
+    int before[kScouts + 1]; // units of own tokens in front of an entry's
+    unsigned leaders[4];     // a bit for each entry: it is the first of a group
     Wishes<RT> wishes[2];    // of the parts in turn
     Key list[kList];         // what look() writes is seen behind the next barrier
+    uint8_t owners[kList];   // entries of the batch
     int counts[2][4];
+};
+// Where the loads of a look stand.
+struct Asked {
+    int j, owner, page;
+    bool there;
 };
 template <int RT>
 struct Scout {
@@ -229,89 +260,145 @@ struct Scout {
     ScoutSmem<RT> &sm;
     int tid;
     // the walk: next item of the share
-    int b, seg, item, u, left;  // left: units of the share
-    int base, parts;
+    int batch, entry, item, u, left;  // entry: that leads (of the batch), kScouts: own tokens; left: units of the share
+    int held, parts;                  // batch that is in shared memory; parts so far
     // the looks at the present part
-    int s, end, next, pending, list_at, looks;
-    unsigned head_at, at;
-    int row, col, page;
+    int seg, next, end, pending, list_at, looks;  // next, end: units
+    unsigned head_at;
+    Asked asked;
+    unsigned at;
+    int j, owner, row, col;
     bool there, bad;
 
     __device__ static void sync() { asm volatile("barrier.cta.sync 1, 128;" ::: "memory"); }
-    __device__ void window(int from, int to) {  // entries from .. to (kScouts of them at most) are held
-        if (from >= base && to < base + kScouts) return;
+    __device__ int entries() const { return min(p.pack, p.B - batch * p.pack); }
+    __device__ void hold() {
+        held = batch;
         sync();
-        bool unused = false;
-        sm.entries[tid] = entry_of(p, min(from + tid, p.B - 1), &unused);
-        base = from;
+        int units = 0;
+        bool first = false;
+        if (tid < entries()) {
+            const int b = batch * p.pack + tid;
+            entry_of(p, b, sm.entries + tid);
+            const Entry &e = sm.entries[tid];
+            units = units_of(e.own1 - e.own0), first = leads(e, b);
+        }
+        int sum = units;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int y = __shfl_up_sync(~0u, sum, o);
+            if ((tid & 31) >= o) sum += y;
+        }
+        const unsigned those = __ballot_sync(~0u, first);
+        if ((tid & 31) == 31) sm.counts[0][tid >> 5] = sum, sm.leaders[tid >> 5] = those;
+        sync();
+        for (int w = 0; w < tid >> 5; ++w) sum += sm.counts[0][w];
+        sm.before[tid + 1] = sum;
+        if (tid == 0) sm.before[0] = 0;
         sync();
     }
+    // The first entry from `entry` on that leads a group, kScouts if there is none.
+    __device__ int leader_from(int from) const {
+        for (int w = from >> 5; w < 4; ++w) {
+            const unsigned those = sm.leaders[w] & (w == from >> 5 ? ~0u << (from & 31) : ~0u);
+            if (those) return 32 * w + __ffs(those) - 1;
+        }
+        return kScouts;
+    }
+    __device__ int items() const { return p.kv_heads * (entry < kScouts ? group_tiles<RT>(p, sm.entries[entry]) : p.own_tiles); }
+    __device__ int units() const { return entry < kScouts ? kOver + units_of(sm.entries[entry].shared) : own_units(sm.before[kScouts]); }
     __device__ void start(const Start &from) {
         const unsigned begin = share(from.total, from.blocks, blockIdx.x);
         unsigned in = begin - from.before;
-        b = from.entry, seg = 0, parts = 0, bad = false, looks = 0;
+        batch = from.batch, parts = 0, bad = false, looks = 0;
         left = (int)(share(from.total, from.blocks, blockIdx.x + 1) - begin);
-        base = -2 * kScouts;
         if (tid == 0) sm.wishes[0].clear();
-        window(b, b);
-        Segment x = segment_of<RT>(p, sm.entries[0], b, 0);
-        const unsigned shared = (unsigned)x.items * x.units;
-        if (in >= shared) in -= shared, seg = 1, x = segment_of<RT>(p, sm.entries[0], b, 1);
-        item = (int)(in / max(1, x.units));
-        u = (int)(in - (unsigned)item * x.units);
+        hold();
+        entry = leader_from(0);
+#pragma unroll 1
+        while (entry < kScouts && in >= (unsigned)items() * units()) in -= (unsigned)items() * units(), entry = leader_from(entry + 1);
+        item = (int)(in / (unsigned)units());
+        u = (int)(in - (unsigned)item * units());
         if (u <= kOver) left += u, u = 0;
     }
     // The next part of the share.  (It comes to an end whatever it finds: every part takes a unit off the share.)
     __device__ bool next_part(Part &part) {
-        for (; left > 0 && b < p.B; seg = 0, item = 0, u = 0, ++b) {
-            window(b, b);
-            const Entry &e = sm.entries[b - base];
-            for (; seg < 2; ++seg, item = 0, u = 0) {
-                const Segment x = segment_of<RT>(p, e, b, seg);
-                if (x.units == 0 || item >= x.items) continue;
-                const int u1 = min(x.units, u + left);
-                if (u1 <= kOver && u1 < x.units) {  // it ends among the units that stand for the item: the next block takes it
-                    left = 0;
-                    return false;
-                }
-                const int tiles = seg == 0 ? x.items / p.kv_heads : p.own_tiles, kv = item / tiles, tile = item - kv * tiles;
-                const int rows = (seg == 0 ? e.count : 1) * p.group, begin = seg == 0 ? 0 : e.own0, stop = seg == 0 ? min(e.shared, e.len) : e.own1;
-                part = {b, seg, kv, tile, u, u1, x.units, begin + max(0, u - kOver) * kUnit, min(stop, begin + max(0, u1 - kOver) * kUnit),
-                        min(RT, rows - tile * RT), e.count > 0, e.s};
+#pragma unroll 1
+        while (left > 0 && batch * p.pack < p.B) {
+            if (held != batch) {
+                hold();
+                entry = leader_from(0);
+            }
+            if (item < items()) {
+                const int n = units(), u1 = min(n, u + left);
+                if (u1 <= kOver && u1 < n) break;  // it ends among the units that stand for the item: the next block takes it
+                const int tiles = entry < kScouts ? group_tiles<RT>(p, sm.entries[entry]) : p.own_tiles, kv = item / tiles, tile = item - kv * tiles;
+                const int rows = (entry < kScouts ? sm.entries[entry].count : entries()) * p.group;
+                part = {batch * p.pack + (entry < kScouts ? entry : 0), entry < kScouts ? 0 : 1, kv, tile, u, u1, n, min(RT, rows - tile * RT)};
                 left -= max(1, u1 - u);
                 u = 0;
                 ++item;
                 return true;
             }
+            item = 0;
+            if (entry == kScouts)
+                ++batch;
+            else
+                entry = leader_from(entry + 1);
         }
+        left = 0;
         return false;
     }
-    __device__ void ask_page(int j) { page = j < end ? p.cache.table[(size_t)s * p.cache.width + page_index(p, j)] : -1; }
-    __device__ void ask_ids() {  // of the thread's token of `next`, whose page has come
-        const int j = next + tid;
-        there = j < end && in_range(page, p.cache.pages);
-        if (j < end && !there) bad = true;
-        if (!there) return;
-        const int slot = j - page_index(p, j) * p.cache.page_size, id = page * p.cache.page_size + slot;
-        row = p.cache.row_ids[id], col = p.cache.col_ids[id];
-        at = (unsigned)page * p.page16 + (unsigned)slot * p.slot16 + head_at;
+    // Who the warp's 32 tokens of unit `unit` belong to, and their pages.
+    __device__ void ask_page(int unit) {
+        asked = {0, 0, -1, false};
+        if (unit >= end) return;
+        const int lane = tid & 31;
+        int first = 0, stop, from = 0;
+        if (seg == 0) {
+            asked.owner = leader;
+            stop = min(sm.entries[leader].shared, sm.entries[leader].len);
+        } else {
+            int n = 0;  // entries that begin at the unit or in front of it
+#pragma unroll
+            for (int i = 0; i < kScouts / 32; ++i) n += sm.before[32 * i + lane] <= unit;
+            asked.owner = __reduce_add_sync(~0u, n) - 1;
+            // (of entries without tokens the last one that begins there is found: it is the one behind them)
+            const Entry &e = sm.entries[asked.owner];
+            first = e.own0, stop = e.own1, from = sm.before[asked.owner];
+        }
+        const int s = sm.entries[asked.owner].s;
+        asked.j = first + (unit - from) * kUnit + lane;
+        asked.there = asked.j < stop && s >= 0;
+        if (asked.there) asked.page = p.cache.table[(size_t)s * p.cache.width + page_index(p, asked.j)];
     }
+    __device__ void ask_ids() {  // of the tokens whose page has been asked for
+        j = asked.j, owner = asked.owner;
+        there = asked.there && in_range(asked.page, p.cache.pages);
+        if (asked.there && !there) bad = true;
+        if (!there) return;
+        const int slot = j - page_index(p, j) * p.cache.page_size, id = asked.page * p.cache.page_size + slot;
+        row = p.cache.row_ids[id], col = p.cache.col_ids[id];
+        at = (unsigned)asked.page * p.page16 + (unsigned)slot * p.slot16 + head_at;
+    }
+    int leader;
     // Behind a barrier that the last look at the part before it is in front of.
     __device__ void begin(const Part &part, Rows<RT> &rows) {
-        s = part.s, next = part.t0, end = s < 0 ? part.t0 : part.t1;
+        seg = part.seg, leader = part.b - batch * p.pack;
+        next = max(0, part.u0 - kOver), end = max(0, part.u1 - kOver);
+        if (seg == 1) end = min(end, sm.before[kScouts]);
         head_at = (unsigned)part.kv * p.head16;
         pending = list_at = 0;
-        ask_page(next + tid);
-        const int at0 = part.tile * RT, first = part.seg == 0 ? at0 / p.group : 0;
-        window(part.b + first, part.b + (part.seg == 0 ? (at0 + part.n_rows - 1) / p.group : 0));
+        ask_page(next + (tid >> 5));
         Wishes<RT> &w = sm.wishes[parts & 1];
         ++parts;
         if (tid == 0) sm.wishes[parts & 1].clear();
         int want_row = kNever, want_col = kNever, below = -2;
         if (tid < part.n_rows) {
-            const int member = part.seg == 0 ? (at0 + tid) / p.group : 0, view = view_at(p, part.kv * p.group + at0 + tid - member * p.group);
-            const Entry &e = sm.entries[part.b + member - base];
-            if (part.seg == 0 ? e.counts && e.first == part.b && e.count > 0 : e.own1 > e.own0) {
+            const int member = member_of<RT>(p, part, tid), view = view_at(p, part.kv * p.group + part.tile * RT + tid - member * p.group);
+            Entry e;
+            entry_of(p, part.b + member, &e);
+            if (seg == 0 ? e.counts && e.first == part.b && e.count > 0 : e.own1 > e.own0) {
                 const bool text = e.q_row == MATE_ID_TEXT || e.q_col == MATE_ID_TEXT;
                 below = text ? INT32_MAX : e.prefix;
                 if (!text && view != MATE_VIEW_COL) want_row = e.q_row;
@@ -320,31 +407,43 @@ struct Scout {
         }
         if (tid < RT) rows.want_row[tid] = want_row, rows.want_col[tid] = want_col, rows.below[tid] = below;
         const int least = __reduce_min_sync(~0u, below < 0 ? INT32_MAX : below), most = __reduce_max_sync(~0u, below);
+        const int views = (__any_sync(~0u, want_row != kNever) ? 1 : 0) | (__any_sync(~0u, want_col != kNever) ? 2 : 0);
         const int row_before = __shfl_up_sync(~0u, want_row, 1), col_before = __shfl_up_sync(~0u, want_col, 1);
         const bool again = (tid & 31) > 0 && row_before == want_row && col_before == want_col;
-        if ((tid & 31) == 0 && most >= 0) atomicMin(&w.least, least), atomicMax(&w.most, most);
+        if ((tid & 31) == 0 && most >= 0) atomicMin(&w.least, least), atomicMax(&w.most, most), atomicOr(&w.views, views);
         if (!again && (want_row != kNever || want_col != kNever)) w.want[atomicAdd(&w.n, 1)] = make_int2(want_row, want_col);
+        __syncwarp();
         ask_ids();
-        ask_page(next + kUnit + tid);
+        ask_page(next + 4 + (tid >> 5));
         sync();
     }
     __device__ const Wishes<RT> &wishes() const { return sm.wishes[parts + 1 & 1]; }  // of the present part
     __device__ bool more() const { return next < end; }
     __device__ void look() {
         const Wishes<RT> &w = wishes();
-        Key key = {at, next + tid, row, col};
+        Key key = {at, j, row, col};
+        const int of = owner;
         bool is = there && row >= 0 && col >= 0;
         if (is) {
             if (row == MATE_ID_TEXT || col == MATE_ID_TEXT) key.place = -1;
-            is = key.place < w.most;
+            if (seg == 0) {
+                is = key.place < w.most;
 #pragma unroll 1
-            for (int i = 0; i < w.n && !is; ++i) is = row == w.want[i].x || col == w.want[i].y;
+                for (int i = 0; i < w.n && !is; ++i) is = row == w.want[i].x || col == w.want[i].y;
+            } else {
+                const Entry &e = sm.entries[of];
+                is = e.q_row == MATE_ID_TEXT || e.q_col == MATE_ID_TEXT || key.place < e.prefix || ((w.views & 1) && row == e.q_row) ||
+                     ((w.views & 2) && col == e.q_col);
+            }
         }
-        next += kUnit;
+        next += 4;
         if (next < end) {
+            __syncwarp();
             ask_ids();
-            ask_page(next + kUnit + tid);
+            __syncwarp();
+            ask_page(next + 4 + (tid >> 5));
         }
+        __syncwarp();
         const unsigned those = __ballot_sync(~0u, is);
         int *count = sm.counts[looks++ & 1];
         if ((tid & 31) == 0) count[tid >> 5] = __popc(those);
@@ -355,11 +454,18 @@ struct Scout {
             if (i < tid >> 5) before += count[i];
             all += count[i];
         }
-        if (is) sm.list[(list_at + pending + before + __popc(those & ((1u << (tid & 31)) - 1))) % kList] = key;
+        const unsigned to = (unsigned)(list_at + pending + before + __popc(those & ((1u << (tid & 31)) - 1))) % kList;
+        if (is) sm.list[to] = key, sm.owners[to] = (uint8_t)of;
         pending += all;
     }
-    __device__ Key key(int i) const { return sm.list[(list_at + i) % kList]; }
-    __device__ void taken(int n) { list_at = (list_at + n) % kList, pending -= n; }
+    __device__ Key key(int i) const { return sm.list[(unsigned)(list_at + i) % kList]; }
+    __device__ int owner_of_key(int i) const { return sm.owners[(unsigned)(list_at + i) % kList]; }
+    // Whether every row that a key is for attends it.
+    __device__ bool is_plain(const Key &key, int of) const {
+        const Entry &e = sm.entries[of];
+        return seg == 0 ? key.place < wishes().least : e.q_row == MATE_ID_TEXT || e.q_col == MATE_ID_TEXT || key.place < e.prefix;
+    }
+    __device__ void taken(int n) { list_at = (int)((unsigned)(list_at + n) % kList), pending -= n; }
 };
 
 __device__ __forceinline__ void put(float x, float *y) { *y = x; }
@@ -378,6 +484,7 @@ struct SimtSmem {
     ScoutSmem<kSimtRows> scout;
     Part part;
     Key keys[kSimtKeys];
+    int owners[kSimtKeys];
     int n, last, plain, done;
 };
 
@@ -390,7 +497,8 @@ __global__ void __launch_bounds__(kSimtThreads) shared_simt_kernel(const __grid_
     constexpr int kVec = 4, kCols = DP / 32, kR = kSimtRows / (kSimtThreads / 32);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, r0 = warp * kR;
     ptx::wait_prior_grid();
-    const Start start = find_start<kSimtRows, kSimtThreads>(p);
+    static_assert(sizeof(sm.q) + sizeof(sm.k) + sizeof(sm.v) + sizeof(sm.s) >= kMaxBatch * sizeof(uint2), "room for the entries' cost");
+    const Start start = find_start<kSimtRows, kSimtThreads>(p, reinterpret_cast<uint2 *>(smem_raw));
     if (blockIdx.x >= start.blocks) return;
     for (int i = tid; i < (int)(sizeof(SimtSmem<DP>) / 4); i += kSimtThreads) reinterpret_cast<uint32_t *>(smem_raw)[i] = 0;  // columns that nobody writes
     Scout<kSimtRows> scout = {p, sm.scout, tid};
@@ -409,8 +517,8 @@ __global__ void __launch_bounds__(kSimtThreads) shared_simt_kernel(const __grid_
         for (int i = tid; i < kSimtRows * (p.d / kVec); i += kSimtThreads) {
             const int r = i / (p.d / kVec), c = (i - r * (p.d / kVec)) * kVec;
             if (r >= part.n_rows) continue;
-            const int at = part.tile * kSimtRows + r, member = part.seg == 0 ? at / p.group : 0;
-            load16((const float *)p.Q + (part.b + member) * p.q_batch + (part.kv * p.group + at - member * p.group) * p.q_head + c, &sm.q[r][c]);
+            const int member = member_of<kSimtRows>(p, part, r), head = part.kv * p.group + part.tile * kSimtRows + r - member * p.group;
+            load16((const float *)p.Q + (part.b + member) * p.q_batch + head * p.q_head + c, &sm.q[r][c]);
         }
         float o[kR][kCols], m[kR], l[kR];
 #pragma unroll
@@ -426,8 +534,8 @@ __global__ void __launch_bounds__(kSimtThreads) shared_simt_kernel(const __grid_
                 const int n = min(scout.pending, kSimtKeys);
                 bool every = true;
                 if (tid < kSimtKeys) {
-                    if (tid < n) sm.keys[tid] = scout.key(tid);
-                    every = __all_sync(~0u, tid >= n || sm.keys[tid].place < scout.wishes().least);
+                    if (tid < n) sm.keys[tid] = scout.key(tid), sm.owners[tid] = scout.owner_of_key(tid);
+                    every = part.seg == 0 && __all_sync(~0u, tid >= n || scout.is_plain(sm.keys[tid], sm.owners[tid]));
                 }
                 if (tid == 0) sm.n = n, sm.last = scout.pending <= kSimtKeys && !scout.more(), sm.plain = every;
                 scout.taken(n);
@@ -471,10 +579,12 @@ __global__ void __launch_bounds__(kSimtThreads) shared_simt_kernel(const __grid_
                 __syncwarp();
                 // weights: a key of a lane
                 const Key key = sm.keys[lane];
+                const int of = sm.owners[lane];
                 uint32_t those[kR];
 #pragma unroll
                 for (int r = 0; r < kR; ++r) {
-                    const bool is = lane < n && attends(sm.rows.want_row[r0 + r], sm.rows.want_col[r0 + r], sm.rows.below[r0 + r], key.place, key.row, key.col);
+                    const bool is = lane < n && (part.seg == 0 || of == member_of<kSimtRows>(p, part, r0 + r)) &&
+                                    attends(sm.rows.want_row[r0 + r], sm.rows.want_col[r0 + r], sm.rows.below[r0 + r], key.place, key.row, key.col);
                     those[r] = __ballot_sync(~0u, is);
                     const float x = is ? sm.s[r0 + r][lane] : -INFINITY;
                     float top = fmaxf(x, m[r]);
@@ -524,31 +634,19 @@ __global__ void __launch_bounds__(kSimtThreads) shared_simt_kernel(const __grid_
             float sum = l[r];
 #pragma unroll
             for (int step = 16; step > 0; step >>= 1) sum += __shfl_xor_sync(~0u, sum, step);
-            const int row = r0 + r, at = part.tile * kSimtRows + row, member = part.seg == 0 ? at / p.group : 0;
+            const int row = r0 + r;
             if (row >= part.n_rows) break;
-            const size_t out = (size_t)(part.b + member) * p.heads + part.kv * p.group + at - member * p.group;
-            const size_t whole = (size_t)part.seg * p.B * p.heads + out;
+            const size_t whole = (size_t)part.seg * p.B * p.heads + row_of<kSimtRows>(p, part, row, member_of<kSimtRows>(p, part, row));
             for (int c = 0; c < kCols; ++c) {
                 const int e = lane * kCols + c;
                 if (e >= p.d) break;
                 const float x = sum == 0.f ? 0.f : o[r][c];  // (a row that attends nothing here: whatever the others attend)
-                if (state != kAll)
-                    to[(size_t)(e / 4 * kSimtRows + row) * 4 + e % 4] = x;
-                else if (part.grouped)
-                    p.whole[whole * p.d + e] = x;
-                else
-                    put(sum == 0.f ? 0.f : x / sum, (float *)p.O + out * p.d + e);
+                (state == kAll ? p.whole + whole * p.d : to)[state == kAll ? e : (e / 4 * kSimtRows + row) * 4 + e % 4] = x;
             }
-            if (lane > 0) continue;
-            if (state != kAll)
-                reinterpret_cast<float2 *>(to + (size_t)p.d * kSimtRows)[row] = make_float2(m[r], sum);
-            else if (part.grouped)
-                p.whole_stats[whole] = make_float2(m[r], sum);
-            else
-                p.LSE[out] = natural(m[r], sum);
+            if (lane == 0) (state == kAll ? p.whole_stats[whole] : reinterpret_cast<float2 *>(to + (size_t)p.d * kSimtRows)[row]) = make_float2(m[r], sum);
         }
         if (tid == 0 && state != kGoesOn) {
-            Joint *joint = joint_of(p, part.seg, part.kv, part.b, part.tile);
+            Joint *joint = joint_of(p, part.seg, part.kv, part.seg == 0 ? part.b : part.b / p.pack, part.tile);
             if (state == kAll)
                 joint->slot = -1;
             else
@@ -584,9 +682,20 @@ struct TcShape {
 };
 struct alignas(16) Meta {
     int n, first, last;  // keys; of the part.  n < 0: the share is done
-    uint32_t plain;      // 0x01010101: every row attends every key
-    int place[kTcKeys], row[kTcKeys], col[kTcKeys];
+    uint32_t plain;      // 0x01010101: every row attends every key that is for it
+    int ranged;          // keys lo[m] to hi[m] are for the rows of entry m, else all for all
+    uint8_t runs[4];     // of every 32 keys: blocks of TcMaps.run keys that lie one behind the other
+    alignas(16) int place[kTcKeys];  // (read four at a time)
+    alignas(16) int row[kTcKeys];
+    alignas(16) int col[kTcKeys];
     unsigned at[kTcKeys];
+    uint8_t lo[kTcRows], hi[kTcRows];
+};
+// Keys and values as matrices whose rows are a slot stride apart: a run of slots is a box, which comes in by one bulk tensor copy for every
+// 64 elements.
+struct TcMaps {
+    CUtensorMap k, v;
+    int run, run_log2;  // rows of a box, 8, 16 or 32; 0: every row is copied by itself
 };
 template <int DP>
 struct TcSmem {  // from a multiple of 1024 bytes on
@@ -619,6 +728,17 @@ __device__ __forceinline__ bool any_scout(bool x) {
     return r != 0;
 }
 
+// Every wait is bounded; the first one to run out raises the flag that ends all of them.
+__device__ __noinline__ bool wait_long(uint32_t bar, uint32_t parity, volatile int *abort) {
+#pragma unroll 1
+    for (uint32_t i = 0; i < ptx::kWaitLimit; ++i) {
+        if (ptx::mbar_try_wait(bar, parity)) return true;
+        if (*abort) return false;
+    }
+    *abort = 1;
+    return false;
+}
+
 // 32 scores of a row: those that do not count become -inf.
 __device__ __forceinline__ void mask_scores(uint32_t (&v)[32], const Meta &meta, int c0, int want_row, int want_col, int below) {
 #pragma unroll
@@ -639,24 +759,30 @@ __device__ __forceinline__ float top_score(const uint32_t (&v)[32], float top) {
         for (int j = 0; j < 4; ++j) t[j] = ptx::fmax3(t[j], __uint_as_float(v[e + 2 * j]), __uint_as_float(v[e + 2 * j + 1]));
     return fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
 }
-// Weights 2^(s scale - base) of 16 keys as pairs of bf16: rounded, and what the rounding left, rounded (their sum has 16 bits: an error of
+// Weights 2^(s scale - base) of 32 keys, 16 at a time, as pairs of bf16: rounded, and what the rounding left, rounded (their sum has 16 bits: an error of
 // 2^-17 of a weight, which the result's rounding to bf16, 2^-9, hides but for one value in some hundred).  The sums take all of them.
-__device__ __forceinline__ void weigh(const uint32_t *v, uint64_t scale2, uint64_t neg_base2, uint32_t (&hi_lo)[16], uint64_t (&sum)[2]) {
+__device__ __forceinline__ void weigh(uint32_t (&v)[32], uint64_t scale2, uint64_t neg_base2, uint64_t (&sum)[2]) {
 #pragma unroll
-    for (int e = 0; e < 16; e += 2) {
-        float x, y;
-        ptx::unpack_f32x2(ptx::fma_f32x2(ptx::pack_f32x2(v[e], v[e + 1]), scale2, neg_base2), x, y);
-        x = ptx::ex2(x), y = ptx::ex2(y);
-        const uint64_t xy = ptx::pack_f32x2(x, y);
-        sum[e >> 1 & 1] = ptx::add_f32x2(sum[e >> 1 & 1], xy);
-        const uint32_t h = ptx::cvt_bf16x2(x, y);
-        ptx::unpack_f32x2(ptx::sub_f32x2(xy, ptx::pack_f32x2(h << 16, h & 0xffff0000u)), x, y);
-        hi_lo[e >> 1] = h, hi_lo[8 + (e >> 1)] = ptx::cvt_bf16x2(x, y);
+    for (int i = 0; i < 32; i += 16) {
+        uint32_t lo[8];
+#pragma unroll
+        for (int e = 0; e < 16; e += 2) {
+            float x, y;
+            ptx::unpack_f32x2(ptx::fma_f32x2(ptx::pack_f32x2(v[i + e], v[i + e + 1]), scale2, neg_base2), x, y);
+            x = ptx::ex2(x), y = ptx::ex2(y);
+            const uint64_t xy = ptx::pack_f32x2(x, y);
+            sum[e >> 1 & 1] = ptx::add_f32x2(sum[e >> 1 & 1], xy);
+            const uint32_t h = ptx::cvt_bf16x2(x, y);
+            ptx::unpack_f32x2(ptx::sub_f32x2(xy, ptx::pack_f32x2(h << 16, h & 0xffff0000u)), x, y);
+            v[i + (e >> 1)] = h, lo[e >> 1] = ptx::cvt_bf16x2(x, y);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[i + 8 + e] = lo[e];
     }
 }
 
 template <int DP>
-__global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_constant__ SharedParams p) {
+__global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_constant__ SharedParams p, const __grid_constant__ TcMaps maps) {
     using namespace ptx;
     using S = TcShape<DP>;
     constexpr int kStages = S::kStages, kHalves = DP / 64;
@@ -666,48 +792,46 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
     const int tid = threadIdx.x, warp = __shfl_sync(~0u, tid >> 5, 0), lane = tid & 31;
     const auto bar = [](const uint64_t &b) { return smem_u32(&b); };
 
-    if (tid == 0) {
-        for (int i = 0; i < 2; ++i) {
-            mbar_init(bar(sm.q_full[i]), kLoadWarps);
-            mbar_init(bar(sm.q_empty[i]), kSoftmaxWarps + 1);
-            mbar_init(bar(sm.s_full[i]), 1), mbar_init(bar(sm.pv_done[i]), 1);
-            mbar_init(bar(sm.p_full[i]), kSoftmaxWarps / 2), mbar_init(bar(sm.team[i]), kSoftmaxWarps / 2);
-            sm.odd[i] = 0;
+    if (warp == 0) {  // (a lane to an index: one after the other they take a third of a microsecond)
+        if (lane < 2) {
+            mbar_init(bar(sm.q_full[lane]), kLoadWarps);
+            mbar_init(bar(sm.q_empty[lane]), kSoftmaxWarps + 1);
+            mbar_init(bar(sm.s_full[lane]), 1), mbar_init(bar(sm.pv_done[lane]), 1);
+            mbar_init(bar(sm.p_full[lane]), kSoftmaxWarps / 2), mbar_init(bar(sm.team[lane]), kSoftmaxWarps / 2);
+            sm.odd[lane] = 0;
         }
-        for (int i = 0; i < kStages; ++i) {
-            mbar_init(bar(sm.k_full[i]), kCopyWarps), mbar_init(bar(sm.v_full[i]), kCopyWarps);
-            mbar_init(bar(sm.k_empty[i]), 1), mbar_init(bar(sm.v_empty[i]), 1);
+        if (lane < kStages) {
+            mbar_init(bar(sm.k_full[lane]), kCopyWarps), mbar_init(bar(sm.v_full[lane]), kCopyWarps);
+            mbar_init(bar(sm.k_empty[lane]), 1), mbar_init(bar(sm.v_empty[lane]), 1);
         }
-        for (int i = 0; i < kMetas; ++i) mbar_init(bar(sm.meta_full[i]), kLoadWarps), mbar_init(bar(sm.meta_empty[i]), kSoftmaxWarps + kCopyWarps + 1);
-        mbar_init(bar(sm.both), kSoftmaxWarps), mbar_init(bar(sm.final_), 1);
-        sm.abort = 0;
+        if (lane < kMetas) mbar_init(bar(sm.meta_full[lane]), kLoadWarps), mbar_init(bar(sm.meta_empty[lane]), kSoftmaxWarps + kCopyWarps + 1);
+        if (lane == 0) {
+            mbar_init(bar(sm.both), kSoftmaxWarps), mbar_init(bar(sm.final_), 1);
+            sm.abort = 0;
+        }
         fence_mbar_init();
     }
+    if (warp == kCopyWarp0 && lane < 2) prefetch_tmap(lane ? &maps.v : &maps.k, maps.run);
     if (warp == kMmaWarp) {
         tmem_alloc(smem_u32(&sm.tmem), kTmemCols);
         tmem_relinquish();
     }
-    if (p.d < DP)  // columns that no copy writes
-        for (int i = tid; i < (2 + 2 * kStages) * S::kTile / 16; i += kTcThreads) reinterpret_cast<uint4 *>(sm.q)[i] = make_uint4(0, 0, 0, 0);
-    fence_proxy_async();
     tc_fence_before();
     wait_prior_grid();
     launch_dependents();  // (what is launched next waits for the end of this before it reads results)
-    const Start start = find_start<kTcRows, kTcThreads>(p);  // (its barriers: the set-up is seen by all)
+    static_assert(sizeof(sm.k) >= kMaxBatch * sizeof(uint2), "room for the entries' cost");
+    const Start start = find_start<kTcRows, kTcThreads>(p, reinterpret_cast<uint2 *>(sm.k));  // (its barriers: the set-up is seen by all)
     tc_fence_after();
+    if (p.d < DP && blockIdx.x < start.blocks) {  // columns that no copy writes
+#pragma unroll 1
+        for (int i = tid; i < (2 + 2 * kStages) * S::kTile / 16; i += kTcThreads) reinterpret_cast<uint4 *>(sm.q)[i] = make_uint4(0, 0, 0, 0);
+    }
+    fence_proxy_async();  // (what has been written where bulk copies will write)
+    __syncthreads();
     const uint32_t tmem = __shfl_sync(~0u, sm.tmem, 0);
 
-    // Every wait is bounded; the first one to run out raises the flag that ends all of them.
     volatile int *abort = &sm.abort;
-    const auto wait = [&](const uint64_t &b, uint32_t parity) -> bool {
-#pragma unroll 1
-        for (uint32_t i = 0; i < kWaitLimit; ++i) {
-            if (mbar_try_wait(smem_u32(&b), parity)) return true;
-            if (*abort) return false;
-        }
-        *abort = 1;
-        return false;
-    };
+    const auto wait = [&](const uint64_t &b, uint32_t parity) { return mbar_try_wait(smem_u32(&b), parity) || wait_long(smem_u32(&b), parity, &sm.abort); };
 
     if (blockIdx.x >= start.blocks) {
     } else if (warp < kSoftmaxWarps) {
@@ -721,7 +845,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
             if (lane == 0) mbar_arrive(bar(b));
             return wait(b, passed++ & 1);
         };
-        int want_row = 0, want_col = 0, below = 0, tiles = 0, own = 0;  // tiles of the part; the team's
+        int want_row = 0, want_col = 0, below = 0, member = 0, tiles = 0, own = 0;  // tiles of the part; the team's
         bool live = false;
         float m = -INFINITY;
         uint64_t sum[2] = {0, 0};
@@ -737,6 +861,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
                 const Rows<kTcRows> &rows = sm.rows[qb];
                 want_row = rows.want_row[r], want_col = rows.want_col[r], below = rows.below[r];
                 live = (warp & 3) * 32 < part.n_rows;
+                member = member_of<kTcRows>(p, part, r);
                 tiles = own = 0;
                 m = -INFINITY;
                 sum[0] = sum[1] = 0;
@@ -749,7 +874,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
                 tc_fence_after();
                 const int stage = c % kStages;
                 bool odd = false;
-                if (!plain) {  // a weight 0 does not undo a value that is not a number: is there one?
+                if (!plain || meta.ranged) {  // a weight 0 does not undo a value that is not a number: is there one?
                     if (!wait(sm.v_full[stage], c / kStages & 1)) break;
                     __nv_bfloat162 z = __floats2bfloat162_rn(0.f, 0.f);
                     const uint4 *v = reinterpret_cast<const uint4 *>(sm.v[stage]);
@@ -763,28 +888,25 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
                     if (!sync(sm.team[team], teams)) break;
                     odd = *(volatile int *)&sm.odd[team] == c + 1;
                 }
+                // the row's keys: none, where the row attends nothing
+                const int m_at = min(member, kTcRows - 1), lo = meta.ranged ? meta.lo[m_at] : 0, hi = below < -1 ? 0 : meta.ranged ? meta.hi[m_at] : n;
                 if (live) {
+                    const bool any = __any_sync(~0u, lo < hi);
+                    const int all_lo = __reduce_max_sync(~0u, lo), all_hi = __reduce_min_sync(~0u, hi);  // keys of all rows
                     float top = -INFINITY;
 #pragma unroll 1
-                    for (int c0 = 0; c0 < n; c0 += 32) {
+                    for (int c0 = 0; any && c0 < n; c0 += 32) {
                         uint32_t v[32];
                         tmem_ld32(tS + c0, v);
                         tc_wait_ld();
                         reg_fence(v);
-                        if (!plain || n < c0 + 32) {  // (behind the last key there is nobody's, which no row attends)
-                            if (!plain)
-                                mask_scores(v, meta, c0, want_row, want_col, below);
-                            else
+                        if (!plain || c0 < all_lo || c0 + 32 > all_hi) {
+                            const uint32_t on = (hi - c0 >= 32 ? ~0u : hi > c0 ? (1u << (hi - c0)) - 1 : 0u) & ~(lo - c0 >= 32 ? ~0u : lo > c0 ? (1u << (lo - c0)) - 1 : 0u);
 #pragma unroll
-                                for (int e = 0; e < 32; ++e)
-                                    if (e >= n - c0) v[e] = 0xff800000u;
-                            uint32_t half[16];
-#pragma unroll
-                            for (int i = 0; i < 2; ++i) {
-#pragma unroll
-                                for (int e = 0; e < 16; ++e) half[e] = v[16 * i + e];
-                                tmem_st16(tS + c0 + 16 * i, half);
-                            }
+                            for (int e = 0; e < 32; ++e)
+                                if (!(on >> e & 1)) v[e] = 0xff800000u;
+                            if (!plain) mask_scores(v, meta, c0, want_row, want_col, below);
+                            tmem_st32(tS + c0, v);
                             tc_wait_st();
                         }
                         top = top_score(v, top);
@@ -814,15 +936,14 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
                     const uint64_t neg2 = pack_f32x2(neg, neg);
 #pragma unroll 1
                     for (int c0 = 0; c0 < n; c0 += 32) {
-                        uint32_t v[32], hi_lo[16];
-                        tmem_ld32(tS + c0, v);
-                        tc_wait_ld();
-                        reg_fence(v);
-#pragma unroll
-                        for (int i = 0; i < 32; i += 16) {
-                            weigh(v + i, scale2, neg2, hi_lo, sum);
-                            tmem_st16(tS + c0 + i, hi_lo);
+                        uint32_t v[32] = {};
+                        if (any) {
+                            tmem_ld32(tS + c0, v);
+                            tc_wait_ld();
+                            reg_fence(v);
+                            weigh(v, scale2, neg2, sum);
                         }
+                        tmem_st32(tS + c0, v);
                     }
                     tc_wait_st();
                 }
@@ -833,7 +954,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
                     };
 #pragma unroll 1
                     for (int key = 0; key < n && live; ++key) {
-                        const bool counts = attends(want_row, want_col, below, meta.place[key], meta.row[key], meta.col[key]);
+                        const bool counts = key >= lo && key < hi && attends(want_row, want_col, below, meta.place[key], meta.row[key], meta.col[key]);
 #pragma unroll 1
                         for (int e = 0; e < DP; ++e) {
                             const float y = __bfloat162float(*at(key, e));
@@ -882,52 +1003,42 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
                     l = fmaf(x.y, f[0], y.y * f[1]);
                 }
                 tc_fence_after();
-                if (below < -1) l = 0.f, m = -INFINITY;  // (a row that attends nothing, whatever the others attend)
                 const int state = part_state(part), slot = parts == 0 ? 0 : 1;
-                const int at = part.tile * kTcRows + r, member = part.seg == 0 ? at / p.group : 0;
-                const size_t out = (size_t)(part.b + member) * p.heads + part.kv * p.group + at - member * p.group;
-                const size_t whole = (size_t)part.seg * p.B * p.heads + out;
+                const size_t whole = (size_t)part.seg * p.B * p.heads + row_of<kTcRows>(p, part, r, member);
                 float *to = p.parts + (size_t)(2 * blockIdx.x + slot) * part_floats(kTcRows, p.d);
                 if (live) {
                     const bool row = r < part.n_rows;
-                    if (state == kAll && !part.grouped) f[0] /= l, f[1] /= l;
                     const int col0 = joined ? team * (DP / 2) : 0, col1 = joined ? col0 + DP / 2 : DP;
+                    const int y_step = state == kAll ? 1 : kTcRows;
+                    float4 *y = state == kAll ? reinterpret_cast<float4 *>(p.whole + whole * p.d + col0) : reinterpret_cast<float4 *>(to) + col0 / 4 * kTcRows + r;
 #pragma unroll 1
-                    for (int col = col0; col < col1; col += 8) {
-                        uint32_t o[8], o2[8] = {};
-                        tmem_ld8(tmem + lanes + kTmemO + (joined ? 0 : team * 128) + col, o);
-                        if (joined) tmem_ld8(tmem + lanes + kTmemO + 128 + col, o2);
+                    for (int col = col0; col < col1; col += 16) {
+                        uint32_t o[16], o2[16] = {};
+                        tmem_ld16(tmem + lanes + kTmemO + (joined ? 0 : team * 128) + col, o);
+                        if (joined) tmem_ld16(tmem + lanes + kTmemO + 128 + col, o2);
                         tc_wait_ld();
                         reg_fence(o);
                         reg_fence(o2);
-                        if (!row || col >= p.d) continue;
-                        float x[8];
+                        if (!row) continue;
+                        float x[16];
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) {
+                        for (int e = 0; e < 16; ++e) {
                             x[e] = __uint_as_float(o[e]) * f[0];
                             if (joined) x[e] = fmaf(__uint_as_float(o2[e]), f[1], x[e]);
                             if (l == 0.f) x[e] = 0.f;
                         }
-                        if (state == kAll && !part.grouped) {
-                            *reinterpret_cast<uint4 *>((__nv_bfloat16 *)p.O + out * p.d + col) =
-                                make_uint4(cvt_bf16x2(x[0], x[1]), cvt_bf16x2(x[2], x[3]), cvt_bf16x2(x[4], x[5]), cvt_bf16x2(x[6], x[7]));
-                        } else {
-                            float4 *y = state == kAll ? reinterpret_cast<float4 *>(p.whole + whole * p.d + col) : reinterpret_cast<float4 *>(to) + col / 4 * kTcRows + r;
-                            y[0] = make_float4(x[0], x[1], x[2], x[3]);
-                            y[state == kAll ? 1 : kTcRows] = make_float4(x[4], x[5], x[6], x[7]);
+#pragma unroll
+                        for (int e = 0; e < 16; e += 8) {
+                            if (col + e >= p.d) break;
+                            y[0] = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]), y[y_step] = make_float4(x[e + 4], x[e + 5], x[e + 6], x[e + 7]);
+                            y += 2 * y_step;
                         }
                     }
-                    if (row && (!joined || team == 0)) {
-                        if (state != kAll)
-                            reinterpret_cast<float2 *>(to + (size_t)p.d * kTcRows)[r] = make_float2(m, l);
-                        else if (part.grouped)
-                            p.whole_stats[whole] = make_float2(m, l);
-                        else
-                            p.LSE[out] = natural(m, l);
-                    }
+                    if (row && (!joined || team == 0))
+                        (state == kAll ? p.whole_stats[whole] : reinterpret_cast<float2 *>(to + (size_t)p.d * kTcRows)[r]) = make_float2(m, l);
                 }
                 if (r == 0 && (!joined || team == 0) && state != kGoesOn) {
-                    Joint *joint = joint_of(p, part.seg, part.kv, part.b, part.tile);
+                    Joint *joint = joint_of(p, part.seg, part.kv, part.seg == 0 ? part.b : part.b / p.pack, part.tile);
                     if (state == kAll)
                         joint->slot = -1;
                     else
@@ -955,12 +1066,13 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
             if (parts >= 2) ok &= wait(sm.q_empty[qb], (parts / 2 - 1) & 1);
             if (any_scout(!ok)) break;
             const uint32_t q = smem_u32(sm.q[qb]);
-            const int chunk = lane % kPer;
-#pragma unroll 1
-            for (int i = 32 * lw + lane / kPer; i < min(32 * lw + 32, part.n_rows); i += kRowsOfCopy) {
-                const int at = part.tile * kTcRows + i, member = part.seg == 0 ? at / p.group : 0;
-                const __nv_bfloat16 *from = (const __nv_bfloat16 *)p.Q + (part.b + member) * p.q_batch + (part.kv * p.group + at - member * p.group) * p.q_head;
-                if (chunk < p.d / 8) cp_async16(S::place(q, i, chunk), from + chunk * 8);
+            const int chunk = lane % kPer, sub = lane / kPer, n_here = min(part.n_rows - 32 * lw, 32);  // the warp's rows
+            const int member = member_of<kTcRows>(p, part, lt), head = part.kv * p.group + part.tile * kTcRows + lt - member * p.group;
+            const int64_t mine = (part.b + member) * p.q_batch + head * p.q_head;  // where the thread's row is
+#pragma unroll 4
+            for (int i = 0; i < n_here; i += kRowsOfCopy) {
+                const int64_t from = __shfl_sync(~0u, mine, i + sub);
+                if (i + sub < n_here && chunk < p.d / 8) cp_async16(S::place(q, 32 * lw + i + sub, chunk), (const __nv_bfloat16 *)p.Q + from + chunk * 8);
             }
             __syncwarp();
             scout.begin(part, sm.rows[qb]);
@@ -968,8 +1080,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
             if (p.flip) {  // a negative scale: its sign goes to the queries
                 asm volatile("cp.async.wait_all;" ::: "memory");
 #pragma unroll 1
-                for (int i = 32 * lw + lane / kPer; i < min(32 * lw + 32, part.n_rows); i += kRowsOfCopy) {
-                    uint4 *x = reinterpret_cast<uint4 *>(sm.q[qb] + (S::place(q, i, chunk) - q));
+                for (int i = sub; i < n_here; i += kRowsOfCopy) {
+                    uint4 *x = reinterpret_cast<uint4 *>(sm.q[qb] + (S::place(q, 32 * lw + i, chunk) - q));
                     constexpr uint32_t kSigns = 0x80008000u;
                     *x = make_uint4(x->x ^ kSigns, x->y ^ kSigns, x->z ^ kSigns, x->w ^ kSigns);
                 }
@@ -981,18 +1093,35 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
             bool last = false;
 #pragma unroll 1
             for (bool first = true; !last; first = false, ++t) {
+#pragma unroll 1
                 while (scout.pending < kTcKeys && scout.more()) scout.look();
                 const int n = min(scout.pending, kTcKeys);
                 last = scout.pending <= kTcKeys && !scout.more();
                 if (t >= kMetas) ok &= wait(sm.meta_empty[t % kMetas], (t / kMetas - 1) & 1);
-                if (any_scout(!ok)) break;
                 Meta &meta = sm.meta[t % kMetas];
+                if (ok) meta.lo[lt] = meta.hi[lt] = 0;
+                if (any_scout(!ok)) break;
                 Key key = {0, INT32_MAX, kNever + 1, kNever + 1};  // nobody's
-                if (lt < n) key = scout.key(lt);
+                bool plain = true;
+                if (lt < n) {
+                    key = scout.key(lt);
+                    const int of = scout.owner_of_key(lt);
+                    plain = scout.is_plain(key, of);
+                    if (part.seg == 1) {
+                        if (lt == 0 || scout.owner_of_key(lt - 1) != of) meta.lo[of] = (uint8_t)lt;
+                        if (lt == n - 1 || scout.owner_of_key(lt + 1) != of) meta.hi[of] = (uint8_t)(lt + 1);
+                    }
+                }
                 meta.place[lt] = key.place, meta.row[lt] = key.row, meta.col[lt] = key.col, meta.at[lt] = key.at;
-                const bool plain = __all_sync(~0u, lt >= n || key.place < scout.wishes().least);
+                plain = __all_sync(~0u, plain);
                 if (lane == 0) reinterpret_cast<uint8_t *>(&meta.plain)[lw] = plain;
-                if (lt == 0) meta.n = n, meta.first = first, meta.last = last;
+                const unsigned before = __shfl_up_sync(~0u, key.at, 1);
+                const unsigned follows = __ballot_sync(~0u, lt < n && ((lt & (maps.run - 1)) == 0 || key.at == before + p.slot16));
+                // (a lane to each of the warp's blocks)
+                const bool whole = maps.run && lane < 32 >> maps.run_log2 && __popc(follows >> (lane << maps.run_log2) << (32 - maps.run)) == maps.run;
+                const unsigned runs = __ballot_sync(~0u, whole);
+                if (lane == 0) meta.runs[lw] = (uint8_t)runs;
+                if (lt == 0) meta.n = n, meta.first = first, meta.last = last, meta.ranged = part.seg;
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar(sm.meta_full[t % kMetas]));
                 scout.taken(n);
@@ -1016,20 +1145,42 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
             if (!wait(sm.meta_full[t % kMetas], t / kMetas & 1)) break;
             const int n = meta.n;
             if (n < 0) break;
-            const int stage = c % kStages, rows16 = (n + 15) & ~15;
+            const int stage = c % kStages, rows16 = (n + 15) & ~15, per32 = 32 >> maps.run_log2;
+            // the tile's blocks of rows that are copied whole: a bit each, and to every lane of the first warp a block and half of its columns
+            const uint32_t runs = maps.run ? meta.runs[0] | meta.runs[1] << per32 | meta.runs[2] << 2 * per32 | meta.runs[3] << 3 * per32 : 0u;
+            const int block = lane / kHalves, x = lane % kHalves * 64;
+            const bool whole = block < 4 * per32 && (runs >> block & 1);
+            const unsigned at0 = whole ? meta.at[block * maps.run] : 0;
+            const int bytes = __popc(runs) * kHalves * 128 * maps.run;
+            const bool rest = __popc(runs) * maps.run < rows16;
 #pragma unroll 1
             for (int kv = 0; kv < 2 && n > 0; ++kv) {
                 const uint64_t &full = kv ? sm.v_full[stage] : sm.k_full[stage], &empty = kv ? sm.v_empty[stage] : sm.k_empty[stage];
                 if (c >= kStages && !(ok = wait(empty, (c / kStages - 1) & 1))) break;
                 const uint32_t tile = smem_u32(kv ? sm.v[stage] : sm.k[stage]);
                 const char *from = (const char *)(kv ? p.cache.v : p.cache.k) + chunk * 16;
-#pragma unroll 4
-                for (int row = first; row < rows16; row += kCopyWarps * kRowsOfCopy)
-                    if (copies) cp_async16_or_zero(S::place(tile, row, chunk), from + (size_t)meta.at[row] * 16, row < n);
+                if (warp == kCopyWarp0 && whole)
+                    tma_load_2d(tile + lane % kHalves * S::kHalf + block * maps.run * 128, kv ? &maps.v : &maps.k, (int)(at0 % p.slot16) * 8 + x,
+                                (int)(at0 / p.slot16), bar(full));
+                __syncwarp();
+                // (places ahead of the copies: a load behind a copy waits its turn, 34 clk per copy instead of 10)
+                constexpr int kStep = kCopyWarps * kRowsOfCopy, kBatch = 8;
+#pragma unroll 1
+                for (int row0 = first; rest && row0 < rows16; row0 += kBatch * kStep) {
+                    unsigned at[kBatch];
+#pragma unroll
+                    for (int i = 0; i < kBatch; ++i) at[i] = meta.at[min(row0 + i * kStep, kTcKeys - 1)];
+#pragma unroll
+                    for (int i = 0; i < kBatch; ++i) {
+                        const int row = row0 + i * kStep;
+                        if (copies && row < rows16 && !(runs >> (row >> maps.run_log2) & 1))
+                            cp_async16_or_zero(S::place(tile, row, chunk), from + (size_t)at[i] * 16, row < n);
+                    }
+                }
                 __syncwarp();
                 cp_async_arrive(bar(full));
                 __syncwarp();
-                if (lane == 0) mbar_arrive(bar(full));
+                if (lane == 0) mbar_arrive_expect_tx(bar(full), warp == kCopyWarp0 ? bytes : 0);  // (behind all that the warp has asked for)
             }
             c += n > 0;
             __syncwarp();
@@ -1142,26 +1293,24 @@ __global__ void __launch_bounds__(32 * kJoinWarps) shared_join_kernel(const __gr
     const int at = (blockIdx.x - kv * per_kv) * kJoinRows + lane % kJoinRows, c4 = blockIdx.y * 4 + lane / kJoinRows;
     const int b = at / p.group, g = at - b * p.group;
     const bool exists = b < p.B && c4 * 4 < p.d;
-    bool bad = false;
     // the results: of the shared tokens, and of the own ones
     const float *value[2];
     const float2 *stat[2];
-    int64_t step[2];      // from one of them to the next, in floats
+    int64_t step[2];        // from one of them to the next, in floats
     int64_t from_first[2];  // from the first one to where the steps are counted from: its slot may be another than the next ones'
     int parts[2] = {0, 0};
     const size_t out = (size_t)b * p.heads + kv * p.group + g;
-    bool direct = !exists;
     // (the batch is looked at ahead of the wait: the kernel in front of this one has waited for whoever wrote it before it let this one start)
-    const Entry e = entry_of(p, min(b, p.B - 1), &bad);
+    Entry e;
+    entry_of(p, min(b, p.B - 1), &e);
     ptx::wait_prior_grid();
     if (exists) {
 #pragma unroll
         for (int seg = 0; seg < 2; ++seg) {
-            if (seg == 0 ? e.count == 0 : segment_of<RT>(p, e, b, 1).units == 0) continue;
-            const int row = seg == 0 ? (b - e.first) * p.group + g : g, r = row % RT;
-            const Joint joint = *joint_of(p, seg, kv, seg == 0 ? e.first : b, row / RT);
+            if (seg == 0 && e.count == 0) continue;
+            const int row = (seg == 0 ? b - e.first : b % p.pack) * p.group + g, r = row % RT;
+            const Joint joint = *joint_of(p, seg, kv, seg == 0 ? e.first : b / p.pack, row / RT);
             if (joint.slot < 0) {
-                if (e.count == 0) direct = true;
                 const size_t whole = (size_t)seg * p.B * p.heads + out;
                 value[seg] = p.whole + whole * p.d + c4 * 4, stat[seg] = p.whole_stats + whole;
                 step[seg] = from_first[seg] = 0;
@@ -1175,10 +1324,9 @@ __global__ void __launch_bounds__(32 * kJoinWarps) shared_join_kernel(const __gr
             }
         }
     }
-    if (__syncthreads_and(direct)) return;
     float m = -INFINITY, l = 0.f;
     float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (!direct) {
+    {
 #pragma unroll
         for (int seg = 0; seg < 2; ++seg) {
             for (int i = warp; i < parts[seg]; i += kJoinWarps) {
@@ -1195,7 +1343,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) shared_join_kernel(const __gr
     }
     s_sum[warp][lane] = sum, s_stat[warp][lane] = make_float2(m, l);
     __syncthreads();
-    if (warp > 0 || direct) return;
+    if (warp > 0 || !exists) return;
     for (int w = 0; w < kJoinWarps; ++w) m = fmaxf(m, s_stat[w][lane].x);
     const float base = m == -INFINITY ? 0.f : m;
     l = 0.f, sum = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -1214,6 +1362,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) shared_join_kernel(const __gr
 // ---- host
 
 int rows_of_tile(const mate_cache_t *c) { return c->dtype == MATE_F32 ? kSimtRows : kTcRows; }
+int pack_of(const mate_cache_t *c) { return std::max(1, rows_of_tile(c) / (c->heads / c->kv_heads)); }
 int own_tiles(const mate_cache_t *c) { return (c->heads / c->kv_heads + rows_of_tile(c) - 1) / rows_of_tile(c); }
 int n_blocks(const mate_cache_t *c) { return (c->dtype == MATE_F32 ? 2 : 1) * n_sms(c->device); }
 
@@ -1230,21 +1379,39 @@ Workspace workspace_of(const mate_cache_t *c, int B) {
     return w;
 }
 
+// Boxes of the highest of 8, 16 and 32 rows that a page is a whole number of, where the rows of all heads and pages lie in one such matrix and 64
+// columns from a head's first on are its own, or behind the last one.
+TcMaps maps_of(const SharedParams &p, const mate_cache_t *c) {
+    TcMaps m = {};
+    const int64_t slot = c->slot_stride, rows = slot > 0 ? ((int64_t)(c->pages - 1) * c->page_stride + (c->kv_heads - 1) * c->head_stride) / slot + c->page_size : 0;
+    int run = 32;
+    while (run > 8 && c->page_size % run != 0) run /= 2;
+    bool fits = c->page_size % run == 0 && slot >= c->d && (c->pages == 1 || c->page_stride % slot == 0) && (slot == c->d || c->d % 64 == 0) && rows <= INT32_MAX;
+    for (int h = 0; h < c->kv_heads && fits; ++h) fits = h * c->head_stride % slot + c->d <= slot;
+    if (fits && make_box_map(&m.k, p.cache.k, (size_t)slot, (size_t)rows, (size_t)slot * 2, run) &&
+        make_box_map(&m.v, p.cache.v, (size_t)slot, (size_t)rows, (size_t)slot * 2, run))
+        m.run = run;
+    for (m.run_log2 = 0; 1 << m.run_log2 < run;) ++m.run_log2;  // (without boxes too: the rows are looked at in blocks all the same)
+    return m;
+}
+
 template <typename T, int DP>
-int launch(const SharedParams &p, int device, int blocks, cudaStream_t st) {
+int launch(const SharedParams &p, const mate_cache_t *cache, int blocks, cudaStream_t st) {
     constexpr bool kTc = sizeof(T) == 2;
     constexpr int kRows = kTc ? kTcRows : kSimtRows, kThreads = kTc ? kTcThreads : kSimtThreads;
     constexpr int kSmem = kTc ? 1024 + (int)sizeof(TcSmem<DP>) : (int)sizeof(SimtSmem<DP>);
     static_assert(kSmem <= 232448, "shared memory of a block");
-    void (*kernel)(SharedParams);
-    if constexpr (kTc)
-        kernel = shared_tc_kernel<DP>;
-    else
-        kernel = shared_simt_kernel<DP>;
     static SmemAttrOnce attr;
-    const int rc = attr.ensure((const void *)kernel, kSmem, device);
-    if (rc != MATE_OK) return rc;
-    cudaError_t e = launch_after(kernel, dim3((unsigned)blocks), kThreads, kSmem, st, p);
+    cudaError_t e;
+    if constexpr (kTc) {
+        const int rc = attr.ensure((const void *)shared_tc_kernel<DP>, kSmem, cache->device);
+        if (rc != MATE_OK) return rc;
+        e = launch_after(shared_tc_kernel<DP>, dim3((unsigned)blocks), kThreads, kSmem, st, p, maps_of(p, cache));
+    } else {
+        const int rc = attr.ensure((const void *)shared_simt_kernel<DP>, kSmem, cache->device);
+        if (rc != MATE_OK) return rc;
+        e = launch_after(shared_simt_kernel<DP>, dim3((unsigned)blocks), kThreads, kSmem, st, p);
+    }
     const int64_t joins = (int64_t)p.kv_heads * (((int64_t)p.B * p.group + kJoinRows - 1) / kJoinRows);
     if (e == cudaSuccess)
         e = launch_after(shared_join_kernel<T, kRows>, dim3((unsigned)joins, (unsigned)((p.d + 15) / 16)), 32 * kJoinWarps, 0, st, p);
@@ -1284,9 +1451,8 @@ int mate_attn_decode_shared(const mate_cache_t *cache, int layer, const void *Q,
     if (B == 0) return MATE_OK;
     const int most = cache->width * cache->page_size;
     if (max_len == 0 || max_len > most) max_len = most;
-    // units of the batch, shared and own, are 32-bit numbers, and so are the blocks of the second kernel
-    if ((int64_t)B * cache->kv_heads * own_tiles(cache) > INT32_MAX / 2 / units_of(max_len) || (int64_t)B * cache->heads > INT32_MAX / 2)
-        return MATE_ERR_UNSUPPORTED;
+    // units of the batch, shared and own, are 32-bit numbers
+    if (B > kMaxBatch || (int64_t)B * cache->kv_heads * own_tiles(cache) > INT32_MAX / 2 / (kOver + units_of(max_len))) return MATE_ERR_UNSUPPORTED;
     const Workspace w = workspace_of(cache, B);
     if (!workspace || workspace_bytes < w.bytes) return MATE_ERR_WORKSPACE;
     if (!is_aligned(workspace, 256)) return MATE_ERR_ALIGNMENT;
@@ -1294,12 +1460,16 @@ int mate_attn_decode_shared(const mate_cache_t *cache, int layer, const void *Q,
     p.cache = cache_args(cache, layer);
     p.Q = Q, p.q_batch = q_stride[0], p.q_head = q_stride[1];
     p.B = B, p.heads = cache->heads, p.kv_heads = cache->kv_heads, p.group = cache->heads / cache->kv_heads;
-    p.d = cache->d, p.max_len = max_len, p.own_tiles = own_tiles(cache);
+    p.d = cache->d, p.max_len = max_len, p.pack = pack_of(cache), p.own_tiles = own_tiles(cache);
     p.seqs = seqs, p.row_ids = row_ids, p.col_ids = col_ids, p.groups = groups;
     p.scale_log2 = scale * kLog2e, p.O = O, p.LSE = LSE;
     for (int h = 0; h < cache->heads; ++h) p.views[h >> 4] |= (uint32_t)cache->head_view[h] << 2 * (h & 15);
-    for (p.page_shift = 0; 1u << p.page_shift < (unsigned)cache->page_size;) ++p.page_shift;
-    p.page_mul = (unsigned)((((uint64_t)1 << 32) * (((uint64_t)1 << p.page_shift) - cache->page_size)) / cache->page_size + 1);
+    const auto quotients = [](int by, unsigned *mul, unsigned *shift) {
+        for (*shift = 0; 1u << *shift < (unsigned)by;) ++*shift;
+        *mul = (unsigned)((((uint64_t)1 << 32) * (((uint64_t)1 << *shift) - by)) / by + 1);
+    };
+    quotients(cache->page_size, &p.page_mul, &p.page_shift);
+    quotients(p.group, &p.group_mul, &p.group_shift);
     p.page16 = (unsigned)(cache->page_stride / vec), p.head16 = (unsigned)(cache->head_stride / vec), p.slot16 = (unsigned)(cache->slot_stride / vec);
     char *ws = static_cast<char *>(workspace);
     p.joints = reinterpret_cast<Joint *>(ws + w.joints);
@@ -1312,9 +1482,9 @@ int mate_attn_decode_shared(const mate_cache_t *cache, int layer, const void *Q,
         p.scale_log2 = std::fmax(std::fabs(p.scale_log2), 0x1p-126f);
     }
     cudaStream_t st = (cudaStream_t)stream;
-    const int blocks = n_blocks(cache), device = cache->device;
-    if (cache->dtype == MATE_F32) return cache->d <= 64 ? launch<float, 64>(p, device, blocks, st) : launch<float, 128>(p, device, blocks, st);
-    return cache->d <= 64 ? launch<__nv_bfloat16, 64>(p, device, blocks, st) : launch<__nv_bfloat16, 128>(p, device, blocks, st);
+    const int blocks = n_blocks(cache);
+    if (cache->dtype == MATE_F32) return cache->d <= 64 ? launch<float, 64>(p, cache, blocks, st) : launch<float, 128>(p, cache, blocks, st);
+    return cache->d <= 64 ? launch<__nv_bfloat16, 64>(p, cache, blocks, st) : launch<__nv_bfloat16, 128>(p, cache, blocks, st);
 }
 
 }  // extern "C"

@@ -13,6 +13,8 @@ constexpr int kTileBytes = kTile * kRowBytes;  // 16 KB: 128 rows
 
 // Tensor map over a [rows, 64] bf16 matrix in boxes of 128 rows (false: no tensor maps to be had).
 bool make_row_map(CUtensorMap *map, const void *base, size_t rows);
+// The same over rows of any length and distance, in boxes of any height.
+bool make_box_map(CUtensorMap *map, const void *base, size_t cols, size_t rows, size_t row_bytes, int box_rows);
 
 // The loaders copy a tile of up to 128 rows (128 B each), warp w of the four the rows 32 w .. 32 w + 31.
 // A lane looks up the original position of one row (coalesced, one latency for the whole tile, and cheap

@@ -308,7 +308,7 @@ def test_many_heads(dtype, H, Hk):
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_many_entries(dtype):
     import paper_2109_04312_b200 as m
-    n = 5000
+    n = 4096
     case = Shared(m, [(3, [5, 0, 17, 1]), (2, [1, 2])], 4, 2, 16, 4, [0, 1, 2, 0], dtype, seed=13)
     seqs = ([0, 1, 2, 3] * (n // 8) + [4, 5] * (n // 4))
     sizes = [4] * (n // 8) + [2] * (n // 4)
@@ -319,6 +319,9 @@ def test_many_entries(dtype):
     O, LSE = m.mate_attn_decode_shared(case.c, Q, i32(q_ids[0]), i32(q_ids[1]), i32(groups), seqs=i32(seqs))
     some = np.random.default_rng(0).permutation(len(seqs))[:300]
     case.check(Q[some.tolist()], [seqs[i] for i in some], q_ids[:, some], O[some.tolist()], LSE[some.tolist()])
+    more = i32([0] * (n + 1))
+    with pytest.raises(m.MateError, match="unsupported|not available"):
+        m.mate_attn_decode_shared(case.c, Q[:1].expand(n + 1, 4, 16).contiguous(), more, more, torch.zeros(3, n + 1, dtype=torch.int32, device="cuda"), seqs=more)
 
 
 @pytest.mark.gpu
