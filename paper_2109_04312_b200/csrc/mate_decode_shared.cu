@@ -31,9 +31,11 @@ constexpr int kMaxHeads = 1024;
 constexpr int kNever = INT32_MIN;  // an id that no token has
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
-// Where the results of an item are: [slot] of the block that begins it, then [0] of the next ones up to `last`.
+// Where the results of an item are: [slot] of the block that begins it, then [0] of the next ones up to the one that has the unit in front of
+// `end`, of `total`.
 struct Joint {
-    int32_t slot, first, last, unused;  // slot < 0: with the rows' whole results
+    int32_t slot, first;  // slot < 0: with the rows' whole results
+    uint32_t end, total;
 };
 
 struct SharedParams {
@@ -47,13 +49,16 @@ struct SharedParams {
     int flip;          // tensor-core kernel: the scale above is positive, and the queries change their sign
     void *O;
     float *LSE;
-    unsigned page16, head16, slot16;  // strides in 16 bytes; no place is beyond 2^32 of them
+    // A token's place: page * page_step + slot * slot_step + kv head * head_step, in rows of row16 times 16 bytes; its kv head begins
+    // kv head * head16 times 16 bytes behind that.  No place is beyond 2^32 times 16 bytes.
+    unsigned page_step, slot_step, head_step, row16, head16;
     // x / page_size and x / group by multiplication: (umulhi(x, mul) + x) >> shift for x < 2^31
     unsigned page_mul, page_shift, group_mul, group_shift;
     Joint *joints;                    // [2][kv_heads][B own_tiles]: shared tokens, by the first entry of the tile's group, and own ones
     float2 *whole_stats;              // [2][B heads]  m and sum P of rows whose item one block has done
     float *whole;                     // [2][B heads][d]
     float *parts;                     // [blocks][2]: values in groups of four by row, then the rows' m and sum P
+    int blocks;                       // of the grid
     uint32_t views[kMaxHeads / 16];   // two bits a head
 };
 __device__ __forceinline__ int page_index(const SharedParams &p, int token) {
@@ -107,7 +112,6 @@ __device__ __noinline__ void entry_of(const SharedParams &p, int b, Entry *to) {
 }
 // Units of tokens.  The first kOver units of an item stand for what it costs whatever its length: none of its tokens belong to them.
 __host__ __device__ __forceinline__ int units_of(int tokens) { return (tokens + kUnit - 1) / kUnit; }
-__device__ __forceinline__ unsigned share(unsigned U, unsigned C, unsigned i) { return U / C * i + U % C * i / C; }
 // Items of the shared tokens of the group that entry b is the first of: kv heads and tiles of rows.
 __device__ __forceinline__ bool leads(const Entry &e, int b) { return e.count > 0 && e.first == b; }
 template <int RT>
@@ -117,15 +121,15 @@ __device__ __forceinline__ int group_tiles(const SharedParams &p, const Entry &e
 // Units of an item of own tokens.  (Without any it has one: its rows have a result too.)
 __device__ __forceinline__ int own_units(int tokens_units) { return tokens_units > 0 ? kOver + tokens_units : 1; }
 
+// Where a block begins: unit `in` of its first batch, for `left` units (0: there is nothing for it to do), the first of them number `at` of all.
 struct Start {
-    unsigned total, before;  // units of all; of the batches of `pack` entries in front of `batch`
-    unsigned blocks;         // that get any: no more than there are units
-    int batch;
+    unsigned total, at, in;
+    int left, batch;
 };
-// All threads call it: the batch that the block's first unit belongs to.  `cost`: [B] in shared memory, free afterwards.
+// All threads call it.  `cost`: [B] in shared memory, free afterwards.
 template <int RT, int NT>
 __device__ Start find_start(const SharedParams &p, uint2 *cost) {
-    __shared__ unsigned s_sum[NT / 32];
+    __shared__ unsigned s_sum[32];
     __shared__ Start s_start;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, batches = (p.B + p.pack - 1) / p.pack;
 #pragma unroll 1
@@ -135,7 +139,8 @@ __device__ Start find_start(const SharedParams &p, uint2 *cost) {
         cost[b] = make_uint2(units_of(e.own1 - e.own0), leads(e, b) ? p.kv_heads * group_tiles<RT>(p, e) * (kOver + units_of(e.shared)) : 0);
         if (e.bad && blockIdx.x == 0) atomicOr(p.cache.status, kCacheBad);
     }
-    if (tid == 0) s_start = {0, 0, 0, 0};
+    if (tid == 0) s_start = {};
+    if (tid < 32) s_sum[tid] = 0;
     __syncthreads();
     // a warp to each batch; its cost replaces that of its first entry
 #pragma unroll 1
@@ -152,59 +157,58 @@ __device__ Start find_start(const SharedParams &p, uint2 *cost) {
     unsigned own = 0;
 #pragma unroll 1
     for (int i = i0; i < i1; ++i) own += cost[i * p.pack].x;
-    unsigned sum = own;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const unsigned y = __shfl_up_sync(~0u, sum, o);
-        if (lane >= o) sum += y;
-    }
-    if (lane == 31) s_sum[warp] = sum;
+    const unsigned of_warp = __reduce_add_sync(~0u, own);
+    if (lane == 0) s_sum[warp] = of_warp;
     __syncthreads();
-    unsigned total = 0, before = sum - own;
+    const unsigned sums = s_sum[lane], total = __reduce_add_sync(~0u, sums), in_front = __reduce_add_sync(~0u, lane < warp ? sums : 0u);
+    const unsigned blocks = min(total, (unsigned)p.blocks), i = blockIdx.x;
+    if (i < blocks) {
+        const unsigned q = total / blocks, r = total - q * blocks, at = q * i + r * i / blocks, end = q * (i + 1) + r * (i + 1) / blocks;
+        if (at - in_front < of_warp) {  // (at >= in_front, too)
+            unsigned sum = own;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const unsigned y = __shfl_up_sync(~0u, sum, o);
+                if (lane >= o) sum += y;
+            }
+            unsigned in = at - in_front - (sum - own);
+            if (in < own) {
+                int k = i0;
 #pragma unroll 1
-    for (int w = 0; w < NT / 32; ++w) {
-        if (w < warp) before += s_sum[w];
-        total += s_sum[w];
-    }
-    const unsigned blocks = min(total, gridDim.x);
-    if (blockIdx.x < blocks) {
-        const unsigned at = share(total, blocks, blockIdx.x);
-        if (at >= before && at < before + own) {
-            int i = i0;
-#pragma unroll 1
-            for (; i < i1 - 1 && at >= before + cost[i * p.pack].x; ++i) before += cost[i * p.pack].x;
-            s_start = {total, before, blocks, i};
+                for (; in >= cost[k * p.pack].x; ++k) in -= cost[k * p.pack].x;
+                s_start = {total, at, in, (int)(end - at), k};
+            }
         }
     }
     __syncthreads();
     return s_start;
 }
 
-// A part of an item: units [u0, u1) of them.
+// A part of an item.
 struct Part {
     int b, seg, kv, tile;  // first entry; shared tokens (0) or own ones (1); tile of rows
-    int u0, u1, units;
+    int from, to;          // its units of tokens
     int n_rows;
+    int state;
+    unsigned end;          // of the item's units, among those of all
 };
 enum { kAll, kBegins, kGoesOn };
-__device__ __forceinline__ int part_state(const Part &part) { return part.u0 > 0 ? kGoesOn : part.u1 == part.units ? kAll : kBegins; }
-// Of a row of the tile: its entry, counted from the part's first, and its place among all rows of the batch.
+// Of a row of the tile: its entry, counted from the part's first, and its place among all rows of the batch (there are fewer than 2^23).
 template <int RT>
 __device__ __forceinline__ int member_of(const SharedParams &p, const Part &part, int r) {
     return by_group(p, part.tile * RT + r);
 }
 template <int RT>
-__device__ __forceinline__ size_t row_of(const SharedParams &p, const Part &part, int r, int member) {
-    return (size_t)(part.b + member) * p.heads + part.kv * p.group + part.tile * RT + r - member * p.group;
+__device__ __forceinline__ int row_of(const SharedParams &p, const Part &part, int r, int member) {
+    return (part.b + member) * p.heads + part.kv * p.group + part.tile * RT + r - member * p.group;
 }
 // (tiles of a group of n entries: fewer than n own_tiles, so those of different groups have different places)
 __device__ __forceinline__ Joint *joint_of(const SharedParams &p, int seg, int kv, int b, int tile) {
     return p.joints + ((size_t)seg * p.kv_heads + kv) * p.B * p.own_tiles + (size_t)b * p.own_tiles + tile;
 }
-// Of the part that begins an item that goes on in the next blocks (it is the last one of its block's share).
-__device__ __noinline__ Joint joint_from(const Part &part, const Start &start, int slot) {
-    const int64_t end = (int64_t)share(start.total, start.blocks, blockIdx.x + 1) - (part.u1 - part.u0) + part.units;
-    return {slot, (int)blockIdx.x, (int)min((end * start.blocks - 1) / start.total, (int64_t)start.blocks - 1), 0};
+__device__ __forceinline__ void put_joint(const SharedParams &p, const Part &part, int slot, unsigned total) {
+    if (part.state == kGoesOn) return;
+    *joint_of(p, part.seg, part.kv, part.seg == 0 ? part.b : part.b / p.pack, part.tile) = {part.state == kAll ? -1 : slot, (int)blockIdx.x, part.end, total};
 }
 
 // ---- who attends what
@@ -230,10 +234,11 @@ struct Wishes {
 };
 // Keys, with what the rows go by.
 struct alignas(16) Key {
-    unsigned at;  // in 16 bytes from the cache's beginning
+    unsigned at;  // where it lies: see SharedParams
     int place, row, col;
 };
-constexpr int kList = 256, kScouts = 128;
+constexpr int kList = 512, kScouts = 128;
+constexpr unsigned kNowhere = ~0u;
 
 // kScouts threads walk the parts of the block's share and look through their tokens, four units at a time, a warp to each; the keys that
 // count go onto a list.  The next ones' ids, and the pages of the ones behind them, are on their way meanwhile.  Barrier 1 is theirs.
@@ -247,28 +252,31 @@ struct ScoutSmem {
     Wishes<RT> wishes[2];    // of the parts in turn
     Key list[kList];         // what look() writes is seen behind the next barrier
     uint8_t owners[kList];   // entries of the batch
-    int counts[2][4];
+    int counts[2][4];        // of the warps' keys; plus kDense
 };
+constexpr int kDense = 64, kNobody = 255;
 // Where the loads of a look stand.
 struct Asked {
     int j, owner, page;
-    bool there;
+    bool there, first;  // first: the entry's first unit
 };
 template <int RT>
 struct Scout {
     const SharedParams &p;
     ScoutSmem<RT> &sm;
-    int tid;
+    int tid, run;  // run: keys that lie one behind the other are copied by that many (1: one by one)
     // the walk: next item of the share
-    int batch, entry, item, u, left;  // entry: that leads (of the batch), kScouts: own tokens; left: units of the share
-    int held, parts;                  // batch that is in shared memory; parts so far
+    int batch, entry, tiles, n_units, item, u;  // entry: that leads (of the batch), kScouts: own tokens; tiles of rows, units of an item of it
+    unsigned in, at_unit;                       // units to pass over yet; number of the next one among those of all
+    int left;                                   // units of the share
+    int held, parts;                            // batch that is in shared memory; parts so far
     // the looks at the present part
     int seg, next, end, pending, list_at, looks;  // next, end: units
     unsigned head_at;
     Asked asked;
     unsigned at;
     int j, owner, row, col;
-    bool there, bad;
+    bool there, first, bad;
 
     __device__ static void sync() { asm volatile("barrier.cta.sync 1, 128;" ::: "memory"); }
     __device__ int entries() const { return min(p.pack, p.B - batch * p.pack); }
@@ -305,21 +313,10 @@ struct Scout {
         }
         return kScouts;
     }
-    __device__ int items() const { return p.kv_heads * (entry < kScouts ? group_tiles<RT>(p, sm.entries[entry]) : p.own_tiles); }
-    __device__ int units() const { return entry < kScouts ? kOver + units_of(sm.entries[entry].shared) : own_units(sm.before[kScouts]); }
     __device__ void start(const Start &from) {
-        const unsigned begin = share(from.total, from.blocks, blockIdx.x);
-        unsigned in = begin - from.before;
-        batch = from.batch, parts = 0, bad = false, looks = 0;
-        left = (int)(share(from.total, from.blocks, blockIdx.x + 1) - begin);
+        batch = from.batch, in = from.in, at_unit = from.at, left = from.left;
+        held = -1, parts = looks = item = u = tiles = n_units = entry = 0, bad = false;
         if (tid == 0) sm.wishes[0].clear();
-        hold();
-        entry = leader_from(0);
-#pragma unroll 1
-        while (entry < kScouts && in >= (unsigned)items() * units()) in -= (unsigned)items() * units(), entry = leader_from(entry + 1);
-        item = (int)(in / (unsigned)units());
-        u = (int)(in - (unsigned)item * units());
-        if (u <= kOver) left += u, u = 0;
     }
     // The next part of the share.  (It comes to an end whatever it finds: every part takes a unit off the share.)
     __device__ bool next_part(Part &part) {
@@ -327,34 +324,46 @@ struct Scout {
         while (left > 0 && batch * p.pack < p.B) {
             if (held != batch) {
                 hold();
-                entry = leader_from(0);
+                entry = -1, tiles = item = 0;
             }
-            if (item < items()) {
-                const int n = units(), u1 = min(n, u + left);
-                if (u1 <= kOver && u1 < n) break;  // it ends among the units that stand for the item: the next block takes it
-                const int tiles = entry < kScouts ? group_tiles<RT>(p, sm.entries[entry]) : p.own_tiles, kv = item / tiles, tile = item - kv * tiles;
+            if (item < p.kv_heads * tiles) {
+                const int u1 = min(n_units, u + left);
+                if (u1 <= kOver && u1 < n_units) break;  // it ends among the units that stand for the item: the next block takes it
+                const int kv = item / tiles, tile = item - kv * tiles;
                 const int rows = (entry < kScouts ? sm.entries[entry].count : entries()) * p.group;
-                part = {batch * p.pack + (entry < kScouts ? entry : 0), entry < kScouts ? 0 : 1, kv, tile, u, u1, n, min(RT, rows - tile * RT)};
+                part = {batch * p.pack + (entry < kScouts ? entry : 0), entry < kScouts ? 0 : 1, kv, tile, max(0, u - kOver), max(0, u1 - kOver),
+                        min(RT, rows - tile * RT), u > 0 ? kGoesOn : u1 == n_units ? kAll : kBegins, at_unit - u + n_units};
                 left -= max(1, u1 - u);
+                at_unit += u1 - u;
                 u = 0;
                 ++item;
                 return true;
             }
-            item = 0;
-            if (entry == kScouts)
+            if (entry == kScouts) {
                 ++batch;
-            else
-                entry = leader_from(entry + 1);
+                continue;
+            }
+            entry = leader_from(entry + 1), item = 0;
+            const bool group = entry < kScouts;
+            tiles = group ? group_tiles<RT>(p, sm.entries[entry]) : p.own_tiles;
+            n_units = group ? kOver + units_of(sm.entries[entry].shared) : own_units(sm.before[kScouts]);
+            const unsigned all = (unsigned)(p.kv_heads * tiles) * n_units;
+            if (in >= all) {
+                in -= all, item = p.kv_heads * tiles;
+            } else if (in > 0) {
+                item = (int)(in / (unsigned)n_units), u = (int)(in - (unsigned)item * n_units), in = 0;
+                if (u <= kOver) left += u, at_unit -= u, u = 0;
+            }
         }
         left = 0;
         return false;
     }
     // Who the warp's 32 tokens of unit `unit` belong to, and their pages.
     __device__ void ask_page(int unit) {
-        asked = {0, 0, -1, false};
+        asked = {0, 0, -1, false, false};
         if (unit >= end) return;
         const int lane = tid & 31;
-        int first = 0, stop, from = 0;
+        int first_token = 0, stop, from = 0;
         if (seg == 0) {
             asked.owner = leader;
             stop = min(sm.entries[leader].shared, sm.entries[leader].len);
@@ -365,29 +374,29 @@ struct Scout {
             asked.owner = __reduce_add_sync(~0u, n) - 1;
             // (of entries without tokens the last one that begins there is found: it is the one behind them)
             const Entry &e = sm.entries[asked.owner];
-            first = e.own0, stop = e.own1, from = sm.before[asked.owner];
+            first_token = e.own0, stop = e.own1, from = sm.before[asked.owner];
+            asked.first = unit == from;
         }
         const int s = sm.entries[asked.owner].s;
-        asked.j = first + (unit - from) * kUnit + lane;
+        asked.j = first_token + (unit - from) * kUnit + lane;
         asked.there = asked.j < stop && s >= 0;
         if (asked.there) asked.page = p.cache.table[(size_t)s * p.cache.width + page_index(p, asked.j)];
     }
     __device__ void ask_ids() {  // of the tokens whose page has been asked for
-        j = asked.j, owner = asked.owner;
+        j = asked.j, owner = asked.owner, first = asked.first;
         there = asked.there && in_range(asked.page, p.cache.pages);
         if (asked.there && !there) bad = true;
         if (!there) return;
         const int slot = j - page_index(p, j) * p.cache.page_size, id = asked.page * p.cache.page_size + slot;
         row = p.cache.row_ids[id], col = p.cache.col_ids[id];
-        at = (unsigned)asked.page * p.page16 + (unsigned)slot * p.slot16 + head_at;
+        at = (unsigned)asked.page * p.page_step + (unsigned)slot * p.slot_step + head_at;
     }
     int leader;
     // Behind a barrier that the last look at the part before it is in front of.
     __device__ void begin(const Part &part, Rows<RT> &rows) {
         seg = part.seg, leader = part.b - batch * p.pack;
-        next = max(0, part.u0 - kOver), end = max(0, part.u1 - kOver);
-        if (seg == 1) end = min(end, sm.before[kScouts]);
-        head_at = (unsigned)part.kv * p.head16;
+        next = part.from, end = seg == 1 ? min(part.to, sm.before[kScouts]) : part.to;
+        head_at = (unsigned)part.kv * p.head_step;
         pending = list_at = 0;
         ask_page(next + (tid >> 5));
         Wishes<RT> &w = sm.wishes[parts & 1];
@@ -396,8 +405,10 @@ struct Scout {
         int want_row = kNever, want_col = kNever, below = -2;
         if (tid < part.n_rows) {
             const int member = member_of<RT>(p, part, tid), view = view_at(p, part.kv * p.group + part.tile * RT + tid - member * p.group);
-            Entry e;
-            entry_of(p, part.b + member, &e);
+            const int held_at = part.b - batch * p.pack + member;
+            Entry other;
+            if (held_at >= entries()) entry_of(p, part.b + member, &other);
+            const Entry &e = held_at >= entries() ? other : sm.entries[held_at];
             if (seg == 0 ? e.counts && e.first == part.b && e.count > 0 : e.own1 > e.own0) {
                 const bool text = e.q_row == MATE_ID_TEXT || e.q_col == MATE_ID_TEXT;
                 below = text ? INT32_MAX : e.prefix;
@@ -423,6 +434,7 @@ struct Scout {
         const Wishes<RT> &w = wishes();
         Key key = {at, j, row, col};
         const int of = owner;
+        const bool was_there = there, was_first = first;
         bool is = there && row >= 0 && col >= 0;
         if (is) {
             if (row == MATE_ID_TEXT || col == MATE_ID_TEXT) key.place = -1;
@@ -444,24 +456,33 @@ struct Scout {
             ask_page(next + 4 + (tid >> 5));
         }
         __syncwarp();
-        const unsigned those = __ballot_sync(~0u, is);
+        const unsigned those = __ballot_sync(~0u, is), valid = __ballot_sync(~0u, was_there);
+        const int lane = tid & 31, warp = tid >> 5;
         int *count = sm.counts[looks++ & 1];
-        if ((tid & 31) == 0) count[tid >> 5] = __popc(those);
+        // Own tokens of which none is left out begin at a multiple of `run`, so that they are copied in runs; in front of them are nobody's.
+        const bool dense = was_first && those == valid && __popc(those) >= run;
+        if (lane == 0) count[warp] = __popc(those) + (dense ? kDense : 0);
         sync();
-        int before = 0, all = 0;
+        int to = pending, gap = 0, all = pending;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            if (i < tid >> 5) before += count[i];
-            all += count[i];
+            const int c = count[i], up = c >= kDense ? (all + run - 1) & -run : all;
+            if (i == warp) to = up, gap = up - all;
+            all = up + (c & (kDense - 1));
         }
-        const unsigned to = (unsigned)(list_at + pending + before + __popc(those & ((1u << (tid & 31)) - 1))) % kList;
-        if (is) sm.list[to] = key, sm.owners[to] = (uint8_t)of;
-        pending += all;
+        if (lane < gap) put_key(to - gap + lane, {kNowhere, INT32_MAX, kNever + 1, kNever + 1}, kNobody);
+        if (is) put_key(to + __popc(those & ((1u << lane) - 1)), key, of);
+        pending = all;
+    }
+    __device__ void put_key(int i, const Key &key, int of) {
+        const unsigned at_list = (unsigned)(list_at + i) % kList;
+        sm.list[at_list] = key, sm.owners[at_list] = (uint8_t)of;
     }
     __device__ Key key(int i) const { return sm.list[(unsigned)(list_at + i) % kList]; }
     __device__ int owner_of_key(int i) const { return sm.owners[(unsigned)(list_at + i) % kList]; }
     // Whether every row that a key is for attends it.
     __device__ bool is_plain(const Key &key, int of) const {
+        if (of == kNobody) return true;
         const Entry &e = sm.entries[of];
         return seg == 0 ? key.place < wishes().least : e.q_row == MATE_ID_TEXT || e.q_col == MATE_ID_TEXT || key.place < e.prefix;
     }
@@ -499,9 +520,9 @@ __global__ void __launch_bounds__(kSimtThreads) shared_simt_kernel(const __grid_
     ptx::wait_prior_grid();
     static_assert(sizeof(sm.q) + sizeof(sm.k) + sizeof(sm.v) + sizeof(sm.s) >= kMaxBatch * sizeof(uint2), "room for the entries' cost");
     const Start start = find_start<kSimtRows, kSimtThreads>(p, reinterpret_cast<uint2 *>(smem_raw));
-    if (blockIdx.x >= start.blocks) return;
+    if (start.left == 0) return;
     for (int i = tid; i < (int)(sizeof(SimtSmem<DP>) / 4); i += kSimtThreads) reinterpret_cast<uint32_t *>(smem_raw)[i] = 0;  // columns that nobody writes
-    Scout<kSimtRows> scout = {p, sm.scout, tid};
+    Scout<kSimtRows> scout = {p, sm.scout, tid, 1};
     __syncthreads();
     if (tid < kScouts) scout.start(start);
     for (int n_parts = 0;; ++n_parts) {
@@ -547,8 +568,9 @@ __global__ void __launch_bounds__(kSimtThreads) shared_simt_kernel(const __grid_
             for (int i = tid; i < kSimtKeys * (p.d / kVec); i += kSimtThreads) {
                 const int k = i / (p.d / kVec), c = (i - k * (p.d / kVec)) * kVec;
                 if (k < n) {
-                    load16((const float *)p.cache.k + (size_t)sm.keys[k].at * kVec + c, &sm.k[k][c]);
-                    load16((const float *)p.cache.v + (size_t)sm.keys[k].at * kVec + c, &sm.v[k][c]);
+                    const size_t at = ((size_t)sm.keys[k].at * p.row16 + (size_t)part.kv * p.head16) * kVec + c;
+                    load16((const float *)p.cache.k + at, &sm.k[k][c]);
+                    load16((const float *)p.cache.v + at, &sm.v[k][c]);
                     for (int e = 0; e < kVec; ++e) odd |= !(fabsf(sm.v[k][c + e]) < INFINITY);
                 } else {
                     for (int e = 0; e < kVec; ++e) sm.k[k][c + e] = sm.v[k][c + e] = 0.f;
@@ -627,7 +649,7 @@ __global__ void __launch_bounds__(kSimtThreads) shared_simt_kernel(const __grid_
             }
             __syncthreads();
         }
-        const int state = part_state(part), slot = n_parts == 0 ? 0 : 1;
+        const int state = part.state, slot = n_parts == 0 ? 0 : 1;
         float *to = p.parts + (size_t)(2 * blockIdx.x + slot) * part_floats(kSimtRows, p.d);
 #pragma unroll
         for (int r = 0; r < kR; ++r) {
@@ -636,7 +658,7 @@ __global__ void __launch_bounds__(kSimtThreads) shared_simt_kernel(const __grid_
             for (int step = 16; step > 0; step >>= 1) sum += __shfl_xor_sync(~0u, sum, step);
             const int row = r0 + r;
             if (row >= part.n_rows) break;
-            const size_t whole = (size_t)part.seg * p.B * p.heads + row_of<kSimtRows>(p, part, row, member_of<kSimtRows>(p, part, row));
+            const size_t whole = (size_t)(part.seg * p.B * p.heads) + row_of<kSimtRows>(p, part, row, member_of<kSimtRows>(p, part, row));
             for (int c = 0; c < kCols; ++c) {
                 const int e = lane * kCols + c;
                 if (e >= p.d) break;
@@ -645,13 +667,7 @@ __global__ void __launch_bounds__(kSimtThreads) shared_simt_kernel(const __grid_
             }
             if (lane == 0) (state == kAll ? p.whole_stats[whole] : reinterpret_cast<float2 *>(to + (size_t)p.d * kSimtRows)[row]) = make_float2(m[r], sum);
         }
-        if (tid == 0 && state != kGoesOn) {
-            Joint *joint = joint_of(p, part.seg, part.kv, part.seg == 0 ? part.b : part.b / p.pack, part.tile);
-            if (state == kAll)
-                joint->slot = -1;
-            else
-                *joint = joint_from(part, start, slot);
-        }
+        if (tid == 0) put_joint(p, part, slot, start.total);
     }
     if (tid < kScouts && scout.bad) atomicOr(p.cache.status, kCacheBad);
 }
@@ -660,8 +676,8 @@ __global__ void __launch_bounds__(kSimtThreads) shared_simt_kernel(const __grid_
 
 constexpr int kTcRows = 128, kTcKeys = 128;
 constexpr int kSoftmaxWarps = 8;              // two teams, which take the tiles in turn; a thread to a row
-constexpr int kLoadWarp0 = kSoftmaxWarps, kLoadWarps = kScouts / 32;
-constexpr int kCopyWarp0 = kLoadWarp0 + kLoadWarps, kCopyWarps = 3;
+constexpr int kScoutWarp0 = kSoftmaxWarps, kScoutWarps = kScouts / 32;
+constexpr int kCopyWarp0 = kScoutWarp0 + kScoutWarps, kCopyWarps = 2;  // keys, values
 constexpr int kMmaWarp = kCopyWarp0 + kCopyWarps;
 constexpr int kTcThreads = 32 * (kMmaWarp + 1);
 constexpr int kMetas = 4;                     // tiles whose keys are known
@@ -684,6 +700,7 @@ struct alignas(16) Meta {
     int n, first, last;  // keys; of the part.  n < 0: the share is done
     uint32_t plain;      // 0x01010101: every row attends every key that is for it
     int ranged;          // keys lo[m] to hi[m] are for the rows of entry m, else all for all
+    unsigned x16;        // where a row's elements begin, in 16 bytes
     uint8_t runs[4];     // of every 32 keys: blocks of TcMaps.run keys that lie one behind the other
     alignas(16) int place[kTcKeys];  // (read four at a time)
     alignas(16) int row[kTcKeys];
@@ -695,7 +712,7 @@ struct alignas(16) Meta {
 // 64 elements.
 struct TcMaps {
     CUtensorMap k, v;
-    int run, run_log2;  // rows of a box, 8, 16 or 32; 0: every row is copied by itself
+    int run, run_log2;  // rows of a box, 16 or 32; 0: every row is copied by itself
 };
 template <int DP>
 struct TcSmem {  // from a multiple of 1024 bytes on
@@ -751,8 +768,9 @@ __device__ __forceinline__ void mask_scores(uint32_t (&v)[32], const Meta &meta,
         if (!attends(want_row, want_col, below, place.w, row.w, col.w)) v[e + 3] = 0xff800000u;
     }
 }
-__device__ __forceinline__ float top_score(const uint32_t (&v)[32], float top) {
-    float t[4] = {top, -INFINITY, -INFINITY, -INFINITY};
+__device__ __forceinline__ uint32_t bits_below(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u; }
+__device__ __forceinline__ float top_score(const uint32_t (&v)[32]) {
+    float t[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
     for (int e = 0; e < 32; e += 8)
 #pragma unroll
@@ -781,6 +799,43 @@ __device__ __forceinline__ void weigh(uint32_t (&v)[32], uint64_t scale2, uint64
     }
 }
 
+// The row's O, or its weights of the first n keys of a tile, times `keep` (rarely).
+__device__ __noinline__ void scale_o(uint32_t tO, int n, float keep) {
+#pragma unroll 1
+    for (int i = 0; i < n; i += 8) {
+        uint32_t o[8];
+        ptx::tmem_ld8(tO + i, o);
+        ptx::tc_wait_ld();
+        ptx::reg_fence(o);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * keep);
+        ptx::tmem_st8(tO + i, o);
+    }
+    ptx::tc_wait_st();
+}
+__device__ __noinline__ void scale_p(uint32_t tP, int n, float keep) {
+    ptx::tc_wait_st();
+#pragma unroll 1
+    for (int i = 0; i < n; i += 16) {
+        uint32_t hi[8], lo[8];
+        ptx::tmem_ld8(tP + i, hi);
+        ptx::tmem_ld8(tP + i + 8, lo);
+        ptx::tc_wait_ld();
+        ptx::reg_fence(hi);
+        ptx::reg_fence(lo);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float x = (__uint_as_float(hi[e] << 16) + __uint_as_float(lo[e] << 16)) * keep;
+            const float y = (__uint_as_float(hi[e] & 0xffff0000u) + __uint_as_float(lo[e] & 0xffff0000u)) * keep;
+            hi[e] = ptx::cvt_bf16x2(x, y);
+            lo[e] = ptx::cvt_bf16x2(x - __uint_as_float(hi[e] << 16), y - __uint_as_float(hi[e] & 0xffff0000u));
+        }
+        ptx::tmem_st8(tP + i, hi);
+        ptx::tmem_st8(tP + i + 8, lo);
+    }
+    ptx::tc_wait_st();
+}
+
 template <int DP>
 __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_constant__ SharedParams p, const __grid_constant__ TcMaps maps) {
     using namespace ptx;
@@ -794,17 +849,17 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
 
     if (warp == 0) {  // (a lane to an index: one after the other they take a third of a microsecond)
         if (lane < 2) {
-            mbar_init(bar(sm.q_full[lane]), kLoadWarps);
+            mbar_init(bar(sm.q_full[lane]), kScoutWarps);
             mbar_init(bar(sm.q_empty[lane]), kSoftmaxWarps + 1);
             mbar_init(bar(sm.s_full[lane]), 1), mbar_init(bar(sm.pv_done[lane]), 1);
             mbar_init(bar(sm.p_full[lane]), kSoftmaxWarps / 2), mbar_init(bar(sm.team[lane]), kSoftmaxWarps / 2);
             sm.odd[lane] = 0;
         }
         if (lane < kStages) {
-            mbar_init(bar(sm.k_full[lane]), kCopyWarps), mbar_init(bar(sm.v_full[lane]), kCopyWarps);
+            mbar_init(bar(sm.k_full[lane]), 1), mbar_init(bar(sm.v_full[lane]), 1);
             mbar_init(bar(sm.k_empty[lane]), 1), mbar_init(bar(sm.v_empty[lane]), 1);
         }
-        if (lane < kMetas) mbar_init(bar(sm.meta_full[lane]), kLoadWarps), mbar_init(bar(sm.meta_empty[lane]), kSoftmaxWarps + kCopyWarps + 1);
+        if (lane < kMetas) mbar_init(bar(sm.meta_full[lane]), kScoutWarps), mbar_init(bar(sm.meta_empty[lane]), kSoftmaxWarps + kCopyWarps + 1);
         if (lane == 0) {
             mbar_init(bar(sm.both), kSoftmaxWarps), mbar_init(bar(sm.final_), 1);
             sm.abort = 0;
@@ -822,7 +877,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
     static_assert(sizeof(sm.k) >= kMaxBatch * sizeof(uint2), "room for the entries' cost");
     const Start start = find_start<kTcRows, kTcThreads>(p, reinterpret_cast<uint2 *>(sm.k));  // (its barriers: the set-up is seen by all)
     tc_fence_after();
-    if (p.d < DP && blockIdx.x < start.blocks) {  // columns that no copy writes
+    if (p.d < DP && start.left) {  // columns that no copy writes
 #pragma unroll 1
         for (int i = tid; i < (2 + 2 * kStages) * S::kTile / 16; i += kTcThreads) reinterpret_cast<uint4 *>(sm.q)[i] = make_uint4(0, 0, 0, 0);
     }
@@ -833,7 +888,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
     volatile int *abort = &sm.abort;
     const auto wait = [&](const uint64_t &b, uint32_t parity) { return mbar_try_wait(smem_u32(&b), parity) || wait_long(smem_u32(&b), parity, &sm.abort); };
 
-    if (blockIdx.x >= start.blocks) {
+    if (start.left == 0) {
     } else if (warp < kSoftmaxWarps) {
         // ------------------------------------------------------------------ softmax and results
         const int team = warp >> 2, r = tid & 127;  // row: the lane of tensor memory
@@ -878,7 +933,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
                     if (!wait(sm.v_full[stage], c / kStages & 1)) break;
                     __nv_bfloat162 z = __floats2bfloat162_rn(0.f, 0.f);
                     const uint4 *v = reinterpret_cast<const uint4 *>(sm.v[stage]);
-#pragma unroll 4
+#pragma unroll 2
                     for (int i = r; i < kHalves * kTcKeys * 8; i += 128) {
                         const uint4 y = (i >> 3 & (kTcKeys - 1)) < n ? v[i] : make_uint4(0, 0, 0, 0);
                         for (uint32_t w : {y.x, y.y, y.z, y.w})
@@ -893,47 +948,11 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
                 if (live) {
                     const bool any = __any_sync(~0u, lo < hi);
                     const int all_lo = __reduce_max_sync(~0u, lo), all_hi = __reduce_min_sync(~0u, hi);  // keys of all rows
-                    float top = -INFINITY;
+                    if (own == 0) {
+                        uint32_t zero[16] = {};
 #pragma unroll 1
-                    for (int c0 = 0; any && c0 < n; c0 += 32) {
-                        uint32_t v[32];
-                        tmem_ld32(tS + c0, v);
-                        tc_wait_ld();
-                        reg_fence(v);
-                        if (!plain || c0 < all_lo || c0 + 32 > all_hi) {
-                            const uint32_t on = (hi - c0 >= 32 ? ~0u : hi > c0 ? (1u << (hi - c0)) - 1 : 0u) & ~(lo - c0 >= 32 ? ~0u : lo > c0 ? (1u << (lo - c0)) - 1 : 0u);
-#pragma unroll
-                            for (int e = 0; e < 32; ++e)
-                                if (!(on >> e & 1)) v[e] = 0xff800000u;
-                            if (!plain) mask_scores(v, meta, c0, want_row, want_col, below);
-                            tmem_st32(tS + c0, v);
-                            tc_wait_st();
-                        }
-                        top = top_score(v, top);
+                        for (int i = 0; i < DP; i += 16) tmem_st16(tO + i, zero);
                     }
-                    // The base of a row moves when a score exceeds it by kRescale, and with the row's first score.
-                    top *= p.scale_log2;
-                    const bool moves = top > m + kRescale;
-                    if (__any_sync(~0u, moves) || own == 0) {
-                        const float keep = moves ? ex2(m - top) : 1.f;
-                        if (moves) m = top;
-                        const uint64_t keep2 = pack_f32x2(keep, keep);
-                        sum[0] = mul_f32x2(sum[0], keep2), sum[1] = mul_f32x2(sum[1], keep2);
-#pragma unroll 1
-                        for (int i = 0; i < DP; i += 16) {
-                            uint32_t o[16] = {};
-                            if (own > 0) {
-                                tmem_ld16(tO + i, o);
-                                tc_wait_ld();
-                                reg_fence(o);
-                            }
-#pragma unroll
-                            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * keep);
-                            tmem_st16(tO + i, o);
-                        }
-                    }
-                    const float neg = m == -INFINITY ? 0.f : -m;
-                    const uint64_t neg2 = pack_f32x2(neg, neg);
 #pragma unroll 1
                     for (int c0 = 0; c0 < n; c0 += 32) {
                         uint32_t v[32] = {};
@@ -941,7 +960,27 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
                             tmem_ld32(tS + c0, v);
                             tc_wait_ld();
                             reg_fence(v);
-                            weigh(v, scale2, neg2, sum);
+                            if (!plain || c0 < all_lo || c0 + 32 > all_hi) {
+                                const uint32_t on = bits_below(hi - c0) & ~bits_below(lo - c0);
+#pragma unroll
+                                for (int e = 0; e < 32; ++e)
+                                    if (!(on >> e & 1)) v[e] = 0xff800000u;
+                                if (!plain) mask_scores(v, meta, c0, want_row, want_col, below);
+                            }
+                            // The base of a row moves when a score exceeds it by kRescale, and with the row's first score: O, the sum and the
+                            // weights of the tile's keys in front of these follow.
+                            const float top = top_score(v) * p.scale_log2;
+                            const bool moves = top > m + kRescale;
+                            if (__any_sync(~0u, moves)) {
+                                const float keep = moves ? ex2(m - top) : 1.f;
+                                if (moves) m = top;
+                                const uint64_t keep2 = pack_f32x2(keep, keep);
+                                sum[0] = mul_f32x2(sum[0], keep2), sum[1] = mul_f32x2(sum[1], keep2);
+                                if (own > 0) scale_o(tO, DP, keep);
+                                if (c0 > 0) scale_p(tS, c0, keep);
+                            }
+                            const float neg = m == -INFINITY ? 0.f : -m;
+                            weigh(v, scale2, pack_f32x2(neg, neg), sum);
                         }
                         tmem_st32(tS + c0, v);
                     }
@@ -1003,46 +1042,34 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
                     l = fmaf(x.y, f[0], y.y * f[1]);
                 }
                 tc_fence_after();
-                const int state = part_state(part), slot = parts == 0 ? 0 : 1;
-                const size_t whole = (size_t)part.seg * p.B * p.heads + row_of<kTcRows>(p, part, r, member);
-                float *to = p.parts + (size_t)(2 * blockIdx.x + slot) * part_floats(kTcRows, p.d);
                 if (live) {
-                    const bool row = r < part.n_rows;
-                    const int col0 = joined ? team * (DP / 2) : 0, col1 = joined ? col0 + DP / 2 : DP;
-                    const int y_step = state == kAll ? 1 : kTcRows;
-                    float4 *y = state == kAll ? reinterpret_cast<float4 *>(p.whole + whole * p.d + col0) : reinterpret_cast<float4 *>(to) + col0 / 4 * kTcRows + r;
+                    const bool row = r < part.n_rows, all = part.state == kAll;
+                    const int slot = parts == 0 ? 0 : 1, whole = part.seg * p.B * p.heads + row_of<kTcRows>(p, part, r, member);
+                    float *to = all ? p.whole + (size_t)whole * p.d : p.parts + (size_t)(2 * blockIdx.x + slot) * part_floats(kTcRows, p.d) + 4 * r;
+                    float2 *stat = all ? p.whole_stats + whole
+                                       : reinterpret_cast<float2 *>(p.parts + (size_t)(2 * blockIdx.x + slot) * part_floats(kTcRows, p.d) + p.d * kTcRows) + r;
+                    const int step = all ? 4 : 4 * kTcRows, col0 = joined && team ? DP / 2 : 0, col1 = min(p.d, joined ? col0 + DP / 2 : DP);
+                    const uint32_t first_o = tmem + lanes + kTmemO + (joined ? 0 : team * 128);
+                    to += col0 / 4 * step;
 #pragma unroll 1
-                    for (int col = col0; col < col1; col += 16) {
-                        uint32_t o[16], o2[16] = {};
-                        tmem_ld16(tmem + lanes + kTmemO + (joined ? 0 : team * 128) + col, o);
-                        if (joined) tmem_ld16(tmem + lanes + kTmemO + 128 + col, o2);
+                    for (int col = col0; col < col1; col += 8) {
+                        uint32_t o[8], o2[8] = {};
+                        tmem_ld8(first_o + col, o);
+                        if (joined) tmem_ld8(first_o + 128 + col, o2);
                         tc_wait_ld();
                         reg_fence(o);
                         reg_fence(o2);
-                        if (!row) continue;
-                        float x[16];
+                        float x[8];
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) {
-                            x[e] = __uint_as_float(o[e]) * f[0];
-                            if (joined) x[e] = fmaf(__uint_as_float(o2[e]), f[1], x[e]);
-                            if (l == 0.f) x[e] = 0.f;
-                        }
-#pragma unroll
-                        for (int e = 0; e < 16; e += 8) {
-                            if (col + e >= p.d) break;
-                            y[0] = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]), y[y_step] = make_float4(x[e + 4], x[e + 5], x[e + 6], x[e + 7]);
-                            y += 2 * y_step;
+                        for (int e = 0; e < 8; ++e) x[e] = l == 0.f ? 0.f : fmaf(__uint_as_float(o2[e]), f[1], __uint_as_float(o[e]) * f[0]);
+                        if (row) {
+                            *reinterpret_cast<float4 *>(to) = make_float4(x[0], x[1], x[2], x[3]);
+                            *reinterpret_cast<float4 *>(to + step) = make_float4(x[4], x[5], x[6], x[7]);
+                            to += 2 * step;
                         }
                     }
-                    if (row && (!joined || team == 0))
-                        (state == kAll ? p.whole_stats[whole] : reinterpret_cast<float2 *>(to + (size_t)p.d * kTcRows)[r]) = make_float2(m, l);
-                }
-                if (r == 0 && (!joined || team == 0) && state != kGoesOn) {
-                    Joint *joint = joint_of(p, part.seg, part.kv, part.seg == 0 ? part.b : part.b / p.pack, part.tile);
-                    if (state == kAll)
-                        joint->slot = -1;
-                    else
-                        *joint = joint_from(part, start, slot);
+                    if (row && (!joined || team == 0)) *stat = make_float2(m, l);
+                    if (r == 0 && (!joined || team == 0)) put_joint(p, part, slot, start.total);
                 }
                 tc_fence_before();
                 if (joined && !sync(sm.both, boths)) break;  // O has been read
@@ -1054,8 +1081,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
     } else if (warp < kCopyWarp0) {
         // ------------------------------------------------------------------ queries, and which keys are read
         // (These warps meet at barriers: they leave together, when one of them says there that a wait of its own has failed.)
-        const int lt = tid - 32 * kLoadWarp0, lw = warp - kLoadWarp0;
-        Scout<kTcRows> scout = {p, sm.scout, lt};
+        const int lt = tid - 32 * kScoutWarp0, lw = warp - kScoutWarp0;
+        Scout<kTcRows> scout = {p, sm.scout, lt, max(1, maps.run)};
         scout.start(start);
         bool ok = true;
         int t = 0;
@@ -1069,7 +1096,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
             const int chunk = lane % kPer, sub = lane / kPer, n_here = min(part.n_rows - 32 * lw, 32);  // the warp's rows
             const int member = member_of<kTcRows>(p, part, lt), head = part.kv * p.group + part.tile * kTcRows + lt - member * p.group;
             const int64_t mine = (part.b + member) * p.q_batch + head * p.q_head;  // where the thread's row is
-#pragma unroll 4
+#pragma unroll 2
             for (int i = 0; i < n_here; i += kRowsOfCopy) {
                 const int64_t from = __shfl_sync(~0u, mine, i + sub);
                 if (i + sub < n_here && chunk < p.d / 8) cp_async16(S::place(q, 32 * lw + i + sub, chunk), (const __nv_bfloat16 *)p.Q + from + chunk * 8);
@@ -1101,13 +1128,13 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
                 Meta &meta = sm.meta[t % kMetas];
                 if (ok) meta.lo[lt] = meta.hi[lt] = 0;
                 if (any_scout(!ok)) break;
-                Key key = {0, INT32_MAX, kNever + 1, kNever + 1};  // nobody's
+                Key key = {kNowhere, INT32_MAX, kNever + 1, kNever + 1};  // nobody's
                 bool plain = true;
                 if (lt < n) {
                     key = scout.key(lt);
                     const int of = scout.owner_of_key(lt);
                     plain = scout.is_plain(key, of);
-                    if (part.seg == 1) {
+                    if (part.seg == 1 && of != kNobody) {
                         if (lt == 0 || scout.owner_of_key(lt - 1) != of) meta.lo[of] = (uint8_t)lt;
                         if (lt == n - 1 || scout.owner_of_key(lt + 1) != of) meta.hi[of] = (uint8_t)(lt + 1);
                     }
@@ -1116,12 +1143,12 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
                 plain = __all_sync(~0u, plain);
                 if (lane == 0) reinterpret_cast<uint8_t *>(&meta.plain)[lw] = plain;
                 const unsigned before = __shfl_up_sync(~0u, key.at, 1);
-                const unsigned follows = __ballot_sync(~0u, lt < n && ((lt & (maps.run - 1)) == 0 || key.at == before + p.slot16));
+                const unsigned follows = __ballot_sync(~0u, key.at != kNowhere && ((lt & (maps.run - 1)) == 0 || key.at == before + p.slot_step));
                 // (a lane to each of the warp's blocks)
                 const bool whole = maps.run && lane < 32 >> maps.run_log2 && __popc(follows >> (lane << maps.run_log2) << (32 - maps.run)) == maps.run;
                 const unsigned runs = __ballot_sync(~0u, whole);
                 if (lane == 0) meta.runs[lw] = (uint8_t)runs;
-                if (lt == 0) meta.n = n, meta.first = first, meta.last = last, meta.ranged = part.seg;
+                if (lt == 0) meta.n = n, meta.first = first, meta.last = last, meta.ranged = part.seg, meta.x16 = (unsigned)part.kv * p.head16;
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar(sm.meta_full[t % kMetas]));
                 scout.taken(n);
@@ -1135,54 +1162,62 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
         if (lane == 0) mbar_arrive(bar(sm.meta_full[t % kMetas]));
         if (scout.bad) atomicOr(p.cache.status, kCacheBad);
     } else if (warp < kMmaWarp) {
-        // ------------------------------------------------------------------ copies of keys and values
-        const int chunk = lane % kPer, first = (warp - kCopyWarp0) * kRowsOfCopy + lane / kPer;
+        // ------------------------------------------------------------------ copies of keys (one warp) and values (the other)
+        const bool leader = elect_one(), v = warp != kCopyWarp0;
+        const CUtensorMap *map = v ? &maps.v : &maps.k;
+        const int chunk = lane % kPer, sub = lane / kPer, blocks = kTcKeys >> maps.run_log2, per32 = 32 >> maps.run_log2;
         const bool copies = chunk < p.d / 8;
-        bool ok = true;
+        const char *from = (const char *)(v ? p.cache.v : p.cache.k) + chunk * 16;
 #pragma unroll 1
-        for (int t = 0, c = 0; ok; ++t) {
+        for (int t = 0, c = 0;; ++t) {
             const Meta &meta = sm.meta[t % kMetas];
             if (!wait(sm.meta_full[t % kMetas], t / kMetas & 1)) break;
             const int n = meta.n;
             if (n < 0) break;
-            const int stage = c % kStages, rows16 = (n + 15) & ~15, per32 = 32 >> maps.run_log2;
-            // the tile's blocks of rows that are copied whole: a bit each, and to every lane of the first warp a block and half of its columns
-            const uint32_t runs = maps.run ? meta.runs[0] | meta.runs[1] << per32 | meta.runs[2] << 2 * per32 | meta.runs[3] << 3 * per32 : 0u;
-            const int block = lane / kHalves, x = lane % kHalves * 64;
-            const bool whole = block < 4 * per32 && (runs >> block & 1);
-            const unsigned at0 = whole ? meta.at[block * maps.run] : 0;
-            const int bytes = __popc(runs) * kHalves * 128 * maps.run;
-            const bool rest = __popc(runs) * maps.run < rows16;
+            if (n > 0) {
+                const int stage = c % kStages, rows16 = (n + 15) & ~15;
+                const uint64_t &full = v ? sm.v_full[stage] : sm.k_full[stage];
+                if (c >= kStages && !wait(v ? sm.v_empty[stage] : sm.k_empty[stage], (c / kStages - 1) & 1)) break;
+                const uint32_t tile = smem_u32(v ? sm.v[stage] : sm.k[stage]);
+                // blocks of rows that are copied whole: a bit each
+                const uint32_t runs = meta.runs[0] | meta.runs[1] << per32 | meta.runs[2] << 2 * per32 | meta.runs[3] << 3 * per32;
+                const unsigned x16 = meta.x16;
 #pragma unroll 1
-            for (int kv = 0; kv < 2 && n > 0; ++kv) {
-                const uint64_t &full = kv ? sm.v_full[stage] : sm.k_full[stage], &empty = kv ? sm.v_empty[stage] : sm.k_empty[stage];
-                if (c >= kStages && !(ok = wait(empty, (c / kStages - 1) & 1))) break;
-                const uint32_t tile = smem_u32(kv ? sm.v[stage] : sm.k[stage]);
-                const char *from = (const char *)(kv ? p.cache.v : p.cache.k) + chunk * 16;
-                if (warp == kCopyWarp0 && whole)
-                    tma_load_2d(tile + lane % kHalves * S::kHalf + block * maps.run * 128, kv ? &maps.v : &maps.k, (int)(at0 % p.slot16) * 8 + x,
-                                (int)(at0 / p.slot16), bar(full));
-                __syncwarp();
-                // (places ahead of the copies: a load behind a copy waits its turn, 34 clk per copy instead of 10)
-                constexpr int kStep = kCopyWarps * kRowsOfCopy, kBatch = 8;
-#pragma unroll 1
-                for (int row0 = first; rest && row0 < rows16; row0 += kBatch * kStep) {
-                    unsigned at[kBatch];
+                for (int i = 0; runs && i < blocks; ++i) {
+                    if (!(runs >> i & 1)) continue;
+                    const int y = (int)meta.at[i << maps.run_log2];
+                    if (leader) {
 #pragma unroll
-                    for (int i = 0; i < kBatch; ++i) at[i] = meta.at[min(row0 + i * kStep, kTcKeys - 1)];
-#pragma unroll
-                    for (int i = 0; i < kBatch; ++i) {
-                        const int row = row0 + i * kStep;
-                        if (copies && row < rows16 && !(runs >> (row >> maps.run_log2) & 1))
-                            cp_async16_or_zero(S::place(tile, row, chunk), from + (size_t)at[i] * 16, row < n);
+                        for (int h = 0; h < kHalves; ++h) tma_load_2d(tile + h * S::kHalf + (i << maps.run_log2) * 128, map, (int)x16 * 8 + 64 * h, y, bar(full));
                     }
+                    __syncwarp();
                 }
-                __syncwarp();
-                cp_async_arrive(bar(full));
-                __syncwarp();
-                if (lane == 0) mbar_arrive_expect_tx(bar(full), warp == kCopyWarp0 ? bytes : 0);  // (behind all that the warp has asked for)
+                if ((__popc(runs) << maps.run_log2) < rows16) {  // the rest row by row, sixteen at a time
+                    const uint32_t first = tile + (chunk >> 3) * S::kHalf + sub * 128 + (((chunk & 7) ^ sub) << 4);
+                    const char *at_x = from + (size_t)x16 * 16;
+                    const unsigned stride = p.row16 * 16;
+#pragma unroll 1
+                    for (int row0 = 0; row0 < rows16; row0 += 16) {
+                        if (runs >> (row0 >> maps.run_log2) & 1) continue;
+                        // (places ahead of the copies: a load behind a copy waits its turn)
+                        unsigned at[16 / kRowsOfCopy];
+#pragma unroll
+                        for (int i = 0; i < 16 / kRowsOfCopy; ++i) at[i] = meta.at[row0 + i * kRowsOfCopy + sub];
+#pragma unroll
+                        for (int i = 0; i < 16 / kRowsOfCopy; ++i) {
+                            // (the row's low three bits, by which its 16 bytes are permuted: those of sub, and i * kRowsOfCopy's)
+                            const uint32_t to = (first ^ (i * kRowsOfCopy & 7) << 4) + (row0 + i * kRowsOfCopy) * 128;
+                            const bool is = at[i] != kNowhere;
+                            if (copies) cp_async16_or_zero(to, at_x + (is ? (size_t)at[i] * stride : 0), is);
+                        }
+                    }
+                    __syncwarp();
+                    cp_async_arrive(bar(full));
+                    __syncwarp();
+                }
+                if (lane == 0) mbar_arrive_expect_tx(bar(full), (__popc(runs) << maps.run_log2) * kHalves * 128);  // (behind all that has been asked for)
+                ++c;
             }
-            c += n > 0;
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(sm.meta_empty[t % kMetas]));
         }
@@ -1281,78 +1316,89 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
 
 // ---- the results of a row put together
 
-// grid: (eight rows of a kv head, 16 columns); a lane has a row and four columns, the warps take a row's results in turn.
-constexpr int kJoinRows = 8, kJoinWarps = 4;
+// A block has kJoinRows rows of a kv head; a lane has a row and four columns, a warp 16 columns and every `splits`-th of the results.  Who has
+// them is found once for the block.
+constexpr int kJoinRows = 8;
+struct Results {
+    const float *value;     // of the row's first column
+    const float2 *stat;
+    int64_t first, step;    // floats to the first one, and from number i i times to the others
+    int column, parts;      // floats from four columns to the next
+};
 template <typename T, int RT>
-__global__ void __launch_bounds__(32 * kJoinWarps) shared_join_kernel(const __grid_constant__ SharedParams p) {
-    __shared__ float4 s_sum[kJoinWarps][32];
-    __shared__ float2 s_stat[kJoinWarps][32];
+__global__ void __launch_bounds__(1024) shared_join_kernel(const __grid_constant__ SharedParams p, int splits) {
+    __shared__ Results s_of[2][kJoinRows];  // shared tokens, own ones
+    __shared__ float4 s_sum[32][32];
+    __shared__ float2 s_stat[32][32];
     ptx::launch_dependents();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int per_kv = (p.B * p.group + kJoinRows - 1) / kJoinRows, kv = blockIdx.x / per_kv;
-    const int at = (blockIdx.x - kv * per_kv) * kJoinRows + lane % kJoinRows, c4 = blockIdx.y * 4 + lane / kJoinRows;
-    const int b = at / p.group, g = at - b * p.group;
-    const bool exists = b < p.B && c4 * 4 < p.d;
-    // the results: of the shared tokens, and of the own ones
-    const float *value[2];
-    const float2 *stat[2];
-    int64_t step[2];        // from one of them to the next, in floats
-    int64_t from_first[2];  // from the first one to where the steps are counted from: its slot may be another than the next ones'
-    int parts[2] = {0, 0};
-    const size_t out = (size_t)b * p.heads + kv * p.group + g;
-    // (the batch is looked at ahead of the wait: the kernel in front of this one has waited for whoever wrote it before it let this one start)
-    Entry e;
-    entry_of(p, min(b, p.B - 1), &e);
-    ptx::wait_prior_grid();
-    if (exists) {
-#pragma unroll
-        for (int seg = 0; seg < 2; ++seg) {
-            if (seg == 0 && e.count == 0) continue;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, per_kv = (p.B * p.group + kJoinRows - 1) / kJoinRows, kv = blockIdx.x / per_kv;
+    const int at0 = (blockIdx.x - kv * per_kv) * kJoinRows;
+    if (tid < 2 * kJoinRows) {
+        const int seg = tid / kJoinRows, i = tid % kJoinRows, b = by_group(p, at0 + i), g = at0 + i - b * p.group;
+        // (the batch is looked at ahead of the wait: the kernel in front of this one has waited for whoever wrote it before it let this one start)
+        Entry e = {};
+        if (b < p.B) entry_of(p, b, &e);
+        ptx::wait_prior_grid();
+        Results of = {};
+        if (b < p.B && (seg == 1 || e.count > 0)) {
             const int row = (seg == 0 ? b - e.first : b % p.pack) * p.group + g, r = row % RT;
             const Joint joint = *joint_of(p, seg, kv, seg == 0 ? e.first : b / p.pack, row / RT);
             if (joint.slot < 0) {
-                const size_t whole = (size_t)seg * p.B * p.heads + out;
-                value[seg] = p.whole + whole * p.d + c4 * 4, stat[seg] = p.whole_stats + whole;
-                step[seg] = from_first[seg] = 0;
-                parts[seg] = 1;
+                const size_t whole = (size_t)(seg * p.B + b) * p.heads + kv * p.group + g;
+                of = {p.whole + whole * p.d, p.whole_stats + whole, 0, 0, 4, 1};
             } else {
+                // up to the block that has the item's last unit: the last one whose share begins in front of the item's end
+                const int64_t blocks = min((int64_t)joint.total, (int64_t)p.blocks), last = ((int64_t)joint.end * blocks - 1) / joint.total;
                 const float *from = p.parts + 2 * joint.first * part_floats(RT, p.d);
-                value[seg] = from + (size_t)(c4 * RT + r) * 4;
-                stat[seg] = reinterpret_cast<const float2 *>(from + (size_t)p.d * RT) + r;
-                step[seg] = 2 * part_floats(RT, p.d), from_first[seg] = joint.slot * part_floats(RT, p.d);
-                parts[seg] = joint.last - joint.first + 1;
+                of = {from + 4 * r, reinterpret_cast<const float2 *>(from + (size_t)p.d * RT) + r, joint.slot * part_floats(RT, p.d),
+                      2 * part_floats(RT, p.d), 4 * RT, (int)min(last, blocks - 1) - joint.first + 1};
             }
         }
+        s_of[seg][i] = of;
+    } else {
+        ptx::wait_prior_grid();
     }
+    __syncthreads();
+    const int cols = (p.d + 15) / 16, split = warp / cols, c4 = (warp - split * cols) * 4 + lane / kJoinRows, i = lane % kJoinRows;
+    const bool exists = at0 + i < p.B * p.group && c4 * 4 < p.d;
     float m = -INFINITY, l = 0.f;
     float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-    {
+    const auto add = [&](const float2 s, const float4 v) {
+        const float top = fmaxf(m, s.x), base = top == -INFINITY ? 0.f : top, keep = ptx::ex2(m - base), w = ptx::ex2(s.x - base);
+        m = top;
+        l = fmaf(l, keep, s.y * w);
+        sum.x = fmaf(sum.x, keep, v.x * w), sum.y = fmaf(sum.y, keep, v.y * w);
+        sum.z = fmaf(sum.z, keep, v.z * w), sum.w = fmaf(sum.w, keep, v.w * w);
+    };
+#pragma unroll 1
+    for (int seg = 0; seg < 2; ++seg) {
+        const Results of = s_of[seg][i];
+        const int n = exists ? of.parts : 0;
+        constexpr int kBatch = 4;
+#pragma unroll 1
+        for (int k0 = split; k0 < n; k0 += kBatch * splits) {
+            float2 s[kBatch];
+            float4 v[kBatch];
 #pragma unroll
-        for (int seg = 0; seg < 2; ++seg) {
-            for (int i = warp; i < parts[seg]; i += kJoinWarps) {
-                const int64_t off = i == 0 ? from_first[seg] : i * step[seg];
-                const float2 s = *(stat[seg] + off / 2);
-                const float4 v = *reinterpret_cast<const float4 *>(value[seg] + off);
-                const float top = fmaxf(m, s.x), base = top == -INFINITY ? 0.f : top, keep = ptx::ex2(m - base), w = ptx::ex2(s.x - base);
-                m = top;
-                l = fmaf(l, keep, s.y * w);
-                sum.x = fmaf(sum.x, keep, v.x * w), sum.y = fmaf(sum.y, keep, v.y * w);
-                sum.z = fmaf(sum.z, keep, v.z * w), sum.w = fmaf(sum.w, keep, v.w * w);
+            for (int j = 0; j < kBatch; ++j) {
+                const int k = k0 + j * splits;
+                const int64_t off = k == 0 ? of.first : k * of.step;
+                s[j] = k < n ? *(of.stat + off / 2) : make_float2(-INFINITY, 0.f);
+                v[j] = k < n ? *reinterpret_cast<const float4 *>(of.value + off + c4 * of.column) : make_float4(0.f, 0.f, 0.f, 0.f);
             }
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j) add(s[j], v[j]);
         }
     }
-    s_sum[warp][lane] = sum, s_stat[warp][lane] = make_float2(m, l);
-    __syncthreads();
-    if (warp > 0 || !exists) return;
-    for (int w = 0; w < kJoinWarps; ++w) m = fmaxf(m, s_stat[w][lane].x);
-    const float base = m == -INFINITY ? 0.f : m;
-    l = 0.f, sum = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int w = 0; w < kJoinWarps; ++w) {
-        const float f = ptx::ex2(s_stat[w][lane].x - base);
-        const float4 v = s_sum[w][lane];
-        l = fmaf(f, s_stat[w][lane].y, l);
-        sum.x = fmaf(f, v.x, sum.x), sum.y = fmaf(f, v.y, sum.y), sum.z = fmaf(f, v.z, sum.z), sum.w = fmaf(f, v.w, sum.w);
+    if (splits > 1) {
+        s_sum[warp][lane] = sum, s_stat[warp][lane] = make_float2(m, l);
+        __syncthreads();
+        if (split > 0) return;
+        for (int w = warp + cols; w < cols * splits; w += cols) add(s_stat[w][lane], s_sum[w][lane]);
     }
+    if (!exists) return;
+    const int b = by_group(p, at0 + i);
+    const size_t out = (size_t)b * p.heads + kv * p.group + at0 + i - b * p.group;
     T *to = (T *)p.O + out * p.d + c4 * 4;
     put(l == 0.f ? 0.f : sum.x / l, to), put(l == 0.f ? 0.f : sum.y / l, to + 1);
     put(l == 0.f ? 0.f : sum.z / l, to + 2), put(l == 0.f ? 0.f : sum.w / l, to + 3);
@@ -1379,24 +1425,27 @@ Workspace workspace_of(const mate_cache_t *c, int B) {
     return w;
 }
 
-// Boxes of the highest of 8, 16 and 32 rows that a page is a whole number of, where the rows of all heads and pages lie in one such matrix and 64
+// Boxes of 32 or 16 rows, where a page is a whole number of them, the rows of all heads and pages lie in one such matrix and 64
 // columns from a head's first on are its own, or behind the last one.
-TcMaps maps_of(const SharedParams &p, const mate_cache_t *c) {
+TcMaps maps_of(SharedParams &p, const mate_cache_t *c) {
     TcMaps m = {};
     const int64_t slot = c->slot_stride, rows = slot > 0 ? ((int64_t)(c->pages - 1) * c->page_stride + (c->kv_heads - 1) * c->head_stride) / slot + c->page_size : 0;
     int run = 32;
-    while (run > 8 && c->page_size % run != 0) run /= 2;
+    if (c->page_size % run != 0) run = 16;
     bool fits = c->page_size % run == 0 && slot >= c->d && (c->pages == 1 || c->page_stride % slot == 0) && (slot == c->d || c->d % 64 == 0) && rows <= INT32_MAX;
-    for (int h = 0; h < c->kv_heads && fits; ++h) fits = h * c->head_stride % slot + c->d <= slot;
-    if (fits && make_box_map(&m.k, p.cache.k, (size_t)slot, (size_t)rows, (size_t)slot * 2, run) &&
+    if (fits && (c->kv_heads - 1) * (c->head_stride % slot) + c->d <= slot && make_box_map(&m.k, p.cache.k, (size_t)slot, (size_t)rows, (size_t)slot * 2, run) &&
         make_box_map(&m.v, p.cache.v, (size_t)slot, (size_t)rows, (size_t)slot * 2, run))
         m.run = run;
+    if (m.run) {  // places in rows of a slot stride
+        p.page_step = (unsigned)(c->page_stride / slot), p.slot_step = 1, p.head_step = (unsigned)(c->head_stride / slot);
+        p.row16 = (unsigned)(slot / 8), p.head16 = (unsigned)(c->head_stride % slot / 8);
+    }
     for (m.run_log2 = 0; 1 << m.run_log2 < run;) ++m.run_log2;  // (without boxes too: the rows are looked at in blocks all the same)
     return m;
 }
 
 template <typename T, int DP>
-int launch(const SharedParams &p, const mate_cache_t *cache, int blocks, cudaStream_t st) {
+int launch(SharedParams &p, const mate_cache_t *cache, cudaStream_t st) {
     constexpr bool kTc = sizeof(T) == 2;
     constexpr int kRows = kTc ? kTcRows : kSimtRows, kThreads = kTc ? kTcThreads : kSimtThreads;
     constexpr int kSmem = kTc ? 1024 + (int)sizeof(TcSmem<DP>) : (int)sizeof(SimtSmem<DP>);
@@ -1406,15 +1455,17 @@ int launch(const SharedParams &p, const mate_cache_t *cache, int blocks, cudaStr
     if constexpr (kTc) {
         const int rc = attr.ensure((const void *)shared_tc_kernel<DP>, kSmem, cache->device);
         if (rc != MATE_OK) return rc;
-        e = launch_after(shared_tc_kernel<DP>, dim3((unsigned)blocks), kThreads, kSmem, st, p, maps_of(p, cache));
+        const TcMaps maps = maps_of(p, cache);
+        e = launch_after(shared_tc_kernel<DP>, dim3((unsigned)p.blocks), kThreads, kSmem, st, p, maps);
     } else {
         const int rc = attr.ensure((const void *)shared_simt_kernel<DP>, kSmem, cache->device);
         if (rc != MATE_OK) return rc;
-        e = launch_after(shared_simt_kernel<DP>, dim3((unsigned)blocks), kThreads, kSmem, st, p);
+        e = launch_after(shared_simt_kernel<DP>, dim3((unsigned)p.blocks), kThreads, kSmem, st, p);
     }
-    const int64_t joins = (int64_t)p.kv_heads * (((int64_t)p.B * p.group + kJoinRows - 1) / kJoinRows);
-    if (e == cudaSuccess)
-        e = launch_after(shared_join_kernel<T, kRows>, dim3((unsigned)joins, (unsigned)((p.d + 15) / 16)), 32 * kJoinWarps, 0, st, p);
+    // sixteen warps to a block; twice as many where there is not a block to each SM (one sequence in many parts)
+    const int joins = p.kv_heads * ((p.B * p.group + kJoinRows - 1) / kJoinRows), cols = (p.d + 15) / 16;
+    const int splits = std::min(8, (joins < n_sms(cache->device) ? 32 : 16) / cols);
+    if (e == cudaSuccess) e = launch_after(shared_join_kernel<T, kRows>, dim3((unsigned)joins), 32 * cols * splits, 0, st, p, splits);
     return e == cudaSuccess ? MATE_OK : MATE_ERR_CUDA;
 }
 
@@ -1470,7 +1521,8 @@ int mate_attn_decode_shared(const mate_cache_t *cache, int layer, const void *Q,
     };
     quotients(cache->page_size, &p.page_mul, &p.page_shift);
     quotients(p.group, &p.group_mul, &p.group_shift);
-    p.page16 = (unsigned)(cache->page_stride / vec), p.head16 = (unsigned)(cache->head_stride / vec), p.slot16 = (unsigned)(cache->slot_stride / vec);
+    p.page_step = (unsigned)(cache->page_stride / vec), p.slot_step = (unsigned)(cache->slot_stride / vec), p.head_step = (unsigned)(cache->head_stride / vec);
+    p.row16 = 1, p.head16 = 0;
     char *ws = static_cast<char *>(workspace);
     p.joints = reinterpret_cast<Joint *>(ws + w.joints);
     p.whole_stats = reinterpret_cast<float2 *>(ws + w.stats);
@@ -1482,9 +1534,9 @@ int mate_attn_decode_shared(const mate_cache_t *cache, int layer, const void *Q,
         p.scale_log2 = std::fmax(std::fabs(p.scale_log2), 0x1p-126f);
     }
     cudaStream_t st = (cudaStream_t)stream;
-    const int blocks = n_blocks(cache);
-    if (cache->dtype == MATE_F32) return cache->d <= 64 ? launch<float, 64>(p, cache, blocks, st) : launch<float, 128>(p, cache, blocks, st);
-    return cache->d <= 64 ? launch<__nv_bfloat16, 64>(p, cache, blocks, st) : launch<__nv_bfloat16, 128>(p, cache, blocks, st);
+    p.blocks = n_blocks(cache);
+    if (cache->dtype == MATE_F32) return cache->d <= 64 ? launch<float, 64>(p, cache, st) : launch<float, 128>(p, cache, st);
+    return cache->d <= 64 ? launch<__nv_bfloat16, 64>(p, cache, st) : launch<__nv_bfloat16, 128>(p, cache, st);
 }
 
 }  // extern "C"
