@@ -126,15 +126,22 @@ struct Start {
     unsigned total, at, in;
     int left, batch;
 };
-// All threads call it.  `cost`: [B] in shared memory, free afterwards.
+// What the threads look up for it is kept for the first batch, as far as there is room.
+constexpr int kKept = 224;
+struct Found {
+    uint2 cost[kMaxBatch];
+    Entry entries[kKept];
+};
+// All threads call it.  `found`: in shared memory, free when the first batch has been taken over.
 template <int RT, int NT>
-__device__ Start find_start(const SharedParams &p, uint2 *cost) {
+__device__ Start find_start(const SharedParams &p, Found &found) {
+    uint2 *cost = found.cost;
     __shared__ unsigned s_sum[32];
     __shared__ Start s_start;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, batches = (p.B + p.pack - 1) / p.pack;
 #pragma unroll 1
     for (int b = tid; b < p.B; b += NT) {
-        Entry e;
+        Entry mine, &e = b < kKept ? found.entries[b] : mine;
         entry_of(p, b, &e);
         cost[b] = make_uint2(units_of(e.own1 - e.own0), leads(e, b) ? p.kv_heads * group_tiles<RT>(p, e) * (kOver + units_of(e.shared)) : 0);
         if (e.bad && blockIdx.x == 0) atomicOr(p.cache.status, kCacheBad);
@@ -239,8 +246,9 @@ struct alignas(16) Key {
 };
 constexpr int kList = 512, kScouts = 128;
 constexpr unsigned kNowhere = ~0u;
+constexpr int kUnits = 8;  // of a look
 
-// kScouts threads walk the parts of the block's share and look through their tokens, four units at a time, a warp to each; the keys that
+// kScouts threads walk the parts of the block's share and look through their tokens, eight units at a time, two to a warp; the keys that
 // count go onto a list.  The next ones' ids, and the pages of the ones behind them, are on their way meanwhile.  Barrier 1 is theirs.
 //
 // Units of own tokens are numbered through over the entries of the batch, each entry beginning with a new one.
@@ -252,9 +260,9 @@ struct ScoutSmem {
     Wishes<RT> wishes[2];    // of the parts in turn
     Key list[kList];         // what look() writes is seen behind the next barrier
     uint8_t owners[kList];   // entries of the batch
-    int counts[2][4];        // of the warps' keys; plus kDense
+    int counts[2][8];        // of the units' keys; plus kDense
 };
-constexpr int kDense = 64, kNobody = 255;
+constexpr int kDense = 64, kNobody = 255, kRun = 16;
 // Where the loads of a look stand.
 struct Asked {
     int j, owner, page;
@@ -264,7 +272,7 @@ template <int RT>
 struct Scout {
     const SharedParams &p;
     ScoutSmem<RT> &sm;
-    int tid, run;  // run: keys that lie one behind the other are copied by that many (1: one by one)
+    int tid, run;  // run: keys that lie one behind the other are copied by that many, kRun or 1
     // the walk: next item of the share
     int batch, entry, tiles, n_units, item, u;  // entry: that leads (of the batch), kScouts: own tokens; tiles of rows, units of an item of it
     unsigned in, at_unit;                       // units to pass over yet; number of the next one among those of all
@@ -273,21 +281,28 @@ struct Scout {
     // the looks at the present part
     int seg, next, end, pending, list_at, looks;  // next, end: units
     unsigned head_at;
-    Asked asked;
-    unsigned at;
-    int j, owner, row, col;
-    bool there, first, bad;
+    Asked asked[2];
+    struct {
+        unsigned at;
+        int j, owner, row, col;
+        bool there, first;
+    } got[2];
+    int leader, shared_end;
+    bool bad;
 
     __device__ static void sync() { asm volatile("barrier.cta.sync 1, 128;" ::: "memory"); }
     __device__ int entries() const { return min(p.pack, p.B - batch * p.pack); }
-    __device__ void hold() {
+    __device__ void hold(const Entry *found) {
         held = batch;
         sync();
         int units = 0;
         bool first = false;
         if (tid < entries()) {
             const int b = batch * p.pack + tid;
-            entry_of(p, b, sm.entries + tid);
+            if (found && b < kKept)
+                sm.entries[tid] = found[b];
+            else
+                entry_of(p, b, sm.entries + tid);
             const Entry &e = sm.entries[tid];
             units = units_of(e.own1 - e.own0), first = leads(e, b);
         }
@@ -313,17 +328,18 @@ struct Scout {
         }
         return kScouts;
     }
-    __device__ void start(const Start &from) {
+    __device__ void start(const Start &from, const Found &found) {
         batch = from.batch, in = from.in, at_unit = from.at, left = from.left;
-        held = -1, parts = looks = item = u = tiles = n_units = entry = 0, bad = false;
+        parts = looks = item = u = tiles = n_units = 0, entry = -1, bad = false;
         if (tid == 0) sm.wishes[0].clear();
+        hold(found.entries);
     }
     // The next part of the share.  (It comes to an end whatever it finds: every part takes a unit off the share.)
     __device__ bool next_part(Part &part) {
 #pragma unroll 1
         while (left > 0 && batch * p.pack < p.B) {
             if (held != batch) {
-                hold();
+                hold(nullptr);
                 entry = -1, tiles = item = 0;
             }
             if (item < p.kv_heads * tiles) {
@@ -358,47 +374,57 @@ struct Scout {
         left = 0;
         return false;
     }
-    // Who the warp's 32 tokens of unit `unit` belong to, and their pages.
-    __device__ void ask_page(int unit) {
-        asked = {0, 0, -1, false, false};
-        if (unit >= end) return;
+    // Who the tokens of the warp's units from `unit` on belong to, and their pages.
+    __device__ void ask_pages(int unit0) {
         const int lane = tid & 31;
-        int first_token = 0, stop, from = 0;
-        if (seg == 0) {
-            asked.owner = leader;
-            stop = min(sm.entries[leader].shared, sm.entries[leader].len);
-        } else {
-            int n = 0;  // entries that begin at the unit or in front of it
 #pragma unroll
-            for (int i = 0; i < kScouts / 32; ++i) n += sm.before[32 * i + lane] <= unit;
-            asked.owner = __reduce_add_sync(~0u, n) - 1;
-            // (of entries without tokens the last one that begins there is found: it is the one behind them)
-            const Entry &e = sm.entries[asked.owner];
-            first_token = e.own0, stop = e.own1, from = sm.before[asked.owner];
-            asked.first = unit == from;
+        for (int k = 0; k < 2; ++k) {
+            const int unit = unit0 + 2 * (tid >> 5) + k;
+            Asked &a = asked[k];
+            a = {0, 0, -1, false, false};
+            if (unit >= end) continue;
+            int first_token = 0, stop, from = 0;
+            if (seg == 0) {
+                a.owner = leader;
+                stop = shared_end;
+            } else {
+                int n = 0;  // entries that begin at the unit or in front of it
+#pragma unroll
+                for (int i = 0; i < kScouts / 32; ++i) n += sm.before[32 * i + lane] <= unit;
+                a.owner = __reduce_add_sync(~0u, n) - 1;
+                // (of entries without tokens the last one that begins there is found: it is the one behind them)
+                const Entry &e = sm.entries[a.owner];
+                first_token = e.own0, stop = e.own1, from = sm.before[a.owner];
+                a.first = unit == from;
+            }
+            const int s = sm.entries[a.owner].s;
+            a.j = first_token + (unit - from) * kUnit + lane;
+            a.there = a.j < stop && s >= 0;
+            if (a.there) a.page = p.cache.table[(size_t)s * p.cache.width + page_index(p, a.j)];
         }
-        const int s = sm.entries[asked.owner].s;
-        asked.j = first_token + (unit - from) * kUnit + lane;
-        asked.there = asked.j < stop && s >= 0;
-        if (asked.there) asked.page = p.cache.table[(size_t)s * p.cache.width + page_index(p, asked.j)];
     }
-    __device__ void ask_ids() {  // of the tokens whose page has been asked for
-        j = asked.j, owner = asked.owner, first = asked.first;
-        there = asked.there && in_range(asked.page, p.cache.pages);
-        if (asked.there && !there) bad = true;
-        if (!there) return;
-        const int slot = j - page_index(p, j) * p.cache.page_size, id = asked.page * p.cache.page_size + slot;
-        row = p.cache.row_ids[id], col = p.cache.col_ids[id];
-        at = (unsigned)asked.page * p.page_step + (unsigned)slot * p.slot_step + head_at;
+    __device__ void ask_ids() {  // of the tokens whose pages have been asked for
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const Asked &a = asked[k];
+            auto &g = got[k];
+            g.j = a.j, g.owner = a.owner, g.first = a.first;
+            g.there = a.there && in_range(a.page, p.cache.pages);
+            if (a.there && !g.there) bad = true;
+            if (!g.there) continue;
+            const int slot = a.j - page_index(p, a.j) * p.cache.page_size, id = a.page * p.cache.page_size + slot;
+            g.row = p.cache.row_ids[id], g.col = p.cache.col_ids[id];
+            g.at = (unsigned)a.page * p.page_step + (unsigned)slot * p.slot_step + head_at;
+        }
     }
-    int leader;
     // Behind a barrier that the last look at the part before it is in front of.
     __device__ void begin(const Part &part, Rows<RT> &rows) {
         seg = part.seg, leader = part.b - batch * p.pack;
         next = part.from, end = seg == 1 ? min(part.to, sm.before[kScouts]) : part.to;
         head_at = (unsigned)part.kv * p.head_step;
         pending = list_at = 0;
-        ask_page(next + (tid >> 5));
+        if (seg == 0) shared_end = min(sm.entries[leader].shared, sm.entries[leader].len);
+        ask_pages(next);
         Wishes<RT> &w = sm.wishes[parts & 1];
         ++parts;
         if (tid == 0) sm.wishes[parts & 1].clear();
@@ -425,53 +451,59 @@ struct Scout {
         if (!again && (want_row != kNever || want_col != kNever)) w.want[atomicAdd(&w.n, 1)] = make_int2(want_row, want_col);
         __syncwarp();
         ask_ids();
-        ask_page(next + 4 + (tid >> 5));
+        ask_pages(next + kUnits);
         sync();
     }
     __device__ const Wishes<RT> &wishes() const { return sm.wishes[parts + 1 & 1]; }  // of the present part
     __device__ bool more() const { return next < end; }
     __device__ void look() {
         const Wishes<RT> &w = wishes();
-        Key key = {at, j, row, col};
-        const int of = owner;
-        const bool was_there = there, was_first = first;
-        bool is = there && row >= 0 && col >= 0;
-        if (is) {
-            if (row == MATE_ID_TEXT || col == MATE_ID_TEXT) key.place = -1;
-            if (seg == 0) {
-                is = key.place < w.most;
-#pragma unroll 1
-                for (int i = 0; i < w.n && !is; ++i) is = row == w.want[i].x || col == w.want[i].y;
-            } else {
-                const Entry &e = sm.entries[of];
-                is = e.q_row == MATE_ID_TEXT || e.q_col == MATE_ID_TEXT || key.place < e.prefix || ((w.views & 1) && row == e.q_row) ||
-                     ((w.views & 2) && col == e.q_col);
-            }
-        }
-        next += 4;
-        if (next < end) {
-            __syncwarp();
-            ask_ids();
-            __syncwarp();
-            ask_page(next + 4 + (tid >> 5));
-        }
-        __syncwarp();
-        const unsigned those = __ballot_sync(~0u, is), valid = __ballot_sync(~0u, was_there);
         const int lane = tid & 31, warp = tid >> 5;
         int *count = sm.counts[looks++ & 1];
-        // Own tokens of which none is left out begin at a multiple of `run`, so that they are copied in runs; in front of them are nobody's.
-        const bool dense = was_first && those == valid && __popc(those) >= run;
-        if (lane == 0) count[warp] = __popc(those) + (dense ? kDense : 0);
-        sync();
-        int to = pending, gap = 0, all = pending;
+        Key key[2];
+        int of[2];
+        unsigned those[2];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int k = 0; k < 2; ++k) {
+            auto &g = got[k];
+            key[k] = {g.at, g.j, g.row, g.col}, of[k] = g.owner;
+            bool is = g.there && g.row >= 0 && g.col >= 0;
+            if (is) {
+                if (g.row == MATE_ID_TEXT || g.col == MATE_ID_TEXT) key[k].place = -1;
+                if (seg == 0) {
+                    is = key[k].place < w.most;
+#pragma unroll 1
+                    for (int i = 0; i < w.n && !is; ++i) is = g.row == w.want[i].x || g.col == w.want[i].y;
+                } else {
+                    const Entry &e = sm.entries[of[k]];
+                    is = e.q_row == MATE_ID_TEXT || e.q_col == MATE_ID_TEXT || key[k].place < e.prefix || ((w.views & 1) && g.row == e.q_row) ||
+                         ((w.views & 2) && g.col == e.q_col);
+                }
+            }
+            those[k] = __ballot_sync(~0u, is);
+            // Own tokens of which none is left out begin at a multiple of `run`, so that they are copied in runs; in front of them are nobody's.
+            const bool dense = g.first && those[k] == __ballot_sync(~0u, g.there) && __popc(those[k]) >= run;
+            if (lane == 0) count[2 * warp + k] = __popc(those[k]) + (dense ? kDense : 0);
+        }
+        next += kUnits;
+        if (next < end) {
+            ask_ids();
+            __syncwarp();
+            ask_pages(next + kUnits);
+        }
+        sync();
+        int to[2], gap[2], all = pending;
+#pragma unroll
+        for (int i = 0; i < kUnits; ++i) {
             const int c = count[i], up = c >= kDense ? (all + run - 1) & -run : all;
-            if (i == warp) to = up, gap = up - all;
+            if (i >> 1 == warp) to[i & 1] = up, gap[i & 1] = up - all;
             all = up + (c & (kDense - 1));
         }
-        if (lane < gap) put_key(to - gap + lane, {kNowhere, INT32_MAX, kNever + 1, kNever + 1}, kNobody);
-        if (is) put_key(to + __popc(those & ((1u << lane) - 1)), key, of);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            if (lane < gap[k]) put_key(to[k] - gap[k] + lane, {kNowhere, INT32_MAX, kNever + 1, kNever + 1}, kNobody);
+            if (those[k] >> lane & 1) put_key(to[k] + __popc(those[k] & ((1u << lane) - 1)), key[k], of[k]);
+        }
         pending = all;
     }
     __device__ void put_key(int i, const Key &key, int of) {
@@ -512,19 +544,22 @@ struct SimtSmem {
 __device__ __forceinline__ void load16(const float *from, float *to) { *reinterpret_cast<float4 *>(to) = *reinterpret_cast<const float4 *>(from); }
 
 template <int DP>
-__global__ void __launch_bounds__(kSimtThreads) shared_simt_kernel(const __grid_constant__ SharedParams p) {
+__global__ void __launch_bounds__(kSimtThreads, 2) shared_simt_kernel(const __grid_constant__ SharedParams p) {
     extern __shared__ __align__(16) char smem_raw[];
     auto &sm = *reinterpret_cast<SimtSmem<DP> *>(smem_raw);
     constexpr int kVec = 4, kCols = DP / 32, kR = kSimtRows / (kSimtThreads / 32);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, r0 = warp * kR;
     ptx::wait_prior_grid();
-    static_assert(sizeof(sm.q) + sizeof(sm.k) + sizeof(sm.v) + sizeof(sm.s) >= kMaxBatch * sizeof(uint2), "room for the entries' cost");
-    const Start start = find_start<kSimtRows, kSimtThreads>(p, reinterpret_cast<uint2 *>(smem_raw));
+    static_assert(sizeof(sm.q) + sizeof(sm.k) + sizeof(sm.v) + sizeof(sm.s) >= sizeof(Found), "room for the entries");
+    Found &found = *reinterpret_cast<Found *>(smem_raw);
+    const Start start = find_start<kSimtRows, kSimtThreads>(p, found);
     if (start.left == 0) return;
-    for (int i = tid; i < (int)(sizeof(SimtSmem<DP>) / 4); i += kSimtThreads) reinterpret_cast<uint32_t *>(smem_raw)[i] = 0;  // columns that nobody writes
     Scout<kSimtRows> scout = {p, sm.scout, tid, 1};
+    if (tid < kScouts) scout.start(start, found);
     __syncthreads();
-    if (tid < kScouts) scout.start(start);
+    for (int i = tid; i < (int)((sizeof(sm.q) + sizeof(sm.k) + sizeof(sm.v) + sizeof(sm.s)) / 4); i += kSimtThreads)
+        reinterpret_cast<uint32_t *>(smem_raw)[i] = 0;  // columns that nobody writes
+    __syncthreads();
     for (int n_parts = 0;; ++n_parts) {
         Part part;
         if (tid < kScouts) {
@@ -677,7 +712,7 @@ __global__ void __launch_bounds__(kSimtThreads) shared_simt_kernel(const __grid_
 constexpr int kTcRows = 128, kTcKeys = 128;
 constexpr int kSoftmaxWarps = 8;              // two teams, which take the tiles in turn; a thread to a row
 constexpr int kScoutWarp0 = kSoftmaxWarps, kScoutWarps = kScouts / 32;
-constexpr int kCopyWarp0 = kScoutWarp0 + kScoutWarps, kCopyWarps = 2;  // keys, values
+constexpr int kCopyWarp0 = kScoutWarp0 + kScoutWarps, kCopyWarps = 3;  // keys, values, a share of the rows of both that are copied one by one
 constexpr int kMmaWarp = kCopyWarp0 + kCopyWarps;
 constexpr int kTcThreads = 32 * (kMmaWarp + 1);
 constexpr int kMetas = 4;                     // tiles whose keys are known
@@ -701,7 +736,7 @@ struct alignas(16) Meta {
     uint32_t plain;      // 0x01010101: every row attends every key that is for it
     int ranged;          // keys lo[m] to hi[m] are for the rows of entry m, else all for all
     unsigned x16;        // where a row's elements begin, in 16 bytes
-    uint8_t runs[4];     // of every 32 keys: blocks of TcMaps.run keys that lie one behind the other
+    uint8_t runs[4];     // of every 32 keys, a bit for each kRun of them: they lie one behind the other
     alignas(16) int place[kTcKeys];  // (read four at a time)
     alignas(16) int row[kTcKeys];
     alignas(16) int col[kTcKeys];
@@ -712,7 +747,7 @@ struct alignas(16) Meta {
 // 64 elements.
 struct TcMaps {
     CUtensorMap k, v;
-    int run, run_log2;  // rows of a box, 16 or 32; 0: every row is copied by itself
+    int run;  // rows of a box: kRun; 0: every row is copied by itself
 };
 template <int DP>
 struct TcSmem {  // from a multiple of 1024 bytes on
@@ -802,14 +837,14 @@ __device__ __forceinline__ void weigh(uint32_t (&v)[32], uint64_t scale2, uint64
 // The row's O, or its weights of the first n keys of a tile, times `keep` (rarely).
 __device__ __noinline__ void scale_o(uint32_t tO, int n, float keep) {
 #pragma unroll 1
-    for (int i = 0; i < n; i += 8) {
-        uint32_t o[8];
-        ptx::tmem_ld8(tO + i, o);
+    for (int i = 0; i < n; i += 16) {
+        uint32_t o[16];
+        ptx::tmem_ld16(tO + i, o);
         ptx::tc_wait_ld();
         ptx::reg_fence(o);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * keep);
-        ptx::tmem_st8(tO + i, o);
+        for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * keep);
+        ptx::tmem_st16(tO + i, o);
     }
     ptx::tc_wait_st();
 }
@@ -856,7 +891,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
             sm.odd[lane] = 0;
         }
         if (lane < kStages) {
-            mbar_init(bar(sm.k_full[lane]), 1), mbar_init(bar(sm.v_full[lane]), 1);
+            mbar_init(bar(sm.k_full[lane]), 2), mbar_init(bar(sm.v_full[lane]), 2);
             mbar_init(bar(sm.k_empty[lane]), 1), mbar_init(bar(sm.v_empty[lane]), 1);
         }
         if (lane < kMetas) mbar_init(bar(sm.meta_full[lane]), kScoutWarps), mbar_init(bar(sm.meta_empty[lane]), kSoftmaxWarps + kCopyWarps + 1);
@@ -874,10 +909,14 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
     tc_fence_before();
     wait_prior_grid();
     launch_dependents();  // (what is launched next waits for the end of this before it reads results)
-    static_assert(sizeof(sm.k) >= kMaxBatch * sizeof(uint2), "room for the entries' cost");
-    const Start start = find_start<kTcRows, kTcThreads>(p, reinterpret_cast<uint2 *>(sm.k));  // (its barriers: the set-up is seen by all)
+    static_assert(sizeof(sm.k) >= sizeof(Found), "room for the entries");
+    Found &found = *reinterpret_cast<Found *>(sm.k);
+    const Start start = find_start<kTcRows, kTcThreads>(p, found);  // (its barriers: the set-up is seen by all)
     tc_fence_after();
-    if (p.d < DP && start.left) {  // columns that no copy writes
+    Scout<kTcRows> scout = {p, sm.scout, tid - 32 * kScoutWarp0, max(1, maps.run)};
+    if (start.left && warp >= kScoutWarp0 && warp < kCopyWarp0) scout.start(start, found);
+    if (p.d < DP) {  // columns that no copy writes
+        __syncthreads();
 #pragma unroll 1
         for (int i = tid; i < (2 + 2 * kStages) * S::kTile / 16; i += kTcThreads) reinterpret_cast<uint4 *>(sm.q)[i] = make_uint4(0, 0, 0, 0);
     }
@@ -971,9 +1010,10 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
                             // weights of the tile's keys in front of these follow.
                             const float top = top_score(v) * p.scale_log2;
                             const bool moves = top > m + kRescale;
-                            if (__any_sync(~0u, moves)) {
-                                const float keep = moves ? ex2(m - top) : 1.f;
-                                if (moves) m = top;
+                            const bool first_score = m == -INFINITY;  // (there is nothing yet that would have to follow)
+                            const float keep = moves && !first_score ? ex2(m - top) : 1.f;
+                            if (moves) m = top;
+                            if (__any_sync(~0u, moves && !first_score)) {
                                 const uint64_t keep2 = pack_f32x2(keep, keep);
                                 sum[0] = mul_f32x2(sum[0], keep2), sum[1] = mul_f32x2(sum[1], keep2);
                                 if (own > 0) scale_o(tO, DP, keep);
@@ -1052,20 +1092,24 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
                     const uint32_t first_o = tmem + lanes + kTmemO + (joined ? 0 : team * 128);
                     to += col0 / 4 * step;
 #pragma unroll 1
-                    for (int col = col0; col < col1; col += 8) {
-                        uint32_t o[8], o2[8] = {};
-                        tmem_ld8(first_o + col, o);
-                        if (joined) tmem_ld8(first_o + 128 + col, o2);
+                    for (int col = col0; col < col1; col += 16) {
+                        uint32_t o[16], o2[16] = {};
+                        tmem_ld16(first_o + col, o);
+                        if (joined) tmem_ld16(first_o + 128 + col, o2);
                         tc_wait_ld();
                         reg_fence(o);
                         reg_fence(o2);
-                        float x[8];
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) x[e] = l == 0.f ? 0.f : fmaf(__uint_as_float(o2[e]), f[1], __uint_as_float(o[e]) * f[0]);
+                        for (int e = 0; e < 16; ++e)
+                            o[e] = l == 0.f ? 0u : __float_as_uint(fmaf(__uint_as_float(o2[e]), f[1], __uint_as_float(o[e]) * f[0]));
                         if (row) {
-                            *reinterpret_cast<float4 *>(to) = make_float4(x[0], x[1], x[2], x[3]);
-                            *reinterpret_cast<float4 *>(to + step) = make_float4(x[4], x[5], x[6], x[7]);
-                            to += 2 * step;
+                            *reinterpret_cast<uint4 *>(to) = make_uint4(o[0], o[1], o[2], o[3]);
+                            *reinterpret_cast<uint4 *>(to + step) = make_uint4(o[4], o[5], o[6], o[7]);
+                            if (col + 8 < p.d) {
+                                *reinterpret_cast<uint4 *>(to + 2 * step) = make_uint4(o[8], o[9], o[10], o[11]);
+                                *reinterpret_cast<uint4 *>(to + 3 * step) = make_uint4(o[12], o[13], o[14], o[15]);
+                            }
+                            to += 4 * step;
                         }
                     }
                     if (row && (!joined || team == 0)) *stat = make_float2(m, l);
@@ -1082,8 +1126,6 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
         // ------------------------------------------------------------------ queries, and which keys are read
         // (These warps meet at barriers: they leave together, when one of them says there that a wait of its own has failed.)
         const int lt = tid - 32 * kScoutWarp0, lw = warp - kScoutWarp0;
-        Scout<kTcRows> scout = {p, sm.scout, lt, max(1, maps.run)};
-        scout.start(start);
         bool ok = true;
         int t = 0;
         Part part;
@@ -1096,7 +1138,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
             const int chunk = lane % kPer, sub = lane / kPer, n_here = min(part.n_rows - 32 * lw, 32);  // the warp's rows
             const int member = member_of<kTcRows>(p, part, lt), head = part.kv * p.group + part.tile * kTcRows + lt - member * p.group;
             const int64_t mine = (part.b + member) * p.q_batch + head * p.q_head;  // where the thread's row is
-#pragma unroll 2
+#pragma unroll 4
             for (int i = 0; i < n_here; i += kRowsOfCopy) {
                 const int64_t from = __shfl_sync(~0u, mine, i + sub);
                 if (i + sub < n_here && chunk < p.d / 8) cp_async16(S::place(q, 32 * lw + i + sub, chunk), (const __nv_bfloat16 *)p.Q + from + chunk * 8);
@@ -1143,10 +1185,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
                 plain = __all_sync(~0u, plain);
                 if (lane == 0) reinterpret_cast<uint8_t *>(&meta.plain)[lw] = plain;
                 const unsigned before = __shfl_up_sync(~0u, key.at, 1);
-                const unsigned follows = __ballot_sync(~0u, key.at != kNowhere && ((lt & (maps.run - 1)) == 0 || key.at == before + p.slot_step));
-                // (a lane to each of the warp's blocks)
-                const bool whole = maps.run && lane < 32 >> maps.run_log2 && __popc(follows >> (lane << maps.run_log2) << (32 - maps.run)) == maps.run;
-                const unsigned runs = __ballot_sync(~0u, whole);
+                const unsigned follows = __ballot_sync(~0u, key.at != kNowhere && (lt % kRun == 0 || key.at == before + p.slot_step));
+                const unsigned runs = maps.run ? ((follows & 0xffff) == 0xffff ? 1 : 0) | (follows >> 16 == 0xffff ? 2 : 0) : 0;
                 if (lane == 0) meta.runs[lw] = (uint8_t)runs;
                 if (lt == 0) meta.n = n, meta.first = first, meta.last = last, meta.ranged = part.seg, meta.x16 = (unsigned)part.kv * p.head16;
                 __syncwarp();
@@ -1162,60 +1202,66 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
         if (lane == 0) mbar_arrive(bar(sm.meta_full[t % kMetas]));
         if (scout.bad) atomicOr(p.cache.status, kCacheBad);
     } else if (warp < kMmaWarp) {
-        // ------------------------------------------------------------------ copies of keys (one warp) and values (the other)
-        const bool leader = elect_one(), v = warp != kCopyWarp0;
-        const CUtensorMap *map = v ? &maps.v : &maps.k;
-        const int chunk = lane % kPer, sub = lane / kPer, blocks = kTcKeys >> maps.run_log2, per32 = 32 >> maps.run_log2;
-        const bool copies = chunk < p.d / 8;
-        const char *from = (const char *)(v ? p.cache.v : p.cache.k) + chunk * 16;
+        // ------------------------------------------------------------------ copies of keys (first warp) and values (second)
+        // Runs by one lane, the rest row by row: of rows of 128 elements the third warp has the second half, of shorter ones every other
+        // sixteen rows.
+        const bool leader = elect_one();
+        const int w = warp - kCopyWarp0, part = w == 2, h = DP == 128 ? part : 0;
+        const int chunk = lane & 7, sub = lane >> 3;  // of a copy of four rows
+        const bool copies = h * 8 + chunk < p.d / 8;
+        const unsigned stride = p.row16 * 16;
+        bool ok = true;
 #pragma unroll 1
-        for (int t = 0, c = 0;; ++t) {
+        for (int t = 0, c = 0; ok; ++t) {
             const Meta &meta = sm.meta[t % kMetas];
             if (!wait(sm.meta_full[t % kMetas], t / kMetas & 1)) break;
             const int n = meta.n;
             if (n < 0) break;
             if (n > 0) {
-                const int stage = c % kStages, rows16 = (n + 15) & ~15;
-                const uint64_t &full = v ? sm.v_full[stage] : sm.k_full[stage];
-                if (c >= kStages && !wait(v ? sm.v_empty[stage] : sm.k_empty[stage], (c / kStages - 1) & 1)) break;
-                const uint32_t tile = smem_u32(v ? sm.v[stage] : sm.k[stage]);
-                // blocks of rows that are copied whole: a bit each
-                const uint32_t runs = meta.runs[0] | meta.runs[1] << per32 | meta.runs[2] << 2 * per32 | meta.runs[3] << 3 * per32;
-                const unsigned x16 = meta.x16;
-#pragma unroll 1
-                for (int i = 0; runs && i < blocks; ++i) {
-                    if (!(runs >> i & 1)) continue;
-                    const int y = (int)meta.at[i << maps.run_log2];
-                    if (leader) {
+                const int stage = c % kStages;
+                const uint32_t blocks = (2u << ((n - 1) / kRun)) - 1;  // that have a key
+                const uint32_t runs = blocks & (meta.runs[0] | meta.runs[1] << 2 | meta.runs[2] << 4 | meta.runs[3] << 6);
+                const uint32_t mine = blocks & ~runs & (DP == 128 ? 0xff : part ? 0xaa : 0x55);
+                const int x16 = (int)meta.x16;
+                unsigned at[8];
 #pragma unroll
-                        for (int h = 0; h < kHalves; ++h) tma_load_2d(tile + h * S::kHalf + (i << maps.run_log2) * 128, map, (int)x16 * 8 + 64 * h, y, bar(full));
+                for (int i = 0; i < 8; ++i) at[i] = meta.at[i * kRun];
+#pragma unroll 1
+                for (int v = w & 1; v <= (w > 0); ++v) {
+                    const uint64_t &full = v ? sm.v_full[stage] : sm.k_full[stage];
+                    const uint32_t tile = smem_u32(v ? sm.v[stage] : sm.k[stage]);
+                    if (c >= kStages && !(ok = wait(v ? sm.v_empty[stage] : sm.k_empty[stage], (c / kStages - 1) & 1))) break;
+                    if (!part && runs && leader) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            if (runs >> i & 1)
+#pragma unroll
+                                for (int k = 0; k < kHalves; ++k)
+                                    tma_load_2d(tile + k * S::kHalf + i * kRun * 128, v ? &maps.v : &maps.k, x16 * 8 + 64 * k, (int)at[i], bar(full));
                     }
                     __syncwarp();
-                }
-                if ((__popc(runs) << maps.run_log2) < rows16) {  // the rest row by row, sixteen at a time
-                    const uint32_t first = tile + (chunk >> 3) * S::kHalf + sub * 128 + (((chunk & 7) ^ sub) << 4);
-                    const char *at_x = from + (size_t)x16 * 16;
-                    const unsigned stride = p.row16 * 16;
+                    if (mine) {
+                        const uint32_t first = tile + h * S::kHalf + sub * 128 + ((chunk ^ sub) << 4);
+                        const char *from = (const char *)(v ? p.cache.v : p.cache.k) + (size_t)x16 * 16 + h * 128 + chunk * 16;
 #pragma unroll 1
-                    for (int row0 = 0; row0 < rows16; row0 += 16) {
-                        if (runs >> (row0 >> maps.run_log2) & 1) continue;
-                        // (places ahead of the copies: a load behind a copy waits its turn)
-                        unsigned at[16 / kRowsOfCopy];
+                        for (uint32_t rest = mine; rest; rest &= rest - 1) {
+                            const int row0 = (__ffs(rest) - 1) * kRun;
+                            unsigned place[4];  // (ahead of the copies: a load behind a copy waits its turn)
 #pragma unroll
-                        for (int i = 0; i < 16 / kRowsOfCopy; ++i) at[i] = meta.at[row0 + i * kRowsOfCopy + sub];
+                            for (int i = 0; i < 4; ++i) place[i] = meta.at[row0 + 4 * i + sub];
 #pragma unroll
-                        for (int i = 0; i < 16 / kRowsOfCopy; ++i) {
-                            // (the row's low three bits, by which its 16 bytes are permuted: those of sub, and i * kRowsOfCopy's)
-                            const uint32_t to = (first ^ (i * kRowsOfCopy & 7) << 4) + (row0 + i * kRowsOfCopy) * 128;
-                            const bool is = at[i] != kNowhere;
-                            if (copies) cp_async16_or_zero(to, at_x + (is ? (size_t)at[i] * stride : 0), is);
+                            for (int i = 0; i < 4; ++i) {
+                                // (the row's low three bits permute its 16 bytes: those of sub, and those of 4 i)
+                                const bool is = place[i] != kNowhere;
+                                if (copies) cp_async16_or_zero((first ^ (i & 1) << 6) + (row0 + 4 * i) * 128, from + (is ? (size_t)place[i] * stride : 0), is);
+                            }
                         }
+                        __syncwarp();
+                        cp_async_arrive(bar(full));
+                        __syncwarp();
                     }
-                    __syncwarp();
-                    cp_async_arrive(bar(full));
-                    __syncwarp();
+                    if (lane == 0) mbar_arrive_expect_tx(bar(full), part ? 0 : __popc(runs) * kHalves * kRun * 128);  // (behind all that has been asked for)
                 }
-                if (lane == 0) mbar_arrive_expect_tx(bar(full), (__popc(runs) << maps.run_log2) * kHalves * 128);  // (behind all that has been asked for)
                 ++c;
             }
             __syncwarp();
@@ -1425,22 +1471,19 @@ Workspace workspace_of(const mate_cache_t *c, int B) {
     return w;
 }
 
-// Boxes of 32 or 16 rows, where a page is a whole number of them, the rows of all heads and pages lie in one such matrix and 64
-// columns from a head's first on are its own, or behind the last one.
+// Boxes of kRun rows, where a page is a whole number of them, the rows of all heads and pages lie in one such matrix and 64 columns from a
+// head's first on are its own, or behind the last one.
 TcMaps maps_of(SharedParams &p, const mate_cache_t *c) {
     TcMaps m = {};
     const int64_t slot = c->slot_stride, rows = slot > 0 ? ((int64_t)(c->pages - 1) * c->page_stride + (c->kv_heads - 1) * c->head_stride) / slot + c->page_size : 0;
-    int run = 32;
-    if (c->page_size % run != 0) run = 16;
-    bool fits = c->page_size % run == 0 && slot >= c->d && (c->pages == 1 || c->page_stride % slot == 0) && (slot == c->d || c->d % 64 == 0) && rows <= INT32_MAX;
-    if (fits && (c->kv_heads - 1) * (c->head_stride % slot) + c->d <= slot && make_box_map(&m.k, p.cache.k, (size_t)slot, (size_t)rows, (size_t)slot * 2, run) &&
-        make_box_map(&m.v, p.cache.v, (size_t)slot, (size_t)rows, (size_t)slot * 2, run))
-        m.run = run;
+    const bool fits = c->page_size % kRun == 0 && slot >= c->d && (c->pages == 1 || c->page_stride % slot == 0) && (slot == c->d || c->d % 64 == 0) && rows <= INT32_MAX;
+    if (fits && (c->kv_heads - 1) * (c->head_stride % slot) + c->d <= slot && make_box_map(&m.k, p.cache.k, (size_t)slot, (size_t)rows, (size_t)slot * 2, kRun) &&
+        make_box_map(&m.v, p.cache.v, (size_t)slot, (size_t)rows, (size_t)slot * 2, kRun))
+        m.run = kRun;
     if (m.run) {  // places in rows of a slot stride
         p.page_step = (unsigned)(c->page_stride / slot), p.slot_step = 1, p.head_step = (unsigned)(c->head_stride / slot);
         p.row16 = (unsigned)(slot / 8), p.head16 = (unsigned)(c->head_stride % slot / 8);
     }
-    for (m.run_log2 = 0; 1 << m.run_log2 < run;) ++m.run_log2;  // (without boxes too: the rows are looked at in blocks all the same)
     return m;
 }
 
