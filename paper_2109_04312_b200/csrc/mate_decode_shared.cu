@@ -712,9 +712,9 @@ __global__ void __launch_bounds__(kSimtThreads, 2) shared_simt_kernel(const __gr
 constexpr int kTcRows = 128, kTcKeys = 128;
 constexpr int kSoftmaxWarps = 8;              // two teams, which take the tiles in turn; a thread to a row
 constexpr int kScoutWarp0 = kSoftmaxWarps, kScoutWarps = kScouts / 32;
-constexpr int kCopyWarp0 = kScoutWarp0 + kScoutWarps, kCopyWarps = 3;  // keys, values, a share of the rows of both that are copied one by one
-constexpr int kMmaWarp = kCopyWarp0 + kCopyWarps;
-constexpr int kTcThreads = 32 * (kMmaWarp + 1);
+constexpr int kCopyWarp0 = kScoutWarp0 + kScoutWarps, kCopyWarps = 2;  // keys, values
+constexpr int kMmaWarp = kCopyWarp0 + kCopyWarps, kMmaWarps = 2;       // a team each
+constexpr int kTcThreads = 32 * (kMmaWarp + kMmaWarps);
 constexpr int kMetas = 4;                     // tiles whose keys are known
 constexpr float kRescale = 8.f;               // log2 units that a score may exceed its row's base by
 // tensor memory: O of the teams (fp32), then S of their tiles (fp32), which P takes the place of: of every 16 keys the weights' upper halves
@@ -885,18 +885,18 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
     if (warp == 0) {  // (a lane to an index: one after the other they take a third of a microsecond)
         if (lane < 2) {
             mbar_init(bar(sm.q_full[lane]), kScoutWarps);
-            mbar_init(bar(sm.q_empty[lane]), kSoftmaxWarps + 1);
+            mbar_init(bar(sm.q_empty[lane]), kSoftmaxWarps + kMmaWarps);
             mbar_init(bar(sm.s_full[lane]), 1), mbar_init(bar(sm.pv_done[lane]), 1);
             mbar_init(bar(sm.p_full[lane]), kSoftmaxWarps / 2), mbar_init(bar(sm.team[lane]), kSoftmaxWarps / 2);
             sm.odd[lane] = 0;
         }
         if (lane < kStages) {
-            mbar_init(bar(sm.k_full[lane]), 2), mbar_init(bar(sm.v_full[lane]), 2);
+            mbar_init(bar(sm.k_full[lane]), 1), mbar_init(bar(sm.v_full[lane]), 1);
             mbar_init(bar(sm.k_empty[lane]), 1), mbar_init(bar(sm.v_empty[lane]), 1);
         }
-        if (lane < kMetas) mbar_init(bar(sm.meta_full[lane]), kScoutWarps), mbar_init(bar(sm.meta_empty[lane]), kSoftmaxWarps + kCopyWarps + 1);
+        if (lane < kMetas) mbar_init(bar(sm.meta_full[lane]), kScoutWarps), mbar_init(bar(sm.meta_empty[lane]), kSoftmaxWarps + kCopyWarps + kMmaWarps);
         if (lane == 0) {
-            mbar_init(bar(sm.both), kSoftmaxWarps), mbar_init(bar(sm.final_), 1);
+            mbar_init(bar(sm.both), kSoftmaxWarps), mbar_init(bar(sm.final_), kMmaWarps);
             sm.abort = 0;
         }
         fence_mbar_init();
@@ -1203,150 +1203,129 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
         if (scout.bad) atomicOr(p.cache.status, kCacheBad);
     } else if (warp < kMmaWarp) {
         // ------------------------------------------------------------------ copies of keys (first warp) and values (second)
-        // Runs by one lane, the rest row by row: of rows of 128 elements the third warp has the second half, of shorter ones every other
-        // sixteen rows.
-        const bool leader = elect_one();
-        const int w = warp - kCopyWarp0, part = w == 2, h = DP == 128 ? part : 0;
+        // Runs by one lane, the rest row by row.
+        const bool leader = elect_one(), v = warp != kCopyWarp0;
+        const CUtensorMap *map = v ? &maps.v : &maps.k;
         const int chunk = lane & 7, sub = lane >> 3;  // of a copy of four rows
-        const bool copies = h * 8 + chunk < p.d / 8;
         const unsigned stride = p.row16 * 16;
-        bool ok = true;
 #pragma unroll 1
-        for (int t = 0, c = 0; ok; ++t) {
+        for (int t = 0, c = 0;; ++t) {
             const Meta &meta = sm.meta[t % kMetas];
             if (!wait(sm.meta_full[t % kMetas], t / kMetas & 1)) break;
             const int n = meta.n;
             if (n < 0) break;
             if (n > 0) {
                 const int stage = c % kStages;
+                const uint64_t &full = v ? sm.v_full[stage] : sm.k_full[stage];
+                const uint32_t tile = smem_u32(v ? sm.v[stage] : sm.k[stage]);
                 const uint32_t blocks = (2u << ((n - 1) / kRun)) - 1;  // that have a key
                 const uint32_t runs = blocks & (meta.runs[0] | meta.runs[1] << 2 | meta.runs[2] << 4 | meta.runs[3] << 6);
-                const uint32_t mine = blocks & ~runs & (DP == 128 ? 0xff : part ? 0xaa : 0x55);
                 const int x16 = (int)meta.x16;
                 unsigned at[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) at[i] = meta.at[i * kRun];
+                if (c >= kStages && !wait(v ? sm.v_empty[stage] : sm.k_empty[stage], (c / kStages - 1) & 1)) break;
+                if (runs && leader) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        if (runs >> i & 1)
+#pragma unroll
+                            for (int h = 0; h < kHalves; ++h) tma_load_2d(tile + h * S::kHalf + i * kRun * 128, map, x16 * 8 + 64 * h, (int)at[i], bar(full));
+                }
+                __syncwarp();
+                if (runs != blocks) {
+                    const uint32_t first = tile + sub * 128 + ((chunk ^ sub) << 4);
+                    const char *from = (const char *)(v ? p.cache.v : p.cache.k) + (size_t)x16 * 16 + chunk * 16;
 #pragma unroll 1
-                for (int v = w & 1; v <= (w > 0); ++v) {
-                    const uint64_t &full = v ? sm.v_full[stage] : sm.k_full[stage];
-                    const uint32_t tile = smem_u32(v ? sm.v[stage] : sm.k[stage]);
-                    if (c >= kStages && !(ok = wait(v ? sm.v_empty[stage] : sm.k_empty[stage], (c / kStages - 1) & 1))) break;
-                    if (!part && runs && leader) {
+                    for (uint32_t rest = blocks & ~runs; rest; rest &= rest - 1) {
+                        const int row0 = (__ffs(rest) - 1) * kRun;
+                        unsigned place[4];  // (ahead of the copies: a load behind a copy waits its turn)
 #pragma unroll
-                        for (int i = 0; i < 8; ++i)
-                            if (runs >> i & 1)
+                        for (int i = 0; i < 4; ++i) place[i] = meta.at[row0 + 4 * i + sub];
 #pragma unroll
-                                for (int k = 0; k < kHalves; ++k)
-                                    tma_load_2d(tile + k * S::kHalf + i * kRun * 128, v ? &maps.v : &maps.k, x16 * 8 + 64 * k, (int)at[i], bar(full));
+                        for (int i = 0; i < 4; ++i) {
+                            // (the row's low three bits permute its 16 bytes: those of sub, and those of 4 i)
+                            const bool is = place[i] != kNowhere;
+                            const char *row = from + (is ? (size_t)place[i] * stride : 0);
+                            const uint32_t to = (first ^ (i & 1) << 6) + (row0 + 4 * i) * 128;
+#pragma unroll
+                            for (int h = 0; h < kHalves; ++h)
+                                if (h * 8 + chunk < p.d / 8) cp_async16_or_zero(to + h * S::kHalf, row + h * 128, is);
+                        }
                     }
                     __syncwarp();
-                    if (mine) {
-                        const uint32_t first = tile + h * S::kHalf + sub * 128 + ((chunk ^ sub) << 4);
-                        const char *from = (const char *)(v ? p.cache.v : p.cache.k) + (size_t)x16 * 16 + h * 128 + chunk * 16;
-#pragma unroll 1
-                        for (uint32_t rest = mine; rest; rest &= rest - 1) {
-                            const int row0 = (__ffs(rest) - 1) * kRun;
-                            unsigned place[4];  // (ahead of the copies: a load behind a copy waits its turn)
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) place[i] = meta.at[row0 + 4 * i + sub];
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                // (the row's low three bits permute its 16 bytes: those of sub, and those of 4 i)
-                                const bool is = place[i] != kNowhere;
-                                if (copies) cp_async16_or_zero((first ^ (i & 1) << 6) + (row0 + 4 * i) * 128, from + (is ? (size_t)place[i] * stride : 0), is);
-                            }
-                        }
-                        __syncwarp();
-                        cp_async_arrive(bar(full));
-                        __syncwarp();
-                    }
-                    if (lane == 0) mbar_arrive_expect_tx(bar(full), part ? 0 : __popc(runs) * kHalves * kRun * 128);  // (behind all that has been asked for)
+                    cp_async_arrive(bar(full));
+                    __syncwarp();
                 }
+                if (lane == 0) mbar_arrive_expect_tx(bar(full), __popc(runs) * kHalves * kRun * 128);  // (behind all that has been asked for)
                 ++c;
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(sm.meta_empty[t % kMetas]));
         }
     } else {
-        // ------------------------------------------------------------------ the products
-        // S = Q K^T of a tile as soon as its keys are there and the team's last P V is done; O += P V as soon as P is there.
+        // ------------------------------------------------------------------ the products, a warp to each team
+        // S = Q K^T of a tile as soon as its keys are there and the team's last P V, whose weights have the place of S, is done; O += P V as
+        // soon as P is there.
         const bool leader = elect_one();
-        int t = 0, parts = 0;     // tile that comes next
-        int cs = 0, cp = 0;       // tiles whose S, and whose P V, have been issued
-        int n_even = 0, n_odd = 0, n = 0, first = 0, last = 0;  // keys of the teams' tiles; the tile that comes next
-        bool known = false, end = false;
-        uint32_t idle = 0;
-        const auto is = [&](const uint64_t &b, uint32_t parity) { return mbar_test_wait(smem_u32(&b), parity); };
+        const int team = warp - kMmaWarp;
+        const uint32_t tS = tmem + kTmemS + team * kTcKeys, tO = tmem + kTmemO + team * 128, idesc_pv = idesc_bf16(kTcRows, DP, 0, 1);
+        int c = 0, mine = 0, parts = 0;
 #pragma unroll 1
-        while (!end || cp < cs) {
-            bool moved = false;
-            if (!end && !known && is(sm.meta_full[t % kMetas], t / kMetas & 1)) {
-                known = moved = true;
-                const Meta &meta = sm.meta[t % kMetas];
-                n = meta.n, first = meta.first, last = meta.last;
-                end = n < 0;
-                __syncwarp();
-                if (lane == 0) mbar_arrive(bar(sm.meta_empty[t % kMetas]));
-            }
-            const int stage = cs % kStages, team = cs & 1;
-            if (known && !end && (n == 0 || (is(sm.k_full[stage], cs / kStages & 1) && (!first || is(sm.q_full[parts & 1], parts / 2 & 1)) &&
-                                             (cs < 2 || is(sm.pv_done[team], (cs / 2 - 1) & 1))))) {
-                if (n > 0) {
-                    fence_proxy_async();  // the copies of 16 bytes come through the generic proxy
-                    tc_fence_after();
-                    const uint32_t idesc = idesc_bf16(kTcRows, (n + 15) & ~15, 0, 0), tS = tmem + kTmemS + team * kTcKeys;
-                    const uint32_t q = smem_desc_lo(smem_u32(sm.q[parts & 1])), k = smem_desc_lo(smem_u32(sm.k[stage]));
-                    if (leader) {
-                        mma_ss_lean<0>(tS, q, k, idesc);
+        for (int t = 0;; ++t) {
+            const Meta &meta = sm.meta[t % kMetas];
+            if (!wait(sm.meta_full[t % kMetas], t / kMetas & 1)) break;
+            const int n = meta.n, last = meta.last;
+            if (n < 0) break;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(sm.meta_empty[t % kMetas]));
+            if (n > 0 && (c & 1) == team) {
+                const int stage = c % kStages, phase = c / kStages & 1, steps = (n + 15) / 16;
+                const uint32_t idesc = idesc_bf16(kTcRows, steps * 16, 0, 0);
+                if (!wait(sm.q_full[parts & 1], parts / 2 & 1) || !wait(sm.k_full[stage], phase)) break;
+                if (mine > 0 && !wait(sm.pv_done[team], (mine - 1) & 1)) break;
+                fence_proxy_async();  // the copies of 16 bytes come through the generic proxy
+                tc_fence_after();
+                const uint32_t q = smem_desc_lo(smem_u32(sm.q[parts & 1])), k = smem_desc_lo(smem_u32(sm.k[stage]));
+                if (leader) {
+                    mma_ss_lean<0>(tS, q, k, idesc);
 #pragma unroll
-                        for (int i = 1; i < DP / 16; ++i) {
-                            const uint32_t off = i / 4 * (S::kHalf >> 4) + i % 4 * 2;
-                            mma_ss_lean<1>(tS, q + off, k + off, idesc);
-                        }
-                        mma_commit(bar(sm.s_full[team]));
-                        mma_commit(bar(sm.k_empty[stage]));
+                    for (int i = 1; i < DP / 16; ++i) {
+                        const uint32_t off = i / 4 * (S::kHalf >> 4) + i % 4 * 2;
+                        mma_ss_lean<1>(tS, q + off, k + off, idesc);
                     }
-                    (team ? n_odd : n_even) = n;
-                    ++cs;
-                }
-                if (last) {
-                    if (leader) mma_commit(bar(sm.q_empty[parts & 1]));
-                    ++parts;
+                    mma_commit(bar(sm.s_full[team]));
+                    mma_commit(bar(sm.k_empty[stage]));
+                    if (last) mma_commit(bar(sm.q_empty[parts & 1]));
                 }
                 __syncwarp();
-                ++t;
-                known = false;
-                moved = true;
-            }
-            if (cp < cs && is(sm.p_full[cp & 1], cp / 2 & 1) && is(sm.v_full[cp % kStages], cp / kStages & 1)) {
+                if (!wait(sm.v_full[stage], phase) || !wait(sm.p_full[team], mine & 1)) break;
                 tc_fence_after();
                 fence_proxy_async();
-                const int from = cp % kStages, steps = ((cp & 1 ? n_odd : n_even) + 15) / 16;
-                const uint32_t idesc = idesc_bf16(kTcRows, 64, 0, 1), v = smem_desc_lo(smem_u32(sm.v[from]));
-                const uint32_t tO = tmem + kTmemO + (cp & 1) * 128, tP = tmem + kTmemS + (cp & 1) * kTcKeys;
+                // (64 columns of V lie kHalf behind the others: the leading byte offset)
+                const uint32_t v = (smem_u32(sm.v[stage]) & 0x3ffffu) >> 4 | (uint32_t)(S::kHalf >> 4) << 16;
                 if (leader) {
-#pragma unroll 1
-                    for (int ks = 0; ks < steps; ++ks)
+                    const auto step = [&](int ks) {
+                        mma_ts_lean<1>(tO, tS + 16 * ks, v + ks * (16 * 128 >> 4), idesc_pv);
+                        mma_ts_lean<1>(tO, tS + 16 * ks + 8, v + ks * (16 * 128 >> 4), idesc_pv);
+                    };
+                    if (steps == kTcKeys / 16) {
 #pragma unroll
-                        for (int h = 0; h < kHalves; ++h) {
-                            const uint32_t b = v + ks * (16 * 128 >> 4) + h * (S::kHalf >> 4);
-                            mma_ts_lean<1>(tO + 64 * h, tP + 16 * ks, b, idesc);
-                            mma_ts_lean<1>(tO + 64 * h, tP + 16 * ks + 8, b, idesc);
-                        }
-                    mma_commit(bar(sm.pv_done[cp & 1]));
-                    mma_commit(bar(sm.v_empty[from]));
+                        for (int ks = 0; ks < kTcKeys / 16; ++ks) step(ks);
+                    } else {
+#pragma unroll 1
+                        for (int ks = 0; ks < steps; ++ks) step(ks);
+                    }
+                    mma_commit(bar(sm.pv_done[team]));
+                    mma_commit(bar(sm.v_empty[stage]));
                 }
                 __syncwarp();
-                ++cp;
-                moved = true;
+                ++mine;
+            } else if (last) {
+                if (leader) mma_commit(bar(sm.q_empty[parts & 1]));
+                __syncwarp();
             }
-            if (moved) {
-                idle = 0;
-            } else if (*abort) {
-                break;
-            } else if (++idle > 1u << 18) {  // (some 20 ms)
-                *abort = 1;
-            }
+            c += n > 0, parts += last;
         }
         if (leader) mma_commit(bar(sm.final_));  // nothing of this block may still run on the tensor pipe when its memory is freed
         __syncwarp();
