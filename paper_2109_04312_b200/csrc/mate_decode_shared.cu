@@ -132,12 +132,10 @@ struct Found {
     uint2 cost[kMaxBatch];
     Entry entries[kKept];
 };
-// All threads call it.  `found`: in shared memory, free when the first batch has been taken over.
+// All threads call it, and each gets it.  `found`: in shared memory, free when the first batch has been taken over.
 template <int RT, int NT>
 __device__ Start find_start(const SharedParams &p, Found &found) {
     uint2 *cost = found.cost;
-    __shared__ unsigned s_sum[32];
-    __shared__ Start s_start;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, batches = (p.B + p.pack - 1) / p.pack;
 #pragma unroll 1
     for (int b = tid; b < p.B; b += NT) {
@@ -146,8 +144,6 @@ __device__ Start find_start(const SharedParams &p, Found &found) {
         cost[b] = make_uint2(units_of(e.own1 - e.own0), leads(e, b) ? p.kv_heads * group_tiles<RT>(p, e) * (kOver + units_of(e.shared)) : 0);
         if (e.bad && blockIdx.x == 0) atomicOr(p.cache.status, kCacheBad);
     }
-    if (tid == 0) s_start = {};
-    if (tid < 32) s_sum[tid] = 0;
     __syncthreads();
     // a warp to each batch; its cost replaces that of its first entry
 #pragma unroll 1
@@ -160,35 +156,33 @@ __device__ Start find_start(const SharedParams &p, Found &found) {
         if (lane == 0) cost[i * p.pack].x = shared + (unsigned)(p.kv_heads * p.own_tiles) * own_units((int)own);
     }
     __syncthreads();
-    const int per = (batches + NT - 1) / NT, i0 = min(batches, tid * per), i1 = min(batches, i0 + per);
-    unsigned own = 0;
+    // every warp for itself, 32 batches at a time: the sum of all, and then the one that has the block's first unit
+    Start start = {};
 #pragma unroll 1
-    for (int i = i0; i < i1; ++i) own += cost[i * p.pack].x;
-    const unsigned of_warp = __reduce_add_sync(~0u, own);
-    if (lane == 0) s_sum[warp] = of_warp;
-    __syncthreads();
-    const unsigned sums = s_sum[lane], total = __reduce_add_sync(~0u, sums), in_front = __reduce_add_sync(~0u, lane < warp ? sums : 0u);
-    const unsigned blocks = min(total, (unsigned)p.blocks), i = blockIdx.x;
-    if (i < blocks) {
-        const unsigned q = total / blocks, r = total - q * blocks, at = q * i + r * i / blocks, end = q * (i + 1) + r * (i + 1) / blocks;
-        if (at - in_front < of_warp) {  // (at >= in_front, too)
-            unsigned sum = own;
+    for (int i = lane; i < batches; i += 32) start.total += cost[i * p.pack].x;
+    start.total = __reduce_add_sync(~0u, start.total);
+    const unsigned blocks = min(start.total, (unsigned)p.blocks), i = blockIdx.x;
+    if (i >= blocks) return start;
+    const unsigned q = start.total / blocks, r = start.total - q * blocks;
+    start.at = q * i + r * i / blocks, start.left = (int)(q * (i + 1) + r * (i + 1) / blocks - start.at);
+    unsigned before = 0;
+#pragma unroll 1
+    for (int i0 = 0;; i0 += 32) {
+        unsigned sum = i0 + lane < batches ? cost[(i0 + lane) * p.pack].x : 0;
 #pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const unsigned y = __shfl_up_sync(~0u, sum, o);
-                if (lane >= o) sum += y;
-            }
-            unsigned in = at - in_front - (sum - own);
-            if (in < own) {
-                int k = i0;
-#pragma unroll 1
-                for (; in >= cost[k * p.pack].x; ++k) in -= cost[k * p.pack].x;
-                s_start = {total, at, in, (int)(end - at), k};
-            }
+        for (int o = 1; o < 32; o <<= 1) {
+            const unsigned y = __shfl_up_sync(~0u, sum, o);
+            if (lane >= o) sum += y;
         }
+        const unsigned behind = __ballot_sync(~0u, before + sum > start.at);
+        if (behind) {
+            const int k = __ffs(behind) - 1;
+            const unsigned front = __shfl_sync(~0u, sum, max(k - 1, 0));
+            start.batch = i0 + k, start.in = start.at - before - (k > 0 ? front : 0);
+            return start;
+        }
+        before += __shfl_sync(~0u, sum, 31);
     }
-    __syncthreads();
-    return s_start;
 }
 
 // A part of an item.
@@ -225,27 +219,34 @@ __device__ __forceinline__ void put_joint(const SharedParams &p, const Part &par
 __device__ __forceinline__ bool attends(int want_row, int want_col, int below, int place, int row, int col) {
     return place < below || row == want_row || col == want_col;
 }
-// The rows of a tile, as those who weigh keys need them,
+constexpr int kScouts = 128;
+struct alignas(16) Wish {
+    int row, col, below;
+    int member;  // of own tokens: only those of this entry (of the batch) count
+    __device__ bool is_for(const int place, const int of_row, const int of_col) const { return attends(row, col, below, place, of_row, of_col); }
+};
+// The rows of a tile,
 template <int RT>
 struct Rows {
-    int want_row[RT], want_col[RT], below[RT];
+    short kind[RT];  // place of a row's wish among those below, -1: it attends nothing
 };
-// and as those who look for keys do.
+// and, as those who look for keys need them, without repetitions of the row before: the rows of 32 have places of their own.
 template <int RT>
 struct Wishes {
     int least, most;  // of `below` over the rows that are there
     int views;        // 1: some want a row, 2: a column
-    int n;            // of a group: without repetitions of the row before
-    int2 want[RT];
-    __device__ void clear() { least = INT32_MAX, most = INT32_MIN, views = n = 0; }
+    int n[kScouts / 32];
+    Wish kind[kScouts];
+    __device__ void clear() { least = INT32_MAX, most = INT32_MIN, views = 0; }
 };
 // Keys, with what the rows go by.
 struct alignas(16) Key {
     unsigned at;  // where it lies: see SharedParams
     int place, row, col;
 };
-constexpr int kList = 512, kScouts = 128;
+constexpr int kList = 512;
 constexpr unsigned kNowhere = ~0u;
+__device__ __forceinline__ Key nobody() { return {kNowhere, INT32_MAX, kNever + 1, kNever + 1}; }  // a key that no row attends
 constexpr int kUnits = 8;  // of a look
 
 // kScouts threads walk the parts of the block's share and look through their tokens, eight units at a time, two to a warp; the keys that
@@ -428,7 +429,7 @@ struct Scout {
         Wishes<RT> &w = sm.wishes[parts & 1];
         ++parts;
         if (tid == 0) sm.wishes[parts & 1].clear();
-        int want_row = kNever, want_col = kNever, below = -2;
+        Wish x = {kNever, kNever, -2, kNobody};
         if (tid < part.n_rows) {
             const int member = member_of<RT>(p, part, tid), view = view_at(p, part.kv * p.group + part.tile * RT + tid - member * p.group);
             const int held_at = part.b - batch * p.pack + member;
@@ -437,18 +438,24 @@ struct Scout {
             const Entry &e = held_at >= entries() ? other : sm.entries[held_at];
             if (seg == 0 ? e.counts && e.first == part.b && e.count > 0 : e.own1 > e.own0) {
                 const bool text = e.q_row == MATE_ID_TEXT || e.q_col == MATE_ID_TEXT;
-                below = text ? INT32_MAX : e.prefix;
-                if (!text && view != MATE_VIEW_COL) want_row = e.q_row;
-                if (!text && view != MATE_VIEW_ROW) want_col = e.q_col;
+                x.below = text ? INT32_MAX : e.prefix;
+                if (!text && view != MATE_VIEW_COL) x.row = e.q_row;
+                if (!text && view != MATE_VIEW_ROW) x.col = e.q_col;
+                x.member = seg == 0 ? 0 : member;
             }
         }
-        if (tid < RT) rows.want_row[tid] = want_row, rows.want_col[tid] = want_col, rows.below[tid] = below;
-        const int least = __reduce_min_sync(~0u, below < 0 ? INT32_MAX : below), most = __reduce_max_sync(~0u, below);
-        const int views = (__any_sync(~0u, want_row != kNever) ? 1 : 0) | (__any_sync(~0u, want_col != kNever) ? 2 : 0);
-        const int row_before = __shfl_up_sync(~0u, want_row, 1), col_before = __shfl_up_sync(~0u, want_col, 1);
-        const bool again = (tid & 31) > 0 && row_before == want_row && col_before == want_col;
-        if ((tid & 31) == 0 && most >= 0) atomicMin(&w.least, least), atomicMax(&w.most, most), atomicOr(&w.views, views);
-        if (!again && (want_row != kNever || want_col != kNever)) w.want[atomicAdd(&w.n, 1)] = make_int2(want_row, want_col);
+        const int lane = tid & 31, least = __reduce_min_sync(~0u, x.below < 0 ? INT32_MAX : x.below), most = __reduce_max_sync(~0u, x.below);
+        const int views = (__any_sync(~0u, x.row != kNever) ? 1 : 0) | (__any_sync(~0u, x.col != kNever) ? 2 : 0);
+        const bool same = (__shfl_up_sync(~0u, x.row, 1) == x.row) & (__shfl_up_sync(~0u, x.col, 1) == x.col) &
+                          (__shfl_up_sync(~0u, x.below, 1) == x.below) & (__shfl_up_sync(~0u, x.member, 1) == x.member);
+        const unsigned begins = __ballot_sync(~0u, lane == 0 || !same);
+        const int kind = (tid & ~31) + __popc(begins & (2u << lane) - 1) - 1;
+        if (begins >> lane & 1) w.kind[kind] = x;
+        if (lane == 0) {
+            w.n[tid >> 5] = most < 0 ? 0 : __popc(begins);
+            if (most >= 0) atomicMin(&w.least, least), atomicMax(&w.most, most), atomicOr(&w.views, views);
+        }
+        if (tid < RT) rows.kind[tid] = (short)(x.below < 0 ? -1 : kind);
         __syncwarp();
         ask_ids();
         ask_pages(next + kUnits);
@@ -462,27 +469,39 @@ struct Scout {
         int *count = sm.counts[looks++ & 1];
         Key key[2];
         int of[2];
+        bool is[2];
         unsigned those[2];
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-            auto &g = got[k];
-            key[k] = {g.at, g.j, g.row, g.col}, of[k] = g.owner;
-            bool is = g.there && g.row >= 0 && g.col >= 0;
-            if (is) {
-                if (g.row == MATE_ID_TEXT || g.col == MATE_ID_TEXT) key[k].place = -1;
-                if (seg == 0) {
-                    is = key[k].place < w.most;
-#pragma unroll 1
-                    for (int i = 0; i < w.n && !is; ++i) is = g.row == w.want[i].x || g.col == w.want[i].y;
-                } else {
-                    const Entry &e = sm.entries[of[k]];
-                    is = e.q_row == MATE_ID_TEXT || e.q_col == MATE_ID_TEXT || key[k].place < e.prefix || ((w.views & 1) && g.row == e.q_row) ||
-                         ((w.views & 2) && g.col == e.q_col);
-                }
+            const auto &g = got[k];
+            key[k] = {g.at, g.row == MATE_ID_TEXT || g.col == MATE_ID_TEXT ? -1 : g.j, g.row, g.col}, of[k] = g.owner;
+            is[k] = g.there && g.row >= 0 && g.col >= 0;
+            if (!is[k]) key[k] = nobody();
+            if (is[k] && seg == 1) {
+                const Entry &e = sm.entries[of[k]];
+                is[k] = e.q_row == MATE_ID_TEXT || e.q_col == MATE_ID_TEXT || key[k].place < e.prefix || ((w.views & 1) && g.row == e.q_row) ||
+                        ((w.views & 2) && g.col == e.q_col);
             }
-            those[k] = __ballot_sync(~0u, is);
+        }
+        if (seg == 0) {
+#pragma unroll
+            for (int k = 0; k < 2; ++k) is[k] = key[k].place < w.most;
+            if (__any_sync(~0u, (key[0].at != kNowhere && !is[0]) || (key[1].at != kNowhere && !is[1])))
+#pragma unroll 1
+                for (int i = 0; i < kScouts; i += 32) {
+                    const int n = w.n[i / 32];
+#pragma unroll 4
+                    for (int j = 0; j < n; ++j) {
+                        const int row = w.kind[i + j].row, col = w.kind[i + j].col;
+                        is[0] |= (key[0].row == row) | (key[0].col == col), is[1] |= (key[1].row == row) | (key[1].col == col);
+                    }
+                }
+        }
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            those[k] = __ballot_sync(~0u, is[k]);
             // Own tokens of which none is left out begin at a multiple of `run`, so that they are copied in runs; in front of them are nobody's.
-            const bool dense = g.first && those[k] == __ballot_sync(~0u, g.there) && __popc(those[k]) >= run;
+            const bool dense = got[k].first && those[k] == __ballot_sync(~0u, got[k].there) && __popc(those[k]) >= run;
             if (lane == 0) count[2 * warp + k] = __popc(those[k]) + (dense ? kDense : 0);
         }
         next += kUnits;
@@ -501,7 +520,7 @@ struct Scout {
         }
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-            if (lane < gap[k]) put_key(to[k] - gap[k] + lane, {kNowhere, INT32_MAX, kNever + 1, kNever + 1}, kNobody);
+            if (lane < gap[k]) put_key(to[k] - gap[k] + lane, nobody(), kNobody);
             if (those[k] >> lane & 1) put_key(to[k] + __popc(those[k] & ((1u << lane) - 1)), key[k], of[k]);
         }
         pending = all;
@@ -512,12 +531,8 @@ struct Scout {
     }
     __device__ Key key(int i) const { return sm.list[(unsigned)(list_at + i) % kList]; }
     __device__ int owner_of_key(int i) const { return sm.owners[(unsigned)(list_at + i) % kList]; }
-    // Whether every row that a key is for attends it.
-    __device__ bool is_plain(const Key &key, int of) const {
-        if (of == kNobody) return true;
-        const Entry &e = sm.entries[of];
-        return seg == 0 ? key.place < wishes().least : e.q_row == MATE_ID_TEXT || e.q_col == MATE_ID_TEXT || key.place < e.prefix;
-    }
+    // Whether every row attends every key that is for it.
+    __device__ bool plain() const { return wishes().least == INT32_MAX; }
     __device__ void taken(int n) { list_at = (int)((unsigned)(list_at + n) % kList), pending -= n; }
 };
 
@@ -591,7 +606,7 @@ __global__ void __launch_bounds__(kSimtThreads, 2) shared_simt_kernel(const __gr
                 bool every = true;
                 if (tid < kSimtKeys) {
                     if (tid < n) sm.keys[tid] = scout.key(tid), sm.owners[tid] = scout.owner_of_key(tid);
-                    every = part.seg == 0 && __all_sync(~0u, tid >= n || scout.is_plain(sm.keys[tid], sm.owners[tid]));
+                    every = part.seg == 0 && scout.plain();
                 }
                 if (tid == 0) sm.n = n, sm.last = scout.pending <= kSimtKeys && !scout.more(), sm.plain = every;
                 scout.taken(n);
@@ -637,11 +652,13 @@ __global__ void __launch_bounds__(kSimtThreads, 2) shared_simt_kernel(const __gr
                 // weights: a key of a lane
                 const Key key = sm.keys[lane];
                 const int of = sm.owners[lane];
+                const Wishes<kSimtRows> &wishes = sm.scout.wishes[n_parts & 1];
                 uint32_t those[kR];
 #pragma unroll
                 for (int r = 0; r < kR; ++r) {
-                    const bool is = lane < n && (part.seg == 0 || of == member_of<kSimtRows>(p, part, r0 + r)) &&
-                                    attends(sm.rows.want_row[r0 + r], sm.rows.want_col[r0 + r], sm.rows.below[r0 + r], key.place, key.row, key.col);
+                    const int kind = sm.rows.kind[r0 + r];
+                    const Wish &wish = wishes.kind[max(kind, 0)];
+                    const bool is = lane < n && kind >= 0 && (part.seg == 0 || of == wish.member) && wish.is_for(key.place, key.row, key.col);
                     those[r] = __ballot_sync(~0u, is);
                     const float x = is ? sm.s[r0 + r][lane] : -INFINITY;
                     float top = fmaxf(x, m[r]);
@@ -726,20 +743,14 @@ struct TcShape {
     static constexpr int kTile = kTcKeys * DP * 2;              // bytes; column halves of 64 elements, 128 bytes a row and swizzled
     static constexpr int kHalf = kTcKeys * 128;
     static constexpr int kStages = DP == 64 ? 4 : 2;            // tiles of keys, and of values
-    // where 16 bytes of a row go
-    __device__ static uint32_t place(uint32_t tile, int row, int chunk) {
-        return tile + (chunk >> 3) * kHalf + row * 128 + (((chunk & 7) ^ (row & 7)) << 4);
-    }
 };
+enum { kFirst = 1, kLast = 2, kRanged = 4, kBits = 8 };  // tiles of a part; keys lo[m] to hi[m] are for the rows of entry m, or as bits[kind] says, else
+                                                          // all keys for all rows that attend anything
 struct alignas(16) Meta {
-    int n, first, last;  // keys; of the part.  n < 0: the share is done
-    uint32_t plain;      // 0x01010101: every row attends every key that is for it
-    int ranged;          // keys lo[m] to hi[m] are for the rows of entry m, else all for all
-    unsigned x16;        // where a row's elements begin, in 16 bytes
-    uint8_t runs[4];     // of every 32 keys, a bit for each kRun of them: they lie one behind the other
-    alignas(16) int place[kTcKeys];  // (read four at a time)
-    alignas(16) int row[kTcKeys];
-    alignas(16) int col[kTcKeys];
+    int n, flags;     // keys; n < 0: the share is done
+    unsigned x16;     // where a row's elements begin, in 16 bytes
+    uint8_t runs[4];  // of every 32 keys, a bit for each kRun of them: they lie one behind the other
+    alignas(16) uint32_t bits[kTcRows][kTcKeys / 32];
     unsigned at[kTcKeys];
     uint8_t lo[kTcRows], hi[kTcRows];
 };
@@ -758,8 +769,8 @@ struct TcSmem {  // from a multiple of 1024 bytes on
     Rows<kTcRows> rows[2];
     Part part[2];
     float2 stats[2][kTcRows];
-    uint64_t q_full[2], q_empty[2], k_full[4], k_empty[4], v_full[4], v_empty[4], meta_full[kMetas], meta_empty[kMetas], s_full[2], p_full[2], pv_done[2],
-        team[2], both, final_;
+    uint64_t part_full[2], q_full[2], q_empty[2], k_full[4], k_empty[4], v_full[4], v_empty[4], meta_full[kMetas], meta_empty[kMetas], s_full[2], p_full[2],
+        pv_done[2], team[2], both, final_;
     int odd[2];
     uint32_t tmem;
     int abort;
@@ -791,18 +802,6 @@ __device__ __noinline__ bool wait_long(uint32_t bar, uint32_t parity, volatile i
     return false;
 }
 
-// 32 scores of a row: those that do not count become -inf.
-__device__ __forceinline__ void mask_scores(uint32_t (&v)[32], const Meta &meta, int c0, int want_row, int want_col, int below) {
-#pragma unroll
-    for (int e = 0; e < 32; e += 4) {
-        const int4 place = *reinterpret_cast<const int4 *>(meta.place + c0 + e), row = *reinterpret_cast<const int4 *>(meta.row + c0 + e),
-                   col = *reinterpret_cast<const int4 *>(meta.col + c0 + e);
-        if (!attends(want_row, want_col, below, place.x, row.x, col.x)) v[e] = 0xff800000u;
-        if (!attends(want_row, want_col, below, place.y, row.y, col.y)) v[e + 1] = 0xff800000u;
-        if (!attends(want_row, want_col, below, place.z, row.z, col.z)) v[e + 2] = 0xff800000u;
-        if (!attends(want_row, want_col, below, place.w, row.w, col.w)) v[e + 3] = 0xff800000u;
-    }
-}
 __device__ __forceinline__ uint32_t bits_below(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u; }
 __device__ __forceinline__ float top_score(const uint32_t (&v)[32]) {
     float t[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
@@ -812,8 +811,8 @@ __device__ __forceinline__ float top_score(const uint32_t (&v)[32]) {
         for (int j = 0; j < 4; ++j) t[j] = ptx::fmax3(t[j], __uint_as_float(v[e + 2 * j]), __uint_as_float(v[e + 2 * j + 1]));
     return fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
 }
-// Weights 2^(s scale - base) of 32 keys, 16 at a time, as pairs of bf16: rounded, and what the rounding left, rounded (their sum has 16 bits: an error of
-// 2^-17 of a weight, which the result's rounding to bf16, 2^-9, hides but for one value in some hundred).  The sums take all of them.
+// Weights 2^(s scale - base), 16 keys at a time, as pairs of bf16: rounded, and what the rounding left, rounded (their sum has 16 bits: an
+// error of 2^-17 of a weight, which the result's rounding to bf16, 2^-9, hides but for one value in some hundred).  The sums take all of them.
 __device__ __forceinline__ void weigh(uint32_t (&v)[32], uint64_t scale2, uint64_t neg_base2, uint64_t (&sum)[2]) {
 #pragma unroll
     for (int i = 0; i < 32; i += 16) {
@@ -834,8 +833,9 @@ __device__ __forceinline__ void weigh(uint32_t (&v)[32], uint64_t scale2, uint64
     }
 }
 
-// The row's O, or its weights of the first n keys of a tile, times `keep` (rarely).
+// The row's O times `keep` (rarely).
 __device__ __noinline__ void scale_o(uint32_t tO, int n, float keep) {
+    ptx::tc_fence_after();
 #pragma unroll 1
     for (int i = 0; i < n; i += 16) {
         uint32_t o[16];
@@ -848,6 +848,8 @@ __device__ __noinline__ void scale_o(uint32_t tO, int n, float keep) {
     }
     ptx::tc_wait_st();
 }
+
+// The row's weights of the keys before, where they have not gone into O yet (more rarely still).
 __device__ __noinline__ void scale_p(uint32_t tP, int n, float keep) {
     ptx::tc_wait_st();
 #pragma unroll 1
@@ -876,7 +878,6 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
     using namespace ptx;
     using S = TcShape<DP>;
     constexpr int kStages = S::kStages, kHalves = DP / 64;
-    constexpr int kPer = DP / 8, kRowsOfCopy = 32 / kPer;  // copies: lanes to a row; rows of an instruction
     extern __shared__ uint8_t tc_smem[];
     TcSmem<DP> &sm = *reinterpret_cast<TcSmem<DP> *>(tc_smem + (-smem_u32(tc_smem) & 1023));
     const int tid = threadIdx.x, warp = __shfl_sync(~0u, tid >> 5, 0), lane = tid & 31;
@@ -884,10 +885,12 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
 
     if (warp == 0) {  // (a lane to an index: one after the other they take a third of a microsecond)
         if (lane < 2) {
-            mbar_init(bar(sm.q_full[lane]), kScoutWarps);
+            mbar_init(bar(sm.part_full[lane]), 1);
+            mbar_init(bar(sm.q_full[lane]), kScoutWarps + 1);
             mbar_init(bar(sm.q_empty[lane]), kSoftmaxWarps + kMmaWarps);
             mbar_init(bar(sm.s_full[lane]), 1), mbar_init(bar(sm.pv_done[lane]), 1);
-            mbar_init(bar(sm.p_full[lane]), kSoftmaxWarps / 2), mbar_init(bar(sm.team[lane]), kSoftmaxWarps / 2);
+            mbar_init(bar(sm.p_full[lane]), kSoftmaxWarps / 2);
+            mbar_init(bar(sm.team[lane]), kSoftmaxWarps / 2);
             sm.odd[lane] = 0;
         }
         if (lane < kStages) {
@@ -939,7 +942,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
             if (lane == 0) mbar_arrive(bar(b));
             return wait(b, passed++ & 1);
         };
-        int want_row = 0, want_col = 0, below = 0, member = 0, tiles = 0, own = 0;  // tiles of the part; the team's
+        int kind = 0, member = 0, tiles = 0, own = 0;  // tiles of the part; the team's
         bool live = false;
         float m = -INFINITY;
         uint64_t sum[2] = {0, 0};
@@ -947,28 +950,26 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
         for (int t = 0;; ++t) {
             const Meta &meta = sm.meta[t % kMetas];
             if (!wait(sm.meta_full[t % kMetas], t / kMetas & 1)) break;
-            const int n = meta.n, qb = parts & 1;
+            const int2 head = *reinterpret_cast<const int2 *>(&meta);
+            const int n = head.x, flags = head.y, qb = parts & 1;
             if (n < 0) break;
             const Part &part = sm.part[qb];
-            if (meta.first) {
+            if (flags & kFirst) {
                 if (!wait(sm.q_full[qb], parts / 2 & 1)) break;
-                const Rows<kTcRows> &rows = sm.rows[qb];
-                want_row = rows.want_row[r], want_col = rows.want_col[r], below = rows.below[r];
+                kind = sm.rows[qb].kind[r];
                 live = (warp & 3) * 32 < part.n_rows;
                 member = member_of<kTcRows>(p, part, r);
                 tiles = own = 0;
                 m = -INFINITY;
                 sum[0] = sum[1] = 0;
             }
-            const bool last = meta.last;
             if (n > 0 && (c & 1) == team) {
-                const bool plain = meta.plain == 0x01010101u;
                 // (S is there, so the P V of the team's tile before, whose place it has, is done)
                 if (!wait(sm.s_full[team], mine & 1)) break;
                 tc_fence_after();
                 const int stage = c % kStages;
                 bool odd = false;
-                if (!plain || meta.ranged) {  // a weight 0 does not undo a value that is not a number: is there one?
+                if (flags & (kRanged | kBits)) {  // a weight 0 does not undo a value that is not a number: is there one?
                     if (!wait(sm.v_full[stage], c / kStages & 1)) break;
                     __nv_bfloat162 z = __floats2bfloat162_rn(0.f, 0.f);
                     const uint4 *v = reinterpret_cast<const uint4 *>(sm.v[stage]);
@@ -982,11 +983,17 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
                     if (!sync(sm.team[team], teams)) break;
                     odd = *(volatile int *)&sm.odd[team] == c + 1;
                 }
-                // the row's keys: none, where the row attends nothing
-                const int m_at = min(member, kTcRows - 1), lo = meta.ranged ? meta.lo[m_at] : 0, hi = below < -1 ? 0 : meta.ranged ? meta.hi[m_at] : n;
+                // the keys that the row attends
+                uint4 on = make_uint4(0, 0, 0, 0);
+                if (kind < 0) {
+                } else if (flags & kBits) {
+                    on = *reinterpret_cast<const uint4 *>(meta.bits[kind]);
+                } else {
+                    const int lo = flags & kRanged ? meta.lo[member] : 0, hi = flags & kRanged ? meta.hi[member] : n;
+                    on = make_uint4(bits_below(hi) & ~bits_below(lo), bits_below(hi - 32) & ~bits_below(lo - 32), bits_below(hi - 64) & ~bits_below(lo - 64),
+                                    bits_below(hi - 96) & ~bits_below(lo - 96));
+                }
                 if (live) {
-                    const bool any = __any_sync(~0u, lo < hi);
-                    const int all_lo = __reduce_max_sync(~0u, lo), all_hi = __reduce_min_sync(~0u, hi);  // keys of all rows
                     if (own == 0) {
                         uint32_t zero[16] = {};
 #pragma unroll 1
@@ -995,16 +1002,14 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
 #pragma unroll 1
                     for (int c0 = 0; c0 < n; c0 += 32) {
                         uint32_t v[32] = {};
-                        if (any) {
+                        if (__any_sync(~0u, on.x)) {
                             tmem_ld32(tS + c0, v);
                             tc_wait_ld();
                             reg_fence(v);
-                            if (!plain || c0 < all_lo || c0 + 32 > all_hi) {
-                                const uint32_t on = bits_below(hi - c0) & ~bits_below(lo - c0);
+                            if (!__all_sync(~0u, on.x == ~0u)) {
 #pragma unroll
                                 for (int e = 0; e < 32; ++e)
-                                    if (!(on >> e & 1)) v[e] = 0xff800000u;
-                                if (!plain) mask_scores(v, meta, c0, want_row, want_col, below);
+                                    if (!(on.x >> e & 1)) v[e] = 0xff800000u;
                             }
                             // The base of a row moves when a score exceeds it by kRescale, and with the row's first score: O, the sum and the
                             // weights of the tile's keys in front of these follow.
@@ -1023,17 +1028,20 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
                             weigh(v, scale2, pack_f32x2(neg, neg), sum);
                         }
                         tmem_st32(tS + c0, v);
+                        on = make_uint4(on.y, on.z, on.w, on.x);
                     }
                     tc_wait_st();
                 }
                 if (odd) {
+                    for (int i = (n + 31) / 32; i < 4; ++i) on = make_uint4(on.y, on.z, on.w, on.x);  // (back to the first)
                     // Values that are not numbers: added here to the rows that attend them, and taken out of the tile.
                     const auto at = [&](int key, int e) {
                         return reinterpret_cast<__nv_bfloat16 *>(sm.v[stage] + e / 64 * S::kHalf + key * 128 + ((e / 8 & 7) ^ (key & 7)) * 16 + e % 8 * 2);
                     };
 #pragma unroll 1
                     for (int key = 0; key < n && live; ++key) {
-                        const bool counts = key >= lo && key < hi && attends(want_row, want_col, below, meta.place[key], meta.row[key], meta.col[key]);
+                        if (key % 32 == 0 && key > 0) on = make_uint4(on.y, on.z, on.w, on.x);
+                        const bool counts = on.x >> (key & 31) & 1;
 #pragma unroll 1
                         for (int e = 0; e < DP; ++e) {
                             const float y = __bfloat162float(*at(key, e));
@@ -1062,7 +1070,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
             tiles += n > 0, c += n > 0;
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(sm.meta_empty[t % kMetas]));
-            if (!last) continue;
+            if (!(flags & kLast)) continue;
 
             // The part is done: by both teams, half of the columns each, if it had more than one tile, else by the one that had it (the first
             // team, if it had none).
@@ -1123,42 +1131,28 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
             ++parts;
         }
     } else if (warp < kCopyWarp0) {
-        // ------------------------------------------------------------------ queries, and which keys are read
+        // ------------------------------------------------------------------ which keys are read
         // (These warps meet at barriers: they leave together, when one of them says there that a wait of its own has failed.)
         const int lt = tid - 32 * kScoutWarp0, lw = warp - kScoutWarp0;
         bool ok = true;
         int t = 0;
         Part part;
 #pragma unroll 1
-        for (int parts = 0; scout.next_part(part); ++parts) {
+        for (int parts = 0;; ++parts) {
             const int qb = parts & 1;
+            const bool is = scout.next_part(part);
+            if (!is) part.n_rows = 0;
             if (parts >= 2) ok &= wait(sm.q_empty[qb], (parts / 2 - 1) & 1);
             if (any_scout(!ok)) break;
-            const uint32_t q = smem_u32(sm.q[qb]);
-            const int chunk = lane % kPer, sub = lane / kPer, n_here = min(part.n_rows - 32 * lw, 32);  // the warp's rows
-            const int member = member_of<kTcRows>(p, part, lt), head = part.kv * p.group + part.tile * kTcRows + lt - member * p.group;
-            const int64_t mine = (part.b + member) * p.q_batch + head * p.q_head;  // where the thread's row is
-#pragma unroll 4
-            for (int i = 0; i < n_here; i += kRowsOfCopy) {
-                const int64_t from = __shfl_sync(~0u, mine, i + sub);
-                if (i + sub < n_here && chunk < p.d / 8) cp_async16(S::place(q, 32 * lw + i + sub, chunk), (const __nv_bfloat16 *)p.Q + from + chunk * 8);
+            if (lt == 0) {
+                sm.part[qb] = part;
+                mbar_arrive(bar(sm.part_full[qb]));
             }
             __syncwarp();
+            if (!is) break;
             scout.begin(part, sm.rows[qb]);
-            if (lt == 0) sm.part[qb] = part;
-            if (p.flip) {  // a negative scale: its sign goes to the queries
-                asm volatile("cp.async.wait_all;" ::: "memory");
-#pragma unroll 1
-                for (int i = sub; i < n_here; i += kRowsOfCopy) {
-                    uint4 *x = reinterpret_cast<uint4 *>(sm.q[qb] + (S::place(q, 32 * lw + i, chunk) - q));
-                    constexpr uint32_t kSigns = 0x80008000u;
-                    *x = make_uint4(x->x ^ kSigns, x->y ^ kSigns, x->z ^ kSigns, x->w ^ kSigns);
-                }
-                __syncwarp();
-            }
-            cp_async_arrive(bar(sm.q_full[qb]));
-            __syncwarp();
             if (lane == 0) mbar_arrive(bar(sm.q_full[qb]));
+            const bool all_plain = scout.plain();
             bool last = false;
 #pragma unroll 1
             for (bool first = true; !last; first = false, ++t) {
@@ -1170,25 +1164,38 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
                 Meta &meta = sm.meta[t % kMetas];
                 if (ok) meta.lo[lt] = meta.hi[lt] = 0;
                 if (any_scout(!ok)) break;
-                Key key = {kNowhere, INT32_MAX, kNever + 1, kNever + 1};  // nobody's
-                bool plain = true;
-                if (lt < n) {
-                    key = scout.key(lt);
-                    const int of = scout.owner_of_key(lt);
-                    plain = scout.is_plain(key, of);
-                    if (part.seg == 1 && of != kNobody) {
-                        if (lt == 0 || scout.owner_of_key(lt - 1) != of) meta.lo[of] = (uint8_t)lt;
-                        if (lt == n - 1 || scout.owner_of_key(lt + 1) != of) meta.hi[of] = (uint8_t)(lt + 1);
+                Key key = nobody();
+                int of = kNobody;
+                if (lt < n) key = scout.key(lt), of = scout.owner_of_key(lt);
+                const bool plain = all_plain || (part.seg == 0 && !any_scout(lt < n && key.place >= scout.wishes().least));
+                if (!plain) {  // a bit for each key, of every kind of row that it may be for
+                    const Wishes<kTcRows> &w = scout.wishes();
+                    const bool own = part.seg == 1, there = key.at != kNowhere;
+                    const unsigned of0 = own ? __reduce_min_sync(~0u, of) : 0, of1 = own ? __reduce_max_sync(~0u, of == kNobody ? 0 : of) : 0;
+#pragma unroll 1
+                    for (int i = 0; i < kScouts; i += 32) {
+                        const int of_kind = lane < w.n[i / 32] ? w.kind[i + lane].member : kNobody;
+                        unsigned word = 0;
+#pragma unroll 1
+                        for (unsigned kinds = __ballot_sync(~0u, of_kind >= of0 && of_kind <= of1); kinds; kinds &= kinds - 1) {
+                            const int k = __ffs(kinds) - 1;
+                            const Wish x = w.kind[i + k];
+                            const unsigned those = __ballot_sync(~0u, there && (!own || of == x.member) && x.is_for(key.place, key.row, key.col));
+                            if (lane == k) word = those;
+                        }
+                        meta.bits[i + lane][lw] = word;
                     }
+                } else if (part.seg == 1 && of != kNobody) {
+                    if (lt == 0 || scout.owner_of_key(lt - 1) != of) meta.lo[of] = (uint8_t)lt;
+                    if (lt == n - 1 || scout.owner_of_key(lt + 1) != of) meta.hi[of] = (uint8_t)(lt + 1);
                 }
-                meta.place[lt] = key.place, meta.row[lt] = key.row, meta.col[lt] = key.col, meta.at[lt] = key.at;
-                plain = __all_sync(~0u, plain);
-                if (lane == 0) reinterpret_cast<uint8_t *>(&meta.plain)[lw] = plain;
+                meta.at[lt] = key.at;
                 const unsigned before = __shfl_up_sync(~0u, key.at, 1);
                 const unsigned follows = __ballot_sync(~0u, key.at != kNowhere && (lt % kRun == 0 || key.at == before + p.slot_step));
                 const unsigned runs = maps.run ? ((follows & 0xffff) == 0xffff ? 1 : 0) | (follows >> 16 == 0xffff ? 2 : 0) : 0;
                 if (lane == 0) meta.runs[lw] = (uint8_t)runs;
-                if (lt == 0) meta.n = n, meta.first = first, meta.last = last, meta.ranged = part.seg, meta.x16 = (unsigned)part.kv * p.head16;
+                if (lt == 0)
+                    meta.n = n, meta.flags = (first ? kFirst : 0) | (last ? kLast : 0) | (!plain ? kBits : part.seg ? kRanged : 0), meta.x16 = (unsigned)part.kv * p.head16;
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar(sm.meta_full[t % kMetas]));
                 scout.taken(n);
@@ -1202,17 +1209,53 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
         if (lane == 0) mbar_arrive(bar(sm.meta_full[t % kMetas]));
         if (scout.bad) atomicOr(p.cache.status, kCacheBad);
     } else if (warp < kMmaWarp) {
-        // ------------------------------------------------------------------ copies of keys (first warp) and values (second)
+        // ------------------------------------------------------------------ copies of queries and keys (first warp) and values (second)
         // Runs by one lane, the rest row by row.
         const bool leader = elect_one(), v = warp != kCopyWarp0;
         const CUtensorMap *map = v ? &maps.v : &maps.k;
         const int chunk = lane & 7, sub = lane >> 3;  // of a copy of four rows
         const unsigned stride = p.row16 * 16;
+        const auto copy_queries = [&](int qb) {  // of the part that comes next
+            const Part &part = sm.part[qb];
+            const uint32_t q = smem_u32(sm.q[qb]);
+            const int n_rows = part.n_rows, b = part.b, head0 = part.kv * p.group + part.tile * kTcRows, at0 = part.tile * kTcRows;
+#pragma unroll 2
+            for (int row = sub; row < n_rows; row += 4) {
+                const int member = by_group(p, at0 + row);
+                const __nv_bfloat16 *from = (const __nv_bfloat16 *)p.Q + (b + member) * p.q_batch + (head0 + row - member * p.group) * p.q_head + chunk * 8;
+                const uint32_t to = q + row * 128 + ((chunk ^ (row & 7)) << 4);
+#pragma unroll
+                for (int h = 0; h < kHalves; ++h)
+                    if (h * 8 + chunk < p.d / 8) cp_async16(to + h * S::kHalf, from + 64 * h);
+            }
+            if (p.flip) {  // a negative scale: its sign goes to the queries
+                asm volatile("cp.async.wait_all;" ::: "memory");
+#pragma unroll 1
+                for (int row = sub; row < n_rows; row += 4)
+#pragma unroll 1
+                    for (int h = 0; h < kHalves; ++h) {
+                        uint4 *x = reinterpret_cast<uint4 *>(sm.q[qb] + h * S::kHalf + row * 128 + ((chunk ^ (row & 7)) << 4));
+                        constexpr uint32_t kSigns = 0x80008000u;
+                        *x = make_uint4(x->x ^ kSigns, x->y ^ kSigns, x->z ^ kSigns, x->w ^ kSigns);
+                    }
+            }
+            __syncwarp();
+            cp_async_arrive(bar(sm.q_full[qb]));
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(sm.q_full[qb]));
+        };
+        int parts = 0;
+        bool asked = false;  // the queries of part number `parts`
 #pragma unroll 1
         for (int t = 0, c = 0;; ++t) {
+            if (!v && !asked) {
+                if (!wait(sm.part_full[parts & 1], parts / 2 & 1) || sm.part[parts & 1].n_rows == 0) break;
+                copy_queries(parts & 1);
+                asked = true;
+            }
             const Meta &meta = sm.meta[t % kMetas];
             if (!wait(sm.meta_full[t % kMetas], t / kMetas & 1)) break;
-            const int n = meta.n;
+            const int n = meta.n, last = meta.flags & kLast;
             if (n < 0) break;
             if (n > 0) {
                 const int stage = c % kStages;
@@ -1260,6 +1303,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
                 if (lane == 0) mbar_arrive_expect_tx(bar(full), __popc(runs) * kHalves * kRun * 128);  // (behind all that has been asked for)
                 ++c;
             }
+            if (last) ++parts, asked = false;
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(sm.meta_empty[t % kMetas]));
         }
@@ -1275,7 +1319,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
         for (int t = 0;; ++t) {
             const Meta &meta = sm.meta[t % kMetas];
             if (!wait(sm.meta_full[t % kMetas], t / kMetas & 1)) break;
-            const int n = meta.n, last = meta.last;
+            const int n = meta.n, last = meta.flags & kLast;
             if (n < 0) break;
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(sm.meta_empty[t % kMetas]));
@@ -1325,7 +1369,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
                 if (leader) mma_commit(bar(sm.q_empty[parts & 1]));
                 __syncwarp();
             }
-            c += n > 0, parts += last;
+            c += n > 0, parts += last != 0;
         }
         if (leader) mma_commit(bar(sm.final_));  // nothing of this block may still run on the tensor pipe when its memory is freed
         __syncwarp();
