@@ -25,7 +25,7 @@ namespace mate {
 namespace {
 
 constexpr int kUnit = 32;     // tokens of a unit of work: what a warp looks through in one go
-constexpr int kOver = 4;      // units that an item costs besides its tokens
+constexpr int kOver = 8;      // units that an item costs besides its tokens
 constexpr int kMaxBatch = 4096;
 constexpr int kMaxHeads = 1024;
 constexpr int kNever = INT32_MIN;  // an id that no token has
@@ -219,7 +219,7 @@ __device__ __forceinline__ void put_joint(const SharedParams &p, const Part &par
 __device__ __forceinline__ bool attends(int want_row, int want_col, int below, int place, int row, int col) {
     return place < below || row == want_row || col == want_col;
 }
-constexpr int kScouts = 128;
+constexpr int kScouts = 128, kKinds = 4;
 struct alignas(16) Wish {
     int row, col, below;
     int member;  // of own tokens: only those of this entry (of the batch) count
@@ -230,12 +230,13 @@ template <int RT>
 struct Rows {
     short kind[RT];  // place of a row's wish among those below, -1: it attends nothing
 };
-// and, as those who look for keys need them, without repetitions of the row before: the rows of 32 have places of their own.
+// and, as those who look for keys need them, without repetitions of the row before: the rows of a warp have 32 places of their own, up to a
+// multiple of kKinds of them in use.
 template <int RT>
 struct Wishes {
     int least, most;  // of `below` over the rows that are there
     int views;        // 1: some want a row, 2: a column
-    int n[kScouts / 32];
+    uint8_t n[kScouts / 32];
     Wish kind[kScouts];
     __device__ void clear() { least = INT32_MAX, most = INT32_MIN, views = 0; }
 };
@@ -321,6 +322,7 @@ struct Scout {
         if (tid == 0) sm.before[0] = 0;
         sync();
     }
+    __device__ bool is_leader(int i) const { return sm.leaders[i >> 5] >> (i & 31) & 1; }
     // The first entry from `entry` on that leads a group, kScouts if there is none.
     __device__ int leader_from(int from) const {
         for (int w = from >> 5; w < 4; ++w) {
@@ -334,6 +336,22 @@ struct Scout {
         parts = looks = item = u = tiles = n_units = 0, entry = -1, bad = false;
         if (tid == 0) sm.wishes[0].clear();
         hold(found.entries);
+        // the leader whose items `in` is among: its number less one, with what is left of `in` there
+        const unsigned cost = is_leader(tid) ? (unsigned)(p.kv_heads * group_tiles<RT>(p, sm.entries[tid])) * (kOver + units_of(sm.entries[tid].shared)) : 0;
+        unsigned sum = cost;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const unsigned y = __shfl_up_sync(~0u, sum, o);
+            if ((tid & 31) >= o) sum += y;
+        }
+        if ((tid & 31) == 31) sm.counts[1][tid >> 5] = (int)sum;
+        sync();
+        for (int w = 0; w < tid >> 5; ++w) sum += (unsigned)sm.counts[1][w];
+        if (sum - cost <= in && in < sum) sm.counts[0][0] = tid, sm.counts[0][1] = (int)(in - (sum - cost));
+        if (tid == kScouts - 1 && sum <= in) sm.counts[0][0] = kScouts, sm.counts[0][1] = (int)(in - sum);
+        sync();
+        entry = sm.counts[0][0] - 1, in = (unsigned)sm.counts[0][1];
+        sync();
     }
     // The next part of the share.  (It comes to an end whatever it finds: every part takes a unit off the share.)
     __device__ bool next_part(Part &part) {
@@ -450,9 +468,11 @@ struct Scout {
                           (__shfl_up_sync(~0u, x.below, 1) == x.below) & (__shfl_up_sync(~0u, x.member, 1) == x.member);
         const unsigned begins = __ballot_sync(~0u, lane == 0 || !same);
         const int kind = (tid & ~31) + __popc(begins & (2u << lane) - 1) - 1;
+        const int kinds = most < 0 ? 0 : (__popc(begins) + kKinds - 1) & -kKinds;
         if (begins >> lane & 1) w.kind[kind] = x;
+        if (lane >= __popc(begins) && lane < kinds) w.kind[tid] = {kNever, kNever, -2, kNobody};
         if (lane == 0) {
-            w.n[tid >> 5] = most < 0 ? 0 : __popc(begins);
+            w.n[tid >> 5] = (uint8_t)kinds;
             if (most >= 0) atomicMin(&w.least, least), atomicMax(&w.most, most), atomicOr(&w.views, views);
         }
         if (tid < RT) rows.kind[tid] = (short)(x.below < 0 ? -1 : kind);
@@ -488,14 +508,14 @@ struct Scout {
             for (int k = 0; k < 2; ++k) is[k] = key[k].place < w.most;
             if (__any_sync(~0u, (key[0].at != kNowhere && !is[0]) || (key[1].at != kNowhere && !is[1])))
 #pragma unroll 1
-                for (int i = 0; i < kScouts; i += 32) {
-                    const int n = w.n[i / 32];
-#pragma unroll 4
-                    for (int j = 0; j < n; ++j) {
-                        const int row = w.kind[i + j].row, col = w.kind[i + j].col;
-                        is[0] |= (key[0].row == row) | (key[0].col == col), is[1] |= (key[1].row == row) | (key[1].col == col);
-                    }
-                }
+                for (int i = 0; i < kScouts; i += 32)
+#pragma unroll 1
+                    for (int j = i; j < i + w.n[i / 32]; j += kKinds)
+#pragma unroll
+                        for (int k = 0; k < kKinds; ++k) {
+                            const int row = w.kind[j + k].row, col = w.kind[j + k].col;
+                            is[0] |= (key[0].row == row) | (key[0].col == col), is[1] |= (key[1].row == row) | (key[1].col == col);
+                        }
         }
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
@@ -973,12 +993,14 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
                     if (!wait(sm.v_full[stage], c / kStages & 1)) break;
                     __nv_bfloat162 z = __floats2bfloat162_rn(0.f, 0.f);
                     const uint4 *v = reinterpret_cast<const uint4 *>(sm.v[stage]);
-#pragma unroll 2
-                    for (int i = r; i < kHalves * kTcKeys * 8; i += 128) {
-                        const uint4 y = (i >> 3 & (kTcKeys - 1)) < n ? v[i] : make_uint4(0, 0, 0, 0);
-                        for (uint32_t w : {y.x, y.y, y.z, y.w})
-                            z = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&w), __floats2bfloat162_rn(0.f, 0.f), z);
-                    }
+#pragma unroll 1
+                    for (int h = 0; h < kHalves; ++h, v += kTcKeys * 8)
+#pragma unroll 4
+                        for (int i = r; i < n * 8; i += 128) {
+                            const uint4 y = v[i];
+                            for (uint32_t w : {y.x, y.y, y.z, y.w})
+                                z = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&w), __floats2bfloat162_rn(0.f, 0.f), z);
+                        }
                     if (__any_sync(~0u, !(__low2float(z) == 0.f && __high2float(z) == 0.f)) && lane == 0) *(volatile int *)&sm.odd[team] = c + 1;
                     if (!sync(sm.team[team], teams)) break;
                     odd = *(volatile int *)&sm.odd[team] == c + 1;
@@ -1174,15 +1196,21 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
                     const unsigned of0 = own ? __reduce_min_sync(~0u, of) : 0, of1 = own ? __reduce_max_sync(~0u, of == kNobody ? 0 : of) : 0;
 #pragma unroll 1
                     for (int i = 0; i < kScouts; i += 32) {
-                        const int of_kind = lane < w.n[i / 32] ? w.kind[i + lane].member : kNobody;
+                        int k0 = 0, k1 = w.n[i / 32];
+                        if (own) {  // those of the keys' owners (they are in order)
+                            const int of_kind = lane < k1 ? w.kind[i + lane].member : kNobody;
+                            const unsigned kinds = __ballot_sync(~0u, of_kind >= of0 && of_kind <= of1);
+                            k0 = kinds ? (__ffs(kinds) - 1) & -kKinds : 32, k1 = 32 - __clz(kinds);
+                        }
                         unsigned word = 0;
 #pragma unroll 1
-                        for (unsigned kinds = __ballot_sync(~0u, of_kind >= of0 && of_kind <= of1); kinds; kinds &= kinds - 1) {
-                            const int k = __ffs(kinds) - 1;
-                            const Wish x = w.kind[i + k];
-                            const unsigned those = __ballot_sync(~0u, there && (!own || of == x.member) && x.is_for(key.place, key.row, key.col));
-                            if (lane == k) word = those;
-                        }
+                        for (int k = i + k0; k < i + k1; k += kKinds)
+#pragma unroll
+                            for (int j = 0; j < kKinds; ++j) {
+                                const Wish x = w.kind[k + j];
+                                const unsigned those = __ballot_sync(~0u, there && (!own || of == x.member) && x.is_for(key.place, key.row, key.col));
+                                if (lt % 32 == k + j - i) word = those;
+                            }
                         meta.bits[i + lane][lw] = word;
                     }
                 } else if (part.seg == 1 && of != kNobody) {
