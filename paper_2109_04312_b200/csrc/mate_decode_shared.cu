@@ -265,6 +265,7 @@ struct ScoutSmem {
     int counts[2][8];        // of the units' keys; plus kDense
 };
 constexpr int kDense = 64, kNobody = 255, kRun = 16;
+constexpr int kLooked = kUnits * (kUnit + kRun - 1);  // what a look may add to the list, at most
 // Where the loads of a look stand.
 struct Asked {
     int j, owner, page;
@@ -764,6 +765,8 @@ struct TcShape {
     static constexpr int kHalf = kTcKeys * 128;
     static constexpr int kStages = DP == 64 ? 4 : 2;            // tiles of keys, and of values
 };
+constexpr int kAhead = kList - kLooked - kTcKeys + 1;  // a look comes while a tile waits for its place, where the list has room for it
+static_assert(kAhead >= 0, "room for a look behind what is less than a tile");
 enum { kFirst = 1, kLast = 2, kRanged = 4, kBits = 8 };  // tiles of a part; keys lo[m] to hi[m] are for the rows of entry m, or as bits[kind] says, else
                                                           // all keys for all rows that attend anything
 struct alignas(16) Meta {
@@ -991,16 +994,18 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
                 bool odd = false;
                 if (flags & (kRanged | kBits)) {  // a weight 0 does not undo a value that is not a number: is there one?
                     if (!wait(sm.v_full[stage], c / kStages & 1)) break;
-                    __nv_bfloat162 z = __floats2bfloat162_rn(0.f, 0.f);
+                    const __nv_bfloat162 zero = __floats2bfloat162_rn(0.f, 0.f);
+                    __nv_bfloat162 z = zero, z2 = zero;
                     const uint4 *v = reinterpret_cast<const uint4 *>(sm.v[stage]);
 #pragma unroll 1
                     for (int h = 0; h < kHalves; ++h, v += kTcKeys * 8)
-#pragma unroll 4
+#pragma unroll 8
                         for (int i = r; i < n * 8; i += 128) {
                             const uint4 y = v[i];
-                            for (uint32_t w : {y.x, y.y, y.z, y.w})
-                                z = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&w), __floats2bfloat162_rn(0.f, 0.f), z);
+                            for (uint32_t w : {y.x, y.y}) z = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&w), zero, z);
+                            for (uint32_t w : {y.z, y.w}) z2 = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&w), zero, z2);
                         }
+                    z = __hadd2(z, z2);
                     if (__any_sync(~0u, !(__low2float(z) == 0.f && __high2float(z) == 0.f)) && lane == 0) *(volatile int *)&sm.odd[team] = c + 1;
                     if (!sync(sm.team[team], teams)) break;
                     odd = *(volatile int *)&sm.odd[team] == c + 1;
@@ -1179,7 +1184,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
 #pragma unroll 1
             for (bool first = true; !last; first = false, ++t) {
 #pragma unroll 1
-                while (scout.pending < kTcKeys && scout.more()) scout.look();
+                while (scout.pending < kTcKeys + (first ? 0 : kAhead) && scout.more()) scout.look();
                 const int n = min(scout.pending, kTcKeys);
                 last = scout.pending <= kTcKeys && !scout.more();
                 if (t >= kMetas) ok &= wait(sm.meta_empty[t % kMetas], (t / kMetas - 1) & 1);
@@ -1443,7 +1448,7 @@ __global__ void __launch_bounds__(1024) shared_join_kernel(const __grid_constant
             if (joint.slot < 0) {
                 const size_t whole = (size_t)(seg * p.B + b) * p.heads + kv * p.group + g;
                 of = {p.whole + whole * p.d, p.whole_stats + whole, 0, 0, 4, 1};
-            } else {
+            } else if (joint.slot <= 1 && in_range(joint.first, p.blocks) && joint.total > 0) {  // (it may be what lay there, after a wait ran out)
                 // up to the block that has the item's last unit: the last one whose share begins in front of the item's end
                 const int64_t blocks = min((int64_t)joint.total, (int64_t)p.blocks), last = ((int64_t)joint.end * blocks - 1) / joint.total;
                 const float *from = p.parts + 2 * joint.first * part_floats(RT, p.d);
