@@ -413,7 +413,7 @@ class Cache:
                    head_view)
 
     def status(self):
-        """Waits, and raises MateError if a call found something out of range, or no free page, since the last time."""
+        """Waits, and raises MateError if a call found something out of range, or no free page, or gave up on a wait, since the last time."""
         self._native.cache_status(self._info)
 
 

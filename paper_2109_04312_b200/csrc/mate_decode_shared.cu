@@ -1532,7 +1532,7 @@ Workspace workspace_of(const mate_cache_t *c, int B) {
 TcMaps maps_of(SharedParams &p, const mate_cache_t *c) {
     TcMaps m = {};
     const int64_t slot = c->slot_stride, rows = slot > 0 ? ((int64_t)(c->pages - 1) * c->page_stride + (c->kv_heads - 1) * c->head_stride) / slot + c->page_size : 0;
-    const bool fits = c->page_size % kRun == 0 && slot >= c->d && (c->pages == 1 || c->page_stride % slot == 0) && (slot == c->d || c->d % 64 == 0) && rows <= INT32_MAX;
+    const bool fits = c->page_size % kRun == 0 && slot >= c->d && (c->pages == 1 || c->page_stride % slot == 0) && (slot == c->d || c->d % 64 == 0) && rows <= INT32_MAX && slot <= 1 << 27;
     if (fits && (c->kv_heads - 1) * (c->head_stride % slot) + c->d <= slot && make_box_map(&m.k, p.cache.k, (size_t)slot, (size_t)rows, (size_t)slot * 2, kRun) &&
         make_box_map(&m.v, p.cache.v, (size_t)slot, (size_t)rows, (size_t)slot * 2, kRun))
         m.run = kRun;

@@ -324,6 +324,84 @@ def test_many_entries(dtype):
         m.mate_attn_decode_shared(case.c, Q[:1].expand(n + 1, 4, 16).contiguous(), more, more, torch.zeros(3, n + 1, dtype=torch.int32, device="cuda"), seqs=more)
 
 
+LAYOUTS = {  # of keys and values in memory that they share with one another, or with what is nobody's: [layers, pages, heads, slots, d]
+    "keys and values slot by slot": lambda x, L, P, H, ps, d: [x(L, P, ps, 2, H, d)[:, :, :, i].transpose(2, 3) for i in range(2)],
+    "keys and values of a head": lambda x, L, P, H, ps, d: [x(L, P, ps, H, 2, d)[..., i, :].transpose(2, 3) for i in range(2)],
+    "keys and values page by page": lambda x, L, P, H, ps, d: [x(L, P, 2, H, ps, d)[:, :, i] for i in range(2)],
+    "slots with room behind": lambda x, L, P, H, ps, d: [x(L, P, H, ps, d + 8)[..., :d] for i in range(2)],
+    "pages with room behind": lambda x, L, P, H, ps, d: [x(L, P, H * ps * d + 24)[..., 16:-8].unflatten(2, (H, ps, d)) for i in range(2)],
+}
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("layout", LAYOUTS)
+@pytest.mark.parametrize("d,ps,dtype", [(64, 16, "bf16"), (128, 48, "bf16"), (128, 24, "bf16"), (96, 32, "bf16"), (40, 16, "bf16"), (64, 16, "f32")])
+def test_layouts(layout, d, ps, dtype):
+    # what lies between the rows is not a number
+    import paper_2109_04312_b200 as m
+    case = Shared(m, [(10, [200, 3, 150, 70]), (0, [300, 40])], 6, 2, d, ps, [0, 0, 1, 1, 2, 0], dtype, seed=14, layers=2, pad=0.02)
+    c = case.c
+    k, v = LAYOUTS[layout](lambda *shape: torch.full(shape, float("nan"), dtype=DT[dtype], device="cuda"), *c.k.shape)
+    k.copy_(c.k), v.copy_(c.v)
+    case.c = m.Cache(k, v, c.row_ids, c.col_ids, c.table, c.lens, c.prefix, c.refs, case.views)
+    run(m, case, layer=1)
+    case.c.status()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_pages_of_many_slots(dtype):
+    import paper_2109_04312_b200 as m
+    case = Shared(m, [(0, [70000]), (1, [5, 0])], 2, 1, 16, 1 << 16, [0, 2], dtype, seed=15, spare=0, rows=500, cols=40)
+    run(m, case)
+    case.c.status()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_the_largest_group(dtype):
+    # one sequence as often as a list may have it, and rows of many entries in a tile
+    import paper_2109_04312_b200 as m
+    n = 4096
+    case = Shared(m, [(3, [2, 9])], 2, 2, 16, 8, [0, 1], dtype, seed=16)
+    seqs = [int(i % 7 == 3) for i in range(n)]
+    groups = np.repeat([[0], [n], [24]], n, 1)
+    assert (m.mate_cache_groups(case.c, i32(seqs)).cpu().numpy() == groups).all()
+    q_ids = case.new_ids(seqs)
+    Q = torch.randn(n, 2, 16, device="cuda").to(DT[dtype])
+    O, LSE = m.mate_attn_decode_shared(case.c, Q, i32(q_ids[0]), i32(q_ids[1]), i32(groups), seqs=i32(seqs))
+    some = np.random.default_rng(1).permutation(n)[:300]
+    case.check(Q[some.tolist()], [seqs[i] for i in some], q_ids[:, some], O[some.tolist()], LSE[some.tolist()])
+    case.c.status()
+
+
+@pytest.mark.gpu
+def test_the_same_bits_from_call_to_call_and_from_cold_memory():
+    # (a wait that runs out, or rows that are read before they are there, would show)
+    import paper_2109_04312_b200 as m
+    for groups, H, Hk, d, ps in (([(4, [3, 0, 20]), (2, [40])], 1024, 1, 16, 8), ([(60, [300, 9, 0])] * 20, 6, 2, 64, 16), ([(40, [90] * 60)], 8, 2, 128, 16)):
+        case = Shared(m, groups, H, Hk, d, ps, [h % 3 for h in range(H)], seed=17, prefix=30)
+        Q, q_ids, O, LSE = run(m, case)
+        args, junk = (i32(q_ids[0]), i32(q_ids[1]), i32(case.groups)), torch.empty(1 << 28, dtype=torch.uint8, device="cuda")
+        for i in range(60):
+            if i % 3 == 0:
+                junk.fill_(i)
+            o, l = m.mate_attn_decode_shared(case.c, Q, *args)
+            assert torch.equal(o, O) and torch.equal(l, LSE), i
+        case.c.status()
+
+
+@pytest.mark.gpu
+def test_a_wait_that_ran_out_is_reported_once():
+    import paper_2109_04312_b200 as m
+    case = Shared(m, [(1, [1])], 1, 1, 16, 16, [0])
+    case.c.status_word.fill_(4)
+    with pytest.raises(m.MateError) as e:
+        case.c.status()
+    assert e.value.status == -5
+    case.c.status()
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_offsets_beyond_32_bits(dtype):
