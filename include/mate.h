@@ -443,11 +443,17 @@ int mate_attn_decode(const mate_cache_t *cache, int layer, const void *Q, const 
  *              the others' must be the same there; each entry has a prefix and ids of its own
  *   workspace  device, 256-byte aligned, mate_cache_shared_workspace_bytes; contents undefined afterwards; calls that overlap need one each
  * Groups that do not fit together, or of more tokens than a sequence (or max_len) has, are left out: their entries are taken
- * alone, or attend their own tokens only, and status says so.  B is at most 4096.  All other arguments, limits and errors as for
- * mate_attn_decode. */
+ * alone, or attend their own tokens only, and status says so.  B is at most 4096.
+ *   flags      0: where the batch may read no more than 128 MB (bf16) or 1 GB (fp32) one sequence after another -- B max_len kv_heads
+ *              keys and values --, that is the faster way, and taken: the results are mate_attn_decode's; MATE_SHARED_ALWAYS: the shared
+ *              tokens are read once all the same
+ * Where they are read once and the type is bf16, weights enter the product with the values as the sum of two bf16, with 16 bits
+ * (mate_attn_decode: with all of their 24).  All other arguments, limits and errors as for mate_attn_decode. */
 int mate_attn_decode_shared(const mate_cache_t *cache, int layer, const void *Q, const int64_t *q_stride, int B, const int32_t *seqs,
-                            const int32_t *row_ids, const int32_t *col_ids, const int32_t *groups, float scale, int max_len, void *O,
-                            float *LSE, void *workspace, size_t workspace_bytes, void *stream);
+                            const int32_t *row_ids, const int32_t *col_ids, const int32_t *groups, float scale, int max_len, unsigned flags,
+                            void *O, float *LSE, void *workspace, size_t workspace_bytes, void *stream);
+
+enum { MATE_SHARED_ALWAYS = 1 };
 
 /* Scratch of mate_attn_decode_shared with n tokens. */
 int mate_cache_shared_workspace_bytes(const mate_cache_t *cache, int n, size_t *bytes);

@@ -473,9 +473,11 @@ def mate_attn_decode(cache, Q, row_ids, col_ids, seqs=None, layer=0, scale=None,
     return cache._native.attn_decode(cache._info, layer, Q, seqs, row_ids, col_ids, scale, max_len, out, lse)
 
 
-def mate_attn_decode_shared(cache, Q, row_ids, col_ids, groups, seqs=None, layer=0, scale=None, max_len=None, out=None, lse=None):
+def mate_attn_decode_shared(cache, Q, row_ids, col_ids, groups, seqs=None, layer=0, scale=None, max_len=None, out=None, lse=None,
+                            always=False):
     """mate_attn_decode for sequences that share their first tokens, such as beams or questions about one table: what a group shares is read
     once for all of its sequences (see mate_attn_decode_shared in mate.h).  groups: int32 [3, B], what mate_cache_groups returns for the same
-    seqs: call it when the batch or the pages of its sequences have changed, once for all layers.  The rest as for mate_attn_decode.
+    seqs: call it when the batch or the pages of its sequences have changed, once for all layers.  max_len: up to where tokens count, and how much
+    the batch may have to read; where that is little each sequence is read by itself, unless always is set.  The rest as for mate_attn_decode.
     Returns (O, LSE)."""
-    return cache._native.attn_decode_shared(cache._info, layer, Q, seqs, row_ids, col_ids, scale, max_len, out, lse, groups)
+    return cache._native.attn_decode_shared(cache._info, layer, Q, seqs, row_ids, col_ids, scale, max_len, out, lse, groups, always)

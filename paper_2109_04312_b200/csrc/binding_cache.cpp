@@ -504,10 +504,10 @@ PyObject *cache_status(PyObject *, PyObject *o) {
 }
 
 // attn_decode(info, layer, Q, seqs, row_ids, col_ids, scale, max_len, out, lse) -> (O, LSE)
-// attn_decode_shared(the same, groups)
+// attn_decode_shared(the same, groups, always)
 PyObject *decode_of(PyObject *const *a, Py_ssize_t n, bool shared) {
     return guarded([&]() -> PyObject * {
-        if (n != 10 + shared) fail(PyExc_TypeError, shared ? "attn_decode_shared takes 11 arguments" : "attn_decode takes 10 arguments");
+        if (n != (shared ? 12 : 10)) fail(PyExc_TypeError, shared ? "attn_decode_shared takes 12 arguments" : "attn_decode takes 10 arguments");
         const CacheInfo &ci = cache_info(a[0]);
         const int layer = as_int(whole(a[1]), "layer");
         const at::Tensor &Q = on_gpu(a[2], "Q", &ci.device);
@@ -521,6 +521,8 @@ PyObject *decode_of(PyObject *const *a, Py_ssize_t n, bool shared) {
         const float scale = scale_of(a[6], ci.c.d);
         const int max_len = a[7] == Py_None ? 0 : as_int(whole(a[7]), "max_len");
         if (a[7] != Py_None && max_len == 0) fail_shape("max_len", "positive");
+        const int always = shared ? PyObject_IsTrue(a[11]) : 0;
+        if (always < 0) throw Raised();
         at::Tensor O, LSE;
         if (a[8] != Py_None) {
             O = on_gpu(a[8], "O", &ci.device);
@@ -545,8 +547,8 @@ PyObject *decode_of(PyObject *const *a, Py_ssize_t n, bool shared) {
             if (!O.defined()) O = empty(Q.sizes(), ci.type, ci.device);
             if (!LSE.defined()) LSE = empty(Q.sizes().slice(0, 2), at::kFloat, ci.device);
             const Scratch ws(b ? need : 0, ci.device);
-            status = shared ? lib.decode_shared(&ci.c, layer, Q.data_ptr(), qs, b, seqs, row, col, groups, scale, max_len, O.data_ptr(),
-                                                LSE.data_ptr<float>(), ws.ptr, ws.bytes, on.stream.stream())
+            status = shared ? lib.decode_shared(&ci.c, layer, Q.data_ptr(), qs, b, seqs, row, col, groups, scale, max_len,
+                                                always ? MATE_SHARED_ALWAYS : 0, O.data_ptr(), LSE.data_ptr<float>(), ws.ptr, ws.bytes, on.stream.stream())
                             : lib.decode(&ci.c, layer, Q.data_ptr(), qs, b, seqs, row, col, scale, max_len, O.data_ptr(), LSE.data_ptr<float>(),
                                          ws.ptr, ws.bytes, on.stream.stream());
         }

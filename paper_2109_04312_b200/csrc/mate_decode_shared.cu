@@ -22,6 +22,7 @@
 #include "tc_tiles.cuh"
 
 namespace mate {
+size_t decode_workspace(const mate_cache_t *cache, int B);  // mate_decode.cu
 namespace {
 
 constexpr int kUnit = 32;     // tokens of a unit of work: what a warp looks through in one go
@@ -1507,7 +1508,28 @@ __global__ void __launch_bounds__(1024) shared_join_kernel(const __grid_constant
     if (c4 == 0) p.LSE[out] = natural(m, l);
 }
 
+// ---- groups that nobody goes by
+
+// Whether they fit together, where each sequence is read by itself.  (Looked at beside the kernel in front, which has waited for whoever wrote them
+// before it let this one start; what is launched next counts on both.)
+constexpr int kCheckThreads = 128;
+__global__ void __launch_bounds__(kCheckThreads) check_kernel(const __grid_constant__ SharedParams p) {
+    ptx::launch_dependents();
+    const int b = blockIdx.x * kCheckThreads + threadIdx.x;
+    Entry e = {};
+    if (b < p.B) entry_of(p, b, &e);
+    ptx::wait_prior_grid();
+    if (e.bad) atomicOr(p.cache.status, kCacheBad);
+}
+
 // ---- host
+
+// Up to here a batch is faster read one sequence after another, by all that the host knows: keys and values of all sequences at their longest.
+// bf16, all in one group, 12 heads of 64 or 8 of 4 x 128 elements: 4 sequences of 4096 tokens (51 and 68 MB) 14 and 17 us alone, 21 and 20 shared;
+// 16 of 4096 (203 and 271 MB) 31 and 36, 21 and 21.  (In eight groups of 8 both take as long at 800 MB, and without groups one by one is always
+// the faster way.)  fp32, whose products are not made by the tensor cores: 64 sequences of 4096 tokens, 2 heads of 3 x 48, 203 MB, 44 and 48;
+// of 16384, 807 MB, 136 and 106; 8 heads of 4 x 128, 541 MB 85 and 101, 2.2 GB 292 and 268.
+double alone_bytes(const mate_cache_t *c) { return c->dtype == MATE_F32 ? 1024.0 * (1 << 20) : 128.0 * (1 << 20); }
 
 int rows_of_tile(const mate_cache_t *c) { return c->dtype == MATE_F32 ? kSimtRows : kTcRows; }
 int pack_of(const mate_cache_t *c) { return std::max(1, rows_of_tile(c) / (c->heads / c->kv_heads)); }
@@ -1579,15 +1601,16 @@ int mate_cache_shared_workspace_bytes(const mate_cache_t *cache, int n, size_t *
     const int rc = check_cache(cache);
     if (rc != MATE_OK) return rc;
     if (n < 0 || !bytes) return MATE_ERR_INVALID_ARG;
-    *bytes = n > 0 ? workspace_of(cache, n).bytes : 0;
+    *bytes = n > 0 ? std::max(workspace_of(cache, n).bytes, decode_workspace(cache, n)) : 0;
     return MATE_OK;
 }
 
 int mate_attn_decode_shared(const mate_cache_t *cache, int layer, const void *Q, const int64_t *q_stride, int B, const int32_t *seqs,
-                            const int32_t *row_ids, const int32_t *col_ids, const int32_t *groups, float scale, int max_len, void *O, float *LSE,
-                            void *workspace, size_t workspace_bytes, void *stream) {
+                            const int32_t *row_ids, const int32_t *col_ids, const int32_t *groups, float scale, int max_len, unsigned flags,
+                            void *O, float *LSE, void *workspace, size_t workspace_bytes, void *stream) {
     int rc = check_cache(cache);
     if (rc != MATE_OK) return rc;
+    if (flags & ~(unsigned)MATE_SHARED_ALWAYS) return MATE_ERR_INVALID_ARG;
     if (layer < 0 || layer >= cache->layers || B < 0 || max_len < 0 || (!seqs && B > cache->seqs)) return MATE_ERR_INVALID_ARG;
     if (B > 0 && (!Q || !q_stride || !row_ids || !col_ids || !groups || !O || !LSE)) return MATE_ERR_INVALID_ARG;
     if (!std::isfinite(scale)) return MATE_ERR_INVALID_ARG;
@@ -1604,7 +1627,7 @@ int mate_attn_decode_shared(const mate_cache_t *cache, int layer, const void *Q,
     // units of the batch, shared and own, are 32-bit numbers
     if (B > kMaxBatch || (int64_t)B * cache->kv_heads * own_tiles(cache) > INT32_MAX / 2 / (kOver + units_of(max_len))) return MATE_ERR_UNSUPPORTED;
     const Workspace w = workspace_of(cache, B);
-    if (!workspace || workspace_bytes < w.bytes) return MATE_ERR_WORKSPACE;
+    if (!workspace || workspace_bytes < std::max(w.bytes, decode_workspace(cache, B))) return MATE_ERR_WORKSPACE;
     if (!is_aligned(workspace, 256)) return MATE_ERR_ALIGNMENT;
     SharedParams p = {};
     p.cache = cache_args(cache, layer);
@@ -1633,6 +1656,11 @@ int mate_attn_decode_shared(const mate_cache_t *cache, int layer, const void *Q,
         p.scale_log2 = std::fmax(std::fabs(p.scale_log2), 0x1p-126f);
     }
     cudaStream_t st = (cudaStream_t)stream;
+    if (!(flags & MATE_SHARED_ALWAYS) && 2.0 * elem_size(cache->dtype) * B * max_len * cache->kv_heads * cache->d <= alone_bytes(cache)) {
+        rc = mate_attn_decode(cache, layer, Q, q_stride, B, seqs, row_ids, col_ids, scale, max_len, O, LSE, workspace, workspace_bytes, stream);
+        if (rc != MATE_OK) return rc;
+        return launch_after(check_kernel, dim3((unsigned)(B + kCheckThreads - 1) / kCheckThreads), kCheckThreads, 0, st, p) == cudaSuccess ? MATE_OK : MATE_ERR_CUDA;
+    }
     p.blocks = n_blocks(cache);
     if (cache->dtype == MATE_F32) return cache->d <= 64 ? launch<float, 64>(p, cache, st) : launch<float, 128>(p, cache, st);
     return cache->d <= 64 ? launch<__nv_bfloat16, 64>(p, cache, st) : launch<__nv_bfloat16, 128>(p, cache, st);

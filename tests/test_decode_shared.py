@@ -1,5 +1,6 @@
 """mate_attn_decode_shared against masked softmax attention in 64 bits, sequence after sequence, and against mate_attn_decode."""
 import ctypes
+import functools
 
 import numpy as np
 import pytest
@@ -61,6 +62,11 @@ class Shared(Case):
                 assert abs(LSE[i, h] - want[1]) <= bl, (i, s, h, LSE[i, h], want[1], bl)
 
 
+def together(m):
+    """What shared tokens are read once by, however small the batch."""
+    return functools.partial(m.mate_attn_decode_shared, always=True)
+
+
 def i32(x):
     return torch.tensor(np.asarray(x), dtype=torch.int32, device="cuda")
 
@@ -70,7 +76,7 @@ def run(m, case, seqs=None, groups=None, scale=None, seed=1, magnitude=1.0, laye
     groups = case.groups if groups is None else groups
     q_ids = case.new_ids(seqs) if q_ids is None else q_ids
     Q = (torch.randn(len(seqs), case.H, case.d, generator=torch.Generator().manual_seed(seed)) * magnitude).to(DT[case.dtype]).cuda()
-    O, LSE = m.mate_attn_decode_shared(case.c, Q, i32(q_ids[0]), i32(q_ids[1]), i32(groups), seqs=i32(seqs), scale=scale, layer=layer, **kw)
+    O, LSE = together(m)(case.c, Q, i32(q_ids[0]), i32(q_ids[1]), i32(groups), seqs=i32(seqs), scale=scale, layer=layer, **kw)
     case.check(Q, seqs, q_ids, O, LSE, scale, layer, kw.get("max_len", 1 << 30))
     return Q, q_ids, O, LSE
 
@@ -145,7 +151,7 @@ def test_scores_that_grow_along_the_tokens(dtype):
         for j in range(case.lens[s]):
             c.k[0, case.table[s, j // 16], :, j % 16] = 0.001 * j * 8 if (j // 128) % 2 == 0 else -1.0
     ids = np.full((2, B), TEXT, np.int32)
-    O, LSE = m.mate_attn_decode_shared(c, Q, i32(ids[0]), i32(ids[1]), i32(case.groups))
+    O, LSE = together(m)(c, Q, i32(ids[0]), i32(ids[1]), i32(case.groups))
     case.check(Q, list(range(B)), ids, O, LSE)
 
 
@@ -159,14 +165,14 @@ def test_what_is_not_a_number_reaches_the_heads_that_attend_it(dtype, d):
     q_ids = np.array([[1, 2, TEXT], [1, 2, TEXT]], np.int32)
     Q = torch.randn(B, 6, d, device="cuda").to(DT[dtype])
     args = (Q, i32(q_ids[0]), i32(q_ids[1]), i32(case.groups))
-    clean = m.mate_attn_decode_shared(c, *args)
+    clean = together(m)(c, *args)
     for what, x in (("k", float("nan")), ("v", float("nan")), ("v", float("inf")), ("v", float("-inf"))):
         for s, j in ((0, 17), (0, 200), (1, 322), (2, 330), (2, 459)):
             page, slot, shared = int(case.table[s, j // 16]), j % 16, j < 320
             t = getattr(c, what)[0, page, 1, slot]
             before = t.clone()
             t[3] = x
-            got = m.mate_attn_decode_shared(c, *args)
+            got = together(m)(c, *args)
             t.copy_(before)
             row, col = case.ids[s][:, j]
             for i in range(B):
@@ -196,17 +202,17 @@ def test_layers_views_outputs_streams(dtype):
     wide = torch.randn(B, 9, 64, device="cuda").to(DT[dtype])
     Q = wide[:, 2:8]
     args = (i32(q_ids[0]), i32(q_ids[1]), i32(case.groups))
-    want = m.mate_attn_decode_shared(case.c, Q, *args, layer=1)
+    want = together(m)(case.c, Q, *args, layer=1)
     out, lse = torch.empty(B, 6, 64, device="cuda", dtype=DT[dtype]), torch.empty(B, 6, device="cuda")
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
     with torch.cuda.stream(side):
-        r = m.mate_attn_decode_shared(case.c, Q, *args, layer=1, out=out, lse=lse)
+        r = together(m)(case.c, Q, *args, layer=1, out=out, lse=lse)
     side.synchronize()
     assert r[0] is out and r[1] is lse and torch.equal(out, want[0]) and torch.equal(lse, want[1])
     q = Q.contiguous()
-    assert torch.equal(m.mate_attn_decode_shared(case.c, q, *args, layer=1, out=q)[0], want[0])
-    e = m.mate_attn_decode_shared(case.c, Q[:0], args[0][:0], args[1][:0], args[2][:, :0].contiguous())
+    assert torch.equal(together(m)(case.c, q, *args, layer=1, out=q)[0], want[0])
+    e = together(m)(case.c, Q[:0], args[0][:0], args[1][:0], args[2][:, :0].contiguous())
     assert e[0].shape == (0, 6, 64) and e[1].shape == (0, 6)
 
 
@@ -219,13 +225,13 @@ def test_two_graphs_and_calls_on_two_streams(dtype):
     q_ids = case.new_ids(list(range(B)))
     Q = torch.randn(B, 6, 64, device="cuda").to(DT[dtype])
     args = (i32(q_ids[0]), i32(q_ids[1]), i32(case.groups))
-    want = [m.mate_attn_decode_shared(case.c, Q, *args, layer=i) for i in range(2)]
+    want = [together(m)(case.c, Q, *args, layer=i) for i in range(2)]
     graphs, outs, streams = [], [], [torch.cuda.Stream() for _ in range(2)]
     torch.cuda.synchronize()
     for i in range(2):
         g = torch.cuda.CUDAGraph()
         with torch.cuda.graph(g, stream=streams[i]):
-            outs.append(m.mate_attn_decode_shared(case.c, Q, *args, layer=i))
+            outs.append(together(m)(case.c, Q, *args, layer=i))
         graphs.append(g)
     for _ in range(20):
         for i in range(2):
@@ -237,7 +243,7 @@ def test_two_graphs_and_calls_on_two_streams(dtype):
     for _ in range(5):  # the same bits on every launch
         for i in range(2):
             with torch.cuda.stream(streams[i]):
-                outs[i] = m.mate_attn_decode_shared(case.c, Q, *args, layer=i)
+                outs[i] = together(m)(case.c, Q, *args, layer=i)
     torch.cuda.synchronize()
     for i in range(2):
         assert torch.equal(outs[i][0], want[i][0]) and torch.equal(outs[i][1], want[i][1])
@@ -259,7 +265,7 @@ def test_groups_that_do_not_fit_together(dtype):
                          ((2, 2), -1, [2]), ((2, 0), 16, [0, 1, 2]), ((1, 4), 0, [4]), ((0, 4), big, [4]), ((1, 2), -big, [2])):
         groups = good.copy()
         groups[at] = x
-        O, LSE = m.mate_attn_decode_shared(case.c, Q, *ids, i32(groups))
+        O, LSE = together(m)(case.c, Q, *ids, i32(groups))
         case.check(Q[alone], alone, q_ids[:, alone], O[alone], LSE[alone])
         assert not O.isnan().any()
         if at != (1, 4) and at != (1, 2):          # (one alone is no error)
@@ -269,27 +275,27 @@ def test_groups_that_do_not_fit_together(dtype):
     # more shared tokens than a sequence has, than there are pages for, a sequence that there is not, pages that there are not
     groups = good.copy()
     groups[2, :3] = 9 * 16 + 20
-    O, LSE = m.mate_attn_decode_shared(case.c, Q, *ids, i32(groups))
+    O, LSE = together(m)(case.c, Q, *ids, i32(groups))
     case.check(Q[3:], [3, 4], q_ids[:, 3:], O[3:], LSE[3:])
     with pytest.raises(m.MateError, match="invalid"):
         case.c.status()
     seqs = i32([0, 1, 77, 3, -4])
-    O, LSE = m.mate_attn_decode_shared(case.c, Q, *ids, i32(good), seqs=seqs)
+    O, LSE = together(m)(case.c, Q, *ids, i32(good), seqs=seqs)
     case.check(Q[:2], [0, 1], q_ids[:, :2], O[:2], LSE[:2])
     assert not O[2].any() and not O[4].any() and (LSE[2] == -np.inf).all()
     with pytest.raises(m.MateError, match="invalid"):
         case.c.status()
     before = case.c.table.clone()
     case.c.table[0, 3], case.c.table[3, 1] = 10 ** 6, -1
-    m.mate_attn_decode_shared(case.c, Q, *ids, i32(good))
+    together(m)(case.c, Q, *ids, i32(good))
     with pytest.raises(m.MateError, match="invalid"):
         case.c.status()
     case.c.table.copy_(before)
     case.c.lens[2] = -5
-    O, LSE = m.mate_attn_decode_shared(case.c, Q, *ids, i32(good))
+    O, LSE = together(m)(case.c, Q, *ids, i32(good))
     case.check(Q[3:], [3, 4], q_ids[:, 3:], O[3:], LSE[3:])
     case.c.lens[2] = 10 ** 9
-    m.mate_attn_decode_shared(case.c, Q, *ids, i32(good))
+    together(m)(case.c, Q, *ids, i32(good))
     with pytest.raises(m.MateError, match="invalid"):
         case.c.status()
 
@@ -316,12 +322,12 @@ def test_many_entries(dtype):
     groups = np.stack([first, np.repeat(sizes, sizes), np.repeat([12 if s == 4 else 8 for s in sizes], sizes)])
     q_ids = case.new_ids(seqs)
     Q = torch.randn(len(seqs), 4, 16, device="cuda").to(DT[dtype])
-    O, LSE = m.mate_attn_decode_shared(case.c, Q, i32(q_ids[0]), i32(q_ids[1]), i32(groups), seqs=i32(seqs))
+    O, LSE = together(m)(case.c, Q, i32(q_ids[0]), i32(q_ids[1]), i32(groups), seqs=i32(seqs))
     some = np.random.default_rng(0).permutation(len(seqs))[:300]
     case.check(Q[some.tolist()], [seqs[i] for i in some], q_ids[:, some], O[some.tolist()], LSE[some.tolist()])
     more = i32([0] * (n + 1))
     with pytest.raises(m.MateError, match="unsupported|not available"):
-        m.mate_attn_decode_shared(case.c, Q[:1].expand(n + 1, 4, 16).contiguous(), more, more, torch.zeros(3, n + 1, dtype=torch.int32, device="cuda"), seqs=more)
+        together(m)(case.c, Q[:1].expand(n + 1, 4, 16).contiguous(), more, more, torch.zeros(3, n + 1, dtype=torch.int32, device="cuda"), seqs=more)
 
 
 LAYOUTS = {  # of keys and values in memory that they share with one another, or with what is nobody's: [layers, pages, heads, slots, d]
@@ -369,7 +375,7 @@ def test_the_largest_group(dtype):
     assert (m.mate_cache_groups(case.c, i32(seqs)).cpu().numpy() == groups).all()
     q_ids = case.new_ids(seqs)
     Q = torch.randn(n, 2, 16, device="cuda").to(DT[dtype])
-    O, LSE = m.mate_attn_decode_shared(case.c, Q, i32(q_ids[0]), i32(q_ids[1]), i32(groups), seqs=i32(seqs))
+    O, LSE = together(m)(case.c, Q, i32(q_ids[0]), i32(q_ids[1]), i32(groups), seqs=i32(seqs))
     some = np.random.default_rng(1).permutation(n)[:300]
     case.check(Q[some.tolist()], [seqs[i] for i in some], q_ids[:, some], O[some.tolist()], LSE[some.tolist()])
     case.c.status()
@@ -386,9 +392,65 @@ def test_the_same_bits_from_call_to_call_and_from_cold_memory():
         for i in range(60):
             if i % 3 == 0:
                 junk.fill_(i)
-            o, l = m.mate_attn_decode_shared(case.c, Q, *args)
+            o, l = together(m)(case.c, Q, *args)
             assert torch.equal(o, O) and torch.equal(l, LSE), i
         case.c.status()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("H,Hk,d", [(6, 2, 64), (12, 12, 128)])
+def test_small_batches_are_read_one_by_one(dtype, H, Hk, d):
+    # the results of the call for one sequence after another, to the bit, and status tells what it tells where they are read together
+    import paper_2109_04312_b200 as m
+    case = Shared(m, [(9, [30, 9, 140]), (4, [7, 1]), (0, [300])], H, Hk, d, 16, [h % 3 for h in range(H)], dtype, seed=18)
+    f, B = m.mate_attn_decode_shared, len(case.lens)
+    seqs = [3, 4, 0, 1, 2, 5, 5]
+    groups = m.mate_cache_groups(case.c, i32(seqs))
+    q_ids = case.new_ids(seqs)
+    Q = torch.randn(len(seqs), H, d, device="cuda").to(DT[dtype])
+    a, b = i32(q_ids[0]), i32(q_ids[1])
+    want = m.mate_attn_decode(case.c, Q, a, b, seqs=i32(seqs), max_len=200)
+    got = f(case.c, Q, a, b, groups, seqs=i32(seqs), max_len=200)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    with pytest.raises(m.MateError, match="invalid"):      # (5 and 5 share more tokens than max_len)
+        case.c.status()
+    want, got = m.mate_attn_decode(case.c, Q, a, b, seqs=i32(seqs)), f(case.c, Q, a, b, groups, seqs=i32(seqs))
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    case.c.status()
+    good, big = case.groups.copy(), 2 ** 31 - 1
+    for at, x in (((0, 1), -5), ((0, 1), 2), ((0, 0), 1), ((1, 0), big), ((1, 3), 3), ((2, 1), big), ((2, 2), -1), ((2, 0), 16), ((0, 4), big), ((2, 5), -7)):
+        groups = good.copy()
+        groups[at] = x
+        for always in (False, True):
+            f(case.c, Q[:B], a[:B], b[:B], i32(groups), always=always)
+            with pytest.raises(m.MateError, match="invalid"):
+                case.c.status()
+        f(case.c, Q[:B], a[:B], b[:B], i32(good))
+        case.c.status()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_the_size_from_which_sequences_are_read_together(dtype):
+    # by max_len: what a batch may read; at the limit itself one by one.  (The sums differ in their order, so some bits do.)
+    import paper_2109_04312_b200 as m
+    B, H, d = 32, 8, 128
+    n = (1 << 30 if dtype == "f32" else 1 << 27) // (B * H * d * 2 * (4 if dtype == "f32" else 2))
+    case = Shared(m, [(20, [3] * B)], H, H, d, 16, [0] * H, dtype, seed=19, prefix=300)
+    c = case.c
+    wide = torch.full((B, n // 16 + 2), -1, dtype=torch.int32, device="cuda")
+    wide[:, :c.table.shape[1]] = c.table
+    c = m.Cache(c.k, c.v, c.row_ids, c.col_ids, wide, c.lens, c.prefix, c.refs, case.views)
+    Q = torch.randn(B, H, d, device="cuda").to(DT[dtype])
+    text, g = torch.full((B,), TEXT, dtype=torch.int32, device="cuda"), i32(case.groups)
+    alone, shared = m.mate_attn_decode(c, Q, text, text), together(m)(c, Q, text, text, g)
+    assert not torch.equal(alone[1], shared[1])
+    for max_len, want in ((n, alone), (n + 1, shared), (None, shared)):
+        got = m.mate_attn_decode_shared(c, Q, text, text, g, max_len=max_len)
+        assert torch.equal(got[1], want[1]) or max_len == n and torch.allclose(got[1], want[1], atol=2e-5)
+        assert max_len == n or torch.equal(got[0], want[0])
+        assert torch.equal(got[1], shared[1]) == (max_len != n)
 
 
 @pytest.mark.gpu
@@ -419,7 +481,7 @@ def test_offsets_beyond_32_bits(dtype):
     Q, text = torch.randn(3, 16, d, device="cuda").to(DT[dtype]), i32([TEXT] * 3)
     groups = m.mate_cache_groups(c)
     assert groups.tolist() == [[0] * 3, [3] * 3, [4 * ps] * 3]
-    O, LSE = m.mate_attn_decode_shared(c, Q, text, text, groups)
+    O, LSE = together(m)(c, Q, text, text, groups)
     for i in range(3):
         pg, n = c.table[i, :6].long(), int(c.lens[i])
         k, v = (t[0, pg].transpose(0, 1).reshape(Hk, -1, d)[:, :n].double().cpu().numpy() for t in (c.k, c.v))
@@ -462,7 +524,7 @@ def test_questions_about_one_table(dtype):
         for layer in range(2):
             turned = m.mate_cache_append_axes(c, k, v, f, where, axes, seqs=seqs, counts=granted, row_ids=text[:, None] if layer == 0 else None,
                                               col_ids=text[:, None] if layer == 0 else None, layer=layer, Q=q)
-            outs.append((turned, m.mate_attn_decode_shared(c, turned[:, :, 0], text, text, groups, seqs=seqs, layer=layer)))
+            outs.append((turned, together(m)(c, turned[:, :, 0], text, text, groups, seqs=seqs, layer=layer)))
         where.add_(1)
 
     step()
@@ -512,13 +574,13 @@ def test_the_c_entries_refuse_before_anything_is_launched():
     s, at = struct()
     z = L(0, 64, 64)
 
-    def call(r=None, layer=0, q=at, qs=z, B=1, seqs=at, row=at, col=at, groups=at, scale=1.0, max_len=0, o=at, l=at):
+    def call(r=None, layer=0, q=at, qs=z, B=1, seqs=at, row=at, col=at, groups=at, scale=1.0, max_len=0, flags=0, o=at, l=at):
         p = lambda x: P(x) if x else None  # noqa: E731
         return lib.mate_attn_decode_shared(ctypes.byref(s) if r is None else r, layer, p(q), qs, B, p(seqs), p(row), p(col), p(groups), ctypes.c_float(scale),
-                                           max_len, p(o), p(l), P(at), ctypes.c_size_t(1 << 40), None)
+                                           max_len, flags, p(o), p(l), P(at), ctypes.c_size_t(1 << 40), None)
 
     for kw in (dict(layer=1), dict(layer=-1), dict(q=0), dict(qs=None), dict(B=-1), dict(seqs=0, B=3), dict(row=0), dict(col=0), dict(groups=0), dict(max_len=-1),
-               dict(o=0), dict(l=0), dict(scale=float("nan")), dict(scale=float("inf"))):
+               dict(o=0), dict(l=0), dict(flags=2), dict(flags=1 << 31), dict(scale=float("nan")), dict(scale=float("inf"))):
         assert call(**kw) == -1, kw
     for kw in (dict(q=at + 2), dict(o=at + 8), dict(qs=L(4, 64, 0)), dict(qs=L(64, 4, 0))):
         assert call(**kw) == -3, kw
