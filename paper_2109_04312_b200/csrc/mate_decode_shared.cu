@@ -1,16 +1,34 @@
 // Attention of one new token per sequence where sequences share their first tokens (mate_attn_decode_shared): the shared keys and
 // values of a group are read once for all of its sequences, whose query heads are the rows of one product,
 //     S = Q K^T,  m = max S,  P = exp(S - m),  O = P V / sum P,  LSE = m + ln sum P
-// per kv head over the shared tokens, the same over each sequence's own tokens behind them, and the two put together by their m and
+// per kv head over the shared tokens, the same over the sequences' own tokens behind them, and the two put together by their m and
 // sum P.
 //
-// Work.  An item is a kv head and a tile of rows of a segment -- a group's shared tokens, or the own tokens of one sequence -- and its
-// length in units of kUnit tokens.  Blocks get equal shares of all items' units (found by every block from the lengths, which the host
-// does not know): a long segment is spread over the GPU, short ones are put together.  What a block leaves of an item that is not
-// a row's whole result -- m, sum P and the sum of values, in fp32 -- is joined by a second kernel, in the order of the tokens: the same bits
-// on every launch.
+// Work.  An item is a kv head and a tile of rows (128 with bf16, 64 with fp32) of a segment: a group's shared tokens, with the query heads of all of
+// its sequences, or the own tokens of as many sequences as their heads fill a tile (reading 32 sequences of 4 heads by turns would be 32 tiles
+// of 4 rows; together they are a few tiles of 128 keys, each of which is for the rows of one sequence).  Its length is counted in units of kUnit tokens,
+// and kOver units stand for what an item costs whatever its length (8: 40 us for 64 questions, 102 for 256 sequences; 4: 42, 105; 16: 41, 102, but
+// beams 33 instead of 30).  Blocks, one to an SM, get equal shares of all items' units (found by every block from the lengths, which the host does
+// not know): a long segment is spread over the GPU, short ones are put together.  What a block leaves of an item that is not a row's whole
+// result -- m, sum P and the sum of values, in fp32 -- is joined by a second kernel, in the order of the tokens: the same bits on every
+// launch.
 //
-// Tokens are looked through 128 at a time by their ids; those that no row of the tile attends are left out before anything of them is read.
+// Tokens are looked through 256 at a time by their ids; those that no row of the tile attends are left out before anything of them is read.  Which
+// row attends which of the rest is found once for all rows that go by the same ids (a bit per key), not by every row.
+//
+// Roles of a bf16 block.  Four warps look for keys (Scout) and fill tiles of 128 of them; two copy keys and values (sixteen slots that follow one
+// another by a bulk tensor copy, the rest in 16 bytes a lane) and the queries; two teams of four warps, a thread to a row, take the tiles in turn and make
+// weights of the scores; a warp for each team issues its products.  Tensor memory: O of both teams 2 x 128 columns, S 2 x 128; the weights take
+// the place of the scores, 16 keys as 8 columns of bf16 pairs and 8 of what the rounding left.  (Weights as one bf16 would be off by 2^-9, more than the
+// result's rounding.)  fp32: shared_simt_kernel, 64 rows against 32 keys, no tensor cores.
+//
+// What bounds it.  The chain of a team's tile, 7.2 thousand cycles of which the other team's overlap half: S 0.5, weights 4 (four chunks of 32 keys, one
+// after the other in a warp), P V 1.3, whose weights lie where the next S goes, barriers and the other team's tile 1.4; the products alone would
+// take 1.6 a tile.  64 questions about 8192 tokens, 8 kv heads of 4 x 128: 40 us, of which start 9 (lengths and groups in two rounds of loads, pages, ids, then
+// the first keys), tiles 18, joining and launches the rest.  Tiles of own keys take 5 thousand cycles each: V has to be looked through ahead of weights of 0
+// (0.8), and copies of own runs are short.  Cells (a token attends a few hundred of 4096): looks, 1.1 thousand cycles per 256 tokens.  Measured and
+// left out: chunks of 64 keys (256 sequences 102 -> 109 us), S of one half of a tile while the other's weights are made (106), three tiles of
+// values and one of queries (106), rows brought to L2 ahead of their copies (103), own tokens counted 1.5 times (106).
 #include <cuda_bf16.h>
 
 #include <algorithm>
@@ -1526,10 +1544,10 @@ __global__ void __launch_bounds__(kCheckThreads) check_kernel(const __grid_const
 
 // Up to here a batch is faster read one sequence after another, by all that the host knows: keys and values of all sequences at their longest.
 // bf16, all in one group, 12 heads of 64 or 8 of 4 x 128 elements: 4 sequences of 4096 tokens (51 and 68 MB) 14 and 17 us alone, 21 and 20 shared;
-// 16 of 4096 (203 and 271 MB) 31 and 36, 21 and 21.  (In eight groups of 8 both take as long at 800 MB, and without groups one by one is always
-// the faster way.)  fp32, whose products are not made by the tensor cores: 64 sequences of 4096 tokens, 2 heads of 3 x 48, 203 MB, 44 and 48;
+// 16 of 4096 (203 and 271 MB) 31 and 36, 21 and 21.  (In eight groups of 8 sequences both take as long at 800 MB; without groups, or where cells
+// leave most tokens out, one by one stays the faster way.  None of it is known here.)  fp32, whose products are not made by the tensor cores: 64 sequences of 4096 tokens, 2 heads of 3 x 48, 203 MB, 44 and 48;
 // of 16384, 807 MB, 136 and 106; 8 heads of 4 x 128, 541 MB 85 and 101, 2.2 GB 292 and 268.
-double alone_bytes(const mate_cache_t *c) { return c->dtype == MATE_F32 ? 1024.0 * (1 << 20) : 128.0 * (1 << 20); }
+double alone_bytes(const mate_cache_t *c) { return c->dtype == MATE_F32 ? 1024.0 * (1 << 20) : 192.0 * (1 << 20); }
 
 int rows_of_tile(const mate_cache_t *c) { return c->dtype == MATE_F32 ? kSimtRows : kTcRows; }
 int pack_of(const mate_cache_t *c) { return std::max(1, rows_of_tile(c) / (c->heads / c->kv_heads)); }

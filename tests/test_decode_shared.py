@@ -436,7 +436,7 @@ def test_the_size_from_which_sequences_are_read_together(dtype):
     # by max_len: what a batch may read; at the limit itself one by one.  (The sums differ in their order, so some bits do.)
     import paper_2109_04312_b200 as m
     B, H, d = 32, 8, 128
-    n = (1 << 30 if dtype == "f32" else 1 << 27) // (B * H * d * 2 * (4 if dtype == "f32" else 2))
+    n = (1 << 30 if dtype == "f32" else 192 << 20) // (B * H * d * 2 * (4 if dtype == "f32" else 2))
     case = Shared(m, [(20, [3] * B)], H, H, d, 16, [0] * H, dtype, seed=19, prefix=300)
     c = case.c
     wide = torch.full((B, n // 16 + 2), -1, dtype=torch.int32, device="cuda")
