@@ -24,11 +24,12 @@
 //
 // What bounds it.  The chain of a team's tile, 7.2 thousand cycles of which the other team's overlap half: S 0.5, weights 4 (four chunks of 32 keys, one
 // after the other in a warp), P V 1.3, whose weights lie where the next S goes, barriers and the other team's tile 1.4; the products alone would
-// take 1.6 a tile.  64 questions about 8192 tokens, 8 kv heads of 4 x 128: 40 us, of which start 9 (lengths and groups in two rounds of loads, pages, ids, then
+// take 1.6 a tile.  64 questions about 8192 tokens, 8 kv heads of 4 x 128: 38 us, of which start 9 (lengths and groups in two rounds of loads, pages, ids, then
 // the first keys), tiles 18, joining and launches the rest.  Tiles of own keys take 5 thousand cycles each: V has to be looked through ahead of weights of 0
 // (0.8), and copies of own runs are short.  Cells (a token attends a few hundred of 4096): looks, 1.1 thousand cycles per 256 tokens.  Measured and
 // left out: chunks of 64 keys (256 sequences 102 -> 109 us), S of one half of a tile while the other's weights are made (106), three tiles of
-// values and one of queries (106), rows brought to L2 ahead of their copies (103), own tokens counted 1.5 times (106).
+// values and one of queries (106), rows brought to L2 ahead of their copies (103); with 64 elements a third place for scores, so that S does not wait for
+// P V (beams 29 -> 30).
 #include <cuda_bf16.h>
 
 #include <algorithm>
@@ -603,6 +604,8 @@ struct SimtSmem {
 
 __device__ __forceinline__ void load16(const float *from, float *to) { *reinterpret_cast<float4 *>(to) = *reinterpret_cast<const float4 *>(from); }
 
+// fp32: eight warps with eight rows each, two rows and four keys of a lane in S, eight rows and DP / 32 columns in P V; scores by shared memory.  Bound
+// by its reads of shared memory beside the products: 64 sequences that share 4096 tokens, 8 kv heads of 4 x 128, 268 us, 16 TFLOP/s.
 template <int DP>
 __global__ void __launch_bounds__(kSimtThreads, 2) shared_simt_kernel(const __grid_constant__ SharedParams p) {
     extern __shared__ __align__(16) char smem_raw[];
@@ -1443,7 +1446,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
 // ---- the results of a row put together
 
 // A block has kJoinRows rows of a kv head; a lane has a row and four columns, a warp 16 columns and every `splits`-th of the results.  Who has
-// them is found once for the block.
+// them is found once for the block.  Latency: the kernel in front leaves no registers, so its blocks come to the SMs when those end, then a
+// row's place, its parts, their sum: 5 us with the launch.  (A block to a row: 64 questions 54 us in all instead of 50.)
 constexpr int kJoinRows = 8;
 struct Results {
     const float *value;     // of the row's first column

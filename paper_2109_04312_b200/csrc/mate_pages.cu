@@ -450,7 +450,8 @@ __device__ __forceinline__ int full_pages(const CacheArgs &c, const int32_t *seq
     return *s < 0 ? 0 : clip_len(c.lens[*s], c.width * c.page_size, bad) / c.page_size;
 }
 // Leading full pages that every entry has in common with the one before it.  A block each, kRun pairs of a thread under way: latency,
-// as long as a row fits one round of them (2048 pages).
+// as long as a row fits one round of them (2048 pages): with groups_kernel 3.7 us for 64 entries of 512 pages, 4.2 of 2048, 7.5 of 8192.  (Both in one
+// cluster of eight blocks: 5.3, 10.5, 30.)
 constexpr int kCommonThreads = 128, kRun = 16;
 __global__ void __launch_bounds__(kCommonThreads) common_kernel(const __grid_constant__ CacheArgs c, const int32_t *seqs, int32_t *common) {
     __shared__ int s_first;

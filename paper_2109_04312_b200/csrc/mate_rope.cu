@@ -47,7 +47,9 @@ struct RopeParams {
     CacheArgs cache;
     const int32_t *seqs, *counts, *row_ids, *col_ids;
 };
-// Positions of several axes, of which every pair goes by one.  (Parameters of their own: those of one axis are copied with every launch.)
+// Positions of several axes, of which every pair goes by one: a thread takes its token's up to four positions and picks a pair's by two bits, 4 x
+// 2048 tokens, 12 and 12 heads of 64 11.0 us (one axis 10.0), 32768 tokens, 32 and 8 heads of 128 backward 107 (106).  (Parameters of their own:
+// those of one axis are copied with every launch.)
 constexpr int kMaxAxes = 4, kMaxPairs = 512;
 struct AxesParams : RopeParams {
     static constexpr bool kAxes = true;
