@@ -84,6 +84,33 @@ __device__ __forceinline__ int seq_of(const int32_t *seqs, int i, int n_seqs) {
     const int s = seqs ? seqs[i] : i;
     return in_range(s, n_seqs) ? s : -1;
 }
+
+// An entry of a batch and its group (of mate_attn_decode_shared).
+struct GroupOf {
+    int s;  // its sequence; -1: none
+    int len, prefix;
+    int first, count, shared;  // count 0: it is in none
+    bool bad;
+};
+// What does not fit together on the device leaves an entry without a group: the rows of one group are the same in all of its entries.  (Two
+// rounds of loads, the second one's indexes brought into range instead of looked at first.)
+__device__ __forceinline__ GroupOf group_of(const CacheArgs &c, const int32_t *seqs, const int32_t *groups, int B, int b, int max_len) {
+    GroupOf e = {};
+    const int s = seqs ? seqs[b] : b, first = groups[b], count = groups[B + b], shared = groups[2 * B + b];
+    const int at = s < 0 ? 0 : s < c.seqs ? s : c.seqs - 1, f = first < 0 ? 0 : first < b ? first : b;
+    const int len = c.lens[at], prefix = c.prefix[at], first_of = groups[f], count_of = groups[B + f], shared_of = groups[2 * B + f];
+    e.s = s == at ? s : -1, e.first = first, e.prefix = prefix < 0 ? 0 : prefix;
+    if (s != at || shared < 0) e.bad = true;
+    if (s == at) e.len = clip_len(len, max_len, &e.bad);
+    if (shared > 0 && count > 1) {
+        if (first == f && count <= B - first && b - first < count && shared <= max_len && first_of == first && count_of == count && shared_of == shared)
+            e.count = count, e.shared = shared;
+        else
+            e.bad = true;
+    }
+    if (e.count > 0 && e.len < shared) e.bad = true;
+    return e;
+}
 #endif
 
 }  // namespace mate

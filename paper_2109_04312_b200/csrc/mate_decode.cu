@@ -68,11 +68,14 @@ struct DecodeParams {
     unsigned page_mul, page_shift;  // x / page_size = (umulhi(x, page_mul) + x) >> page_shift for x < 2^31
     Joint *joints;         // [B][items]; null: a block per item
     float *partial;        // [grid][2][rows of a block][d + 2]
+    unsigned check_from;             // blocks from this one on look at the groups that the batch was given with
+    const int32_t *groups;
     uint32_t views[kMaxHeads / 16];  // two bits a head
 };
 __device__ __forceinline__ int page_index(const DecodeParams &p, int token) {
     return (int)((__umulhi((unsigned)token, p.page_mul) + (unsigned)token) >> p.page_shift);
 }
+__device__ __noinline__ bool is_misfit(const DecodeParams &p, int b) { return b < p.B && group_of(p.cache, p.seqs, p.groups, p.B, b, p.max_len).bad; }
 __device__ __forceinline__ int view_at(const DecodeParams &p, int h) { return p.views[h >> 4] >> 2 * (h & 15) & 3; }
 
 // ---- types
@@ -150,7 +153,7 @@ struct Start {
     int entry;
 };
 // All threads call it: the entry that the block's first unit belongs to.
-__device__ Start find_start(const DecodeParams &p, int items) {
+__device__ Start find_start(const DecodeParams &p, unsigned grid, int items) {
     __shared__ unsigned s_sum[kWarps];
     __shared__ Start s_start;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -173,7 +176,7 @@ __device__ Start find_start(const DecodeParams &p, int items) {
         if (w < warp) before += s_sum[w];
         total += s_sum[w];
     }
-    const unsigned blocks = min(total, gridDim.x), at = share(total, blocks, min(blockIdx.x, blocks - 1));
+    const unsigned blocks = min(total, grid), at = share(total, blocks, min(blockIdx.x, blocks - 1));
     if (at >= before && at < before + own) {
         int b = b0;
         for (; b < b1 - 1; ++b) {
@@ -742,7 +745,7 @@ template <typename T, int DP, int NB, int W>
 constexpr int kExtra = sizeof(T) == 4 ? 4 * Shape<T, DP, NB>::kRows * (DP + W * Shape<T, DP, NB>::kKeys) : 0;
 
 // W = kManyWarps: every block takes an item
-template <typename T, int DP, int NB, int W>
+template <typename T, int DP, int NB, int W, bool kGroups>
 __global__ void __launch_bounds__(32 * W, W == kWarps ? Shape<T, DP, NB>::kBlocksPerSm : 1) decode_kernel(const __grid_constant__ DecodeParams p) {
     using S = Shape<T, DP, NB>;
     extern __shared__ char smem_raw[];
@@ -754,6 +757,13 @@ __global__ void __launch_bounds__(32 * W, W == kWarps ? Shape<T, DP, NB>::kBlock
     __shared__ int s_out_at[W];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, items = p.kv_heads * p.blocks_of_group;
     const int max_rows = min(S::kRows, p.group);
+    if constexpr (kGroups) {  // (each sequence is read by itself, whatever they say)
+        if (blockIdx.x >= p.check_from) {
+            ptx::wait_prior_grid();
+            if (is_misfit(p, (int)(blockIdx.x - p.check_from) * 32 * W + tid)) atomicOr(p.cache.status, kCacheBad);
+            return;
+        }
+    }
     float *own = reinterpret_cast<float *>(smem + W * kRing * kStage);
     if (p.d < DP)  // columns that no copy writes
         for (int i = tid; i < W * kRing * kStage / 16; i += 32 * W) reinterpret_cast<uint4 *>(smem)[i] = make_uint4(0, 0, 0, 0);
@@ -764,7 +774,7 @@ __global__ void __launch_bounds__(32 * W, W == kWarps ? Shape<T, DP, NB>::kBlock
     Walk walk;
     Start start = {};
     if (W == kWarps && p.joints) {
-        start = find_start(p, items);
+        start = find_start(p, kGroups ? p.check_from : gridDim.x, items);
         if (blockIdx.x >= start.blocks) return;
         const unsigned at = share(start.total, start.blocks, blockIdx.x);
         walk.left = (int)(share(start.total, start.blocks, blockIdx.x + 1) - at);
@@ -863,6 +873,15 @@ __global__ void __launch_bounds__(32 * W, W == kWarps ? Shape<T, DP, NB>::kBlock
     if (load.bad) atomicOr(p.cache.status, kCacheBad);
 }
 
+// The groups of an fp32 batch.  (Looked at beside the kernel in front, which has waited for whoever wrote them before it let this one start; what is
+// launched next counts on both.)
+__global__ void __launch_bounds__(kThreads) check_kernel(const __grid_constant__ DecodeParams p) {
+    ptx::launch_dependents();
+    const bool bad = is_misfit(p, blockIdx.x * kThreads + threadIdx.x);
+    ptx::wait_prior_grid();
+    if (bad) atomicOr(p.cache.status, kCacheBad);
+}
+
 // Joins the partial results of an item that fell to several blocks of the kernel before.  grid: (item, row of its block of the group)
 template <typename T, int kN>
 __global__ void __launch_bounds__(kN) join_kernel(const __grid_constant__ DecodeParams p, int block_rows) {
@@ -948,16 +967,28 @@ int shares(const mate_cache_t *c, int B, int max_len) {
     return units <= (kOver + (items < kMany ? kWhole : kWholeOfMany)) * items ? 0 : (int)(units < most ? units : most);
 }
 
-template <typename T, int DP, int NB, int W>
-int launch_warps(const DecodeParams &p, unsigned grid, int device, cudaStream_t st) {
+template <typename T, int DP, int NB, int W, bool kGroups>
+int launch_kernel(const DecodeParams &p, unsigned grid, int device, cudaStream_t st) {
     static SmemAttrOnce attr;
     constexpr int kSmem = kAlign + W * kRing * kStage + kExtra<T, DP, NB, W>;
-    const int rc = attr.ensure((const void *)decode_kernel<T, DP, NB, W>, kSmem, device);
+    const int rc = attr.ensure((const void *)decode_kernel<T, DP, NB, W, kGroups>, kSmem, device);
     if (rc != MATE_OK) return rc;
-    return launch_after(decode_kernel<T, DP, NB, W>, dim3(grid), 32 * W, kSmem, st, p) == cudaSuccess ? MATE_OK : MATE_ERR_CUDA;
+    return launch_after(decode_kernel<T, DP, NB, W, kGroups>, dim3(grid), 32 * W, kSmem, st, p) == cudaSuccess ? MATE_OK : MATE_ERR_CUDA;
+}
+// Groups are looked at by blocks of their own, behind the others (bf16; a kernel of its own for that takes a microsecond longer), or by check_kernel (fp32,
+// where the lines cost a call of 10 us 6 %).
+template <typename T, int DP, int NB, int W>
+int launch_warps(DecodeParams &p, unsigned grid, int device, cudaStream_t st) {
+    if constexpr (sizeof(T) == 2) {
+        if (p.groups) {
+            p.check_from = grid;
+            return launch_kernel<T, DP, NB, W, true>(p, grid + (unsigned)(p.B + 32 * W - 1) / (32 * W), device, st);
+        }
+    }
+    return launch_kernel<T, DP, NB, W, false>(p, grid, device, st);
 }
 template <typename T, int DP, int NB>
-int launch(const DecodeParams &p, int blocks, int device, cudaStream_t st) {
+int launch(DecodeParams &p, int blocks, int device, cudaStream_t st) {
     constexpr int kRows = Shape<T, DP, NB>::kRows;
     const int rows = kRows < p.group ? kRows : p.group, items = p.kv_heads * p.blocks_of_group;
     const int64_t all = (int64_t)p.B * items;
@@ -985,12 +1016,10 @@ size_t decode_workspace(const mate_cache_t *c, int B) {
     return blocks ? sizeof(Joint) * B * c->kv_heads * blocks_of_group(c) + sizeof(float) * 2 * rows * (c->d + 2) * (size_t)blocks : 0;
 }
 
-}  // namespace mate
-
-extern "C" int mate_attn_decode(const mate_cache_t *cache, int layer, const void *Q, const int64_t *q_stride, int B, const int32_t *seqs,
-                                const int32_t *row_ids, const int32_t *col_ids, float scale, int max_len, void *O, float *LSE,
-                                void *workspace, size_t workspace_bytes, void *stream) {
-    using namespace mate;
+// groups: null, or those of mate_attn_decode_shared, which are looked at only
+int decode(const mate_cache_t *cache, int layer, const void *Q, const int64_t *q_stride, int B, const int32_t *seqs, const int32_t *row_ids,
+           const int32_t *col_ids, const int32_t *groups, float scale, int max_len, void *O, float *LSE, void *workspace, size_t workspace_bytes,
+           void *stream) {
     int rc = check_cache(cache);
     if (rc != MATE_OK) return rc;
     if (layer < 0 || layer >= cache->layers || B < 0 || max_len < 0 || (!seqs && B > cache->seqs)) return MATE_ERR_INVALID_ARG;
@@ -1013,7 +1042,7 @@ extern "C" int mate_attn_decode(const mate_cache_t *cache, int layer, const void
     p.B = B, p.heads = cache->heads, p.kv_heads = cache->kv_heads, p.group = cache->heads / cache->kv_heads;
     p.blocks_of_group = blocks_of_group(cache), p.d = cache->d;
     p.max_len = max_len;
-    p.seqs = seqs, p.row_ids = row_ids, p.col_ids = col_ids;
+    p.seqs = seqs, p.row_ids = row_ids, p.col_ids = col_ids, p.groups = groups;
     p.scale_log2 = scale * kLog2e, p.O = O, p.LSE = LSE;
     for (int h = 0; h < cache->heads; ++h) p.views[h >> 4] |= (uint32_t)cache->head_view[h] << 2 * (h & 15);
     for (p.page_shift = 0; 1u << p.page_shift < (unsigned)cache->page_size;) ++p.page_shift;
@@ -1038,5 +1067,17 @@ extern "C" int mate_attn_decode(const mate_cache_t *cache, int layer, const void
                                                 : launch<__nv_bfloat16, DP, 1>(p, blocks, cache->device, st);
         }
     };
-    return cache->d <= 64 ? run(std::false_type()) : run(std::true_type());
+    rc = cache->d <= 64 ? run(std::false_type()) : run(std::true_type());
+    if (rc == MATE_OK && groups && cache->dtype == MATE_F32 &&
+        launch_after(check_kernel, dim3((unsigned)(B + kThreads - 1) / kThreads), kThreads, 0, st, p) != cudaSuccess)
+        rc = MATE_ERR_CUDA;
+    return rc;
+}
+
+}  // namespace mate
+
+extern "C" int mate_attn_decode(const mate_cache_t *cache, int layer, const void *Q, const int64_t *q_stride, int B, const int32_t *seqs,
+                                const int32_t *row_ids, const int32_t *col_ids, float scale, int max_len, void *O, float *LSE,
+                                void *workspace, size_t workspace_bytes, void *stream) {
+    return mate::decode(cache, layer, Q, q_stride, B, seqs, row_ids, col_ids, nullptr, scale, max_len, O, LSE, workspace, workspace_bytes, stream);
 }

@@ -41,7 +41,11 @@
 #include "tc_tiles.cuh"
 
 namespace mate {
-size_t decode_workspace(const mate_cache_t *cache, int B);  // mate_decode.cu
+// mate_decode.cu
+size_t decode_workspace(const mate_cache_t *cache, int B);
+int decode(const mate_cache_t *cache, int layer, const void *Q, const int64_t *q_stride, int B, const int32_t *seqs, const int32_t *row_ids,
+           const int32_t *col_ids, const int32_t *groups, float scale, int max_len, void *O, float *LSE, void *workspace, size_t workspace_bytes,
+           void *stream);
 namespace {
 
 constexpr int kUnit = 32;     // tokens of a unit of work: what a warp looks through in one go
@@ -104,31 +108,15 @@ struct Entry {
     int bad;
 };
 // (called, not put in line: what a block runs through once misses the instruction cache, which holds 32 KB for all of its roles)
-// What does not fit together on the device leaves an entry without a group: the rows of one group are the same in all of its entries.  (Two
-// rounds of loads, the second one's indexes brought into range instead of looked at first.)
 __device__ __noinline__ void entry_of(const SharedParams &p, int b, Entry *to) {
-    bool is_bad = false, *bad = &is_bad;
-    const int s = p.seqs ? p.seqs[b] : b, q_row = p.row_ids[b], q_col = p.col_ids[b];
-    const int first = p.groups[b], count = p.groups[p.B + b], shared = p.groups[2 * p.B + b];
-    const int at = min(max(s, 0), p.cache.seqs - 1), f = min(max(first, 0), b);
-    int len = p.cache.lens[at];
-    const int prefix = p.cache.prefix[at], first_of = p.groups[f], count_of = p.groups[p.B + f], shared_of = p.groups[2 * p.B + f];
-    Entry e = {s == at ? s : -1, 0, 0, 0, 0, first, 0, 0, q_row, q_col, max(0, prefix)};
-    if (s != at || shared < 0) *bad = true;
-    if (s == at) e.len = clip_len(len, p.max_len, bad);
-    if (shared > 0 && count > 1) {
-        if (first == f && count <= p.B - first && b - first < count && shared <= p.max_len && first_of == first && count_of == count &&
-            shared_of == shared)
-            e.count = count, e.shared = shared;
-        else
-            *bad = true;
-    }
-    const bool has = e.count > 0 && e.len >= shared, padding = q_row < 0 || q_col < 0 || e.s < 0;
-    if (e.count > 0 && !has) *bad = true;
+    const int q_row = p.row_ids[b], q_col = p.col_ids[b];
+    const GroupOf g = group_of(p.cache, p.seqs, p.groups, p.B, b, p.max_len);
+    Entry e = {g.s, g.len, 0, 0, g.count, g.first, g.shared, 0, q_row, q_col, g.prefix};
+    const bool has = g.count > 0 && g.len >= g.shared, padding = q_row < 0 || q_col < 0 || g.s < 0;
     e.counts = has && !padding;
-    e.own0 = has ? shared : 0;
+    e.own0 = has ? g.shared : 0;
     e.own1 = padding ? e.own0 : e.len;
-    e.bad = is_bad;
+    e.bad = g.bad;
     *to = e;
 }
 // Units of tokens.  The first kOver units of an item stand for what it costs whatever its length: none of its tokens belong to them.
@@ -1535,20 +1523,6 @@ __global__ void __launch_bounds__(1024) shared_join_kernel(const __grid_constant
     if (c4 == 0) p.LSE[out] = natural(m, l);
 }
 
-// ---- groups that nobody goes by
-
-// Whether they fit together, where each sequence is read by itself.  (Looked at beside the kernel in front, which has waited for whoever wrote them
-// before it let this one start; what is launched next counts on both.)
-constexpr int kCheckThreads = 128;
-__global__ void __launch_bounds__(kCheckThreads) check_kernel(const __grid_constant__ SharedParams p) {
-    ptx::launch_dependents();
-    const int b = blockIdx.x * kCheckThreads + threadIdx.x;
-    Entry e = {};
-    if (b < p.B) entry_of(p, b, &e);
-    ptx::wait_prior_grid();
-    if (e.bad) atomicOr(p.cache.status, kCacheBad);
-}
-
 // ---- host
 
 // Up to here a batch is faster read one sequence after another, by all that the host knows: keys and values of all sequences at their longest.
@@ -1656,6 +1630,9 @@ int mate_attn_decode_shared(const mate_cache_t *cache, int layer, const void *Q,
     const Workspace w = workspace_of(cache, B);
     if (!workspace || workspace_bytes < std::max(w.bytes, decode_workspace(cache, B))) return MATE_ERR_WORKSPACE;
     if (!is_aligned(workspace, 256)) return MATE_ERR_ALIGNMENT;
+    if (!(flags & MATE_SHARED_ALWAYS) && 2.0 * elem_size(cache->dtype) * B * max_len * cache->kv_heads * cache->d <= alone_bytes(cache)) {
+        return decode(cache, layer, Q, q_stride, B, seqs, row_ids, col_ids, groups, scale, max_len, O, LSE, workspace, workspace_bytes, stream);
+    }
     SharedParams p = {};
     p.cache = cache_args(cache, layer);
     p.Q = Q, p.q_batch = q_stride[0], p.q_head = q_stride[1];
@@ -1686,11 +1663,6 @@ int mate_attn_decode_shared(const mate_cache_t *cache, int layer, const void *Q,
         p.scale_log2 = std::fmax(std::fabs(p.scale_log2), 0x1p-126f);
     }
     cudaStream_t st = (cudaStream_t)stream;
-    if (!(flags & MATE_SHARED_ALWAYS) && 2.0 * elem_size(cache->dtype) * B * max_len * cache->kv_heads * cache->d <= alone_bytes(cache)) {
-        rc = mate_attn_decode(cache, layer, Q, q_stride, B, seqs, row_ids, col_ids, scale, max_len, O, LSE, workspace, workspace_bytes, stream);
-        if (rc != MATE_OK) return rc;
-        return launch_after(check_kernel, dim3((unsigned)(B + kCheckThreads - 1) / kCheckThreads), kCheckThreads, 0, st, p) == cudaSuccess ? MATE_OK : MATE_ERR_CUDA;
-    }
     p.blocks = n_blocks(cache);
     if (cache->dtype == MATE_F32) return cache->d <= 64 ? launch<float, 64>(p, cache, st) : launch<float, 128>(p, cache, st);
     return cache->d <= 64 ? launch<__nv_bfloat16, 64>(p, cache, st) : launch<__nv_bfloat16, 128>(p, cache, st);
