@@ -443,7 +443,8 @@ int mate_attn_decode(const mate_cache_t *cache, int layer, const void *Q, const 
  *              the others' must be the same there; each entry has a prefix and ids of its own
  *   workspace  device, 256-byte aligned, mate_cache_shared_workspace_bytes; contents undefined afterwards; calls that overlap need one each
  * Groups that do not fit together, or of more tokens than a sequence (or max_len) has, are left out: their entries are taken
- * alone, or attend their own tokens only, and status says so.  B is at most 4096.
+ * alone, or attend their own tokens only, and status says so.  So is a group among whose entries another one begins: an entry is in one
+ * group at most.  B is at most 4096.
  *   flags      0: where the batch may read no more than 192 MB (bf16) or 1 GB (fp32) one sequence after another -- B max_len kv_heads
  *              keys and values --, that is the faster way, and taken: the results are mate_attn_decode's; MATE_SHARED_ALWAYS: the shared
  *              tokens are read once all the same

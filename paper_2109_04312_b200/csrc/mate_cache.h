@@ -78,6 +78,37 @@ __host__ __device__ inline int owner_of(const N *off, int n, int r) {
     return lo;
 }
 
+// What an entry of a batch says of its group (of mate_attn_decode_shared): the first entry of it, how many it has, and the tokens that they share.
+struct Claim {
+    int first, count, shared;
+};
+__host__ __device__ inline Claim claim_of(const int32_t *groups, int B, int b) { return {groups[b], groups[B + b], groups[2 * B + b]}; }
+// Whether it says that it is in one, and whether that is in range.
+__host__ __device__ inline bool claims(const Claim &c) { return c.shared > 0 && c.count > 1; }
+__host__ __device__ inline bool fits(const Claim &c, int b, int B, int max_len) {
+    return claims(c) && c.first >= 0 && c.first <= b && c.count <= B - c.first && b - c.first < c.count && c.shared <= max_len;
+}
+__host__ __device__ inline bool begins_group(const Claim &c, int b, int B, int max_len) { return c.first == b && fits(c, b, B, max_len); }
+// Whether a group begins among the entries behind the first one of `count`, by a bit for each entry that begins one.  Where none does in any group, no
+// two have an entry in common (of two that have, the one that begins later begins inside the other), and all of them together have B entries at most:
+// that is what makes their rows, and the places of their results, their own.
+__host__ __device__ inline bool begins_inside(const uint32_t *begins, int first, int count) {
+    const int from = first + 1, to = first + count;  // to > from
+    for (int w = from >> 5; w <= (to - 1) >> 5; ++w) {
+        uint32_t those = begins[w];
+        if (w == from >> 5) those &= ~0u << (from & 31);
+        if (w == (to - 1) >> 5) those &= ~0u >> (31 - ((to - 1) & 31));
+        if (those) return true;
+    }
+    return false;
+}
+// Whether an entry is in the group that it claims: the group's first entry says the same, and no other group begins inside it.
+__host__ __device__ inline bool is_member(const Claim &c, int b, const Claim &of_first, const uint32_t *begins, int B, int max_len) {
+    return fits(c, b, B, max_len) && of_first.first == c.first && of_first.count == c.count && of_first.shared == c.shared &&
+           !(begins && begins_inside(begins, c.first, c.count));
+}
+__host__ __device__ inline bool bit_of(const uint32_t *bits, int b) { return bits[b >> 5] >> (b & 31) & 1; }
+
 #ifdef __CUDACC__
 // Sequence of entry i of a list (null: i itself), -1 where there is none.
 __device__ __forceinline__ int seq_of(const int32_t *seqs, int i, int n_seqs) {
@@ -92,24 +123,36 @@ struct GroupOf {
     int first, count, shared;  // count 0: it is in none
     bool bad;
 };
-// What does not fit together on the device leaves an entry without a group: the rows of one group are the same in all of its entries.  (Two
-// rounds of loads, the second one's indexes brought into range instead of looked at first.)
-__device__ __forceinline__ GroupOf group_of(const CacheArgs &c, const int32_t *seqs, const int32_t *groups, int B, int b, int max_len) {
+// What does not fit together on the device leaves an entry without a group: the rows of one group are the same in all of its entries.  none: another
+// group is known to begin inside the entry's, which is not looked for here.  (Two rounds of loads, the second one's indexes brought into range
+// instead of looked at first.)
+__device__ __forceinline__ GroupOf group_of(const CacheArgs &c, const int32_t *seqs, const int32_t *groups, bool none, int B, int b, int max_len) {
     GroupOf e = {};
-    const int s = seqs ? seqs[b] : b, first = groups[b], count = groups[B + b], shared = groups[2 * B + b];
-    const int at = s < 0 ? 0 : s < c.seqs ? s : c.seqs - 1, f = first < 0 ? 0 : first < b ? first : b;
-    const int len = c.lens[at], prefix = c.prefix[at], first_of = groups[f], count_of = groups[B + f], shared_of = groups[2 * B + f];
-    e.s = s == at ? s : -1, e.first = first, e.prefix = prefix < 0 ? 0 : prefix;
-    if (s != at || shared < 0) e.bad = true;
+    const Claim mine = claim_of(groups, B, b);
+    const int s = seqs ? seqs[b] : b, at = s < 0 ? 0 : s < c.seqs ? s : c.seqs - 1;
+    const int len = c.lens[at], prefix = c.prefix[at];
+    const Claim of_first = claim_of(groups, B, mine.first < 0 ? 0 : mine.first < b ? mine.first : b);
+    e.s = s == at ? s : -1, e.first = mine.first, e.prefix = prefix < 0 ? 0 : prefix;
+    if (s != at || mine.shared < 0) e.bad = true;
     if (s == at) e.len = clip_len(len, max_len, &e.bad);
-    if (shared > 0 && count > 1) {
-        if (first == f && count <= B - first && b - first < count && shared <= max_len && first_of == first && count_of == count && shared_of == shared)
-            e.count = count, e.shared = shared;
+    if (claims(mine)) {
+        if (!none && is_member(mine, b, of_first, nullptr, B, max_len))
+            e.count = mine.count, e.shared = mine.shared;
         else
             e.bad = true;
     }
-    if (e.count > 0 && e.len < shared) e.bad = true;
+    if (e.count > 0 && e.len < mine.shared) e.bad = true;
     return e;
+}
+// A bit for each entry that begins a group.  All of a block's NT threads call it, with a barrier behind it.
+template <int NT>
+__device__ __forceinline__ void find_begins(const int32_t *groups, int B, int max_len, uint32_t *begins) {
+#pragma unroll 4
+    for (int b0 = threadIdx.x & ~31; b0 < B; b0 += NT) {
+        const int b = b0 + (int)(threadIdx.x & 31);
+        const unsigned those = __ballot_sync(~0u, b < B && begins_group(claim_of(groups, B, b), b, B, max_len));
+        if ((threadIdx.x & 31) == 0) begins[b0 >> 5] = those;
+    }
 }
 #endif
 

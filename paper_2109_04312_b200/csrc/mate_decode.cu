@@ -75,7 +75,19 @@ struct DecodeParams {
 __device__ __forceinline__ int page_index(const DecodeParams &p, int token) {
     return (int)((__umulhi((unsigned)token, p.page_mul) + (unsigned)token) >> p.page_shift);
 }
-__device__ __noinline__ bool is_misfit(const DecodeParams &p, int b) { return b < p.B && group_of(p.cache, p.seqs, p.groups, p.B, b, p.max_len).bad; }
+// Whether the groups that the batch was given with do not fit together, by the thread's entry of block number `block` of those that look.  begins:
+// kBeginWords words of shared memory.
+constexpr int kMaxEntries = 4096, kBeginWords = kMaxEntries / 32;
+template <int NT>
+__device__ __noinline__ bool is_misfit(const DecodeParams &p, int block, uint32_t *begins) {
+    find_begins<NT>(p.groups, p.B, p.max_len, begins);
+    __syncthreads();
+    const int b = block * NT + (int)threadIdx.x;
+    if (b >= p.B) return false;
+    const Claim c = claim_of(p.groups, p.B, b);
+    const bool none = fits(c, b, p.B, p.max_len) && begins_inside(begins, c.first, c.count);
+    return group_of(p.cache, p.seqs, p.groups, none, p.B, b, p.max_len).bad;
+}
 __device__ __forceinline__ int view_at(const DecodeParams &p, int h) { return p.views[h >> 4] >> 2 * (h & 15) & 3; }
 
 // ---- types
@@ -760,7 +772,8 @@ __global__ void __launch_bounds__(32 * W, W == kWarps ? Shape<T, DP, NB>::kBlock
     if constexpr (kGroups) {  // (each sequence is read by itself, whatever they say)
         if (blockIdx.x >= p.check_from) {
             ptx::wait_prior_grid();
-            if (is_misfit(p, (int)(blockIdx.x - p.check_from) * 32 * W + tid)) atomicOr(p.cache.status, kCacheBad);
+            static_assert(W * kRing * kStage >= 4 * kBeginWords, "room for a bit for each entry");
+            if (is_misfit<32 * W>(p, (int)(blockIdx.x - p.check_from), reinterpret_cast<uint32_t *>(smem_raw))) atomicOr(p.cache.status, kCacheBad);
             return;
         }
     }
@@ -876,8 +889,9 @@ __global__ void __launch_bounds__(32 * W, W == kWarps ? Shape<T, DP, NB>::kBlock
 // The groups of an fp32 batch.  (Looked at beside the kernel in front, which has waited for whoever wrote them before it let this one start; what is
 // launched next counts on both.)
 __global__ void __launch_bounds__(kThreads) check_kernel(const __grid_constant__ DecodeParams p) {
+    __shared__ uint32_t s_begins[kBeginWords];
     ptx::launch_dependents();
-    const bool bad = is_misfit(p, blockIdx.x * kThreads + threadIdx.x);
+    const bool bad = is_misfit<kThreads>(p, blockIdx.x, s_begins);
     ptx::wait_prior_grid();
     if (bad) atomicOr(p.cache.status, kCacheBad);
 }

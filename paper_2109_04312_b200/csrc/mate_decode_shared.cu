@@ -82,6 +82,7 @@ struct SharedParams {
     Joint *joints;                    // [2][kv_heads][B own_tiles]: shared tokens, by the first entry of the tile's group, and own ones
     float2 *whole_stats;              // [2][B heads]  m and sum P of rows whose item one block has done
     float *whole;                     // [2][B heads][d]
+    uint8_t *grouped;                 // [B] whether an entry is in a group, for the kernel that joins
     float *parts;                     // [blocks][2]: values in groups of four by row, then the rows' m and sum P
     int blocks;                       // of the grid
     uint32_t views[kMaxHeads / 16];   // two bits a head
@@ -107,10 +108,11 @@ struct Entry {
     int q_row, q_col, prefix;
     int bad;
 };
+// none: as find_start makes it, or null: whether groups have entries in common is not looked at.
 // (called, not put in line: what a block runs through once misses the instruction cache, which holds 32 KB for all of its roles)
-__device__ __noinline__ void entry_of(const SharedParams &p, int b, Entry *to) {
+__device__ __noinline__ void entry_of(const SharedParams &p, int b, const uint32_t *none, Entry *to) {
     const int q_row = p.row_ids[b], q_col = p.col_ids[b];
-    const GroupOf g = group_of(p.cache, p.seqs, p.groups, p.B, b, p.max_len);
+    const GroupOf g = group_of(p.cache, p.seqs, p.groups, none && bit_of(none, b), p.B, b, p.max_len);
     Entry e = {g.s, g.len, 0, 0, g.count, g.first, g.shared, 0, q_row, q_col, g.prefix};
     const bool has = g.count > 0 && g.len >= g.shared, padding = q_row < 0 || q_col < 0 || g.s < 0;
     e.counts = has && !padding;
@@ -138,24 +140,65 @@ struct Start {
     int left, batch;
 };
 // What the threads look up for it is kept for the first batch, as far as there is room.
-constexpr int kKept = 224;
+constexpr int kKept = 208;
 struct Found {
     uint2 cost[kMaxBatch];
+    uint32_t begins[kMaxBatch / 32];  // a bit for each entry that begins a group
     Entry entries[kKept];
 };
-// All threads call it, and each gets it.  `found`: in shared memory, free when the first batch has been taken over.
+template <int RT>
+__device__ __forceinline__ uint2 cost_of(const SharedParams &p, const Entry &e, int b) {
+    return make_uint2(units_of(e.own1 - e.own0), leads(e, b) ? p.kv_heads * group_tiles<RT>(p, e) * (kOver + units_of(e.shared)) : 0);
+}
+// A group that another one begins inside of is none: otherwise two items would have the same rows, and two groups' tiles the same joint.  (Rarely called.)
 template <int RT, int NT>
-__device__ Start find_start(const SharedParams &p, Found &found) {
+__device__ __noinline__ void leave_out(const SharedParams &p, Found &found, uint32_t *none) {
+    uint2 *cost = found.cost;
+    const int tid = threadIdx.x, lane = tid & 31;
+#pragma unroll 1
+    for (int b0 = tid & ~31; b0 < p.B; b0 += NT) {
+        const int b = b0 + lane;
+        const Claim c = b < p.B ? claim_of(p.groups, p.B, b) : Claim();
+        const bool is = fits(c, b, p.B, p.max_len) && begins_inside(found.begins, c.first, c.count);
+        const unsigned those = __ballot_sync(~0u, is);
+        if (lane == 0) none[b0 >> 5] = those;
+        __syncwarp();
+        if (!is) continue;
+        Entry mine, &e = b < kKept ? found.entries[b] : mine;
+        entry_of(p, b, none, &e);
+        cost[b] = cost_of<RT>(p, e, b);
+        if (blockIdx.x == 0) p.grouped[b] = 0, atomicOr(p.cache.status, kCacheBad);
+    }
+}
+// All threads call it, and each gets it.  `found`: in shared memory, free when the first batch has been taken over.  none: a bit for each entry
+// whose group is none because another one begins inside it, there for as long as the block wants entries.
+template <int RT, int NT>
+__device__ Start find_start(const SharedParams &p, Found &found, uint32_t (&none)[kMaxBatch / 32]) {
     uint2 *cost = found.cost;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, batches = (p.B + p.pack - 1) / p.pack;
 #pragma unroll 1
-    for (int b = tid; b < p.B; b += NT) {
-        Entry mine, &e = b < kKept ? found.entries[b] : mine;
-        entry_of(p, b, &e);
-        cost[b] = make_uint2(units_of(e.own1 - e.own0), leads(e, b) ? p.kv_heads * group_tiles<RT>(p, e) * (kOver + units_of(e.shared)) : 0);
-        if (e.bad && blockIdx.x == 0) atomicOr(p.cache.status, kCacheBad);
+    for (int b0 = tid & ~31; b0 < p.B; b0 += NT) {
+        const int b = b0 + lane;
+        bool first = false;
+        if (b < p.B) {
+            Entry mine, &e = b < kKept ? found.entries[b] : mine;
+            entry_of(p, b, nullptr, &e);
+            cost[b] = cost_of<RT>(p, e, b), first = leads(e, b);
+            if (blockIdx.x == 0) p.grouped[b] = e.count > 0;
+            if (e.bad && blockIdx.x == 0) atomicOr(p.cache.status, kCacheBad);
+        }
+        const unsigned those = __ballot_sync(~0u, first);
+        if (lane == 0) found.begins[b0 >> 5] = those, none[b0 >> 5] = 0;
     }
     __syncthreads();
+    bool inside = false;
+#pragma unroll 1
+    for (int b = tid; b < p.B; b += NT)
+        if (bit_of(found.begins, b)) inside |= begins_inside(found.begins, b, min(p.groups[p.B + b], p.B - b));
+    if (__syncthreads_or(inside)) {
+        leave_out<RT, NT>(p, found, none);
+        __syncthreads();
+    }
     // a warp to each batch; its cost replaces that of its first entry
 #pragma unroll 1
     for (int i = warp; i < batches; i += NT / 32) {
@@ -214,7 +257,7 @@ template <int RT>
 __device__ __forceinline__ int row_of(const SharedParams &p, const Part &part, int r, int member) {
     return (part.b + member) * p.heads + part.kv * p.group + part.tile * RT + r - member * p.group;
 }
-// (tiles of a group of n entries: fewer than n own_tiles, so those of different groups have different places)
+// (tiles of a group of n entries: n own_tiles at most, so those of different groups, which have no entry in common, have different places)
 __device__ __forceinline__ Joint *joint_of(const SharedParams &p, int seg, int kv, int b, int tile) {
     return p.joints + ((size_t)seg * p.kv_heads + kv) * p.B * p.own_tiles + (size_t)b * p.own_tiles + tile;
 }
@@ -270,6 +313,7 @@ struct ScoutSmem {
     Entry entries[kScouts];  // of the batch
     int before[kScouts + 1]; // units of own tokens in front of an entry's
     unsigned leaders[4];     // a bit for each entry: it is the first of a group
+    uint32_t none[kMaxBatch / 32];  // of all entries there are: see find_start
     Wishes<RT> wishes[2];    // of the parts in turn
     Key list[kList];         // what look() writes is seen behind the next barrier
     uint8_t owners[kList];   // entries of the batch
@@ -316,7 +360,7 @@ struct Scout {
             if (found && b < kKept)
                 sm.entries[tid] = found[b];
             else
-                entry_of(p, b, sm.entries + tid);
+                entry_of(p, b, sm.none, sm.entries + tid);
             const Entry &e = sm.entries[tid];
             units = units_of(e.own1 - e.own0), first = leads(e, b);
         }
@@ -466,7 +510,7 @@ struct Scout {
             const int member = member_of<RT>(p, part, tid), view = view_at(p, part.kv * p.group + part.tile * RT + tid - member * p.group);
             const int held_at = part.b - batch * p.pack + member;
             Entry other;
-            if (held_at >= entries()) entry_of(p, part.b + member, &other);
+            if (held_at >= entries()) entry_of(p, part.b + member, sm.none, &other);
             const Entry &e = held_at >= entries() ? other : sm.entries[held_at];
             if (seg == 0 ? e.counts && e.first == part.b && e.count > 0 : e.own1 > e.own0) {
                 const bool text = e.q_row == MATE_ID_TEXT || e.q_col == MATE_ID_TEXT;
@@ -603,7 +647,7 @@ __global__ void __launch_bounds__(kSimtThreads, 2) shared_simt_kernel(const __gr
     ptx::wait_prior_grid();
     static_assert(sizeof(sm.q) + sizeof(sm.k) + sizeof(sm.v) + sizeof(sm.s) >= sizeof(Found), "room for the entries");
     Found &found = *reinterpret_cast<Found *>(smem_raw);
-    const Start start = find_start<kSimtRows, kSimtThreads>(p, found);
+    const Start start = find_start<kSimtRows, kSimtThreads>(p, found, sm.scout.none);
     if (start.left == 0) return;
     Scout<kSimtRows> scout = {p, sm.scout, tid, 1};
     if (tid < kScouts) scout.start(start, found);
@@ -952,7 +996,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
     launch_dependents();  // (what is launched next waits for the end of this before it reads results)
     static_assert(sizeof(sm.k) >= sizeof(Found), "room for the entries");
     Found &found = *reinterpret_cast<Found *>(sm.k);
-    const Start start = find_start<kTcRows, kTcThreads>(p, found);  // (its barriers: the set-up is seen by all)
+    const Start start = find_start<kTcRows, kTcThreads>(p, found, sm.scout.none);  // (its barriers: the set-up is seen by all)
     tc_fence_after();
     Scout<kTcRows> scout = {p, sm.scout, tid - 32 * kScoutWarp0, max(1, maps.run)};
     if (start.left && warp >= kScoutWarp0 && warp < kCopyWarp0) scout.start(start, found);
@@ -1455,13 +1499,15 @@ __global__ void __launch_bounds__(1024) shared_join_kernel(const __grid_constant
         const int seg = tid / kJoinRows, i = tid % kJoinRows, b = by_group(p, at0 + i), g = at0 + i - b * p.group;
         // (the batch is looked at ahead of the wait: the kernel in front of this one has waited for whoever wrote it before it let this one start)
         Entry e = {};
-        if (b < p.B) entry_of(p, b, &e);
+        if (b < p.B) entry_of(p, b, nullptr, &e);
         ptx::wait_prior_grid();
         Results of = {};
         if (b < p.B && (seg == 1 || e.count > 0)) {
             const int row = (seg == 0 ? b - e.first : b % p.pack) * p.group + g, r = row % RT;
+            const bool there = seg == 1 || p.grouped[b];  // (asked for together with what follows)
             const Joint joint = *joint_of(p, seg, kv, seg == 0 ? e.first : b / p.pack, row / RT);
-            if (joint.slot < 0) {
+            if (!there) {
+            } else if (joint.slot < 0) {
                 const size_t whole = (size_t)(seg * p.B + b) * p.heads + kv * p.group + g;
                 of = {p.whole + whole * p.d, p.whole_stats + whole, 0, 0, 4, 1};
             } else if (joint.slot <= 1 && in_range(joint.first, p.blocks) && joint.total > 0) {  // (it may be what lay there, after a wait ran out)
@@ -1539,13 +1585,14 @@ int n_blocks(const mate_cache_t *c) { return (c->dtype == MATE_F32 ? 2 : 1) * n_
 
 size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 struct Workspace {
-    size_t joints, stats, whole, parts, bytes;
+    size_t joints, stats, whole, grouped, parts, bytes;
 };
 Workspace workspace_of(const mate_cache_t *c, int B) {
     Workspace w = {};
     w.stats = align256(sizeof(Joint) * 2 * (size_t)c->kv_heads * B * own_tiles(c));
     w.whole = w.stats + align256(sizeof(float2) * 2 * (size_t)B * c->heads);
-    w.parts = w.whole + align256(sizeof(float) * 2 * (size_t)B * c->heads * c->d);
+    w.grouped = w.whole + align256(sizeof(float) * 2 * (size_t)B * c->heads * c->d);
+    w.parts = w.grouped + align256((size_t)B);
     w.bytes = w.parts + sizeof(float) * 2 * (size_t)n_blocks(c) * part_floats(rows_of_tile(c), c->d);
     return w;
 }
@@ -1625,7 +1672,7 @@ int mate_attn_decode_shared(const mate_cache_t *cache, int layer, const void *Q,
     if (B == 0) return MATE_OK;
     const int most = cache->width * cache->page_size;
     if (max_len == 0 || max_len > most) max_len = most;
-    // units of the batch, shared and own (these by up to a quarter more), are unsigned 32-bit numbers
+    // units of the batch, shared (of groups that have no entry in common) and own (these by up to a quarter more), are unsigned 32-bit numbers
     if (B > kMaxBatch || (int64_t)B * cache->kv_heads * own_tiles(cache) > INT32_MAX / 2 / (kOver + units_of(max_len))) return MATE_ERR_UNSUPPORTED;
     const Workspace w = workspace_of(cache, B);
     if (!workspace || workspace_bytes < std::max(w.bytes, decode_workspace(cache, B))) return MATE_ERR_WORKSPACE;
@@ -1656,6 +1703,7 @@ int mate_attn_decode_shared(const mate_cache_t *cache, int layer, const void *Q,
     p.joints = reinterpret_cast<Joint *>(ws + w.joints);
     p.whole_stats = reinterpret_cast<float2 *>(ws + w.stats);
     p.whole = reinterpret_cast<float *>(ws + w.whole);
+    p.grouped = reinterpret_cast<uint8_t *>(ws + w.grouped);
     p.parts = reinterpret_cast<float *>(ws + w.parts);
     if (cache->dtype == MATE_BF16) {
         // a score of -inf stays one whatever it is multiplied by: a factor above 0, so small for a scale of 0 that every weight is 1
