@@ -369,7 +369,10 @@ def _axes(axes):
     if isinstance(axes, bytes):
         return axes
     try:
-        return bytes(axes if isinstance(axes, (list, tuple)) else np.asarray(axes).tolist())
+        x = axes if isinstance(axes, (list, tuple)) else np.asarray(axes).tolist()
+        if not isinstance(x, (list, tuple)):  # (of a number, bytes would make that many zeros)
+            raise TypeError("not a sequence")
+        return bytes(x)
     except (TypeError, ValueError) as e:
         raise ValueError("axes must be whole numbers, one for each frequency") from e
 
