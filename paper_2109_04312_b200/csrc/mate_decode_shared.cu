@@ -39,6 +39,7 @@
 #include "mate_cache.h"
 #include "sm100_ptx.cuh"
 #include "tc_tiles.cuh"
+#include "wait_together.h"
 
 namespace mate {
 // mate_decode.cu
@@ -873,16 +874,17 @@ __device__ __forceinline__ bool any_scout(bool x) {
     return r != 0;
 }
 
-// Every wait is bounded; the first one to run out raises the flag that ends all of them.
-__device__ __noinline__ bool wait_long(uint32_t bar, uint32_t parity, volatile int *abort) {
-#pragma unroll 1
-    for (uint32_t i = 0; i < ptx::kWaitLimit; ++i) {
-        if (ptx::mbar_try_wait(bar, parity)) return true;
-        if (*abort) return false;
-    }
-    *abort = 1;
-    return false;
-}
+// Every wait is bounded; the first one to run out raises the flag that ends all of them.  A warp passes a wait, or leaves its role, as a whole.
+struct Wait {
+    uint32_t bar, parity;
+    volatile int *abort;
+    __device__ bool there() const { return ptx::mbar_try_wait(bar, parity); }
+    __device__ bool all(bool x) const { return __all_sync(~0u, x); }
+    __device__ bool any(bool x) const { return __any_sync(~0u, x); }
+    __device__ bool given_up() const { return *abort; }
+    __device__ void give_up() const { *abort = 1; }
+};
+__device__ __noinline__ bool wait_long(uint32_t bar, uint32_t parity, volatile int *abort) { return wait_together(Wait{bar, parity, abort}, ptx::kWaitLimit); }
 
 __device__ __forceinline__ uint32_t bits_below(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u; }
 __device__ __forceinline__ float top_score(const uint32_t (&v)[32]) {
@@ -1010,7 +1012,9 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
     const uint32_t tmem = __shfl_sync(~0u, sm.tmem, 0);
 
     volatile int *abort = &sm.abort;
-    const auto wait = [&](const uint64_t &b, uint32_t parity) { return mbar_try_wait(smem_u32(&b), parity) || wait_long(smem_u32(&b), parity, &sm.abort); };
+    const auto wait = [&](const uint64_t &b, uint32_t parity) {
+        return __all_sync(~0u, mbar_try_wait(smem_u32(&b), parity)) || wait_long(smem_u32(&b), parity, &sm.abort);
+    };
 
     if (start.left == 0) {
     } else if (warp < kSoftmaxWarps) {
@@ -1294,11 +1298,13 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
             }
             if (!last) break;
         }
-        // behind the last one
+        // behind the last one (where a wait has failed its place may still be read, and the flag ends the other roles)
         if (t >= kMetas) ok &= wait(sm.meta_empty[t % kMetas], (t / kMetas - 1) & 1);
-        if (lt == 0) sm.meta[t % kMetas].n = -1;
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(sm.meta_full[t % kMetas]));
+        if (!any_scout(!ok)) {
+            if (lt == 0) sm.meta[t % kMetas].n = -1;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(sm.meta_full[t % kMetas]));
+        }
         if (scout.bad) atomicOr(p.cache.status, kCacheBad);
     } else if (warp < kMmaWarp) {
         // ------------------------------------------------------------------ copies of queries and keys (first warp) and values (second)
@@ -1336,10 +1342,10 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(sm.q_full[qb]));
         };
-        int parts = 0;
-        bool asked = false;  // the queries of part number `parts`
+        int parts = 0, c = 0;  // parts, tiles that have been asked for
+        bool asked = false;    // the queries of part number `parts`
 #pragma unroll 1
-        for (int t = 0, c = 0;; ++t) {
+        for (int t = 0;; ++t) {
             if (!v && !asked) {
                 if (!wait(sm.part_full[parts & 1], parts / 2 & 1) || sm.part[parts & 1].n_rows == 0) break;
                 copy_queries(parts & 1);
@@ -1399,6 +1405,11 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(sm.meta_empty[t % kMetas]));
         }
+        // No copy outlives the block, whoever has given up: the last tile of every stage is waited for.
+        asm volatile("cp.async.wait_all;" ::: "memory");
+#pragma unroll 1
+        for (int stage = 0; stage < min(c, kStages); ++stage)
+            mbar_wait_bounded(bar(v ? sm.v_full[stage] : sm.k_full[stage]), (c - 1 - stage) / kStages & 1, kWaitLimit);
     } else {
         // ------------------------------------------------------------------ the products, a warp to each team
         // S = Q K^T of a tile as soon as its keys are there and the team's last P V, whose weights have the place of S, is done; O += P V as
@@ -1467,8 +1478,6 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
         __syncwarp();
         mbar_wait_bounded(bar(sm.final_), 0, kWaitLimit);
     }
-    if (*abort)  // copies may still be on their way to shared memory: they take a few microseconds
-        for (int i = 0; i < 50; ++i) __nanosleep(1000);
     tc_fence_before();
     __syncthreads();
     if (tid == 0 && *abort) atomicOr(p.cache.status, kCacheTimeout);
