@@ -396,7 +396,9 @@ int mate_cache_compact(const mate_cache_t *cache, int32_t *n_live, void *workspa
 
 /* Which entries of a list of sequences (null: 0 .. n - 1) share their first pages, as mate_cache_fork makes them: entry i belongs to the
  * group of entry i - 1 if both have at least m full pages and the first m of them are the same, m = max(1, min_len / page_size rounded
- * up).  (Sequences that share pages but do not follow one another in the list make groups of their own.)  For every entry:
+ * up).  (Sequences that share pages but do not follow one another in the list make groups of their own.)  There is one level of groups: where all
+ * sequences begin with the same few pages, instructions say, and some of them share a table behind those, a min_len beyond the instructions gives a
+ * group to each table; with less they are all one group, which shares the instructions only.  For every entry:
  *   groups[i]          the first entry of its group
  *   groups[n + i]      the group's entries, which follow one another
  *   groups[2 n + i]    tokens that they all share: the largest number of leading full pages that are the same in all of them, times
@@ -429,7 +431,8 @@ int mate_cache_status(const mate_cache_t *cache, void *stream);
  *              three share no memory
  *   workspace  device, 256-byte aligned, mate_cache_workspace_bytes; contents undefined afterwards; calls that overlap need one each
  * Scores, softmax, weights and sums in fp32; with bf16 only the result is rounded.  A NaN or Inf in the key or value of a token
- * reaches the heads that attend the token and no others.  heads <= 1024.  Asynchronous on `stream`. */
+ * reaches the heads that attend the token and no others (an Inf in a bf16 value as an Inf or as a NaN: it is multiplied by a weight in
+ * parts, some of which may be 0).  heads <= 1024.  Asynchronous on `stream`. */
 int mate_attn_decode(const mate_cache_t *cache, int layer, const void *Q, const int64_t *q_stride, int B, const int32_t *seqs,
                      const int32_t *row_ids, const int32_t *col_ids, float scale, int max_len, void *O, float *LSE, void *workspace,
                      size_t workspace_bytes, void *stream);
@@ -446,8 +449,11 @@ int mate_attn_decode(const mate_cache_t *cache, int layer, const void *Q, const 
  * alone, or attend their own tokens only, and status says so.  So is a group among whose entries another one begins: an entry is in one
  * group at most.  B is at most 4096.
  *   flags      0: where the batch may read no more than 192 MB (bf16) or 1 GB (fp32) one sequence after another -- B max_len kv_heads
- *              keys and values --, that is the faster way, and taken: the results are mate_attn_decode's; MATE_SHARED_ALWAYS: the shared
+ *              keys and values --, that way is taken: the results are mate_attn_decode's; MATE_SHARED_ALWAYS: the shared
  *              tokens are read once all the same
+ * Reading them once pays for many sequences in one group or a few.  Beyond those sizes mate_attn_decode is the faster call for batches without groups (bf16 1.6
+ * to 2.5 times), with fp32 for all but groups of some dozens, and where the new tokens are those of cells that attend little of a long table.
+ * The batch's work is counted in 32 bits: B kv_heads ceil(heads / kv_heads / (bf16 ? 128 : 64)) (8 + max_len / 32) is below 2^30.
  * Where they are read once and the type is bf16, weights enter the product with the values as the sum of two bf16, with 16 bits
  * (mate_attn_decode: with all of their 24).  All other arguments, limits and errors as for mate_attn_decode. */
 int mate_attn_decode_shared(const mate_cache_t *cache, int layer, const void *Q, const int64_t *q_stride, int B, const int32_t *seqs,

@@ -463,7 +463,9 @@ def mate_cache_compact(cache, n_live=None):
 def mate_cache_groups(cache, seqs=None, min_len=1, out=None):
     """Which entries of a list of sequences (None: all) that follow one another share their first pages, at least min_len tokens of them
     (see mate_cache_groups in mate.h).  seqs: int32 CUDA tensor [n].  Returns int32 [3, n]: of every entry its group's first entry, the
-    group's size, and the tokens that its sequences share (0 for a group of one).  out: where it goes, contiguous, apart from seqs."""
+    group's size, and the tokens that its sequences share (0 for a group of one).  There is one level: where all sequences begin with the same few
+    pages and some share a table behind them, a min_len beyond those pages gives each table a group.  out: where it goes, contiguous, apart from
+    seqs."""
     return cache._native.cache_groups(cache._info, seqs, min_len, out)
 
 
@@ -481,6 +483,7 @@ def mate_attn_decode_shared(cache, Q, row_ids, col_ids, groups, seqs=None, layer
     """mate_attn_decode for sequences that share their first tokens, such as beams or questions about one table: what a group shares is read
     once for all of its sequences (see mate_attn_decode_shared in mate.h).  groups: int32 [3, B], what mate_cache_groups returns for the same
     seqs: call it when the batch or the pages of its sequences have changed, once for all layers.  max_len: up to where tokens count, and how much
-    the batch may have to read; where that is little each sequence is read by itself, unless always is set.  The rest as for mate_attn_decode.
+    the batch may have to read; where that is little each sequence is read by itself, unless always is set.  It pays for many sequences in one group or a
+    few (see mate.h for where mate_attn_decode is faster).  The rest as for mate_attn_decode.
     Returns (O, LSE)."""
     return cache._native.attn_decode_shared(cache._info, layer, Q, seqs, row_ids, col_ids, scale, max_len, out, lse, groups, always)

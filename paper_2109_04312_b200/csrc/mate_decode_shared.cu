@@ -7,8 +7,8 @@
 // Work.  An item is a kv head and a tile of rows (128 with bf16, 64 with fp32) of a segment: a group's shared tokens, with the query heads of all of
 // its sequences, or the own tokens of as many sequences as their heads fill a tile (reading 32 sequences of 4 heads by turns would be 32 tiles
 // of 4 rows; together they are a few tiles of 128 keys, each of which is for the rows of one sequence).  Its length is counted in units of kUnit tokens,
-// and kOver units stand for what an item costs whatever its length (8: 40 us for 64 questions, 102 for 256 sequences; 4: 42, 105; 16: 41, 102, but
-// beams 33 instead of 30).  Blocks, one to an SM, get equal shares of all items' units (found by every block from the lengths, which the host does
+// and kOver units stand for what an item costs whatever its length (8: 39.1 us for 64 questions, 101 for 256 sequences, 30.1 for beams; 4: 40.0, 102,
+// 29.5; 16: 40.7, 102, 32.6).  Blocks, one to an SM, get equal shares of all items' units (found by every block from the lengths, which the host does
 // not know): a long segment is spread over the GPU, short ones are put together.  What a block leaves of an item that is not a row's whole
 // result -- m, sum P and the sum of values, in fp32 -- is joined by a second kernel, in the order of the tokens: the same bits on every
 // launch.
@@ -24,12 +24,15 @@
 //
 // What bounds it.  The chain of a team's tile, 7.2 thousand cycles of which the other team's overlap half: S 0.5, weights 4 (four chunks of 32 keys, one
 // after the other in a warp), P V 1.3, whose weights lie where the next S goes, barriers and the other team's tile 1.4; the products alone would
-// take 1.6 a tile.  64 questions about 8192 tokens, 8 kv heads of 4 x 128: 38 us, of which start 9 (lengths and groups in two rounds of loads, pages, ids, then
+// take 1.6 a tile.  64 questions about 8192 tokens, 8 kv heads of 4 x 128: 39 us, of which start 10 (lengths and groups in two rounds of loads, pages, ids, then
 // the first keys), tiles 18, joining and launches the rest.  Tiles of own keys take 5 thousand cycles each: V has to be looked through ahead of weights of 0
 // (0.8), and copies of own runs are short.  Cells (a token attends a few hundred of 4096): looks, 1.1 thousand cycles per 256 tokens.  Measured and
-// left out: chunks of 64 keys (256 sequences 102 -> 109 us), S of one half of a tile while the other's weights are made (106), three tiles of
-// values and one of queries (106), rows brought to L2 ahead of their copies (103); with 64 elements a third place for scores, so that S does not wait for
-// P V (beams 29 -> 30).
+// left out, with what they cost where the rest took 102 us for 256 sequences: chunks of 64 keys (109), S of one half of a tile while the other's weights
+// are made (106), three tiles of values and one of queries (106), rows brought to L2 ahead of their copies (103); with 64 elements a third place for
+// scores, so that S does not wait for P V (beams 29 -> 30).
+//
+// Where it is the wrong way: sequences without groups, or in groups of few rows, and own tokens by the thousand, whose tiles multiply 128 rows by keys that
+// one sequence's heads count for; see alone_bytes.
 #include <cuda_bf16.h>
 
 #include <algorithm>
@@ -1580,11 +1583,15 @@ __global__ void __launch_bounds__(1024) shared_join_kernel(const __grid_constant
 
 // ---- host
 
-// Up to here a batch is faster read one sequence after another, by all that the host knows: keys and values of all sequences at their longest.
-// bf16, all in one group, 12 heads of 64 or 8 of 4 x 128 elements: 4 sequences of 4096 tokens (51 and 68 MB) 14 and 17 us alone, 21 and 20 shared;
-// 16 of 4096 (203 and 271 MB) 31 and 36, 21 and 21.  (In eight groups of 8 sequences both take as long at 800 MB; without groups, or where cells
-// leave most tokens out, one by one stays the faster way.  None of it is known here.)  fp32, whose products are not made by the tensor cores: 64 sequences of 4096 tokens, 2 heads of 3 x 48, 203 MB, 44 and 48;
-// of 16384, 807 MB, 136 and 106; 8 heads of 4 x 128, 541 MB 85 and 101, 2.2 GB 292 and 268.
+// Up to here a batch is read one sequence after another: by keys and values of all sequences at their longest, which is all that the host knows.  us
+// one by one and together, 32 own tokens each:
+//   bf16, all in one group, 12 heads of 64 or 8 of 4 x 128 elements: 4 sequences of 4096 tokens (51 and 68 MB) 14 and 21, 17 and 20; 16 of 4096 (203
+//   and 271 MB) 31 and 22, 36 and 21; 64 of 16384 (4.3 GB) 400 and 51.  In eight groups of 8 they come together later: 1024 tokens (277 MB) 21 and 38,
+//   4096 (812 MB and 1.1 GB) 35 and 37, 42 and 35.  Without groups one by one stays the faster way however long they are: 16 of 4096 tokens (203 MB) 23 and
+//   49, of 16384 66 and 164, 84 and 134; and so it is where cells leave most tokens out (29 and 43).
+//   fp32, whose products are not made by the tensor cores: 64 sequences of 16384 tokens, 2 heads of 3 x 48 (807 MB), 136 and 106; 8 heads of 4 x 128, 16 of
+//   4096 (541 MB) 85 and 101, 64 of 4096 (2.2 GB) 292 and 268, 16 of 16384 284 and 241; in eight groups of 8 93 and 225, without groups 158 and 1450.
+// So the rule is for batches in one group or a few; what groups there are only the device knows.  A caller who knows of few takes mate_attn_decode.
 double alone_bytes(const mate_cache_t *c) { return c->dtype == MATE_F32 ? 1024.0 * (1 << 20) : 192.0 * (1 << 20); }
 
 int rows_of_tile(const mate_cache_t *c) { return c->dtype == MATE_F32 ? kSimtRows : kTcRows; }
@@ -1694,8 +1701,8 @@ int mate_attn_decode_shared(const mate_cache_t *cache, int layer, const void *Q,
     p.Q = Q, p.q_batch = q_stride[0], p.q_head = q_stride[1];
     p.B = B, p.heads = cache->heads, p.kv_heads = cache->kv_heads, p.group = cache->heads / cache->kv_heads;
     p.d = cache->d, p.max_len = max_len, p.pack = pack_of(cache), p.own_tiles = own_tiles(cache);
-    // (whose copies are shorter: 64 questions with 128 tokens of their own, heads of 128 elements, 40.1 us by eight eighths, 38.8 by nine, 37.9 by ten,
-    // 38.9 by eleven, 256 sequences 101, 99, 99, 100; heads of 64: beams 29.3, 29.5, 29.6, 29.9, cells 40.5, 41.2, 41.4, 41.5)
+    // (whose copies are shorter: 64 questions with 128 tokens of their own, heads of 128 elements, 39.1 us, without it 41.1, 256 sequences 101 and 102.5;
+    // heads of 64: beams 30.2 with it and 30.1 without, cells 42.3 and 42.9; when it was chosen an eighth gave 38.8 and three 38.9 where a quarter gave 37.9)
     p.own_quarter = cache->dtype == MATE_BF16 && cache->d > 64;
     p.seqs = seqs, p.row_ids = row_ids, p.col_ids = col_ids, p.groups = groups;
     p.scale_log2 = scale * kLog2e, p.O = O, p.LSE = LSE;
