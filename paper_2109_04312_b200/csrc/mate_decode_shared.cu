@@ -7,8 +7,8 @@
 // Work.  An item is a kv head and a tile of rows (128 with bf16, 64 with fp32) of a segment: a group's shared tokens, with the query heads of all of
 // its sequences, or the own tokens of as many sequences as their heads fill a tile (reading 32 sequences of 4 heads by turns would be 32 tiles
 // of 4 rows; together they are a few tiles of 128 keys, each of which is for the rows of one sequence).  Its length is counted in units of kUnit tokens,
-// and kOver units stand for what an item costs whatever its length (8: 40.8 us for 64 questions, 102 for 256 sequences, 32.2 for beams; 4: 41.9, 102,
-// 31.9; 16, with two parts a weight, 1.6, 1 and 2.5 us more than 8).  Blocks, one to an SM, get equal shares of all items' units (found by every block from the lengths, which the host does
+// and kOver units stand for what an item costs whatever its length (8: 39.1 us for 64 questions, 101 for 256 sequences, 30.1 for beams; 4: 40.0, 102,
+// 29.5; 16: 40.7, 102, 32.6).  Blocks, one to an SM, get equal shares of all items' units (found by every block from the lengths, which the host does
 // not know): a long segment is spread over the GPU, short ones are put together.  What a block leaves of an item that is not a row's whole
 // result -- m, sum P and the sum of values, in fp32 -- is joined by a second kernel, in the order of the tokens: the same bits on every
 // launch.
@@ -18,22 +18,18 @@
 //
 // Roles of a bf16 block.  Four warps look for keys (Scout) and fill tiles of 128 of them; two copy keys and values (sixteen slots that follow one
 // another by a bulk tensor copy, the rest in 16 bytes a lane) and the queries; two teams of four warps, a thread to a row, take the tiles in turn and make
-// weights of the scores; one warp issues the products S, one P V.  Tensor memory: O 128 columns, and for each team S 128 columns, whose place the weights
-// take, and 64 more: a weight is the sum of three bf16, which is all of its 24 bits, as in mate_attn_decode (two of them, 16 bits, left
-// differences of large weights off by up to 3 %, and one result in some hundred rounded to the neighbouring bf16).  An O for each team, as there
-// was with two parts, would leave no room for the third; with one for both the teams have one base for a row, which they hand on from tile to tile.
-// fp32: shared_simt_kernel, 64 rows against 32 keys, no tensor cores.
+// weights of the scores; a warp for each team issues its products.  Tensor memory: O of both teams 2 x 128 columns, S 2 x 128; the weights take
+// the place of the scores, 16 keys as 8 columns of bf16 pairs and 8 of what the rounding left.  (Weights as one bf16 would be off by 2^-9, more than the
+// result's rounding.)  fp32: shared_simt_kernel, 64 rows against 32 keys, no tensor cores.
 //
-// What bounds it.  The chain of a team's tile, 7.6 thousand cycles, which the other team's overlap: weights 3.2 (four chunks of 32 keys, one after the other in
-// a warp), the base and the weights' way to tensor memory 0.6, P V, whose weights lie where the next S goes, and S 2.1, waits for what is where and
-// barriers the rest; the products alone would take 2.1 a tile.  64 questions about 8192 tokens, 8 kv heads of 4 x 128: 40.8 us, of which start 10 (lengths
-// and groups in two rounds of loads, pages, ids, then the first keys), tiles 20, joining and launches the rest.  Tiles of own keys take 5.3 thousand cycles
-// each, most of them until their values are there: copies of own runs are short.  Cells (a token attends a few hundred of 4096): looks, 1.1 thousand cycles
-// per 256 tokens.  Measured and left out, 256 sequences 101.8 us: the teams with half of every tile each, so that they wait for one another twice a
-// tile (112.5; with the highest scores found on the way 120); the highest score of a tile looked for ahead of its weights (108.7), and the first half
-// of the weights handed over early (111); parts of the weights cut off by masks instead of rounded (102.2).  With two parts and an O for each team, where the
-// rest took 102: chunks of 64 keys (109), S of one half of a tile while the other's weights are made (106), three tiles of values and one of queries (106),
-// rows brought to L2 ahead of their copies (103).
+// What bounds it.  The chain of a team's tile, 7.2 thousand cycles of which the other team's overlap half: S 0.5, weights 4 (four chunks of 32 keys, one
+// after the other in a warp), P V 1.3, whose weights lie where the next S goes, barriers and the other team's tile 1.4; the products alone would
+// take 1.6 a tile.  64 questions about 8192 tokens, 8 kv heads of 4 x 128: 39 us, of which start 10 (lengths and groups in two rounds of loads, pages, ids, then
+// the first keys), tiles 18, joining and launches the rest.  Tiles of own keys take 5 thousand cycles each: V has to be looked through ahead of weights of 0
+// (0.8), and copies of own runs are short.  Cells (a token attends a few hundred of 4096): looks, 1.1 thousand cycles per 256 tokens.  Measured and
+// left out, with what they cost where the rest took 102 us for 256 sequences: chunks of 64 keys (109), S of one half of a tile while the other's weights
+// are made (106), three tiles of values and one of queries (106), rows brought to L2 ahead of their copies (103); with 64 elements a third place for
+// scores, so that S does not wait for P V (beams 29 -> 30).
 //
 // Where it is the wrong way: sequences without groups, or in groups of few rows, and own tokens by the thousand, whose tiles multiply 128 rows by keys that
 // one sequence's heads count for; see alone_bytes.
@@ -818,14 +814,13 @@ constexpr int kTcRows = 128, kTcKeys = 128;
 constexpr int kSoftmaxWarps = 8;              // two teams, which take the tiles in turn; a thread to a row
 constexpr int kScoutWarp0 = kSoftmaxWarps, kScoutWarps = kScouts / 32;
 constexpr int kCopyWarp0 = kScoutWarp0 + kScoutWarps, kCopyWarps = 2;  // keys, values
-constexpr int kMmaWarp = kCopyWarp0 + kCopyWarps, kMmaWarps = 2;       // scores, weights times values
+constexpr int kMmaWarp = kCopyWarp0 + kCopyWarps, kMmaWarps = 2;       // a team each
 constexpr int kTcThreads = 32 * (kMmaWarp + kMmaWarps);
 constexpr int kMetas = 4;                     // tiles whose keys are known
-constexpr float kRescale = 8.f;               // log2 units that a score may exceed its row's base by, and that the first ones may be off 0 by with a base of 0
-// tensor memory: O (fp32), then two places for S of a tile (fp32), which P takes the place of: a weight is the sum of three bf16, and of every 16 keys the
-// first (8 columns of pairs) and second parts lie where the scores were; the third parts behind them all
-constexpr uint32_t kTmemCols = 512, kTmemO = 0, kTmemS = 128, kTmemThird = kTcKeys, kTmemTile = kTcKeys + kTcKeys / 2;
-static_assert(kTmemS + 2 * kTmemTile <= kTmemCols, "columns of tensor memory");
+constexpr float kRescale = 8.f;               // log2 units that a score may exceed its row's base by
+// tensor memory: O of the teams (fp32), then S of their tiles (fp32), which P takes the place of: of every 16 keys the weights' upper halves
+// (8 columns of bf16 pairs) and their lower ones
+constexpr uint32_t kTmemCols = 512, kTmemO = 0, kTmemS = 256;
 
 template <int DP>
 struct TcShape {
@@ -859,9 +854,9 @@ struct TcSmem {  // from a multiple of 1024 bytes on
     ScoutSmem<kTcRows> scout;
     Rows<kTcRows> rows[2];
     Part part[2];
-    float2 stats[2][kTcRows];  // of the rows, with the last tile of each team: base, and behind the part's last one the sum
+    float2 stats[2][kTcRows];
     uint64_t part_full[2], q_full[2], q_empty[2], k_full[4], k_empty[4], v_full[4], v_empty[4], meta_full[kMetas], meta_empty[kMetas], s_full[2], p_full[2],
-        pv_done[2], based[2][kSoftmaxWarps / 2], pair[kSoftmaxWarps / 2], team[2], final_;
+        pv_done[2], team[2], both, final_;
     int odd[2];
     uint32_t tmem;
     int abort;
@@ -903,32 +898,25 @@ __device__ __forceinline__ float top_score(const uint32_t (&v)[32]) {
         for (int j = 0; j < 4; ++j) t[j] = ptx::fmax3(t[j], __uint_as_float(v[e + 2 * j]), __uint_as_float(v[e + 2 * j + 1]));
     return fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
 }
-// A pair of weights as three pairs of bf16, whose sum has all of the 24 bits: rounded, what the rounding left, rounded, and what that left.
-__device__ __forceinline__ void cut(float x, float y, uint32_t &first, uint32_t &second, uint32_t &third) {
-    const auto part = [](float &lo, float &hi) {
-        const uint32_t h = ptx::cvt_bf16x2(lo, hi);
-        ptx::unpack_f32x2(ptx::sub_f32x2(ptx::pack_f32x2(lo, hi), ptx::pack_f32x2(h << 16, h & 0xffff0000u)), lo, hi);
-        return h;
-    };
-    first = part(x, y);
-    second = part(x, y);
-    third = ptx::cvt_bf16x2(x, y);
-}
-// Weights 2^(s scale - base) of 32 keys: of every 16 the first and second parts, and the third ones.
-__device__ __forceinline__ void weigh(uint32_t (&v)[32], uint32_t (&third)[16], uint64_t scale2, uint64_t neg_base2, uint64_t (&sum)[2]) {
+// Weights 2^(s scale - base), 16 keys at a time, as pairs of bf16: rounded, and what the rounding left, rounded (their sum has 16 bits: an
+// error of 2^-17 of a weight, which the result's rounding to bf16, 2^-9, hides but for one value in some hundred).  The sums take all of them.
+__device__ __forceinline__ void weigh(uint32_t (&v)[32], uint64_t scale2, uint64_t neg_base2, uint64_t (&sum)[2]) {
 #pragma unroll
     for (int i = 0; i < 32; i += 16) {
-        uint32_t second[8];
+        uint32_t lo[8];
 #pragma unroll
         for (int e = 0; e < 16; e += 2) {
             float x, y;
             ptx::unpack_f32x2(ptx::fma_f32x2(ptx::pack_f32x2(v[i + e], v[i + e + 1]), scale2, neg_base2), x, y);
             x = ptx::ex2(x), y = ptx::ex2(y);
-            sum[e >> 1 & 1] = ptx::add_f32x2(sum[e >> 1 & 1], ptx::pack_f32x2(x, y));
-            cut(x, y, v[i + (e >> 1)], second[e >> 1], third[(i + e) >> 1]);
+            const uint64_t xy = ptx::pack_f32x2(x, y);
+            sum[e >> 1 & 1] = ptx::add_f32x2(sum[e >> 1 & 1], xy);
+            const uint32_t h = ptx::cvt_bf16x2(x, y);
+            ptx::unpack_f32x2(ptx::sub_f32x2(xy, ptx::pack_f32x2(h << 16, h & 0xffff0000u)), x, y);
+            v[i + (e >> 1)] = h, lo[e >> 1] = ptx::cvt_bf16x2(x, y);
         }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[i + 8 + e] = second[e];
+        for (int e = 0; e < 8; ++e) v[i + 8 + e] = lo[e];
     }
 }
 
@@ -948,50 +936,28 @@ __device__ __noinline__ void scale_o(uint32_t tO, int n, float keep) {
     ptx::tc_wait_st();
 }
 
-// The row's weights of 32 keys times `keep` (rarely): of the first two parts from tP on, of the third one from tThird on.
-__device__ __noinline__ void scale_p(uint32_t tP, uint32_t tThird, float keep) {
+// The row's weights of the keys before, where they have not gone into O yet (more rarely still).
+__device__ __noinline__ void scale_p(uint32_t tP, int n, float keep) {
     ptx::tc_wait_st();
 #pragma unroll 1
-    for (int i = 0; i < 32; i += 16) {
-        uint32_t first[8], second[8], third[8];
-        ptx::tmem_ld8(tP + i, first);
-        ptx::tmem_ld8(tP + i + 8, second);
-        ptx::tmem_ld8(tThird + i / 2, third);
+    for (int i = 0; i < n; i += 16) {
+        uint32_t hi[8], lo[8];
+        ptx::tmem_ld8(tP + i, hi);
+        ptx::tmem_ld8(tP + i + 8, lo);
         ptx::tc_wait_ld();
-        ptx::reg_fence(first);
-        ptx::reg_fence(second);
-        ptx::reg_fence(third);
+        ptx::reg_fence(hi);
+        ptx::reg_fence(lo);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const auto both = [&](auto half) { return half(first[e]) + (half(second[e]) + half(third[e])); };
-            const float x = both([](uint32_t z) { return __uint_as_float(z << 16); }), y = both([](uint32_t z) { return __uint_as_float(z & 0xffff0000u); });
-            cut(x * keep, y * keep, first[e], second[e], third[e]);
+            const float x = (__uint_as_float(hi[e] << 16) + __uint_as_float(lo[e] << 16)) * keep;
+            const float y = (__uint_as_float(hi[e] & 0xffff0000u) + __uint_as_float(lo[e] & 0xffff0000u)) * keep;
+            hi[e] = ptx::cvt_bf16x2(x, y);
+            lo[e] = ptx::cvt_bf16x2(x - __uint_as_float(hi[e] << 16), y - __uint_as_float(hi[e] & 0xffff0000u));
         }
-        ptx::tmem_st8(tP + i, first);
-        ptx::tmem_st8(tP + i + 8, second);
-        ptx::tmem_st8(tThird + i / 2, third);
+        ptx::tmem_st8(tP + i, hi);
+        ptx::tmem_st8(tP + i + 8, lo);
     }
     ptx::tc_wait_st();
-}
-
-// Weights of 32 keys that none of the warp's rows attend.
-__device__ __noinline__ void no_weights(uint32_t tP, uint32_t tThird) {
-    const uint32_t zero[16] = {};
-    ptx::tmem_st16(tP, zero);
-    ptx::tmem_st16(tP + 16, zero);
-    ptx::tmem_st16(tThird, zero);
-}
-
-// The scores of 32 keys, without those that the row does not attend.
-__device__ __forceinline__ void scores(uint32_t tS, uint32_t on, uint32_t (&v)[32]) {
-    ptx::tmem_ld32(tS, v);
-    ptx::tc_wait_ld();
-    ptx::reg_fence(v);
-    if (!__all_sync(~0u, on == ~0u)) {
-#pragma unroll
-        for (int e = 0; e < 32; ++e)
-            if (!(on >> e & 1)) v[e] = 0xff800000u;
-    }
 }
 
 template <int DP>
@@ -1008,21 +974,19 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
         if (lane < 2) {
             mbar_init(bar(sm.part_full[lane]), 1);
             mbar_init(bar(sm.q_full[lane]), kScoutWarps + 1);
-            mbar_init(bar(sm.q_empty[lane]), kSoftmaxWarps + 1);
+            mbar_init(bar(sm.q_empty[lane]), kSoftmaxWarps + kMmaWarps);
             mbar_init(bar(sm.s_full[lane]), 1), mbar_init(bar(sm.pv_done[lane]), 1);
             mbar_init(bar(sm.p_full[lane]), kSoftmaxWarps / 2);
             mbar_init(bar(sm.team[lane]), kSoftmaxWarps / 2);
             sm.odd[lane] = 0;
         }
-        if (lane < kSoftmaxWarps) mbar_init(bar(sm.based[lane & 1][lane >> 1]), 1);
-        if (lane < kSoftmaxWarps / 2) mbar_init(bar(sm.pair[lane]), 2);
         if (lane < kStages) {
             mbar_init(bar(sm.k_full[lane]), 1), mbar_init(bar(sm.v_full[lane]), 1);
             mbar_init(bar(sm.k_empty[lane]), 1), mbar_init(bar(sm.v_empty[lane]), 1);
         }
         if (lane < kMetas) mbar_init(bar(sm.meta_full[lane]), kScoutWarps), mbar_init(bar(sm.meta_empty[lane]), kSoftmaxWarps + kCopyWarps + kMmaWarps);
         if (lane == 0) {
-            mbar_init(bar(sm.final_), kMmaWarps);
+            mbar_init(bar(sm.both), kSoftmaxWarps), mbar_init(bar(sm.final_), kMmaWarps);
             sm.abort = 0;
         }
         fence_mbar_init();
@@ -1058,20 +1022,19 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
     if (start.left == 0) {
     } else if (warp < kSoftmaxWarps) {
         // ------------------------------------------------------------------ softmax and results
-        const int team = warp >> 2, quarter = warp & 3, r = tid & 127;  // row: the lane of tensor memory
-        const uint32_t lanes = (uint32_t)(quarter * 32) << 16, tS = tmem + lanes + kTmemS + team * kTmemTile, tO = tmem + lanes + kTmemO;
+        const int team = warp >> 2, r = tid & 127;  // row: the lane of tensor memory
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, tS = tmem + lanes + kTmemS + team * kTcKeys, tO = tmem + lanes + kTmemO + team * 128;
         const uint64_t scale2 = pack_f32x2(p.scale_log2, p.scale_log2);
-        int c = 0, parts = 0, pairs = 0, teams = 0;  // tiles with keys; parts; barriers passed
+        int c = 0, mine = 0, parts = 0, teams = 0, boths = 0;  // tiles with keys, and the team's; parts; barriers passed
         const auto sync = [&](const uint64_t &b, int &passed) {  // (bounded like the other waits)
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(b));
             return wait(b, passed++ & 1);
         };
-        const auto wait_pv = [&](int tile) { return wait(sm.pv_done[tile & 1], tile >> 1 & 1); };
-        int kind = 0, member = 0, tiles = 0;  // tiles of the part
+        int kind = 0, member = 0, tiles = 0, own = 0;  // tiles of the part; the team's
         bool live = false;
-        float m = -INFINITY;                  // the row's base with the team's last tile
-        uint64_t sum[2] = {0, 0};             // of the weights of the team's tiles, by that base
+        float m = -INFINITY;
+        uint64_t sum[2] = {0, 0};
 #pragma unroll 1
         for (int t = 0;; ++t) {
             const Meta &meta = sm.meta[t % kMetas];
@@ -1083,94 +1046,18 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
             if (flags & kFirst) {
                 if (!wait(sm.q_full[qb], parts / 2 & 1)) break;
                 kind = sm.rows[qb].kind[r];
-                live = quarter * 32 < part.n_rows;
+                live = (warp & 3) * 32 < part.n_rows;
                 member = member_of<kTcRows>(p, part, r);
-                tiles = 0;
+                tiles = own = 0;
                 m = -INFINITY;
                 sum[0] = sum[1] = 0;
             }
             if (n > 0 && (c & 1) == team) {
                 // (S is there, so the P V of the team's tile before, whose place it has, is done)
-                if (!wait(sm.s_full[team], c >> 1 & 1)) break;
+                if (!wait(sm.s_full[team], mine & 1)) break;
                 tc_fence_after();
-                // the keys that the row attends
-                uint4 on = make_uint4(0, 0, 0, 0);
-                if (kind < 0) {
-                } else if (!(flags & (kRanged | kBits)) && n == kTcKeys) {
-                    on = make_uint4(~0u, ~0u, ~0u, ~0u);
-                } else if (flags & kBits) {
-                    on = *reinterpret_cast<const uint4 *>(meta.bits[kind]);
-                } else {
-                    const int lo = flags & kRanged ? meta.lo[member] : 0, hi = flags & kRanged ? meta.hi[member] : n;
-                    on = make_uint4(bits_below(hi) & ~bits_below(lo), bits_below(hi - 32) & ~bits_below(lo - 32), bits_below(hi - 64) & ~bits_below(lo - 64),
-                                    bits_below(hi - 96) & ~bits_below(lo - 96));
-                }
-                const auto next32 = [&] { on = make_uint4(on.y, on.z, on.w, on.x); };
-                // The base of a row is 0 where the first scores that it has are small, so that both teams find the same one, and moves when a score exceeds it
-                // by kRescale: O, the sum and the weights of the tile's keys in front follow (rarely).  A team goes by the base of its own last tile; behind its
-                // weights it hears of the other's, goes over to the higher one of both and tells.
-                float base = m, before = -INFINITY;
-                const auto scale_tile = [&](int to, float keep) {  // the weights of the keys in front of `to`
-#pragma unroll 1
-                    for (int c0 = 0; c0 < to; c0 += 32) scale_p(tS + c0, tS + kTmemThird + c0 / 2, keep);
-                };
-                const auto scale_sum = [&](float keep) {
-                    const uint64_t keep2 = pack_f32x2(keep, keep);
-                    sum[0] = mul_f32x2(sum[0], keep2), sum[1] = mul_f32x2(sum[1], keep2);
-                };
-                if (live) {
-                    if (tiles == 0) {
-                        uint32_t zero[16] = {};
-#pragma unroll 1
-                        for (int i = 0; i < DP; i += 16) tmem_st16(tO + i, zero);
-                    }
-#pragma unroll 1
-                    for (int c0 = 0; c0 < kTcKeys; c0 += 32, next32()) {
-                        if (c0 >= n) continue;
-                        if (!__any_sync(~0u, on.x)) {
-                            no_weights(tS + c0, tS + kTmemThird + c0 / 2);
-                            continue;
-                        }
-                        uint32_t v[32], third[16];
-                        scores(tS + c0, on.x, v);
-                        const float top = top_score(v) * p.scale_log2;
-                        const bool moves = top > base + kRescale;
-                        if (__any_sync(~0u, moves)) {
-                            const bool first = base == -INFINITY;  // (nothing has to follow the first score)
-                            const float to = first && fabsf(top) <= kRescale ? 0.f : top, keep = moves && !first ? ex2(base - to) : 1.f;
-                            if (__any_sync(~0u, keep != 1.f)) {
-                                scale_sum(keep);
-                                scale_tile(c0, keep);
-                            }
-                            if (moves) base = to;
-                        }
-                        const float neg = base == -INFINITY ? 0.f : -base;
-                        weigh(v, third, scale2, pack_f32x2(neg, neg), sum);
-                        tmem_st32(tS + c0, v);
-                        tmem_st16(tS + kTmemThird + c0 / 2, third);
-                    }
-                }
-                if (tiles > 0) {
-                    if (!wait(sm.based[team ^ 1][quarter], (c - 1) >> 1 & 1)) break;
-                    before = sm.stats[team ^ 1][r].x;
-                }
-                m = fmaxf(base, before);
-                sm.stats[team][r].x = m;  // (the other team has read what stood there ahead of what it has just told)
-                __syncwarp();
-                if (lane == 0) mbar_arrive(bar(sm.based[team][quarter]));
-                if (live) {
-                    const float mine = base == -INFINITY ? 1.f : ex2(base - m), keep = before == -INFINITY ? 1.f : ex2(before - m);
-                    if (__any_sync(~0u, mine != 1.f)) {
-                        scale_sum(mine);
-                        scale_tile(n, mine);
-                    }
-                    if (__any_sync(~0u, keep != 1.f)) {  // O is at rest when the tile before has gone into it
-                        if (!wait_pv(c - 1)) break;
-                        scale_o(tO, DP, keep);
-                    }
-                    tc_wait_st();
-                }
                 const int stage = c % kStages;
+                bool odd = false;
                 if (flags & (kRanged | kBits)) {  // a weight 0 does not undo a value that is not a number: is there one?
                     if (!wait(sm.v_full[stage], c / kStages & 1)) break;
                     const __nv_bfloat162 zero = __floats2bfloat162_rn(0.f, 0.f);
@@ -1187,91 +1074,152 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
                     z = __hadd2(z, z2);
                     if (__any_sync(~0u, !(__low2float(z) == 0.f && __high2float(z) == 0.f)) && lane == 0) *(volatile int *)&sm.odd[team] = c + 1;
                     if (!sync(sm.team[team], teams)) break;
-                    if (*(volatile int *)&sm.odd[team] == c + 1) {
-                        // Values that are not numbers: added here to the rows that attend them, and taken out of the tile.
-                        const auto at = [&](int key, int e) {
-                            return reinterpret_cast<__nv_bfloat16 *>(sm.v[stage] + e / 64 * S::kHalf + key * 128 + ((e / 8 & 7) ^ (key & 7)) * 16 + e % 8 * 2);
-                        };
-                        if (tiles > 0 && !wait_pv(c - 1)) break;
-                        tc_fence_after();
+                    odd = *(volatile int *)&sm.odd[team] == c + 1;
+                }
+                // the keys that the row attends
+                uint4 on = make_uint4(0, 0, 0, 0);
+                if (kind < 0) {
+                } else if (flags & kBits) {
+                    on = *reinterpret_cast<const uint4 *>(meta.bits[kind]);
+                } else {
+                    const int lo = flags & kRanged ? meta.lo[member] : 0, hi = flags & kRanged ? meta.hi[member] : n;
+                    on = make_uint4(bits_below(hi) & ~bits_below(lo), bits_below(hi - 32) & ~bits_below(lo - 32), bits_below(hi - 64) & ~bits_below(lo - 64),
+                                    bits_below(hi - 96) & ~bits_below(lo - 96));
+                }
+                if (live) {
+                    if (own == 0) {
+                        uint32_t zero[16] = {};
 #pragma unroll 1
-                        for (int key = 0; key < n && live; ++key) {
-                            if (key % 32 == 0 && key > 0) next32();
-                            const bool counts = on.x >> (key & 31) & 1;
-#pragma unroll 1
-                            for (int e = 0; e < DP; ++e) {
-                                const float y = __bfloat162float(*at(key, e));
-                                if (fabsf(y) < INFINITY) continue;
-                                const uint32_t col = tS + key / 16 * 16 + key % 16 / 2, half = key & 1 ? 0xffff0000u : 0xffffu, up = key & 1 ? 0 : 16;
-                                float w = 0.f;
-                                for (uint32_t x : {tmem_ld1(col), tmem_ld1(col + 8), tmem_ld1(tS + kTmemThird + key / 2)}) w += __uint_as_float((x & half) << up);
-                                const float o = __uint_as_float(tmem_ld1(tO + e));
-                                tmem_st1(tO + e, __float_as_uint(counts ? fmaf(w, y, o) : o));
-                                tc_wait_st();
-                            }
-                        }
-                        if (!sync(sm.team[team], teams)) break;
-#pragma unroll 1
-                        for (int i = r; i < n * DP; i += 128) {
-                            __nv_bfloat16 *y = at(i / DP, i % DP);
-                            if (!(fabsf(__bfloat162float(*y)) < INFINITY)) *y = __float2bfloat16_rn(0.f);
-                        }
-                        fence_proxy_async();
+                        for (int i = 0; i < DP; i += 16) tmem_st16(tO + i, zero);
                     }
+#pragma unroll 1
+                    for (int c0 = 0; c0 < n; c0 += 32) {
+                        uint32_t v[32] = {};
+                        if (__any_sync(~0u, on.x)) {
+                            tmem_ld32(tS + c0, v);
+                            tc_wait_ld();
+                            reg_fence(v);
+                            if (!__all_sync(~0u, on.x == ~0u)) {
+#pragma unroll
+                                for (int e = 0; e < 32; ++e)
+                                    if (!(on.x >> e & 1)) v[e] = 0xff800000u;
+                            }
+                            // The base of a row moves when a score exceeds it by kRescale, and with the row's first score: O, the sum and the
+                            // weights of the tile's keys in front of these follow.
+                            const float top = top_score(v) * p.scale_log2;
+                            const bool moves = top > m + kRescale;
+                            const bool first_score = m == -INFINITY;  // (there is nothing yet that would have to follow)
+                            const float keep = moves && !first_score ? ex2(m - top) : 1.f;
+                            if (moves) m = top;
+                            if (__any_sync(~0u, moves && !first_score)) {
+                                const uint64_t keep2 = pack_f32x2(keep, keep);
+                                sum[0] = mul_f32x2(sum[0], keep2), sum[1] = mul_f32x2(sum[1], keep2);
+                                if (own > 0) scale_o(tO, DP, keep);
+                                if (c0 > 0) scale_p(tS, c0, keep);
+                            }
+                            const float neg = m == -INFINITY ? 0.f : -m;
+                            weigh(v, scale2, pack_f32x2(neg, neg), sum);
+                        }
+                        tmem_st32(tS + c0, v);
+                        on = make_uint4(on.y, on.z, on.w, on.x);
+                    }
+                    tc_wait_st();
+                }
+                if (odd) {
+                    for (int i = (n + 31) / 32; i < 4; ++i) on = make_uint4(on.y, on.z, on.w, on.x);  // (back to the first)
+                    // Values that are not numbers: added here to the rows that attend them, and taken out of the tile.
+                    const auto at = [&](int key, int e) {
+                        return reinterpret_cast<__nv_bfloat16 *>(sm.v[stage] + e / 64 * S::kHalf + key * 128 + ((e / 8 & 7) ^ (key & 7)) * 16 + e % 8 * 2);
+                    };
+#pragma unroll 1
+                    for (int key = 0; key < n && live; ++key) {
+                        if (key % 32 == 0 && key > 0) on = make_uint4(on.y, on.z, on.w, on.x);
+                        const bool counts = on.x >> (key & 31) & 1;
+#pragma unroll 1
+                        for (int e = 0; e < DP; ++e) {
+                            const float y = __bfloat162float(*at(key, e));
+                            if (fabsf(y) < INFINITY) continue;
+                            const uint32_t col = tS + key / 16 * 16 + key % 16 / 2, hi = tmem_ld1(col), lo = tmem_ld1(col + 8);
+                            const uint32_t cut = key & 1 ? 0xffff0000u : 0xffffu, up = key & 1 ? 0 : 16;
+                            const float w = __uint_as_float((hi & cut) << up) + __uint_as_float((lo & cut) << up);
+                            const float o = __uint_as_float(tmem_ld1(tO + e));
+                            tmem_st1(tO + e, __float_as_uint(counts ? fmaf(w, y, o) : o));
+                            tc_wait_st();
+                        }
+                    }
+                    if (!sync(sm.team[team], teams)) break;
+#pragma unroll 1
+                    for (int i = r; i < n * DP; i += 128) {
+                        __nv_bfloat16 *y = at(i / DP, i % DP);
+                        if (!(fabsf(__bfloat162float(*y)) < INFINITY)) *y = __float2bfloat16_rn(0.f);
+                    }
+                    fence_proxy_async();
                 }
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar(sm.p_full[team]));
+                ++mine, ++own;
             }
             tiles += n > 0, c += n > 0;
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(sm.meta_empty[t % kMetas]));
             if (!(flags & kLast)) continue;
 
-            // The part is done: the teams put their sums together, and each has half of O's columns.
-            float a, b;
-            unpack_f32x2(add_f32x2(sum[0], sum[1]), a, b);
-            // (Who had the last tile waits for it and the other one for them: to them alone the phase in front is known to be over.)
-            if (tiles > 0 && (c - 1 & 1) == team && !wait_pv(c - 1)) break;
-            sm.stats[team][r] = make_float2(m, a + b);
-            tc_fence_before();
-            if (!sync(sm.pair[quarter], pairs)) break;
-            const float2 x = sm.stats[0][r], y = sm.stats[1][r];
-            m = fmaxf(x.x, y.x);  // O's base: that of the last tile
-            const float base = m == -INFINITY ? 0.f : m, l = fmaf(x.y, ex2(x.x - base), y.y * ex2(y.x - base));
-            tc_fence_after();
-            if (live) {
-                const bool row = r < part.n_rows, all = part.state == kAll;
-                const int slot = parts == 0 ? 0 : 1, whole = part.seg * p.B * p.heads + row_of<kTcRows>(p, part, r, member);
-                float *to = all ? p.whole + (size_t)whole * p.d : p.parts + (size_t)(2 * blockIdx.x + slot) * part_floats(kTcRows, p.d) + 4 * r;
-                float2 *stat = all ? p.whole_stats + whole
-                                   : reinterpret_cast<float2 *>(p.parts + (size_t)(2 * blockIdx.x + slot) * part_floats(kTcRows, p.d) + p.d * kTcRows) + r;
-                const int step = all ? 4 : 4 * kTcRows, col0 = team * (DP / 2), col1 = min(p.d, col0 + DP / 2);
-                to += col0 / 4 * step;
-#pragma unroll 1
-                for (int col = col0; col < col1; col += 16) {
-                    uint32_t o[16];
-                    tmem_ld16(tO + col, o);
-                    tc_wait_ld();
-                    reg_fence(o);
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) o[e] = l == 0.f ? 0u : o[e];
-                    if (row) {
-                        *reinterpret_cast<uint4 *>(to) = make_uint4(o[0], o[1], o[2], o[3]);
-                        *reinterpret_cast<uint4 *>(to + step) = make_uint4(o[4], o[5], o[6], o[7]);
-                        if (col + 8 < p.d) {
-                            *reinterpret_cast<uint4 *>(to + 2 * step) = make_uint4(o[8], o[9], o[10], o[11]);
-                            *reinterpret_cast<uint4 *>(to + 3 * step) = make_uint4(o[12], o[13], o[14], o[15]);
-                        }
-                        to += 4 * step;
-                    }
+            // The part is done: by both teams, half of the columns each, if it had more than one tile, else by the one that had it (the first
+            // team, if it had none).
+            const bool joined = tiles > 1;
+            if (joined || own > 0 || (tiles == 0 && team == 0)) {
+                float a, b;
+                unpack_f32x2(add_f32x2(sum[0], sum[1]), a, b);
+                float l = a + b, f[2] = {1.f, 1.f};
+                if (own > 0 && !wait(sm.pv_done[team], (mine - 1) & 1)) break;
+                if (joined) {
+                    sm.stats[team][r] = make_float2(m, l);
+                    if (!sync(sm.both, boths)) break;
+                    const float2 x = sm.stats[0][r], y = sm.stats[1][r];
+                    m = fmaxf(x.x, y.x);
+                    const float base = m == -INFINITY ? 0.f : m;
+                    f[0] = ex2(x.x - base), f[1] = ex2(y.x - base);
+                    l = fmaf(x.y, f[0], y.y * f[1]);
                 }
-                if (row && team == 0) *stat = make_float2(m, l);
-                if (tid == 0) put_joint(p, part, slot, start.total);
+                tc_fence_after();
+                if (live) {
+                    const bool row = r < part.n_rows, all = part.state == kAll;
+                    const int slot = parts == 0 ? 0 : 1, whole = part.seg * p.B * p.heads + row_of<kTcRows>(p, part, r, member);
+                    float *to = all ? p.whole + (size_t)whole * p.d : p.parts + (size_t)(2 * blockIdx.x + slot) * part_floats(kTcRows, p.d) + 4 * r;
+                    float2 *stat = all ? p.whole_stats + whole
+                                       : reinterpret_cast<float2 *>(p.parts + (size_t)(2 * blockIdx.x + slot) * part_floats(kTcRows, p.d) + p.d * kTcRows) + r;
+                    const int step = all ? 4 : 4 * kTcRows, col0 = joined && team ? DP / 2 : 0, col1 = min(p.d, joined ? col0 + DP / 2 : DP);
+                    const uint32_t first_o = tmem + lanes + kTmemO + (joined ? 0 : team * 128);
+                    to += col0 / 4 * step;
+#pragma unroll 1
+                    for (int col = col0; col < col1; col += 16) {
+                        uint32_t o[16], o2[16] = {};
+                        tmem_ld16(first_o + col, o);
+                        if (joined) tmem_ld16(first_o + 128 + col, o2);
+                        tc_wait_ld();
+                        reg_fence(o);
+                        reg_fence(o2);
+#pragma unroll
+                        for (int e = 0; e < 16; ++e)
+                            o[e] = l == 0.f ? 0u : __float_as_uint(fmaf(__uint_as_float(o2[e]), f[1], __uint_as_float(o[e]) * f[0]));
+                        if (row) {
+                            *reinterpret_cast<uint4 *>(to) = make_uint4(o[0], o[1], o[2], o[3]);
+                            *reinterpret_cast<uint4 *>(to + step) = make_uint4(o[4], o[5], o[6], o[7]);
+                            if (col + 8 < p.d) {
+                                *reinterpret_cast<uint4 *>(to + 2 * step) = make_uint4(o[8], o[9], o[10], o[11]);
+                                *reinterpret_cast<uint4 *>(to + 3 * step) = make_uint4(o[12], o[13], o[14], o[15]);
+                            }
+                            to += 4 * step;
+                        }
+                    }
+                    if (row && (!joined || team == 0)) *stat = make_float2(m, l);
+                    if (r == 0 && (!joined || team == 0)) put_joint(p, part, slot, start.total);
+                }
+                tc_fence_before();
+                if (joined && !sync(sm.both, boths)) break;  // O has been read
             }
-            tc_fence_before();
-            if (!sync(sm.pair[quarter], pairs)) break;  // O and the sums have been read
-            tc_fence_after();
+            __syncwarp();
             if (lane == 0) mbar_arrive(bar(sm.q_empty[qb]));
             ++parts;
         }
@@ -1466,13 +1414,13 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
         for (int stage = 0; stage < min(c, kStages); ++stage)
             mbar_wait_bounded(bar(v ? sm.v_full[stage] : sm.k_full[stage]), (c - 1 - stage) / kStages & 1, kWaitLimit);
     } else {
-        // ------------------------------------------------------------------ the products, a warp to each
-        // S = Q K^T of a tile as soon as its keys are there and the P V of the last tile but one, whose weights have the place of S, is done; O += P V as
+        // ------------------------------------------------------------------ the products, a warp to each team
+        // S = Q K^T of a tile as soon as its keys are there and the team's last P V, whose weights have the place of S, is done; O += P V as
         // soon as P is there.
         const bool leader = elect_one();
-        const bool scores = warp == kMmaWarp;
-        const uint32_t tO = tmem + kTmemO, idesc_pv = idesc_bf16(kTcRows, DP, 0, 1);
-        int c = 0, parts = 0;
+        const int team = warp - kMmaWarp;
+        const uint32_t tS = tmem + kTmemS + team * kTcKeys, tO = tmem + kTmemO + team * 128, idesc_pv = idesc_bf16(kTcRows, DP, 0, 1);
+        int c = 0, mine = 0, parts = 0;
 #pragma unroll 1
         for (int t = 0;; ++t) {
             const Meta &meta = sm.meta[t % kMetas];
@@ -1481,12 +1429,11 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
             if (n < 0) break;
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(sm.meta_empty[t % kMetas]));
-            const int stage = c % kStages, phase = c / kStages & 1, steps = (n + 15) / 16;
-            const uint32_t tS = tmem + kTmemS + (c & 1) * kTmemTile;
-            if (n > 0 && scores) {
+            if (n > 0 && (c & 1) == team) {
+                const int stage = c % kStages, phase = c / kStages & 1, steps = (n + 15) / 16;
                 const uint32_t idesc = idesc_bf16(kTcRows, steps * 16, 0, 0);
                 if (!wait(sm.q_full[parts & 1], parts / 2 & 1) || !wait(sm.k_full[stage], phase)) break;
-                if (c >= 2 && !wait(sm.pv_done[c & 1], (c >> 1) - 1 & 1)) break;
+                if (mine > 0 && !wait(sm.pv_done[team], (mine - 1) & 1)) break;
                 fence_proxy_async();  // the copies of 16 bytes come through the generic proxy
                 tc_fence_after();
                 const uint32_t q = smem_desc_lo(smem_u32(sm.q[parts & 1])), k = smem_desc_lo(smem_u32(sm.k[stage]));
@@ -1497,11 +1444,12 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
                         const uint32_t off = i / 4 * (S::kHalf >> 4) + i % 4 * 2;
                         mma_ss_lean<1>(tS, q + off, k + off, idesc);
                     }
-                    mma_commit(bar(sm.s_full[c & 1]));
+                    mma_commit(bar(sm.s_full[team]));
                     mma_commit(bar(sm.k_empty[stage]));
+                    if (last) mma_commit(bar(sm.q_empty[parts & 1]));
                 }
-            } else if (n > 0) {
-                if (!wait(sm.v_full[stage], phase) || !wait(sm.p_full[c & 1], c >> 1 & 1)) break;
+                __syncwarp();
+                if (!wait(sm.v_full[stage], phase) || !wait(sm.p_full[team], mine & 1)) break;
                 tc_fence_after();
                 fence_proxy_async();
                 // (64 columns of V lie kHalf behind the others: the leading byte offset)
@@ -1510,7 +1458,6 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
                     const auto step = [&](int ks) {
                         mma_ts_lean<1>(tO, tS + 16 * ks, v + ks * (16 * 128 >> 4), idesc_pv);
                         mma_ts_lean<1>(tO, tS + 16 * ks + 8, v + ks * (16 * 128 >> 4), idesc_pv);
-                        mma_ts_lean<1>(tO, tS + kTmemThird + 8 * ks, v + ks * (16 * 128 >> 4), idesc_pv);
                     };
                     if (steps == kTcKeys / 16) {
 #pragma unroll
@@ -1519,13 +1466,15 @@ __global__ void __launch_bounds__(kTcThreads, 1) shared_tc_kernel(const __grid_c
 #pragma unroll 1
                         for (int ks = 0; ks < steps; ++ks) step(ks);
                     }
-                    mma_commit(bar(sm.pv_done[c & 1]));
+                    mma_commit(bar(sm.pv_done[team]));
                     mma_commit(bar(sm.v_empty[stage]));
                 }
+                __syncwarp();
+                ++mine;
+            } else if (last) {
+                if (leader) mma_commit(bar(sm.q_empty[parts & 1]));
+                __syncwarp();
             }
-            __syncwarp();
-            if (last && scores && leader) mma_commit(bar(sm.q_empty[parts & 1]));
-            __syncwarp();
             c += n > 0, parts += last != 0;
         }
         if (leader) mma_commit(bar(sm.final_));  // nothing of this block may still run on the tensor pipe when its memory is freed
@@ -1752,9 +1701,9 @@ int mate_attn_decode_shared(const mate_cache_t *cache, int layer, const void *Q,
     p.Q = Q, p.q_batch = q_stride[0], p.q_head = q_stride[1];
     p.B = B, p.heads = cache->heads, p.kv_heads = cache->kv_heads, p.group = cache->heads / cache->kv_heads;
     p.d = cache->d, p.max_len = max_len, p.pack = pack_of(cache), p.own_tiles = own_tiles(cache);
-    // (whose copies are shorter: cells 45.7 us, without it 46.2, beams 32.0 and 32.2; with two parts a weight 64 questions with 128 tokens of their own 39.1 and
-    // 41.1, 256 sequences 101 and 102.5, and an eighth or three instead of a quarter 0.9 us more for the questions)
-    p.own_quarter = cache->dtype == MATE_BF16;
+    // (whose copies are shorter: 64 questions with 128 tokens of their own, heads of 128 elements, 39.1 us, without it 41.1, 256 sequences 101 and 102.5;
+    // heads of 64: beams 30.2 with it and 30.1 without, cells 42.3 and 42.9; when it was chosen an eighth gave 38.8 and three 38.9 where a quarter gave 37.9)
+    p.own_quarter = cache->dtype == MATE_BF16 && cache->d > 64;
     p.seqs = seqs, p.row_ids = row_ids, p.col_ids = col_ids, p.groups = groups;
     p.scale_log2 = scale * kLog2e, p.O = O, p.LSE = LSE;
     for (int h = 0; h < cache->heads; ++h) p.views[h >> 4] |= (uint32_t)cache->head_view[h] << 2 * (h & 15);
