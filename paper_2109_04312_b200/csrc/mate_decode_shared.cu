@@ -19,8 +19,16 @@
 // Roles of a bf16 block.  Four warps look for keys (Scout) and fill tiles of 128 of them; two copy keys and values (sixteen slots that follow one
 // another by a bulk tensor copy, the rest in 16 bytes a lane) and the queries; two teams of four warps, a thread to a row, take the tiles in turn and make
 // weights of the scores; a warp for each team issues its products.  Tensor memory: O of both teams 2 x 128 columns, S 2 x 128; the weights take
-// the place of the scores, 16 keys as 8 columns of bf16 pairs and 8 of what the rounding left.  (Weights as one bf16 would be off by 2^-9, more than the
+// the place of the scores, 16 keys as 8 columns of bf16 pairs and 8 of what the rounding left.  (Weights as one bf16 would be off by 2^-8, as much as the
 // result's rounding.)  fp32: shared_simt_kernel, 64 rows against 32 keys, no tensor cores.
+//
+// What is lost beside the rounding of the result to bf16 (half a step, 2e-3 to 4e-3 of it): a weight by its 16 bits 2^-16 at most, and the sums in tensor memory,
+// which are cut off behind fp32's 24 bits, always towards 0, with every product: of 16 products a tile 64 questions and 256 sequences lose 1e-5 of a
+// result, so that one in some 300 rounds to the other bf16; 65536 tokens of one block lose 5e-5 (values of mean 1: 1e-4; mate_attn_decode, whose
+// warps have less of a sequence each, 2e-5 and 4e-5), one result in 40.  A third part for every weight, all of the 24 bits, has no room beside an O for each team with more
+// than 64 elements.  With one O for both teams it has, but then three times as many products go into a sum: 65536 tokens lose 1.2e-4, one result in 18, and
+// 256 sequences take 102 us.  Putting O by, sixteen columns a tile, ends the loss (one result in 400, however many tokens) and takes 113 to 121 us.  With
+// 64 elements a third part takes beams from 30.1 to 32.6 us and cells from 43.0 to 44.9, and as many results round to the other bf16.
 //
 // What bounds it.  The chain of a team's tile, 7.2 thousand cycles of which the other team's overlap half: S 0.5, weights 4 (four chunks of 32 keys, one
 // after the other in a warp), P V 1.3, whose weights lie where the next S goes, barriers and the other team's tile 1.4; the products alone would
@@ -898,8 +906,8 @@ __device__ __forceinline__ float top_score(const uint32_t (&v)[32]) {
         for (int j = 0; j < 4; ++j) t[j] = ptx::fmax3(t[j], __uint_as_float(v[e + 2 * j]), __uint_as_float(v[e + 2 * j + 1]));
     return fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
 }
-// Weights 2^(s scale - base), 16 keys at a time, as pairs of bf16: rounded, and what the rounding left, rounded (their sum has 16 bits: an
-// error of 2^-17 of a weight, which the result's rounding to bf16, 2^-9, hides but for one value in some hundred).  The sums take all of them.
+// Weights 2^(s scale - base), 16 keys at a time, as pairs of bf16: rounded, and what the rounding left, half a step of 2^-8, rounded by half a step of that.
+// Their sum has 16 bits: a weight is off by 2^-16 at most, the difference of two weights that are 2^-12 apart by 3 %.  The sums take all of them.
 __device__ __forceinline__ void weigh(uint32_t (&v)[32], uint64_t scale2, uint64_t neg_base2, uint64_t (&sum)[2]) {
 #pragma unroll
     for (int i = 0; i < 32; i += 16) {
