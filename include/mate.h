@@ -451,12 +451,15 @@ int mate_attn_decode(const mate_cache_t *cache, int layer, const void *Q, const 
  *   flags      0: where the batch may read no more than 192 MB (bf16) or 1 GB (fp32) one sequence after another -- B max_len kv_heads
  *              keys and values --, that way is taken: the results are mate_attn_decode's; MATE_SHARED_ALWAYS: the shared
  *              tokens are read once all the same
- * Reading them once pays for many sequences in one group or a few.  Beyond those sizes mate_attn_decode is the faster call for batches without groups (bf16 1.6
- * to 2.5 times), with fp32 for all but groups of some dozens, and where the new tokens are those of cells that attend little of a long table.
- * The batch's work is counted in 32 bits: B kv_heads ceil(heads / kv_heads / (bf16 ? 128 : 64)) (8 + max_len / 32) is below 2^30.
+ * Reading them once pays for many sequences in one group or a few.  Beyond those sizes mate_attn_decode is the faster call for batches
+ * without groups (bf16 1.6 to 2.5 times, fp32 9 times), with fp32 for groups of fewer than sixteen or so, and where the new tokens are those of
+ * cells that attend little of a long table.
+ * The batch's work is counted in 32 bits: MATE_ERR_UNSUPPORTED where B kv_heads ceil(heads / kv_heads / (bf16 ? 128 : 64)) (8 + max_len / 32)
+ * is 2^30 or more.
  * Where they are read once and the type is bf16, weights enter the product with the values as the sum of two bf16, with 16 bits
- * (mate_attn_decode: with all of their 24).  Sums of either call are in fp32 by the tensor cores, which cut off, towards 0, what is behind the 24 bits: the more
- * tokens, the more (65536 tokens that one block sums up: 1e-4 of a result, a twentieth of half a step of bf16).  All other arguments, limits and errors as for mate_attn_decode. */
+ * (mate_attn_decode: with all of their 24).  Sums of either call are in fp32 by the tensor cores, which cut off, towards 0, what is behind the
+ * 24 bits: the more tokens, the more (65536 tokens that one block sums up: 1e-4 of a result, a twentieth of half a step of bf16).  All other
+ * arguments, limits and errors as for mate_attn_decode. */
 int mate_attn_decode_shared(const mate_cache_t *cache, int layer, const void *Q, const int64_t *q_stride, int B, const int32_t *seqs,
                             const int32_t *row_ids, const int32_t *col_ids, const int32_t *groups, float scale, int max_len, unsigned flags,
                             void *O, float *LSE, void *workspace, size_t workspace_bytes, void *stream);

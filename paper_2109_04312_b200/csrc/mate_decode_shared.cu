@@ -22,13 +22,14 @@
 // the place of the scores, 16 keys as 8 columns of bf16 pairs and 8 of what the rounding left.  (Weights as one bf16 would be off by 2^-8, as much as the
 // result's rounding.)  fp32: shared_simt_kernel, 64 rows against 32 keys, no tensor cores.
 //
-// What is lost beside the rounding of the result to bf16 (half a step, 2e-3 to 4e-3 of it): a weight by its 16 bits 2^-16 at most, and the sums in tensor memory,
-// which are cut off behind fp32's 24 bits, always towards 0, with every product: of 16 products a tile 64 questions and 256 sequences lose 1e-5 of a
-// result, so that one in some 300 rounds to the other bf16; 65536 tokens of one block lose 5e-5 (values of mean 1: 1e-4; mate_attn_decode, whose
-// warps have less of a sequence each, 2e-5 and 4e-5), one result in 40.  A third part for every weight, all of the 24 bits, has no room beside an O for each team with more
-// than 64 elements.  With one O for both teams it has, but then three times as many products go into a sum: 65536 tokens lose 1.2e-4, one result in 18, and
-// 256 sequences take 102 us.  Putting O by, sixteen columns a tile, ends the loss (one result in 400, however many tokens) and takes 113 to 121 us.  With
-// 64 elements a third part takes beams from 30.1 to 32.6 us and cells from 43.0 to 44.9, and as many results round to the other bf16.
+// What is lost beside the rounding of the result to bf16 (half a step, 2e-3 to 4e-3 of it): a weight by its 16 bits 2^-16 at most, and the sums in
+// tensor memory, which are cut off behind fp32's 24 bits, always towards 0, with every product: of 16 products a tile 64 questions and 256 sequences lose
+// 1e-5 of a result, so that one in some 300 rounds to the other bf16; 65536 tokens of one block lose 5e-5 (values of mean 1: 1e-4;
+// mate_attn_decode, whose warps have less of a sequence each, 2e-5 and 4e-5), one result in 40.  A third part for every weight, all of the 24 bits, has no
+// room beside an O for each team with more than 64 elements.  With one O for both teams it has, but then three times as many products go into a
+// sum: 65536 tokens lose 1.2e-4, one result in 18, and 256 sequences take 102 us.  Putting O by, sixteen columns a tile, ends the loss (one
+// result in 400, however many tokens) and takes 113 to 121 us.  With 64 elements a third part takes beams from 30.1 to 32.6 us and cells from 43.0
+// to 44.9, and no fewer results round to the other bf16.
 //
 // What bounds it.  The chain of a team's tile, 7.2 thousand cycles of which the other team's overlap half: S 0.5, weights 4 (four chunks of 32 keys, one
 // after the other in a warp), P V 1.3, whose weights lie where the next S goes, barriers and the other team's tile 1.4; the products alone would
